@@ -44,7 +44,8 @@ typedef enum {
     ATB_ERR_UNSUPPORTED_DEVICE = 5, /* current device is not compute capability 10.0            */
     ATB_ERR_CUDA = 6,               /* a CUDA runtime / driver call failed (see the message)    */
     ATB_ERR_BUFFER_TOO_SMALL = 7,   /* an output array given by the caller is too short         */
-    ATB_ERR_DEVICE_TIMEOUT = 8      /* a kernel gave up a bounded wait (reported by atb_device_status) */
+    ATB_ERR_DEVICE_TIMEOUT = 8,     /* a kernel gave up a bounded wait (reported by atb_device_status) */
+    ATB_ERR_BAD_ARGUMENT = 9        /* an enum or scalar argument has no such value              */
 } atb_status_t;
 
 /* Name of a status code; never NULL. */
@@ -340,6 +341,93 @@ atb_status_t atb_score_tiling(const atb_hw_params_t* hw, int64_t K, atb_tiling_t
  * Returns ATB_ERR_BAD_SHAPE if no supported tiling is feasible. */
 atb_status_t atb_select_tiling(int64_t M, int64_t N, int64_t K, const atb_hw_params_t* hw,
                                atb_tiling_t* best, atb_tiling_score_t* scores, int* n_scores);
+
+/* =====================================================================================================
+ * What stands between the products of a network: layer norm, the gated feed-forward block, and the softmax
+ * cross entropy of a linear head, each forward and backward.  The general rules above hold for them too; in
+ * addition
+ *   - matrices are row-major, ld* is the number of elements between rows; bf16 operands of products are
+ *     16-byte aligned with leading dimensions that are multiples of 8;
+ *   - an output must not overlap an input, another output or the workspace;
+ *   - sums, norms' statistics, softmax statistics and losses are FP32; every call with the same arguments
+ *     on the same GPU model gives the same bits (no atomics);
+ *   - a workspace is device memory, 16-byte aligned, of at least the bytes that the function beside the
+ *     operator returns; it is overwritten and may be reused by the next call on the same stream.
+ * ===================================================================================================== */
+typedef enum { ATB_F32 = 0, ATB_BF16 = 1 } atb_dtype_t;
+
+/* Layer norm of the M rows of X (N columns):
+ *   mean = sum(x) / N, rstd = 1 / sqrt(sum((x - mean)^2) / N + eps), y = (x - mean) * rstd * W + B.
+ *   X_dev, Y_dev: x_type [M][ldx], [M][ldy];  W_dev, B_dev: w_type [N], each may be NULL (1 and 0);
+ *   mean_dev, rstd_dev: FP32 [M], written for the backward pass, each may be NULL.
+ * Any M, N >= 0 (0: nothing is done), any leading dimension >= N, any alignment of whole elements; rows that are
+ * multiples of 8 elements on 16-byte boundaries run on 16-byte accesses.
+ * Errors: BAD_ARGUMENT (types, eps < 0), BAD_SHAPE, NULL_POINTER, MISALIGNED, UNSUPPORTED_DEVICE, CUDA. */
+atb_status_t atb_layer_norm(int64_t M, int64_t N, int x_type, const void* X_dev, int64_t ldx, int w_type,
+                            const void* W_dev, const void* B_dev, float eps, void* Y_dev, int64_t ldy,
+                            float* mean_dev, float* rstd_dev, void* stream);
+/* The same with Y written as the BFP16 planes of an M x N matrix, in the layout and by the rule of
+ * atb_quantize_bfp16 applied to the FP32 results bit for bit: the A operand of a product without a pass of its own.
+ * N % 8 == 0; X, W, B and the rows of X on 16-byte boundaries. */
+atb_status_t atb_layer_norm_bfp16(int64_t M, int64_t N, int x_type, const void* X_dev, int64_t ldx, int w_type,
+                                  const void* W_dev, const void* B_dev, float eps, int8_t* mant_dev, uint8_t* exp_dev,
+                                  float* mean_dev, float* rstd_dev, void* stream);
+/* Gradients of atb_layer_norm from dY and the saved statistics, with z = (x - mean) * rstd and g = dy * W:
+ *   dX = rstd * (g - sum(g) / N - z * sum(g * z) / N),  dW = sum over rows of dy * z,  dB = sum over rows of dy.
+ *   dX_dev: x_type; dW_dev, dB_dev: w_type [N]; each may be NULL (not wanted).  M == 0 writes dW = dB = 0.
+ *   The workspace is needed only for dW and dB. */
+size_t atb_layer_norm_backward_workspace_bytes(int64_t M, int64_t N);
+atb_status_t atb_layer_norm_backward(int64_t M, int64_t N, int x_type, const void* dY_dev, int64_t lddy, const void* X_dev,
+                                     int64_t ldx, int w_type, const void* W_dev, const float* mean_dev, const float* rstd_dev,
+                                     void* dX_dev, int64_t lddx, void* dW_dev, void* dB_dev,
+                                     void* workspace_dev, size_t workspace_bytes, void* stream);
+
+/* act(g): g * sigmoid(g); g * Phi(g) by erf; g * (1 + tanh(sqrt(2/pi) (g + 0.044715 g^3))) / 2 */
+typedef enum { ATB_ACT_SILU = 0, ATB_ACT_GELU = 1, ATB_ACT_GELU_TANH = 2 } atb_act_t;
+
+/* Gated feed-forward block in bf16 with FP32 accumulation: H = act(X Wg) * (X Wu), Y = H Wd.
+ *   X_dev [M][ldx] (D columns), Wg_dev and Wu_dev [D][ldw] (F columns; they may be the two halves of one matrix),
+ *   Wd_dev [F][ldwd] (D columns), Y_dev [M][ldy];
+ *   H_dev bf16 [M][F], written: the rounded product that feeds Wd, which the backward pass needs again;
+ *   G_dev, U_dev bf16 [M][F]: X Wg and X Wu for the backward pass, both or neither.
+ * M >= 0 (0: nothing is done), D and F >= 8 and multiples of 8.
+ * Errors: BAD_ARGUMENT (act), BAD_SHAPE, NULL_POINTER, MISALIGNED, BUFFER_TOO_SMALL, UNSUPPORTED_DEVICE, CUDA. */
+size_t atb_gated_ffn_workspace_bytes(int64_t M, int64_t D, int64_t F);      /* may be 0: no workspace, NULL accepted */
+atb_status_t atb_gated_ffn(int64_t M, int64_t D, int64_t F, int act, const void* X_dev, int64_t ldx, const void* Wg_dev,
+                           const void* Wu_dev, int64_t ldw, const void* Wd_dev, int64_t ldwd, void* Y_dev, int64_t ldy,
+                           void* H_dev, void* G_dev, void* U_dev, void* workspace_dev, size_t workspace_bytes, void* stream);
+/* Gradients of atb_gated_ffn from dY and what the forward call kept:
+ *   dH = dY Wd^T, dU = dH * act(G), dG = dH * U * act'(G) (rounded to bf16 for the products below),
+ *   dX = dG Wg^T + dU Wu^T, dWg = X^T dG, dWu = X^T dU, dWd = H^T dY.
+ *   dX_dev [M][lddx]; dWg_dev, dWu_dev [D][lddw]; dWd_dev [F][lddwd]: bf16, written (not added to); dX, dWd and the
+ *   pair dWg, dWu may be NULL (not wanted).  M == 0 writes zero weight gradients. */
+size_t atb_gated_ffn_backward_workspace_bytes(int64_t M, int64_t D, int64_t F);
+atb_status_t atb_gated_ffn_backward(int64_t M, int64_t D, int64_t F, int act, const void* dY_dev, int64_t lddy, const void* X_dev,
+                                    int64_t ldx, const void* Wg_dev, const void* Wu_dev, int64_t ldw, const void* Wd_dev, int64_t ldwd,
+                                    const void* H_dev, const void* G_dev, const void* U_dev, void* dX_dev, int64_t lddx, void* dWg_dev,
+                                    void* dWu_dev, int64_t lddw, void* dWd_dev, int64_t lddwd, void* workspace_dev,
+                                    size_t workspace_bytes, void* stream);
+
+/* Softmax cross entropy of a linear head, L = X W^T (M x V), without keeping L:
+ *   lse[m] = log sum_v exp(L[m][v]),  loss[m] = lse[m] - L[m][label[m]], 0 where label[m] == ignore_index.
+ *   X_dev bf16 [M][ldx], W_dev bf16 [V][ldw] (D columns each), labels_dev int64 [M], loss_dev and lse_dev FP32 [M].
+ * A label outside [0, V) that is not ignore_index makes loss and lse of its row NaN (and with them every gradient).
+ * M >= 0 (0: nothing is done), V >= 1 (any value), D >= 8 and a multiple of 8.
+ * Errors: BAD_SHAPE, NULL_POINTER, MISALIGNED, BUFFER_TOO_SMALL, UNSUPPORTED_DEVICE, CUDA. */
+size_t atb_linear_cross_entropy_workspace_bytes(int64_t M, int64_t V, int64_t D);
+atb_status_t atb_linear_cross_entropy(int64_t M, int64_t V, int64_t D, const void* X_dev, int64_t ldx, const void* W_dev, int64_t ldw,
+                                      const int64_t* labels_dev, int64_t ignore_index, float* loss_dev, float* lse_dev,
+                                      void* workspace_dev, size_t workspace_bytes, void* stream);
+/* Gradients of sum_m dloss[m] * loss[m]:  dL = (exp(L - lse) - onehot(label)) * dloss (bf16; 0 in ignored rows),
+ *   dX = dL W, dW = dL^T X (bf16, written; each may be NULL).  M == 0 writes dW = 0.
+ *   L is computed again, `piece` words of the vocabulary at a time (rounded up to whole tiles; 0: the library's choice,
+ *   which keeps dL within 512 MB or 2048 words), so that the workspace holds M x piece of dL, and FP32 sums of dX
+ *   where there is more than one piece.  Results of different `piece` agree within the rounding of the FP32 sums. */
+size_t atb_linear_cross_entropy_backward_workspace_bytes(int64_t M, int64_t V, int64_t D, int64_t piece);
+atb_status_t atb_linear_cross_entropy_backward(int64_t M, int64_t V, int64_t D, const void* X_dev, int64_t ldx, const void* W_dev,
+                                               int64_t ldw, const int64_t* labels_dev, int64_t ignore_index, const float* lse_dev,
+                                               const float* dloss_dev, void* dX_dev, int64_t lddx, void* dW_dev, int64_t lddw,
+                                               int64_t piece, void* workspace_dev, size_t workspace_bytes, void* stream);
 
 #ifdef __cplusplus
 }

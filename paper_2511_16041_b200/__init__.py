@@ -22,7 +22,7 @@ ATB_OK = 0
 STATUS_NAMES = {
     0: "ATB_OK", 1: "ATB_ERR_NULL_POINTER", 2: "ATB_ERR_BAD_SHAPE", 3: "ATB_ERR_BAD_TILING",
     4: "ATB_ERR_MISALIGNED", 5: "ATB_ERR_UNSUPPORTED_DEVICE", 6: "ATB_ERR_CUDA",
-    7: "ATB_ERR_BUFFER_TOO_SMALL", 8: "ATB_ERR_DEVICE_TIMEOUT",
+    7: "ATB_ERR_BUFFER_TOO_SMALL", 8: "ATB_ERR_DEVICE_TIMEOUT", 9: "ATB_ERR_BAD_ARGUMENT",
 }
 
 
@@ -75,6 +75,10 @@ EXPORTED_SYMBOLS = [
     "atb_gemm_splitk_noalloc",
     "atb_tiling_supported", "atb_tiling_plan", "atb_device_status",
     "atb_hw_params_b200", "atb_hw_params_xdna2", "atb_score_tiling", "atb_select_tiling",
+    "atb_layer_norm", "atb_layer_norm_bfp16", "atb_layer_norm_backward", "atb_layer_norm_backward_workspace_bytes",
+    "atb_gated_ffn", "atb_gated_ffn_workspace_bytes", "atb_gated_ffn_backward", "atb_gated_ffn_backward_workspace_bytes",
+    "atb_linear_cross_entropy", "atb_linear_cross_entropy_workspace_bytes",
+    "atb_linear_cross_entropy_backward", "atb_linear_cross_entropy_backward_workspace_bytes",
 ]
 
 
@@ -130,6 +134,23 @@ def load_library():
     lib.atb_select_tiling.argtypes = [i64, i64, i64, ctypes.POINTER(atb_hw_params_t),
                                       ctypes.POINTER(atb_tiling_t), ctypes.POINTER(atb_tiling_score_t),
                                       ctypes.POINTER(ci)]
+    cf, sz = ctypes.c_float, ctypes.c_size_t
+    for name, restype, argtypes in (
+            ("atb_layer_norm", ci, [i64, i64, ci, vp, i64, ci, vp, vp, cf, vp, i64, vp, vp, vp]),
+            ("atb_layer_norm_bfp16", ci, [i64, i64, ci, vp, i64, ci, vp, vp, cf, vp, vp, vp, vp, vp]),
+            ("atb_layer_norm_backward_workspace_bytes", sz, [i64, i64]),
+            ("atb_layer_norm_backward", ci, [i64, i64, ci, vp, i64, vp, i64, ci, vp, vp, vp, vp, i64, vp, vp, vp, sz, vp]),
+            ("atb_gated_ffn_workspace_bytes", sz, [i64, i64, i64]),
+            ("atb_gated_ffn", ci, [i64, i64, i64, ci, vp, i64, vp, vp, i64, vp, i64, vp, i64, vp, vp, vp, vp, sz, vp]),
+            ("atb_gated_ffn_backward_workspace_bytes", sz, [i64, i64, i64]),
+            ("atb_gated_ffn_backward", ci, [i64, i64, i64, ci, vp, i64, vp, i64, vp, vp, i64, vp, i64, vp, vp, vp, vp, i64, vp, vp, i64,
+                                            vp, i64, vp, sz, vp]),
+            ("atb_linear_cross_entropy_workspace_bytes", sz, [i64, i64, i64]),
+            ("atb_linear_cross_entropy", ci, [i64, i64, i64, vp, i64, vp, i64, vp, i64, vp, vp, vp, sz, vp]),
+            ("atb_linear_cross_entropy_backward_workspace_bytes", sz, [i64, i64, i64, i64]),
+            ("atb_linear_cross_entropy_backward", ci, [i64, i64, i64, vp, i64, vp, i64, vp, i64, vp, vp, vp, i64, vp, i64, i64, vp, sz, vp])):
+        fn = getattr(lib, name)
+        fn.restype, fn.argtypes = restype, argtypes
     _lib = lib
     return lib
 
@@ -350,6 +371,278 @@ def atb_select_tiling(M: int, N: int, K: int, hw: atb_hw_params_t | None = None,
     _check(load_library().atb_select_tiling(M, N, K, ctypes.byref(hw) if hw is not None else None,
                                             ctypes.byref(best), scores, ctypes.byref(n)))
     return Tiling(best.T_MA, best.T_MC, best.T_K, best.T_N), [scores[i] for i in range(n.value)]
+
+
+# ------------------------------------------------------------------ between the products: norm, feed-forward, loss
+ATB_F32, ATB_BF16 = 0, 1
+ACTIVATIONS = {"silu": 0, "gelu": 1, "gelu_tanh": 2}
+
+
+def _dtype(t):
+    import torch
+    if t.dtype == torch.float32:
+        return ATB_F32
+    if t.dtype == torch.bfloat16:
+        return ATB_BF16
+    raise TypeError(f"{t.dtype}: float32 or bfloat16")
+
+
+def _matrix(t, rows, cols, dtype, name):
+    """Checks a row-major CUDA matrix and returns its leading dimension."""
+    if not t.is_cuda or t.dim() != 2 or t.dtype != dtype or t.shape != (rows, cols) or (cols > 1 and t.stride(1) != 1):
+        raise ValueError(f"{name}: a row-major CUDA matrix {(rows, cols)} of {dtype}, got {tuple(t.shape)} of {t.dtype}")
+    return t.stride(0) if rows > 1 else max(cols, t.stride(0))
+
+
+def _vector(t, n, dtype, name):
+    if t is not None and (not t.is_cuda or t.dim() != 1 or t.dtype != dtype or t.shape[0] != n or (n > 1 and t.stride(0) != 1)):
+        raise ValueError(f"{name}: a contiguous CUDA vector of {n} {dtype}, got {tuple(t.shape)} of {t.dtype}")
+
+
+def _opt_ptr(t):
+    return None if t is None else t.data_ptr()
+
+
+def _workspace(workspace, need, device):
+    """The caller's workspace, or a new one of ``need`` bytes."""
+    import torch
+    if workspace is None:
+        workspace = torch.empty(need, dtype=torch.uint8, device=device)
+    return workspace.data_ptr(), workspace.numel() * workspace.element_size(), workspace
+
+
+def _on_stream(device, stream):
+    """Raises unless the call's device is the current one; returns the raw stream."""
+    import torch
+    if device.index != torch.cuda.current_device():
+        raise ValueError(f"the tensors are on {device}, the current device is cuda:{torch.cuda.current_device()}")
+    return _stream_ptr(stream)
+
+
+def _norm_weights(W, B, N, x_dtype):
+    given = W if W is not None else B
+    w_dtype = given.dtype if given is not None else x_dtype
+    _vector(W, N, w_dtype, "W")
+    _vector(B, N, w_dtype, "B")
+    return ATB_F32 if given is None else _dtype(given), w_dtype
+
+
+def atb_layer_norm(X, W=None, B=None, eps=1e-5, Y=None, mean=None, rstd=None, stream=None):
+    """Layer norm of the rows of ``X`` (float32 or bfloat16 ``[M, N]``); ``W``, ``B``: ``[N]`` of one type, or None.
+
+    Returns ``(Y, mean, rstd)``: the result in X's type and the float32 statistics that the backward pass takes."""
+    import torch
+    if X.dim() != 2:
+        raise ValueError("X: a matrix")
+    M, N = X.shape
+    ldx = _matrix(X, M, N, X.dtype, "X")
+    w_type, _ = _norm_weights(W, B, N, X.dtype)
+    if Y is None:
+        Y = torch.empty((M, N), dtype=X.dtype, device=X.device)
+    ldy = _matrix(Y, M, N, X.dtype, "Y")
+    if mean is None:
+        mean = torch.empty(M, dtype=torch.float32, device=X.device)
+    if rstd is None:
+        rstd = torch.empty(M, dtype=torch.float32, device=X.device)
+    _vector(mean, M, torch.float32, "mean")
+    _vector(rstd, M, torch.float32, "rstd")
+    _check(load_library().atb_layer_norm(M, N, _dtype(X), X.data_ptr(), ldx, w_type, _opt_ptr(W), _opt_ptr(B), eps, Y.data_ptr(), ldy,
+                                         mean.data_ptr(), rstd.data_ptr(), _on_stream(X.device, stream)))
+    return Y, mean, rstd
+
+
+def atb_layer_norm_bfp16(X, W=None, B=None, eps=1e-5, mant=None, exp=None, mean=None, rstd=None, stream=None):
+    """Layer norm that leaves as BFP16 planes, the A operand of ``atb_gemm``.  Returns ``(mant, exp, mean, rstd)``."""
+    import torch
+    if X.dim() != 2:
+        raise ValueError("X: a matrix")
+    M, N = X.shape
+    ldx = _matrix(X, M, N, X.dtype, "X")
+    w_type, _ = _norm_weights(W, B, N, X.dtype)
+    if mant is None:
+        mant = torch.empty((M, N), dtype=torch.int8, device=X.device)
+    if exp is None:
+        exp = torch.empty(atb_bfp16_exp_bytes(M, N), dtype=torch.uint8, device=X.device)
+    if not mant.is_contiguous():
+        raise ValueError("mant: contiguous")
+    _matrix(mant, M, N, torch.int8, "mant")
+    _vector(exp, atb_bfp16_exp_bytes(M, N), torch.uint8, "exp")
+    if mean is None:
+        mean = torch.empty(M, dtype=torch.float32, device=X.device)
+    if rstd is None:
+        rstd = torch.empty(M, dtype=torch.float32, device=X.device)
+    _vector(mean, M, torch.float32, "mean")
+    _vector(rstd, M, torch.float32, "rstd")
+    _check(load_library().atb_layer_norm_bfp16(M, N, _dtype(X), X.data_ptr(), ldx, w_type, _opt_ptr(W), _opt_ptr(B), eps,
+                                               mant.data_ptr(), exp.data_ptr(), mean.data_ptr(), rstd.data_ptr(),
+                                               _on_stream(X.device, stream)))
+    return mant, exp, mean, rstd
+
+
+def atb_layer_norm_backward_workspace_bytes(M: int, N: int) -> int:
+    return int(load_library().atb_layer_norm_backward_workspace_bytes(M, N))
+
+
+def atb_layer_norm_backward(dY, X, W, mean, rstd, dX=None, dW=None, dB=None, workspace=None, stream=None):
+    """Gradients ``(dX, dW, dB)`` of ``atb_layer_norm``; dW and dB in W's type (float32 where W is None)."""
+    import torch
+    if X.dim() != 2:
+        raise ValueError("X: a matrix")
+    M, N = X.shape
+    ldx = _matrix(X, M, N, X.dtype, "X")
+    lddy = _matrix(dY, M, N, X.dtype, "dY")
+    w_dtype = torch.float32 if W is None else W.dtype
+    _vector(W, N, w_dtype, "W")
+    _vector(mean, M, torch.float32, "mean")
+    _vector(rstd, M, torch.float32, "rstd")
+    if dX is None:
+        dX = torch.empty((M, N), dtype=X.dtype, device=X.device)
+    if dW is None:
+        dW = torch.empty(N, dtype=w_dtype, device=X.device)
+    if dB is None:
+        dB = torch.empty(N, dtype=w_dtype, device=X.device)
+    lddx = _matrix(dX, M, N, X.dtype, "dX")
+    _vector(dW, N, w_dtype, "dW")
+    _vector(dB, N, w_dtype, "dB")
+    lib = load_library()
+    ws, ws_bytes, workspace = _workspace(workspace, lib.atb_layer_norm_backward_workspace_bytes(M, N), X.device)
+    _check(lib.atb_layer_norm_backward(M, N, _dtype(X), dY.data_ptr(), lddy, X.data_ptr(), ldx, _dtype(dW), _opt_ptr(W), mean.data_ptr(),
+                                       rstd.data_ptr(), dX.data_ptr(), lddx, dW.data_ptr(), dB.data_ptr(), ws, ws_bytes,
+                                       _on_stream(X.device, stream)))
+    return dX, dW, dB
+
+
+def _ffn_shapes(X, Wg, Wu, Wd):
+    import torch
+    if X.dim() != 2 or Wg.dim() != 2:
+        raise ValueError("X, Wg: matrices")
+    (M, D), F = X.shape, Wg.shape[1]
+    bf16 = torch.bfloat16
+    ldx, ldw, ldwd = _matrix(X, M, D, bf16, "X"), _matrix(Wg, D, F, bf16, "Wg"), _matrix(Wd, F, D, bf16, "Wd")
+    if _matrix(Wu, D, F, bf16, "Wu") != ldw:
+        raise ValueError("Wg and Wu need the same row stride")
+    return M, D, F, ldx, ldw, ldwd
+
+
+def _act(act):
+    return ACTIVATIONS[act] if act in ACTIVATIONS else int(act)
+
+
+def atb_gated_ffn_workspace_bytes(M: int, D: int, F: int) -> int:
+    return int(load_library().atb_gated_ffn_workspace_bytes(M, D, F))
+
+
+def atb_gated_ffn(X, Wg, Wu, Wd, act="silu", save=False, Y=None, H=None, G=None, U=None, workspace=None, stream=None):
+    """``Y = (act(X Wg) * (X Wu)) Wd`` on bfloat16 matrices ``X [M, D]``, ``Wg``, ``Wu`` ``[D, F]``, ``Wd [F, D]``.
+
+    ``act``: "silu", "gelu" or "gelu_tanh".  Returns Y, or with ``save`` ``(Y, H, G, U)``: what the backward pass takes."""
+    import torch
+    M, D, F, ldx, ldw, ldwd = _ffn_shapes(X, Wg, Wu, Wd)
+    bf16 = torch.bfloat16
+    if Y is None:
+        Y = torch.empty((M, D), dtype=bf16, device=X.device)
+    if H is None:
+        H = torch.empty((M, F), dtype=bf16, device=X.device)
+    if save:
+        G = torch.empty((M, F), dtype=bf16, device=X.device) if G is None else G
+        U = torch.empty((M, F), dtype=bf16, device=X.device) if U is None else U
+    ldy = _matrix(Y, M, D, bf16, "Y")
+    for t, name in ((H, "H"), (G, "G"), (U, "U")):
+        if t is not None and (_matrix(t, M, F, bf16, name) != F):
+            raise ValueError(f"{name}: contiguous")
+    lib = load_library()
+    ws, ws_bytes, workspace = _workspace(workspace, lib.atb_gated_ffn_workspace_bytes(M, D, F), X.device)
+    _check(lib.atb_gated_ffn(M, D, F, _act(act), X.data_ptr(), ldx, Wg.data_ptr(), Wu.data_ptr(), ldw, Wd.data_ptr(), ldwd, Y.data_ptr(), ldy,
+                             H.data_ptr(), _opt_ptr(G), _opt_ptr(U), ws, ws_bytes, _on_stream(X.device, stream)))
+    return (Y, H, G, U) if save else Y
+
+
+def atb_gated_ffn_backward_workspace_bytes(M: int, D: int, F: int) -> int:
+    return int(load_library().atb_gated_ffn_backward_workspace_bytes(M, D, F))
+
+
+def atb_gated_ffn_backward(dY, X, Wg, Wu, Wd, H, G, U, act="silu", dX=None, dWg=None, dWu=None, dWd=None, workspace=None, stream=None):
+    """Gradients ``(dX, dWg, dWu, dWd)`` of ``atb_gated_ffn`` from ``dY`` and the ``H``, ``G``, ``U`` that it saved."""
+    import torch
+    M, D, F, ldx, ldw, ldwd = _ffn_shapes(X, Wg, Wu, Wd)
+    bf16 = torch.bfloat16
+    lddy = _matrix(dY, M, D, bf16, "dY")
+    for t, name in ((H, "H"), (G, "G"), (U, "U")):
+        if _matrix(t, M, F, bf16, name) != F:
+            raise ValueError(f"{name}: contiguous")
+    if dX is None:
+        dX = torch.empty((M, D), dtype=bf16, device=X.device)
+    if dWg is None:
+        dWg = torch.empty((D, F), dtype=bf16, device=X.device)
+    if dWu is None:
+        dWu = torch.empty((D, F), dtype=bf16, device=X.device)
+    if dWd is None:
+        dWd = torch.empty((F, D), dtype=bf16, device=X.device)
+    lddx, lddw, lddwd = _matrix(dX, M, D, bf16, "dX"), _matrix(dWg, D, F, bf16, "dWg"), _matrix(dWd, F, D, bf16, "dWd")
+    if _matrix(dWu, D, F, bf16, "dWu") != lddw:
+        raise ValueError("dWg and dWu need the same row stride")
+    lib = load_library()
+    ws, ws_bytes, workspace = _workspace(workspace, lib.atb_gated_ffn_backward_workspace_bytes(M, D, F), X.device)
+    _check(lib.atb_gated_ffn_backward(M, D, F, _act(act), dY.data_ptr(), lddy, X.data_ptr(), ldx, Wg.data_ptr(), Wu.data_ptr(), ldw,
+                                      Wd.data_ptr(), ldwd, H.data_ptr(), G.data_ptr(), U.data_ptr(), dX.data_ptr(), lddx, dWg.data_ptr(),
+                                      dWu.data_ptr(), lddw, dWd.data_ptr(), lddwd, ws, ws_bytes, _on_stream(X.device, stream)))
+    return dX, dWg, dWu, dWd
+
+
+def _head_shapes(X, W, labels):
+    import torch
+    if X.dim() != 2 or W.dim() != 2:
+        raise ValueError("X, W: matrices")
+    (M, D), V = X.shape, W.shape[0]
+    ldx, ldw = _matrix(X, M, D, torch.bfloat16, "X"), _matrix(W, V, D, torch.bfloat16, "W")
+    _vector(labels, M, torch.int64, "labels")
+    return M, V, D, ldx, ldw
+
+
+def atb_linear_cross_entropy_workspace_bytes(M: int, V: int, D: int) -> int:
+    return int(load_library().atb_linear_cross_entropy_workspace_bytes(M, V, D))
+
+
+def atb_linear_cross_entropy(X, W, labels, ignore_index=-100, loss=None, lse=None, workspace=None, stream=None):
+    """Cross entropy of the logits ``X W^T`` (bfloat16 ``X [M, D]``, ``W [V, D]``, int64 ``labels [M]``), which are not kept.
+
+    Returns float32 ``(loss, lse)``, ``[M]`` each; rows whose label is ``ignore_index`` have loss 0."""
+    import torch
+    M, V, D, ldx, ldw = _head_shapes(X, W, labels)
+    if loss is None:
+        loss = torch.empty(M, dtype=torch.float32, device=X.device)
+    if lse is None:
+        lse = torch.empty(M, dtype=torch.float32, device=X.device)
+    _vector(loss, M, torch.float32, "loss")
+    _vector(lse, M, torch.float32, "lse")
+    lib = load_library()
+    ws, ws_bytes, workspace = _workspace(workspace, lib.atb_linear_cross_entropy_workspace_bytes(M, V, D), X.device)
+    _check(lib.atb_linear_cross_entropy(M, V, D, X.data_ptr(), ldx, W.data_ptr(), ldw, labels.data_ptr(), ignore_index, loss.data_ptr(),
+                                        lse.data_ptr(), ws, ws_bytes, _on_stream(X.device, stream)))
+    return loss, lse
+
+
+def atb_linear_cross_entropy_backward_workspace_bytes(M: int, V: int, D: int, piece: int = 0) -> int:
+    return int(load_library().atb_linear_cross_entropy_backward_workspace_bytes(M, V, D, piece))
+
+
+def atb_linear_cross_entropy_backward(dloss, X, W, labels, lse, ignore_index=-100, dX=None, dW=None, piece=0, workspace=None, stream=None):
+    """Gradients ``(dX, dW)`` (bfloat16) of ``sum(dloss * loss)``; ``piece``: words of the vocabulary per pass (0: chosen)."""
+    import torch
+    M, V, D, ldx, ldw = _head_shapes(X, W, labels)
+    _vector(dloss, M, torch.float32, "dloss")
+    _vector(lse, M, torch.float32, "lse")
+    if dX is None:
+        dX = torch.empty((M, D), dtype=torch.bfloat16, device=X.device)
+    if dW is None:
+        dW = torch.empty((V, D), dtype=torch.bfloat16, device=X.device)
+    lddx, lddw = _matrix(dX, M, D, torch.bfloat16, "dX"), _matrix(dW, V, D, torch.bfloat16, "dW")
+    lib = load_library()
+    ws, ws_bytes, workspace = _workspace(workspace, lib.atb_linear_cross_entropy_backward_workspace_bytes(M, V, D, piece), X.device)
+    _check(lib.atb_linear_cross_entropy_backward(M, V, D, X.data_ptr(), ldx, W.data_ptr(), ldw, labels.data_ptr(), ignore_index,
+                                                 lse.data_ptr(), dloss.data_ptr(), dX.data_ptr(), lddx, dW.data_ptr(), lddw, piece, ws, ws_bytes,
+                                                 _on_stream(X.device, stream)))
+    return dX, dW
 
 
 # ------------------------------------------------------------------ layout helpers (no arithmetic)

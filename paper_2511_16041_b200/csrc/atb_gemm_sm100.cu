@@ -577,6 +577,9 @@ extern "C" atb_status_t atb_device_status(void* stream) {
     flag = atb::take_cfg_error_flag();
     if (flag != 0)
         return atb::fail(ATB_ERR_DEVICE_TIMEOUT, "a precision-configuration GEMM kernel gave up a bounded wait (code 0x%03x)", flag);
+    flag = atb::take_mm_error_flag();
+    if (flag != 0)
+        return atb::fail(ATB_ERR_DEVICE_TIMEOUT, "a BF16 product kernel gave up a bounded wait (code 0x%03x)", flag);
     return ATB_OK;
 }
 

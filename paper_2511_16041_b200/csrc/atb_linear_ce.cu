@@ -1,0 +1,194 @@
+// Softmax cross entropy of a linear head without its logits, forward and backward.
+//
+//   l = x W^T, lse = log sum_v exp(l_v), loss = lse - l[label];  dl = (exp(l - lse) - [v = label]) dloss, dx = dl W, dW = dl^T x
+//
+// Forward: the logits of a tile stay in tensor memory; what leaves is, per row and group of columns, the maximum and
+// the sum of exp(l - maximum), 8 bytes for 128 logits, and the label's logit.  A second kernel joins them.
+// Backward: the logits are computed again, a piece of the vocabulary at a time; the epilogue turns them into dl, which
+// the workspace holds for one piece (bf16: it is the operand of the next two products).  dW of the piece is complete;
+// dx is added up over the pieces in FP32, in their order, and rounded once.
+#include <cuda_bf16.h>
+
+#include "atb_bf16_mm.h"
+
+namespace {
+
+// One warp per row: joins the row's (maximum, sum) pairs, in a fixed order.
+__global__ void __launch_bounds__(256) linear_ce_join_kernel(int64_t M, int64_t V, const float2* stats, int64_t per_row, const float* label_logit,
+                                                             const int64_t* labels, int64_t ignore_index, float* loss, float* lse) {
+    const int64_t row = static_cast<int64_t>(blockIdx.x) * 8 + (threadIdx.x >> 5);
+    const int lane = threadIdx.x & 31;
+    if (row >= M) return;
+    float m = -INFINITY, s = 0.f;
+    for (int64_t i = lane; i < per_row; i += 32) {
+        const float2 v = stats[row * per_row + i];
+        const float top = fmaxf(m, v.x), ref = top == -INFINITY ? 0.f : top;
+        s = s * expf(m - ref) + v.y * expf(v.x - ref);
+        m = top;
+    }
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) {
+        const float m2 = __shfl_xor_sync(0xFFFFFFFFu, m, o), s2 = __shfl_xor_sync(0xFFFFFFFFu, s, o);
+        const float top = fmaxf(m, m2), ref = top == -INFINITY ? 0.f : top;
+        s = s * expf(m - ref) + s2 * expf(m2 - ref);
+        m = top;
+    }
+    if (lane == 0) {
+        const int64_t label = labels[row];
+        float z = m + logf(s), l = 0.f;
+        if (label != ignore_index) {
+            if (label < 0 || label >= V) z = l = __int_as_float(0x7FC00000);     // no such word: NaN, and so every gradient
+            else l = z - label_logit[row];
+        }
+        lse[row] = z;
+        loss[row] = l;
+    }
+}
+
+__global__ void __launch_bounds__(256) linear_ce_round_kernel(const float* src, int64_t M, int64_t N, __nv_bfloat16* dst, int64_t ld) {
+    const int64_t per_row = N / 8;
+    for (int64_t i = static_cast<int64_t>(blockIdx.x) * 256 + threadIdx.x; i < M * per_row; i += static_cast<int64_t>(gridDim.x) * 256) {
+        const int64_t m = i / per_row, n = (i - m * per_row) * 8;
+        const float4 a = *reinterpret_cast<const float4*>(src + m * N + n), b = *reinterpret_cast<const float4*>(src + m * N + n + 4);
+        __nv_bfloat162 o[4] = {__floats2bfloat162_rn(a.x, a.y), __floats2bfloat162_rn(a.z, a.w), __floats2bfloat162_rn(b.x, b.y),
+                               __floats2bfloat162_rn(b.z, b.w)};
+        *reinterpret_cast<uint4*>(dst + m * ld + n) = *reinterpret_cast<const uint4*>(o);
+    }
+}
+
+atb_status_t check_head(int64_t M, int64_t V, int64_t D) {
+    if (M < 0 || V < 1 || D < 8 || D % 8 != 0 || M > (1ll << 30) || V > (1ll << 30) || D > (1ll << 30))
+        return atb::fail(ATB_ERR_BAD_SHAPE, "need M >= 0, V >= 1, D >= 8 with D %% 8 == 0 (got %lld, %lld, %lld)", (long long)M, (long long)V, (long long)D);
+    return ATB_OK;
+}
+bool ld_ok(int64_t ld, int64_t least) { return ld >= least && ld % 8 == 0; }
+size_t align256(size_t n) { return (n + 255) / 256 * 256; }
+
+// Words of a piece: the caller's number rounded up to whole tiles, or (0) as many as keep dl within 512 MB.
+int64_t piece_words(int64_t M, int64_t V, int64_t piece) {
+    if (piece <= 0) {
+        piece = (1ll << 28) / M / 256 * 256;
+        if (piece < 2048) piece = 2048;
+    }
+    piece = atb::round_up(piece < V ? piece : V, 256);
+    return piece;
+}
+
+}  // namespace
+
+extern "C" size_t atb_linear_cross_entropy_workspace_bytes(int64_t M, int64_t V, int64_t D) {
+    if (M < 1 || V < 1 || D < 1) return 0;
+    return align256(static_cast<size_t>(M) * static_cast<size_t>(atb::mm_stats_per_row(M, V)) * sizeof(float2)) + static_cast<size_t>(M) * sizeof(float);
+}
+
+extern "C" atb_status_t atb_linear_cross_entropy(int64_t M, int64_t V, int64_t D, const void* X_dev, int64_t ldx, const void* W_dev, int64_t ldw,
+                                                 const int64_t* labels_dev, int64_t ignore_index, float* loss_dev, float* lse_dev,
+                                                 void* workspace_dev, size_t workspace_bytes, void* stream) {
+    atb::clear_error();
+    atb_status_t s = check_head(M, V, D);
+    if (s != ATB_OK) return s;
+    if (M == 0) return ATB_OK;
+    if (!X_dev || !W_dev || !labels_dev || !loss_dev || !lse_dev || !workspace_dev)
+        return atb::fail(ATB_ERR_NULL_POINTER, "all device pointers, including the workspace, must be non-NULL");
+    if (!ld_ok(ldx, D) || !ld_ok(ldw, D))
+        return atb::fail(ATB_ERR_BAD_SHAPE, "ldx=%lld and ldw=%lld must be >= D and multiples of 8", (long long)ldx, (long long)ldw);
+    if (!atb::aligned16(X_dev) || !atb::aligned16(W_dev) || !atb::aligned16(workspace_dev) || (reinterpret_cast<uintptr_t>(labels_dev) & 7) ||
+        (reinterpret_cast<uintptr_t>(loss_dev) & 3) || (reinterpret_cast<uintptr_t>(lse_dev) & 3))
+        return atb::fail(ATB_ERR_MISALIGNED, "X, W and the workspace must be 16-byte aligned, labels, loss and lse to their elements");
+    const size_t need = atb_linear_cross_entropy_workspace_bytes(M, V, D);
+    if (workspace_bytes < need) return atb::fail(ATB_ERR_BUFFER_TOO_SMALL, "workspace of %zu bytes is smaller than the %zu needed", workspace_bytes, need);
+    cudaStream_t st = static_cast<cudaStream_t>(stream);
+    atb::MmProblem q;
+    q.layout = atb::kMmNT; q.epilogue = atb::kMmRowStats;
+    q.M = M; q.N = V; q.K = D;
+    q.A[0] = {X_dev, ldx}; q.B[0] = {W_dev, ldw};
+    q.labels = labels_dev;
+    q.stats = static_cast<float2*>(workspace_dev);
+    q.stats_ld = atb::mm_stats_per_row(M, V);
+    q.label_logit = reinterpret_cast<float*>(static_cast<char*>(workspace_dev) + (need - static_cast<size_t>(M) * sizeof(float)));
+    s = atb::mm_launch(q, st);
+    if (s != ATB_OK) return s;
+    linear_ce_join_kernel<<<static_cast<unsigned>(atb::ceil_div(M, 8)), 256, 0, st>>>(M, V, q.stats, q.stats_ld, q.label_logit, labels_dev, ignore_index,
+                                                                                     loss_dev, lse_dev);
+    const cudaError_t e = cudaGetLastError();
+    if (e != cudaSuccess) return atb::fail(ATB_ERR_CUDA, "linear cross entropy launch: %s", cudaGetErrorString(e));
+    return ATB_OK;
+}
+
+extern "C" size_t atb_linear_cross_entropy_backward_workspace_bytes(int64_t M, int64_t V, int64_t D, int64_t piece) {
+    if (M < 1 || V < 1 || D < 1) return 0;
+    const int64_t words = piece_words(M, V, piece);
+    const size_t dl = align256(static_cast<size_t>(M) * static_cast<size_t>(words) * 2);
+    return dl + (words < V ? static_cast<size_t>(M) * static_cast<size_t>(D) * sizeof(float) : 0);
+}
+
+extern "C" atb_status_t atb_linear_cross_entropy_backward(int64_t M, int64_t V, int64_t D, const void* X_dev, int64_t ldx, const void* W_dev,
+                                                          int64_t ldw, const int64_t* labels_dev, int64_t ignore_index, const float* lse_dev,
+                                                          const float* dloss_dev, void* dX_dev, int64_t lddx, void* dW_dev, int64_t lddw,
+                                                          int64_t piece, void* workspace_dev, size_t workspace_bytes, void* stream) {
+    atb::clear_error();
+    atb_status_t s = check_head(M, V, D);
+    if (s != ATB_OK) return s;
+    if (M > 0 && (!X_dev || !W_dev || !labels_dev || !lse_dev || !dloss_dev || !workspace_dev))
+        return atb::fail(ATB_ERR_NULL_POINTER, "X, W, labels, lse, dloss and the workspace must be non-NULL");
+    if (piece < 0) return atb::fail(ATB_ERR_BAD_ARGUMENT, "piece must be >= 0 (0: the library's choice)");
+    if ((M > 0 && (!ld_ok(ldx, D) || !ld_ok(ldw, D) || (dX_dev && !ld_ok(lddx, D)))) || (dW_dev && !ld_ok(lddw, D)))
+        return atb::fail(ATB_ERR_BAD_SHAPE, "ldx, ldw, lddx and lddw must be >= D and multiples of 8");
+    if (!atb::aligned16(X_dev) || !atb::aligned16(W_dev) || !atb::aligned16(dX_dev) || !atb::aligned16(dW_dev) || !atb::aligned16(workspace_dev) ||
+        (reinterpret_cast<uintptr_t>(labels_dev) & 7) || (reinterpret_cast<uintptr_t>(lse_dev) & 3) || (reinterpret_cast<uintptr_t>(dloss_dev) & 3))
+        return atb::fail(ATB_ERR_MISALIGNED, "X, W, dX, dW and the workspace must be 16-byte aligned, labels, lse and dloss to their elements");
+    const size_t need = atb_linear_cross_entropy_backward_workspace_bytes(M, V, D, piece);
+    if (workspace_bytes < need) return atb::fail(ATB_ERR_BUFFER_TOO_SMALL, "workspace of %zu bytes is smaller than the %zu needed", workspace_bytes, need);
+    cudaStream_t st = static_cast<cudaStream_t>(stream);
+    int sms = 0;
+    s = atb::op_device(&sms, nullptr);
+    if (s != ATB_OK) return s;
+    if (M == 0) {
+        const cudaError_t e = dW_dev ? cudaMemset2DAsync(dW_dev, lddw * 2, 0, D * 2, V, st) : cudaSuccess;
+        return e == cudaSuccess ? ATB_OK : atb::fail(ATB_ERR_CUDA, "cudaMemset2DAsync: %s", cudaGetErrorString(e));
+    }
+    if (!dX_dev && !dW_dev) return ATB_OK;
+    const int64_t words = piece_words(M, V, piece);
+    uint16_t* const dl = static_cast<uint16_t*>(workspace_dev);
+    float* const sum = reinterpret_cast<float*>(static_cast<char*>(workspace_dev) + align256(static_cast<size_t>(M) * static_cast<size_t>(words) * 2));
+    for (int64_t v0 = 0; v0 < V; v0 += words) {
+        const int64_t n = V - v0 < words ? V - v0 : words;
+        const uint16_t* const Wv = static_cast<const uint16_t*>(W_dev) + v0 * ldw;
+        atb::MmProblem q;
+        q.layout = atb::kMmNT; q.epilogue = atb::kMmDlogits;
+        q.M = M; q.N = n; q.K = D;
+        q.A[0] = {X_dev, ldx}; q.B[0] = {Wv, ldw};
+        q.C[0] = dl; q.ldc[0] = words;
+        q.labels = labels_dev; q.ignore_index = ignore_index; q.col0 = v0;
+        q.lse = lse_dev; q.scale = dloss_dev;
+        s = atb::mm_launch(q, st);
+        if (s != ATB_OK) return s;
+        if (dX_dev) {
+            atb::MmProblem dx;
+            dx.layout = atb::kMmNN;
+            dx.M = M; dx.N = D; dx.K = n;
+            dx.A[0] = {dl, words}; dx.B[0] = {Wv, ldw};
+            if (words < V) { dx.epilogue = atb::kMmAccumulate; dx.C32 = sum; dx.first = v0 == 0; }
+            else { dx.epilogue = atb::kMmStore; dx.C[0] = dX_dev; dx.ldc[0] = lddx; }
+            s = atb::mm_launch(dx, st);
+            if (s != ATB_OK) return s;
+        }
+        if (dW_dev) {
+            atb::MmProblem dw;
+            dw.layout = atb::kMmTN; dw.epilogue = atb::kMmStore;
+            dw.M = n; dw.N = D; dw.K = M;
+            dw.A[0] = {dl, words}; dw.B[0] = {X_dev, ldx};
+            dw.C[0] = static_cast<uint16_t*>(dW_dev) + v0 * lddw; dw.ldc[0] = lddw;
+            s = atb::mm_launch(dw, st);
+            if (s != ATB_OK) return s;
+        }
+    }
+    if (dX_dev && words < V) {
+        const int64_t vecs = M * (D / 8);
+        const int blocks = static_cast<int>(atb::ceil_div(vecs, 256) < sms * 8 ? atb::ceil_div(vecs, 256) : sms * 8);
+        linear_ce_round_kernel<<<blocks, 256, 0, st>>>(sum, M, D, static_cast<__nv_bfloat16*>(dX_dev), lddx);
+    }
+    const cudaError_t e = cudaGetLastError();
+    if (e != cudaSuccess) return atb::fail(ATB_ERR_CUDA, "linear cross entropy backward launch: %s", cudaGetErrorString(e));
+    return ATB_OK;
+}

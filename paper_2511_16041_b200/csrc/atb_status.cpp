@@ -32,6 +32,7 @@ const char* atb_status_string(atb_status_t s) {
         case ATB_ERR_CUDA: return "ATB_ERR_CUDA";
         case ATB_ERR_BUFFER_TOO_SMALL: return "ATB_ERR_BUFFER_TOO_SMALL";
         case ATB_ERR_DEVICE_TIMEOUT: return "ATB_ERR_DEVICE_TIMEOUT";
+        case ATB_ERR_BAD_ARGUMENT: return "ATB_ERR_BAD_ARGUMENT";
     }
     return "ATB_ERR_UNKNOWN";
 }
