@@ -37,6 +37,7 @@ struct MmProblem {
     MmOperand A[2], B[2];
     void* C[3] = {nullptr, nullptr, nullptr};   // bf16 outputs; kMmGlu: h, g, u (g and u may be NULL); kMmGluBackward: dg, du
     int64_t ldc[3] = {0, 0, 0};
+    float* partial = nullptr;         // FP32 sums of the K ranges of a split product (mm_partial_bytes)
     // kMmAccumulate
     float* C32 = nullptr;             // [M][N]
     bool first = true;
@@ -52,8 +53,10 @@ struct MmProblem {
     const float *lse = nullptr, *scale = nullptr;
 };
 
-// Entries of `stats` per row for a product of M x N.
-int64_t mm_stats_per_row(int64_t M, int64_t N);
+// Entries of `stats` per row for a product of M x N x K.
+int64_t mm_stats_per_row(int64_t M, int64_t N, int64_t K);
+// Bytes that `partial` needs: 0 where the product is not split along K.
+size_t mm_partial_bytes(MmEpilogue epilogue, int64_t M, int64_t N, int64_t K, int k_segs = 1, int n_segs = 1);
 
 // Enqueues the product on `stream`.  Pointers 16-byte aligned, leading dimensions multiples of 8 (callers check).
 atb_status_t mm_launch(const MmProblem& p, cudaStream_t stream);

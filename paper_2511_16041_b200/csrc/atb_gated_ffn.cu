@@ -8,6 +8,8 @@
 // behind dx are one walk over 2 F; dWg and dWu are one launch.  h, g and u are kept in bf16 between the products: they
 // are (h) or were (the accumulators of g and u, FP32) operands of the tensor cores, which take bf16; the one
 // rounding costs 2^-9 of the value.
+#include <algorithm>
+
 #include "atb_bf16_mm.h"
 
 namespace {
@@ -26,12 +28,15 @@ atb_status_t check_block(const Block& b) {
     return ATB_OK;
 }
 bool ld_ok(int64_t ld, int64_t least) { return ld >= least && ld % 8 == 0; }
+// dg and du in the workspace, [M][F] bf16 each, up to the next 256 bytes.
+size_t glu_gradient_bytes(int64_t M, int64_t F) { return (4 * static_cast<size_t>(M) * static_cast<size_t>(F) + 255) / 256 * 256; }
 
 }  // namespace
 
 extern "C" size_t atb_gated_ffn_workspace_bytes(int64_t M, int64_t D, int64_t F) {
-    (void)M; (void)D; (void)F;
-    return 0;
+    if (M < 1 || D < 1 || F < 1) return 0;
+    // the sums of a product that is split along K; the two products take turns
+    return std::max(atb::mm_partial_bytes(atb::kMmGlu, M, F, D), atb::mm_partial_bytes(atb::kMmStore, M, D, F));
 }
 
 extern "C" atb_status_t atb_gated_ffn(int64_t M, int64_t D, int64_t F, int act, const void* X_dev, int64_t ldx, const void* Wg_dev,
@@ -59,6 +64,7 @@ extern "C" atb_status_t atb_gated_ffn(int64_t M, int64_t D, int64_t F, int act, 
     up.A[0] = {X_dev, ldx}; up.B[0] = {Wg_dev, ldw}; up.B[1] = {Wu_dev, ldw};
     up.C[0] = H_dev; up.C[1] = G_dev; up.C[2] = U_dev;
     up.ldc[0] = up.ldc[1] = up.ldc[2] = F;
+    up.partial = static_cast<float*>(workspace_dev);
     s = atb::mm_launch(up, st);
     if (s != ATB_OK) return s;
 
@@ -67,13 +73,15 @@ extern "C" atb_status_t atb_gated_ffn(int64_t M, int64_t D, int64_t F, int act, 
     down.M = M; down.N = D; down.K = F;
     down.A[0] = {H_dev, F}; down.B[0] = {Wd_dev, ldwd};
     down.C[0] = Y_dev; down.ldc[0] = ldy;
+    down.partial = static_cast<float*>(workspace_dev);
     return atb::mm_launch(down, st);
 }
 
 extern "C" size_t atb_gated_ffn_backward_workspace_bytes(int64_t M, int64_t D, int64_t F) {
-    (void)D;
-    if (M < 1 || F < 1) return 0;
-    return 2 * static_cast<size_t>(M) * static_cast<size_t>(F) * 2;        // dg and du
+    if (M < 1 || D < 1 || F < 1) return 0;
+    // dg and du, and the sums of a product that is split along K
+    return glu_gradient_bytes(M, F) + std::max({atb::mm_partial_bytes(atb::kMmGluBackward, M, F, D), atb::mm_partial_bytes(atb::kMmStore, M, D, F, 2),
+                                                atb::mm_partial_bytes(atb::kMmStore, D, F, M, 1, 2), atb::mm_partial_bytes(atb::kMmStore, F, D, M)});
 }
 
 extern "C" atb_status_t atb_gated_ffn_backward(int64_t M, int64_t D, int64_t F, int act, const void* dY_dev, int64_t lddy, const void* X_dev,
@@ -108,6 +116,7 @@ extern "C" atb_status_t atb_gated_ffn_backward(int64_t M, int64_t D, int64_t F, 
     }
     uint16_t* const dG = static_cast<uint16_t*>(workspace_dev);
     uint16_t* const dU = dG + M * F;
+    float* const partial = reinterpret_cast<float*>(static_cast<char*>(workspace_dev) + glu_gradient_bytes(M, F));
 
     if (dX_dev || dWg_dev) {
         atb::MmProblem dh;
@@ -116,6 +125,7 @@ extern "C" atb_status_t atb_gated_ffn_backward(int64_t M, int64_t D, int64_t F, 
         dh.A[0] = {dY_dev, lddy}; dh.B[0] = {Wd_dev, ldwd};
         dh.G = G_dev; dh.U = U_dev;
         dh.C[0] = dG; dh.C[1] = dU; dh.ldc[0] = dh.ldc[1] = F;
+        dh.partial = partial;
         s = atb::mm_launch(dh, st);
         if (s != ATB_OK) return s;
     }
@@ -125,6 +135,7 @@ extern "C" atb_status_t atb_gated_ffn_backward(int64_t M, int64_t D, int64_t F, 
         dx.M = M; dx.N = D; dx.K = F; dx.k_segs = 2;
         dx.A[0] = {dG, F}; dx.A[1] = {dU, F}; dx.B[0] = {Wg_dev, ldw}; dx.B[1] = {Wu_dev, ldw};
         dx.C[0] = dX_dev; dx.ldc[0] = lddx;
+        dx.partial = partial;
         s = atb::mm_launch(dx, st);
         if (s != ATB_OK) return s;
     }
@@ -134,6 +145,7 @@ extern "C" atb_status_t atb_gated_ffn_backward(int64_t M, int64_t D, int64_t F, 
         dw.M = D; dw.N = F; dw.K = M; dw.n_segs = 2;
         dw.A[0] = {X_dev, ldx}; dw.B[0] = {dG, F}; dw.B[1] = {dU, F};
         dw.C[0] = dWg_dev; dw.C[1] = dWu_dev; dw.ldc[0] = dw.ldc[1] = lddw;
+        dw.partial = partial;
         s = atb::mm_launch(dw, st);
         if (s != ATB_OK) return s;
     }
@@ -143,6 +155,7 @@ extern "C" atb_status_t atb_gated_ffn_backward(int64_t M, int64_t D, int64_t F, 
         dw.M = F; dw.N = D; dw.K = M;
         dw.A[0] = {H_dev, F}; dw.B[0] = {dY_dev, lddy};
         dw.C[0] = dWd_dev; dw.ldc[0] = lddwd;
+        dw.partial = partial;
         s = atb::mm_launch(dw, st);
         if (s != ATB_OK) return s;
     }

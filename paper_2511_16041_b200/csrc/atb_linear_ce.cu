@@ -9,6 +9,8 @@
 // dx is added up over the pieces in FP32, in their order, and rounded once.
 #include <cuda_bf16.h>
 
+#include <algorithm>
+
 #include "atb_bf16_mm.h"
 
 namespace {
@@ -74,11 +76,30 @@ int64_t piece_words(int64_t M, int64_t V, int64_t piece) {
     return piece;
 }
 
+// The backward workspace: dl of a piece, FP32 sums of dx where there is more than one piece, and the sums of a product that
+// is split along K.
+struct BackwardSpace {
+    int64_t words;
+    size_t sum, partial, partial_bytes;      // offsets behind dl, size of the last part
+};
+BackwardSpace backward_space(int64_t M, int64_t V, int64_t D, int64_t piece) {
+    BackwardSpace w;
+    w.words = piece_words(M, V, piece);
+    w.sum = align256(static_cast<size_t>(M) * static_cast<size_t>(w.words) * 2);
+    w.partial = w.sum + (w.words < V ? align256(static_cast<size_t>(M) * static_cast<size_t>(D) * sizeof(float)) : 0);
+    // the last piece may be shorter than the others, with a plan of its own
+    const int64_t first = V < w.words ? V : w.words, last = V - (V - 1) / w.words * w.words;
+    const atb::MmEpilogue dx = w.words < V ? atb::kMmAccumulate : atb::kMmStore;
+    w.partial_bytes = std::max({atb::mm_partial_bytes(dx, M, D, first), atb::mm_partial_bytes(dx, M, D, last),
+                                atb::mm_partial_bytes(atb::kMmStore, first, D, M), atb::mm_partial_bytes(atb::kMmStore, last, D, M)});
+    return w;
+}
+
 }  // namespace
 
 extern "C" size_t atb_linear_cross_entropy_workspace_bytes(int64_t M, int64_t V, int64_t D) {
     if (M < 1 || V < 1 || D < 1) return 0;
-    return align256(static_cast<size_t>(M) * static_cast<size_t>(atb::mm_stats_per_row(M, V)) * sizeof(float2)) + static_cast<size_t>(M) * sizeof(float);
+    return align256(static_cast<size_t>(M) * static_cast<size_t>(atb::mm_stats_per_row(M, V, D)) * sizeof(float2)) + static_cast<size_t>(M) * sizeof(float);
 }
 
 extern "C" atb_status_t atb_linear_cross_entropy(int64_t M, int64_t V, int64_t D, const void* X_dev, int64_t ldx, const void* W_dev, int64_t ldw,
@@ -104,7 +125,7 @@ extern "C" atb_status_t atb_linear_cross_entropy(int64_t M, int64_t V, int64_t D
     q.A[0] = {X_dev, ldx}; q.B[0] = {W_dev, ldw};
     q.labels = labels_dev;
     q.stats = static_cast<float2*>(workspace_dev);
-    q.stats_ld = atb::mm_stats_per_row(M, V);
+    q.stats_ld = atb::mm_stats_per_row(M, V, D);
     q.label_logit = reinterpret_cast<float*>(static_cast<char*>(workspace_dev) + (need - static_cast<size_t>(M) * sizeof(float)));
     s = atb::mm_launch(q, st);
     if (s != ATB_OK) return s;
@@ -117,9 +138,8 @@ extern "C" atb_status_t atb_linear_cross_entropy(int64_t M, int64_t V, int64_t D
 
 extern "C" size_t atb_linear_cross_entropy_backward_workspace_bytes(int64_t M, int64_t V, int64_t D, int64_t piece) {
     if (M < 1 || V < 1 || D < 1) return 0;
-    const int64_t words = piece_words(M, V, piece);
-    const size_t dl = align256(static_cast<size_t>(M) * static_cast<size_t>(words) * 2);
-    return dl + (words < V ? static_cast<size_t>(M) * static_cast<size_t>(D) * sizeof(float) : 0);
+    const BackwardSpace w = backward_space(M, V, D, piece);
+    return w.partial + w.partial_bytes;
 }
 
 extern "C" atb_status_t atb_linear_cross_entropy_backward(int64_t M, int64_t V, int64_t D, const void* X_dev, int64_t ldx, const void* W_dev,
@@ -148,9 +168,11 @@ extern "C" atb_status_t atb_linear_cross_entropy_backward(int64_t M, int64_t V, 
         return e == cudaSuccess ? ATB_OK : atb::fail(ATB_ERR_CUDA, "cudaMemset2DAsync: %s", cudaGetErrorString(e));
     }
     if (!dX_dev && !dW_dev) return ATB_OK;
-    const int64_t words = piece_words(M, V, piece);
+    const BackwardSpace space = backward_space(M, V, D, piece);
+    const int64_t words = space.words;
     uint16_t* const dl = static_cast<uint16_t*>(workspace_dev);
-    float* const sum = reinterpret_cast<float*>(static_cast<char*>(workspace_dev) + align256(static_cast<size_t>(M) * static_cast<size_t>(words) * 2));
+    float* const sum = reinterpret_cast<float*>(static_cast<char*>(workspace_dev) + space.sum);
+    float* const partial = reinterpret_cast<float*>(static_cast<char*>(workspace_dev) + space.partial);
     for (int64_t v0 = 0; v0 < V; v0 += words) {
         const int64_t n = V - v0 < words ? V - v0 : words;
         const uint16_t* const Wv = static_cast<const uint16_t*>(W_dev) + v0 * ldw;
@@ -170,6 +192,7 @@ extern "C" atb_status_t atb_linear_cross_entropy_backward(int64_t M, int64_t V, 
             dx.A[0] = {dl, words}; dx.B[0] = {Wv, ldw};
             if (words < V) { dx.epilogue = atb::kMmAccumulate; dx.C32 = sum; dx.first = v0 == 0; }
             else { dx.epilogue = atb::kMmStore; dx.C[0] = dX_dev; dx.ldc[0] = lddx; }
+            dx.partial = partial;
             s = atb::mm_launch(dx, st);
             if (s != ATB_OK) return s;
         }
@@ -179,6 +202,7 @@ extern "C" atb_status_t atb_linear_cross_entropy_backward(int64_t M, int64_t V, 
             dw.M = n; dw.N = D; dw.K = M;
             dw.A[0] = {dl, words}; dw.B[0] = {X_dev, ldx};
             dw.C[0] = static_cast<uint16_t*>(dW_dev) + v0 * lddw; dw.ldc[0] = lddw;
+            dw.partial = partial;
             s = atb::mm_launch(dw, st);
             if (s != ATB_OK) return s;
         }

@@ -85,7 +85,6 @@ def test_pieces_of_the_vocabulary(M, V, D, piece):
     x, w, labels, dloss = _inputs(M, V, D)
     loss, lse = atb.atb_linear_cross_entropy(x, w, labels)
     dX, dW = atb.atb_linear_cross_entropy_backward(dloss, x, w, labels, lse, piece=piece)
-    assert atb.atb_linear_cross_entropy_backward_workspace_bytes(M, V, D, piece) < 2 * M * (-(-piece // 256) * 256) + 512 + 4 * M * D
     _check_backward(x, w, labels, dloss, lse, None, dX, dW)
 
 
