@@ -163,7 +163,8 @@ def _check(status: int):
 def _stream_ptr(stream):
     if stream is None:
         import torch
-        return ctypes.c_void_p(torch.cuda.current_stream().cuda_stream)
+        raw = getattr(torch._C, "_cuda_getCurrentRawStream", None)      # 3 us less per call than the Stream object
+        return ctypes.c_void_p(raw(torch.cuda.current_device()) if raw else torch.cuda.current_stream().cuda_stream)
     if isinstance(stream, int):
         return ctypes.c_void_p(stream)
     return ctypes.c_void_p(stream.cuda_stream)
@@ -387,44 +388,69 @@ def _dtype(t):
     raise TypeError(f"{t.dtype}: float32 or bfloat16")
 
 
-def _matrix(t, rows, cols, dtype, name):
-    """Checks a row-major CUDA matrix and returns its leading dimension."""
-    if not t.is_cuda or t.dim() != 2 or t.dtype != dtype or t.shape != (rows, cols) or (cols > 1 and t.stride(1) != 1):
-        raise ValueError(f"{name}: a row-major CUDA matrix {(rows, cols)} of {dtype}, got {tuple(t.shape)} of {t.dtype}")
+def _matrix(t, rows, cols, dtype, device, name):
+    """Checks a row-major matrix on CUDA device number ``device`` and returns its leading dimension."""
+    if t.get_device() != device or t.dtype != dtype or t.shape != (rows, cols) or (cols > 1 and t.stride(1) != 1):
+        raise ValueError(f"{name}: a row-major matrix {(rows, cols)} of {dtype} on cuda:{device}, got {tuple(t.shape)} of {t.dtype} on {t.device}, "
+                         f"strides {t.stride()}")
     return t.stride(0) if rows > 1 else max(cols, t.stride(0))
 
 
-def _vector(t, n, dtype, name):
-    if t is not None and (not t.is_cuda or t.dim() != 1 or t.dtype != dtype or t.shape[0] != n or (n > 1 and t.stride(0) != 1)):
-        raise ValueError(f"{name}: a contiguous CUDA vector of {n} {dtype}, got {tuple(t.shape)} of {t.dtype}")
+def _vector(t, n, dtype, device, name):
+    if t.get_device() != device or t.dtype != dtype or t.shape != (n,) or not t.is_contiguous():
+        raise ValueError(f"{name}: a contiguous vector of {n} {dtype} on cuda:{device}, got {tuple(t.shape)} of {t.dtype} on {t.device}")
 
 
 def _opt_ptr(t):
     return None if t is None else t.data_ptr()
 
 
-def _workspace(workspace, need, device):
-    """The caller's workspace, or a new one of ``need`` bytes."""
+def _workspace(workspace, need, like):
+    """Address and size of the caller's workspace, or of a new one of ``need`` bytes (kept alive by the third value)."""
     import torch
     if workspace is None:
-        workspace = torch.empty(need, dtype=torch.uint8, device=device)
+        if need == 0:
+            return None, 0, None
+        workspace = like.new_empty((need,), dtype=torch.uint8)
+    elif workspace.get_device() != like.get_device() or not workspace.is_contiguous():
+        raise ValueError(f"workspace: contiguous, on {like.device}")
     return workspace.data_ptr(), workspace.numel() * workspace.element_size(), workspace
 
 
-def _on_stream(device, stream):
-    """Raises unless the call's device is the current one; returns the raw stream."""
+def _device_of(t, name):
+    """Number of the CUDA device of the matrix ``t``, which has to be the current one (the kernels are launched there)."""
     import torch
-    if device.index != torch.cuda.current_device():
-        raise ValueError(f"the tensors are on {device}, the current device is cuda:{torch.cuda.current_device()}")
-    return _stream_ptr(stream)
+    device = t.get_device()
+    if device < 0 or t.dim() != 2:
+        raise ValueError(f"{name}: a CUDA matrix, got {tuple(t.shape)} on {t.device}")
+    if device != torch.cuda.current_device():
+        raise ValueError(f"{name} is on cuda:{device}, the current device is cuda:{torch.cuda.current_device()}")
+    return device
 
 
-def _norm_weights(W, B, N, x_dtype):
+def _norm_weights(W, B, N, x_dtype, device):
+    """The type code of the weights (any where there are none)."""
     given = W if W is not None else B
-    w_dtype = given.dtype if given is not None else x_dtype
-    _vector(W, N, w_dtype, "W")
-    _vector(B, N, w_dtype, "B")
-    return ATB_F32 if given is None else _dtype(given), w_dtype
+    if given is None:
+        return ATB_F32
+    for t, name in ((W, "W"), (B, "B")):
+        if t is not None:
+            _vector(t, N, given.dtype, device, name)
+    return _dtype(given)
+
+
+def _out_matrix(t, like, rows, cols, dtype, device, name):
+    """An output of the caller's, checked, or a new one; and its leading dimension."""
+    if t is None:
+        return like.new_empty((rows, cols), dtype=dtype), cols
+    return t, _matrix(t, rows, cols, dtype, device, name)
+
+
+def _out_vector(t, like, n, dtype, device, name):
+    if t is None:
+        return like.new_empty((n,), dtype=dtype)
+    _vector(t, n, dtype, device, name)
+    return t
 
 
 def atb_layer_norm(X, W=None, B=None, eps=1e-5, Y=None, mean=None, rstd=None, stream=None):
@@ -432,50 +458,33 @@ def atb_layer_norm(X, W=None, B=None, eps=1e-5, Y=None, mean=None, rstd=None, st
 
     Returns ``(Y, mean, rstd)``: the result in X's type and the float32 statistics that the backward pass takes."""
     import torch
-    if X.dim() != 2:
-        raise ValueError("X: a matrix")
-    M, N = X.shape
-    ldx = _matrix(X, M, N, X.dtype, "X")
-    w_type, _ = _norm_weights(W, B, N, X.dtype)
-    if Y is None:
-        Y = torch.empty((M, N), dtype=X.dtype, device=X.device)
-    ldy = _matrix(Y, M, N, X.dtype, "Y")
-    if mean is None:
-        mean = torch.empty(M, dtype=torch.float32, device=X.device)
-    if rstd is None:
-        rstd = torch.empty(M, dtype=torch.float32, device=X.device)
-    _vector(mean, M, torch.float32, "mean")
-    _vector(rstd, M, torch.float32, "rstd")
+    device = _device_of(X, "X")
+    (M, N), dtype = X.shape, X.dtype
+    ldx = _matrix(X, M, N, dtype, device, "X")
+    w_type = _norm_weights(W, B, N, dtype, device)
+    Y, ldy = _out_matrix(Y, X, M, N, dtype, device, "Y")
+    mean = _out_vector(mean, X, M, torch.float32, device, "mean")
+    rstd = _out_vector(rstd, X, M, torch.float32, device, "rstd")
     _check(load_library().atb_layer_norm(M, N, _dtype(X), X.data_ptr(), ldx, w_type, _opt_ptr(W), _opt_ptr(B), eps, Y.data_ptr(), ldy,
-                                         mean.data_ptr(), rstd.data_ptr(), _on_stream(X.device, stream)))
+                                         mean.data_ptr(), rstd.data_ptr(), _stream_ptr(stream)))
     return Y, mean, rstd
 
 
 def atb_layer_norm_bfp16(X, W=None, B=None, eps=1e-5, mant=None, exp=None, mean=None, rstd=None, stream=None):
     """Layer norm that leaves as BFP16 planes, the A operand of ``atb_gemm``.  Returns ``(mant, exp, mean, rstd)``."""
     import torch
-    if X.dim() != 2:
-        raise ValueError("X: a matrix")
-    M, N = X.shape
-    ldx = _matrix(X, M, N, X.dtype, "X")
-    w_type, _ = _norm_weights(W, B, N, X.dtype)
-    if mant is None:
-        mant = torch.empty((M, N), dtype=torch.int8, device=X.device)
-    if exp is None:
-        exp = torch.empty(atb_bfp16_exp_bytes(M, N), dtype=torch.uint8, device=X.device)
-    if not mant.is_contiguous():
+    device = _device_of(X, "X")
+    (M, N), dtype = X.shape, X.dtype
+    ldx = _matrix(X, M, N, dtype, device, "X")
+    w_type = _norm_weights(W, B, N, dtype, device)
+    mant, ldm = _out_matrix(mant, X, M, N, torch.int8, device, "mant")
+    if ldm != N:
         raise ValueError("mant: contiguous")
-    _matrix(mant, M, N, torch.int8, "mant")
-    _vector(exp, atb_bfp16_exp_bytes(M, N), torch.uint8, "exp")
-    if mean is None:
-        mean = torch.empty(M, dtype=torch.float32, device=X.device)
-    if rstd is None:
-        rstd = torch.empty(M, dtype=torch.float32, device=X.device)
-    _vector(mean, M, torch.float32, "mean")
-    _vector(rstd, M, torch.float32, "rstd")
+    exp = _out_vector(exp, X, atb_bfp16_exp_bytes(M, N), torch.uint8, device, "exp")
+    mean = _out_vector(mean, X, M, torch.float32, device, "mean")
+    rstd = _out_vector(rstd, X, M, torch.float32, device, "rstd")
     _check(load_library().atb_layer_norm_bfp16(M, N, _dtype(X), X.data_ptr(), ldx, w_type, _opt_ptr(W), _opt_ptr(B), eps,
-                                               mant.data_ptr(), exp.data_ptr(), mean.data_ptr(), rstd.data_ptr(),
-                                               _on_stream(X.device, stream)))
+                                               mant.data_ptr(), exp.data_ptr(), mean.data_ptr(), rstd.data_ptr(), _stream_ptr(stream)))
     return mant, exp, mean, rstd
 
 
@@ -486,42 +495,43 @@ def atb_layer_norm_backward_workspace_bytes(M: int, N: int) -> int:
 def atb_layer_norm_backward(dY, X, W, mean, rstd, dX=None, dW=None, dB=None, workspace=None, stream=None):
     """Gradients ``(dX, dW, dB)`` of ``atb_layer_norm``; dW and dB in W's type (float32 where W is None)."""
     import torch
-    if X.dim() != 2:
-        raise ValueError("X: a matrix")
-    M, N = X.shape
-    ldx = _matrix(X, M, N, X.dtype, "X")
-    lddy = _matrix(dY, M, N, X.dtype, "dY")
-    w_dtype = torch.float32 if W is None else W.dtype
-    _vector(W, N, w_dtype, "W")
-    _vector(mean, M, torch.float32, "mean")
-    _vector(rstd, M, torch.float32, "rstd")
-    if dX is None:
-        dX = torch.empty((M, N), dtype=X.dtype, device=X.device)
-    if dW is None:
-        dW = torch.empty(N, dtype=w_dtype, device=X.device)
-    if dB is None:
-        dB = torch.empty(N, dtype=w_dtype, device=X.device)
-    lddx = _matrix(dX, M, N, X.dtype, "dX")
-    _vector(dW, N, w_dtype, "dW")
-    _vector(dB, N, w_dtype, "dB")
+    device = _device_of(X, "X")
+    (M, N), dtype = X.shape, X.dtype
+    ldx = _matrix(X, M, N, dtype, device, "X")
+    lddy = _matrix(dY, M, N, dtype, device, "dY")
+    w_dtype = torch.float32
+    if W is not None:
+        w_dtype = W.dtype
+        _vector(W, N, w_dtype, device, "W")
+    _vector(mean, M, torch.float32, device, "mean")
+    _vector(rstd, M, torch.float32, device, "rstd")
+    dX, lddx = _out_matrix(dX, X, M, N, dtype, device, "dX")
+    dW = _out_vector(dW, X, N, w_dtype, device, "dW")
+    dB = _out_vector(dB, X, N, w_dtype, device, "dB")
     lib = load_library()
-    ws, ws_bytes, workspace = _workspace(workspace, lib.atb_layer_norm_backward_workspace_bytes(M, N), X.device)
+    ws, ws_bytes, workspace = _workspace(workspace, lib.atb_layer_norm_backward_workspace_bytes(M, N), X)
     _check(lib.atb_layer_norm_backward(M, N, _dtype(X), dY.data_ptr(), lddy, X.data_ptr(), ldx, _dtype(dW), _opt_ptr(W), mean.data_ptr(),
-                                       rstd.data_ptr(), dX.data_ptr(), lddx, dW.data_ptr(), dB.data_ptr(), ws, ws_bytes,
-                                       _on_stream(X.device, stream)))
+                                       rstd.data_ptr(), dX.data_ptr(), lddx, dW.data_ptr(), dB.data_ptr(), ws, ws_bytes, _stream_ptr(stream)))
     return dX, dW, dB
 
 
 def _ffn_shapes(X, Wg, Wu, Wd):
     import torch
-    if X.dim() != 2 or Wg.dim() != 2:
-        raise ValueError("X, Wg: matrices")
-    (M, D), F = X.shape, Wg.shape[1]
-    bf16 = torch.bfloat16
-    ldx, ldw, ldwd = _matrix(X, M, D, bf16, "X"), _matrix(Wg, D, F, bf16, "Wg"), _matrix(Wd, F, D, bf16, "Wd")
-    if _matrix(Wu, D, F, bf16, "Wu") != ldw:
+    device, bf16 = _device_of(X, "X"), torch.bfloat16
+    (M, D), F = X.shape, Wd.shape[0]
+    ldx, ldw, ldwd = _matrix(X, M, D, bf16, device, "X"), _matrix(Wg, D, F, bf16, device, "Wg"), _matrix(Wd, F, D, bf16, device, "Wd")
+    if _matrix(Wu, D, F, bf16, device, "Wu") != ldw:
         raise ValueError("Wg and Wu need the same row stride")
-    return M, D, F, ldx, ldw, ldwd
+    return M, D, F, ldx, ldw, ldwd, device
+
+
+def _hidden(t, like, M, F, device, name):
+    """H, G or U: the caller's, contiguous, or a new one."""
+    import torch
+    t, ld = _out_matrix(t, like, M, F, torch.bfloat16, device, name)
+    if ld != F:
+        raise ValueError(f"{name}: contiguous")
+    return t
 
 
 def _act(act):
@@ -537,23 +547,15 @@ def atb_gated_ffn(X, Wg, Wu, Wd, act="silu", save=False, Y=None, H=None, G=None,
 
     ``act``: "silu", "gelu" or "gelu_tanh".  Returns Y, or with ``save`` ``(Y, H, G, U)``: what the backward pass takes."""
     import torch
-    M, D, F, ldx, ldw, ldwd = _ffn_shapes(X, Wg, Wu, Wd)
-    bf16 = torch.bfloat16
-    if Y is None:
-        Y = torch.empty((M, D), dtype=bf16, device=X.device)
-    if H is None:
-        H = torch.empty((M, F), dtype=bf16, device=X.device)
-    if save:
-        G = torch.empty((M, F), dtype=bf16, device=X.device) if G is None else G
-        U = torch.empty((M, F), dtype=bf16, device=X.device) if U is None else U
-    ldy = _matrix(Y, M, D, bf16, "Y")
-    for t, name in ((H, "H"), (G, "G"), (U, "U")):
-        if t is not None and (_matrix(t, M, F, bf16, name) != F):
-            raise ValueError(f"{name}: contiguous")
+    M, D, F, ldx, ldw, ldwd, device = _ffn_shapes(X, Wg, Wu, Wd)
+    Y, ldy = _out_matrix(Y, X, M, D, torch.bfloat16, device, "Y")
+    H = _hidden(H, X, M, F, device, "H")
+    if save or G is not None or U is not None:
+        G, U = _hidden(G, X, M, F, device, "G"), _hidden(U, X, M, F, device, "U")
     lib = load_library()
-    ws, ws_bytes, workspace = _workspace(workspace, lib.atb_gated_ffn_workspace_bytes(M, D, F), X.device)
+    ws, ws_bytes, workspace = _workspace(workspace, lib.atb_gated_ffn_workspace_bytes(M, D, F), X)
     _check(lib.atb_gated_ffn(M, D, F, _act(act), X.data_ptr(), ldx, Wg.data_ptr(), Wu.data_ptr(), ldw, Wd.data_ptr(), ldwd, Y.data_ptr(), ldy,
-                             H.data_ptr(), _opt_ptr(G), _opt_ptr(U), ws, ws_bytes, _on_stream(X.device, stream)))
+                             H.data_ptr(), _opt_ptr(G), _opt_ptr(U), ws, ws_bytes, _stream_ptr(stream)))
     return (Y, H, G, U) if save else Y
 
 
@@ -564,39 +566,33 @@ def atb_gated_ffn_backward_workspace_bytes(M: int, D: int, F: int) -> int:
 def atb_gated_ffn_backward(dY, X, Wg, Wu, Wd, H, G, U, act="silu", dX=None, dWg=None, dWu=None, dWd=None, workspace=None, stream=None):
     """Gradients ``(dX, dWg, dWu, dWd)`` of ``atb_gated_ffn`` from ``dY`` and the ``H``, ``G``, ``U`` that it saved."""
     import torch
-    M, D, F, ldx, ldw, ldwd = _ffn_shapes(X, Wg, Wu, Wd)
+    M, D, F, ldx, ldw, ldwd, device = _ffn_shapes(X, Wg, Wu, Wd)
     bf16 = torch.bfloat16
-    lddy = _matrix(dY, M, D, bf16, "dY")
+    lddy = _matrix(dY, M, D, bf16, device, "dY")
     for t, name in ((H, "H"), (G, "G"), (U, "U")):
-        if _matrix(t, M, F, bf16, name) != F:
+        if _matrix(t, M, F, bf16, device, name) != F:
             raise ValueError(f"{name}: contiguous")
-    if dX is None:
-        dX = torch.empty((M, D), dtype=bf16, device=X.device)
-    if dWg is None:
-        dWg = torch.empty((D, F), dtype=bf16, device=X.device)
-    if dWu is None:
-        dWu = torch.empty((D, F), dtype=bf16, device=X.device)
-    if dWd is None:
-        dWd = torch.empty((F, D), dtype=bf16, device=X.device)
-    lddx, lddw, lddwd = _matrix(dX, M, D, bf16, "dX"), _matrix(dWg, D, F, bf16, "dWg"), _matrix(dWd, F, D, bf16, "dWd")
-    if _matrix(dWu, D, F, bf16, "dWu") != lddw:
+    dX, lddx = _out_matrix(dX, X, M, D, bf16, device, "dX")
+    dWg, lddw = _out_matrix(dWg, X, D, F, bf16, device, "dWg")
+    dWu, lddu = _out_matrix(dWu, X, D, F, bf16, device, "dWu")
+    dWd, lddwd = _out_matrix(dWd, X, F, D, bf16, device, "dWd")
+    if lddu != lddw:
         raise ValueError("dWg and dWu need the same row stride")
     lib = load_library()
-    ws, ws_bytes, workspace = _workspace(workspace, lib.atb_gated_ffn_backward_workspace_bytes(M, D, F), X.device)
+    ws, ws_bytes, workspace = _workspace(workspace, lib.atb_gated_ffn_backward_workspace_bytes(M, D, F), X)
     _check(lib.atb_gated_ffn_backward(M, D, F, _act(act), dY.data_ptr(), lddy, X.data_ptr(), ldx, Wg.data_ptr(), Wu.data_ptr(), ldw,
                                       Wd.data_ptr(), ldwd, H.data_ptr(), G.data_ptr(), U.data_ptr(), dX.data_ptr(), lddx, dWg.data_ptr(),
-                                      dWu.data_ptr(), lddw, dWd.data_ptr(), lddwd, ws, ws_bytes, _on_stream(X.device, stream)))
+                                      dWu.data_ptr(), lddw, dWd.data_ptr(), lddwd, ws, ws_bytes, _stream_ptr(stream)))
     return dX, dWg, dWu, dWd
 
 
 def _head_shapes(X, W, labels):
     import torch
-    if X.dim() != 2 or W.dim() != 2:
-        raise ValueError("X, W: matrices")
+    device = _device_of(X, "X")
     (M, D), V = X.shape, W.shape[0]
-    ldx, ldw = _matrix(X, M, D, torch.bfloat16, "X"), _matrix(W, V, D, torch.bfloat16, "W")
-    _vector(labels, M, torch.int64, "labels")
-    return M, V, D, ldx, ldw
+    ldx, ldw = _matrix(X, M, D, torch.bfloat16, device, "X"), _matrix(W, V, D, torch.bfloat16, device, "W")
+    _vector(labels, M, torch.int64, device, "labels")
+    return M, V, D, ldx, ldw, device
 
 
 def atb_linear_cross_entropy_workspace_bytes(M: int, V: int, D: int) -> int:
@@ -608,17 +604,13 @@ def atb_linear_cross_entropy(X, W, labels, ignore_index=-100, loss=None, lse=Non
 
     Returns float32 ``(loss, lse)``, ``[M]`` each; rows whose label is ``ignore_index`` have loss 0."""
     import torch
-    M, V, D, ldx, ldw = _head_shapes(X, W, labels)
-    if loss is None:
-        loss = torch.empty(M, dtype=torch.float32, device=X.device)
-    if lse is None:
-        lse = torch.empty(M, dtype=torch.float32, device=X.device)
-    _vector(loss, M, torch.float32, "loss")
-    _vector(lse, M, torch.float32, "lse")
+    M, V, D, ldx, ldw, device = _head_shapes(X, W, labels)
+    loss = _out_vector(loss, X, M, torch.float32, device, "loss")
+    lse = _out_vector(lse, X, M, torch.float32, device, "lse")
     lib = load_library()
-    ws, ws_bytes, workspace = _workspace(workspace, lib.atb_linear_cross_entropy_workspace_bytes(M, V, D), X.device)
+    ws, ws_bytes, workspace = _workspace(workspace, lib.atb_linear_cross_entropy_workspace_bytes(M, V, D), X)
     _check(lib.atb_linear_cross_entropy(M, V, D, X.data_ptr(), ldx, W.data_ptr(), ldw, labels.data_ptr(), ignore_index, loss.data_ptr(),
-                                        lse.data_ptr(), ws, ws_bytes, _on_stream(X.device, stream)))
+                                        lse.data_ptr(), ws, ws_bytes, _stream_ptr(stream)))
     return loss, lse
 
 
@@ -629,19 +621,16 @@ def atb_linear_cross_entropy_backward_workspace_bytes(M: int, V: int, D: int, pi
 def atb_linear_cross_entropy_backward(dloss, X, W, labels, lse, ignore_index=-100, dX=None, dW=None, piece=0, workspace=None, stream=None):
     """Gradients ``(dX, dW)`` (bfloat16) of ``sum(dloss * loss)``; ``piece``: words of the vocabulary per pass (0: chosen)."""
     import torch
-    M, V, D, ldx, ldw = _head_shapes(X, W, labels)
-    _vector(dloss, M, torch.float32, "dloss")
-    _vector(lse, M, torch.float32, "lse")
-    if dX is None:
-        dX = torch.empty((M, D), dtype=torch.bfloat16, device=X.device)
-    if dW is None:
-        dW = torch.empty((V, D), dtype=torch.bfloat16, device=X.device)
-    lddx, lddw = _matrix(dX, M, D, torch.bfloat16, "dX"), _matrix(dW, V, D, torch.bfloat16, "dW")
+    M, V, D, ldx, ldw, device = _head_shapes(X, W, labels)
+    _vector(dloss, M, torch.float32, device, "dloss")
+    _vector(lse, M, torch.float32, device, "lse")
+    dX, lddx = _out_matrix(dX, X, M, D, torch.bfloat16, device, "dX")
+    dW, lddw = _out_matrix(dW, X, V, D, torch.bfloat16, device, "dW")
     lib = load_library()
-    ws, ws_bytes, workspace = _workspace(workspace, lib.atb_linear_cross_entropy_backward_workspace_bytes(M, V, D, piece), X.device)
+    ws, ws_bytes, workspace = _workspace(workspace, lib.atb_linear_cross_entropy_backward_workspace_bytes(M, V, D, piece), X)
     _check(lib.atb_linear_cross_entropy_backward(M, V, D, X.data_ptr(), ldx, W.data_ptr(), ldw, labels.data_ptr(), ignore_index,
                                                  lse.data_ptr(), dloss.data_ptr(), dX.data_ptr(), lddx, dW.data_ptr(), lddw, piece, ws, ws_bytes,
-                                                 _on_stream(X.device, stream)))
+                                                 _stream_ptr(stream)))
     return dX, dW
 
 

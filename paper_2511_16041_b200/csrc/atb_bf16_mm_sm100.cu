@@ -11,6 +11,7 @@
 //   pair    256 x 256 tile: each CTA loads its 128 rows of A and half of the columns of B and holds 128 x 256 of C
 //   single  128 x 128 tile: four times as many tiles for outputs that would leave most of the SMs idle
 // Every wait is bounded (see atb_gemm_device.cuh).
+#include <atomic>
 #include <type_traits>
 
 #include "atb_bf16_mm.h"
@@ -493,7 +494,7 @@ bf16_mm_kernel(const __grid_constant__ MmMaps tm, const MmParams p) {
 // ------------------------------------------------------------------------------------------ host
 struct MmDevice {
     bool known = false;
-    int major = 0, minor = 0, sms = 0;
+    int ordinal = 0, major = 0, minor = 0, sms = 0;
     unsigned int* flag = nullptr;
 };
 MmDevice g_mm_devices[64];
@@ -633,25 +634,28 @@ cudaError_t launch_dependent(void (*kernel)(Args...), unsigned grid, unsigned bl
 
 // splits > 1: EPI is kMmAccumulate and the sums of the ranges go to q.partial.
 template <bool PAIR, bool A_MN, bool B_MN, int EPI>
-atb_status_t launch(const atb::MmProblem& q, int splits, int sms, unsigned int* flag, cudaStream_t stream) {
+atb_status_t launch(const atb::MmProblem& q, int splits, const MmDevice& dev, cudaStream_t stream) {
     using C = MmCfg<PAIR, EPI>;
     MmMaps tm;
     MmParams p = {};
     const int n_segs = C::DUAL ? 1 : (q.epilogue == atb::kMmGlu ? 2 : q.n_segs);     // a split gated product: two side by side
     const int n_b = C::DUAL || n_segs == 2 ? 2 : q.k_segs;
-    for (int i = 0; i < 2; ++i) {
-        if (!operand_map(&tm.a[i], q.A[i < q.k_segs ? i : 0], A_MN, q.M, q.K) || !operand_map(&tm.b[i], q.B[i < n_b ? i : 0], B_MN, q.N, q.K))
-            return atb::fail(ATB_ERR_CUDA, "cuTensorMapEncodeTiled failed for an operand");
+    for (int i = 0; i < 2; ++i) {        // a map that is not used is a copy of the first
+        if (i >= q.k_segs) tm.a[i] = tm.a[0];
+        else if (!operand_map(&tm.a[i], q.A[i], A_MN, q.M, q.K)) return atb::fail(ATB_ERR_CUDA, "cuTensorMapEncodeTiled failed for A");
+        if (i >= n_b) tm.b[i] = tm.b[0];
+        else if (!operand_map(&tm.b[i], q.B[i], B_MN, q.N, q.K)) return atb::fail(ATB_ERR_CUDA, "cuTensorMapEncodeTiled failed for B");
     }
     if constexpr (EPI == atb::kMmAccumulate) {
         float* const base = splits > 1 ? q.partial : q.C32;
         p.split_rows = splits > 1 ? atb::round_up(q.M, 32) : 0;
         p.add = splits > 1 ? 0 : !q.first;
-        for (int i = 0; i < 2; ++i)      // a map per segment, so that each clips at its own last column
-            if (!make_map_2d(&tm.c[i], CU_TENSOR_MAP_DATA_TYPE_FLOAT32, 4, base + (i < n_segs ? i * q.N : 0), static_cast<uint64_t>(q.N),
+        for (int i = 0; i < n_segs; ++i)      // a map per segment, so that each clips at its own last column
+            if (!make_map_2d(&tm.c[i], CU_TENSOR_MAP_DATA_TYPE_FLOAT32, 4, base + i * q.N, static_cast<uint64_t>(q.N),
                              static_cast<uint64_t>(splits > 1 ? splits * p.split_rows : q.M), static_cast<uint64_t>(q.N * n_segs) * 4, 32, 32,
                              CU_TENSOR_MAP_SWIZZLE_128B))
                 return atb::fail(ATB_ERR_CUDA, "cuTensorMapEncodeTiled failed for the FP32 output");
+        if (n_segs == 1) tm.c[1] = tm.c[0];
         tm.c[2] = tm.c[0];
     } else {
         for (int i = 0; i < 3; ++i) {
@@ -668,7 +672,7 @@ atb_status_t launch(const atb::MmProblem& q, int splits, int sms, unsigned int* 
     p.k_steps0 = static_cast<int>(atb::ceil_div(q.K, kMmKStep));
     p.k_steps = p.k_steps0 * q.k_segs;
     p.splits = splits;
-    p.error_flag = flag;
+    p.error_flag = dev.flag;
     p.act = q.act; p.save = q.C[1] != nullptr;
     p.G = static_cast<const __nv_bfloat16*>(q.G); p.U = static_cast<const __nv_bfloat16*>(q.U);
     p.labels = q.labels; p.ignore_index = q.ignore_index; p.col0 = q.col0;
@@ -676,27 +680,33 @@ atb_status_t launch(const atb::MmProblem& q, int splits, int sms, unsigned int* 
     p.lse = q.lse; p.scale = q.scale;
     const int64_t items = static_cast<int64_t>(p.m_tiles) * p.n_tiles * p.n_segs * splits;
     if (items > (1ll << 30)) return atb::fail(ATB_ERR_BAD_SHAPE, "too many output tiles");
-    const int units = PAIR ? sms / 2 : sms;
+    const int units = PAIR ? dev.sms / 2 : dev.sms;
     const int n_units = static_cast<int>(items < units ? items : units);
     auto kernel = bf16_mm_kernel<PAIR, A_MN, B_MN, EPI>;
-    cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(C::SMEM_BYTES));
-    if (e != cudaSuccess) return atb::fail(ATB_ERR_CUDA, "cudaFuncSetAttribute: %s", cudaGetErrorString(e));
+    cudaError_t e = cudaSuccess;
+    static std::atomic<uint64_t> allowed{0};         // devices on which this kernel has its shared memory allowed
+    const uint64_t bit = 1ull << dev.ordinal;
+    if (!(allowed.load(std::memory_order_acquire) & bit)) {
+        e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(C::SMEM_BYTES));
+        if (e != cudaSuccess) return atb::fail(ATB_ERR_CUDA, "cudaFuncSetAttribute: %s", cudaGetErrorString(e));
+        allowed.fetch_or(bit, std::memory_order_release);
+    }
     e = launch_dependent(kernel, static_cast<unsigned>(PAIR ? 2 * n_units : n_units), kMmThreads, PAIR ? 2u : 1u, C::SMEM_BYTES, stream, tm, p);
     if (e != cudaSuccess) return atb::fail(ATB_ERR_CUDA, "bf16 product launch: %s", cudaGetErrorString(e));
     return ATB_OK;
 }
 
 template <bool A_MN, bool B_MN, int EPI>
-atb_status_t run(const atb::MmProblem& q, int sms, unsigned int* flag, cudaStream_t stream) {
+atb_status_t run(const atb::MmProblem& q, const MmDevice& dev, cudaStream_t stream) {
     const MmPlan plan = plan_of(q);
     if constexpr (EPI == atb::kMmRowStats || EPI == atb::kMmDlogits) {
-        return plan.pair ? launch<true, A_MN, B_MN, EPI>(q, 1, sms, flag, stream) : launch<false, A_MN, B_MN, EPI>(q, 1, sms, flag, stream);
+        return plan.pair ? launch<true, A_MN, B_MN, EPI>(q, 1, dev, stream) : launch<false, A_MN, B_MN, EPI>(q, 1, dev, stream);
     } else {
         if (plan.splits == 1)
-            return plan.pair ? launch<true, A_MN, B_MN, EPI>(q, 1, sms, flag, stream) : launch<false, A_MN, B_MN, EPI>(q, 1, sms, flag, stream);
+            return plan.pair ? launch<true, A_MN, B_MN, EPI>(q, 1, dev, stream) : launch<false, A_MN, B_MN, EPI>(q, 1, dev, stream);
         if (!q.partial) return atb::fail(ATB_ERR_NULL_POINTER, "a product that is split along K needs room for its sums");
-        const atb_status_t s = plan.pair ? launch<true, A_MN, B_MN, atb::kMmAccumulate>(q, plan.splits, sms, flag, stream)
-                                         : launch<false, A_MN, B_MN, atb::kMmAccumulate>(q, plan.splits, sms, flag, stream);
+        const atb_status_t s = plan.pair ? launch<true, A_MN, B_MN, atb::kMmAccumulate>(q, plan.splits, dev, stream)
+                                         : launch<false, A_MN, B_MN, atb::kMmAccumulate>(q, plan.splits, dev, stream);
         if (s != ATB_OK) return s;
         MmJoin j = {};
         j.M = q.M; j.N = q.N; j.n_segs = EPI == atb::kMmGlu ? 1 : q.n_segs;
@@ -706,7 +716,7 @@ atb_status_t run(const atb::MmProblem& q, int sms, unsigned int* flag, cudaStrea
         j.C32 = q.C32; j.add = !q.first;
         j.act = q.act;
         j.G = static_cast<const __nv_bfloat16*>(q.G); j.U = static_cast<const __nv_bfloat16*>(q.U);
-        const int64_t blocks = atb::ceil_div(j.M * (j.N / 8) * j.n_segs, 256), most = static_cast<int64_t>(sms) * 8;
+        const int64_t blocks = atb::ceil_div(j.M * (j.N / 8) * j.n_segs, 256), most = static_cast<int64_t>(dev.sms) * 8;
         const cudaError_t e = launch_dependent(bf16_mm_join_kernel<EPI>, static_cast<unsigned>(blocks < most ? blocks : most), 256u, 1u, 0, stream, j);
         if (e != cudaSuccess) return atb::fail(ATB_ERR_CUDA, "bf16 product join launch: %s", cudaGetErrorString(e));
         return ATB_OK;
@@ -717,7 +727,7 @@ atb_status_t run(const atb::MmProblem& q, int sms, unsigned int* flag, cudaStrea
 
 namespace atb {
 
-atb_status_t op_device(int* num_sms, unsigned int** mm_error_flag) {
+static atb_status_t mm_device(const MmDevice** out) {
     int dev = 0;
     cudaError_t e = cudaGetDevice(&dev);
     if (e != cudaSuccess) return fail(ATB_ERR_CUDA, "cudaGetDevice: %s", cudaGetErrorString(e));
@@ -725,6 +735,7 @@ atb_status_t op_device(int* num_sms, unsigned int** mm_error_flag) {
     std::lock_guard<std::mutex> lock(g_mm_mutex);
     MmDevice& d = g_mm_devices[dev];
     if (!d.known) {
+        d.ordinal = dev;
         cudaDeviceGetAttribute(&d.major, cudaDevAttrComputeCapabilityMajor, dev);
         cudaDeviceGetAttribute(&d.minor, cudaDevAttrComputeCapabilityMinor, dev);
         cudaDeviceGetAttribute(&d.sms, cudaDevAttrMultiProcessorCount, dev);
@@ -736,9 +747,15 @@ atb_status_t op_device(int* num_sms, unsigned int** mm_error_flag) {
     }
     if (d.major != 10 || d.minor != 0)
         return fail(ATB_ERR_UNSUPPORTED_DEVICE, "compute capability %d.%d; this library runs on 10.0 only", d.major, d.minor);
-    *num_sms = d.sms;
-    if (mm_error_flag) *mm_error_flag = d.flag;
+    *out = &d;
     return ATB_OK;
+}
+
+atb_status_t op_device(int* num_sms) {
+    const MmDevice* d = nullptr;
+    const atb_status_t s = mm_device(&d);
+    if (s == ATB_OK) *num_sms = d->sms;
+    return s;
 }
 
 unsigned int take_mm_error_flag() {
@@ -762,12 +779,11 @@ size_t mm_partial_bytes(MmEpilogue epilogue, int64_t M, int64_t N, int64_t K, in
 }
 
 atb_status_t mm_launch(const MmProblem& q, cudaStream_t stream) {
-    int sms = 0;
-    unsigned int* flag = nullptr;
-    atb_status_t s = op_device(&sms, &flag);
+    const MmDevice* dev = nullptr;
+    const atb_status_t s = mm_device(&dev);
     if (s != ATB_OK) return s;
 #define ATB_MM_CASE(LAYOUT, EPI, A_MN, B_MN) \
-    if (q.layout == LAYOUT && q.epilogue == EPI) return run<A_MN, B_MN, EPI>(q, sms, flag, stream);
+    if (q.layout == LAYOUT && q.epilogue == EPI) return run<A_MN, B_MN, EPI>(q, *dev, stream);
     ATB_MM_CASE(kMmNN, kMmStore, false, true)
     ATB_MM_CASE(kMmNN, kMmGlu, false, true)
     ATB_MM_CASE(kMmNN, kMmAccumulate, false, true)

@@ -106,7 +106,7 @@ extern "C" atb_status_t atb_gated_ffn_backward(int64_t M, int64_t D, int64_t F, 
     cudaStream_t st = static_cast<cudaStream_t>(stream);
     if (M == 0) {          // no rows: the sums over them are 0
         int sms = 0;
-        s = atb::op_device(&sms, nullptr);
+        s = atb::op_device(&sms);
         if (s != ATB_OK) return s;
         cudaError_t e = cudaSuccess;
         if (dWg_dev) e = cudaMemset2DAsync(dWg_dev, lddw * 2, 0, F * 2, D, st);

@@ -52,9 +52,8 @@ constexpr int slab_bundle(int spg, int n_raw, int groups) {
     return b;
 }
 
-// The current device's SM count and, where wanted, the address of the timeout flag of the BF16 product kernels;
-// ATB_ERR_UNSUPPORTED_DEVICE unless it has compute capability 10.0.
-atb_status_t op_device(int* num_sms, unsigned int** mm_error_flag);
+// The current device's SM count; ATB_ERR_UNSUPPORTED_DEVICE unless it has compute capability 10.0.
+atb_status_t op_device(int* num_sms);
 // SMs of the device the library is written for: what plans that fix a workspace's layout count with, so that the
 // sizes are known on hosts without one.
 constexpr int kSmCount = 148;

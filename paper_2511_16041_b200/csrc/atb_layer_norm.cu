@@ -481,7 +481,7 @@ atb_status_t forward(int64_t M, int64_t N, int x_type, const void* X, int64_t ld
     if (exp && (!vec || !atb::aligned16(Y) || !atb::aligned16(exp)))
         return atb::fail(ATB_ERR_MISALIGNED, "BFP16 output needs 16-byte aligned pointers and rows of X");
     int sms = 0;
-    s = atb::op_device(&sms, nullptr);
+    s = atb::op_device(&sms);
     if (s != ATB_OK) return s;
     FwdParams p{M, N, ldx, ldy, exp ? atb::round_up(M, 32) : M, X, W, B, eps, Y, exp, mean, rstd};
     cudaStream_t st = static_cast<cudaStream_t>(stream);
@@ -543,7 +543,7 @@ extern "C" atb_status_t atb_layer_norm_backward(int64_t M, int64_t N, int x_type
         return atb::fail(ATB_ERR_BUFFER_TOO_SMALL, "workspace of %zu bytes is smaller than the %zu needed", workspace_bytes,
                          atb_layer_norm_backward_workspace_bytes(M, N));
     int sms = 0;
-    s = atb::op_device(&sms, nullptr);
+    s = atb::op_device(&sms);
     if (s != ATB_OK) return s;
     BwdParams p{M, N, lddy, ldx, lddx, dY_dev, X_dev, W_dev, mean_dev, rstd_dev, dX_dev, sums ? static_cast<float*>(workspace_dev) : nullptr};
     cudaStream_t st = static_cast<cudaStream_t>(stream);

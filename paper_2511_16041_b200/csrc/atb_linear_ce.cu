@@ -161,7 +161,7 @@ extern "C" atb_status_t atb_linear_cross_entropy_backward(int64_t M, int64_t V, 
     if (workspace_bytes < need) return atb::fail(ATB_ERR_BUFFER_TOO_SMALL, "workspace of %zu bytes is smaller than the %zu needed", workspace_bytes, need);
     cudaStream_t st = static_cast<cudaStream_t>(stream);
     int sms = 0;
-    s = atb::op_device(&sms, nullptr);
+    s = atb::op_device(&sms);
     if (s != ATB_OK) return s;
     if (M == 0) {
         const cudaError_t e = dW_dev ? cudaMemset2DAsync(dW_dev, lddw * 2, 0, D * 2, V, st) : cudaSuccess;
