@@ -11,6 +11,7 @@
 #include <algorithm>
 
 #include "atb_bf16_mm.h"
+#include "atb_few_rows.h"
 
 namespace {
 
@@ -34,7 +35,7 @@ size_t glu_gradient_bytes(int64_t M, int64_t F) { return (4 * static_cast<size_t
 }  // namespace
 
 extern "C" size_t atb_gated_ffn_workspace_bytes(int64_t M, int64_t D, int64_t F) {
-    if (M < 1 || D < 1 || F < 1) return 0;
+    if (M <= atb::kFewRows || D < 1 || F < 1) return 0;
     // the sums of a product that is split along K; the two products take turns
     return std::max(atb::mm_partial_bytes(atb::kMmGlu, M, F, D), atb::mm_partial_bytes(atb::kMmStore, M, D, F));
 }
@@ -58,6 +59,10 @@ extern "C" atb_status_t atb_gated_ffn(int64_t M, int64_t D, int64_t F, int act, 
     if (workspace_bytes < need) return atb::fail(ATB_ERR_BUFFER_TOO_SMALL, "workspace of %zu bytes is smaller than the %zu needed", workspace_bytes, need);
     cudaStream_t st = static_cast<cudaStream_t>(stream);
 
+    if (M <= atb::kFewRows) {
+        s = atb::few_rows_glu(M, D, F, act, X_dev, ldx, Wg_dev, Wu_dev, ldw, H_dev, G_dev, U_dev, st);
+        return s != ATB_OK ? s : atb::few_rows_product(M, F, D, H_dev, F, Wd_dev, ldwd, Y_dev, ldy, true, st);
+    }
     atb::MmProblem up;
     up.layout = atb::kMmNN; up.epilogue = atb::kMmGlu;
     up.M = M; up.N = F; up.K = D; up.act = act;
