@@ -4,26 +4,38 @@
 //   g = dy w,  dx = r (g - sum(g) / N - z sum(g z) / N),  dw = sum over rows of dy z,  db = sum over rows of dy
 //
 // Bound by memory: the forward pass reads x and writes y, the backward pass reads dy and x and writes dx, and
-// nothing else of that size moves.  A row stays in the registers of the threads that share it (TPR threads, up to
-// kFwdElems or kBwdElems elements each), so that mean, variance and result take one read; the variance is summed around
-// the mean, in a second pass over the registers, since sum(x^2) - N mu^2 loses its digits where |mu| >> sqrt(v).
-// All sums are FP32.  Rows wider than the widest kernel are read again for every sum (*_wide kernels).
-// Backward: a block walks rows blockIdx.x, + gridDim.x, ...; a thread keeps the same columns for all of them
-// and adds dw and db up in registers.  Blocks write their sums to the workspace, a second kernel adds those up in a
-// fixed order: no atomics, the same bits on every call.
+// nothing else of that size moves.  TPR threads share a row, at most kElems elements each, in registers: mean,
+// variance and result take one read.  Blocks stay and walk rows blockIdx.x, + gridDim.x, ...: a thread keeps the same
+// columns, so that w and b are loaded once and dw and db add up in registers, and the next kAhead (3, or 2 of FP32) rows are on their way
+// into shared memory (cp.async) while a row is worked on.  Rows on 16-byte boundaries: a thread copies what it will
+// read itself, so that no barrier is needed.  Other rows are copied in 16-byte pieces all the same, from the boundary below
+// their first element on, and read element by element from there.
+// The variance is summed around means: of a warp's elements around their own mean in registers, and the warps' pairs
+// (mean, sum of squares) joined by sum n_w (mean_w - mu)^2, in one exchange; sum(x^2) - N mu^2 would lose its digits
+// where |mu| >> sqrt(v).  All sums are FP32.  Rows wider than the widest kernel are read again for every sum (*_wide kernels).
+// Blocks write their sums of dw and db to the workspace, a second kernel adds those up in a fixed order: no atomics,
+// the same bits on every call.
 #include <cuda_bf16.h>
 #include <cuda_runtime.h>
 
 #include "atb_internal.h"
 #include "bfp16_block.cuh"
+#include "sm100_ptx.cuh"
 
 namespace {
 
-constexpr int kFwdElems = 32, kBwdElems = 16;     // elements of a row per thread
-constexpr int kMaxBlocks = 296;                   // backward: blocks that walk the rows (2 per SM)
+constexpr int kElems = 16;           // most elements of a row per thread
+template <class T>
+constexpr int kAhead = sizeof(T) == 2 ? 3 : 2;      // rows on their way per block
+
+// Blocks that stay on an SM: about 100 KB of rows on their way in each kernel.
+__host__ __device__ constexpr int blocks_per_sm(int tpr, bool backward) {
+    const int b = tpr == 32 ? 6 : tpr == 128 ? 8 : tpr == 256 ? 4 : tpr == 512 ? 2 : 1;
+    return backward ? (b + 1) / 2 : b;
+}
 
 // ---------------------------------------------------------------------------------- loads and stores
-// VEC consecutive elements as they are in memory, VEC = 8 (16-byte accesses) or 1.
+// VEC consecutive elements as they are in memory: 8 (accesses of 16 bytes) or 1.
 template <class T, int VEC>
 struct Raw {
     uint32_t w[VEC * sizeof(T) / 4];
@@ -35,13 +47,14 @@ struct Raw<__nv_bfloat16, 1> {
 
 template <class T, int VEC>
 __device__ __forceinline__ void load_raw(const T* p, Raw<T, VEC>& r) {
-    if constexpr (VEC == 8) {
+    constexpr int BYTES = static_cast<int>(sizeof(T)) * VEC;
+    if constexpr (BYTES >= 16) {
 #pragma unroll
-        for (int i = 0; i < static_cast<int>(sizeof(T)) / 2; ++i) {
-            const uint4 u = *reinterpret_cast<const uint4*>(reinterpret_cast<const char*>(p) + 16 * i);
+        for (int i = 0; i < BYTES / 16; ++i) {
+            const uint4 u = reinterpret_cast<const uint4*>(p)[i];
             r.w[4 * i] = u.x; r.w[4 * i + 1] = u.y; r.w[4 * i + 2] = u.z; r.w[4 * i + 3] = u.w;
         }
-    } else if constexpr (sizeof(T) == 4) {
+    } else if constexpr (BYTES == 4) {
         r.w[0] = *reinterpret_cast<const uint32_t*>(p);
     } else {
         r.w[0] = *reinterpret_cast<const uint16_t*>(p);
@@ -52,9 +65,9 @@ __device__ __forceinline__ void to_float(const Raw<T, VEC>& r, float (&v)[VEC]) 
     if constexpr (sizeof(T) == 4) {
 #pragma unroll
         for (int i = 0; i < VEC; ++i) v[i] = __uint_as_float(r.w[i]);
-    } else if constexpr (VEC == 8) {
+    } else if constexpr (VEC > 1) {
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
+        for (int i = 0; i < VEC / 2; ++i) {
             v[2 * i] = __uint_as_float(r.w[i] << 16);
             v[2 * i + 1] = __uint_as_float(r.w[i] & 0xFFFF0000u);
         }
@@ -68,19 +81,31 @@ __device__ __forceinline__ void load_f(const T* p, float (&v)[VEC]) {
     load_raw(p, r);
     to_float(r, v);
 }
+// Columns n .. n + VEC - 1 of a vector of N weights, or `none` where there is no vector.
+template <class T, int VEC>
+__device__ __forceinline__ void load_or(const T* p, int64_t n, int64_t N, float none, Raw<T, VEC>& r) {
+    const uint32_t bits = __float_as_uint(none), half = bits >> 16;
+#pragma unroll
+    for (int i = 0; i < static_cast<int>(sizeof(r.w) / sizeof(r.w[0])); ++i) {
+        if constexpr (sizeof(T) == 4) r.w[i] = bits;
+        else if constexpr (VEC == 1) r.w[i] = static_cast<uint16_t>(half);
+        else r.w[i] = half | half << 16;
+    }
+    if (p && n < N) load_raw<T, VEC>(p + n, r);
+}
 template <class T, int VEC>
 __device__ __forceinline__ void store_f(T* p, const float (&v)[VEC]) {
     if constexpr (sizeof(T) == 4) {
-        if constexpr (VEC == 8) {
-            reinterpret_cast<float4*>(p)[0] = make_float4(v[0], v[1], v[2], v[3]);
-            reinterpret_cast<float4*>(p)[1] = make_float4(v[4], v[5], v[6], v[7]);
+        if constexpr (VEC > 1) {
+#pragma unroll
+            for (int i = 0; i < VEC / 4; ++i) reinterpret_cast<float4*>(p)[i] = make_float4(v[4 * i], v[4 * i + 1], v[4 * i + 2], v[4 * i + 3]);
         } else {
             *p = v[0];
         }
-    } else if constexpr (VEC == 8) {
-        uint32_t o[4];
+    } else if constexpr (VEC > 1) {
+        uint32_t o[VEC / 2];
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
+        for (int i = 0; i < VEC / 2; ++i) {
             const __nv_bfloat162 b2 = __floats2bfloat162_rn(v[2 * i], v[2 * i + 1]);
             o[i] = *reinterpret_cast<const uint32_t*>(&b2);
         }
@@ -91,15 +116,19 @@ __device__ __forceinline__ void store_f(T* p, const float (&v)[VEC]) {
 }
 
 // ---------------------------------------------------------------------------------- sums over a row's threads
-// Every thread of the row gets the sum of K values over the TPR threads.  TPR = 32: one warp; else the whole block,
-// through `red`, of which each call of a row takes another slice (a slice is written again only after a
-// barrier that follows its last read).
-template <int TPR, int K>
-__device__ __forceinline__ void row_sum(float (&v)[K], float (*red)[K]) {
+template <int K>
+__device__ __forceinline__ void warp_sum(float (&v)[K]) {
 #pragma unroll
     for (int o = 16; o > 0; o >>= 1)
 #pragma unroll
         for (int k = 0; k < K; ++k) v[k] += __shfl_xor_sync(0xFFFFFFFFu, v[k], o);
+}
+// Every thread of the row gets the sum of K values over the TPR threads.  TPR = 32: one warp; else the whole block,
+// through `red`, of which a row takes another slice than the row before it (a slice is written again only after a
+// barrier that follows its last read).
+template <int TPR, int K>
+__device__ __forceinline__ void row_sum(float (&v)[K], float (*red)[K]) {
+    warp_sum(v);
     if constexpr (TPR > 32) {
         constexpr int W = TPR / 32;
         const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
@@ -117,6 +146,95 @@ __device__ __forceinline__ void row_sum(float (&v)[K], float (*red)[K]) {
     }
 }
 
+// ---------------------------------------------------------------------------------- rows on their way
+__device__ __forceinline__ void copy16(uint32_t dst, const void* src) {
+    asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(dst), "l"(src) : "memory");
+}
+// VEC = 8: NV groups of 8 elements per thread and row, group i of thread t at column (i TPR + t) 8.  A bf16 group is one
+// 16-byte piece, which the thread copies itself; the 64 pieces of a warp's FP32 groups are copied by the warp, 512
+// consecutive bytes at a time.
+template <class T, int VEC, int TPR, int NV>
+struct RowSource {
+    static_assert(VEC == 8, "");
+    static constexpr int CHUNKS = static_cast<int>(sizeof(T)) / 2;
+    static constexpr bool SHARED = CHUNKS == 2;        // a thread reads what others of its warp have copied
+    static constexpr int THREADS = TPR == 32 ? 128 : TPR;
+    static constexpr uint32_t STAGE_BYTES = THREADS * NV * CHUNKS * 16;
+    uint32_t base;                                     // this warp's first slot
+    const T* first;
+    int64_t ld;
+    int N, col;                                        // col: first column of this lane's first piece
+    __device__ __forceinline__ RowSource(uint32_t smem, const void* x, int64_t ld_, int64_t, int N_, int t)
+        : base(smem + (threadIdx.x & ~31u) * CHUNKS * 16), first(static_cast<const T*>(x)), ld(ld_), N(N_),
+          col((t & ~31) * 8 + (t & 31) * (8 / CHUNKS)) {}
+    __device__ __forceinline__ void fetch(int stage, int64_t m) const {
+        const T* row = first + m * ld + col;
+        const uint32_t dst = base + stage * STAGE_BYTES + (threadIdx.x & 31) * 16;
+#pragma unroll
+        for (int i = 0; i < NV; ++i)
+#pragma unroll
+            for (int c = 0; c < CHUNKS; ++c)
+                if (col + i * TPR * 8 + c * 128 < N) copy16(dst + i * CHUNKS * THREADS * 16 + c * 512, row + i * TPR * 8 + c * 128);
+    }
+    __device__ __forceinline__ void read(int stage, int64_t, int i, Raw<T, VEC>& r) const {
+        const uint32_t at = base + stage * STAGE_BYTES + i * CHUNKS * THREADS * 16 + (threadIdx.x & 31) * CHUNKS * 16;
+#pragma unroll
+        for (int c = 0; c < CHUNKS; ++c)
+            asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(r.w[4 * c]), "=r"(r.w[4 * c + 1]), "=r"(r.w[4 * c + 2]), "=r"(r.w[4 * c + 3])
+                         : "r"(at + 16 * c) : "memory");
+    }
+};
+// VEC = 1: element i TPR + t of the row, wherever the row starts.  The row's threads copy the 16-byte pieces that cover it; what
+// a piece holds besides the row is not read, and a row with a piece that is not wholly inside the matrix is copied by elements.
+template <class T, int TPR, int NV>
+struct RowSource<T, 1, TPR, NV> {
+    static constexpr bool SHARED = true;
+    static constexpr uint32_t ROW_BYTES = TPR * NV * sizeof(T) + 16, STAGE_BYTES = (TPR == 32 ? 4 : 1) * ROW_BYTES;
+    uint32_t base;
+    const T* first;
+    int64_t ld;
+    uintptr_t end;                                     // of the matrix
+    int N, t;
+    __device__ __forceinline__ RowSource(uint32_t smem, const void* x, int64_t ld_, int64_t M, int N_, int t_)
+        : base(smem + (TPR == 32 ? threadIdx.x >> 5 : 0) * ROW_BYTES), first(static_cast<const T*>(x)), ld(ld_),
+          end(reinterpret_cast<uintptr_t>(first + (M - 1) * ld + N_)), N(N_), t(t_) {}
+    __device__ __forceinline__ void fetch(int stage, int64_t m) const {
+        const uintptr_t row = reinterpret_cast<uintptr_t>(first + m * ld), from = row & ~static_cast<uintptr_t>(15);
+        const uint32_t skip = static_cast<uint32_t>(row - from);
+        const int bytes = static_cast<int>(skip + N * sizeof(T));                   // from `from` to the row's end
+        const uint32_t dst = base + stage * STAGE_BYTES;
+        if (from >= reinterpret_cast<uintptr_t>(first) && from + ((bytes + 15) & ~15) <= end) {
+            constexpr int ROUNDS = static_cast<int>((NV * sizeof(T) + 15) / 16 + 1);      // of TPR pieces, most
+#pragma unroll
+            for (int k = 0; k < ROUNDS; ++k) {
+                const int o = 16 * (t + k * TPR);
+                if (o < bytes) copy16(dst + o, reinterpret_cast<const char*>(from) + o);
+            }
+        } else {
+            for (int n = t; n < N; n += TPR) {
+                const uint32_t to = dst + skip + n * static_cast<uint32_t>(sizeof(T));
+                if constexpr (sizeof(T) == 4) asm volatile("st.shared.b32 [%0], %1;" ::"r"(to), "r"(reinterpret_cast<const uint32_t*>(row)[n]) : "memory");
+                else asm volatile("st.shared.b16 [%0], %1;" ::"r"(to), "h"(reinterpret_cast<const uint16_t*>(row)[n]) : "memory");
+            }
+        }
+    }
+    __device__ __forceinline__ void read(int stage, int64_t m, int i, Raw<T, 1>& r) const {
+        const uint32_t at = base + stage * STAGE_BYTES + (static_cast<uint32_t>(reinterpret_cast<uintptr_t>(first + m * ld)) & 15u) + t * static_cast<uint32_t>(sizeof(T));
+        if constexpr (sizeof(T) == 4) asm volatile("ld.shared.b32 %0, [%1];" : "=r"(r.w[0]) : "r"(at + i * TPR * 4) : "memory");
+        else asm volatile("ld.shared.b16 %0, [%1];" : "=h"(r.w[0]) : "r"(at + i * TPR * 2) : "memory");
+    }
+};
+// Between this thread's wait for its copies and its reads: the other threads' copies have landed too.
+template <class Source, int VEC, int TPR>
+__device__ __forceinline__ void row_barrier() {
+    if constexpr (Source::SHARED) {
+        if constexpr (VEC == 1 && TPR > 32) __syncthreads(); else __syncwarp();
+    }
+}
+__device__ __forceinline__ void async_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
+template <int N>
+__device__ __forceinline__ void async_wait() { asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory"); }
+
 // ---------------------------------------------------------------------------------- forward
 struct FwdParams {
     int64_t M, N, ldx, ldy, rows;          // rows: rows the grid covers (M, or M padded for the BFP16 planes)
@@ -127,86 +245,109 @@ struct FwdParams {
     float *mean, *rstd;
 };
 
-// Writes VEC results of row m from column n on: values, or one BFP16 block.
-template <class TX, int VEC, bool BFP>
-__device__ __forceinline__ void put(const FwdParams& p, int64_t m, int64_t n, const float (&v)[VEC]) {
-    if constexpr (BFP) {
-        uint32_t packed[2];
-        const int E = bfp16::quantize_block8(v, packed);
-        *reinterpret_cast<uint2*>(static_cast<int8_t*>(p.y) + m * p.N + n) = make_uint2(packed[0], packed[1]);
-        p.exp[((n >> 6) * p.rows + m) * 8 + ((n >> 3) & 7)] = static_cast<uint8_t>(E);
-    } else {
-        store_f<TX, VEC>(static_cast<TX*>(p.y) + m * p.ldy + n, v);
-    }
+// One BFP16 block of row m, columns n .. n + 7.
+__device__ __forceinline__ void put_block(const FwdParams& p, int64_t m, int64_t n, const float (&v)[8]) {
+    uint32_t packed[2];
+    const int E = bfp16::quantize_block8(v, packed);
+    *reinterpret_cast<uint2*>(static_cast<int8_t*>(p.y) + m * p.N + n) = make_uint2(packed[0], packed[1]);
+    p.exp[((n >> 6) * p.rows + m) * 8 + ((n >> 3) & 7)] = static_cast<uint8_t>(E);
 }
 // The exponent plane's padding of row m: blocks past the last column, and whole rows past M.
 __device__ __forceinline__ void put_exp_padding(const FwdParams& p, int64_t m, int t, int threads) {
     const int64_t first = m < p.M ? p.N >> 3 : 0, last = ((p.N + 63) >> 6) * 8;
     for (int64_t j = first + t; j < last; j += threads) p.exp[((j >> 3) * p.rows + m) * 8 + (j & 7)] = 0;
 }
-template <class TX, class TW, int VEC, bool BFP>
-__device__ __forceinline__ void scale_and_put(const FwdParams& p, int64_t m, int64_t n, float (&v)[VEC], float mu, float r) {
-    float w[VEC], b[VEC];
-    if (p.w) load_f<TW, VEC>(static_cast<const TW*>(p.w) + n, w);
-    if (p.b) load_f<TW, VEC>(static_cast<const TW*>(p.b) + n, b);
+template <class TX, class TW, int VEC, int TPR, int NV, bool BFP>
+__global__ void __launch_bounds__(TPR == 32 ? 128 : TPR, blocks_per_sm(TPR, false)) layer_norm_kernel(const FwdParams p) {
+    using Source = RowSource<TX, VEC, TPR, NV>;
+    constexpr int WALKERS = TPR == 32 ? 4 : 1, W = TPR / 32;
+    constexpr int STAGES = kAhead<TX> + 1;
+    extern __shared__ __align__(16) uint8_t ring[];
+    __shared__ float2 red[2][W];
+    const int t = TPR == 32 ? threadIdx.x & 31 : threadIdx.x, lane = threadIdx.x & 31, warp = TPR == 32 ? 0 : threadIdx.x >> 5;
+    const int N = static_cast<int>(p.N), col = t * VEC;                 // group i: columns col + i TPR VEC ..
+    const int64_t first = static_cast<int64_t>(blockIdx.x) * WALKERS + (TPR == 32 ? threadIdx.x >> 5 : 0), step = static_cast<int64_t>(gridDim.x) * WALKERS;
+    const Source src(sm100::smem_u32(ring), p.x, p.ldx, p.M, N, t);
+    // elements of warp `lane` (join) and of this warp (the mean that its squares are summed around)
+    int count = 0;
 #pragma unroll
-    for (int e = 0; e < VEC; ++e) {
-        v[e] = (v[e] - mu) * r;
-        if (p.w) v[e] *= w[e];
-        if (p.b) v[e] += b[e];
+    for (int i = 0; i < NV; ++i) count += max(0, min(32 * VEC, N - (i * TPR + lane * 32) * VEC));
+    if (lane >= W) count = 0;
+    const float elems = static_cast<float>(count), inv_n = 1.f / static_cast<float>(N);
+    const int own = __shfl_sync(0xFFFFFFFFu, count, warp);
+    const float inv_own = own > 0 ? 1.f / static_cast<float>(own) : 0.f;
+    sm100::grid_dependency_wait();
+    sm100::grid_dependency_launch();
+#pragma unroll
+    for (int s = 0; s < kAhead<TX>; ++s) {
+        if (first + s * step < p.M) src.fetch(s, first + s * step);
+        async_commit();
     }
-    put<TX, VEC, BFP>(p, m, n, v);
-}
-
-template <class TX, class TW, int VEC, int TPR, bool BFP>
-__global__ void __launch_bounds__(TPR == 32 ? 128 : TPR) layer_norm_kernel(const FwdParams p) {
-    constexpr int NV = kFwdElems / VEC, ROWS = TPR == 32 ? 4 : 1;
-    __shared__ float red[2][32][1];
-    const int t = TPR == 32 ? threadIdx.x & 31 : threadIdx.x;
-    const int64_t m = static_cast<int64_t>(blockIdx.x) * ROWS + (TPR == 32 ? threadIdx.x >> 5 : 0);
-    if (m >= p.rows) return;                                   // a whole warp (TPR = 32) or a whole block
-    if constexpr (BFP) {
-        put_exp_padding(p, m, t, TPR);
-        if (m >= p.M) return;
-    }
-    const TX* x = static_cast<const TX*>(p.x) + m * p.ldx;
-    Raw<TX, VEC> raw[NV];
+    Raw<TW, VEC> w[NV], b[NV];
 #pragma unroll
     for (int i = 0; i < NV; ++i) {
-        const int64_t n = (static_cast<int64_t>(i) * TPR + t) * VEC;
-        if (n < p.N) load_raw<TX, VEC>(x + n, raw[i]);
+        load_or<TW, VEC>(static_cast<const TW*>(p.w), col + i * TPR * VEC, N, 1.f, w[i]);
+        load_or<TW, VEC>(static_cast<const TW*>(p.b), col + i * TPR * VEC, N, 0.f, b[i]);
     }
-    float s[1] = {0.f}, v[VEC];
+    int stage = 0, turn = 0;
+    for (int64_t m = first; m < p.rows; m += step, turn ^= 1) {
+        if constexpr (BFP) put_exp_padding(p, m, t, TPR);
+        if (m < p.M) {                     // the same for all threads of the row
+            const int ahead = stage == 0 ? kAhead<TX> : stage - 1;       // the stage that the row before this one has left
+            if (m + kAhead<TX> * step < p.M) src.fetch(ahead, m + kAhead<TX> * step);
+            async_commit();
+            async_wait<kAhead<TX>>();
+            row_barrier<Source, VEC, TPR>();
+            float v[NV][VEC], s[1] = {0.f};
 #pragma unroll
-    for (int i = 0; i < NV; ++i)
-        if ((static_cast<int64_t>(i) * TPR + t) * VEC < p.N) {
-            to_float(raw[i], v);
+            for (int i = 0; i < NV; ++i) {
+                if (col + i * TPR * VEC < N) {
+                    Raw<TX, VEC> raw;
+                    src.read(stage, m, i, raw);
+                    to_float(raw, v[i]);
 #pragma unroll
-            for (int e = 0; e < VEC; ++e) s[0] += v[e];
-        }
-    const float inv_n = 1.f / static_cast<float>(p.N);
-    row_sum<TPR, 1>(s, red[0]);
-    const float mu = s[0] * inv_n;
-    s[0] = 0.f;
+                    for (int e = 0; e < VEC; ++e) s[0] += v[i][e];
+                }
+            }
+            warp_sum(s);
+            float mu = s[0] * inv_own;
+            s[0] = 0.f;
 #pragma unroll
-    for (int i = 0; i < NV; ++i)
-        if ((static_cast<int64_t>(i) * TPR + t) * VEC < p.N) {
-            to_float(raw[i], v);
+            for (int i = 0; i < NV; ++i)
+                if (col + i * TPR * VEC < N)
 #pragma unroll
-            for (int e = 0; e < VEC; ++e) s[0] += (v[e] - mu) * (v[e] - mu);
-        }
-    row_sum<TPR, 1>(s, red[1]);
-    const float r = rsqrtf(s[0] * inv_n + p.eps);
-    if (t == 0) {
-        if (p.mean) p.mean[m] = mu;
-        if (p.rstd) p.rstd[m] = r;
-    }
+                    for (int e = 0; e < VEC; ++e) s[0] += (v[i][e] - mu) * (v[i][e] - mu);
+            warp_sum(s);
+            if constexpr (TPR > 32) {
+                if (lane == 0) red[turn][warp] = make_float2(mu, s[0]);
+                __syncthreads();
+                // every warp joins the warps' pairs: lane l has warp l's
+                const float2 part = lane < W ? red[turn][lane] : make_float2(0.f, 0.f);
+                float sum[1] = {elems * part.x};
+                warp_sum(sum);
+                mu = sum[0] * inv_n;
+                s[0] = part.y + elems * (part.x - mu) * (part.x - mu);
+                warp_sum(s);
+            }
+            const float r = rsqrtf(s[0] * inv_n + p.eps);
+            if (t == 0) {
+                if (p.mean) p.mean[m] = mu;
+                if (p.rstd) p.rstd[m] = r;
+            }
+            TX* const y = BFP ? nullptr : static_cast<TX*>(p.y) + m * p.ldy + col;
 #pragma unroll
-    for (int i = 0; i < NV; ++i) {
-        const int64_t n = (static_cast<int64_t>(i) * TPR + t) * VEC;
-        if (n < p.N) {
-            to_float(raw[i], v);
-            scale_and_put<TX, TW, VEC, BFP>(p, m, n, v, mu, r);
+            for (int i = 0; i < NV; ++i) {
+                if (col + i * TPR * VEC < N) {
+                    float fw[VEC], fb[VEC];
+                    to_float(w[i], fw);
+                    to_float(b[i], fb);
+#pragma unroll
+                    for (int e = 0; e < VEC; ++e) v[i][e] = fmaf((v[i][e] - mu) * r, fw[e], fb[e]);
+                    if constexpr (BFP) put_block(p, m, col + i * TPR * VEC, v[i]);
+                    else store_f<TX, VEC>(y + i * TPR * VEC, v[i]);
+                }
+            }
+            stage = stage + 1 == STAGES ? 0 : stage + 1;
         }
     }
 }
@@ -244,7 +385,16 @@ __global__ void __launch_bounds__(1024) layer_norm_wide_kernel(const FwdParams p
     }
     for (int64_t n = threadIdx.x * VEC; n < p.N; n += 1024 * VEC) {
         load_f<TX, VEC>(x + n, v);
-        scale_and_put<TX, TW, VEC, BFP>(p, m, n, v, mu, r);
+        Raw<TW, VEC> raw;
+        float fw[VEC], fb[VEC];
+        load_or<TW, VEC>(static_cast<const TW*>(p.w), n, p.N, 1.f, raw);
+        to_float(raw, fw);
+        load_or<TW, VEC>(static_cast<const TW*>(p.b), n, p.N, 0.f, raw);
+        to_float(raw, fb);
+#pragma unroll
+        for (int e = 0; e < VEC; ++e) v[e] = fmaf((v[e] - mu) * r, fw[e], fb[e]);
+        if constexpr (BFP) put_block(p, m, n, v);
+        else store_f<TX, VEC>(static_cast<TX*>(p.y) + m * p.ldy + n, v);
     }
 }
 
@@ -257,78 +407,97 @@ struct BwdParams {
     float* part;                           // [blocks][2][N]: sums of dw and db of each block
 };
 
-template <class TX, class TW, int VEC, int TPR>
-__global__ void __launch_bounds__(TPR == 32 ? 128 : TPR) layer_norm_backward_kernel(const BwdParams p) {
-    constexpr int NV = kBwdElems / VEC, WALKERS = TPR == 32 ? 4 : 1;      // rows a block has in hand at a time
-    __shared__ float red[2][32][2];
+template <class TX, class TW, int VEC, int TPR, int NV>
+__global__ void __launch_bounds__(TPR == 32 ? 128 : TPR, blocks_per_sm(TPR, true)) layer_norm_backward_kernel(const BwdParams p) {
+    using Source = RowSource<TX, VEC, TPR, NV>;
+    constexpr int WALKERS = TPR == 32 ? 4 : 1, W = TPR / 32;
+    constexpr int STAGES = kAhead<TX> + 1;
+    extern __shared__ __align__(16) uint8_t ring[];
+    __shared__ float red[2][W][2];
     const int t = TPR == 32 ? threadIdx.x & 31 : threadIdx.x;
-    const int64_t walker = static_cast<int64_t>(blockIdx.x) * WALKERS + (TPR == 32 ? threadIdx.x >> 5 : 0);
-    const float inv_n = 1.f / static_cast<float>(p.N);
+    const int N = static_cast<int>(p.N), col = t * VEC;                 // group i: columns col + i TPR VEC ..
+    const int64_t first = static_cast<int64_t>(blockIdx.x) * WALKERS + (TPR == 32 ? threadIdx.x >> 5 : 0), step = static_cast<int64_t>(gridDim.x) * WALKERS;
+    const Source sx(sm100::smem_u32(ring), p.x, p.ldx, p.M, N, t), sd(sm100::smem_u32(ring) + STAGES * Source::STAGE_BYTES, p.dy, p.lddy, p.M, N, t);
+    const float inv_n = 1.f / static_cast<float>(N);
+    sm100::grid_dependency_wait();
+    sm100::grid_dependency_launch();
+#pragma unroll
+    for (int s = 0; s < kAhead<TX>; ++s) {
+        if (first + s * step < p.M) {
+            sx.fetch(s, first + s * step);
+            sd.fetch(s, first + s * step);
+        }
+        async_commit();
+    }
+    Raw<TW, VEC> w[NV];
     float dw[NV][VEC], db[NV][VEC];
 #pragma unroll
-    for (int i = 0; i < NV; ++i)
+    for (int i = 0; i < NV; ++i) {
+        load_or<TW, VEC>(static_cast<const TW*>(p.w), col + i * TPR * VEC, N, 1.f, w[i]);
 #pragma unroll
         for (int e = 0; e < VEC; ++e) dw[i][e] = db[i][e] = 0.f;
-    int turn = 0;
-    for (int64_t m = walker; m < p.M; m += static_cast<int64_t>(gridDim.x) * WALKERS, turn ^= 1) {
-        const TX* x = static_cast<const TX*>(p.x) + m * p.ldx;
-        const TX* dy = static_cast<const TX*>(p.dy) + m * p.lddy;
-        Raw<TX, VEC> rx[NV], rd[NV];
-#pragma unroll
-        for (int i = 0; i < NV; ++i) {
-            const int64_t n = (static_cast<int64_t>(i) * TPR + t) * VEC;
-            if (n < p.N) { load_raw<TX, VEC>(x + n, rx[i]); load_raw<TX, VEC>(dy + n, rd[i]); }
+    }
+    int stage = 0, turn = 0;
+    float mu = 0.f, r = 0.f;
+    if (first < p.M) { mu = p.mean[first]; r = p.rstd[first]; }
+    for (int64_t m = first; m < p.M; m += step, turn ^= 1) {
+        const int ahead = stage == 0 ? kAhead<TX> : stage - 1;           // the stage that the row before this one has left
+        if (m + kAhead<TX> * step < p.M) {
+            sx.fetch(ahead, m + kAhead<TX> * step);
+            sd.fetch(ahead, m + kAhead<TX> * step);
         }
-        const float mu = p.mean[m], r = p.rstd[m];
-        float s[2] = {0.f, 0.f};
+        async_commit();
+        float next_mu = 0.f, next_r = 0.f;
+        if (m + step < p.M) { next_mu = p.mean[m + step]; next_r = p.rstd[m + step]; }
+        async_wait<kAhead<TX>>();
+        row_barrier<Source, VEC, TPR>();
+        float z[NV][VEC], g[NV][VEC], s[2] = {0.f, 0.f};
 #pragma unroll
         for (int i = 0; i < NV; ++i) {
-            const int64_t n = (static_cast<int64_t>(i) * TPR + t) * VEC;
-            if (n < p.N) {
-                float vx[VEC], vd[VEC], w[VEC];
-                to_float(rx[i], vx);
-                to_float(rd[i], vd);
-                if (p.w) load_f<TW, VEC>(static_cast<const TW*>(p.w) + n, w);
+            if (col + i * TPR * VEC < N) {
+                Raw<TX, VEC> raw;
+                float f[VEC];
+                sx.read(stage, m, i, raw);
+                to_float(raw, z[i]);
+                sd.read(stage, m, i, raw);
+                to_float(raw, g[i]);
+                to_float(w[i], f);
 #pragma unroll
                 for (int e = 0; e < VEC; ++e) {
-                    const float z = (vx[e] - mu) * r, g = p.w ? vd[e] * w[e] : vd[e];
-                    s[0] += g;
-                    s[1] += g * z;
-                    dw[i][e] += vd[e] * z;
-                    db[i][e] += vd[e];
+                    z[i][e] = (z[i][e] - mu) * r;
+                    dw[i][e] = fmaf(g[i][e], z[i][e], dw[i][e]);
+                    db[i][e] += g[i][e];
+                    g[i][e] *= f[e];
+                    s[0] += g[i][e];
+                    s[1] = fmaf(g[i][e], z[i][e], s[1]);
                 }
             }
         }
         row_sum<TPR, 2>(s, red[turn]);
-        const float c0 = s[0] * inv_n, c1 = s[1] * inv_n;
         if (p.dx) {
-            TX* dx = static_cast<TX*>(p.dx) + m * p.lddx;
+            const float c0 = s[0] * inv_n, c1 = s[1] * inv_n;
+            TX* const dx = static_cast<TX*>(p.dx) + m * p.lddx + col;
 #pragma unroll
             for (int i = 0; i < NV; ++i) {
-                const int64_t n = (static_cast<int64_t>(i) * TPR + t) * VEC;
-                if (n < p.N) {
-                    float vx[VEC], vd[VEC], w[VEC];
-                    to_float(rx[i], vx);
-                    to_float(rd[i], vd);
-                    if (p.w) load_f<TW, VEC>(static_cast<const TW*>(p.w) + n, w);
+                if (col + i * TPR * VEC < N) {
 #pragma unroll
-                    for (int e = 0; e < VEC; ++e) {
-                        const float z = (vx[e] - mu) * r, g = p.w ? vd[e] * w[e] : vd[e];
-                        vx[e] = r * (g - c0 - z * c1);
-                    }
-                    store_f<TX, VEC>(dx + n, vx);
+                    for (int e = 0; e < VEC; ++e) g[i][e] = r * (g[i][e] - c0 - z[i][e] * c1);
+                    store_f<TX, VEC>(dx + i * TPR * VEC, g[i]);
                 }
             }
         }
+        mu = next_mu;
+        r = next_r;
+        stage = stage + 1 == STAGES ? 0 : stage + 1;
     }
     if (p.part) {                          // a walker's sums: [walker][2][N]
-        float* out = p.part + walker * 2 * p.N;
+        float* out = p.part + first * 2 * p.N + col;
 #pragma unroll
         for (int i = 0; i < NV; ++i) {
-            const int64_t n = (static_cast<int64_t>(i) * TPR + t) * VEC;
-            if (n < p.N)
-#pragma unroll
-                for (int e = 0; e < VEC; ++e) { out[n + e] = dw[i][e]; out[p.N + n + e] = db[i][e]; }
+            if (col + i * TPR * VEC < N) {
+                store_f<float, VEC>(out + i * TPR * VEC, dw[i]);
+                store_f<float, VEC>(out + p.N + i * TPR * VEC, db[i]);             // N is a multiple of VEC
+            }
         }
     }
 }
@@ -376,20 +545,26 @@ __global__ void __launch_bounds__(256) layer_norm_backward_columns_kernel(const 
     out[p.N + n] = db;
 }
 
-// dw[n], db[n] = sum over the `parts` partial sums, in a fixed order: 32 columns of [dw | db] per block, 8 warps that
-// take every 8th partial sum, then the 8 in turn.
+// dw[n], db[n] = sum over the `parts` partial sums, in a fixed order: 32 columns of [dw | db] per block, 16 warps that
+// take every 16th partial sum, then the 16 in turn.
+constexpr int kSumWarps = 16;
 template <class TW>
-__global__ void __launch_bounds__(256) layer_norm_backward_sum_kernel(const float* part, int parts, int64_t N, TW* dw, TW* db) {
-    __shared__ float s[8][32];
+__global__ void __launch_bounds__(32 * kSumWarps) layer_norm_backward_sum_kernel(const float* part, int parts, int64_t N, TW* dw, TW* db) {
+    __shared__ float s[kSumWarps][32];
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     const int64_t c = static_cast<int64_t>(blockIdx.x) * 32 + lane;
+    sm100::grid_dependency_wait();
+    sm100::grid_dependency_launch();
     float v = 0.f;
-    if (c < 2 * N)
-        for (int i = warp; i < parts; i += 8) v += part[static_cast<int64_t>(i) * 2 * N + c];
+    if (c < 2 * N) {
+#pragma unroll 8
+        for (int i = warp; i < parts; i += kSumWarps) v += part[static_cast<int64_t>(i) * 2 * N + c];
+    }
     s[warp][lane] = v;
     __syncthreads();
     if (warp == 0 && c < 2 * N) {
-        for (int i = 1; i < 8; ++i) v += s[i][lane];
+#pragma unroll
+        for (int i = 1; i < kSumWarps; ++i) v += s[i][lane];
         TW* out = c < N ? dw : db;
         const float r[1] = {v};
         if (out) store_f<TW, 1>(out + (c < N ? c : c - N), r);
@@ -397,52 +572,96 @@ __global__ void __launch_bounds__(256) layer_norm_backward_sum_kernel(const floa
 }
 
 // ---------------------------------------------------------------------------------- host
-// Threads per row: the fewest of 32, 128, 256, 512, 1024 (forward) that hold a row of N elements; 0: a wide kernel.
-int threads_per_row(int64_t N, int elems, int most) {
+// Threads per row: the fewest of 32, 128, 256, 512, 1024 (at most `most`) that hold a row of N elements; 0: a wide kernel.
+int threads_per_row(int64_t N, int most) {
     for (int t : {32, 128, 256, 512, 1024})
-        if (t <= most && N <= static_cast<int64_t>(t) * elems) return t;
+        if (t <= most && N <= static_cast<int64_t>(t) * kElems) return t;
     return 0;
 }
+constexpr int kFwdThreads = 1024, kBwdThreads = 512;      // the backward sums take 2 kElems registers
 
-template <class TX, class TW, int VEC, bool BFP>
-void launch_fwd(const FwdParams& p, cudaStream_t st) {
-    const unsigned rows = static_cast<unsigned>(p.rows), quads = static_cast<unsigned>((p.rows + 3) / 4);
-    switch (threads_per_row(p.N, kFwdElems, 1024)) {
-        case 32: layer_norm_kernel<TX, TW, VEC, 32, BFP><<<quads, 128, 0, st>>>(p); break;
-        case 128: layer_norm_kernel<TX, TW, VEC, 128, BFP><<<rows, 128, 0, st>>>(p); break;
-        case 256: layer_norm_kernel<TX, TW, VEC, 256, BFP><<<rows, 256, 0, st>>>(p); break;
-        case 512: layer_norm_kernel<TX, TW, VEC, 512, BFP><<<rows, 512, 0, st>>>(p); break;
-        case 1024: layer_norm_kernel<TX, TW, VEC, 1024, BFP><<<rows, 1024, 0, st>>>(p); break;
-        default: layer_norm_wide_kernel<TX, TW, VEC, BFP><<<rows, 1024, 0, st>>>(p);
+template <class... Args>
+cudaError_t launch_dependent(void (*kernel)(Args...), unsigned grid, unsigned block, size_t smem, cudaStream_t stream, Args... args) {
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3(grid, 1, 1);
+    cfg.blockDim = dim3(block, 1, 1);
+    cfg.dynamicSmemBytes = smem;
+    cfg.stream = stream;
+    cudaLaunchAttribute attr[1];
+    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;     // may be set up while the kernel before it drains
+    attr[0].val.programmaticStreamSerializationAllowed = 1;
+    cfg.attrs = attr;
+    cfg.numAttrs = 1;
+    return cudaLaunchKernelEx(&cfg, kernel, args...);
+}
+// A kernel whose rows on their way may take more, with its static arrays, than the 48 KB of shared memory that need no leave.
+template <class... Args>
+cudaError_t launch_ring(void (*kernel)(Args...), unsigned grid, unsigned block, size_t smem, cudaStream_t stream, Args... args) {
+    if (smem > 40 * 1024) {
+        const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(smem));
+        if (e != cudaSuccess) return e;
     }
+    return launch_dependent(kernel, grid, block, smem, stream, args...);
 }
 
-// Blocks that walk the rows: enough to fill the SMs, and at least 4 rows for each walker, whose sums of 8 N bytes
-// go through the workspace.
+template <class TX, class TW, int VEC, bool BFP, int TPR>
+cudaError_t launch_fwd_rows(const FwdParams& p, cudaStream_t st) {
+    constexpr int NV = kElems / VEC, HALF = NV > 1 ? NV / 2 : 1, THREADS = TPR == 32 ? 128 : TPR;
+    const int64_t walkers = TPR == 32 ? 4 : 1, all = (p.rows + walkers - 1) / walkers, most = static_cast<int64_t>(atb::kSmCount) * blocks_per_sm(TPR, false);
+    const unsigned blocks = static_cast<unsigned>(all < most ? all : most);
+    if (p.N <= static_cast<int64_t>(TPR) * kElems / 2)
+        return launch_ring(layer_norm_kernel<TX, TW, VEC, TPR, HALF, BFP>, blocks, THREADS, (kAhead<TX> + 1) * RowSource<TX, VEC, TPR, HALF>::STAGE_BYTES, st, p);
+    return launch_ring(layer_norm_kernel<TX, TW, VEC, TPR, NV, BFP>, blocks, THREADS, (kAhead<TX> + 1) * RowSource<TX, VEC, TPR, NV>::STAGE_BYTES, st, p);
+}
+template <class TX, class TW, int VEC, bool BFP>
+cudaError_t launch_fwd(const FwdParams& p, cudaStream_t st) {
+    switch (threads_per_row(p.N, kFwdThreads)) {
+        case 32: return launch_fwd_rows<TX, TW, VEC, BFP, 32>(p, st);
+        case 128: return launch_fwd_rows<TX, TW, VEC, BFP, 128>(p, st);
+        case 256: return launch_fwd_rows<TX, TW, VEC, BFP, 256>(p, st);
+        case 512: return launch_fwd_rows<TX, TW, VEC, BFP, 512>(p, st);
+        case 1024: return launch_fwd_rows<TX, TW, VEC, BFP, 1024>(p, st);
+    }
+    layer_norm_wide_kernel<TX, TW, VEC, BFP><<<static_cast<unsigned>(p.rows), 1024, 0, st>>>(p);
+    return cudaGetLastError();
+}
+
+// Blocks that walk the rows: one per SM and more while each walker still has 16 rows, since its sums of 8 N bytes go
+// through the workspace.  The same on every host: the workspace's size depends on it.
 int walking_blocks(int64_t M, int64_t N) {
-    const int tpr = threads_per_row(N, kBwdElems, 512);
-    const int64_t walkers = tpr == 32 ? 4 : 1;
-    int64_t blocks = (M + 4 * walkers - 1) / (4 * walkers);
-    if (blocks > kMaxBlocks) blocks = kMaxBlocks;
+    const int tpr = threads_per_row(N, kBwdThreads);
+    const int64_t walkers = tpr == 32 ? 4 : 1, all = (M + walkers - 1) / walkers, most = static_cast<int64_t>(atb::kSmCount) * blocks_per_sm(tpr, true);
+    int64_t blocks = (M + 16 * walkers - 1) / (16 * walkers);
+    if (blocks < atb::kSmCount) blocks = atb::kSmCount;
+    if (blocks > most) blocks = most;
+    if (blocks > all) blocks = all;
     return static_cast<int>(blocks < 1 ? 1 : blocks);
 }
 int partial_sums(int64_t M, int64_t N) {
-    return walking_blocks(M, N) * (threads_per_row(N, kBwdElems, 512) == 32 ? 4 : 1);
+    return walking_blocks(M, N) * (threads_per_row(N, kBwdThreads) == 32 ? 4 : 1);
 }
 
-template <class TX, class TW, int VEC>
-void launch_bwd(const BwdParams& p, cudaStream_t st) {
+template <class TX, class TW, int VEC, int TPR>
+cudaError_t launch_bwd_rows(const BwdParams& p, cudaStream_t st) {
+    constexpr int NV = kElems / VEC, HALF = NV > 1 ? NV / 2 : 1, THREADS = TPR == 32 ? 128 : TPR;
     const unsigned blocks = static_cast<unsigned>(walking_blocks(p.M, p.N));
-    switch (threads_per_row(p.N, kBwdElems, 512)) {
-        case 32: layer_norm_backward_kernel<TX, TW, VEC, 32><<<blocks, 128, 0, st>>>(p); break;
-        case 128: layer_norm_backward_kernel<TX, TW, VEC, 128><<<blocks, 128, 0, st>>>(p); break;
-        case 256: layer_norm_backward_kernel<TX, TW, VEC, 256><<<blocks, 256, 0, st>>>(p); break;
-        case 512: layer_norm_backward_kernel<TX, TW, VEC, 512><<<blocks, 512, 0, st>>>(p); break;
-        default:
-            if (p.dx) layer_norm_backward_wide_kernel<TX, TW><<<static_cast<unsigned>(p.M), 1024, 0, st>>>(p);
-            if (p.part)
-                layer_norm_backward_columns_kernel<TX><<<dim3(static_cast<unsigned>((p.N + 255) / 256), blocks), 256, 0, st>>>(p);
+    if (p.N <= static_cast<int64_t>(TPR) * kElems / 2)
+        return launch_ring(layer_norm_backward_kernel<TX, TW, VEC, TPR, HALF>, blocks, THREADS,
+                           2 * (kAhead<TX> + 1) * RowSource<TX, VEC, TPR, HALF>::STAGE_BYTES, st, p);
+    return launch_ring(layer_norm_backward_kernel<TX, TW, VEC, TPR, NV>, blocks, THREADS, 2 * (kAhead<TX> + 1) * RowSource<TX, VEC, TPR, NV>::STAGE_BYTES, st, p);
+}
+template <class TX, class TW, int VEC>
+cudaError_t launch_bwd(const BwdParams& p, cudaStream_t st) {
+    switch (threads_per_row(p.N, kBwdThreads)) {
+        case 32: return launch_bwd_rows<TX, TW, VEC, 32>(p, st);
+        case 128: return launch_bwd_rows<TX, TW, VEC, 128>(p, st);
+        case 256: return launch_bwd_rows<TX, TW, VEC, 256>(p, st);
+        case 512: return launch_bwd_rows<TX, TW, VEC, 512>(p, st);
     }
+    if (p.dx) layer_norm_backward_wide_kernel<TX, TW><<<static_cast<unsigned>(p.M), 1024, 0, st>>>(p);
+    if (p.part)
+        layer_norm_backward_columns_kernel<TX><<<dim3(static_cast<unsigned>((p.N + 255) / 256), static_cast<unsigned>(walking_blocks(p.M, p.N))), 256, 0, st>>>(p);
+    return cudaGetLastError();
 }
 
 bool known_type(int t) { return t == ATB_F32 || t == ATB_BF16; }
@@ -485,13 +704,13 @@ atb_status_t forward(int64_t M, int64_t N, int x_type, const void* X, int64_t ld
     if (s != ATB_OK) return s;
     FwdParams p{M, N, ldx, ldy, exp ? atb::round_up(M, 32) : M, X, W, B, eps, Y, exp, mean, rstd};
     cudaStream_t st = static_cast<cudaStream_t>(stream);
-#define ATB_LN_BFP(TX, TW) launch_fwd<TX, TW, 8, true>(p, st)
-#define ATB_LN_VEC(TX, TW) launch_fwd<TX, TW, 8, false>(p, st)
-#define ATB_LN_ONE(TX, TW) launch_fwd<TX, TW, 1, false>(p, st)
+    cudaError_t e = cudaSuccess;
+#define ATB_LN_BFP(TX, TW) e = launch_fwd<TX, TW, 8, true>(p, st)
+#define ATB_LN_VEC(TX, TW) e = launch_fwd<TX, TW, 8, false>(p, st)
+#define ATB_LN_ONE(TX, TW) e = launch_fwd<TX, TW, 1, false>(p, st)
     if (exp) { ATB_LN_TYPES(ATB_LN_BFP) }
     else if (vec) { ATB_LN_TYPES(ATB_LN_VEC) }
     else { ATB_LN_TYPES(ATB_LN_ONE) }
-    const cudaError_t e = cudaGetLastError();
     if (e != cudaSuccess) return atb::fail(ATB_ERR_CUDA, "layer norm launch: %s", cudaGetErrorString(e));
     return ATB_OK;
 }
@@ -549,22 +768,24 @@ extern "C" atb_status_t atb_layer_norm_backward(int64_t M, int64_t N, int x_type
     cudaStream_t st = static_cast<cudaStream_t>(stream);
     const bool vec = N % 8 == 0 && vec_ok(X_dev, ldx, x_type) && vec_ok(dY_dev, lddy, x_type) && atb::aligned16(W_dev) &&
                      (!dX_dev || vec_ok(dX_dev, lddx, x_type));
+    cudaError_t e = cudaSuccess;
     if (M > 0 && (dX_dev || sums)) {
-#define ATB_LN_BWD_VEC(TX, TW) launch_bwd<TX, TW, 8>(p, st)
-#define ATB_LN_BWD_ONE(TX, TW) launch_bwd<TX, TW, 1>(p, st)
+#define ATB_LN_BWD_VEC(TX, TW) e = launch_bwd<TX, TW, 8>(p, st)
+#define ATB_LN_BWD_ONE(TX, TW) e = launch_bwd<TX, TW, 1>(p, st)
         if (vec) { ATB_LN_TYPES(ATB_LN_BWD_VEC) }
         else { ATB_LN_TYPES(ATB_LN_BWD_ONE) }
     }
-    if (sums) {
+    if (e == cudaSuccess && sums) {
         const unsigned blocks = static_cast<unsigned>((2 * N + 31) / 32);
         const int parts = M > 0 ? partial_sums(M, N) : 0;
+        const float* const part = p.part;
         if (w_type == ATB_F32)
-            layer_norm_backward_sum_kernel<float><<<blocks, 256, 0, st>>>(p.part, parts, N, static_cast<float*>(dW_dev), static_cast<float*>(dB_dev));
+            e = launch_dependent(layer_norm_backward_sum_kernel<float>, blocks, 32u * kSumWarps, 0, st, part, parts, N, static_cast<float*>(dW_dev),
+                                 static_cast<float*>(dB_dev));
         else
-            layer_norm_backward_sum_kernel<__nv_bfloat16><<<blocks, 256, 0, st>>>(p.part, parts, N, static_cast<__nv_bfloat16*>(dW_dev),
-                                                                                  static_cast<__nv_bfloat16*>(dB_dev));
+            e = launch_dependent(layer_norm_backward_sum_kernel<__nv_bfloat16>, blocks, 32u * kSumWarps, 0, st, part, parts, N,
+                                 static_cast<__nv_bfloat16*>(dW_dev), static_cast<__nv_bfloat16*>(dB_dev));
     }
-    const cudaError_t e = cudaGetLastError();
     if (e != cudaSuccess) return atb::fail(ATB_ERR_CUDA, "layer norm backward launch: %s", cudaGetErrorString(e));
     return ATB_OK;
 }
