@@ -390,14 +390,16 @@ def _dtype(t):
 
 def _matrix(t, rows, cols, dtype, device, name):
     """Checks a row-major matrix on CUDA device number ``device`` and returns its leading dimension."""
-    if t.get_device() != device or t.dtype != dtype or t.shape != (rows, cols) or (cols > 1 and t.stride(1) != 1):
-        raise ValueError(f"{name}: a row-major matrix {(rows, cols)} of {dtype} on cuda:{device}, got {tuple(t.shape)} of {t.dtype} on {t.device}, "
-                         f"strides {t.stride()}")
-    return t.stride(0) if rows > 1 else max(cols, t.stride(0))
+    if t.dtype is dtype and t.shape == (rows, cols) and t.get_device() == device:
+        ld, one = t.stride()
+        if one == 1 or cols <= 1:
+            return ld if rows > 1 or ld > cols else cols
+    raise ValueError(f"{name}: a row-major matrix {(rows, cols)} of {dtype} on cuda:{device}, got {tuple(t.shape)} of {t.dtype} on {t.device}, "
+                     f"strides {t.stride()}")
 
 
 def _vector(t, n, dtype, device, name):
-    if t.get_device() != device or t.dtype != dtype or t.shape != (n,) or not t.is_contiguous():
+    if t.dtype is not dtype or t.shape != (n,) or t.get_device() != device or not t.is_contiguous():
         raise ValueError(f"{name}: a contiguous vector of {n} {dtype} on cuda:{device}, got {tuple(t.shape)} of {t.dtype} on {t.device}")
 
 
@@ -440,17 +442,24 @@ def _norm_weights(W, B, N, x_dtype, device):
 
 
 def _out_matrix(t, like, rows, cols, dtype, device, name):
-    """An output of the caller's, checked, or a new one; and its leading dimension."""
-    if t is None:
-        return like.new_empty((rows, cols), dtype=dtype), cols
-    return t, _matrix(t, rows, cols, dtype, device, name)
+    """An output of the caller's, checked, or a new one; and its leading dimension.  ``like``: a tensor on the device, best one
+    of the output's shape and type (a copy of its description costs the host least)."""
+    if t is not None:
+        return t, _matrix(t, rows, cols, dtype, device, name)
+    if like.dtype is dtype and like.shape == (rows, cols) and like.is_contiguous():
+        import torch
+        return torch.empty_like(like), cols
+    return like.new_empty((rows, cols), dtype=dtype), cols
 
 
 def _out_vector(t, like, n, dtype, device, name):
-    if t is None:
-        return like.new_empty((n,), dtype=dtype)
-    _vector(t, n, dtype, device, name)
-    return t
+    if t is not None:
+        _vector(t, n, dtype, device, name)
+        return t
+    if like.dtype is dtype and like.shape == (n,) and like.is_contiguous():
+        import torch
+        return torch.empty_like(like)
+    return like.new_empty((n,), dtype=dtype)
 
 
 def atb_layer_norm(X, W=None, B=None, eps=1e-5, Y=None, mean=None, rstd=None, stream=None):
@@ -464,7 +473,7 @@ def atb_layer_norm(X, W=None, B=None, eps=1e-5, Y=None, mean=None, rstd=None, st
     w_type = _norm_weights(W, B, N, dtype, device)
     Y, ldy = _out_matrix(Y, X, M, N, dtype, device, "Y")
     mean = _out_vector(mean, X, M, torch.float32, device, "mean")
-    rstd = _out_vector(rstd, X, M, torch.float32, device, "rstd")
+    rstd = _out_vector(rstd, mean, M, torch.float32, device, "rstd")
     _check(load_library().atb_layer_norm(M, N, _dtype(X), X.data_ptr(), ldx, w_type, _opt_ptr(W), _opt_ptr(B), eps, Y.data_ptr(), ldy,
                                          mean.data_ptr(), rstd.data_ptr(), _stream_ptr(stream)))
     return Y, mean, rstd
@@ -482,7 +491,7 @@ def atb_layer_norm_bfp16(X, W=None, B=None, eps=1e-5, mant=None, exp=None, mean=
         raise ValueError("mant: contiguous")
     exp = _out_vector(exp, X, atb_bfp16_exp_bytes(M, N), torch.uint8, device, "exp")
     mean = _out_vector(mean, X, M, torch.float32, device, "mean")
-    rstd = _out_vector(rstd, X, M, torch.float32, device, "rstd")
+    rstd = _out_vector(rstd, mean, M, torch.float32, device, "rstd")
     _check(load_library().atb_layer_norm_bfp16(M, N, _dtype(X), X.data_ptr(), ldx, w_type, _opt_ptr(W), _opt_ptr(B), eps,
                                                mant.data_ptr(), exp.data_ptr(), mean.data_ptr(), rstd.data_ptr(), _stream_ptr(stream)))
     return mant, exp, mean, rstd
@@ -506,8 +515,8 @@ def atb_layer_norm_backward(dY, X, W, mean, rstd, dX=None, dW=None, dB=None, wor
     _vector(mean, M, torch.float32, device, "mean")
     _vector(rstd, M, torch.float32, device, "rstd")
     dX, lddx = _out_matrix(dX, X, M, N, dtype, device, "dX")
-    dW = _out_vector(dW, X, N, w_dtype, device, "dW")
-    dB = _out_vector(dB, X, N, w_dtype, device, "dB")
+    dW = _out_vector(dW, X if W is None else W, N, w_dtype, device, "dW")
+    dB = _out_vector(dB, dW, N, w_dtype, device, "dB")
     lib = load_library()
     ws, ws_bytes, workspace = _workspace(workspace, lib.atb_layer_norm_backward_workspace_bytes(M, N), X)
     _check(lib.atb_layer_norm_backward(M, N, _dtype(X), dY.data_ptr(), lddy, X.data_ptr(), ldx, _dtype(dW), _opt_ptr(W), mean.data_ptr(),
@@ -551,7 +560,7 @@ def atb_gated_ffn(X, Wg, Wu, Wd, act="silu", save=False, Y=None, H=None, G=None,
     Y, ldy = _out_matrix(Y, X, M, D, torch.bfloat16, device, "Y")
     H = _hidden(H, X, M, F, device, "H")
     if save or G is not None or U is not None:
-        G, U = _hidden(G, X, M, F, device, "G"), _hidden(U, X, M, F, device, "U")
+        G, U = _hidden(G, H, M, F, device, "G"), _hidden(U, H, M, F, device, "U")
     lib = load_library()
     ws, ws_bytes, workspace = _workspace(workspace, lib.atb_gated_ffn_workspace_bytes(M, D, F), X)
     _check(lib.atb_gated_ffn(M, D, F, _act(act), X.data_ptr(), ldx, Wg.data_ptr(), Wu.data_ptr(), ldw, Wd.data_ptr(), ldwd, Y.data_ptr(), ldy,
@@ -573,9 +582,9 @@ def atb_gated_ffn_backward(dY, X, Wg, Wu, Wd, H, G, U, act="silu", dX=None, dWg=
         if _matrix(t, M, F, bf16, device, name) != F:
             raise ValueError(f"{name}: contiguous")
     dX, lddx = _out_matrix(dX, X, M, D, bf16, device, "dX")
-    dWg, lddw = _out_matrix(dWg, X, D, F, bf16, device, "dWg")
-    dWu, lddu = _out_matrix(dWu, X, D, F, bf16, device, "dWu")
-    dWd, lddwd = _out_matrix(dWd, X, F, D, bf16, device, "dWd")
+    dWg, lddw = _out_matrix(dWg, Wg, D, F, bf16, device, "dWg")
+    dWu, lddu = _out_matrix(dWu, Wu, D, F, bf16, device, "dWu")
+    dWd, lddwd = _out_matrix(dWd, Wd, F, D, bf16, device, "dWd")
     if lddu != lddw:
         raise ValueError("dWg and dWu need the same row stride")
     lib = load_library()
@@ -606,7 +615,7 @@ def atb_linear_cross_entropy(X, W, labels, ignore_index=-100, loss=None, lse=Non
     import torch
     M, V, D, ldx, ldw, device = _head_shapes(X, W, labels)
     loss = _out_vector(loss, X, M, torch.float32, device, "loss")
-    lse = _out_vector(lse, X, M, torch.float32, device, "lse")
+    lse = _out_vector(lse, loss, M, torch.float32, device, "lse")
     lib = load_library()
     ws, ws_bytes, workspace = _workspace(workspace, lib.atb_linear_cross_entropy_workspace_bytes(M, V, D), X)
     _check(lib.atb_linear_cross_entropy(M, V, D, X.data_ptr(), ldx, W.data_ptr(), ldw, labels.data_ptr(), ignore_index, loss.data_ptr(),
@@ -625,7 +634,7 @@ def atb_linear_cross_entropy_backward(dloss, X, W, labels, lse, ignore_index=-10
     _vector(dloss, M, torch.float32, device, "dloss")
     _vector(lse, M, torch.float32, device, "lse")
     dX, lddx = _out_matrix(dX, X, M, D, torch.bfloat16, device, "dX")
-    dW, lddw = _out_matrix(dW, X, V, D, torch.bfloat16, device, "dW")
+    dW, lddw = _out_matrix(dW, W, V, D, torch.bfloat16, device, "dW")
     lib = load_library()
     ws, ws_bytes, workspace = _workspace(workspace, lib.atb_linear_cross_entropy_backward_workspace_bytes(M, V, D, piece), X)
     _check(lib.atb_linear_cross_entropy_backward(M, V, D, X.data_ptr(), ldx, W.data_ptr(), ldw, labels.data_ptr(), ignore_index,
