@@ -37,7 +37,6 @@ struct MmProblem {
     MmOperand A[2], B[2];
     void* C[3] = {nullptr, nullptr, nullptr};   // bf16 outputs; kMmGlu: h, g, u (g and u may be NULL); kMmGluBackward: dg, du
     int64_t ldc[3] = {0, 0, 0};
-    float* partial = nullptr;         // FP32 sums of the K ranges of a split product (mm_partial_bytes)
     // kMmAccumulate
     float* C32 = nullptr;             // [M][N]
     bool first = true;
@@ -53,12 +52,23 @@ struct MmProblem {
     const float *lse = nullptr, *scale = nullptr;
 };
 
+// The sizes alone, for the plans below.
+inline MmProblem mm_sizes(MmEpilogue epilogue, int64_t M, int64_t N, int64_t K, int k_segs = 1, int n_segs = 1) {
+    MmProblem q;
+    q.epilogue = epilogue; q.M = M; q.N = N; q.K = K; q.k_segs = k_segs; q.n_segs = n_segs;
+    return q;
+}
+
+constexpr int kMmGroup = 3;           // most products of one launch
+
 // Entries of `stats` per row for a product of M x N x K.
 int64_t mm_stats_per_row(int64_t M, int64_t N, int64_t K);
-// Bytes that `partial` needs: 0 where the product is not split along K.
-size_t mm_partial_bytes(MmEpilogue epilogue, int64_t M, int64_t N, int64_t K, int k_segs = 1, int n_segs = 1);
+// Bytes of FP32 sums that a launch of these n products needs room for: 0 where none is split along K.
+size_t mm_partial_bytes(const MmProblem* q, int n);
 
-// Enqueues the product on `stream`.  Pointers 16-byte aligned, leading dimensions multiples of 8 (callers check).
-atb_status_t mm_launch(const MmProblem& p, cudaStream_t stream);
+// Enqueues n <= kMmGroup products that do not depend on one another as one launch (and one more that joins the sums of
+// those that are split along K): any number of kMmStore and kMmAccumulate products, or one of another kind.
+// Pointers 16-byte aligned, leading dimensions multiples of 8 (callers check).  partial: mm_partial_bytes(q, n) bytes.
+atb_status_t mm_launch(const MmProblem* q, int n, void* partial, cudaStream_t stream);
 
 }  // namespace atb

@@ -10,6 +10,9 @@
 // tile's K loop.
 //   pair    256 x 256 tile: each CTA loads its 128 rows of A and half of the columns of B and holds 128 x 256 of C
 //   single  128 x 128 tile: four times as many tiles for outputs that would leave most of the SMs idle
+// Up to three products that do not depend on one another (the gradients of a layer's input and weights) share a launch:
+// their tiles are dealt out as one list, so that one product's last wave is filled by the next one's tiles.  A product
+// of few tiles is cut along K into ranges whose FP32 sums a second kernel joins.
 // Every wait is bounded (see atb_gemm_device.cuh).
 #include <atomic>
 #include <type_traits>
@@ -21,6 +24,7 @@
 namespace {
 
 using namespace glu;
+using atb::kMmGroup;
 
 __device__ unsigned int g_mm_error_flag = 0;
 
@@ -30,20 +34,23 @@ constexpr uint32_t kMmTileBytes = 2 * kMmBoxBytes;      // a CTA's part of A, or
 constexpr int kMmEpiWarps = 8, kMmFirstEpiWarp = 2;
 constexpr int kMmThreads = (kMmFirstEpiWarp + kMmEpiWarps) * 32;
 
-struct MmMaps {
-    CUtensorMap a[2], b[2], c[3];
+// One product of a launch, as the kernel sees it.
+struct MmJob {
+    int64_t M, N;
+    int a_mn, b_mn;                    // operands stored across K
+    int m_tiles, n_tiles, n_segs;      // n_tiles: of one segment
+    int k_steps0, k_steps;             // steps of the first K segment, of both
+    int splits;                        // the K loop is cut into this many ranges, units of work of their own
+    int first_item;                    // of this product in the launch's list of (range, tile)
+    int fp32, add;                     // C in FP32 (the sums of a range, rows split * split_rows on; or C32), added to it
+    int64_t split_rows;
 };
 
 struct MmParams {
-    int64_t M, N;
-    int m_tiles, n_tiles, n_segs;      // n_tiles: of one segment
-    int k_steps0, k_steps;             // steps of the first K segment, of both
+    MmJob job[kMmGroup];
+    int n_jobs, items;
     unsigned int* error_flag;
-    int splits;                        // the K loop is cut into this many ranges, units of work of their own
-    int64_t split_rows;                // kMmAccumulate: rows of the output between the sums of one range and the next
-    int add;                           // kMmAccumulate: added to the output
     int act, save;
-    const __nv_bfloat16 *G, *U;
     const int64_t* labels;
     int64_t ignore_index, col0;
     float2* stats;
@@ -52,18 +59,33 @@ struct MmParams {
     const float *lse, *scale;
 };
 
-struct MmJoin {
-    int64_t M, N, cols, split_rows;
-    int n_segs, splits, act, add;
+// Tensor maps: product j has A at a[2 j], a[2 j + 1] (K segments), B and C alike (segments).  The epilogues of a single product
+// use c[0 .. 3]: h, g, u; dg, du, g, u; dl.
+template <int JOBS>
+struct MmMaps {
+    CUtensorMap a[2 * JOBS], b[2 * JOBS], c[JOBS == 1 ? 4 : 2 * JOBS];
+};
+
+struct MmJoinJob {
+    int64_t M, N, cols, split_rows, first;       // first: of this product in the list of groups of eight columns
+    int n_segs, splits, add;
     const float* src;
     void* C[3];
     int64_t ldc[3];
     float* C32;
+};
+struct MmJoin {
+    MmJoinJob job[kMmGroup];
+    int n_jobs, act;
+    int64_t all;
     const __nv_bfloat16 *G, *U;
 };
 
+constexpr int kMmPlain = 100;          // kMmStore and kMmAccumulate: one kernel
+
 template <bool PAIR, int EPI>
 struct MmCfg {
+    static constexpr int JOBS = EPI == kMmPlain ? kMmGroup : 1;
     static constexpr int BN = PAIR ? 256 : 128;             // accumulator columns
     static constexpr int TILE_M = PAIR ? 256 : 128;
     static constexpr bool DUAL = EPI == atb::kMmGlu;        // half of the columns from B[0], half from B[1]
@@ -74,7 +96,7 @@ struct MmCfg {
     static constexpr uint32_t STAGE_BYTES = 2 * kMmTileBytes;
     static constexpr uint32_t BOX_OFF = STAGES * STAGE_BYTES;
     static constexpr uint32_t BAR_OFF = BOX_OFF + kMmEpiWarps * BOXES * kEpilogueBoxBytes;
-    static constexpr uint32_t SMEM_BYTES = 1024 + BAR_OFF + 8 * (2 * STAGES + 4) + 16;
+    static constexpr uint32_t SMEM_BYTES = 1024 + BAR_OFF + 8 * (2 * STAGES + 4 + kMmEpiWarps) + 16;
     static_assert(SMEM_BYTES <= kSmemBudget, "shared memory");
 };
 
@@ -97,27 +119,65 @@ __device__ __forceinline__ void glu_backward_pair(uint32_t gw, uint32_t uw, floa
 // added to memory by one, which clips at the edges of the output.
 template <int BOXES>
 struct BoxWriter {
-    uint32_t base;
+    uint32_t base, bar;                    // the boxes; barrier of the loads into them
     int lane, next = 0;
-    __device__ BoxWriter(uint32_t b, int l) : base(b), lane(l) {}
+    uint32_t phase = 0;
+    __device__ BoxWriter(uint32_t b, uint32_t bar_, int l) : base(b), bar(bar_), lane(l) {}
     __device__ __forceinline__ void put(const CUtensorMap* map, const uint32_t (&o)[32], int64_t col, int64_t row0, bool inside, bool add = false) {
         if (lane == 0) tma_store_wait_read<BOXES - 1>();       // the store that last used this box has read it
         __syncwarp();
-        const uint32_t box = base + next * kEpilogueBoxBytes, row = box + lane * 128, sw = lane & 7;
+        write(next, o);
+        if (lane == 0) {
+            if (inside) {
+                if (add) tma_reduce_add_2d(map, box(next), static_cast<int>(col), static_cast<int>(row0));
+                else tma_store_2d(map, box(next), static_cast<int>(col), static_cast<int>(row0));
+            }
+            tma_store_commit();                                // an empty group keeps the count of groups per box
+        }
+        next = next + 1 == BOXES ? 0 : next + 1;
+    }
+    // The other direction: 64 columns of two inputs into the two boxes, and what becomes of them out of the same boxes.
+    __device__ __forceinline__ void fetch(const CUtensorMap* m0, const CUtensorMap* m1, int64_t col, int64_t row0) {
+        if (lane == 0) {
+            tma_store_wait_read<0>();
+            mbar_arrive_expect_tx(bar, 2 * kEpilogueBoxBytes);
+            tma_load_2d(box(0), m0, static_cast<int>(col), static_cast<int>(row0), bar);
+            tma_load_2d(box(1), m1, static_cast<int>(col), static_cast<int>(row0), bar);
+        }
+        __syncwarp();
+    }
+    __device__ __forceinline__ bool fetched(const Ctx& cx) {
+        const bool ok = wait_bar(cx, bar, phase, 0x202);
+        phase ^= 1u;
+        next = 0;
+        return ok;
+    }
+    // Columns 32 part .. + 31 of this lane's row (packed bf16).
+    __device__ __forceinline__ void read(int b, int part, uint32_t (&v)[16]) const {
+        const uint32_t row = box(b) + lane * 128, sw = lane & 7;
+#pragma unroll
+        for (int j = 0; j < 4; ++j)
+            asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(v[4 * j]), "=r"(v[4 * j + 1]), "=r"(v[4 * j + 2]), "=r"(v[4 * j + 3])
+                         : "r"(row + ((static_cast<uint32_t>(4 * part + j) ^ sw) << 4)) : "memory");
+    }
+    __device__ __forceinline__ void put_in_place(const CUtensorMap* map, const uint32_t (&o)[32], int64_t col, int64_t row0) {
+        write(next, o);
+        if (lane == 0) {
+            tma_store_2d(map, box(next), static_cast<int>(col), static_cast<int>(row0));
+            tma_store_commit();
+        }
+        ++next;
+    }
+private:
+    __device__ __forceinline__ uint32_t box(int b) const { return base + b * kEpilogueBoxBytes; }
+    __device__ __forceinline__ void write(int b, const uint32_t (&o)[32]) const {
+        const uint32_t row = box(b) + lane * 128, sw = lane & 7;
 #pragma unroll
         for (int j = 0; j < 8; ++j)
             asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(row + ((static_cast<uint32_t>(j) ^ sw) << 4)),
                          "r"(o[4 * j]), "r"(o[4 * j + 1]), "r"(o[4 * j + 2]), "r"(o[4 * j + 3]) : "memory");
         fence_proxy_async_smem();
         __syncwarp();
-        if (lane == 0) {
-            if (inside) {
-                if (add) tma_reduce_add_2d(map, box, static_cast<int>(col), static_cast<int>(row0));
-                else tma_store_2d(map, box, static_cast<int>(col), static_cast<int>(row0));
-            }
-            tma_store_commit();                                // an empty group keeps the count of groups per box
-        }
-        next = next + 1 == BOXES ? 0 : next + 1;
     }
 };
 
@@ -125,35 +185,36 @@ struct BoxWriter {
 // Rows row0 .. row0 + 31 (one per lane); t_addr: the warp's lanes of the tile's accumulator, column 0; half: which of
 // the tile's column groups this warp has; col0: first column of the tile in C.
 template <class C, int EPI>
-__device__ __forceinline__ void mm_epilogue(const MmMaps& tm, const MmParams& p, BoxWriter<C::BOXES>& out, uint32_t t_addr, int half,
-                                            int64_t row0, int64_t col0, int seg, int split, int lane) {
+__device__ __forceinline__ void mm_epilogue(const MmMaps<C::JOBS>& tm, const MmParams& p, const MmJob& jb, int c_map, BoxWriter<C::BOXES>& out,
+                                            uint32_t t_addr, int half, int64_t row0, int64_t col0, int split, int lane, const Ctx& cx) {
     const int64_t row = row0 + lane;
-    const bool row_in = row < p.M, warp_in = row0 < p.M;
+    const bool row_in = row < jb.M, warp_in = row0 < jb.M;
     col0 += half * C::COLS;
     t_addr += half * C::COLS;
-    if constexpr (EPI == atb::kMmStore) {
+    if constexpr (EPI == kMmPlain) {
+        if (!jb.fp32) {
 #pragma unroll 1
-        for (int c = 0; c < C::COLS; c += 64) {
-            uint32_t v[32], w[32], o[32];
-            tmem_ld_32x32b_x32(t_addr + c, v);
-            tmem_ld_32x32b_x32(t_addr + c + 32, w);
-            tmem_ld_wait_for(v);
-            tmem_ld_wait_for(w);
+            for (int c = 0; c < C::COLS; c += 64) {
+                uint32_t v[32], w[32], o[32];
+                tmem_ld_32x32b_x32(t_addr + c, v);
+                tmem_ld_32x32b_x32(t_addr + c + 32, w);
+                tmem_ld_wait_for(v);
+                tmem_ld_wait_for(w);
 #pragma unroll
-            for (int e = 0; e < 16; ++e) {
-                o[e] = pack_bf16(__uint_as_float(v[2 * e]), __uint_as_float(v[2 * e + 1]));
-                o[16 + e] = pack_bf16(__uint_as_float(w[2 * e]), __uint_as_float(w[2 * e + 1]));
+                for (int e = 0; e < 16; ++e) {
+                    o[e] = pack_bf16(__uint_as_float(v[2 * e]), __uint_as_float(v[2 * e + 1]));
+                    o[16 + e] = pack_bf16(__uint_as_float(w[2 * e]), __uint_as_float(w[2 * e + 1]));
+                }
+                out.put(&tm.c[c_map], o, col0 + c, row0, warp_in && col0 + c < jb.N);
             }
-            out.put(&tm.c[seg], o, col0 + c, row0, warp_in && col0 + c < p.N);
-        }
-    } else if constexpr (EPI == atb::kMmAccumulate) {
-        // FP32: rows of this K range's sums (see MmParams::split_rows), or added to what is there
+        } else {
 #pragma unroll 1
-        for (int c = 0; c < C::COLS; c += 32) {
-            uint32_t v[32];
-            tmem_ld_32x32b_x32(t_addr + c, v);
-            tmem_ld_wait_for(v);
-            out.put(&tm.c[seg], v, col0 + c, split * p.split_rows + row0, warp_in && col0 + c < p.N, p.add);
+            for (int c = 0; c < C::COLS; c += 32) {
+                uint32_t v[32];
+                tmem_ld_32x32b_x32(t_addr + c, v);
+                tmem_ld_wait_for(v);
+                out.put(&tm.c[c_map], v, col0 + c, split * jb.split_rows + row0, warp_in && col0 + c < jb.N, jb.add);
+            }
         }
     } else if constexpr (EPI == atb::kMmGlu) {
         // accumulator columns 0 .. TILE_N - 1 hold g, the next TILE_N hold u
@@ -176,7 +237,7 @@ __device__ __forceinline__ void mm_epilogue(const MmMaps& tm, const MmParams& p,
                     ou[16 * part + e] = pack_bf16(__uint_as_float(u[2 * e]), __uint_as_float(u[2 * e + 1]));
                 }
             }
-            const bool inside = warp_in && col0 < p.N;
+            const bool inside = warp_in && col0 < jb.N;
             out.put(&tm.c[0], h, col0, row0, inside);
             if (p.save) {
                 out.put(&tm.c[1], og, col0, row0, inside);
@@ -184,35 +245,29 @@ __device__ __forceinline__ void mm_epilogue(const MmMaps& tm, const MmParams& p,
             }
         });
     } else if constexpr (EPI == atb::kMmGluBackward) {
+        // g and u of 64 columns arrive in the two boxes (the first ones fetched before the accumulator was waited for); a lane
+        // replaces its row in them by dg and du
+        if (!warp_in) return;
         with_act(p.act, [&](auto act) {
 #pragma unroll 1
-            for (int c = 0; c < C::COLS; c += 64) {
+            for (int c = 0; c < C::COLS && col0 + c < jb.N; c += 64) {
+                if (c > 0) out.fetch(&tm.c[2], &tm.c[3], col0 + c, row0);
+                if (!out.fetched(cx)) return;
                 uint32_t og[32], ou[32];
 #pragma unroll
                 for (int part = 0; part < 2; ++part) {
-                    const int64_t col = col0 + c + 32 * part;
-                    uint32_t dh[32];
+                    uint32_t dh[32], g[16], u[16];
                     tmem_ld_32x32b_x32(t_addr + c + 32 * part, dh);
-                    uint4 g[4], u[4];
-#pragma unroll
-                    for (int j = 0; j < 4; ++j) {
-                        g[j] = u[j] = make_uint4(0, 0, 0, 0);
-                        if (row_in && col + 8 * j < p.N) {         // N is a multiple of 8
-                            g[j] = *reinterpret_cast<const uint4*>(p.G + row * p.N + col + 8 * j);
-                            u[j] = *reinterpret_cast<const uint4*>(p.U + row * p.N + col + 8 * j);
-                        }
-                    }
+                    out.read(0, part, g);
+                    out.read(1, part, u);
                     tmem_ld_wait_for(dh);
 #pragma unroll
-                    for (int e = 0; e < 16; ++e) {
-                        const uint32_t gw = reinterpret_cast<const uint32_t*>(g)[e], uw = reinterpret_cast<const uint32_t*>(u)[e];
-                        glu_backward_pair<act.value>(gw, uw, __uint_as_float(dh[2 * e]), __uint_as_float(dh[2 * e + 1]), og[16 * part + e],
+                    for (int e = 0; e < 16; ++e)
+                        glu_backward_pair<act.value>(g[e], u[e], __uint_as_float(dh[2 * e]), __uint_as_float(dh[2 * e + 1]), og[16 * part + e],
                                                      ou[16 * part + e]);
-                    }
                 }
-                const bool inside = warp_in && col0 + c < p.N;
-                out.put(&tm.c[0], og, col0 + c, row0, inside);
-                out.put(&tm.c[1], ou, col0 + c, row0, inside);
+                out.put_in_place(&tm.c[0], og, col0 + c, row0);
+                out.put_in_place(&tm.c[1], ou, col0 + c, row0);
             }
         });
     } else if constexpr (EPI == atb::kMmRowStats) {
@@ -225,7 +280,7 @@ __device__ __forceinline__ void mm_epilogue(const MmMaps& tm, const MmParams& p,
             uint32_t v[32];
             tmem_ld_32x32b_x32(t_addr + c, v);
             tmem_ld_wait_for(v);
-            const int64_t left = p.N - (col0 + c);             // columns of this group inside the vocabulary
+            const int64_t left = jb.N - (col0 + c);             // columns of this group inside the vocabulary
             if (left <= 0) continue;
             const bool here = label >= c && label < c + 32 && label - c < left;
             if (__any_sync(0xFFFFFFFFu, here)) {
@@ -248,7 +303,7 @@ __device__ __forceinline__ void mm_epilogue(const MmMaps& tm, const MmParams& p,
             for (int e = 0; e < 32; ++e) s += exp2_fast((__uint_as_float(v[e]) - ref) * kLog2e);
             m = top;
         }
-        if (row_in && col0 < p.N) p.stats[row * p.stats_ld + col0 / C::COLS] = make_float2(m, s);
+        if (row_in && col0 < jb.N) p.stats[row * p.stats_ld + col0 / C::COLS] = make_float2(m, s);
     } else {
         int64_t label = -1;
         float lse = 0.f, scale = 0.f;
@@ -278,7 +333,7 @@ __device__ __forceinline__ void mm_epilogue(const MmMaps& tm, const MmParams& p,
 #pragma unroll
                 for (int e = 0; e < 16; ++e) o[16 * part + e] = pack_bf16(__uint_as_float(v[2 * e]), __uint_as_float(v[2 * e + 1]));
             }
-            out.put(&tm.c[0], o, col0 + c, row0, warp_in && col0 + c < p.N);
+            out.put(&tm.c[0], o, col0 + c, row0, warp_in && col0 + c < jb.N);
         }
     }
 }
@@ -290,31 +345,47 @@ __device__ __forceinline__ void mm_tma(uint32_t dst, const CUtensorMap* m, int x
     else tma_load_2d(dst, m, x, y, bar);
 }
 // 128 rows (or columns) from mn0 on, K-elements k0 .. k0 + 63: two boxes.
-template <bool PAIR, bool MN_MAJOR>
-__device__ __forceinline__ void mm_load(uint32_t dst, const CUtensorMap* m0, const CUtensorMap* m1, int mn0, int mn1, int k0, uint32_t bar) {
-    mm_tma<PAIR>(dst, m0, MN_MAJOR ? mn0 : k0, MN_MAJOR ? k0 : mn0, bar);
-    mm_tma<PAIR>(dst + kMmBoxBytes, m1, MN_MAJOR ? mn1 : k0, MN_MAJOR ? k0 : mn1, bar);
+template <bool PAIR>
+__device__ __forceinline__ void mm_load(uint32_t dst, const CUtensorMap* m0, const CUtensorMap* m1, bool mn_major, int mn0, int mn1, int k0, uint32_t bar) {
+    mm_tma<PAIR>(dst, m0, mn_major ? mn0 : k0, mn_major ? k0 : mn0, bar);
+    mm_tma<PAIR>(dst + kMmBoxBytes, m1, mn_major ? mn1 : k0, mn_major ? k0 : mn1, bar);
 }
-// First K-step of a range.
-__device__ __forceinline__ int mm_split_begin(const MmParams& p, int split) {
-    return static_cast<int>(static_cast<int64_t>(p.k_steps) * split / p.splits);
-}
-// Descriptor of the 16 K-elements from kk * 16 on of a 128-wide operand tile (see umma_smem_desc_sw128).
-template <bool MN_MAJOR>
-__device__ __forceinline__ uint64_t mm_desc(uint32_t tile, int kk) {
-    return MN_MAJOR ? umma_smem_desc_sw128(tile + kk * 2048, kMmBoxBytes, 1024) : umma_smem_desc_sw128(tile + kk * 32, 16, 1024);
+// Descriptor of a 128-wide operand tile (see umma_smem_desc_sw128); 16 K-elements on it grows by mm_desc_step.
+__device__ __forceinline__ uint64_t mm_desc(uint32_t tile, bool mn_major) { return umma_smem_desc_sw128(tile, mn_major ? kMmBoxBytes : 16u, 1024); }
+__device__ __forceinline__ uint32_t mm_desc_step(bool mn_major) { return (mn_major ? 2048u : 32u) >> 4; }
+
+// One unit of work: a tile of a product and a range of its K-steps.
+struct MmItem {
+    int job, mt, nt, seg, split, k_begin, k_end;
+};
+template <int JOBS>
+__device__ __forceinline__ MmItem mm_item(const MmParams& p, int item) {
+    MmItem w;
+    w.job = 0;
+    if constexpr (JOBS > 1)
+        while (w.job + 1 < p.n_jobs && item >= p.job[w.job + 1].first_item) ++w.job;
+    const MmJob& jb = p.job[w.job];
+    const int all_n = jb.n_tiles * jb.n_segs, tiles = jb.m_tiles * all_n;
+    item -= jb.first_item;
+    w.split = item / tiles;
+    tile_coords<8>(item - w.split * tiles, jb.m_tiles, all_n, w.mt, w.nt);
+    w.seg = w.nt >= jb.n_tiles ? 1 : 0;
+    w.nt -= w.seg * jb.n_tiles;
+    w.k_begin = static_cast<int>(static_cast<int64_t>(jb.k_steps) * w.split / jb.splits);
+    w.k_end = static_cast<int>(static_cast<int64_t>(jb.k_steps) * (w.split + 1) / jb.splits);
+    return w;
 }
 
-template <bool PAIR, bool A_MN, bool B_MN, int EPI>
+template <bool PAIR, int EPI>
 __global__ void __launch_bounds__(kMmThreads, 1)
-bf16_mm_kernel(const __grid_constant__ MmMaps tm, const MmParams p) {
+bf16_mm_kernel(const __grid_constant__ MmMaps<MmCfg<PAIR, EPI>::JOBS> tm, const __grid_constant__ MmParams p) {
     using C = MmCfg<PAIR, EPI>;
     extern __shared__ uint8_t smem_raw[];
     const uint32_t smem_base = (smem_u32(smem_raw) + 1023u) & ~1023u;
     const uint32_t bar_base = smem_base + C::BAR_OFF;
     const uint32_t full = bar_base, empty = full + 8 * C::STAGES;
-    const uint32_t acc_full = empty + 8 * C::STAGES, acc_empty = acc_full + 16;
-    const uint32_t misc = acc_empty + 16;                  // [0]: TMEM base, [1]: abort flag
+    const uint32_t acc_full = empty + 8 * C::STAGES, acc_empty = acc_full + 16, box_bar = acc_empty + 16;
+    const uint32_t misc = box_bar + 8 * kMmEpiWarps;       // [0]: TMEM base, [1]: abort flag
     volatile uint32_t* const misc_gen = reinterpret_cast<volatile uint32_t*>(smem_raw + (misc - smem_u32(smem_raw)));
 
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
@@ -324,6 +395,7 @@ bf16_mm_kernel(const __grid_constant__ MmMaps tm, const MmParams p) {
     if (threadIdx.x == 0) {
         for (int i = 0; i < C::STAGES; ++i) { mbar_init(full + 8 * i, 1); mbar_init(empty + 8 * i, 1); }
         for (int i = 0; i < 2; ++i) { mbar_init(acc_full + 8 * i, 1); mbar_init(acc_empty + 8 * i, kMmEpiWarps * (PAIR ? 2 : 1)); }
+        for (int i = 0; i < kMmEpiWarps; ++i) mbar_init(box_bar + 8 * i, 1);
         misc_gen[1] = 0u;
         fence_mbar_init();
         prefetch_tensormap(&tm.a[0]);
@@ -339,11 +411,10 @@ bf16_mm_kernel(const __grid_constant__ MmMaps tm, const MmParams p) {
     if constexpr (PAIR) cluster_sync_all();                // the peer's barriers exist before anything arrives on them
     tcgen05_fence_after_sync();
     const uint32_t tmem_base = misc_gen[0];
-
-    const int all_n = p.n_tiles * p.n_segs, tiles = p.m_tiles * all_n, total = tiles * p.splits;
     // what a kernel before this one on the stream wrote may be read from here on
     grid_dependency_wait();
     grid_dependency_launch();
+
     const int unit = PAIR ? blockIdx.x >> 1 : blockIdx.x, units = PAIR ? gridDim.x >> 1 : gridDim.x;
 
     if (warp == 0) {
@@ -352,29 +423,29 @@ bf16_mm_kernel(const __grid_constant__ MmMaps tm, const MmParams p) {
             Ring r;
             bool ok = true;
             int it = 0;
-            for (int tile = unit; ok && tile < total; tile += units, ++it) {
-                int mt, nt;
-                const int split = tile / tiles, k_begin = mm_split_begin(p, split), k_end = mm_split_begin(p, split + 1);
-                tile_coords<8>(tile - split * tiles, p.m_tiles, all_n, mt, nt);
-                const int seg = nt >= p.n_tiles ? 1 : 0;
-                nt -= seg * p.n_tiles;
-                const int m0 = mt * C::TILE_M + static_cast<int>(rank) * 128;
+            for (int item = unit; ok && item < p.items; item += units, ++it) {
+                const MmItem w = mm_item<C::JOBS>(p, item);
+                const MmJob& jb = p.job[w.job];
+                const bool a_mn = jb.a_mn, b_mn = jb.b_mn;
+                const CUtensorMap* const ta = &tm.a[2 * w.job];
+                const CUtensorMap* const tb = &tm.b[2 * w.job];
+                const int m0 = w.mt * C::TILE_M + static_cast<int>(rank) * 128;
                 // where this CTA's two boxes of B start: halves of the gate's and the up projection's columns, or
                 // 128 consecutive columns
-                const int n0 = C::DUAL ? nt * C::TILE_N : nt * C::TILE_N + static_cast<int>(rank) * 128;
+                const int n0 = C::DUAL ? w.nt * C::TILE_N : w.nt * C::TILE_N + static_cast<int>(rank) * 128;
                 const int n1 = (C::DUAL && !PAIR) ? n0 : n0 + 64;
-                for (int k0 = k_begin; k0 < k_end; ++k0) {
-                    int k = serpentine_k(it, k0, k_begin, k_end);
-                    const int kseg = k >= p.k_steps0 ? 1 : 0;
-                    k -= kseg * p.k_steps0;
+                for (int k0 = w.k_begin; k0 < w.k_end; ++k0) {
+                    int k = serpentine_k(it, k0, w.k_begin, w.k_end);
+                    const int kseg = k >= jb.k_steps0 ? 1 : 0;
+                    k -= kseg * jb.k_steps0;
                     if (!(ok = wait_bar_t<true, PAIR>(cx, empty + 8 * r.stage, r.phase ^ 1u, 0x001))) break;
                     if (rank == 0) mbar_arrive_expect_tx(full + 8 * r.stage, C::STAGE_BYTES * (PAIR ? 2 : 1));
                     const uint32_t bar = PAIR ? mapa_shared(full + 8 * r.stage, 0) : full + 8 * r.stage;
                     const uint32_t dst = smem_base + r.stage * C::STAGE_BYTES;
-                    const int b0 = C::DUAL ? (PAIR ? static_cast<int>(rank) : 0) : (seg | kseg);
-                    const int b1 = C::DUAL ? (PAIR ? static_cast<int>(rank) : 1) : (seg | kseg);
-                    mm_load<PAIR, A_MN>(dst, &tm.a[kseg], &tm.a[kseg], m0, m0 + 64, k * kMmKStep, bar);
-                    mm_load<PAIR, B_MN>(dst + kMmTileBytes, &tm.b[b0], &tm.b[b1], n0, n1, k * kMmKStep, bar);
+                    const int b0 = C::DUAL ? (PAIR ? static_cast<int>(rank) : 0) : (w.seg | kseg);
+                    const int b1 = C::DUAL ? (PAIR ? static_cast<int>(rank) : 1) : (w.seg | kseg);
+                    mm_load<PAIR>(dst, ta + kseg, ta + kseg, a_mn, m0, m0 + 64, k * kMmKStep, bar);
+                    mm_load<PAIR>(dst + kMmTileBytes, tb + b0, tb + b1, b_mn, n0, n1, k * kMmKStep, bar);
                     r.advance(C::STAGES);
                 }
             }
@@ -382,27 +453,30 @@ bf16_mm_kernel(const __grid_constant__ MmMaps tm, const MmParams p) {
     } else if (warp == 1) {
         // ================================ UMMA issuer =================================
         if (rank == 0 && elect_one()) {
-            constexpr uint32_t idesc = umma_idesc_bf16_f32(PAIR ? 256 : 128, C::BN, A_MN, B_MN);
             Ring r;
             bool ok = true;
             int it = 0;
-            for (int tile = unit; ok && tile < total; tile += units, ++it) {
-                const int acc = it & 1;
+            for (int item = unit; ok && item < p.items; item += units, ++it) {
+                const MmItem w = mm_item<C::JOBS>(p, item);
+                const bool a_mn = p.job[w.job].a_mn, b_mn = p.job[w.job].b_mn;
+                const uint32_t idesc = umma_idesc_bf16_f32(PAIR ? 256 : 128, C::BN, a_mn, b_mn);
+                const uint32_t a_step = mm_desc_step(a_mn), b_step = mm_desc_step(b_mn);
+                const int acc = it & 1, steps = w.k_end - w.k_begin;
                 const uint32_t acc_phase = static_cast<uint32_t>(it >> 1) & 1u;
                 // the epilogue has drained this accumulator (the tile before the previous one)
                 if (!(ok = wait_bar_t<true, PAIR>(cx, acc_empty + 8 * acc, acc_phase ^ 1u, 0x102))) break;
-                const int split = tile / tiles, steps = mm_split_begin(p, split + 1) - mm_split_begin(p, split);
                 for (int k = 0; k < steps; ++k) {
                     if (!(ok = wait_bar_t<true, PAIR>(cx, full + 8 * r.stage, r.phase, 0x101))) break;
                     tcgen05_fence_after_sync();
-                    const uint32_t as = smem_base + r.stage * C::STAGE_BYTES, bs = as + kMmTileBytes;
+                    const uint32_t as = smem_base + r.stage * C::STAGE_BYTES;
+                    const uint64_t a_desc = mm_desc(as, a_mn), b_desc = mm_desc(as + kMmTileBytes, b_mn);
 #pragma unroll
                     for (int kk = 0; kk < kMmKStep / 16; ++kk) {
                         const uint32_t accumulate = (k > 0 || kk > 0) ? 1u : 0u;
                         if constexpr (PAIR)
-                            umma_f16_ss_pair(tmem_base + acc * C::BN, mm_desc<A_MN>(as, kk), mm_desc<B_MN>(bs, kk), idesc, accumulate);
+                            umma_f16_ss_pair(tmem_base + acc * C::BN, a_desc + kk * a_step, b_desc + kk * b_step, idesc, accumulate);
                         else
-                            umma_f16_ss(tmem_base + acc * C::BN, mm_desc<A_MN>(as, kk), mm_desc<B_MN>(bs, kk), idesc, accumulate);
+                            umma_f16_ss(tmem_base + acc * C::BN, a_desc + kk * a_step, b_desc + kk * b_step, idesc, accumulate);
                     }
                     if constexpr (PAIR) umma_commit_pair(empty + 8 * r.stage, 3); else umma_commit(empty + 8 * r.stage);
                     r.advance(C::STAGES);
@@ -413,22 +487,22 @@ bf16_mm_kernel(const __grid_constant__ MmMaps tm, const MmParams p) {
         }
     } else {
         // ================================ epilogue ====================================
-        const int q = warp & 3, half = (warp - kMmFirstEpiWarp) >> 2;
-        BoxWriter<C::BOXES> out(smem_base + C::BOX_OFF + static_cast<uint32_t>(warp - kMmFirstEpiWarp) * C::BOXES * kEpilogueBoxBytes, lane);
+        const int e = warp - kMmFirstEpiWarp, q = warp & 3, half = e >> 2;
+        BoxWriter<C::BOXES> out(smem_base + C::BOX_OFF + static_cast<uint32_t>(e) * C::BOXES * kEpilogueBoxBytes, box_bar + 8 * e, lane);
         int it = 0;
         bool ok = true;
-        for (int tile = unit; ok && tile < total; tile += units, ++it) {
-            int mt, nt;
-            const int split = tile / tiles;
-            tile_coords<8>(tile - split * tiles, p.m_tiles, all_n, mt, nt);
-            const int seg = nt >= p.n_tiles ? 1 : 0;
-            nt -= seg * p.n_tiles;
+        for (int item = unit; ok && item < p.items; item += units, ++it) {
+            const MmItem w = mm_item<C::JOBS>(p, item);
+            const MmJob& jb = p.job[w.job];
+            const int64_t row0 = static_cast<int64_t>(w.mt) * C::TILE_M + rank * 128 + q * 32, col0 = static_cast<int64_t>(w.nt) * C::TILE_N;
             const int acc = it & 1;
+            if constexpr (EPI == atb::kMmGluBackward)
+                if (row0 < jb.M && col0 + half * C::COLS < jb.N) out.fetch(&tm.c[2], &tm.c[3], col0 + half * C::COLS, row0);
             if (!(ok = wait_bar_t<false, PAIR>(cx, acc_full + 8 * acc, static_cast<uint32_t>(it >> 1) & 1u, 0x201))) break;
             tcgen05_fence_after_sync();
             if (half * C::COLS < C::TILE_N)
-                mm_epilogue<C, EPI>(tm, p, out, tmem_base + (static_cast<uint32_t>(q * 32) << 16) + static_cast<uint32_t>(acc * C::BN), half,
-                                    static_cast<int64_t>(mt) * C::TILE_M + rank * 128 + q * 32, static_cast<int64_t>(nt) * C::TILE_N, seg, split, lane);
+                mm_epilogue<C, EPI>(tm, p, jb, 2 * w.job + w.seg, out, tmem_base + (static_cast<uint32_t>(q * 32) << 16) + static_cast<uint32_t>(acc * C::BN),
+                                    half, row0, col0, w.split, lane, cx);
             tcgen05_fence_before_sync();
             __syncwarp();
             if (lane == 0) {
@@ -467,46 +541,52 @@ bool operand_map(CUtensorMap* m, const atb::MmOperand& o, bool mn_major, int64_t
                        static_cast<uint64_t>(mn_major ? K : mn), static_cast<uint64_t>(o.ld) * 2, 64, 64, CU_TENSOR_MAP_SWIZZLE_128B);
 }
 
-// Joins the K ranges of a split product: sums of the ranges in their order, then what the epilogue would have done.
+// Joins the K ranges of split products: sums of the ranges in their order, then what the epilogue would have done.
 // src: [splits][split_rows][cols]; eight columns per thread.
 template <int EPI>
-__global__ void __launch_bounds__(256) bf16_mm_join_kernel(const MmJoin p) {
+__global__ void __launch_bounds__(256) bf16_mm_join_kernel(const __grid_constant__ MmJoin p) {
     grid_dependency_wait();
     grid_dependency_launch();
-    const int64_t per_row = p.N / 8, all = p.M * per_row * p.n_segs;
-    const auto sum = [&](int64_t m, int64_t col, float (&v)[8]) {
-        const float* src = p.src + m * p.cols + col;
-        float4 a = *reinterpret_cast<const float4*>(src), b = *reinterpret_cast<const float4*>(src + 4);
-        for (int i = 1; i < p.splits; ++i) {
-            src += p.split_rows * p.cols;
-            const float4 c = *reinterpret_cast<const float4*>(src), d = *reinterpret_cast<const float4*>(src + 4);
-            a.x += c.x; a.y += c.y; a.z += c.z; a.w += c.w;
-            b.x += d.x; b.y += d.y; b.z += d.z; b.w += d.w;
-        }
-        v[0] = a.x; v[1] = a.y; v[2] = a.z; v[3] = a.w;
-        v[4] = b.x; v[5] = b.y; v[6] = b.z; v[7] = b.w;
-    };
     const auto put = [](void* C, int64_t at, const uint32_t (&o)[4]) {
         *reinterpret_cast<uint4*>(static_cast<__nv_bfloat16*>(C) + at) = make_uint4(o[0], o[1], o[2], o[3]);
     };
-    for (int64_t i = static_cast<int64_t>(blockIdx.x) * 256 + threadIdx.x; i < all; i += static_cast<int64_t>(gridDim.x) * 256) {
-        const int64_t m = i / (per_row * p.n_segs), j = i - m * per_row * p.n_segs;
-        const int seg = j >= per_row ? 1 : 0;
-        const int64_t n = (j - seg * per_row) * 8;
+    for (int64_t i = static_cast<int64_t>(blockIdx.x) * 256 + threadIdx.x; i < p.all; i += static_cast<int64_t>(gridDim.x) * 256) {
+        int j = 0;
+        if constexpr (EPI == kMmPlain)
+            while (j + 1 < p.n_jobs && i >= p.job[j + 1].first) ++j;
+        const MmJoinJob& q = p.job[j];
+        const auto sum = [&](int64_t m, int64_t col, float (&v)[8]) {
+            const float* src = q.src + m * q.cols + col;
+            float4 a = *reinterpret_cast<const float4*>(src), b = *reinterpret_cast<const float4*>(src + 4);
+            for (int s = 1; s < q.splits; ++s) {
+                src += q.split_rows * q.cols;
+                const float4 c = *reinterpret_cast<const float4*>(src), d = *reinterpret_cast<const float4*>(src + 4);
+                a.x += c.x; a.y += c.y; a.z += c.z; a.w += c.w;
+                b.x += d.x; b.y += d.y; b.z += d.z; b.w += d.w;
+            }
+            v[0] = a.x; v[1] = a.y; v[2] = a.z; v[3] = a.w;
+            v[4] = b.x; v[5] = b.y; v[6] = b.z; v[7] = b.w;
+        };
+        const int64_t per_row = q.N / 8, at = i - q.first;
+        const int64_t m = at / (per_row * q.n_segs), g8 = at - m * per_row * q.n_segs;
+        const int seg = g8 >= per_row ? 1 : 0;
+        const int64_t n = (g8 - seg * per_row) * 8;
         float v[8];
-        sum(m, seg * p.N + n, v);
+        sum(m, seg * q.N + n, v);
         uint32_t o[4];
-        if constexpr (EPI == atb::kMmStore) {
+        if constexpr (EPI == kMmPlain) {
+            if (q.C32) {
+                float* dst = q.C32 + m * q.N + n;
 #pragma unroll
-            for (int e = 0; e < 4; ++e) o[e] = pack_bf16(v[2 * e], v[2 * e + 1]);
-            put(p.C[seg], m * p.ldc[seg] + n, o);
-        } else if constexpr (EPI == atb::kMmAccumulate) {
-            float* dst = p.C32 + m * p.N + n;
+                for (int e = 0; e < 8; ++e) dst[e] = q.add ? dst[e] + v[e] : v[e];
+            } else {
 #pragma unroll
-            for (int e = 0; e < 8; ++e) dst[e] = p.add ? dst[e] + v[e] : v[e];
+                for (int e = 0; e < 4; ++e) o[e] = pack_bf16(v[2 * e], v[2 * e + 1]);
+                put(q.C[seg], m * q.ldc[seg] + n, o);
+            }
         } else if constexpr (EPI == atb::kMmGlu) {
             float u[8];
-            sum(m, p.N + n, u);
+            sum(m, q.N + n, u);
             with_act(p.act, [&](auto act) {
 #pragma unroll
                 for (int e = 0; e < 4; ++e) {
@@ -516,63 +596,103 @@ __global__ void __launch_bounds__(256) bf16_mm_join_kernel(const MmJoin p) {
                     o[e] = pack_bf16(a0 * u[2 * e], a1 * u[2 * e + 1]);
                 }
             });
-            put(p.C[0], m * p.ldc[0] + n, o);
-            if (p.C[1]) {
+            put(q.C[0], m * q.ldc[0] + n, o);
+            if (q.C[1]) {
 #pragma unroll
                 for (int e = 0; e < 4; ++e) o[e] = pack_bf16(v[2 * e], v[2 * e + 1]);
-                put(p.C[1], m * p.ldc[1] + n, o);
+                put(q.C[1], m * q.ldc[1] + n, o);
 #pragma unroll
                 for (int e = 0; e < 4; ++e) o[e] = pack_bf16(u[2 * e], u[2 * e + 1]);
-                put(p.C[2], m * p.ldc[2] + n, o);
+                put(q.C[2], m * q.ldc[2] + n, o);
             }
         } else {
-            const uint4 g = *reinterpret_cast<const uint4*>(p.G + m * p.N + n), u = *reinterpret_cast<const uint4*>(p.U + m * p.N + n);
+            const uint4 g = *reinterpret_cast<const uint4*>(p.G + m * q.N + n), u = *reinterpret_cast<const uint4*>(p.U + m * q.N + n);
             const uint32_t gw[4] = {g.x, g.y, g.z, g.w}, uw[4] = {u.x, u.y, u.z, u.w};
             uint32_t o2[4];
             with_act(p.act, [&](auto act) {
 #pragma unroll
                 for (int e = 0; e < 4; ++e) glu_backward_pair<act.value>(gw[e], uw[e], v[2 * e], v[2 * e + 1], o[e], o2[e]);
             });
-            put(p.C[0], m * p.ldc[0] + n, o);
-            put(p.C[1], m * p.ldc[1] + n, o2);
+            put(q.C[0], m * q.ldc[0] + n, o);
+            put(q.C[1], m * q.ldc[1] + n, o2);
         }
     }
 }
 
-// How a product is laid out on the SMs.
+// How a launch is laid out on the SMs: the form, the K ranges of each product, and the order of the products in the list of
+// work items (longest items first).
 struct MmPlan {
-    bool pair;
-    int splits;
+    bool pair = false, split = false;
+    int splits[kMmGroup] = {1, 1, 1}, order[kMmGroup] = {0, 1, 2};
 };
+
+bool can_split(int epilogue) { return epilogue != atb::kMmRowStats && epilogue != atb::kMmDlogits; }
+int64_t accumulator_columns(const atb::MmProblem& q) { return q.N * (q.epilogue == atb::kMmGlu ? 2 : q.n_segs); }
+size_t partial_bytes(const atb::MmProblem& q, int splits) {
+    return splits > 1 ? static_cast<size_t>(splits) * static_cast<size_t>(atb::round_up(q.M, 32)) * static_cast<size_t>(accumulator_columns(q)) * sizeof(float) : 0;
+}
 
 // Cycles of the candidates, by what measured: a K-step of 64 takes 512 cycles in both forms (the pair's 256 x 256 tile is
 // bound by the tensor cores; the single CTA's 128 x 128 tile has half the reuse, and its 32 KB per step arrive no
-// faster), a work item 2500 more to fill and drain where no other item hides it, and joining the K ranges 4000 for a launch
-// and the FP32 sums, written and read once, at 3 KB per cycle.
-MmPlan mm_plan(int64_t M, int64_t columns, int64_t k_steps, bool may_split) {
-    MmPlan best{false, 1};
+// faster), the last work item 2500 more to fill and drain, and joining K ranges 4000 for a launch and the FP32
+// sums, written and read once, at 3 KB per cycle.  Items are dealt out in turn, the shortest ones last: beyond the even
+// share, the slowest unit waits for the part of the last round that has no items.
+MmPlan make_plan(const atb::MmProblem* q, int n) {
+    MmPlan best;
     double least = 1e300;
+    int64_t k_steps[kMmGroup], longest = 1;
+    for (int j = 0; j < n; ++j) {
+        k_steps[j] = atb::ceil_div(q[j].K, kMmKStep) * q[j].k_segs;
+        if (k_steps[j] > longest) longest = k_steps[j];
+    }
     for (int form = 0; form < 2; ++form) {
-        const bool pair = form == 1;
-        if (pair && M <= 128) continue;
-        const int64_t tile = pair ? 256 : 128, units = pair ? atb::kSmCount / 2 : atb::kSmCount;
-        const int64_t tiles = atb::ceil_div(M, tile) * atb::ceil_div(columns, tile);
+        const int tile = form ? 256 : 128, units = form ? atb::kSmCount / 2 : atb::kSmCount;
+        int64_t tiles[kMmGroup], all_tiles = 0;
+        bool tall = false;                             // a pair needs more than one CTA's rows somewhere
+        for (int j = 0; j < n; ++j) {
+            tall = tall || q[j].M > 128;
+            tiles[j] = atb::ceil_div(q[j].M, tile) * atb::ceil_div(accumulator_columns(q[j]), tile);
+            all_tiles += tiles[j];
+        }
+        if (form && !tall) continue;
         for (int s = 1; s <= 16; ++s) {
-            if (s > 1 && (!may_split || k_steps / s < 4 || tiles * (s - 1) >= 4 * units)) break;
-            const double waves = static_cast<double>(atb::ceil_div(tiles * s, units));
-            double t = waves * 512.0 * static_cast<double>(k_steps) / s + 2500.0;
-            if (s > 1) t += 4000.0 + 8.0 * s * static_cast<double>(M) * static_cast<double>(columns) / 3000.0;
-            if (t < least * 0.98) { least = t; best = {pair, s}; }
+            if (s > 1 && all_tiles * (s - 1) >= 4ll * units) break;
+            MmPlan c;
+            c.pair = form == 1;
+            double work = 0, shortest = 1e300, bytes = 0;
+            int64_t items = 0;
+            for (int j = 0; j < n; ++j) {
+                // ranges of about the length that s ranges of the longest K have, at least 4 steps each
+                int64_t r = (k_steps[j] * s + longest / 2) / longest;
+                if (r > k_steps[j] / 4) r = k_steps[j] / 4;
+                if (r < 1 || !can_split(q[j].epilogue)) r = 1;
+                c.splits[j] = static_cast<int>(r);
+                const double len = static_cast<double>(k_steps[j]) / static_cast<double>(r);
+                work += static_cast<double>(tiles[j] * k_steps[j]);
+                if (len < shortest) shortest = len;
+                items += tiles[j] * r;
+                if (r > 1) { c.split = true; bytes += 2.0 * static_cast<double>(partial_bytes(q[j], c.splits[j])); }
+            }
+            const double rounds = static_cast<double>(atb::ceil_div(items, units)) - static_cast<double>(items) / units;
+            const double t = 512.0 * (work / units + rounds * shortest) + 2500.0 + (c.split ? 4000.0 + bytes / 3000.0 : 0.0);
+            if (t < least * 0.98) { least = t; best = c; }
+            if (s > 1 && !c.split) break;
         }
     }
+    for (int i = 1; i < n; ++i)                        // longest items first
+        for (int k = i; k > 0; --k) {
+            const int a = best.order[k - 1], b = best.order[k];
+            if (k_steps[b] * best.splits[a] > k_steps[a] * best.splits[b]) { best.order[k - 1] = b; best.order[k] = a; }
+        }
     return best;
 }
-bool can_split(int epilogue) {
-    return epilogue == atb::kMmStore || epilogue == atb::kMmAccumulate || epilogue == atb::kMmGlu || epilogue == atb::kMmGluBackward;
-}
-int64_t accumulator_columns(int epilogue, int64_t N, int n_segs) { return N * (epilogue == atb::kMmGlu ? 2 : n_segs); }
-MmPlan plan_of(const atb::MmProblem& q) {
-    return mm_plan(q.M, accumulator_columns(q.epilogue, q.N, q.n_segs), atb::ceil_div(q.K, kMmKStep) * q.k_segs, can_split(q.epilogue));
+
+// Output boxes of 32 rows x 128 bytes.
+template <class T>
+bool output_map(CUtensorMap* m, const void* base, int64_t N, int64_t M, int64_t ld) {
+    constexpr bool F32 = sizeof(T) == 4;
+    return make_map_2d(m, F32 ? CU_TENSOR_MAP_DATA_TYPE_FLOAT32 : CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, sizeof(T), base, static_cast<uint64_t>(N),
+                       static_cast<uint64_t>(M), static_cast<uint64_t>(ld) * sizeof(T), 128 / sizeof(T), 32, CU_TENSOR_MAP_SWIZZLE_128B);
 }
 
 template <class... Args>
@@ -594,57 +714,78 @@ cudaError_t launch_dependent(void (*kernel)(Args...), unsigned grid, unsigned bl
     return cudaLaunchKernelEx(&cfg, kernel, args...);
 }
 
-// splits > 1: EPI is kMmAccumulate and the sums of the ranges go to q.partial.
-template <bool PAIR, bool A_MN, bool B_MN, int EPI>
-atb_status_t launch(const atb::MmProblem& q, int splits, const MmDevice& dev, cudaStream_t stream) {
+// One kernel over the n products of q.  EPI == kMmPlain: bf16, FP32, or the sums of K ranges in `partial`.
+template <bool PAIR, int EPI>
+atb_status_t launch(const atb::MmProblem* q, int n, const MmPlan& plan, char* partial, const MmDevice& dev, cudaStream_t stream) {
     using C = MmCfg<PAIR, EPI>;
-    MmMaps tm;
+    MmMaps<C::JOBS> tm;
     MmParams p = {};
-    const int n_segs = C::DUAL ? 1 : (q.epilogue == atb::kMmGlu ? 2 : q.n_segs);     // a split gated product: two side by side
-    const int n_b = C::DUAL || n_segs == 2 ? 2 : q.k_segs;
-    for (int i = 0; i < 2; ++i) {        // a map that is not used is a copy of the first
-        if (i >= q.k_segs) tm.a[i] = tm.a[0];
-        else if (!operand_map(&tm.a[i], q.A[i], A_MN, q.M, q.K)) return atb::fail(ATB_ERR_CUDA, "cuTensorMapEncodeTiled failed for A");
-        if (i >= n_b) tm.b[i] = tm.b[0];
-        else if (!operand_map(&tm.b[i], q.B[i], B_MN, q.N, q.K)) return atb::fail(ATB_ERR_CUDA, "cuTensorMapEncodeTiled failed for B");
-    }
-    if constexpr (EPI == atb::kMmAccumulate) {
-        float* const base = splits > 1 ? q.partial : q.C32;
-        p.split_rows = splits > 1 ? atb::round_up(q.M, 32) : 0;
-        p.add = splits > 1 ? 0 : !q.first;
-        for (int i = 0; i < n_segs; ++i)      // a map per segment, so that each clips at its own last column
-            if (!make_map_2d(&tm.c[i], CU_TENSOR_MAP_DATA_TYPE_FLOAT32, 4, base + i * q.N, static_cast<uint64_t>(q.N),
-                             static_cast<uint64_t>(splits > 1 ? splits * p.split_rows : q.M), static_cast<uint64_t>(q.N * n_segs) * 4, 32, 32,
-                             CU_TENSOR_MAP_SWIZZLE_128B))
-                return atb::fail(ATB_ERR_CUDA, "cuTensorMapEncodeTiled failed for the FP32 output");
-        if (n_segs == 1) tm.c[1] = tm.c[0];
-        tm.c[2] = tm.c[0];
-    } else {
-        for (int i = 0; i < 3; ++i) {
-            if (!q.C[i]) { tm.c[i] = i ? tm.c[0] : tm.a[0]; continue; }              // not written: any valid map
-            if (!make_map_2d(&tm.c[i], CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 2, q.C[i], static_cast<uint64_t>(q.N), static_cast<uint64_t>(q.M),
-                             static_cast<uint64_t>(q.ldc[i]) * 2, 64, 32, CU_TENSOR_MAP_SWIZZLE_128B))
-                return atb::fail(ATB_ERR_CUDA, "cuTensorMapEncodeTiled failed for an output");
+    size_t offset[kMmGroup], end = 0;
+    for (int j = 0; j < n; ++j) { offset[j] = end; end += partial_bytes(q[j], plan.splits[j]); }
+    int64_t items = 0;
+    for (int i = 0; i < C::JOBS; ++i) {
+        if (i >= n) {                      // maps that are not used are copies of the first product's
+            tm.a[2 * i] = tm.a[2 * i + 1] = tm.a[0];
+            tm.b[2 * i] = tm.b[2 * i + 1] = tm.b[0];
+            tm.c[2 * i] = tm.c[2 * i + 1] = tm.c[0];
+            continue;
+        }
+        const int j = plan.order[i];
+        const atb::MmProblem& x = q[j];
+        const bool a_mn = x.layout == atb::kMmTN, b_mn = x.layout != atb::kMmNT;
+        const int n_segs = C::DUAL ? 1 : (x.epilogue == atb::kMmGlu ? 2 : x.n_segs);     // a split gated product: two side by side
+        const int n_b = C::DUAL || n_segs == 2 ? 2 : x.k_segs;
+        for (int s = 0; s < 2; ++s) {
+            if (s >= x.k_segs) tm.a[2 * i + s] = tm.a[2 * i];
+            else if (!operand_map(&tm.a[2 * i + s], x.A[s], a_mn, x.M, x.K)) return atb::fail(ATB_ERR_CUDA, "cuTensorMapEncodeTiled failed for A");
+            if (s >= n_b) tm.b[2 * i + s] = tm.b[2 * i];
+            else if (!operand_map(&tm.b[2 * i + s], x.B[s], b_mn, x.N, x.K)) return atb::fail(ATB_ERR_CUDA, "cuTensorMapEncodeTiled failed for B");
+        }
+        MmJob& jb = p.job[i];
+        jb.M = x.M; jb.N = x.N;
+        jb.a_mn = a_mn; jb.b_mn = b_mn;
+        jb.m_tiles = static_cast<int>(atb::ceil_div(x.M, C::TILE_M));
+        jb.n_tiles = static_cast<int>(atb::ceil_div(x.N, C::TILE_N));
+        jb.n_segs = n_segs;
+        jb.k_steps0 = static_cast<int>(atb::ceil_div(x.K, kMmKStep));
+        jb.k_steps = jb.k_steps0 * x.k_segs;
+        jb.splits = EPI == kMmPlain ? plan.splits[j] : 1;
+        jb.first_item = static_cast<int>(items);
+        items += static_cast<int64_t>(jb.m_tiles) * jb.n_tiles * jb.n_segs * jb.splits;
+        if (items > (1ll << 30)) return atb::fail(ATB_ERR_BAD_SHAPE, "too many output tiles");
+        if constexpr (EPI == kMmPlain) {
+            jb.fp32 = jb.splits > 1 || x.epilogue == atb::kMmAccumulate;
+            jb.split_rows = jb.splits > 1 ? atb::round_up(x.M, 32) : 0;
+            jb.add = jb.splits == 1 && jb.fp32 && !x.first;
+            for (int s = 0; s < 2; ++s) {
+                CUtensorMap* const m = &tm.c[2 * i + s];
+                bool ok = true;
+                if (s >= n_segs) *m = tm.c[2 * i];
+                else if (jb.splits > 1)     // a map per segment, so that each clips at its own last column
+                    ok = output_map<float>(m, reinterpret_cast<float*>(partial + offset[j]) + s * x.N, x.N, jb.splits * jb.split_rows, x.N * n_segs);
+                else if (jb.fp32) ok = output_map<float>(m, x.C32, x.N, x.M, x.N);
+                else ok = output_map<__nv_bfloat16>(m, x.C[s], x.N, x.M, x.ldc[s]);
+                if (!ok) return atb::fail(ATB_ERR_CUDA, "cuTensorMapEncodeTiled failed for C");
+            }
+        } else {
+            const void* const c[4] = {x.C[0], x.C[1], EPI == atb::kMmGluBackward ? x.G : x.C[2], EPI == atb::kMmGluBackward ? x.U : nullptr};
+            for (int s = 0; s < 4; ++s) {
+                if (!c[s]) { tm.c[s] = s ? tm.c[0] : tm.a[0]; continue; }              // not written: any valid map
+                const int64_t ld = EPI == atb::kMmGluBackward && s >= 2 ? x.N : x.ldc[s];
+                if (!output_map<__nv_bfloat16>(&tm.c[s], c[s], x.N, x.M, ld)) return atb::fail(ATB_ERR_CUDA, "cuTensorMapEncodeTiled failed for C");
+            }
         }
     }
-    p.M = q.M; p.N = q.N;
-    p.m_tiles = static_cast<int>(atb::ceil_div(q.M, C::TILE_M));
-    p.n_tiles = static_cast<int>(atb::ceil_div(q.N, C::TILE_N));
-    p.n_segs = n_segs;
-    p.k_steps0 = static_cast<int>(atb::ceil_div(q.K, kMmKStep));
-    p.k_steps = p.k_steps0 * q.k_segs;
-    p.splits = splits;
+    p.n_jobs = n;
+    p.items = static_cast<int>(items);
     p.error_flag = dev.flag;
-    p.act = q.act; p.save = q.C[1] != nullptr;
-    p.G = static_cast<const __nv_bfloat16*>(q.G); p.U = static_cast<const __nv_bfloat16*>(q.U);
-    p.labels = q.labels; p.ignore_index = q.ignore_index; p.col0 = q.col0;
-    p.stats = q.stats; p.stats_ld = q.stats_ld; p.label_logit = q.label_logit;
-    p.lse = q.lse; p.scale = q.scale;
-    const int64_t items = static_cast<int64_t>(p.m_tiles) * p.n_tiles * p.n_segs * splits;
-    if (items > (1ll << 30)) return atb::fail(ATB_ERR_BAD_SHAPE, "too many output tiles");
+    p.act = q->act; p.save = q->C[1] != nullptr;
+    p.labels = q->labels; p.ignore_index = q->ignore_index; p.col0 = q->col0;
+    p.stats = q->stats; p.stats_ld = q->stats_ld; p.label_logit = q->label_logit;
+    p.lse = q->lse; p.scale = q->scale;
     const int units = PAIR ? dev.sms / 2 : dev.sms;
     const int n_units = static_cast<int>(items < units ? items : units);
-    auto kernel = bf16_mm_kernel<PAIR, A_MN, B_MN, EPI>;
+    auto kernel = bf16_mm_kernel<PAIR, EPI>;
     cudaError_t e = cudaSuccess;
     static std::atomic<uint64_t> allowed{0};         // devices on which this kernel has its shared memory allowed
     const uint64_t bit = 1ull << dev.ordinal;
@@ -658,30 +799,44 @@ atb_status_t launch(const atb::MmProblem& q, int splits, const MmDevice& dev, cu
     return ATB_OK;
 }
 
-template <bool A_MN, bool B_MN, int EPI>
-atb_status_t run(const atb::MmProblem& q, const MmDevice& dev, cudaStream_t stream) {
-    const MmPlan plan = plan_of(q);
+template <int EPI>
+atb_status_t join(const atb::MmProblem* q, int n, const MmPlan& plan, const char* partial, const MmDevice& dev, cudaStream_t stream) {
+    MmJoin p = {};
+    size_t offset = 0;
+    for (int j = 0; j < n; ++j) {
+        if (plan.splits[j] > 1) {
+            MmJoinJob& jb = p.job[p.n_jobs++];
+            jb.M = q[j].M; jb.N = q[j].N;
+            jb.n_segs = EPI == atb::kMmGlu ? 1 : q[j].n_segs;
+            jb.cols = accumulator_columns(q[j]);
+            jb.src = reinterpret_cast<const float*>(partial + offset);
+            jb.splits = plan.splits[j];
+            jb.split_rows = atb::round_up(q[j].M, 32);
+            for (int i = 0; i < 3; ++i) { jb.C[i] = q[j].C[i]; jb.ldc[i] = q[j].ldc[i]; }
+            jb.C32 = q[j].epilogue == atb::kMmAccumulate ? q[j].C32 : nullptr;
+            jb.add = !q[j].first;
+            jb.first = p.all;
+            p.all += jb.M * (jb.N / 8) * jb.n_segs;
+        }
+        offset += partial_bytes(q[j], plan.splits[j]);
+    }
+    p.act = q->act;
+    p.G = static_cast<const __nv_bfloat16*>(q->G); p.U = static_cast<const __nv_bfloat16*>(q->U);
+    const int64_t blocks = atb::ceil_div(p.all, 256), most = static_cast<int64_t>(dev.sms) * 8;
+    const cudaError_t e = launch_dependent(bf16_mm_join_kernel<EPI>, static_cast<unsigned>(blocks < most ? blocks : most), 256u, 1u, 0, stream, p);
+    if (e != cudaSuccess) return atb::fail(ATB_ERR_CUDA, "bf16 product join launch: %s", cudaGetErrorString(e));
+    return ATB_OK;
+}
+
+template <int EPI>
+atb_status_t run(const atb::MmProblem* q, int n, const MmPlan& plan, char* partial, const MmDevice& dev, cudaStream_t stream) {
+    if (!plan.split) return plan.pair ? launch<true, EPI>(q, n, plan, partial, dev, stream) : launch<false, EPI>(q, n, plan, partial, dev, stream);
     if constexpr (EPI == atb::kMmRowStats || EPI == atb::kMmDlogits) {
-        return plan.pair ? launch<true, A_MN, B_MN, EPI>(q, 1, dev, stream) : launch<false, A_MN, B_MN, EPI>(q, 1, dev, stream);
+        return atb::fail(ATB_ERR_BAD_ARGUMENT, "this epilogue takes whole sums");
     } else {
-        if (plan.splits == 1)
-            return plan.pair ? launch<true, A_MN, B_MN, EPI>(q, 1, dev, stream) : launch<false, A_MN, B_MN, EPI>(q, 1, dev, stream);
-        if (!q.partial) return atb::fail(ATB_ERR_NULL_POINTER, "a product that is split along K needs room for its sums");
-        const atb_status_t s = plan.pair ? launch<true, A_MN, B_MN, atb::kMmAccumulate>(q, plan.splits, dev, stream)
-                                         : launch<false, A_MN, B_MN, atb::kMmAccumulate>(q, plan.splits, dev, stream);
-        if (s != ATB_OK) return s;
-        MmJoin j = {};
-        j.M = q.M; j.N = q.N; j.n_segs = EPI == atb::kMmGlu ? 1 : q.n_segs;
-        j.cols = accumulator_columns(EPI, q.N, q.n_segs);
-        j.src = q.partial; j.splits = plan.splits; j.split_rows = atb::round_up(q.M, 32);
-        for (int i = 0; i < 3; ++i) { j.C[i] = q.C[i]; j.ldc[i] = q.ldc[i]; }
-        j.C32 = q.C32; j.add = !q.first;
-        j.act = q.act;
-        j.G = static_cast<const __nv_bfloat16*>(q.G); j.U = static_cast<const __nv_bfloat16*>(q.U);
-        const int64_t blocks = atb::ceil_div(j.M * (j.N / 8) * j.n_segs, 256), most = static_cast<int64_t>(dev.sms) * 8;
-        const cudaError_t e = launch_dependent(bf16_mm_join_kernel<EPI>, static_cast<unsigned>(blocks < most ? blocks : most), 256u, 1u, 0, stream, j);
-        if (e != cudaSuccess) return atb::fail(ATB_ERR_CUDA, "bf16 product join launch: %s", cudaGetErrorString(e));
-        return ATB_OK;
+        if (!partial) return atb::fail(ATB_ERR_NULL_POINTER, "a product that is split along K needs room for its sums");
+        const atb_status_t s = plan.pair ? launch<true, kMmPlain>(q, n, plan, partial, dev, stream) : launch<false, kMmPlain>(q, n, plan, partial, dev, stream);
+        return s != ATB_OK ? s : join<EPI>(q, n, plan, partial, dev, stream);
     }
 }
 
@@ -731,31 +886,31 @@ unsigned int take_mm_error_flag() {
 }
 
 int64_t mm_stats_per_row(int64_t M, int64_t N, int64_t K) {
-    return ceil_div(N, mm_plan(M, N, ceil_div(K, kMmKStep), false).pair ? 128 : 64);
+    const MmProblem q = mm_sizes(kMmRowStats, M, N, K);
+    return ceil_div(N, make_plan(&q, 1).pair ? 128 : 64);
 }
 
-size_t mm_partial_bytes(MmEpilogue epilogue, int64_t M, int64_t N, int64_t K, int k_segs, int n_segs) {
-    const int64_t columns = accumulator_columns(epilogue, N, n_segs);
-    const MmPlan plan = mm_plan(M, columns, ceil_div(K, kMmKStep) * k_segs, can_split(epilogue));
-    return plan.splits > 1 ? static_cast<size_t>(plan.splits) * static_cast<size_t>(round_up(M, 32)) * static_cast<size_t>(columns) * sizeof(float) : 0;
+size_t mm_partial_bytes(const MmProblem* q, int n) {
+    const MmPlan plan = make_plan(q, n);
+    size_t bytes = 0;
+    for (int j = 0; j < n; ++j) bytes += partial_bytes(q[j], plan.splits[j]);
+    return bytes;
 }
 
-atb_status_t mm_launch(const MmProblem& q, cudaStream_t stream) {
+atb_status_t mm_launch(const MmProblem* q, int n, void* partial, cudaStream_t stream) {
     const MmDevice* dev = nullptr;
     const atb_status_t s = mm_device(&dev);
     if (s != ATB_OK) return s;
-#define ATB_MM_CASE(LAYOUT, EPI, A_MN, B_MN) \
-    if (q.layout == LAYOUT && q.epilogue == EPI) return run<A_MN, B_MN, EPI>(q, *dev, stream);
-    ATB_MM_CASE(kMmNN, kMmStore, false, true)
-    ATB_MM_CASE(kMmNN, kMmGlu, false, true)
-    ATB_MM_CASE(kMmNN, kMmAccumulate, false, true)
-    ATB_MM_CASE(kMmNT, kMmStore, false, false)
-    ATB_MM_CASE(kMmNT, kMmGluBackward, false, false)
-    ATB_MM_CASE(kMmNT, kMmRowStats, false, false)
-    ATB_MM_CASE(kMmNT, kMmDlogits, false, false)
-    ATB_MM_CASE(kMmTN, kMmStore, true, true)
-#undef ATB_MM_CASE
-    return fail(ATB_ERR_BAD_ARGUMENT, "no product kernel for layout %d with epilogue %d", static_cast<int>(q.layout), static_cast<int>(q.epilogue));
+    const MmPlan plan = make_plan(q, n);
+    char* const room = static_cast<char*>(partial);
+    switch (q->epilogue) {
+        case kMmStore: case kMmAccumulate: return run<kMmPlain>(q, n, plan, room, *dev, stream);
+        case kMmGlu: return run<kMmGlu>(q, n, plan, room, *dev, stream);
+        case kMmGluBackward: return run<kMmGluBackward>(q, n, plan, room, *dev, stream);
+        case kMmRowStats: return run<kMmRowStats>(q, n, plan, room, *dev, stream);
+        case kMmDlogits: return run<kMmDlogits>(q, n, plan, room, *dev, stream);
+    }
+    return fail(ATB_ERR_BAD_ARGUMENT, "no product kernel for epilogue %d", static_cast<int>(q->epilogue));
 }
 
 }  // namespace atb

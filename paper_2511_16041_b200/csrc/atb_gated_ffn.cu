@@ -5,7 +5,7 @@
 //
 // Forward: one kernel for both projections, the activation and the product (x is loaded once for both), one for y.
 // Backward: dh never reaches memory - the epilogue of its product turns it into dg and du; the two products
-// behind dx are one walk over 2 F; dWg and dWu are one launch.  h, g and u are kept in bf16 between the products: they
+// behind dx are one walk over 2 F, and dx and the three weight gradients are one launch.  h, g and u are kept in bf16 between the products: they
 // are (h) or were (the accumulators of g and u, FP32) operands of the tensor cores, which take bf16; the one
 // rounding costs 2^-9 of the value.
 #include <algorithm>
@@ -32,12 +32,22 @@ bool ld_ok(int64_t ld, int64_t least) { return ld >= least && ld % 8 == 0; }
 // dg and du in the workspace, [M][F] bf16 each, up to the next 256 bytes.
 size_t glu_gradient_bytes(int64_t M, int64_t F) { return (4 * static_cast<size_t>(M) * static_cast<size_t>(F) + 255) / 256 * 256; }
 
+// The products behind dh, which are one launch: sizes and layouts of those wanted.
+int gradient_products(atb::MmProblem* q, int64_t M, int64_t D, int64_t F, bool dx, bool dw, bool dwd) {
+    int n = 0;
+    if (dx) { q[n] = atb::mm_sizes(atb::kMmStore, M, D, F, 2, 1); q[n++].layout = atb::kMmNT; }
+    if (dw) { q[n] = atb::mm_sizes(atb::kMmStore, D, F, M, 1, 2); q[n++].layout = atb::kMmTN; }
+    if (dwd) { q[n] = atb::mm_sizes(atb::kMmStore, F, D, M); q[n++].layout = atb::kMmTN; }
+    return n;
+}
+
 }  // namespace
 
 extern "C" size_t atb_gated_ffn_workspace_bytes(int64_t M, int64_t D, int64_t F) {
     if (M <= atb::kFewRows || D < 1 || F < 1) return 0;
     // the sums of a product that is split along K; the two products take turns
-    return std::max(atb::mm_partial_bytes(atb::kMmGlu, M, F, D), atb::mm_partial_bytes(atb::kMmStore, M, D, F));
+    const atb::MmProblem up = atb::mm_sizes(atb::kMmGlu, M, F, D), down = atb::mm_sizes(atb::kMmStore, M, D, F);
+    return std::max(atb::mm_partial_bytes(&up, 1), atb::mm_partial_bytes(&down, 1));
 }
 
 extern "C" atb_status_t atb_gated_ffn(int64_t M, int64_t D, int64_t F, int act, const void* X_dev, int64_t ldx, const void* Wg_dev,
@@ -69,8 +79,7 @@ extern "C" atb_status_t atb_gated_ffn(int64_t M, int64_t D, int64_t F, int act, 
     up.A[0] = {X_dev, ldx}; up.B[0] = {Wg_dev, ldw}; up.B[1] = {Wu_dev, ldw};
     up.C[0] = H_dev; up.C[1] = G_dev; up.C[2] = U_dev;
     up.ldc[0] = up.ldc[1] = up.ldc[2] = F;
-    up.partial = static_cast<float*>(workspace_dev);
-    s = atb::mm_launch(up, st);
+    s = atb::mm_launch(&up, 1, workspace_dev, st);
     if (s != ATB_OK) return s;
 
     atb::MmProblem down;
@@ -78,15 +87,20 @@ extern "C" atb_status_t atb_gated_ffn(int64_t M, int64_t D, int64_t F, int act, 
     down.M = M; down.N = D; down.K = F;
     down.A[0] = {H_dev, F}; down.B[0] = {Wd_dev, ldwd};
     down.C[0] = Y_dev; down.ldc[0] = ldy;
-    down.partial = static_cast<float*>(workspace_dev);
-    return atb::mm_launch(down, st);
+    return atb::mm_launch(&down, 1, workspace_dev, st);
 }
 
 extern "C" size_t atb_gated_ffn_backward_workspace_bytes(int64_t M, int64_t D, int64_t F) {
     if (M < 1 || D < 1 || F < 1) return 0;
-    // dg and du, and the sums of a product that is split along K
-    return glu_gradient_bytes(M, F) + std::max({atb::mm_partial_bytes(atb::kMmGluBackward, M, F, D), atb::mm_partial_bytes(atb::kMmStore, M, D, F, 2),
-                                                atb::mm_partial_bytes(atb::kMmStore, D, F, M, 1, 2), atb::mm_partial_bytes(atb::kMmStore, F, D, M)});
+    // dg and du, and the sums of products that are split along K: the largest need of any choice of gradients
+    const atb::MmProblem dh = atb::mm_sizes(atb::kMmGluBackward, M, F, D);
+    size_t sums = atb::mm_partial_bytes(&dh, 1);
+    for (int wanted = 1; wanted < 8; ++wanted) {
+        atb::MmProblem q[atb::kMmGroup];
+        const int n = gradient_products(q, M, D, F, wanted & 1, wanted & 2, wanted & 4);
+        sums = std::max(sums, atb::mm_partial_bytes(q, n));
+    }
+    return glu_gradient_bytes(M, F) + sums;
 }
 
 extern "C" atb_status_t atb_gated_ffn_backward(int64_t M, int64_t D, int64_t F, int act, const void* dY_dev, int64_t lddy, const void* X_dev,
@@ -121,7 +135,7 @@ extern "C" atb_status_t atb_gated_ffn_backward(int64_t M, int64_t D, int64_t F, 
     }
     uint16_t* const dG = static_cast<uint16_t*>(workspace_dev);
     uint16_t* const dU = dG + M * F;
-    float* const partial = reinterpret_cast<float*>(static_cast<char*>(workspace_dev) + glu_gradient_bytes(M, F));
+    void* const partial = static_cast<char*>(workspace_dev) + glu_gradient_bytes(M, F);
 
     if (dX_dev || dWg_dev) {
         atb::MmProblem dh;
@@ -130,39 +144,27 @@ extern "C" atb_status_t atb_gated_ffn_backward(int64_t M, int64_t D, int64_t F, 
         dh.A[0] = {dY_dev, lddy}; dh.B[0] = {Wd_dev, ldwd};
         dh.G = G_dev; dh.U = U_dev;
         dh.C[0] = dG; dh.C[1] = dU; dh.ldc[0] = dh.ldc[1] = F;
-        dh.partial = partial;
-        s = atb::mm_launch(dh, st);
+        s = atb::mm_launch(&dh, 1, partial, st);
         if (s != ATB_OK) return s;
     }
+    atb::MmProblem q[atb::kMmGroup];
+    const int n = gradient_products(q, M, D, F, dX_dev, dWg_dev, dWd_dev);
+    if (n == 0) return ATB_OK;
+    atb::MmProblem* next = q;
     if (dX_dev) {
-        atb::MmProblem dx;
-        dx.layout = atb::kMmNT; dx.epilogue = atb::kMmStore;
-        dx.M = M; dx.N = D; dx.K = F; dx.k_segs = 2;
+        atb::MmProblem& dx = *next++;
         dx.A[0] = {dG, F}; dx.A[1] = {dU, F}; dx.B[0] = {Wg_dev, ldw}; dx.B[1] = {Wu_dev, ldw};
         dx.C[0] = dX_dev; dx.ldc[0] = lddx;
-        dx.partial = partial;
-        s = atb::mm_launch(dx, st);
-        if (s != ATB_OK) return s;
     }
     if (dWg_dev) {
-        atb::MmProblem dw;
-        dw.layout = atb::kMmTN; dw.epilogue = atb::kMmStore;
-        dw.M = D; dw.N = F; dw.K = M; dw.n_segs = 2;
+        atb::MmProblem& dw = *next++;
         dw.A[0] = {X_dev, ldx}; dw.B[0] = {dG, F}; dw.B[1] = {dU, F};
         dw.C[0] = dWg_dev; dw.C[1] = dWu_dev; dw.ldc[0] = dw.ldc[1] = lddw;
-        dw.partial = partial;
-        s = atb::mm_launch(dw, st);
-        if (s != ATB_OK) return s;
     }
     if (dWd_dev) {
-        atb::MmProblem dw;
-        dw.layout = atb::kMmTN; dw.epilogue = atb::kMmStore;
-        dw.M = F; dw.N = D; dw.K = M;
+        atb::MmProblem& dw = *next++;
         dw.A[0] = {H_dev, F}; dw.B[0] = {dY_dev, lddy};
         dw.C[0] = dWd_dev; dw.ldc[0] = lddwd;
-        dw.partial = partial;
-        s = atb::mm_launch(dw, st);
-        if (s != ATB_OK) return s;
     }
-    return ATB_OK;
+    return atb::mm_launch(q, n, partial, st);
 }

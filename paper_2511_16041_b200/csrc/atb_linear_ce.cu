@@ -76,6 +76,14 @@ int64_t piece_words(int64_t M, int64_t V, int64_t piece) {
     return piece;
 }
 
+// The products behind dl of a piece of n words, which are one launch: sizes and layouts of those wanted.
+int gradient_products(atb::MmProblem* q, int64_t M, int64_t n, int64_t D, bool pieces, bool dx, bool dw) {
+    int products = 0;
+    if (dx) { q[products] = atb::mm_sizes(pieces ? atb::kMmAccumulate : atb::kMmStore, M, D, n); q[products++].layout = atb::kMmNN; }
+    if (dw) { q[products] = atb::mm_sizes(atb::kMmStore, n, D, M); q[products++].layout = atb::kMmTN; }
+    return products;
+}
+
 // The backward workspace: dl of a piece, FP32 sums of dx where there is more than one piece, and the sums of a product that
 // is split along K.
 struct BackwardSpace {
@@ -89,9 +97,13 @@ BackwardSpace backward_space(int64_t M, int64_t V, int64_t D, int64_t piece) {
     w.partial = w.sum + (w.words < V ? align256(static_cast<size_t>(M) * static_cast<size_t>(D) * sizeof(float)) : 0);
     // the last piece may be shorter than the others, with a plan of its own
     const int64_t first = V < w.words ? V : w.words, last = V - (V - 1) / w.words * w.words;
-    const atb::MmEpilogue dx = w.words < V ? atb::kMmAccumulate : atb::kMmStore;
-    w.partial_bytes = std::max({atb::mm_partial_bytes(dx, M, D, first), atb::mm_partial_bytes(dx, M, D, last),
-                                atb::mm_partial_bytes(atb::kMmStore, first, D, M), atb::mm_partial_bytes(atb::kMmStore, last, D, M)});
+    w.partial_bytes = 0;
+    for (const int64_t n : {first, last})
+        for (int wanted = 1; wanted < 4; ++wanted) {
+            atb::MmProblem q[atb::kMmGroup];
+            const int products = gradient_products(q, M, n, D, w.words < V, wanted & 1, wanted & 2);
+            w.partial_bytes = std::max(w.partial_bytes, atb::mm_partial_bytes(q, products));
+        }
     return w;
 }
 
@@ -127,7 +139,7 @@ extern "C" atb_status_t atb_linear_cross_entropy(int64_t M, int64_t V, int64_t D
     q.stats = static_cast<float2*>(workspace_dev);
     q.stats_ld = atb::mm_stats_per_row(M, V, D);
     q.label_logit = reinterpret_cast<float*>(static_cast<char*>(workspace_dev) + (need - static_cast<size_t>(M) * sizeof(float)));
-    s = atb::mm_launch(q, st);
+    s = atb::mm_launch(&q, 1, nullptr, st);
     if (s != ATB_OK) return s;
     linear_ce_join_kernel<<<static_cast<unsigned>(atb::ceil_div(M, 8)), 256, 0, st>>>(M, V, q.stats, q.stats_ld, q.label_logit, labels_dev, ignore_index,
                                                                                      loss_dev, lse_dev);
@@ -172,7 +184,7 @@ extern "C" atb_status_t atb_linear_cross_entropy_backward(int64_t M, int64_t V, 
     const int64_t words = space.words;
     uint16_t* const dl = static_cast<uint16_t*>(workspace_dev);
     float* const sum = reinterpret_cast<float*>(static_cast<char*>(workspace_dev) + space.sum);
-    float* const partial = reinterpret_cast<float*>(static_cast<char*>(workspace_dev) + space.partial);
+    void* const partial = static_cast<char*>(workspace_dev) + space.partial;
     for (int64_t v0 = 0; v0 < V; v0 += words) {
         const int64_t n = V - v0 < words ? V - v0 : words;
         const uint16_t* const Wv = static_cast<const uint16_t*>(W_dev) + v0 * ldw;
@@ -183,29 +195,23 @@ extern "C" atb_status_t atb_linear_cross_entropy_backward(int64_t M, int64_t V, 
         q.C[0] = dl; q.ldc[0] = words;
         q.labels = labels_dev; q.ignore_index = ignore_index; q.col0 = v0;
         q.lse = lse_dev; q.scale = dloss_dev;
-        s = atb::mm_launch(q, st);
+        s = atb::mm_launch(&q, 1, nullptr, st);
         if (s != ATB_OK) return s;
+        atb::MmProblem grad[atb::kMmGroup];
+        const int products = gradient_products(grad, M, n, D, words < V, dX_dev, dW_dev);
         if (dX_dev) {
-            atb::MmProblem dx;
-            dx.layout = atb::kMmNN;
-            dx.M = M; dx.N = D; dx.K = n;
+            atb::MmProblem& dx = grad[0];
             dx.A[0] = {dl, words}; dx.B[0] = {Wv, ldw};
-            if (words < V) { dx.epilogue = atb::kMmAccumulate; dx.C32 = sum; dx.first = v0 == 0; }
-            else { dx.epilogue = atb::kMmStore; dx.C[0] = dX_dev; dx.ldc[0] = lddx; }
-            dx.partial = partial;
-            s = atb::mm_launch(dx, st);
-            if (s != ATB_OK) return s;
+            dx.C32 = sum; dx.first = v0 == 0;
+            dx.C[0] = dX_dev; dx.ldc[0] = lddx;
         }
         if (dW_dev) {
-            atb::MmProblem dw;
-            dw.layout = atb::kMmTN; dw.epilogue = atb::kMmStore;
-            dw.M = n; dw.N = D; dw.K = M;
+            atb::MmProblem& dw = grad[products - 1];
             dw.A[0] = {dl, words}; dw.B[0] = {X_dev, ldx};
             dw.C[0] = static_cast<uint16_t*>(dW_dev) + v0 * lddw; dw.ldc[0] = lddw;
-            dw.partial = partial;
-            s = atb::mm_launch(dw, st);
-            if (s != ATB_OK) return s;
         }
+        s = atb::mm_launch(grad, products, partial, st);
+        if (s != ATB_OK) return s;
     }
     if (dX_dev && words < V) {
         const int64_t vecs = M * (D / 8);
