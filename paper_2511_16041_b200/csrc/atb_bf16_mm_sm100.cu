@@ -14,6 +14,7 @@
 // their tiles are dealt out as one list, so that one product's last wave is filled by the next one's tiles.  A product
 // of few tiles is cut along K into ranges whose FP32 sums a second kernel joins.
 // Every wait is bounded (see atb_gemm_device.cuh).
+#include <algorithm>
 #include <atomic>
 #include <type_traits>
 
@@ -358,6 +359,13 @@ __device__ __forceinline__ uint32_t mm_desc_step(bool mn_major) { return (mn_maj
 struct MmItem {
     int job, mt, nt, seg, split, k_begin, k_end;
 };
+// Place in the list of the it-th item of this CTA or pair: dealt out to and fro, so that the units that get the longer items
+// of one round get the shorter ones of the next.
+template <bool PAIR>
+__device__ __forceinline__ int mm_item_at(int it) {
+    const int unit = PAIR ? blockIdx.x >> 1 : blockIdx.x, units = PAIR ? gridDim.x >> 1 : gridDim.x;
+    return it * units + ((it & 1) ? units - 1 - unit : unit);
+}
 template <int JOBS>
 __device__ __forceinline__ MmItem mm_item(const MmParams& p, int item) {
     MmItem w;
@@ -415,15 +423,13 @@ bf16_mm_kernel(const __grid_constant__ MmMaps<MmCfg<PAIR, EPI>::JOBS> tm, const 
     grid_dependency_wait();
     grid_dependency_launch();
 
-    const int unit = PAIR ? blockIdx.x >> 1 : blockIdx.x, units = PAIR ? gridDim.x >> 1 : gridDim.x;
-
     if (warp == 0) {
         // ================================ TMA producer ================================
         if (elect_one()) {
             Ring r;
             bool ok = true;
             int it = 0;
-            for (int item = unit; ok && item < p.items; item += units, ++it) {
+            for (int item; ok && (item = mm_item_at<PAIR>(it)) < p.items; ++it) {
                 const MmItem w = mm_item<C::JOBS>(p, item);
                 const MmJob& jb = p.job[w.job];
                 const bool a_mn = jb.a_mn, b_mn = jb.b_mn;
@@ -456,7 +462,7 @@ bf16_mm_kernel(const __grid_constant__ MmMaps<MmCfg<PAIR, EPI>::JOBS> tm, const 
             Ring r;
             bool ok = true;
             int it = 0;
-            for (int item = unit; ok && item < p.items; item += units, ++it) {
+            for (int item; ok && (item = mm_item_at<PAIR>(it)) < p.items; ++it) {
                 const MmItem w = mm_item<C::JOBS>(p, item);
                 const bool a_mn = p.job[w.job].a_mn, b_mn = p.job[w.job].b_mn;
                 const uint32_t idesc = umma_idesc_bf16_f32(PAIR ? 256 : 128, C::BN, a_mn, b_mn);
@@ -491,7 +497,7 @@ bf16_mm_kernel(const __grid_constant__ MmMaps<MmCfg<PAIR, EPI>::JOBS> tm, const 
         BoxWriter<C::BOXES> out(smem_base + C::BOX_OFF + static_cast<uint32_t>(e) * C::BOXES * kEpilogueBoxBytes, box_bar + 8 * e, lane);
         int it = 0;
         bool ok = true;
-        for (int item = unit; ok && item < p.items; item += units, ++it) {
+        for (int item; ok && (item = mm_item_at<PAIR>(it)) < p.items; ++it) {
             const MmItem w = mm_item<C::JOBS>(p, item);
             const MmJob& jb = p.job[w.job];
             const int64_t row0 = static_cast<int64_t>(w.mt) * C::TILE_M + rank * 128 + q * 32, col0 = static_cast<int64_t>(w.nt) * C::TILE_N;
@@ -632,11 +638,37 @@ size_t partial_bytes(const atb::MmProblem& q, int splits) {
     return splits > 1 ? static_cast<size_t>(splits) * static_cast<size_t>(atb::round_up(q.M, 32)) * static_cast<size_t>(accumulator_columns(q)) * sizeof(float) : 0;
 }
 
+// Steps that the slowest unit has: items in order of their length, dealt out to and fro (mm_item_at).  Three units are looked
+// at; where there are many rounds, all are close to the even share.
+double slowest_unit(const int64_t* count, const double* length, int n, int units) {
+    int64_t items = 0;
+    double work = 0, shortest = 1e300;
+    for (int j = 0; j < n; ++j) {
+        items += count[j];
+        work += static_cast<double>(count[j]) * length[j];
+        if (length[j] < shortest) shortest = length[j];
+    }
+    const int64_t rounds = atb::ceil_div(items, units);
+    if (rounds > 8) return work / units + 0.5 * shortest;
+    double most = 0;
+    for (const int u : {0, units / 2, units - 1}) {
+        double load = 0;
+        for (int64_t r = 0; r < rounds; ++r) {
+            int64_t at = r * units + ((r & 1) ? units - 1 - u : u);
+            if (at >= items) continue;
+            int j = 0;
+            while (at >= count[j]) at -= count[j++];
+            load += length[j];
+        }
+        if (load > most) most = load;
+    }
+    return most;
+}
+
 // Cycles of the candidates, by what measured: a K-step of 64 takes 512 cycles in both forms (the pair's 256 x 256 tile is
 // bound by the tensor cores; the single CTA's 128 x 128 tile has half the reuse, and its 32 KB per step arrive no
 // faster), the last work item 2500 more to fill and drain, and joining K ranges 4000 for a launch and the FP32
-// sums, written and read once, at 3 KB per cycle.  Items are dealt out in turn, the shortest ones last: beyond the even
-// share, the slowest unit waits for the part of the last round that has no items.
+// sums, written and read once, at 3 KB per cycle.
 MmPlan make_plan(const atb::MmProblem* q, int n) {
     MmPlan best;
     double least = 1e300;
@@ -659,31 +691,26 @@ MmPlan make_plan(const atb::MmProblem* q, int n) {
             if (s > 1 && all_tiles * (s - 1) >= 4ll * units) break;
             MmPlan c;
             c.pair = form == 1;
-            double work = 0, shortest = 1e300, bytes = 0;
-            int64_t items = 0;
+            double bytes = 0, len[kMmGroup];
             for (int j = 0; j < n; ++j) {
                 // ranges of about the length that s ranges of the longest K have, at least 4 steps each
                 int64_t r = (k_steps[j] * s + longest / 2) / longest;
                 if (r > k_steps[j] / 4) r = k_steps[j] / 4;
                 if (r < 1 || !can_split(q[j].epilogue)) r = 1;
                 c.splits[j] = static_cast<int>(r);
-                const double len = static_cast<double>(k_steps[j]) / static_cast<double>(r);
-                work += static_cast<double>(tiles[j] * k_steps[j]);
-                if (len < shortest) shortest = len;
-                items += tiles[j] * r;
+                len[j] = static_cast<double>(k_steps[j]) / static_cast<double>(r);
                 if (r > 1) { c.split = true; bytes += 2.0 * static_cast<double>(partial_bytes(q[j], c.splits[j])); }
             }
-            const double rounds = static_cast<double>(atb::ceil_div(items, units)) - static_cast<double>(items) / units;
-            const double t = 512.0 * (work / units + rounds * shortest) + 2500.0 + (c.split ? 4000.0 + bytes / 3000.0 : 0.0);
-            if (t < least * 0.98) { least = t; best = c; }
             if (s > 1 && !c.split) break;
+            for (int i = 1; i < n; ++i)                // longest items first
+                for (int k = i; k > 0 && len[c.order[k]] > len[c.order[k - 1]]; --k) std::swap(c.order[k], c.order[k - 1]);
+            int64_t count[kMmGroup];
+            double length[kMmGroup];
+            for (int i = 0; i < n; ++i) { count[i] = tiles[c.order[i]] * c.splits[c.order[i]]; length[i] = len[c.order[i]]; }
+            const double t = 512.0 * slowest_unit(count, length, n, units) + 2500.0 + (c.split ? 4000.0 + bytes / 3000.0 : 0.0);
+            if (t < least * 0.98) { least = t; best = c; }
         }
     }
-    for (int i = 1; i < n; ++i)                        // longest items first
-        for (int k = i; k > 0; --k) {
-            const int a = best.order[k - 1], b = best.order[k];
-            if (k_steps[b] * best.splits[a] > k_steps[a] * best.splits[b]) { best.order[k - 1] = b; best.order[k] = a; }
-        }
     return best;
 }
 
