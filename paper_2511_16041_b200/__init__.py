@@ -163,8 +163,7 @@ def _check(status: int):
 def _stream_ptr(stream):
     if stream is None:
         import torch
-        raw = getattr(torch._C, "_cuda_getCurrentRawStream", None)      # 3 us less per call than the Stream object
-        return ctypes.c_void_p(raw(torch.cuda.current_device()) if raw else torch.cuda.current_stream().cuda_stream)
+        return ctypes.c_void_p(torch.cuda.current_stream().cuda_stream)
     if isinstance(stream, int):
         return ctypes.c_void_p(stream)
     return ctypes.c_void_p(stream.cuda_stream)
@@ -375,126 +374,54 @@ def atb_select_tiling(M: int, N: int, K: int, hw: atb_hw_params_t | None = None,
 
 
 # ------------------------------------------------------------------ between the products: norm, feed-forward, loss
-ATB_F32, ATB_BF16 = 0, 1
 ACTIVATIONS = {"silu": 0, "gelu": 1, "gelu_tanh": 2}
 
 
-def _dtype(t):
-    import torch
-    if t.dtype == torch.float32:
-        return ATB_F32
-    if t.dtype == torch.bfloat16:
-        return ATB_BF16
-    raise TypeError(f"{t.dtype}: float32 or bfloat16")
+_ops = None
 
 
-def _matrix(t, rows, cols, dtype, device, name):
-    """Checks a row-major matrix on CUDA device number ``device`` and returns its leading dimension."""
-    if t.dtype is dtype and t.shape == (rows, cols) and t.get_device() == device:
-        ld, one = t.stride()
-        if one == 1 or cols <= 1:
-            return ld if rows > 1 or ld > cols else cols
-    raise ValueError(f"{name}: a row-major matrix {(rows, cols)} of {dtype} on cuda:{device}, got {tuple(t.shape)} of {t.dtype} on {t.device}, "
-                     f"strides {t.stride()}")
+def load_ops():
+    """The compiled side of the functions below (``_atb_torch``, built in-tree beside the library), bound to the loaded library.
+    Raises if it is missing: there is no other path."""
+    global _ops
+    if _ops is None:
+        import importlib.util
+        import torch                                          # noqa: F401  (its libraries, before the module that needs them)
+        path = os.path.join(_HERE, "_atb_torch.so")
+        if not os.path.exists(path):
+            raise RuntimeError(f"{path} is missing: build it with `python -m paper_2511_16041_b200._build`")
+        spec = importlib.util.spec_from_file_location("_atb_torch", path)
+        ops = importlib.util.module_from_spec(spec)
+        spec.loader.exec_module(ops)
+        lib = load_library()
+        for name in ops.ENTRIES:
+            ops.bind(name, ctypes.cast(getattr(lib, name), ctypes.c_void_p).value)
+        _ops = ops
+    return _ops
 
 
-def _vector(t, n, dtype, device, name):
-    if t.dtype is not dtype or t.shape != (n,) or t.get_device() != device or not t.is_contiguous():
-        raise ValueError(f"{name}: a contiguous vector of {n} {dtype} on cuda:{device}, got {tuple(t.shape)} of {t.dtype} on {t.device}")
+def _raw(stream):
+    """A stream argument as the compiled side takes it: None (the current stream) or the handle."""
+    return stream if stream is None or isinstance(stream, int) else stream.cuda_stream
 
 
-def _opt_ptr(t):
-    return None if t is None else t.data_ptr()
-
-
-def _workspace(workspace, need, like):
-    """Address and size of the caller's workspace, or of a new one of ``need`` bytes (kept alive by the third value)."""
-    import torch
-    if workspace is None:
-        if need == 0:
-            return None, 0, None
-        workspace = like.new_empty((need,), dtype=torch.uint8)
-    elif workspace.get_device() != like.get_device() or not workspace.is_contiguous():
-        raise ValueError(f"workspace: contiguous, on {like.device}")
-    return workspace.data_ptr(), workspace.numel() * workspace.element_size(), workspace
-
-
-def _device_of(t, name):
-    """Number of the CUDA device of the matrix ``t``, which has to be the current one (the kernels are launched there)."""
-    import torch
-    device = t.get_device()
-    if device < 0 or t.dim() != 2:
-        raise ValueError(f"{name}: a CUDA matrix, got {tuple(t.shape)} on {t.device}")
-    if device != torch.cuda.current_device():
-        raise ValueError(f"{name} is on cuda:{device}, the current device is cuda:{torch.cuda.current_device()}")
-    return device
-
-
-def _norm_weights(W, B, N, x_dtype, device):
-    """The type code of the weights (any where there are none)."""
-    given = W if W is not None else B
-    if given is None:
-        return ATB_F32
-    for t, name in ((W, "W"), (B, "B")):
-        if t is not None:
-            _vector(t, N, given.dtype, device, name)
-    return _dtype(given)
-
-
-def _out_matrix(t, like, rows, cols, dtype, device, name):
-    """An output of the caller's, checked, or a new one; and its leading dimension.  ``like``: a tensor on the device, best one
-    of the output's shape and type (a copy of its description costs the host least)."""
-    if t is not None:
-        return t, _matrix(t, rows, cols, dtype, device, name)
-    if like.dtype is dtype and like.shape == (rows, cols) and like.is_contiguous():
-        import torch
-        return torch.empty_like(like), cols
-    return like.new_empty((rows, cols), dtype=dtype), cols
-
-
-def _out_vector(t, like, n, dtype, device, name):
-    if t is not None:
-        _vector(t, n, dtype, device, name)
-        return t
-    if like.dtype is dtype and like.shape == (n,) and like.is_contiguous():
-        import torch
-        return torch.empty_like(like)
-    return like.new_empty((n,), dtype=dtype)
+def _result(r):
+    """The outputs, or the error behind the status that came in their place."""
+    if type(r) is int:
+        _check(r)
+    return r
 
 
 def atb_layer_norm(X, W=None, B=None, eps=1e-5, Y=None, mean=None, rstd=None, stream=None):
     """Layer norm of the rows of ``X`` (float32 or bfloat16 ``[M, N]``); ``W``, ``B``: ``[N]`` of one type, or None.
 
     Returns ``(Y, mean, rstd)``: the result in X's type and the float32 statistics that the backward pass takes."""
-    import torch
-    device = _device_of(X, "X")
-    (M, N), dtype = X.shape, X.dtype
-    ldx = _matrix(X, M, N, dtype, device, "X")
-    w_type = _norm_weights(W, B, N, dtype, device)
-    Y, ldy = _out_matrix(Y, X, M, N, dtype, device, "Y")
-    mean = _out_vector(mean, X, M, torch.float32, device, "mean")
-    rstd = _out_vector(rstd, mean, M, torch.float32, device, "rstd")
-    _check(load_library().atb_layer_norm(M, N, _dtype(X), X.data_ptr(), ldx, w_type, _opt_ptr(W), _opt_ptr(B), eps, Y.data_ptr(), ldy,
-                                         mean.data_ptr(), rstd.data_ptr(), _stream_ptr(stream)))
-    return Y, mean, rstd
+    return _result((_ops or load_ops()).layer_norm(X, W, B, eps, Y, mean, rstd, _raw(stream)))
 
 
 def atb_layer_norm_bfp16(X, W=None, B=None, eps=1e-5, mant=None, exp=None, mean=None, rstd=None, stream=None):
     """Layer norm that leaves as BFP16 planes, the A operand of ``atb_gemm``.  Returns ``(mant, exp, mean, rstd)``."""
-    import torch
-    device = _device_of(X, "X")
-    (M, N), dtype = X.shape, X.dtype
-    ldx = _matrix(X, M, N, dtype, device, "X")
-    w_type = _norm_weights(W, B, N, dtype, device)
-    mant, ldm = _out_matrix(mant, X, M, N, torch.int8, device, "mant")
-    if ldm != N:
-        raise ValueError("mant: contiguous")
-    exp = _out_vector(exp, X, atb_bfp16_exp_bytes(M, N), torch.uint8, device, "exp")
-    mean = _out_vector(mean, X, M, torch.float32, device, "mean")
-    rstd = _out_vector(rstd, mean, M, torch.float32, device, "rstd")
-    _check(load_library().atb_layer_norm_bfp16(M, N, _dtype(X), X.data_ptr(), ldx, w_type, _opt_ptr(W), _opt_ptr(B), eps,
-                                               mant.data_ptr(), exp.data_ptr(), mean.data_ptr(), rstd.data_ptr(), _stream_ptr(stream)))
-    return mant, exp, mean, rstd
+    return _result((_ops or load_ops()).layer_norm_bfp16(X, W, B, eps, mant, exp, mean, rstd, _raw(stream)))
 
 
 def atb_layer_norm_backward_workspace_bytes(M: int, N: int) -> int:
@@ -503,44 +430,7 @@ def atb_layer_norm_backward_workspace_bytes(M: int, N: int) -> int:
 
 def atb_layer_norm_backward(dY, X, W, mean, rstd, dX=None, dW=None, dB=None, workspace=None, stream=None):
     """Gradients ``(dX, dW, dB)`` of ``atb_layer_norm``; dW and dB in W's type (float32 where W is None)."""
-    import torch
-    device = _device_of(X, "X")
-    (M, N), dtype = X.shape, X.dtype
-    ldx = _matrix(X, M, N, dtype, device, "X")
-    lddy = _matrix(dY, M, N, dtype, device, "dY")
-    w_dtype = torch.float32
-    if W is not None:
-        w_dtype = W.dtype
-        _vector(W, N, w_dtype, device, "W")
-    _vector(mean, M, torch.float32, device, "mean")
-    _vector(rstd, M, torch.float32, device, "rstd")
-    dX, lddx = _out_matrix(dX, X, M, N, dtype, device, "dX")
-    dW = _out_vector(dW, X if W is None else W, N, w_dtype, device, "dW")
-    dB = _out_vector(dB, dW, N, w_dtype, device, "dB")
-    lib = load_library()
-    ws, ws_bytes, workspace = _workspace(workspace, lib.atb_layer_norm_backward_workspace_bytes(M, N), X)
-    _check(lib.atb_layer_norm_backward(M, N, _dtype(X), dY.data_ptr(), lddy, X.data_ptr(), ldx, _dtype(dW), _opt_ptr(W), mean.data_ptr(),
-                                       rstd.data_ptr(), dX.data_ptr(), lddx, dW.data_ptr(), dB.data_ptr(), ws, ws_bytes, _stream_ptr(stream)))
-    return dX, dW, dB
-
-
-def _ffn_shapes(X, Wg, Wu, Wd):
-    import torch
-    device, bf16 = _device_of(X, "X"), torch.bfloat16
-    (M, D), F = X.shape, Wd.shape[0]
-    ldx, ldw, ldwd = _matrix(X, M, D, bf16, device, "X"), _matrix(Wg, D, F, bf16, device, "Wg"), _matrix(Wd, F, D, bf16, device, "Wd")
-    if _matrix(Wu, D, F, bf16, device, "Wu") != ldw:
-        raise ValueError("Wg and Wu need the same row stride")
-    return M, D, F, ldx, ldw, ldwd, device
-
-
-def _hidden(t, like, M, F, device, name):
-    """H, G or U: the caller's, contiguous, or a new one."""
-    import torch
-    t, ld = _out_matrix(t, like, M, F, torch.bfloat16, device, name)
-    if ld != F:
-        raise ValueError(f"{name}: contiguous")
-    return t
+    return _result((_ops or load_ops()).layer_norm_backward(dY, X, W, mean, rstd, dX, dW, dB, workspace, _raw(stream)))
 
 
 def _act(act):
@@ -555,17 +445,8 @@ def atb_gated_ffn(X, Wg, Wu, Wd, act="silu", save=False, Y=None, H=None, G=None,
     """``Y = (act(X Wg) * (X Wu)) Wd`` on bfloat16 matrices ``X [M, D]``, ``Wg``, ``Wu`` ``[D, F]``, ``Wd [F, D]``.
 
     ``act``: "silu", "gelu" or "gelu_tanh".  Returns Y, or with ``save`` ``(Y, H, G, U)``: what the backward pass takes."""
-    import torch
-    M, D, F, ldx, ldw, ldwd, device = _ffn_shapes(X, Wg, Wu, Wd)
-    Y, ldy = _out_matrix(Y, X, M, D, torch.bfloat16, device, "Y")
-    H = _hidden(H, X, M, F, device, "H")
-    if save or G is not None or U is not None:
-        G, U = _hidden(G, H, M, F, device, "G"), _hidden(U, H, M, F, device, "U")
-    lib = load_library()
-    ws, ws_bytes, workspace = _workspace(workspace, lib.atb_gated_ffn_workspace_bytes(M, D, F), X)
-    _check(lib.atb_gated_ffn(M, D, F, _act(act), X.data_ptr(), ldx, Wg.data_ptr(), Wu.data_ptr(), ldw, Wd.data_ptr(), ldwd, Y.data_ptr(), ldy,
-                             H.data_ptr(), _opt_ptr(G), _opt_ptr(U), ws, ws_bytes, _stream_ptr(stream)))
-    return (Y, H, G, U) if save else Y
+    r = _result((_ops or load_ops()).gated_ffn(X, Wg, Wu, Wd, _act(act), save, Y, H, G, U, workspace, _raw(stream)))
+    return r if save else r[0]
 
 
 def atb_gated_ffn_backward_workspace_bytes(M: int, D: int, F: int) -> int:
@@ -574,34 +455,7 @@ def atb_gated_ffn_backward_workspace_bytes(M: int, D: int, F: int) -> int:
 
 def atb_gated_ffn_backward(dY, X, Wg, Wu, Wd, H, G, U, act="silu", dX=None, dWg=None, dWu=None, dWd=None, workspace=None, stream=None):
     """Gradients ``(dX, dWg, dWu, dWd)`` of ``atb_gated_ffn`` from ``dY`` and the ``H``, ``G``, ``U`` that it saved."""
-    import torch
-    M, D, F, ldx, ldw, ldwd, device = _ffn_shapes(X, Wg, Wu, Wd)
-    bf16 = torch.bfloat16
-    lddy = _matrix(dY, M, D, bf16, device, "dY")
-    for t, name in ((H, "H"), (G, "G"), (U, "U")):
-        if _matrix(t, M, F, bf16, device, name) != F:
-            raise ValueError(f"{name}: contiguous")
-    dX, lddx = _out_matrix(dX, X, M, D, bf16, device, "dX")
-    dWg, lddw = _out_matrix(dWg, Wg, D, F, bf16, device, "dWg")
-    dWu, lddu = _out_matrix(dWu, Wu, D, F, bf16, device, "dWu")
-    dWd, lddwd = _out_matrix(dWd, Wd, F, D, bf16, device, "dWd")
-    if lddu != lddw:
-        raise ValueError("dWg and dWu need the same row stride")
-    lib = load_library()
-    ws, ws_bytes, workspace = _workspace(workspace, lib.atb_gated_ffn_backward_workspace_bytes(M, D, F), X)
-    _check(lib.atb_gated_ffn_backward(M, D, F, _act(act), dY.data_ptr(), lddy, X.data_ptr(), ldx, Wg.data_ptr(), Wu.data_ptr(), ldw,
-                                      Wd.data_ptr(), ldwd, H.data_ptr(), G.data_ptr(), U.data_ptr(), dX.data_ptr(), lddx, dWg.data_ptr(),
-                                      dWu.data_ptr(), lddw, dWd.data_ptr(), lddwd, ws, ws_bytes, _stream_ptr(stream)))
-    return dX, dWg, dWu, dWd
-
-
-def _head_shapes(X, W, labels):
-    import torch
-    device = _device_of(X, "X")
-    (M, D), V = X.shape, W.shape[0]
-    ldx, ldw = _matrix(X, M, D, torch.bfloat16, device, "X"), _matrix(W, V, D, torch.bfloat16, device, "W")
-    _vector(labels, M, torch.int64, device, "labels")
-    return M, V, D, ldx, ldw, device
+    return _result((_ops or load_ops()).gated_ffn_backward(dY, X, Wg, Wu, Wd, H, G, U, _act(act), dX, dWg, dWu, dWd, workspace, _raw(stream)))
 
 
 def atb_linear_cross_entropy_workspace_bytes(M: int, V: int, D: int) -> int:
@@ -612,15 +466,7 @@ def atb_linear_cross_entropy(X, W, labels, ignore_index=-100, loss=None, lse=Non
     """Cross entropy of the logits ``X W^T`` (bfloat16 ``X [M, D]``, ``W [V, D]``, int64 ``labels [M]``), which are not kept.
 
     Returns float32 ``(loss, lse)``, ``[M]`` each; rows whose label is ``ignore_index`` have loss 0."""
-    import torch
-    M, V, D, ldx, ldw, device = _head_shapes(X, W, labels)
-    loss = _out_vector(loss, X, M, torch.float32, device, "loss")
-    lse = _out_vector(lse, loss, M, torch.float32, device, "lse")
-    lib = load_library()
-    ws, ws_bytes, workspace = _workspace(workspace, lib.atb_linear_cross_entropy_workspace_bytes(M, V, D), X)
-    _check(lib.atb_linear_cross_entropy(M, V, D, X.data_ptr(), ldx, W.data_ptr(), ldw, labels.data_ptr(), ignore_index, loss.data_ptr(),
-                                        lse.data_ptr(), ws, ws_bytes, _stream_ptr(stream)))
-    return loss, lse
+    return _result((_ops or load_ops()).linear_cross_entropy(X, W, labels, ignore_index, loss, lse, workspace, _raw(stream)))
 
 
 def atb_linear_cross_entropy_backward_workspace_bytes(M: int, V: int, D: int, piece: int = 0) -> int:
@@ -629,18 +475,7 @@ def atb_linear_cross_entropy_backward_workspace_bytes(M: int, V: int, D: int, pi
 
 def atb_linear_cross_entropy_backward(dloss, X, W, labels, lse, ignore_index=-100, dX=None, dW=None, piece=0, workspace=None, stream=None):
     """Gradients ``(dX, dW)`` (bfloat16) of ``sum(dloss * loss)``; ``piece``: words of the vocabulary per pass (0: chosen)."""
-    import torch
-    M, V, D, ldx, ldw, device = _head_shapes(X, W, labels)
-    _vector(dloss, M, torch.float32, device, "dloss")
-    _vector(lse, M, torch.float32, device, "lse")
-    dX, lddx = _out_matrix(dX, X, M, D, torch.bfloat16, device, "dX")
-    dW, lddw = _out_matrix(dW, W, V, D, torch.bfloat16, device, "dW")
-    lib = load_library()
-    ws, ws_bytes, workspace = _workspace(workspace, lib.atb_linear_cross_entropy_backward_workspace_bytes(M, V, D, piece), X)
-    _check(lib.atb_linear_cross_entropy_backward(M, V, D, X.data_ptr(), ldx, W.data_ptr(), ldw, labels.data_ptr(), ignore_index,
-                                                 lse.data_ptr(), dloss.data_ptr(), dX.data_ptr(), lddx, dW.data_ptr(), lddw, piece, ws, ws_bytes,
-                                                 _stream_ptr(stream)))
-    return dX, dW
+    return _result((_ops or load_ops()).linear_cross_entropy_backward(dloss, X, W, labels, lse, ignore_index, dX, dW, piece, workspace, _raw(stream)))
 
 
 # ------------------------------------------------------------------ layout helpers (no arithmetic)

@@ -76,9 +76,33 @@ def _build(lib: str, obj_dir: str, extra: list, force: bool, verbose: bool) -> s
     return lib
 
 
+TORCH_MODULE = os.path.join(HERE, "_atb_torch.so")
+TORCH_SOURCE = os.path.join(CSRC, "atb_torch.cpp")
+
+
+def build_torch_module(force: bool = False) -> str:
+    """Compiles the tensor side of the binding (``_atb_torch.so``, host code against the installed torch).  Returns its path."""
+    import sysconfig
+    import torch
+    deps = [TORCH_SOURCE, os.path.join(ROOT, "include", "atb.h")]
+    if not force and os.path.exists(TORCH_MODULE) and all(os.path.getmtime(d) <= os.path.getmtime(TORCH_MODULE) for d in deps):
+        return TORCH_MODULE
+    tdir = os.path.dirname(torch.__file__)
+    # nvcc as the driver of the host compiler, as for the library: the two share its C++ runtime
+    cmd = [_nvcc(), "-std=c++17", "-O2", "-shared", "-Xcompiler", "-fPIC", "-D_GLIBCXX_USE_CXX11_ABI=%d" % torch.compiled_with_cxx11_abi(),
+           "-I", os.path.join(tdir, "include"), "-I", os.path.join(tdir, "include", "torch", "csrc", "api", "include"),
+           "-I", sysconfig.get_paths()["include"], "-I", os.path.join(ROOT, "include"), "-cudart", "none",
+           TORCH_SOURCE, "-o", TORCH_MODULE, "-L", os.path.join(tdir, "lib"), "-ltorch_python", "-ltorch_cpu", "-lc10_cuda", "-lc10"]
+    r = subprocess.run(cmd, stdout=subprocess.PIPE, stderr=subprocess.STDOUT, text=True)
+    if r.returncode != 0:
+        raise RuntimeError("the torch module does not build: %s\n%s" % (" ".join(cmd), r.stdout))
+    return TORCH_MODULE
+
+
 if __name__ == "__main__":
     import sys
     print(build_library(force="--force" in sys.argv, verbose="-v" in sys.argv))
+    print(build_torch_module(force="--force" in sys.argv))
     for name in VARIANTS:
         if "--variants" in sys.argv:
             print(build_library(force="--force" in sys.argv, variant=name))

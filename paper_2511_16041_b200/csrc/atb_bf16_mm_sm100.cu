@@ -639,17 +639,16 @@ size_t partial_bytes(const atb::MmProblem& q, int splits) {
 }
 
 // Steps that the slowest unit has: items in order of their length, dealt out to and fro (mm_item_at).  Three units are looked
-// at; where there are many rounds, all are close to the even share.
+// at; where there are many rounds, all are close to the even share, unless one of the longest items is more than that.
 double slowest_unit(const int64_t* count, const double* length, int n, int units) {
     int64_t items = 0;
-    double work = 0, shortest = 1e300;
+    double work = 0, shortest = length[n - 1];
     for (int j = 0; j < n; ++j) {
         items += count[j];
         work += static_cast<double>(count[j]) * length[j];
-        if (length[j] < shortest) shortest = length[j];
     }
     const int64_t rounds = atb::ceil_div(items, units);
-    if (rounds > 8) return work / units + 0.5 * shortest;
+    if (rounds > 8) return std::max(work / units + 0.5 * shortest, length[0] + static_cast<double>(rounds - 1) * shortest);
     double most = 0;
     for (const int u : {0, units / 2, units - 1}) {
         double load = 0;
@@ -687,8 +686,8 @@ MmPlan make_plan(const atb::MmProblem* q, int n) {
             all_tiles += tiles[j];
         }
         if (form && !tall) continue;
-        for (int s = 1; s <= 16; ++s) {
-            if (s > 1 && all_tiles * (s - 1) >= 4ll * units) break;
+        for (const int s : {1, 2, 3, 4, 6, 8, 12, 16}) {
+            if (s > 1 && all_tiles * s > 4ll * units) break;
             MmPlan c;
             c.pair = form == 1;
             double bytes = 0, len[kMmGroup];

@@ -40,6 +40,13 @@ int gradient_products(atb::MmProblem* q, int64_t M, int64_t D, int64_t F, bool d
     if (dwd) { q[n] = atb::mm_sizes(atb::kMmStore, F, D, M); q[n++].layout = atb::kMmTN; }
     return n;
 }
+// Workspace of the gradients wanted: dg and du, and the sums of products that are split along K.
+size_t gradient_bytes(int64_t M, int64_t D, int64_t F, bool dx, bool dw, bool dwd) {
+    atb::MmProblem q[atb::kMmGroup];
+    const atb::MmProblem dh = atb::mm_sizes(atb::kMmGluBackward, M, F, D);
+    const int n = gradient_products(q, M, D, F, dx, dw, dwd);
+    return glu_gradient_bytes(M, F) + std::max(atb::mm_partial_bytes(&dh, 1), n ? atb::mm_partial_bytes(q, n) : 0);
+}
 
 }  // namespace
 
@@ -92,15 +99,9 @@ extern "C" atb_status_t atb_gated_ffn(int64_t M, int64_t D, int64_t F, int act, 
 
 extern "C" size_t atb_gated_ffn_backward_workspace_bytes(int64_t M, int64_t D, int64_t F) {
     if (M < 1 || D < 1 || F < 1) return 0;
-    // dg and du, and the sums of products that are split along K: the largest need of any choice of gradients
-    const atb::MmProblem dh = atb::mm_sizes(atb::kMmGluBackward, M, F, D);
-    size_t sums = atb::mm_partial_bytes(&dh, 1);
-    for (int wanted = 1; wanted < 8; ++wanted) {
-        atb::MmProblem q[atb::kMmGroup];
-        const int n = gradient_products(q, M, D, F, wanted & 1, wanted & 2, wanted & 4);
-        sums = std::max(sums, atb::mm_partial_bytes(q, n));
-    }
-    return glu_gradient_bytes(M, F) + sums;
+    size_t need = 0;                       // the largest of any choice of gradients
+    for (int wanted = 1; wanted < 8; ++wanted) need = std::max(need, gradient_bytes(M, D, F, wanted & 1, wanted & 2, wanted & 4));
+    return need;
 }
 
 extern "C" atb_status_t atb_gated_ffn_backward(int64_t M, int64_t D, int64_t F, int act, const void* dY_dev, int64_t lddy, const void* X_dev,
@@ -120,7 +121,7 @@ extern "C" atb_status_t atb_gated_ffn_backward(int64_t M, int64_t D, int64_t F, 
     for (const void* p : {dY_dev, X_dev, Wg_dev, Wu_dev, Wd_dev, H_dev, G_dev, U_dev, (const void*)dX_dev, (const void*)dWg_dev, (const void*)dWu_dev,
                           (const void*)dWd_dev, (const void*)workspace_dev})
         if (!atb::aligned16(p)) return atb::fail(ATB_ERR_MISALIGNED, "all device pointers must be 16-byte aligned");
-    const size_t need = atb_gated_ffn_backward_workspace_bytes(M, D, F);
+    const size_t need = M > 0 ? gradient_bytes(M, D, F, dX_dev, dWg_dev, dWd_dev) : 0;
     if (workspace_bytes < need) return atb::fail(ATB_ERR_BUFFER_TOO_SMALL, "workspace of %zu bytes is smaller than the %zu needed", workspace_bytes, need);
     cudaStream_t st = static_cast<cudaStream_t>(stream);
     if (M == 0) {          // no rows: the sums over them are 0

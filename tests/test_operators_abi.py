@@ -1,5 +1,8 @@
 """Refusals of the layer norm, gated feed-forward and linear cross entropy entry points: checked on the host before
 anything is launched, so they need no GPU (pointers are never followed)."""
+import pytest
+import torch
+
 import paper_2511_16041_b200 as atb
 
 P = 1 << 20                                                   # an aligned address that nothing reads
@@ -113,3 +116,13 @@ def test_linear_cross_entropy_backward_refusals():
         assert call(**{name: None}) == NULL, name
         assert call(**{name: P + 2}) == MISALIGNED, name
     assert call(n=need - 1) == SMALL
+
+
+def test_the_binding_refuses_tensors_that_are_not_on_a_gpu():
+    x, v, l = torch.zeros(4, 16), torch.zeros(16), torch.zeros(4, dtype=torch.int64)
+    for call in (lambda: atb.atb_layer_norm(x, v, v), lambda: atb.atb_layer_norm_bfp16(x, v, v), lambda: atb.atb_layer_norm(None),
+                 lambda: atb.atb_layer_norm_backward(x, x, v, v[:4], v[:4]), lambda: atb.atb_gated_ffn(x, x, x, x),
+                 lambda: atb.atb_gated_ffn_backward(x, x, x, x, x, x, x, x), lambda: atb.atb_linear_cross_entropy(x, x, l),
+                 lambda: atb.atb_linear_cross_entropy_backward(v, x, x, l, v), lambda: atb.atb_layer_norm(3), lambda: atb.atb_layer_norm(v)):
+        with pytest.raises(ValueError):
+            call()
