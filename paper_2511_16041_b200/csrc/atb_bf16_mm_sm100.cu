@@ -678,16 +678,16 @@ MmPlan make_plan(const atb::MmProblem* q, int n) {
     }
     for (int form = 0; form < 2; ++form) {
         const int tile = form ? 256 : 128, units = form ? atb::kSmCount / 2 : atb::kSmCount;
-        int64_t tiles[kMmGroup], all_tiles = 0;
+        int64_t tiles[kMmGroup], longest_tiles = 0;        // longest_tiles: of the products with the longest K
         bool tall = false;                             // a pair needs more than one CTA's rows somewhere
         for (int j = 0; j < n; ++j) {
             tall = tall || q[j].M > 128;
             tiles[j] = atb::ceil_div(q[j].M, tile) * atb::ceil_div(accumulator_columns(q[j]), tile);
-            all_tiles += tiles[j];
+            if (k_steps[j] == longest) longest_tiles += tiles[j];
         }
         if (form && !tall) continue;
         for (const int s : {1, 2, 3, 4, 6, 8, 12, 16}) {
-            if (s > 1 && all_tiles * s > 4ll * units) break;
+            if (s > 1 && longest_tiles * s > 4ll * units) break;
             MmPlan c;
             c.pair = form == 1;
             double bytes = 0, len[kMmGroup];
