@@ -53,9 +53,9 @@ struct MmProblem {
 };
 
 // The sizes alone, for the plans below.
-inline MmProblem mm_sizes(MmEpilogue epilogue, int64_t M, int64_t N, int64_t K, int k_segs = 1, int n_segs = 1) {
+inline MmProblem mm_sizes(MmLayout layout, MmEpilogue epilogue, int64_t M, int64_t N, int64_t K, int k_segs = 1, int n_segs = 1) {
     MmProblem q;
-    q.epilogue = epilogue; q.M = M; q.N = N; q.K = K; q.k_segs = k_segs; q.n_segs = n_segs;
+    q.layout = layout; q.epilogue = epilogue; q.M = M; q.N = N; q.K = K; q.k_segs = k_segs; q.n_segs = n_segs;
     return q;
 }
 

@@ -42,6 +42,7 @@ struct MmJob {
     int m_tiles, n_tiles, n_segs;      // n_tiles: of one segment
     int k_steps0, k_steps;             // steps of the first K segment, of both
     int splits;                        // the K loop is cut into this many ranges, units of work of their own
+    int a_rows;                        // rows of A that a CTA loads: 128, or what there is of a K-major A of 64 rows and less
     int first_item;                    // of this product in the launch's list of (range, tile)
     int fp32, add;                     // C in FP32 (the sums of a range, rows split * split_rows on; or C32), added to it
     int64_t split_rows;
@@ -50,6 +51,8 @@ struct MmJob {
 struct MmParams {
     MmJob job[kMmGroup];
     int n_jobs, items;
+    int stages;                            // of the operand ring, of a_bytes + kMmTileBytes each
+    uint32_t a_bytes;
     unsigned int* error_flag;
     int act, save;
     const int64_t* labels;
@@ -93,11 +96,12 @@ struct MmCfg {
     static constexpr int TILE_N = DUAL ? BN / 2 : BN;       // columns of C per tile
     static constexpr int COLS = DUAL ? 64 : BN / 2;         // columns of C of an epilogue warp (a 64-column tile has one group)
     static constexpr int BOXES = (EPI == atb::kMmGlu || EPI == atb::kMmGluBackward) ? 2 : 1;   // staging boxes of a warp
-    static constexpr int STAGES = BOXES == 2 ? 5 : 6;
     static constexpr uint32_t STAGE_BYTES = 2 * kMmTileBytes;
-    static constexpr uint32_t BOX_OFF = STAGES * STAGE_BYTES;
+    // Ring of operand stages: 5 or 6, more (single CTAs) where A is a few rows and a stage little more than its B tile
+    static constexpr uint32_t BOX_OFF = (BOXES == 2 ? 5 : 6) * STAGE_BYTES;
+    static constexpr int MOST_STAGES = PAIR ? BOX_OFF / STAGE_BYTES : 10;
     static constexpr uint32_t BAR_OFF = BOX_OFF + kMmEpiWarps * BOXES * kEpilogueBoxBytes;
-    static constexpr uint32_t SMEM_BYTES = 1024 + BAR_OFF + 8 * (2 * STAGES + 4 + kMmEpiWarps) + 16;
+    static constexpr uint32_t SMEM_BYTES = 1024 + BAR_OFF + 8 * (2 * MOST_STAGES + 4 + kMmEpiWarps) + 16;
     static_assert(SMEM_BYTES <= kSmemBudget, "shared memory");
 };
 
@@ -391,8 +395,8 @@ bf16_mm_kernel(const __grid_constant__ MmMaps<MmCfg<PAIR, EPI>::JOBS> tm, const 
     extern __shared__ uint8_t smem_raw[];
     const uint32_t smem_base = (smem_u32(smem_raw) + 1023u) & ~1023u;
     const uint32_t bar_base = smem_base + C::BAR_OFF;
-    const uint32_t full = bar_base, empty = full + 8 * C::STAGES;
-    const uint32_t acc_full = empty + 8 * C::STAGES, acc_empty = acc_full + 16, box_bar = acc_empty + 16;
+    const uint32_t full = bar_base, empty = full + 8 * C::MOST_STAGES;
+    const uint32_t acc_full = empty + 8 * C::MOST_STAGES, acc_empty = acc_full + 16, box_bar = acc_empty + 16;
     const uint32_t misc = box_bar + 8 * kMmEpiWarps;       // [0]: TMEM base, [1]: abort flag
     volatile uint32_t* const misc_gen = reinterpret_cast<volatile uint32_t*>(smem_raw + (misc - smem_u32(smem_raw)));
 
@@ -401,7 +405,7 @@ bf16_mm_kernel(const __grid_constant__ MmMaps<MmCfg<PAIR, EPI>::JOBS> tm, const 
     Ctx cx{misc_gen + 1, p.error_flag};
 
     if (threadIdx.x == 0) {
-        for (int i = 0; i < C::STAGES; ++i) { mbar_init(full + 8 * i, 1); mbar_init(empty + 8 * i, 1); }
+        for (int i = 0; i < C::MOST_STAGES; ++i) { mbar_init(full + 8 * i, 1); mbar_init(empty + 8 * i, 1); }
         for (int i = 0; i < 2; ++i) { mbar_init(acc_full + 8 * i, 1); mbar_init(acc_empty + 8 * i, kMmEpiWarps * (PAIR ? 2 : 1)); }
         for (int i = 0; i < kMmEpiWarps; ++i) mbar_init(box_bar + 8 * i, 1);
         misc_gen[1] = 0u;
@@ -419,6 +423,8 @@ bf16_mm_kernel(const __grid_constant__ MmMaps<MmCfg<PAIR, EPI>::JOBS> tm, const 
     if constexpr (PAIR) cluster_sync_all();                // the peer's barriers exist before anything arrives on them
     tcgen05_fence_after_sync();
     const uint32_t tmem_base = misc_gen[0];
+    const int stages = PAIR ? C::MOST_STAGES : p.stages;
+    const uint32_t a_bytes = PAIR ? kMmTileBytes : p.a_bytes, stage_bytes = a_bytes + kMmTileBytes;
     // what a kernel before this one on the stream wrote may be read from here on
     grid_dependency_wait();
     grid_dependency_launch();
@@ -445,14 +451,15 @@ bf16_mm_kernel(const __grid_constant__ MmMaps<MmCfg<PAIR, EPI>::JOBS> tm, const 
                     const int kseg = k >= jb.k_steps0 ? 1 : 0;
                     k -= kseg * jb.k_steps0;
                     if (!(ok = wait_bar_t<true, PAIR>(cx, empty + 8 * r.stage, r.phase ^ 1u, 0x001))) break;
-                    if (rank == 0) mbar_arrive_expect_tx(full + 8 * r.stage, C::STAGE_BYTES * (PAIR ? 2 : 1));
+                    if (rank == 0) mbar_arrive_expect_tx(full + 8 * r.stage, PAIR ? 2 * C::STAGE_BYTES : kMmTileBytes + jb.a_rows * 128u);
                     const uint32_t bar = PAIR ? mapa_shared(full + 8 * r.stage, 0) : full + 8 * r.stage;
-                    const uint32_t dst = smem_base + r.stage * C::STAGE_BYTES;
+                    const uint32_t dst = smem_base + r.stage * stage_bytes;
                     const int b0 = C::DUAL ? (PAIR ? static_cast<int>(rank) : 0) : (w.seg | kseg);
                     const int b1 = C::DUAL ? (PAIR ? static_cast<int>(rank) : 1) : (w.seg | kseg);
-                    mm_load<PAIR>(dst, ta + kseg, ta + kseg, a_mn, m0, m0 + 64, k * kMmKStep, bar);
-                    mm_load<PAIR>(dst + kMmTileBytes, tb + b0, tb + b1, b_mn, n0, n1, k * kMmKStep, bar);
-                    r.advance(C::STAGES);
+                    if (PAIR || jb.a_rows == 128) mm_load<PAIR>(dst, ta + kseg, ta + kseg, a_mn, m0, m0 + 64, k * kMmKStep, bar);
+                    else mm_tma<PAIR>(dst, ta + kseg, k * kMmKStep, m0, bar);       // the tile's other rows are whatever lies behind: no row of C that exists reads them
+                    mm_load<PAIR>(dst + a_bytes, tb + b0, tb + b1, b_mn, n0, n1, k * kMmKStep, bar);
+                    r.advance(stages);
                 }
             }
         }
@@ -474,8 +481,8 @@ bf16_mm_kernel(const __grid_constant__ MmMaps<MmCfg<PAIR, EPI>::JOBS> tm, const 
                 for (int k = 0; k < steps; ++k) {
                     if (!(ok = wait_bar_t<true, PAIR>(cx, full + 8 * r.stage, r.phase, 0x101))) break;
                     tcgen05_fence_after_sync();
-                    const uint32_t as = smem_base + r.stage * C::STAGE_BYTES;
-                    const uint64_t a_desc = mm_desc(as, a_mn), b_desc = mm_desc(as + kMmTileBytes, b_mn);
+                    const uint32_t as = smem_base + r.stage * stage_bytes;
+                    const uint64_t a_desc = mm_desc(as, a_mn), b_desc = mm_desc(as + a_bytes, b_mn);
 #pragma unroll
                     for (int kk = 0; kk < kMmKStep / 16; ++kk) {
                         const uint32_t accumulate = (k > 0 || kk > 0) ? 1u : 0u;
@@ -485,7 +492,7 @@ bf16_mm_kernel(const __grid_constant__ MmMaps<MmCfg<PAIR, EPI>::JOBS> tm, const 
                             umma_f16_ss(tmem_base + acc * C::BN, a_desc + kk * a_step, b_desc + kk * b_step, idesc, accumulate);
                     }
                     if constexpr (PAIR) umma_commit_pair(empty + 8 * r.stage, 3); else umma_commit(empty + 8 * r.stage);
-                    r.advance(C::STAGES);
+                    r.advance(stages);
                 }
                 if (!ok) break;
                 if constexpr (PAIR) umma_commit_pair(acc_full + 8 * acc, 3); else umma_commit(acc_full + 8 * acc);
@@ -542,9 +549,9 @@ struct MmDevice {
 MmDevice g_mm_devices[64];
 std::mutex g_mm_mutex;
 
-bool operand_map(CUtensorMap* m, const atb::MmOperand& o, bool mn_major, int64_t mn, int64_t K) {
+bool operand_map(CUtensorMap* m, const atb::MmOperand& o, bool mn_major, int64_t mn, int64_t K, int rows = 64) {
     return make_map_2d(m, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 2, o.base, static_cast<uint64_t>(mn_major ? mn : K),
-                       static_cast<uint64_t>(mn_major ? K : mn), static_cast<uint64_t>(o.ld) * 2, 64, 64, CU_TENSOR_MAP_SWIZZLE_128B);
+                       static_cast<uint64_t>(mn_major ? K : mn), static_cast<uint64_t>(o.ld) * 2, 64, static_cast<uint32_t>(rows), CU_TENSOR_MAP_SWIZZLE_128B);
 }
 
 // Joins the K ranges of split products: sums of the ranges in their order, then what the epilogue would have done.
@@ -625,6 +632,9 @@ __global__ void __launch_bounds__(256) bf16_mm_join_kernel(const __grid_constant
     }
 }
 
+// A is stored along K and has so few rows that one box holds them.
+bool few_rows(const atb::MmProblem& q) { return q.layout != atb::kMmTN && q.M <= 64; }
+
 // How a launch is laid out on the SMs: the form, the K ranges of each product, and the order of the products in the list of
 // work items (longest items first).
 struct MmPlan {
@@ -666,13 +676,18 @@ double slowest_unit(const int64_t* count, const double* length, int n, int units
 
 // Cycles of the candidates, by what measured: a K-step of 64 takes 512 cycles in both forms (the pair's 256 x 256 tile is
 // bound by the tensor cores; the single CTA's 128 x 128 tile has half the reuse, and its 32 KB per step arrive no
-// faster), the last work item 2500 more to fill and drain, and joining K ranges 4000 for a launch and the FP32
+// faster), 650 where A is a few rows and B alone has to arrive, from memory; all operands come from memory at 3400 bytes per
+// cycle, if that is more; the last work item 2500 more to fill and drain, and joining K ranges 4000 for a launch and the FP32
 // sums, written and read once, at 3 KB per cycle.
 MmPlan make_plan(const atb::MmProblem* q, int n) {
     MmPlan best;
     double least = 1e300;
     int64_t k_steps[kMmGroup], longest = 1;
+    double operand_bytes = 0;
+    bool few = true;
     for (int j = 0; j < n; ++j) {
+        few = few && few_rows(q[j]);
+        operand_bytes += 2.0 * static_cast<double>(q[j].K * q[j].k_segs) * static_cast<double>(q[j].M + accumulator_columns(q[j]));
         k_steps[j] = atb::ceil_div(q[j].K, kMmKStep) * q[j].k_segs;
         if (k_steps[j] > longest) longest = k_steps[j];
     }
@@ -686,6 +701,7 @@ MmPlan make_plan(const atb::MmProblem* q, int n) {
             if (k_steps[j] == longest) longest_tiles += tiles[j];
         }
         if (form && !tall) continue;
+        const double step = few && !form ? 650.0 : 512.0;
         for (const int s : {1, 2, 3, 4, 6, 8, 12, 16}) {
             if (s > 1 && longest_tiles * s > 4ll * units) break;
             MmPlan c;
@@ -706,7 +722,8 @@ MmPlan make_plan(const atb::MmProblem* q, int n) {
             int64_t count[kMmGroup];
             double length[kMmGroup];
             for (int i = 0; i < n; ++i) { count[i] = tiles[c.order[i]] * c.splits[c.order[i]]; length[i] = len[c.order[i]]; }
-            const double t = 512.0 * slowest_unit(count, length, n, units) + 2500.0 + (c.split ? 4000.0 + bytes / 3000.0 : 0.0);
+            const double t = std::max(step * slowest_unit(count, length, n, units), operand_bytes / 3400.0) + 2500.0 +
+                             (c.split ? 4000.0 + bytes / 3000.0 : 0.0);
             if (t < least * 0.98) { least = t; best = c; }
         }
     }
@@ -761,15 +778,18 @@ atb_status_t launch(const atb::MmProblem* q, int n, const MmPlan& plan, char* pa
         const bool a_mn = x.layout == atb::kMmTN, b_mn = x.layout != atb::kMmNT;
         const int n_segs = C::DUAL ? 1 : (x.epilogue == atb::kMmGlu ? 2 : x.n_segs);     // a split gated product: two side by side
         const int n_b = C::DUAL || n_segs == 2 ? 2 : x.k_segs;
+        const bool few = !PAIR && few_rows(x);                     // one box of A holds every row
+        const int a_box = few ? static_cast<int>(atb::round_up(x.M, 8)) : 64;
         for (int s = 0; s < 2; ++s) {
             if (s >= x.k_segs) tm.a[2 * i + s] = tm.a[2 * i];
-            else if (!operand_map(&tm.a[2 * i + s], x.A[s], a_mn, x.M, x.K)) return atb::fail(ATB_ERR_CUDA, "cuTensorMapEncodeTiled failed for A");
+            else if (!operand_map(&tm.a[2 * i + s], x.A[s], a_mn, x.M, x.K, a_box)) return atb::fail(ATB_ERR_CUDA, "cuTensorMapEncodeTiled failed for A");
             if (s >= n_b) tm.b[2 * i + s] = tm.b[2 * i];
             else if (!operand_map(&tm.b[2 * i + s], x.B[s], b_mn, x.N, x.K)) return atb::fail(ATB_ERR_CUDA, "cuTensorMapEncodeTiled failed for B");
         }
         MmJob& jb = p.job[i];
         jb.M = x.M; jb.N = x.N;
         jb.a_mn = a_mn; jb.b_mn = b_mn;
+        jb.a_rows = few ? a_box : 128;
         jb.m_tiles = static_cast<int>(atb::ceil_div(x.M, C::TILE_M));
         jb.n_tiles = static_cast<int>(atb::ceil_div(x.N, C::TILE_N));
         jb.n_segs = n_segs;
@@ -802,6 +822,10 @@ atb_status_t launch(const atb::MmProblem* q, int n, const MmPlan& plan, char* pa
             }
         }
     }
+    int a_rows = 0;
+    for (int i = 0; i < n; ++i) a_rows = std::max(a_rows, p.job[i].a_rows);
+    p.a_bytes = static_cast<uint32_t>(a_rows) * 128u;          // a_rows is a multiple of 8: whole swizzle atoms of 1 KB
+    p.stages = std::min<int>(C::MOST_STAGES, C::BOX_OFF / (p.a_bytes + kMmTileBytes));
     p.n_jobs = n;
     p.items = static_cast<int>(items);
     p.error_flag = dev.flag;
@@ -912,7 +936,7 @@ unsigned int take_mm_error_flag() {
 }
 
 int64_t mm_stats_per_row(int64_t M, int64_t N, int64_t K) {
-    const MmProblem q = mm_sizes(kMmRowStats, M, N, K);
+    const MmProblem q = mm_sizes(kMmNT, kMmRowStats, M, N, K);
     return ceil_div(N, make_plan(&q, 1).pair ? 128 : 64);
 }
 

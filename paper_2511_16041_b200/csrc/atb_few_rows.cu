@@ -1,4 +1,4 @@
-// Products of a few rows (a token or a handful, M <= kFewRows) with a weight matrix stored [K][N] (sm_100a):
+// Products of one or two rows (M <= kFewRows) with a weight matrix stored [K][N] (sm_100a):
 //   y = x W, or with two matrices of one shape  h = act(x Wg) * (x Wu).
 //
 // Bound by memory: every weight is read once, for 2 M operations.  A cluster of CTAs takes COLS = 64 or 32 columns (128 or 64
@@ -33,7 +33,7 @@ struct FewParams {
 
 // CTAs per SM (launch bounds): what leaves every thread the registers for its loads in flight (32 per matrix) and its sums
 // (8 per row and matrix).
-constexpr int resident(int MT, int NW) { return NW == 1 ? (MT == 1 ? 7 : 5) : (MT <= 2 ? 4 : 3); }
+constexpr int resident(int MT, int NW) { return NW == 2 ? 4 : MT == 1 ? 7 : 5; }
 
 
 __device__ __forceinline__ float lo(uint32_t w) { return __uint_as_float(w << 16); }
@@ -84,7 +84,7 @@ __global__ void __launch_bounds__(kThreads, resident(MT, NW)) few_rows_kernel(co
     const auto load_x = [&] {
 #pragma unroll
         for (int m = 0; m < MT; ++m)
-            xv[m] = (MT == 1 || m < p.M) ? *reinterpret_cast<const uint4*>(p.x + m * p.ldx + k) : make_uint4(0, 0, 0, 0);
+            xv[m] = *reinterpret_cast<const uint4*>(p.x + m * p.ldx + k);
     };
     if (mine) {
         if (k < p.K) load_x();
@@ -146,7 +146,7 @@ __global__ void __launch_bounds__(kThreads, resident(MT, NW)) few_rows_kernel(co
 #pragma unroll
             for (int n = 0; n < NW; ++n) v[n] += s[(n * MT + m) * COLS + c];
         }
-        if (m < p.M && col0 + c < p.N) {
+        if (col0 + c < p.N) {
             if constexpr (NW == 1) {
                 p.y[m * p.ldy + col0 + c] = __float2bfloat16_rn(v[0]);
             } else {
@@ -212,8 +212,7 @@ atb_status_t run(const FewParams& p, cudaStream_t stream) {
     int sms = 0;
     const atb_status_t s = atb::op_device(&sms);
     if (s != ATB_OK) return s;
-    const cudaError_t e = p.M == 1 ? launch<1, NW>(p, sms, stream) : p.M == 2 ? launch<2, NW>(p, sms, stream)
-                                  : launch<4, NW>(p, sms, stream);
+    const cudaError_t e = p.M == 1 ? launch<1, NW>(p, sms, stream) : launch<2, NW>(p, sms, stream);
     if (e != cudaSuccess) return atb::fail(ATB_ERR_CUDA, "few-row product launch: %s", cudaGetErrorString(e));
     return ATB_OK;
 }

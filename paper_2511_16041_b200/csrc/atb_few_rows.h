@@ -6,7 +6,7 @@
 
 namespace atb {
 
-constexpr int64_t kFewRows = 4;      // the most rows
+constexpr int64_t kFewRows = 2;      // the most rows
 
 // Y = X W (W [K][N]), and H = act(X Wg) * (X Wu) with the two products in G and U where those are not NULL (H, G, U [M][N]).
 // weights_settled: the kernel ahead on the stream is one of this library's, which waits for all before it and does not write W;

@@ -35,15 +35,15 @@ size_t glu_gradient_bytes(int64_t M, int64_t F) { return (4 * static_cast<size_t
 // The products behind dh, which are one launch: sizes and layouts of those wanted.
 int gradient_products(atb::MmProblem* q, int64_t M, int64_t D, int64_t F, bool dx, bool dw, bool dwd) {
     int n = 0;
-    if (dx) { q[n] = atb::mm_sizes(atb::kMmStore, M, D, F, 2, 1); q[n++].layout = atb::kMmNT; }
-    if (dw) { q[n] = atb::mm_sizes(atb::kMmStore, D, F, M, 1, 2); q[n++].layout = atb::kMmTN; }
-    if (dwd) { q[n] = atb::mm_sizes(atb::kMmStore, F, D, M); q[n++].layout = atb::kMmTN; }
+    if (dx) q[n++] = atb::mm_sizes(atb::kMmNT, atb::kMmStore, M, D, F, 2, 1);
+    if (dw) q[n++] = atb::mm_sizes(atb::kMmTN, atb::kMmStore, D, F, M, 1, 2);
+    if (dwd) q[n++] = atb::mm_sizes(atb::kMmTN, atb::kMmStore, F, D, M);
     return n;
 }
 // Workspace of the gradients wanted: dg and du, and the sums of products that are split along K.
 size_t gradient_bytes(int64_t M, int64_t D, int64_t F, bool dx, bool dw, bool dwd) {
     atb::MmProblem q[atb::kMmGroup];
-    const atb::MmProblem dh = atb::mm_sizes(atb::kMmGluBackward, M, F, D);
+    const atb::MmProblem dh = atb::mm_sizes(atb::kMmNT, atb::kMmGluBackward, M, F, D);
     const int n = gradient_products(q, M, D, F, dx, dw, dwd);
     return glu_gradient_bytes(M, F) + std::max(atb::mm_partial_bytes(&dh, 1), n ? atb::mm_partial_bytes(q, n) : 0);
 }
@@ -53,7 +53,7 @@ size_t gradient_bytes(int64_t M, int64_t D, int64_t F, bool dx, bool dw, bool dw
 extern "C" size_t atb_gated_ffn_workspace_bytes(int64_t M, int64_t D, int64_t F) {
     if (M <= atb::kFewRows || D < 1 || F < 1) return 0;
     // the sums of a product that is split along K; the two products take turns
-    const atb::MmProblem up = atb::mm_sizes(atb::kMmGlu, M, F, D), down = atb::mm_sizes(atb::kMmStore, M, D, F);
+    const atb::MmProblem up = atb::mm_sizes(atb::kMmNN, atb::kMmGlu, M, F, D), down = atb::mm_sizes(atb::kMmNN, atb::kMmStore, M, D, F);
     return std::max(atb::mm_partial_bytes(&up, 1), atb::mm_partial_bytes(&down, 1));
 }
 

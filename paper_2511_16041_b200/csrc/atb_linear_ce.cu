@@ -79,8 +79,8 @@ int64_t piece_words(int64_t M, int64_t V, int64_t piece) {
 // The products behind dl of a piece of n words, which are one launch: sizes and layouts of those wanted.
 int gradient_products(atb::MmProblem* q, int64_t M, int64_t n, int64_t D, bool pieces, bool dx, bool dw) {
     int products = 0;
-    if (dx) { q[products] = atb::mm_sizes(pieces ? atb::kMmAccumulate : atb::kMmStore, M, D, n); q[products++].layout = atb::kMmNN; }
-    if (dw) { q[products] = atb::mm_sizes(atb::kMmStore, n, D, M); q[products++].layout = atb::kMmTN; }
+    if (dx) q[products++] = atb::mm_sizes(atb::kMmNN, pieces ? atb::kMmAccumulate : atb::kMmStore, M, D, n);
+    if (dw) q[products++] = atb::mm_sizes(atb::kMmTN, atb::kMmStore, n, D, M);
     return products;
 }
 
