@@ -20,6 +20,7 @@
 
 #include "atb_bf16_mm.h"
 #include "atb_gemm_device.cuh"
+#include "dependent_launch.cuh"
 #include "glu.cuh"
 
 namespace {
@@ -738,25 +739,6 @@ bool output_map(CUtensorMap* m, const void* base, int64_t N, int64_t M, int64_t 
                        static_cast<uint64_t>(M), static_cast<uint64_t>(ld) * sizeof(T), 128 / sizeof(T), 32, CU_TENSOR_MAP_SWIZZLE_128B);
 }
 
-template <class... Args>
-cudaError_t launch_dependent(void (*kernel)(Args...), unsigned grid, unsigned block, unsigned cluster, size_t smem, cudaStream_t stream, Args... args) {
-    cudaLaunchConfig_t cfg = {};
-    cfg.gridDim = dim3(grid, 1, 1);
-    cfg.blockDim = dim3(block, 1, 1);
-    cfg.dynamicSmemBytes = smem;
-    cfg.stream = stream;
-    cudaLaunchAttribute attr[2];
-    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;     // may be set up while the kernel before it drains
-    attr[0].val.programmaticStreamSerializationAllowed = 1;
-    attr[1].id = cudaLaunchAttributeClusterDimension;
-    attr[1].val.clusterDim.x = cluster;
-    attr[1].val.clusterDim.y = 1;
-    attr[1].val.clusterDim.z = 1;
-    cfg.attrs = attr;
-    cfg.numAttrs = cluster > 1 ? 2 : 1;
-    return cudaLaunchKernelEx(&cfg, kernel, args...);
-}
-
 // One kernel over the n products of q.  EPI == kMmPlain: bf16, FP32, or the sums of K ranges in `partial`.
 template <bool PAIR, int EPI>
 atb_status_t launch(const atb::MmProblem* q, int n, const MmPlan& plan, char* partial, const MmDevice& dev, cudaStream_t stream) {
@@ -844,7 +826,7 @@ atb_status_t launch(const atb::MmProblem* q, int n, const MmPlan& plan, char* pa
         if (e != cudaSuccess) return atb::fail(ATB_ERR_CUDA, "cudaFuncSetAttribute: %s", cudaGetErrorString(e));
         allowed.fetch_or(bit, std::memory_order_release);
     }
-    e = launch_dependent(kernel, static_cast<unsigned>(PAIR ? 2 * n_units : n_units), kMmThreads, PAIR ? 2u : 1u, C::SMEM_BYTES, stream, tm, p);
+    e = atb::launch_dependent(kernel, static_cast<unsigned>(PAIR ? 2 * n_units : n_units), kMmThreads, PAIR ? 2u : 1u, C::SMEM_BYTES, stream, tm, p);
     if (e != cudaSuccess) return atb::fail(ATB_ERR_CUDA, "bf16 product launch: %s", cudaGetErrorString(e));
     return ATB_OK;
 }
@@ -873,7 +855,7 @@ atb_status_t join(const atb::MmProblem* q, int n, const MmPlan& plan, const char
     p.act = q->act;
     p.G = static_cast<const __nv_bfloat16*>(q->G); p.U = static_cast<const __nv_bfloat16*>(q->U);
     const int64_t blocks = atb::ceil_div(p.all, 256), most = static_cast<int64_t>(dev.sms) * 8;
-    const cudaError_t e = launch_dependent(bf16_mm_join_kernel<EPI>, static_cast<unsigned>(blocks < most ? blocks : most), 256u, 1u, 0, stream, p);
+    const cudaError_t e = atb::launch_dependent(bf16_mm_join_kernel<EPI>, static_cast<unsigned>(blocks < most ? blocks : most), 256u, 1u, 0, stream, p);
     if (e != cudaSuccess) return atb::fail(ATB_ERR_CUDA, "bf16 product join launch: %s", cudaGetErrorString(e));
     return ATB_OK;
 }

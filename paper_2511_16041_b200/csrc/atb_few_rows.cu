@@ -13,8 +13,8 @@
 #include <algorithm>
 
 #include "atb_few_rows.h"
+#include "dependent_launch.cuh"
 #include "glu.cuh"
-#include "sm100_ptx.cuh"
 
 namespace {
 
@@ -191,20 +191,9 @@ Deal deal(int64_t K, int64_t N, int per_sm, int sms) {
 template <int MT, int NW>
 cudaError_t launch(const FewParams& p, int sms, cudaStream_t stream) {
     const Deal d = deal(p.K, p.N, resident(MT, NW), sms);
-    cudaLaunchConfig_t cfg = {};
-    cfg.gridDim = dim3(static_cast<unsigned>(atb::ceil_div(p.N, d.cols) * d.ranks), 1, 1);
-    cfg.blockDim = dim3(kThreads, 1, 1);
-    cfg.stream = stream;
-    cudaLaunchAttribute attr[2];
-    attr[0].id = cudaLaunchAttributeClusterDimension;
-    attr[0].val.clusterDim.x = static_cast<unsigned>(d.ranks);
-    attr[0].val.clusterDim.y = 1;
-    attr[0].val.clusterDim.z = 1;
-    attr[1].id = cudaLaunchAttributeProgrammaticStreamSerialization;
-    attr[1].val.programmaticStreamSerializationAllowed = 1;
-    cfg.attrs = attr;
-    cfg.numAttrs = 2;
-    return d.cols == 64 ? cudaLaunchKernelEx(&cfg, few_rows_kernel<MT, NW, 64>, p) : cudaLaunchKernelEx(&cfg, few_rows_kernel<MT, NW, 32>, p);
+    const unsigned grid = static_cast<unsigned>(atb::ceil_div(p.N, d.cols) * d.ranks), ranks = static_cast<unsigned>(d.ranks);
+    return d.cols == 64 ? atb::launch_dependent(few_rows_kernel<MT, NW, 64>, grid, kThreads, ranks, 0, stream, p)
+                        : atb::launch_dependent(few_rows_kernel<MT, NW, 32>, grid, kThreads, ranks, 0, stream, p);
 }
 
 template <int NW>

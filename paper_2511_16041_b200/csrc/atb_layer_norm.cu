@@ -20,7 +20,7 @@
 
 #include "atb_internal.h"
 #include "bfp16_block.cuh"
-#include "sm100_ptx.cuh"
+#include "dependent_launch.cuh"
 
 namespace {
 
@@ -580,20 +580,6 @@ int threads_per_row(int64_t N, int most) {
 }
 constexpr int kFwdThreads = 1024, kBwdThreads = 512;      // the backward sums take 2 kElems registers
 
-template <class... Args>
-cudaError_t launch_dependent(void (*kernel)(Args...), unsigned grid, unsigned block, size_t smem, cudaStream_t stream, Args... args) {
-    cudaLaunchConfig_t cfg = {};
-    cfg.gridDim = dim3(grid, 1, 1);
-    cfg.blockDim = dim3(block, 1, 1);
-    cfg.dynamicSmemBytes = smem;
-    cfg.stream = stream;
-    cudaLaunchAttribute attr[1];
-    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;     // may be set up while the kernel before it drains
-    attr[0].val.programmaticStreamSerializationAllowed = 1;
-    cfg.attrs = attr;
-    cfg.numAttrs = 1;
-    return cudaLaunchKernelEx(&cfg, kernel, args...);
-}
 // A kernel whose rows on their way may take more, with its static arrays, than the 48 KB of shared memory that need no leave.
 template <class... Args>
 cudaError_t launch_ring(void (*kernel)(Args...), unsigned grid, unsigned block, size_t smem, cudaStream_t stream, Args... args) {
@@ -601,7 +587,7 @@ cudaError_t launch_ring(void (*kernel)(Args...), unsigned grid, unsigned block, 
         const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(smem));
         if (e != cudaSuccess) return e;
     }
-    return launch_dependent(kernel, grid, block, smem, stream, args...);
+    return atb::launch_dependent(kernel, grid, block, 1u, smem, stream, args...);
 }
 
 template <class TX, class TW, int VEC, bool BFP, int TPR>
@@ -780,10 +766,10 @@ extern "C" atb_status_t atb_layer_norm_backward(int64_t M, int64_t N, int x_type
         const int parts = M > 0 ? partial_sums(M, N) : 0;
         const float* const part = p.part;
         if (w_type == ATB_F32)
-            e = launch_dependent(layer_norm_backward_sum_kernel<float>, blocks, 32u * kSumWarps, 0, st, part, parts, N, static_cast<float*>(dW_dev),
+            e = atb::launch_dependent(layer_norm_backward_sum_kernel<float>, blocks, 32u * kSumWarps, 1u, 0, st, part, parts, N, static_cast<float*>(dW_dev),
                                  static_cast<float*>(dB_dev));
         else
-            e = launch_dependent(layer_norm_backward_sum_kernel<__nv_bfloat16>, blocks, 32u * kSumWarps, 0, st, part, parts, N,
+            e = atb::launch_dependent(layer_norm_backward_sum_kernel<__nv_bfloat16>, blocks, 32u * kSumWarps, 1u, 0, st, part, parts, N,
                                  static_cast<__nv_bfloat16*>(dW_dev), static_cast<__nv_bfloat16*>(dB_dev));
     }
     if (e != cudaSuccess) return atb::fail(ATB_ERR_CUDA, "layer norm backward launch: %s", cudaGetErrorString(e));

@@ -12,30 +12,40 @@
 #include <algorithm>
 
 #include "atb_bf16_mm.h"
+#include "dependent_launch.cuh"
 
 namespace {
 
-// One warp per row: joins the row's (maximum, sum) pairs, in a fixed order.
-__global__ void __launch_bounds__(256) linear_ce_join_kernel(int64_t M, int64_t V, const float2* stats, int64_t per_row, const float* label_logit,
-                                                             const int64_t* labels, int64_t ignore_index, float* loss, float* lse) {
-    const int64_t row = static_cast<int64_t>(blockIdx.x) * 8 + (threadIdx.x >> 5);
-    const int lane = threadIdx.x & 31;
-    if (row >= M) return;
+// (maximum, sum of exp(x - maximum)) of two sets of numbers, of their union; an empty set is (-inf, 0).
+__device__ __forceinline__ void join_stats(float& m, float& s, float m2, float s2) {
+    const float top = fmaxf(m, m2), ref = top == -INFINITY ? 0.f : top;
+    s = s * expf(m - ref) + s2 * expf(m2 - ref);
+    m = top;
+}
+
+// One block per row: joins the row's pairs, in a fixed order.  Latency counts: a row's pairs are few, and where rows are few
+// too this kernel is short of work; the loads of a thread are independent of one another.
+constexpr int kJoinThreads = 128;
+__global__ void __launch_bounds__(kJoinThreads) linear_ce_join_kernel(int64_t V, const float2* stats, int64_t per_row, const float* label_logit,
+                                                                      const int64_t* labels, int64_t ignore_index, float* loss, float* lse) {
+    __shared__ float2 part[kJoinThreads / 32];
+    sm100::grid_dependency_wait();
+    sm100::grid_dependency_launch();
+    const int64_t row = blockIdx.x;
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     float m = -INFINITY, s = 0.f;
-    for (int64_t i = lane; i < per_row; i += 32) {
+#pragma unroll 4
+    for (int64_t i = threadIdx.x; i < per_row; i += kJoinThreads) {
         const float2 v = stats[row * per_row + i];
-        const float top = fmaxf(m, v.x), ref = top == -INFINITY ? 0.f : top;
-        s = s * expf(m - ref) + v.y * expf(v.x - ref);
-        m = top;
+        join_stats(m, s, v.x, v.y);
     }
 #pragma unroll
-    for (int o = 16; o > 0; o >>= 1) {
-        const float m2 = __shfl_xor_sync(0xFFFFFFFFu, m, o), s2 = __shfl_xor_sync(0xFFFFFFFFu, s, o);
-        const float top = fmaxf(m, m2), ref = top == -INFINITY ? 0.f : top;
-        s = s * expf(m - ref) + s2 * expf(m2 - ref);
-        m = top;
-    }
-    if (lane == 0) {
+    for (int o = 16; o > 0; o >>= 1) join_stats(m, s, __shfl_xor_sync(0xFFFFFFFFu, m, o), __shfl_xor_sync(0xFFFFFFFFu, s, o));
+    if (lane == 0) part[warp] = make_float2(m, s);
+    __syncthreads();
+    if (threadIdx.x == 0) {
+#pragma unroll
+        for (int w = 1; w < kJoinThreads / 32; ++w) join_stats(m, s, part[w].x, part[w].y);
         const int64_t label = labels[row];
         float z = m + logf(s), l = 0.f;
         if (label != ignore_index) {
@@ -48,6 +58,8 @@ __global__ void __launch_bounds__(256) linear_ce_join_kernel(int64_t M, int64_t 
 }
 
 __global__ void __launch_bounds__(256) linear_ce_round_kernel(const float* src, int64_t M, int64_t N, __nv_bfloat16* dst, int64_t ld) {
+    sm100::grid_dependency_wait();
+    sm100::grid_dependency_launch();
     const int64_t per_row = N / 8;
     for (int64_t i = static_cast<int64_t>(blockIdx.x) * 256 + threadIdx.x; i < M * per_row; i += static_cast<int64_t>(gridDim.x) * 256) {
         const int64_t m = i / per_row, n = (i - m * per_row) * 8;
@@ -141,9 +153,8 @@ extern "C" atb_status_t atb_linear_cross_entropy(int64_t M, int64_t V, int64_t D
     q.label_logit = reinterpret_cast<float*>(static_cast<char*>(workspace_dev) + (need - static_cast<size_t>(M) * sizeof(float)));
     s = atb::mm_launch(&q, 1, nullptr, st);
     if (s != ATB_OK) return s;
-    linear_ce_join_kernel<<<static_cast<unsigned>(atb::ceil_div(M, 8)), 256, 0, st>>>(M, V, q.stats, q.stats_ld, q.label_logit, labels_dev, ignore_index,
-                                                                                     loss_dev, lse_dev);
-    const cudaError_t e = cudaGetLastError();
+    const cudaError_t e = atb::launch_dependent(linear_ce_join_kernel, static_cast<unsigned>(M), kJoinThreads, 1u, 0, st, V, static_cast<const float2*>(q.stats),
+                                                q.stats_ld, static_cast<const float*>(q.label_logit), labels_dev, ignore_index, loss_dev, lse_dev);
     if (e != cudaSuccess) return atb::fail(ATB_ERR_CUDA, "linear cross entropy launch: %s", cudaGetErrorString(e));
     return ATB_OK;
 }
@@ -213,12 +224,13 @@ extern "C" atb_status_t atb_linear_cross_entropy_backward(int64_t M, int64_t V, 
         s = atb::mm_launch(grad, products, partial, st);
         if (s != ATB_OK) return s;
     }
+    cudaError_t e = cudaSuccess;
     if (dX_dev && words < V) {
         const int64_t vecs = M * (D / 8);
         const int blocks = static_cast<int>(atb::ceil_div(vecs, 256) < sms * 8 ? atb::ceil_div(vecs, 256) : sms * 8);
-        linear_ce_round_kernel<<<blocks, 256, 0, st>>>(sum, M, D, static_cast<__nv_bfloat16*>(dX_dev), lddx);
+        e = atb::launch_dependent(linear_ce_round_kernel, static_cast<unsigned>(blocks), 256u, 1u, 0, st, static_cast<const float*>(sum), M, D,
+                                  static_cast<__nv_bfloat16*>(dX_dev), lddx);
     }
-    const cudaError_t e = cudaGetLastError();
     if (e != cudaSuccess) return atb::fail(ATB_ERR_CUDA, "linear cross entropy backward launch: %s", cudaGetErrorString(e));
     return ATB_OK;
 }
