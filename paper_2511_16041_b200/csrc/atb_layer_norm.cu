@@ -115,6 +115,75 @@ __device__ __forceinline__ void store_f(T* p, const float (&v)[VEC]) {
     }
 }
 
+// ---------------------------------------------------------------------------------- pairs
+// The backward kernel works on its elements in pairs by the two-wide FP32 instructions, which round each half like the scalar
+// ones: 3 to 10 % faster than scalar arithmetic.  (The forward kernel, with half the arithmetic per byte, was 5 to 15 %
+// slower in this form.)
+__device__ __forceinline__ uint64_t bits2(float2 v) {
+    uint64_t r;
+    asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(v.x), "f"(v.y));
+    return r;
+}
+__device__ __forceinline__ float2 pair_of(uint64_t b) {
+    float2 v;
+    asm("mov.b64 {%0, %1}, %2;" : "=f"(v.x), "=f"(v.y) : "l"(b));
+    return v;
+}
+__device__ __forceinline__ float2 add2(float2 a, float2 b) {
+    uint64_t r;
+    asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(bits2(a)), "l"(bits2(b)));
+    return pair_of(r);
+}
+__device__ __forceinline__ float2 mul2(float2 a, float2 b) {
+    uint64_t r;
+    asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(bits2(a)), "l"(bits2(b)));
+    return pair_of(r);
+}
+__device__ __forceinline__ float2 fma2(float2 a, float2 b, float2 c) {
+    uint64_t r;
+    asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(bits2(a)), "l"(bits2(b)), "l"(bits2(c)));
+    return pair_of(r);
+}
+__device__ __forceinline__ float2 both(float v) { return make_float2(v, v); }
+
+// A thread's elements as pairs: NV groups of VEC, pairs of neighbours (VEC = 8) or of one element each of two groups (VEC = 1).
+template <class T, int VEC, int NV>
+__device__ __forceinline__ void to_pairs(const Raw<T, VEC> (&r)[NV], float2 (&v)[NV * VEC / 2]) {
+    static_assert(NV * VEC % 2 == 0, "");
+    if constexpr (VEC == 1) {
+#pragma unroll
+        for (int i = 0; i < NV; i += 2) {
+            float a[1], b[1];
+            to_float(r[i], a);
+            to_float(r[i + 1], b);
+            v[i / 2] = make_float2(a[0], b[0]);
+        }
+    } else {
+#pragma unroll
+        for (int i = 0; i < NV; ++i) {
+            float f[VEC];
+            to_float(r[i], f);
+#pragma unroll
+            for (int e = 0; e < VEC / 2; ++e) v[i * VEC / 2 + e] = make_float2(f[2 * e], f[2 * e + 1]);
+        }
+    }
+}
+// Group i of them.
+template <int VEC, int P>
+__device__ __forceinline__ void group(const float2 (&v)[P], int i, float (&f)[VEC]) {
+    if constexpr (VEC == 1) {
+        f[0] = i & 1 ? v[i / 2].y : v[i / 2].x;
+    } else {
+#pragma unroll
+        for (int e = 0; e < VEC / 2; ++e) { f[2 * e] = v[i * VEC / 2 + e].x; f[2 * e + 1] = v[i * VEC / 2 + e].y; }
+    }
+}
+template <class T, int VEC>
+__device__ __forceinline__ void clear(Raw<T, VEC>& r) {
+#pragma unroll
+    for (int i = 0; i < static_cast<int>(sizeof(r.w) / sizeof(r.w[0])); ++i) r.w[i] = 0;
+}
+
 // ---------------------------------------------------------------------------------- sums over a row's threads
 template <int K>
 __device__ __forceinline__ void warp_sum(float (&v)[K]) {
@@ -334,6 +403,8 @@ __global__ void __launch_bounds__(TPR == 32 ? 128 : TPR, blocks_per_sm(TPR, fals
                 if (p.mean) p.mean[m] = mu;
                 if (p.rstd) p.rstd[m] = r;
             }
+            // z = x r - mu r: the rounded mu r is off by 2^-24 |mu| r, less than what the rounded mean is
+            const float shift = -mu * r;
             TX* const y = BFP ? nullptr : static_cast<TX*>(p.y) + m * p.ldy + col;
 #pragma unroll
             for (int i = 0; i < NV; ++i) {
@@ -342,7 +413,7 @@ __global__ void __launch_bounds__(TPR == 32 ? 128 : TPR, blocks_per_sm(TPR, fals
                     to_float(w[i], fw);
                     to_float(b[i], fb);
 #pragma unroll
-                    for (int e = 0; e < VEC; ++e) v[i][e] = fmaf((v[i][e] - mu) * r, fw[e], fb[e]);
+                    for (int e = 0; e < VEC; ++e) v[i][e] = fmaf(fmaf(v[i][e], r, shift), fw[e], fb[e]);
                     if constexpr (BFP) put_block(p, m, col + i * TPR * VEC, v[i]);
                     else store_f<TX, VEC>(y + i * TPR * VEC, v[i]);
                 }
@@ -411,7 +482,7 @@ template <class TX, class TW, int VEC, int TPR, int NV>
 __global__ void __launch_bounds__(TPR == 32 ? 128 : TPR, blocks_per_sm(TPR, true)) layer_norm_backward_kernel(const BwdParams p) {
     using Source = RowSource<TX, VEC, TPR, NV>;
     constexpr int WALKERS = TPR == 32 ? 4 : 1, W = TPR / 32;
-    constexpr int STAGES = kAhead<TX> + 1;
+    constexpr int STAGES = kAhead<TX> + 1, P = NV * VEC / 2;
     extern __shared__ __align__(16) uint8_t ring[];
     __shared__ float red[2][W][2];
     const int t = TPR == 32 ? threadIdx.x & 31 : threadIdx.x;
@@ -430,13 +501,11 @@ __global__ void __launch_bounds__(TPR == 32 ? 128 : TPR, blocks_per_sm(TPR, true
         async_commit();
     }
     Raw<TW, VEC> w[NV];
-    float dw[NV][VEC], db[NV][VEC];
+    float2 dw[P], db[P];
 #pragma unroll
-    for (int i = 0; i < NV; ++i) {
-        load_or<TW, VEC>(static_cast<const TW*>(p.w), col + i * TPR * VEC, N, 1.f, w[i]);
+    for (int i = 0; i < NV; ++i) load_or<TW, VEC>(static_cast<const TW*>(p.w), col + i * TPR * VEC, N, 1.f, w[i]);
 #pragma unroll
-        for (int e = 0; e < VEC; ++e) dw[i][e] = db[i][e] = 0.f;
-    }
+    for (int k = 0; k < P; ++k) dw[k] = db[k] = make_float2(0.f, 0.f);
     int stage = 0, turn = 0;
     float mu = 0.f, r = 0.f;
     if (first < p.M) { mu = p.mean[first]; r = p.rstd[first]; }
@@ -451,38 +520,49 @@ __global__ void __launch_bounds__(TPR == 32 ? 128 : TPR, blocks_per_sm(TPR, true
         if (m + step < p.M) { next_mu = p.mean[m + step]; next_r = p.rstd[m + step]; }
         async_wait<kAhead<TX>>();
         row_barrier<Source, VEC, TPR>();
-        float z[NV][VEC], g[NV][VEC], s[2] = {0.f, 0.f};
+        // elements past the row's end have dy = 0 and count in no sum
+        Raw<TX, VEC> raw[NV];
+        float2 z[P], g[P], s0 = make_float2(0.f, 0.f), s1 = s0;
 #pragma unroll
         for (int i = 0; i < NV; ++i) {
-            if (col + i * TPR * VEC < N) {
-                Raw<TX, VEC> raw;
-                float f[VEC];
-                sx.read(stage, m, i, raw);
-                to_float(raw, z[i]);
-                sd.read(stage, m, i, raw);
-                to_float(raw, g[i]);
-                to_float(w[i], f);
+            if (col + i * TPR * VEC < N) sx.read(stage, m, i, raw[i]);
+            else clear(raw[i]);
+        }
+        to_pairs<TX, VEC, NV>(raw, z);
 #pragma unroll
-                for (int e = 0; e < VEC; ++e) {
-                    z[i][e] = (z[i][e] - mu) * r;
-                    dw[i][e] = fmaf(g[i][e], z[i][e], dw[i][e]);
-                    db[i][e] += g[i][e];
-                    g[i][e] *= f[e];
-                    s[0] += g[i][e];
-                    s[1] = fmaf(g[i][e], z[i][e], s[1]);
-                }
+        for (int i = 0; i < NV; ++i) {
+            if (col + i * TPR * VEC < N) sd.read(stage, m, i, raw[i]);
+            else clear(raw[i]);
+        }
+        to_pairs<TX, VEC, NV>(raw, g);
+        {
+            float2 f[P];
+            to_pairs<TW, VEC, NV>(w, f);
+            const float2 scale = both(r), shift = both(-mu * r);
+#pragma unroll
+            for (int k = 0; k < P; ++k) {
+                z[k] = fma2(z[k], scale, shift);
+                dw[k] = fma2(g[k], z[k], dw[k]);
+                db[k] = add2(db[k], g[k]);
+                g[k] = mul2(g[k], f[k]);
+                s0 = add2(s0, g[k]);
+                s1 = fma2(g[k], z[k], s1);
             }
         }
+        float s[2] = {s0.x + s0.y, s1.x + s1.y};
         row_sum<TPR, 2>(s, red[turn]);
         if (p.dx) {
-            const float c0 = s[0] * inv_n, c1 = s[1] * inv_n;
+            // r (g - c0 - z c1)
+            const float2 scale = both(r), c0 = both(-r * (s[0] * inv_n)), c1 = both(-r * (s[1] * inv_n));
             TX* const dx = static_cast<TX*>(p.dx) + m * p.lddx + col;
+#pragma unroll
+            for (int k = 0; k < P; ++k) g[k] = fma2(z[k], c1, fma2(g[k], scale, c0));
 #pragma unroll
             for (int i = 0; i < NV; ++i) {
                 if (col + i * TPR * VEC < N) {
-#pragma unroll
-                    for (int e = 0; e < VEC; ++e) g[i][e] = r * (g[i][e] - c0 - z[i][e] * c1);
-                    store_f<TX, VEC>(dx + i * TPR * VEC, g[i]);
+                    float f[VEC];
+                    group<VEC, P>(g, i, f);
+                    store_f<TX, VEC>(dx + i * TPR * VEC, f);
                 }
             }
         }
@@ -495,8 +575,11 @@ __global__ void __launch_bounds__(TPR == 32 ? 128 : TPR, blocks_per_sm(TPR, true
 #pragma unroll
         for (int i = 0; i < NV; ++i) {
             if (col + i * TPR * VEC < N) {
-                store_f<float, VEC>(out + i * TPR * VEC, dw[i]);
-                store_f<float, VEC>(out + p.N + i * TPR * VEC, db[i]);             // N is a multiple of VEC
+                float f[VEC];
+                group<VEC, P>(dw, i, f);
+                store_f<float, VEC>(out + i * TPR * VEC, f);
+                group<VEC, P>(db, i, f);
+                store_f<float, VEC>(out + p.N + i * TPR * VEC, f);                 // N is a multiple of VEC
             }
         }
     }
