@@ -11,7 +11,7 @@ LIB = os.path.join(HERE, "libatb.so")
 SOURCES = ["atb_status.cpp", "atb_model.cpp", "atb_quantize.cu", "atb_gemm_sm100.cu", "atb_gemm_pair_sm100.cu",
            "atb_gemm_cfg_sm100.cu", "atb_layer_norm.cu", "atb_bf16_mm_sm100.cu", "atb_gated_ffn.cu", "atb_linear_ce.cu",
            "atb_few_rows.cu"]
-HEADERS = ["atb_internal.h", "sm100_ptx.cuh", "atb_gemm_device.cuh", "bfp16_block.cuh", "atb_bf16_mm.h", "atb_few_rows.h", "glu.cuh", "dependent_launch.cuh"]
+HEADERS = ["atb_internal.h", "sm100_ptx.cuh", "atb_gemm_device.cuh", "bfp16_block.cuh", "atb_bf16_mm.h", "atb_few_rows.h", "glu.cuh", "dependent_launch.cuh", "f32x2.cuh"]
 
 
 def _nvcc() -> str:

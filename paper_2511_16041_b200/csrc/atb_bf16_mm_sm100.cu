@@ -111,14 +111,24 @@ __device__ __forceinline__ uint32_t pack_bf16(float lo, float hi) {
     return *reinterpret_cast<const uint32_t*>(&b2);
 }
 
+__device__ __forceinline__ float2 unpack_bf16(uint32_t w) { return make_float2(__uint_as_float(w << 16), __uint_as_float(w & 0xFFFF0000u)); }
+
+// h = act(g) u of two neighbours, packed.
+template <int ACT>
+__device__ __forceinline__ uint32_t glu_pair(float2 g, float2 u) {
+    float2 a, slope;
+    act_value_slope<ACT>(g, a, slope);
+    const float2 h = f32x2::mul2(a, u);
+    return pack_bf16(h.x, h.y);
+}
 // dg = dh u act'(g) and du = dh act(g) of two neighbours, g and u packed bf16.
 template <int ACT>
-__device__ __forceinline__ void glu_backward_pair(uint32_t gw, uint32_t uw, float dh0, float dh1, uint32_t& dg, uint32_t& du) {
-    float a0, s0, a1, s1;
-    act_value_slope<ACT>(__uint_as_float(gw << 16), a0, s0);
-    act_value_slope<ACT>(__uint_as_float(gw & 0xFFFF0000u), a1, s1);
-    dg = pack_bf16(dh0 * __uint_as_float(uw << 16) * s0, dh1 * __uint_as_float(uw & 0xFFFF0000u) * s1);
-    du = pack_bf16(dh0 * a0, dh1 * a1);
+__device__ __forceinline__ void glu_backward_pair(uint32_t g, uint32_t u, float2 dh, uint32_t& dg, uint32_t& du) {
+    float2 a, slope;
+    act_value_slope<ACT>(unpack_bf16(g), a, slope);
+    const float2 x = f32x2::mul2(f32x2::mul2(dh, unpack_bf16(u)), slope), y = f32x2::mul2(dh, a);
+    dg = pack_bf16(x.x, x.y);
+    du = pack_bf16(y.x, y.y);
 }
 
 // A warp's staging boxes of 32 rows x 64 bf16 or 32 fp32 (128-byte swizzle), used in turn; each leaves by a TMA store, or is
@@ -235,10 +245,8 @@ __device__ __forceinline__ void mm_epilogue(const MmMaps<C::JOBS>& tm, const MmP
                 tmem_ld_wait_for(u);
 #pragma unroll
                 for (int e = 0; e < 16; ++e) {
-                    float a0, a1, slope;
-                    act_value_slope<act.value>(__uint_as_float(g[2 * e]), a0, slope);
-                    act_value_slope<act.value>(__uint_as_float(g[2 * e + 1]), a1, slope);
-                    h[16 * part + e] = pack_bf16(a0 * __uint_as_float(u[2 * e]), a1 * __uint_as_float(u[2 * e + 1]));
+                    h[16 * part + e] = glu_pair<act.value>(make_float2(__uint_as_float(g[2 * e]), __uint_as_float(g[2 * e + 1])),
+                                                           make_float2(__uint_as_float(u[2 * e]), __uint_as_float(u[2 * e + 1])));
                     og[16 * part + e] = pack_bf16(__uint_as_float(g[2 * e]), __uint_as_float(g[2 * e + 1]));
                     ou[16 * part + e] = pack_bf16(__uint_as_float(u[2 * e]), __uint_as_float(u[2 * e + 1]));
                 }
@@ -269,8 +277,8 @@ __device__ __forceinline__ void mm_epilogue(const MmMaps<C::JOBS>& tm, const MmP
                     tmem_ld_wait_for(dh);
 #pragma unroll
                     for (int e = 0; e < 16; ++e)
-                        glu_backward_pair<act.value>(g[e], u[e], __uint_as_float(dh[2 * e]), __uint_as_float(dh[2 * e + 1]), og[16 * part + e],
-                                                     ou[16 * part + e]);
+                        glu_backward_pair<act.value>(g[e], u[e], make_float2(__uint_as_float(dh[2 * e]), __uint_as_float(dh[2 * e + 1])),
+                                                     og[16 * part + e], ou[16 * part + e]);
                 }
                 out.put_in_place(&tm.c[0], og, col0 + c, row0);
                 out.put_in_place(&tm.c[1], ou, col0 + c, row0);
@@ -603,12 +611,7 @@ __global__ void __launch_bounds__(256) bf16_mm_join_kernel(const __grid_constant
             sum(m, q.N + n, u);
             with_act(p.act, [&](auto act) {
 #pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    float a0, a1, slope;
-                    act_value_slope<act.value>(v[2 * e], a0, slope);
-                    act_value_slope<act.value>(v[2 * e + 1], a1, slope);
-                    o[e] = pack_bf16(a0 * u[2 * e], a1 * u[2 * e + 1]);
-                }
+                for (int e = 0; e < 4; ++e) o[e] = glu_pair<act.value>(make_float2(v[2 * e], v[2 * e + 1]), make_float2(u[2 * e], u[2 * e + 1]));
             });
             put(q.C[0], m * q.ldc[0] + n, o);
             if (q.C[1]) {
@@ -625,7 +628,7 @@ __global__ void __launch_bounds__(256) bf16_mm_join_kernel(const __grid_constant
             uint32_t o2[4];
             with_act(p.act, [&](auto act) {
 #pragma unroll
-                for (int e = 0; e < 4; ++e) glu_backward_pair<act.value>(gw[e], uw[e], v[2 * e], v[2 * e + 1], o[e], o2[e]);
+                for (int e = 0; e < 4; ++e) glu_backward_pair<act.value>(gw[e], uw[e], make_float2(v[2 * e], v[2 * e + 1]), o[e], o2[e]);
             });
             put(q.C[0], m * q.ldc[0] + n, o);
             put(q.C[1], m * q.ldc[1] + n, o2);

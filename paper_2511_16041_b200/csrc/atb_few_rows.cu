@@ -151,9 +151,9 @@ __global__ void __launch_bounds__(kThreads, resident(MT, NW)) few_rows_kernel(co
                 p.y[m * p.ldy + col0 + c] = __float2bfloat16_rn(v[0]);
             } else {
                 glu::with_act(p.act, [&](auto act) {
-                    float a, slope;
-                    glu::act_value_slope<act.value>(v[0], a, slope);
-                    p.y[m * p.ldy + col0 + c] = __float2bfloat16_rn(a * v[NW - 1]);
+                    float2 a, slope;
+                    glu::act_value_slope<act.value>(make_float2(v[0], v[0]), a, slope);
+                    p.y[m * p.ldy + col0 + c] = __float2bfloat16_rn(a.x * v[NW - 1]);
                 });
                 if (p.g) {
                     p.g[m * p.ldg + col0 + c] = __float2bfloat16_rn(v[0]);

@@ -21,6 +21,7 @@
 #include "atb_internal.h"
 #include "bfp16_block.cuh"
 #include "dependent_launch.cuh"
+#include "f32x2.cuh"
 
 namespace {
 
@@ -119,32 +120,7 @@ __device__ __forceinline__ void store_f(T* p, const float (&v)[VEC]) {
 // The backward kernel works on its elements in pairs by the two-wide FP32 instructions, which round each half like the scalar
 // ones: 3 to 10 % faster than scalar arithmetic.  (The forward kernel, with half the arithmetic per byte, was 5 to 15 %
 // slower in this form.)
-__device__ __forceinline__ uint64_t bits2(float2 v) {
-    uint64_t r;
-    asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(v.x), "f"(v.y));
-    return r;
-}
-__device__ __forceinline__ float2 pair_of(uint64_t b) {
-    float2 v;
-    asm("mov.b64 {%0, %1}, %2;" : "=f"(v.x), "=f"(v.y) : "l"(b));
-    return v;
-}
-__device__ __forceinline__ float2 add2(float2 a, float2 b) {
-    uint64_t r;
-    asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(bits2(a)), "l"(bits2(b)));
-    return pair_of(r);
-}
-__device__ __forceinline__ float2 mul2(float2 a, float2 b) {
-    uint64_t r;
-    asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(bits2(a)), "l"(bits2(b)));
-    return pair_of(r);
-}
-__device__ __forceinline__ float2 fma2(float2 a, float2 b, float2 c) {
-    uint64_t r;
-    asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(bits2(a)), "l"(bits2(b)), "l"(bits2(c)));
-    return pair_of(r);
-}
-__device__ __forceinline__ float2 both(float v) { return make_float2(v, v); }
+using namespace f32x2;
 
 // A thread's elements as pairs: NV groups of VEC, pairs of neighbours (VEC = 8) or of one element each of two groups (VEC = 1).
 template <class T, int VEC, int NV>

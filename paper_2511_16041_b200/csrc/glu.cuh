@@ -5,6 +5,7 @@
 #include <type_traits>
 
 #include "atb.h"
+#include "f32x2.cuh"
 
 namespace glu {
 
@@ -16,28 +17,48 @@ __device__ __forceinline__ float exp2_fast(float x) {
 }
 constexpr float kLog2e = 1.4426950408889634f;
 
-// act(g) and act'(g).  exp by the fast instruction (2 ulp and the argument's rounding): the results are rounded to
-// bf16, 2^-9.  Phi by formula 7.1.26 of Abramowitz and Stegun (erfc(x) = exp(-x^2) times a polynomial of degree 5 in
+__device__ __forceinline__ float rcp_fast(float x) {
+    float y;
+    asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+    return y;
+}
+
+// act(g) and act'(g) of two values.  The kernels that call this are short of issue slots where K is shallow, hence the two-wide
+// arithmetic and the fast instructions for exp and 1 / x (1 to 2 ulp and the argument's rounding; the results are rounded to
+// bf16, 2^-9).  Phi by formula 7.1.26 of Abramowitz and Stegun (erfc(x) = exp(-x^2) times a polynomial of degree 5 in
 // 1 / (1 + p x), error below 1.5e-7 for x >= 0; Phi(-g) = 1 - Phi(g)): its exponential is the one that the slope needs.
 template <int ACT>
-__device__ __forceinline__ void act_value_slope(float g, float& a, float& slope) {
+__device__ __forceinline__ void act_value_slope(float2 g, float2& a, float2& slope) {
+    using namespace f32x2;
+    const float2 one = both(1.f);
     if constexpr (ACT == ATB_ACT_SILU) {
-        const float s = __fdividef(1.f, 1.f + exp2_fast(-g * kLog2e));
-        a = g * s;
-        slope = s + a * (1.f - s);
+        const float2 x = mul2(g, both(-kLog2e));
+        const float2 d = add2(make_float2(exp2_fast(x.x), exp2_fast(x.y)), one);
+        const float2 s = make_float2(rcp_fast(d.x), rcp_fast(d.y));
+        a = mul2(g, s);
+        slope = fma2(a, fma2(s, both(-1.f), one), s);
     } else if constexpr (ACT == ATB_ACT_GELU) {
-        const float x = fabsf(g) * 0.70710678118654752f;
-        const float t = __fdividef(1.f, 1.f + 0.3275911f * x), e = exp2_fast(-0.5f * kLog2e * g * g);
-        const float poly = t * (0.254829592f + t * (-0.284496736f + t * (1.421413741f + t * (-1.453152027f + t * 1.061405429f))));
-        const float tail = 0.5f * poly * e, phi = g < 0.f ? tail : 1.f - tail;
-        a = g * phi;
-        slope = phi + g * e * 0.39894228040143268f;
+        const float2 d = fma2(make_float2(fabsf(g.x), fabsf(g.y)), both(0.3275911f * 0.70710678118654752f), one);
+        const float2 t = make_float2(rcp_fast(d.x), rcp_fast(d.y));
+        const float2 x = mul2(mul2(g, both(-0.5f * kLog2e)), g);
+        const float2 e = make_float2(exp2_fast(x.x), exp2_fast(x.y));
+        float2 poly = fma2(t, both(0.5f * 1.061405429f), both(0.5f * -1.453152027f));
+        poly = fma2(t, poly, both(0.5f * 1.421413741f));
+        poly = fma2(t, poly, both(0.5f * -0.284496736f));
+        poly = fma2(t, poly, both(0.5f * 0.254829592f));
+        const float2 tail = mul2(mul2(t, poly), e), rest = fma2(tail, both(-1.f), one);
+        const float2 phi = make_float2(g.x < 0.f ? tail.x : rest.x, g.y < 0.f ? tail.y : rest.y);
+        a = mul2(g, phi);
+        slope = fma2(mul2(g, both(0.39894228040143268f)), e, phi);
     } else {
-        // 0.5 (1 + tanh z) = 1 / (1 + exp(-2 z))
-        const float c = 0.79788456080286536f, q = fminf(g * g, 1e9f);     // s is 0 or 1 long before that
-        const float s = __fdividef(1.f, 1.f + exp2_fast(-2.f * kLog2e * c * g * (1.f + 0.044715f * q)));
-        a = g * s;
-        slope = s + 2.f * a * (1.f - s) * c * (1.f + 0.134145f * q);
+        // 0.5 (1 + tanh z) = 1 / (1 + exp(-2 z)), z = c g (1 + 0.044715 g^2): 0 or 1 long before g^2 = 1e9
+        constexpr float c = 0.79788456080286536f;
+        const float2 sq = mul2(g, g), q = make_float2(fminf(sq.x, 1e9f), fminf(sq.y, 1e9f));
+        const float2 x = mul2(fma2(q, both(-2.f * kLog2e * c * 0.044715f), both(-2.f * kLog2e * c)), g);
+        const float2 d = add2(make_float2(exp2_fast(x.x), exp2_fast(x.y)), one);
+        const float2 s = make_float2(rcp_fast(d.x), rcp_fast(d.y));
+        a = mul2(g, s);
+        slope = fma2(mul2(a, fma2(q, both(2.f * c * 0.134145f), both(2.f * c))), fma2(s, both(-1.f), one), s);
     }
 }
 // f<ACT>() for the runtime value, one branch for a whole tile.
