@@ -31,8 +31,9 @@ def is_stale(lib: str = LIB) -> bool:
 
 # Diagnostic variants of the library: never the product, each loaded only by the test that needs it.
 #   timeout_test: every bounded wait gives up after 2 ms and one dequantiser warp of CTA 0 keeps back its
-#                 first arrival, so that the timeout path (abort flag, drain, TMEM release, status) runs.
-VARIANTS = {"timeout_test": ["-DATB_TEST_WAIT_NS=2000000ull", "-DATB_TEST_WITHHOLD_DEQ_ARRIVAL"]}
+#                 first arrival, so that the timeout path (abort flag, drain, TMEM release, status) runs; in the BF16
+#                 product kernels one epilogue warp of CTA 0 does.
+VARIANTS = {"timeout_test": ["-DATB_TEST_WAIT_NS=2000000ull", "-DATB_TEST_WITHHOLD_DEQ_ARRIVAL", "-DATB_TEST_WITHHOLD_ACC_ARRIVAL"]}
 
 
 def variant_path(variant: str) -> str:

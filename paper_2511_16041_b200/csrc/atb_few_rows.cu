@@ -32,8 +32,9 @@ struct FewParams {
 };
 
 // CTAs per SM (launch bounds): what leaves every thread the registers for its loads in flight (32 per matrix) and its sums
-// (8 per row and matrix).
-constexpr int resident(int MT, int NW) { return NW == 2 ? 4 : MT == 1 ? 7 : 5; }
+// (8 per row and matrix).  Measured at 4096 x 10944, one row, block of both products: 6 for NW = 1: 46.4 us, 7: 50.4 us, 5: 46.9 us;
+// NW = 2 with 5 instead of 4: 51.2 us, with 3: 53.9 us.
+constexpr int resident(int MT, int NW) { return NW == 2 ? 4 : MT == 1 ? 6 : 5; }
 
 
 __device__ __forceinline__ float lo(uint32_t w) { return __uint_as_float(w << 16); }
