@@ -26,8 +26,11 @@
 namespace {
 
 constexpr int kElems = 16;           // most elements of a row per thread
-template <class T>
-constexpr int kAhead = sizeof(T) == 2 ? 3 : 2;      // rows on their way per block
+// Rows on their way per block: what the shared memory holds beside the row in hand.
+template <class T, int TPR = 0>
+constexpr int kAhead = sizeof(T) == 2 && TPR < 1024 ? 3 : 2;
+template <class T, int TPR>
+constexpr int kAheadFwd = sizeof(T) == 2 ? 3 : 2;
 
 // Blocks that stay on an SM: about 100 KB of rows on their way in each kernel.
 __host__ __device__ constexpr int blocks_per_sm(int tpr, bool backward) {
@@ -306,7 +309,7 @@ template <class TX, class TW, int VEC, int TPR, int NV, bool BFP>
 __global__ void __launch_bounds__(TPR == 32 ? 128 : TPR, blocks_per_sm(TPR, false)) layer_norm_kernel(const FwdParams p) {
     using Source = RowSource<TX, VEC, TPR, NV>;
     constexpr int WALKERS = TPR == 32 ? 4 : 1, W = TPR / 32;
-    constexpr int STAGES = kAhead<TX> + 1;
+    constexpr int STAGES = kAheadFwd<TX, TPR> + 1;
     extern __shared__ __align__(16) uint8_t ring[];
     __shared__ float2 red[2][W];
     const int t = TPR == 32 ? threadIdx.x & 31 : threadIdx.x, lane = threadIdx.x & 31, warp = TPR == 32 ? 0 : threadIdx.x >> 5;
@@ -324,7 +327,7 @@ __global__ void __launch_bounds__(TPR == 32 ? 128 : TPR, blocks_per_sm(TPR, fals
     sm100::grid_dependency_wait();
     sm100::grid_dependency_launch();
 #pragma unroll
-    for (int s = 0; s < kAhead<TX>; ++s) {
+    for (int s = 0; s < kAheadFwd<TX, TPR>; ++s) {
         if (first + s * step < p.M) src.fetch(s, first + s * step);
         async_commit();
     }
@@ -338,10 +341,10 @@ __global__ void __launch_bounds__(TPR == 32 ? 128 : TPR, blocks_per_sm(TPR, fals
     for (int64_t m = first; m < p.rows; m += step, turn ^= 1) {
         if constexpr (BFP) put_exp_padding(p, m, t, TPR);
         if (m < p.M) {                     // the same for all threads of the row
-            const int ahead = stage == 0 ? kAhead<TX> : stage - 1;       // the stage that the row before this one has left
-            if (m + kAhead<TX> * step < p.M) src.fetch(ahead, m + kAhead<TX> * step);
+            const int ahead = stage == 0 ? kAheadFwd<TX, TPR> : stage - 1;       // the stage that the row before this one has left
+            if (m + kAheadFwd<TX, TPR> * step < p.M) src.fetch(ahead, m + kAheadFwd<TX, TPR> * step);
             async_commit();
-            async_wait<kAhead<TX>>();
+            async_wait<kAheadFwd<TX, TPR>>();
             row_barrier<Source, VEC, TPR>();
             float v[NV][VEC], s[1] = {0.f};
 #pragma unroll
@@ -458,7 +461,9 @@ template <class TX, class TW, int VEC, int TPR, int NV>
 __global__ void __launch_bounds__(TPR == 32 ? 128 : TPR, blocks_per_sm(TPR, true)) layer_norm_backward_kernel(const BwdParams p) {
     using Source = RowSource<TX, VEC, TPR, NV>;
     constexpr int WALKERS = TPR == 32 ? 4 : 1, W = TPR / 32;
-    constexpr int STAGES = kAhead<TX> + 1, P = NV * VEC / 2;
+    constexpr int STAGES = kAhead<TX, TPR> + 1, P = NV * VEC / 2;
+    // 1024 threads have 64 registers each: with 16 elements the row is read from shared memory again after the sums
+    constexpr bool REREAD = TPR == 1024 && P == kElems / 2;
     extern __shared__ __align__(16) uint8_t ring[];
     __shared__ float red[2][W][2];
     const int t = TPR == 32 ? threadIdx.x & 31 : threadIdx.x;
@@ -469,7 +474,7 @@ __global__ void __launch_bounds__(TPR == 32 ? 128 : TPR, blocks_per_sm(TPR, true
     sm100::grid_dependency_wait();
     sm100::grid_dependency_launch();
 #pragma unroll
-    for (int s = 0; s < kAhead<TX>; ++s) {
+    for (int s = 0; s < kAhead<TX, TPR>; ++s) {
         if (first + s * step < p.M) {
             sx.fetch(s, first + s * step);
             sd.fetch(s, first + s * step);
@@ -486,38 +491,42 @@ __global__ void __launch_bounds__(TPR == 32 ? 128 : TPR, blocks_per_sm(TPR, true
     float mu = 0.f, r = 0.f;
     if (first < p.M) { mu = p.mean[first]; r = p.rstd[first]; }
     for (int64_t m = first; m < p.M; m += step, turn ^= 1) {
-        const int ahead = stage == 0 ? kAhead<TX> : stage - 1;           // the stage that the row before this one has left
-        if (m + kAhead<TX> * step < p.M) {
-            sx.fetch(ahead, m + kAhead<TX> * step);
-            sd.fetch(ahead, m + kAhead<TX> * step);
+        const int ahead = stage == 0 ? kAhead<TX, TPR> : stage - 1;           // the stage that the row before this one has left
+        if (m + kAhead<TX, TPR> * step < p.M) {
+            sx.fetch(ahead, m + kAhead<TX, TPR> * step);
+            sd.fetch(ahead, m + kAhead<TX, TPR> * step);
         }
         async_commit();
         float next_mu = 0.f, next_r = 0.f;
         if (m + step < p.M) { next_mu = p.mean[m + step]; next_r = p.rstd[m + step]; }
-        async_wait<kAhead<TX>>();
+        async_wait<kAhead<TX, TPR>>();
         row_barrier<Source, VEC, TPR>();
-        // elements past the row's end have dy = 0 and count in no sum
-        Raw<TX, VEC> raw[NV];
+        // z, dy and g = dy w of this thread; elements past the row's end have dy = 0 and count in no sum
         float2 z[P], g[P], s0 = make_float2(0.f, 0.f), s1 = s0;
+        const float2 scale = both(r), shift = both(-mu * r);
+        const auto load = [&] {
+            Raw<TX, VEC> raw[NV];
 #pragma unroll
-        for (int i = 0; i < NV; ++i) {
-            if (col + i * TPR * VEC < N) sx.read(stage, m, i, raw[i]);
-            else clear(raw[i]);
-        }
-        to_pairs<TX, VEC, NV>(raw, z);
+            for (int i = 0; i < NV; ++i) {
+                if (col + i * TPR * VEC < N) sx.read(stage, m, i, raw[i]);
+                else clear(raw[i]);
+            }
+            to_pairs<TX, VEC, NV>(raw, z);
 #pragma unroll
-        for (int i = 0; i < NV; ++i) {
-            if (col + i * TPR * VEC < N) sd.read(stage, m, i, raw[i]);
-            else clear(raw[i]);
-        }
-        to_pairs<TX, VEC, NV>(raw, g);
+            for (int k = 0; k < P; ++k) z[k] = fma2(z[k], scale, shift);
+#pragma unroll
+            for (int i = 0; i < NV; ++i) {
+                if (col + i * TPR * VEC < N) sd.read(stage, m, i, raw[i]);
+                else clear(raw[i]);
+            }
+            to_pairs<TX, VEC, NV>(raw, g);
+        };
+        load();
         {
             float2 f[P];
             to_pairs<TW, VEC, NV>(w, f);
-            const float2 scale = both(r), shift = both(-mu * r);
 #pragma unroll
             for (int k = 0; k < P; ++k) {
-                z[k] = fma2(z[k], scale, shift);
                 dw[k] = fma2(g[k], z[k], dw[k]);
                 db[k] = add2(db[k], g[k]);
                 g[k] = mul2(g[k], f[k]);
@@ -529,7 +538,14 @@ __global__ void __launch_bounds__(TPR == 32 ? 128 : TPR, blocks_per_sm(TPR, true
         row_sum<TPR, 2>(s, red[turn]);
         if (p.dx) {
             // r (g - c0 - z c1)
-            const float2 scale = both(r), c0 = both(-r * (s[0] * inv_n)), c1 = both(-r * (s[1] * inv_n));
+            const float2 c0 = both(-r * (s[0] * inv_n)), c1 = both(-r * (s[1] * inv_n));
+            if constexpr (REREAD) {
+                load();
+                float2 f[P];
+                to_pairs<TW, VEC, NV>(w, f);
+#pragma unroll
+                for (int k = 0; k < P; ++k) g[k] = mul2(g[k], f[k]);
+            }
             TX* const dx = static_cast<TX*>(p.dx) + m * p.lddx + col;
 #pragma unroll
             for (int k = 0; k < P; ++k) g[k] = fma2(z[k], c1, fma2(g[k], scale, c0));
@@ -542,6 +558,7 @@ __global__ void __launch_bounds__(TPR == 32 ? 128 : TPR, blocks_per_sm(TPR, true
                 }
             }
         }
+        if constexpr (REREAD && VEC == 1) __syncthreads();      // the row's stage is the next to be filled
         mu = next_mu;
         r = next_r;
         stage = stage + 1 == STAGES ? 0 : stage + 1;
@@ -637,7 +654,10 @@ int threads_per_row(int64_t N, int most) {
         if (t <= most && N <= static_cast<int64_t>(t) * kElems) return t;
     return 0;
 }
-constexpr int kFwdThreads = 1024, kBwdThreads = 512;      // the backward sums take 2 kElems registers
+constexpr int kMostThreads = 1024;
+// Backward, FP32: two rows of 16384 do not leave room for the next ones.
+template <class TX>
+constexpr int kBwdThreads = sizeof(TX) == 2 ? 1024 : 512;
 
 // A kernel whose rows on their way may take more, with its static arrays, than the 48 KB of shared memory that need no leave.
 template <class... Args>
@@ -655,12 +675,12 @@ cudaError_t launch_fwd_rows(const FwdParams& p, cudaStream_t st) {
     const int64_t walkers = TPR == 32 ? 4 : 1, all = (p.rows + walkers - 1) / walkers, most = static_cast<int64_t>(atb::kSmCount) * blocks_per_sm(TPR, false);
     const unsigned blocks = static_cast<unsigned>(all < most ? all : most);
     if (p.N <= static_cast<int64_t>(TPR) * kElems / 2)
-        return launch_ring(layer_norm_kernel<TX, TW, VEC, TPR, HALF, BFP>, blocks, THREADS, (kAhead<TX> + 1) * RowSource<TX, VEC, TPR, HALF>::STAGE_BYTES, st, p);
-    return launch_ring(layer_norm_kernel<TX, TW, VEC, TPR, NV, BFP>, blocks, THREADS, (kAhead<TX> + 1) * RowSource<TX, VEC, TPR, NV>::STAGE_BYTES, st, p);
+        return launch_ring(layer_norm_kernel<TX, TW, VEC, TPR, HALF, BFP>, blocks, THREADS, (kAheadFwd<TX, TPR> + 1) * RowSource<TX, VEC, TPR, HALF>::STAGE_BYTES, st, p);
+    return launch_ring(layer_norm_kernel<TX, TW, VEC, TPR, NV, BFP>, blocks, THREADS, (kAheadFwd<TX, TPR> + 1) * RowSource<TX, VEC, TPR, NV>::STAGE_BYTES, st, p);
 }
 template <class TX, class TW, int VEC, bool BFP>
 cudaError_t launch_fwd(const FwdParams& p, cudaStream_t st) {
-    switch (threads_per_row(p.N, kFwdThreads)) {
+    switch (threads_per_row(p.N, kMostThreads)) {
         case 32: return launch_fwd_rows<TX, TW, VEC, BFP, 32>(p, st);
         case 128: return launch_fwd_rows<TX, TW, VEC, BFP, 128>(p, st);
         case 256: return launch_fwd_rows<TX, TW, VEC, BFP, 256>(p, st);
@@ -674,7 +694,7 @@ cudaError_t launch_fwd(const FwdParams& p, cudaStream_t st) {
 // Blocks that walk the rows: one per SM and more while each walker still has 16 rows, since its sums of 8 N bytes go
 // through the workspace.  The same on every host: the workspace's size depends on it.
 int walking_blocks(int64_t M, int64_t N) {
-    const int tpr = threads_per_row(N, kBwdThreads);
+    const int tpr = threads_per_row(N, kMostThreads);
     const int64_t walkers = tpr == 32 ? 4 : 1, all = (M + walkers - 1) / walkers, most = static_cast<int64_t>(atb::kSmCount) * blocks_per_sm(tpr, true);
     int64_t blocks = (M + 16 * walkers - 1) / (16 * walkers);
     if (blocks < atb::kSmCount) blocks = atb::kSmCount;
@@ -683,7 +703,7 @@ int walking_blocks(int64_t M, int64_t N) {
     return static_cast<int>(blocks < 1 ? 1 : blocks);
 }
 int partial_sums(int64_t M, int64_t N) {
-    return walking_blocks(M, N) * (threads_per_row(N, kBwdThreads) == 32 ? 4 : 1);
+    return walking_blocks(M, N) * (threads_per_row(N, kMostThreads) == 32 ? 4 : 1);
 }
 
 template <class TX, class TW, int VEC, int TPR>
@@ -692,16 +712,18 @@ cudaError_t launch_bwd_rows(const BwdParams& p, cudaStream_t st) {
     const unsigned blocks = static_cast<unsigned>(walking_blocks(p.M, p.N));
     if (p.N <= static_cast<int64_t>(TPR) * kElems / 2)
         return launch_ring(layer_norm_backward_kernel<TX, TW, VEC, TPR, HALF>, blocks, THREADS,
-                           2 * (kAhead<TX> + 1) * RowSource<TX, VEC, TPR, HALF>::STAGE_BYTES, st, p);
-    return launch_ring(layer_norm_backward_kernel<TX, TW, VEC, TPR, NV>, blocks, THREADS, 2 * (kAhead<TX> + 1) * RowSource<TX, VEC, TPR, NV>::STAGE_BYTES, st, p);
+                           2 * (kAhead<TX, TPR> + 1) * RowSource<TX, VEC, TPR, HALF>::STAGE_BYTES, st, p);
+    return launch_ring(layer_norm_backward_kernel<TX, TW, VEC, TPR, NV>, blocks, THREADS, 2 * (kAhead<TX, TPR> + 1) * RowSource<TX, VEC, TPR, NV>::STAGE_BYTES, st, p);
 }
 template <class TX, class TW, int VEC>
 cudaError_t launch_bwd(const BwdParams& p, cudaStream_t st) {
-    switch (threads_per_row(p.N, kBwdThreads)) {
+    switch (threads_per_row(p.N, kBwdThreads<TX>)) {
         case 32: return launch_bwd_rows<TX, TW, VEC, 32>(p, st);
         case 128: return launch_bwd_rows<TX, TW, VEC, 128>(p, st);
         case 256: return launch_bwd_rows<TX, TW, VEC, 256>(p, st);
         case 512: return launch_bwd_rows<TX, TW, VEC, 512>(p, st);
+        case 1024:
+            if constexpr (kBwdThreads<TX> == 1024) return launch_bwd_rows<TX, TW, VEC, 1024>(p, st);
     }
     if (p.dx) layer_norm_backward_wide_kernel<TX, TW><<<static_cast<unsigned>(p.M), 1024, 0, st>>>(p);
     if (p.part)
