@@ -73,7 +73,9 @@ def _run_both(M, D, F, act, pad=0, seed=0):
 
 SHAPES = [(1, 8, 8), (1, 64, 64), (2, 72, 136), (3, 1024, 2736), (4, 264, 520), (7, 128, 4104), (8, 1000, 328), (9, 512, 1024), (16, 2048, 1024),
           (31, 64, 72), (64, 328, 264), (127, 128, 256), (128, 256, 128), (129, 136, 264), (256, 512, 1368), (257, 200, 520), (500, 1024, 2736),
-          (1000, 320, 4104)]
+          (1000, 320, 4104),
+          # several tiles for every CTA or pair, in every product: accumulators and rings wrap round
+          (20, 64, 40000), (128, 4104, 10008), (3000, 200, 4104), (2500, 2056, 520)]
 
 
 @pytest.mark.parametrize("M,D,F", SHAPES)

@@ -62,7 +62,9 @@ def _check_backward(x, w, labels, dloss, lse, dl, dX, dW, ignore=IGNORE):
 
 
 SHAPES = [(1, 1, 8), (1, 7, 64), (2, 130, 72), (3, 1000, 256), (16, 3200, 512), (33, 63, 136), (100, 129, 64), (128, 513, 200), (129, 257, 64),
-          (200, 5003, 128), (300, 2048, 1024), (600, 1025, 96)]
+          (200, 5003, 128), (300, 2048, 1024), (600, 1025, 96),
+          # several tiles for every CTA or pair
+          (20, 60011, 64), (100, 60011, 72), (900, 30011, 136)]
 
 
 @pytest.mark.parametrize("M,V,D", SHAPES)
@@ -76,6 +78,7 @@ def test_forward_and_backward(M, V, D):
         dX, dW = atb.atb_linear_cross_entropy_backward(dloss, x, w, labels, lse, workspace=ws)
         atb.atb_device_status()
         words = -(-V // 256) * 256                             # one piece: rows of whole tiles
+        assert atb.atb_linear_cross_entropy_backward_workspace_bytes(M, V, D, V) == need
         dl = ws[:2 * M * words].view(BF16).view(M, words)[:, :V]
         _check_backward(x, w, labels, dloss, lse, dl, dX, dW)
 
