@@ -9,7 +9,8 @@
 // UMMAs, eight warps run the epilogue.  The accumulator is held twice, so that a tile's epilogue runs beside the next
 // tile's K loop.
 //   pair    256 x 256 tile: each CTA loads its 128 rows of A and half of the columns of B and holds 128 x 256 of C
-//   single  128 x 128 tile: four times as many tiles for outputs that would leave most of the SMs idle
+//   single  128 x 128 tile: four times as many tiles for outputs that would leave most of the SMs idle; for the head of a few
+//           rows, which is bound by reading W, the tile's width is what deals the words out evenly (16 to 128)
 // Up to three products that do not depend on one another (the gradients of a layer's input and weights) share a launch:
 // their tiles are dealt out as one list, so that one product's last wave is filled by the next one's tiles.  A product
 // of few tiles is cut along K into ranges whose FP32 sums a second kernel joins.
@@ -52,8 +53,8 @@ struct MmJob {
 struct MmParams {
     MmJob job[kMmGroup];
     int n_jobs, items;
-    int stages;                            // of the operand ring, of a_bytes + kMmTileBytes each
-    uint32_t a_bytes;
+    int stages, tile_n;                    // stages of the operand ring, of a_bytes + b_bytes each
+    uint32_t a_bytes, b_bytes;
     unsigned int* error_flag;
     int act, save;
     const int64_t* labels;
@@ -62,6 +63,8 @@ struct MmParams {
     int64_t stats_ld;
     float* label_logit;
     const float *lse, *scale;
+    void* dl;                              // kMmDlogits, tiles of any width
+    int64_t dl_ld;
 };
 
 // Tensor maps: product j has A at a[2 j], a[2 j + 1] (K segments), B and C alike (segments).  The epilogues of a single product
@@ -100,7 +103,9 @@ struct MmCfg {
     static constexpr uint32_t STAGE_BYTES = 2 * kMmTileBytes;
     // Ring of operand stages: 5 or 6, more (single CTAs) where A is a few rows and a stage little more than its B tile
     static constexpr uint32_t BOX_OFF = (BOXES == 2 ? 5 : 6) * STAGE_BYTES;
-    static constexpr int MOST_STAGES = PAIR ? BOX_OFF / STAGE_BYTES : 10;
+    static constexpr int MOST_STAGES = PAIR ? BOX_OFF / STAGE_BYTES : 32;
+    // The tile's width is the launch's (MmParams::tile_n)
+    static constexpr bool ANY_WIDTH = !PAIR && (EPI == atb::kMmRowStats || EPI == atb::kMmDlogits);
     static constexpr uint32_t BAR_OFF = BOX_OFF + kMmEpiWarps * BOXES * kEpilogueBoxBytes;
     static constexpr uint32_t SMEM_BYTES = 1024 + BAR_OFF + 8 * (2 * MOST_STAGES + 4 + kMmEpiWarps) + 16;
     static_assert(SMEM_BYTES <= kSmemBudget, "shared memory");
@@ -152,6 +157,24 @@ struct BoxWriter {
         }
         next = next + 1 == BOXES ? 0 : next + 1;
     }
+    // By plain stores of 16-byte pieces, 8 lanes to a row: rows below M, pieces that start below column N.
+    __device__ __forceinline__ void put_pieces(__nv_bfloat16* C, int64_t ld, const uint32_t (&o)[32], int64_t col, int64_t row0, int64_t M, int64_t N) const {
+        __syncwarp();                      // the box's last contents have been read
+        write(0, o);
+        __syncwarp();
+        const int och = lane & 7, orow = lane >> 3;
+        const int64_t at = col + och * 8, rows_left = M - row0 - orow;
+        __nv_bfloat16* dst = C + (row0 + orow) * ld + at;
+        const uint32_t src = box(0) + orow * 128;
+        if (at >= N) return;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            uint4 v;
+            asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w)
+                         : "r"(src + i * 512 + ((static_cast<uint32_t>(och) ^ static_cast<uint32_t>((4 * i + orow) & 7)) << 4)) : "memory");
+            if (4 * i < rows_left) *reinterpret_cast<uint4*>(dst + 4 * i * ld) = v;
+        }
+    }
     // The other direction: 64 columns of two inputs into the two boxes, and what becomes of them out of the same boxes.
     __device__ __forceinline__ void fetch(const CUtensorMap* m0, const CUtensorMap* m1, int64_t col, int64_t row0) {
         if (lane == 0) {
@@ -199,14 +222,16 @@ private:
 
 // ------------------------------------------------------------------------------------------ epilogue of one warp
 // Rows row0 .. row0 + 31 (one per lane); t_addr: the warp's lanes of the tile's accumulator, column 0; half: which of
-// the tile's column groups this warp has; col0: first column of the tile in C.
+// the tile's column groups this warp has, of `cols` columns; col0: first column of the tile in C.
 template <class C, int EPI>
 __device__ __forceinline__ void mm_epilogue(const MmMaps<C::JOBS>& tm, const MmParams& p, const MmJob& jb, int c_map, BoxWriter<C::BOXES>& out,
-                                            uint32_t t_addr, int half, int64_t row0, int64_t col0, int split, int lane, const Ctx& cx) {
+                                            uint32_t t_addr, int half, int64_t row0, int64_t col0, int cols, int split, int lane, const Ctx& cx) {
     const int64_t row = row0 + lane;
     const bool row_in = row < jb.M, warp_in = row0 < jb.M;
+    const int64_t slot = C::ANY_WIDTH ? col0 / p.tile_n * (p.tile_n > C::COLS ? 2 : 1) + half : col0 / C::COLS + half;     // kMmRowStats
     col0 += half * C::COLS;
     t_addr += half * C::COLS;
+    (void)slot;
     if constexpr (EPI == kMmPlain) {
         if (!jb.fp32) {
 #pragma unroll 1
@@ -285,17 +310,17 @@ __device__ __forceinline__ void mm_epilogue(const MmMaps<C::JOBS>& tm, const MmP
             }
         });
     } else if constexpr (EPI == atb::kMmRowStats) {
-        // the label's column, counted from this warp's first one
+        // columns of this warp inside the vocabulary; the label's, counted from the first
+        const int mine = static_cast<int>(min(static_cast<int64_t>(cols), jb.N - col0));
         int64_t label = -1;
         if (row_in) label = p.labels[row] - p.col0 - col0;
         float m = -INFINITY, s = 0.f;
 #pragma unroll 1
-        for (int c = 0; c < C::COLS; c += 32) {
+        for (int c = 0; c < mine; c += 32) {
             uint32_t v[32];
             tmem_ld_32x32b_x32(t_addr + c, v);
             tmem_ld_wait_for(v);
-            const int64_t left = jb.N - (col0 + c);             // columns of this group inside the vocabulary
-            if (left <= 0) continue;
+            const int left = mine - c;
             const bool here = label >= c && label < c + 32 && label - c < left;
             if (__any_sync(0xFFFFFFFFu, here)) {
 #pragma unroll
@@ -317,7 +342,7 @@ __device__ __forceinline__ void mm_epilogue(const MmMaps<C::JOBS>& tm, const MmP
             for (int e = 0; e < 32; ++e) s += exp2_fast((__uint_as_float(v[e]) - ref) * kLog2e);
             m = top;
         }
-        if (row_in && col0 < jb.N) p.stats[row * p.stats_ld + col0 / C::COLS] = make_float2(m, s);
+        if (row_in && mine > 0) p.stats[row * p.stats_ld + slot] = make_float2(m, s);
     } else {
         int64_t label = -1;
         float lse = 0.f, scale = 0.f;
@@ -330,7 +355,7 @@ __device__ __forceinline__ void mm_epilogue(const MmMaps<C::JOBS>& tm, const MmP
             scale = p.scale[row];
         }
 #pragma unroll 1
-        for (int c = 0; c < C::COLS; c += 64) {
+        for (int c = 0; c < cols; c += 64) {
             uint32_t o[32];
 #pragma unroll
             for (int part = 0; part < 2; ++part) {
@@ -347,7 +372,10 @@ __device__ __forceinline__ void mm_epilogue(const MmMaps<C::JOBS>& tm, const MmP
 #pragma unroll
                 for (int e = 0; e < 16; ++e) o[16 * part + e] = pack_bf16(__uint_as_float(v[2 * e]), __uint_as_float(v[2 * e + 1]));
             }
-            out.put(&tm.c[0], o, col0 + c, row0, warp_in && col0 + c < jb.N);
+            // a tile of any width ends inside a box, which a TMA store would write beyond it; the words of dl's rows past the piece's
+            // end are room for whole 16-byte pieces
+            if constexpr (C::ANY_WIDTH) out.put_pieces(static_cast<__nv_bfloat16*>(p.dl), p.dl_ld, o, col0 + c, row0, jb.M, min(col0 + cols, jb.N));
+            else out.put(&tm.c[0], o, col0 + c, row0, warp_in && col0 + c < jb.N);
         }
     }
 }
@@ -433,7 +461,8 @@ bf16_mm_kernel(const __grid_constant__ MmMaps<MmCfg<PAIR, EPI>::JOBS> tm, const 
     tcgen05_fence_after_sync();
     const uint32_t tmem_base = misc_gen[0];
     const int stages = PAIR ? C::MOST_STAGES : p.stages;
-    const uint32_t a_bytes = PAIR ? kMmTileBytes : p.a_bytes, stage_bytes = a_bytes + kMmTileBytes;
+    const uint32_t a_bytes = PAIR ? kMmTileBytes : p.a_bytes, b_bytes = C::ANY_WIDTH ? p.b_bytes : kMmTileBytes, stage_bytes = a_bytes + b_bytes;
+    const int tile_n = C::ANY_WIDTH ? p.tile_n : C::TILE_N;
     // what a kernel before this one on the stream wrote may be read from here on
     grid_dependency_wait();
     grid_dependency_launch();
@@ -453,21 +482,22 @@ bf16_mm_kernel(const __grid_constant__ MmMaps<MmCfg<PAIR, EPI>::JOBS> tm, const 
                 const int m0 = w.mt * C::TILE_M + static_cast<int>(rank) * 128;
                 // where this CTA's two boxes of B start: halves of the gate's and the up projection's columns, or
                 // 128 consecutive columns
-                const int n0 = C::DUAL ? w.nt * C::TILE_N : w.nt * C::TILE_N + static_cast<int>(rank) * 128;
+                const int n0 = C::DUAL ? w.nt * C::TILE_N : w.nt * tile_n + static_cast<int>(rank) * 128;
                 const int n1 = (C::DUAL && !PAIR) ? n0 : n0 + 64;
                 for (int k0 = w.k_begin; k0 < w.k_end; ++k0) {
                     int k = serpentine_k(it, k0, w.k_begin, w.k_end);
                     const int kseg = k >= jb.k_steps0 ? 1 : 0;
                     k -= kseg * jb.k_steps0;
                     if (!(ok = wait_bar_t<true, PAIR>(cx, empty + 8 * r.stage, r.phase ^ 1u, 0x001))) break;
-                    if (rank == 0) mbar_arrive_expect_tx(full + 8 * r.stage, PAIR ? 2 * C::STAGE_BYTES : kMmTileBytes + jb.a_rows * 128u);
+                    if (rank == 0) mbar_arrive_expect_tx(full + 8 * r.stage, PAIR ? 2 * C::STAGE_BYTES : b_bytes + jb.a_rows * 128u);
                     const uint32_t bar = PAIR ? mapa_shared(full + 8 * r.stage, 0) : full + 8 * r.stage;
                     const uint32_t dst = smem_base + r.stage * stage_bytes;
                     const int b0 = C::DUAL ? (PAIR ? static_cast<int>(rank) : 0) : (w.seg | kseg);
                     const int b1 = C::DUAL ? (PAIR ? static_cast<int>(rank) : 1) : (w.seg | kseg);
                     if (PAIR || jb.a_rows == 128) mm_load<PAIR>(dst, ta + kseg, ta + kseg, a_mn, m0, m0 + 64, k * kMmKStep, bar);
                     else mm_tma<PAIR>(dst, ta + kseg, k * kMmKStep, m0, bar);       // the tile's other rows are whatever lies behind: no row of C that exists reads them
-                    mm_load<PAIR>(dst + a_bytes, tb + b0, tb + b1, b_mn, n0, n1, k * kMmKStep, bar);
+                    if constexpr (C::ANY_WIDTH) mm_tma<PAIR>(dst + a_bytes, tb + b0, k * kMmKStep, n0, bar);       // one box of tile_n rows of B^T
+                    else mm_load<PAIR>(dst + a_bytes, tb + b0, tb + b1, b_mn, n0, n1, k * kMmKStep, bar);
                     r.advance(stages);
                 }
             }
@@ -481,7 +511,7 @@ bf16_mm_kernel(const __grid_constant__ MmMaps<MmCfg<PAIR, EPI>::JOBS> tm, const 
             for (int item; ok && (item = mm_item_at<PAIR>(it)) < p.items; ++it) {
                 const MmItem w = mm_item<C::JOBS>(p, item);
                 const bool a_mn = p.job[w.job].a_mn, b_mn = p.job[w.job].b_mn;
-                const uint32_t idesc = umma_idesc_bf16_f32(PAIR ? 256 : 128, C::BN, a_mn, b_mn);
+                const uint32_t idesc = umma_idesc_bf16_f32(PAIR ? 256 : 128, C::ANY_WIDTH ? tile_n : C::BN, a_mn, b_mn);
                 const uint32_t a_step = mm_desc_step(a_mn), b_step = mm_desc_step(b_mn);
                 const int acc = it & 1, steps = w.k_end - w.k_begin;
                 const uint32_t acc_phase = static_cast<uint32_t>(it >> 1) & 1u;
@@ -516,15 +546,15 @@ bf16_mm_kernel(const __grid_constant__ MmMaps<MmCfg<PAIR, EPI>::JOBS> tm, const 
         for (int item; ok && (item = mm_item_at<PAIR>(it)) < p.items; ++it) {
             const MmItem w = mm_item<C::JOBS>(p, item);
             const MmJob& jb = p.job[w.job];
-            const int64_t row0 = static_cast<int64_t>(w.mt) * C::TILE_M + rank * 128 + q * 32, col0 = static_cast<int64_t>(w.nt) * C::TILE_N;
+            const int64_t row0 = static_cast<int64_t>(w.mt) * C::TILE_M + rank * 128 + q * 32, col0 = static_cast<int64_t>(w.nt) * tile_n;
             const int acc = it & 1;
             if constexpr (EPI == atb::kMmGluBackward)
                 if (row0 < jb.M && col0 + half * C::COLS < jb.N) out.fetch(&tm.c[2], &tm.c[3], col0 + half * C::COLS, row0);
             if (!(ok = wait_bar_t<false, PAIR>(cx, acc_full + 8 * acc, static_cast<uint32_t>(it >> 1) & 1u, 0x201))) break;
             tcgen05_fence_after_sync();
-            if (half * C::COLS < C::TILE_N)
+            if (half * C::COLS < tile_n)
                 mm_epilogue<C, EPI>(tm, p, jb, 2 * w.job + w.seg, out, tmem_base + (static_cast<uint32_t>(q * 32) << 16) + static_cast<uint32_t>(acc * C::BN),
-                                    half, row0, col0, w.split, lane, cx);
+                                    half, row0, col0, min(C::COLS, tile_n - half * C::COLS), w.split, lane, cx);
             tcgen05_fence_before_sync();
             __syncwarp();
 #ifdef ATB_TEST_WITHHOLD_ACC_ARRIVAL
@@ -649,6 +679,7 @@ bool few_rows(const atb::MmProblem& q) { return q.layout != atb::kMmTN && q.M <=
 // work items (longest items first).
 struct MmPlan {
     bool pair = false, split = false;
+    int width = 128;                       // columns of a tile of a single CTA (kMmRowStats, kMmDlogits)
     int splits[kMmGroup] = {1, 1, 1}, order[kMmGroup] = {0, 1, 2};
 };
 
@@ -737,6 +768,16 @@ MmPlan make_plan(const atb::MmProblem* q, int n) {
             if (t < least * 0.98) { least = t; best = c; }
         }
     }
+    if (!best.pair && !can_split(q->epilogue) && few) {
+        // A few rows' head reads W once, and an SM draws no more than its share of the memory's rate: the width (multiples of 16) that
+        // leaves the slowest SM the fewest columns, each tile counting 24 more.  V = 20731, D = 2160: 80 instead of 128 columns,
+        // two rounds each.
+        int64_t fewest = INT64_MAX;
+        for (int width = 128; width >= 16; width -= 16) {
+            const int64_t columns = atb::ceil_div(atb::ceil_div(q->N, width), atb::kSmCount) * (width + 24);
+            if (columns < fewest) { fewest = columns; best.width = width; }
+        }
+    }
     return best;
 }
 
@@ -775,14 +816,14 @@ atb_status_t launch(const atb::MmProblem* q, int n, const MmPlan& plan, char* pa
             if (s >= x.k_segs) tm.a[2 * i + s] = tm.a[2 * i];
             else if (!operand_map(&tm.a[2 * i + s], x.A[s], a_mn, x.M, x.K, a_box)) return atb::fail(ATB_ERR_CUDA, "cuTensorMapEncodeTiled failed for A");
             if (s >= n_b) tm.b[2 * i + s] = tm.b[2 * i];
-            else if (!operand_map(&tm.b[2 * i + s], x.B[s], b_mn, x.N, x.K)) return atb::fail(ATB_ERR_CUDA, "cuTensorMapEncodeTiled failed for B");
+            else if (!operand_map(&tm.b[2 * i + s], x.B[s], b_mn, x.N, x.K, C::ANY_WIDTH ? plan.width : 64)) return atb::fail(ATB_ERR_CUDA, "cuTensorMapEncodeTiled failed for B");
         }
         MmJob& jb = p.job[i];
         jb.M = x.M; jb.N = x.N;
         jb.a_mn = a_mn; jb.b_mn = b_mn;
         jb.a_rows = few ? a_box : 128;
         jb.m_tiles = static_cast<int>(atb::ceil_div(x.M, C::TILE_M));
-        jb.n_tiles = static_cast<int>(atb::ceil_div(x.N, C::TILE_N));
+        jb.n_tiles = static_cast<int>(atb::ceil_div(x.N, C::ANY_WIDTH ? plan.width : C::TILE_N));
         jb.n_segs = n_segs;
         jb.k_steps0 = static_cast<int>(atb::ceil_div(x.K, kMmKStep));
         jb.k_steps = jb.k_steps0 * x.k_segs;
@@ -816,7 +857,10 @@ atb_status_t launch(const atb::MmProblem* q, int n, const MmPlan& plan, char* pa
     int a_rows = 0;
     for (int i = 0; i < n; ++i) a_rows = std::max(a_rows, p.job[i].a_rows);
     p.a_bytes = static_cast<uint32_t>(a_rows) * 128u;          // a_rows is a multiple of 8: whole swizzle atoms of 1 KB
-    p.stages = std::min<int>(C::MOST_STAGES, C::BOX_OFF / (p.a_bytes + kMmTileBytes));
+    p.tile_n = C::ANY_WIDTH ? plan.width : C::TILE_N;
+    p.b_bytes = C::ANY_WIDTH ? static_cast<uint32_t>(plan.width) * 128u : kMmTileBytes;
+    p.stages = std::min<int>(C::MOST_STAGES, C::BOX_OFF / (p.a_bytes + p.b_bytes));
+    p.dl = q->C[0]; p.dl_ld = q->ldc[0];
     p.n_jobs = n;
     p.items = static_cast<int>(items);
     p.error_flag = dev.flag;
@@ -928,7 +972,11 @@ unsigned int take_mm_error_flag() {
 
 int64_t mm_stats_per_row(int64_t M, int64_t N, int64_t K) {
     const MmProblem q = mm_sizes(kMmNT, kMmRowStats, M, N, K);
-    return ceil_div(N, make_plan(&q, 1).pair ? 128 : 64);
+    const MmPlan plan = make_plan(&q, 1);
+    // two groups of columns per tile, or one of at most 64; the last tile may end in its first
+    const int tile = plan.pair ? 256 : plan.width, group = plan.pair ? 128 : 64, groups = tile > group ? 2 : 1;
+    const int64_t whole = (N - 1) / tile, rest = N - whole * tile;
+    return whole * groups + (rest > group ? 2 : 1);
 }
 
 size_t mm_partial_bytes(const MmProblem* q, int n) {
