@@ -15,6 +15,10 @@
 // where |mu| >> sqrt(v).  All sums are FP32.  Rows wider than the widest kernel are read again for every sum (*_wide kernels).
 // Blocks write their sums of dw and db to the workspace, a second kernel adds those up in a fixed order: no atomics,
 // the same bits on every call.
+// Measured (compulsory bytes, of a measured copy rate of 6.55 TB/s): 16384 x 8192 bf16, FP32 weights: forward 97 us, 5.5 TB/s,
+// backward 139 us, 5.8 TB/s; 8192 x 8192 FP32: 97 and 132 us, 5.5 and 6.1 TB/s; 8192 x 4096 bf16: 28 and 41 us, 4.8 TB/s;
+// 20000 x 1001, off 16-byte boundaries: FP32 31 and 50 us, 5.1 and 4.8 TB/s, bf16 29 and 42 us, 2.7 and 2.9 TB/s (bound by
+// instructions: an element at a time).  With one block per row and nothing on its way the first of these took 117 and 268 us.
 #include <cuda_bf16.h>
 #include <cuda_runtime.h>
 

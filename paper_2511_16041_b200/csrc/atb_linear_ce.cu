@@ -7,6 +7,10 @@
 // Backward: the logits are computed again, a piece of the vocabulary at a time; the epilogue turns them into dl, which
 // the workspace holds for one piece (bf16: it is the operand of the next two products).  dW of the piece is complete;
 // dx is added up over the pieces in FP32, in their order, and rounded once.
+// Tensor bound from a few hundred rows on: M = 8192, V = 131072, D = 4096 takes 26 ms for loss and gradients, 8 M V D operations
+// at 1.35 PFLOP/s, which is what the library product sustains under the power cap (1.38); M = 4096, V = 131072, D = 2048, loss
+// alone, 1.6 ms, 1.36 PFLOP/s.  Computing the logits again costs a quarter of that; keeping them would take M x V numbers.
+// A few rows are bound by reading W: 16 rows, V = 32000, D = 2048 28 us, 4.6 TB/s with both launches.
 #include <cuda_bf16.h>
 
 #include <algorithm>
