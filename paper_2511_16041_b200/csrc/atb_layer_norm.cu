@@ -15,9 +15,9 @@
 // where |mu| >> sqrt(v).  All sums are FP32.  Rows wider than the widest kernel are read again for every sum (*_wide kernels).
 // Blocks write their sums of dw and db to the workspace, a second kernel adds those up in a fixed order: no atomics,
 // the same bits on every call.
-// Measured (compulsory bytes, of a measured copy rate of 6.55 TB/s): 16384 x 8192 bf16, FP32 weights: forward 97 us, 5.5 TB/s,
+// Measured (compulsory bytes, of a measured copy rate of 6.55 TB/s): 16384 x 8192 bf16, FP32 weights: forward 94 us, 5.7 TB/s,
 // backward 139 us, 5.8 TB/s; 8192 x 8192 FP32: 97 and 132 us, 5.5 and 6.1 TB/s; 8192 x 4096 bf16: 28 and 41 us, 4.8 TB/s;
-// 20000 x 1001, off 16-byte boundaries: FP32 31 and 50 us, 5.1 and 4.8 TB/s, bf16 29 and 42 us, 2.7 and 2.9 TB/s (bound by
+// 12265 x 2494 off 16-byte boundaries: FP32 46 and 70 us, 5.4 and 5.2 TB/s, bf16 43 and 57 us, 2.9 and 3.2 TB/s (bound by
 // instructions: an element at a time).  With one block per row and nothing on its way the first of these took 117 and 268 us.
 #include <cuda_bf16.h>
 #include <cuda_runtime.h>
@@ -31,15 +31,25 @@ namespace {
 
 constexpr int kElems = 16;           // most elements of a row per thread
 // Rows on their way per block: what the shared memory holds beside the row in hand.
-template <class T, int TPR = 0>
-constexpr int kAhead = sizeof(T) == 2 && TPR < 1024 ? 3 : 2;
+template <class T, int TPR>
+constexpr int kAhead = sizeof(T) == 2 ? (TPR < 1024 ? 3 : 2) : (TPR < 768 ? 2 : 1);
 template <class T, int TPR>
 constexpr int kAheadFwd = sizeof(T) == 2 ? 3 : 2;
 
 // Blocks that stay on an SM: about 100 KB of rows on their way in each kernel.
-__host__ __device__ constexpr int blocks_per_sm(int tpr, bool backward) {
-    const int b = tpr == 32 ? 6 : tpr == 128 ? 8 : tpr == 256 ? 4 : tpr == 512 ? 2 : 1;
-    return backward ? (b + 1) / 2 : b;
+// vec: rows on 16-byte boundaries; an element at a time takes 80 registers (forward) instead of 64.
+__host__ __device__ constexpr int blocks_per_sm(int tpr, bool backward, bool vec) {
+    switch (tpr) {
+        case 32: return backward ? 3 : 6;              // four rows of 32 threads
+        case 64: return backward ? 8 : 12;
+        case 96: return backward ? 5 : vec ? 10 : 8;
+        case 128: return backward ? 4 : vec ? 8 : 6;
+        case 192: return backward ? 2 : vec ? 5 : 4;
+        case 256: return backward ? 2 : vec ? 4 : 3;
+        case 384: return backward ? 1 : 2;
+        case 512: return backward || !vec ? 1 : 2;
+        default: return 1;
+    }
 }
 
 // ---------------------------------------------------------------------------------- loads and stores
@@ -192,7 +202,7 @@ __device__ __forceinline__ void row_sum(float (&v)[K], float (*red)[K]) {
         for (int k = 0; k < K; ++k) {
             v[k] = lane < W ? red[lane][k] : 0.f;
 #pragma unroll
-            for (int o = W / 2; o > 0; o >>= 1) v[k] += __shfl_xor_sync(0xFFFFFFFFu, v[k], o);
+            for (int o = W > 16 ? 16 : W > 8 ? 8 : W > 4 ? 4 : W > 2 ? 2 : 1; o > 0; o >>= 1) v[k] += __shfl_xor_sync(0xFFFFFFFFu, v[k], o);
             v[k] = __shfl_sync(0xFFFFFFFFu, v[k], 0);
         }
     }
@@ -310,7 +320,7 @@ __device__ __forceinline__ void put_exp_padding(const FwdParams& p, int64_t m, i
     for (int64_t j = first + t; j < last; j += threads) p.exp[((j >> 3) * p.rows + m) * 8 + (j & 7)] = 0;
 }
 template <class TX, class TW, int VEC, int TPR, int NV, bool BFP>
-__global__ void __launch_bounds__(TPR == 32 ? 128 : TPR, blocks_per_sm(TPR, false)) layer_norm_kernel(const FwdParams p) {
+__global__ void __launch_bounds__(TPR == 32 ? 128 : TPR, blocks_per_sm(TPR, false, VEC > 1)) layer_norm_kernel(const FwdParams p) {
     using Source = RowSource<TX, VEC, TPR, NV>;
     constexpr int WALKERS = TPR == 32 ? 4 : 1, W = TPR / 32;
     constexpr int STAGES = kAheadFwd<TX, TPR> + 1;
@@ -462,12 +472,12 @@ struct BwdParams {
 };
 
 template <class TX, class TW, int VEC, int TPR, int NV>
-__global__ void __launch_bounds__(TPR == 32 ? 128 : TPR, blocks_per_sm(TPR, true)) layer_norm_backward_kernel(const BwdParams p) {
+__global__ void __launch_bounds__(TPR == 32 ? 128 : TPR, blocks_per_sm(TPR, true, VEC > 1)) layer_norm_backward_kernel(const BwdParams p) {
     using Source = RowSource<TX, VEC, TPR, NV>;
     constexpr int WALKERS = TPR == 32 ? 4 : 1, W = TPR / 32;
     constexpr int STAGES = kAhead<TX, TPR> + 1, P = NV * VEC / 2;
-    // 1024 threads have 64 registers each: with 16 elements the row is read from shared memory again after the sums
-    constexpr bool REREAD = TPR == 1024 && P == kElems / 2;
+    // 768 and 1024 threads have 80 and 64 registers each: the row is read from shared memory again after the sums
+    constexpr bool REREAD = TPR >= 768;
     extern __shared__ __align__(16) uint8_t ring[];
     __shared__ float red[2][W][2];
     const int t = TPR == 32 ? threadIdx.x & 31 : threadIdx.x;
@@ -652,16 +662,18 @@ __global__ void __launch_bounds__(32 * kSumWarps) layer_norm_backward_sum_kernel
 }
 
 // ---------------------------------------------------------------------------------- host
-// Threads per row: the fewest of 32, 128, 256, 512, 1024 (at most `most`) that hold a row of N elements; 0: a wide kernel.
+// Threads per row: the fewest (at most `most`) that hold a row of N elements, so that a thread has 11 to 16; 0: a wide kernel.
+// 8192 rows of 6000 bf16 elements take 37.7 us forward with 384 threads, 44.5 us with 512; 65536 rows of 1024 45 us with 64, 57 us
+// with 128 threads of 8 elements.
 int threads_per_row(int64_t N, int most) {
-    for (int t : {32, 128, 256, 512, 1024})
+    for (int t : {32, 64, 96, 128, 192, 256, 384, 512, 768, 1024})
         if (t <= most && N <= static_cast<int64_t>(t) * kElems) return t;
     return 0;
 }
 constexpr int kMostThreads = 1024;
 // Backward, FP32: two rows of 16384 do not leave room for the next ones.
 template <class TX>
-constexpr int kBwdThreads = sizeof(TX) == 2 ? 1024 : 512;
+constexpr int kBwdThreads = sizeof(TX) == 2 ? 1024 : 768;
 
 // A kernel whose rows on their way may take more, with its static arrays, than the 48 KB of shared memory that need no leave.
 template <class... Args>
@@ -675,20 +687,26 @@ cudaError_t launch_ring(void (*kernel)(Args...), unsigned grid, unsigned block, 
 
 template <class TX, class TW, int VEC, bool BFP, int TPR>
 cudaError_t launch_fwd_rows(const FwdParams& p, cudaStream_t st) {
-    constexpr int NV = kElems / VEC, HALF = NV > 1 ? NV / 2 : 1, THREADS = TPR == 32 ? 128 : TPR;
-    const int64_t walkers = TPR == 32 ? 4 : 1, all = (p.rows + walkers - 1) / walkers, most = static_cast<int64_t>(atb::kSmCount) * blocks_per_sm(TPR, false);
+    constexpr int NV = kElems / VEC, HALF = NV / 2, THREADS = TPR == 32 ? 128 : TPR;
+    const int64_t walkers = TPR == 32 ? 4 : 1, all = (p.rows + walkers - 1) / walkers, most = static_cast<int64_t>(atb::kSmCount) * blocks_per_sm(TPR, false, VEC > 1);
     const unsigned blocks = static_cast<unsigned>(all < most ? all : most);
-    if (p.N <= static_cast<int64_t>(TPR) * kElems / 2)
-        return launch_ring(layer_norm_kernel<TX, TW, VEC, TPR, HALF, BFP>, blocks, THREADS, (kAheadFwd<TX, TPR> + 1) * RowSource<TX, VEC, TPR, HALF>::STAGE_BYTES, st, p);
+    if constexpr (TPR == 32)               // the narrowest rows
+        if (p.N <= TPR * kElems / 2)
+            return launch_ring(layer_norm_kernel<TX, TW, VEC, TPR, HALF, BFP>, blocks, THREADS, (kAheadFwd<TX, TPR> + 1) * RowSource<TX, VEC, TPR, HALF>::STAGE_BYTES, st, p);
     return launch_ring(layer_norm_kernel<TX, TW, VEC, TPR, NV, BFP>, blocks, THREADS, (kAheadFwd<TX, TPR> + 1) * RowSource<TX, VEC, TPR, NV>::STAGE_BYTES, st, p);
 }
 template <class TX, class TW, int VEC, bool BFP>
 cudaError_t launch_fwd(const FwdParams& p, cudaStream_t st) {
     switch (threads_per_row(p.N, kMostThreads)) {
         case 32: return launch_fwd_rows<TX, TW, VEC, BFP, 32>(p, st);
+        case 64: return launch_fwd_rows<TX, TW, VEC, BFP, 64>(p, st);
+        case 96: return launch_fwd_rows<TX, TW, VEC, BFP, 96>(p, st);
         case 128: return launch_fwd_rows<TX, TW, VEC, BFP, 128>(p, st);
+        case 192: return launch_fwd_rows<TX, TW, VEC, BFP, 192>(p, st);
         case 256: return launch_fwd_rows<TX, TW, VEC, BFP, 256>(p, st);
+        case 384: return launch_fwd_rows<TX, TW, VEC, BFP, 384>(p, st);
         case 512: return launch_fwd_rows<TX, TW, VEC, BFP, 512>(p, st);
+        case 768: return launch_fwd_rows<TX, TW, VEC, BFP, 768>(p, st);
         case 1024: return launch_fwd_rows<TX, TW, VEC, BFP, 1024>(p, st);
     }
     layer_norm_wide_kernel<TX, TW, VEC, BFP><<<static_cast<unsigned>(p.rows), 1024, 0, st>>>(p);
@@ -699,7 +717,7 @@ cudaError_t launch_fwd(const FwdParams& p, cudaStream_t st) {
 // through the workspace.  The same on every host: the workspace's size depends on it.
 int walking_blocks(int64_t M, int64_t N) {
     const int tpr = threads_per_row(N, kMostThreads);
-    const int64_t walkers = tpr == 32 ? 4 : 1, all = (M + walkers - 1) / walkers, most = static_cast<int64_t>(atb::kSmCount) * blocks_per_sm(tpr, true);
+    const int64_t walkers = tpr == 32 ? 4 : 1, all = (M + walkers - 1) / walkers, most = static_cast<int64_t>(atb::kSmCount) * blocks_per_sm(tpr, true, true);
     int64_t blocks = (M + 16 * walkers - 1) / (16 * walkers);
     if (blocks < atb::kSmCount) blocks = atb::kSmCount;
     if (blocks > most) blocks = most;
@@ -712,10 +730,11 @@ int partial_sums(int64_t M, int64_t N) {
 
 template <class TX, class TW, int VEC, int TPR>
 cudaError_t launch_bwd_rows(const BwdParams& p, cudaStream_t st) {
-    constexpr int NV = kElems / VEC, HALF = NV > 1 ? NV / 2 : 1, THREADS = TPR == 32 ? 128 : TPR;
+    constexpr int NV = kElems / VEC, HALF = NV / 2, THREADS = TPR == 32 ? 128 : TPR;
     const unsigned blocks = static_cast<unsigned>(walking_blocks(p.M, p.N));
-    if (p.N <= static_cast<int64_t>(TPR) * kElems / 2)
-        return launch_ring(layer_norm_backward_kernel<TX, TW, VEC, TPR, HALF>, blocks, THREADS,
+    if constexpr (TPR == 32)               // the narrowest rows
+        if (p.N <= TPR * kElems / 2)
+            return launch_ring(layer_norm_backward_kernel<TX, TW, VEC, TPR, HALF>, blocks, THREADS,
                            2 * (kAhead<TX, TPR> + 1) * RowSource<TX, VEC, TPR, HALF>::STAGE_BYTES, st, p);
     return launch_ring(layer_norm_backward_kernel<TX, TW, VEC, TPR, NV>, blocks, THREADS, 2 * (kAhead<TX, TPR> + 1) * RowSource<TX, VEC, TPR, NV>::STAGE_BYTES, st, p);
 }
@@ -723,9 +742,14 @@ template <class TX, class TW, int VEC>
 cudaError_t launch_bwd(const BwdParams& p, cudaStream_t st) {
     switch (threads_per_row(p.N, kBwdThreads<TX>)) {
         case 32: return launch_bwd_rows<TX, TW, VEC, 32>(p, st);
+        case 64: return launch_bwd_rows<TX, TW, VEC, 64>(p, st);
+        case 96: return launch_bwd_rows<TX, TW, VEC, 96>(p, st);
         case 128: return launch_bwd_rows<TX, TW, VEC, 128>(p, st);
+        case 192: return launch_bwd_rows<TX, TW, VEC, 192>(p, st);
         case 256: return launch_bwd_rows<TX, TW, VEC, 256>(p, st);
+        case 384: return launch_bwd_rows<TX, TW, VEC, 384>(p, st);
         case 512: return launch_bwd_rows<TX, TW, VEC, 512>(p, st);
+        case 768: return launch_bwd_rows<TX, TW, VEC, 768>(p, st);
         case 1024:
             if constexpr (kBwdThreads<TX> == 1024) return launch_bwd_rows<TX, TW, VEC, 1024>(p, st);
     }

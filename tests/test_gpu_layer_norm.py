@@ -35,7 +35,8 @@ def _forward_bound(x, y, z, rstd, w, b, out_dtype):
 SHAPES = [(1, 8), (1, 1), (3, 5), (2, 64), (5, 512), (7, 513), (4, 520), (33, 1000), (2, 1001), (9, 4096), (3, 4104), (2, 8192), (2, 8200),
           (3, 16384), (2, 16385), (2, 32768), (2, 40000), (1, 32776), (700, 72)]
 # rows enough for every kernel's blocks to walk several of them
-SHAPES += [(6000, 257), (3000, 520), (2500, 1001), (1500, 2048), (1400, 4095), (700, 8192), (500, 9001), (460, 16384)]
+SHAPES += [(6000, 257), (3000, 520), (2500, 1001), (1500, 2048), (1400, 4095), (700, 8192), (500, 9001), (460, 16384),
+           (4000, 1024), (3000, 1032), (2200, 1537), (900, 2500), (700, 3080), (500, 6144), (480, 6150), (320, 12288), (310, 12301)]
 
 
 @pytest.mark.parametrize("dtype,wdtype", [(F32, F32), (F32, BF16), (BF16, F32), (BF16, BF16)])
