@@ -418,8 +418,9 @@ size_t atb_linear_cross_entropy_workspace_bytes(int64_t M, int64_t V, int64_t D)
 atb_status_t atb_linear_cross_entropy(int64_t M, int64_t V, int64_t D, const void* X_dev, int64_t ldx, const void* W_dev, int64_t ldw,
                                       const int64_t* labels_dev, int64_t ignore_index, float* loss_dev, float* lse_dev,
                                       void* workspace_dev, size_t workspace_bytes, void* stream);
-/* Gradients of sum_m dloss[m] * loss[m]:  dL = (exp(L - lse) - onehot(label)) * dloss (bf16; 0 in ignored rows),
- *   dX = dL W, dW = dL^T X (bf16, written; each may be NULL).  M == 0 writes dW = 0.
+/* Gradients of sum_m dloss[m] * loss[m]:  dL = (exp(L - lse) - onehot(label)) * dloss / unit (bf16; 0 in ignored rows),
+ *   dX = unit * dL W, dW = unit * dL^T X (bf16, written; each may be NULL), where unit is the largest finite |dloss| of the
+ *   rows that count, so that equal dloss (a mean) are not rounded.  M == 0 writes dW = 0.
  *   L is computed again, `piece` words of the vocabulary at a time (rounded up to whole tiles; 0: the library's choice,
  *   which keeps dL within 512 MB or 2048 words), so that the workspace holds M x piece of dL, FP32 sums of dX
  *   where there is more than one piece, and FP32 sums of products that are split along K to fill the SMs.  Results of different `piece` agree within the rounding of the FP32 sums. */

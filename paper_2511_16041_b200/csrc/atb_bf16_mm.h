@@ -25,7 +25,7 @@ enum MmEpilogue {
     kMmGlu = 2,                  // h = act(g) u from two products that share A; g and u too where wanted
     kMmGluBackward = 3,          // the product is dh; with the saved g and u: dg, du
     kMmRowStats = 4,             // per row and group of columns: maximum and sum of exp(c - maximum); the label's c
-    kMmDlogits = 5,              // (exp(c - lse) - [column is the label]) * scale (bf16)
+    kMmDlogits = 5,              // (exp(c - lse) - [column is the label]) * scale / unit (bf16)
 };
 
 struct MmProblem {
@@ -39,7 +39,8 @@ struct MmProblem {
     int64_t ldc[3] = {0, 0, 0};
     // kMmAccumulate
     float* C32 = nullptr;             // [M][N]
-    bool first = true;
+    bool first = true;                // kMmDlogits: finds *unit and writes it; else reads it
+    const float* factor = nullptr;    // kMmStore, kMmAccumulate: the product is multiplied by *factor where given
     // kMmGlu, kMmGluBackward
     int act = 0;
     const void *G = nullptr, *U = nullptr;      // [M][N] bf16
@@ -50,6 +51,7 @@ struct MmProblem {
     int64_t stats_ld = 0;
     float* label_logit = nullptr;     // [M]
     const float *lse = nullptr, *scale = nullptr;
+    float* unit = nullptr;            // kMmDlogits: largest finite |scale| of the rows that count, 1 where that is 0
 };
 
 // The sizes alone, for the plans below.

@@ -56,6 +56,7 @@ struct MmJob {
     int first_item;                    // of this product in the launch's list of (range, tile)
     int fp32, add;                     // C in FP32 (the sums of a range, rows split * split_rows on; or C32), added to it
     int64_t split_rows;
+    const float* factor;               // of C, or NULL
 };
 
 struct MmParams {
@@ -71,6 +72,9 @@ struct MmParams {
     int64_t stats_ld;
     float* label_logit;
     const float *lse, *scale;
+    float* unit;
+    int64_t rows;                          // kMmDlogits: of the product
+    bool first;
     void* dl;                              // kMmDlogits, tiles of any width
     int64_t dl_ld;
 };
@@ -85,7 +89,7 @@ struct MmMaps {
 struct MmJoinJob {
     int64_t M, N, cols, split_rows, first;       // first: of this product in the list of groups of eight columns
     int n_segs, splits, add;
-    const float* src;
+    const float *src, *factor;
     void* C[3];
     int64_t ldc[3];
     float* C32;
@@ -228,12 +232,41 @@ private:
     }
 };
 
+// The unit that dl is held in.  Rounded to bf16 as it is, a scale of 1 / 255 (a mean over 255 rows) would put the same 0.4 % on every
+// row's label, and so on dx and dW; in units of the largest scale, equal scales are exactly 1, and the products behind dl
+// multiply by the unit in FP32.  Every CTA finds it for itself while its first tile is on its way (M = 8192: 32 rows per thread),
+// all alike; the first launch of a call leaves it for the launches behind.  Infinite and NaN scales stay their rows' own affair.
+__device__ __forceinline__ float mm_unit(const MmParams& p, uint32_t boxes, uint32_t box_stride, int e, int lane) {
+    if (!p.first) return *p.unit;
+    float most = 0.f;
+#pragma unroll 8
+    for (int64_t m = e * 32 + lane; m < p.rows; m += kMmEpiWarps * 32) {
+        const float a = fabsf(p.scale[m]);
+        if (p.labels[m] != p.ignore_index && a <= 3.402823466e38f) most = fmaxf(most, a);
+    }
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) most = fmaxf(most, __shfl_xor_sync(0xFFFFFFFFu, most, o));
+    // through the first word of each warp's staging boxes, which hold nothing yet
+    if (lane == 0) asm volatile("st.shared.f32 [%0], %1;" ::"r"(boxes + e * box_stride), "f"(most) : "memory");
+    asm volatile("bar.sync 1, %0;" ::"n"(kMmEpiWarps * 32) : "memory");
+#pragma unroll
+    for (int w = 0; w < kMmEpiWarps; ++w) {
+        float v;
+        asm volatile("ld.shared.f32 %0, [%1];" : "=f"(v) : "r"(boxes + w * box_stride) : "memory");
+        most = fmaxf(most, v);
+    }
+    asm volatile("bar.sync 1, %0;" ::"n"(kMmEpiWarps * 32) : "memory");
+    if (most == 0.f) most = 1.f;
+    if (blockIdx.x == 0 && e == 0 && lane == 0) *p.unit = most;
+    return most;
+}
+
 // ------------------------------------------------------------------------------------------ epilogue of one warp
 // Rows row0 .. row0 + 31 (one per lane); t_addr: the warp's lanes of the tile's accumulator, column 0; half: which of
 // the tile's column groups this warp has, of `cols` columns; col0: first column of the tile in C.
 template <class C, int EPI>
 __device__ __forceinline__ void mm_epilogue(const MmMaps<C::JOBS>& tm, const MmParams& p, const MmJob& jb, int c_map, BoxWriter<C::BOXES>& out,
-                                            uint32_t t_addr, int half, int64_t row0, int64_t col0, int cols, int split, int lane, const Ctx& cx) {
+                                            uint32_t t_addr, int half, int64_t row0, int64_t col0, int cols, int split, float unit, int lane, const Ctx& cx) {
     const int64_t row = row0 + lane;
     const bool row_in = row < jb.M, warp_in = row0 < jb.M;
     const int64_t slot = C::ANY_WIDTH ? col0 / p.tile_n * (p.tile_n > C::COLS ? 2 : 1) + half : col0 / C::COLS + half;     // kMmRowStats
@@ -241,6 +274,7 @@ __device__ __forceinline__ void mm_epilogue(const MmMaps<C::JOBS>& tm, const MmP
     t_addr += half * C::COLS;
     (void)slot;
     if constexpr (EPI == kMmPlain) {
+        const float factor = jb.factor ? *jb.factor : 1.f;
         if (!jb.fp32) {
 #pragma unroll 1
             for (int c = 0; c < C::COLS; c += 64) {
@@ -251,8 +285,8 @@ __device__ __forceinline__ void mm_epilogue(const MmMaps<C::JOBS>& tm, const MmP
                 tmem_ld_wait_for(w);
 #pragma unroll
                 for (int e = 0; e < 16; ++e) {
-                    o[e] = pack_bf16(__uint_as_float(v[2 * e]), __uint_as_float(v[2 * e + 1]));
-                    o[16 + e] = pack_bf16(__uint_as_float(w[2 * e]), __uint_as_float(w[2 * e + 1]));
+                    o[e] = pack_bf16(factor * __uint_as_float(v[2 * e]), factor * __uint_as_float(v[2 * e + 1]));
+                    o[16 + e] = pack_bf16(factor * __uint_as_float(w[2 * e]), factor * __uint_as_float(w[2 * e + 1]));
                 }
                 out.put(&tm.c[c_map], o, col0 + c, row0, warp_in && col0 + c < jb.N);
             }
@@ -262,6 +296,8 @@ __device__ __forceinline__ void mm_epilogue(const MmMaps<C::JOBS>& tm, const MmP
                 uint32_t v[32];
                 tmem_ld_32x32b_x32(t_addr + c, v);
                 tmem_ld_wait_for(v);
+#pragma unroll
+                for (int e = 0; e < 32; ++e) v[e] = __float_as_uint(factor * __uint_as_float(v[e]));
                 out.put(&tm.c[c_map], v, col0 + c, split * jb.split_rows + row0, warp_in && col0 + c < jb.N, jb.add);
             }
         }
@@ -360,7 +396,7 @@ __device__ __forceinline__ void mm_epilogue(const MmMaps<C::JOBS>& tm, const MmP
             counts = l != p.ignore_index;
             label = l - p.col0 - col0;
             lse = p.lse[row];
-            scale = p.scale[row];
+            scale = p.scale[row] / unit;
         }
 #pragma unroll 1
         for (int c = 0; c < cols; c += 64) {
@@ -551,6 +587,8 @@ bf16_mm_kernel(const __grid_constant__ MmMaps<MmCfg<PAIR, EPI>::JOBS> tm, const 
         BoxWriter<C::BOXES> out(smem_base + C::BOX_OFF + static_cast<uint32_t>(e) * C::BOXES * kEpilogueBoxBytes, box_bar + 8 * e, lane);
         int it = 0;
         bool ok = true;
+        float unit = 1.f;
+        if constexpr (EPI == atb::kMmDlogits) unit = mm_unit(p, smem_base + C::BOX_OFF, C::BOXES * kEpilogueBoxBytes, e, lane);
         for (int item; ok && (item = mm_item_at<PAIR>(it)) < p.items; ++it) {
             const MmItem w = mm_item<C::JOBS>(p, item);
             const MmJob& jb = p.job[w.job];
@@ -562,7 +600,7 @@ bf16_mm_kernel(const __grid_constant__ MmMaps<MmCfg<PAIR, EPI>::JOBS> tm, const 
             tcgen05_fence_after_sync();
             if (half * C::COLS < tile_n)
                 mm_epilogue<C, EPI>(tm, p, jb, 2 * w.job + w.seg, out, tmem_base + (static_cast<uint32_t>(q * 32) << 16) + static_cast<uint32_t>(acc * C::BN),
-                                    half, row0, col0, min(C::COLS, tile_n - half * C::COLS), w.split, lane, cx);
+                                    half, row0, col0, min(C::COLS, tile_n - half * C::COLS), w.split, unit, lane, cx);
             tcgen05_fence_before_sync();
             __syncwarp();
 #ifdef ATB_TEST_WITHHOLD_ACC_ARRIVAL
@@ -641,6 +679,9 @@ __global__ void __launch_bounds__(256) bf16_mm_join_kernel(const __grid_constant
         sum(m, seg * q.N + n, v);
         uint32_t o[4];
         if constexpr (EPI == kMmPlain) {
+            const float factor = q.factor ? *q.factor : 1.f;
+#pragma unroll
+            for (int e = 0; e < 8; ++e) v[e] *= factor;
             if (q.C32) {
                 float* dst = q.C32 + m * q.N + n;
 #pragma unroll
@@ -843,6 +884,7 @@ atb_status_t launch(const atb::MmProblem* q, int n, const MmPlan& plan, char* pa
             jb.fp32 = jb.splits > 1 || x.epilogue == atb::kMmAccumulate;
             jb.split_rows = jb.splits > 1 ? atb::round_up(x.M, 32) : 0;
             jb.add = jb.splits == 1 && jb.fp32 && !x.first;
+            jb.factor = jb.splits == 1 ? x.factor : nullptr;
             for (int s = 0; s < 2; ++s) {
                 CUtensorMap* const m = &tm.c[2 * i + s];
                 bool ok = true;
@@ -876,6 +918,7 @@ atb_status_t launch(const atb::MmProblem* q, int n, const MmPlan& plan, char* pa
     p.labels = q->labels; p.ignore_index = q->ignore_index; p.col0 = q->col0;
     p.stats = q->stats; p.stats_ld = q->stats_ld; p.label_logit = q->label_logit;
     p.lse = q->lse; p.scale = q->scale;
+    p.unit = q->unit; p.rows = q->M; p.first = q->first;
     const int units = PAIR ? dev.sms / 2 : dev.sms;
     const int n_units = static_cast<int>(items < units ? items : units);
     auto kernel = bf16_mm_kernel<PAIR, EPI>;
@@ -908,6 +951,7 @@ atb_status_t join(const atb::MmProblem* q, int n, const MmPlan& plan, const char
             for (int i = 0; i < 3; ++i) { jb.C[i] = q[j].C[i]; jb.ldc[i] = q[j].ldc[i]; }
             jb.C32 = q[j].epilogue == atb::kMmAccumulate ? q[j].C32 : nullptr;
             jb.add = !q[j].first;
+            jb.factor = q[j].factor;
             jb.first = p.all;
             p.all += jb.M * (jb.N / 8) * jb.n_segs;
         }

@@ -5,7 +5,7 @@
 // Forward: the logits of a tile stay in tensor memory; what leaves is, per row and group of columns, the maximum and
 // the sum of exp(l - maximum), 8 bytes for 128 logits, and the label's logit.  A second kernel joins them.
 // Backward: the logits are computed again, a piece of the vocabulary at a time; the epilogue turns them into dl, which
-// the workspace holds for one piece (bf16: it is the operand of the next two products).  dW of the piece is complete;
+// the workspace holds for one piece (bf16: it is the operand of the next two products; in units of the largest dloss, see mm_unit).  dW of the piece is complete;
 // dx is added up over the pieces in FP32, in their order, and rounded once.
 // Tensor bound from a few hundred rows on: M = 8192, V = 131072, D = 4096 takes 26 ms for loss and gradients, 8 M V D operations
 // at 1.35 PFLOP/s, which is what the library product sustains under the power cap (1.38); M = 4096, V = 131072, D = 2048, loss
@@ -100,17 +100,18 @@ int gradient_products(atb::MmProblem* q, int64_t M, int64_t n, int64_t D, bool p
     return products;
 }
 
-// The backward workspace: dl of a piece, FP32 sums of dx where there is more than one piece, and the sums of a product that
-// is split along K.
+// The backward workspace: dl of a piece, FP32 sums of dx where there is more than one piece, the unit of dl, and the sums of a
+// product that is split along K.
 struct BackwardSpace {
     int64_t words;
-    size_t sum, partial, partial_bytes;      // offsets behind dl, size of the last part
+    size_t sum, unit, partial, partial_bytes;      // offsets behind dl, size of the last part
 };
 BackwardSpace backward_space(int64_t M, int64_t V, int64_t D, int64_t piece) {
     BackwardSpace w;
     w.words = piece_words(M, V, piece);
     w.sum = align256(static_cast<size_t>(M) * static_cast<size_t>(w.words) * 2);
-    w.partial = w.sum + (w.words < V ? align256(static_cast<size_t>(M) * static_cast<size_t>(D) * sizeof(float)) : 0);
+    w.unit = w.sum + (w.words < V ? align256(static_cast<size_t>(M) * static_cast<size_t>(D) * sizeof(float)) : 0);
+    w.partial = w.unit + 256;
     // the last piece may be shorter than the others, with a plan of its own
     const int64_t first = V < w.words ? V : w.words, last = V - (V - 1) / w.words * w.words;
     w.partial_bytes = 0;
@@ -199,6 +200,7 @@ extern "C" atb_status_t atb_linear_cross_entropy_backward(int64_t M, int64_t V, 
     const int64_t words = space.words;
     uint16_t* const dl = static_cast<uint16_t*>(workspace_dev);
     float* const sum = reinterpret_cast<float*>(static_cast<char*>(workspace_dev) + space.sum);
+    float* const unit = reinterpret_cast<float*>(static_cast<char*>(workspace_dev) + space.unit);
     void* const partial = static_cast<char*>(workspace_dev) + space.partial;
     for (int64_t v0 = 0; v0 < V; v0 += words) {
         const int64_t n = V - v0 < words ? V - v0 : words;
@@ -209,11 +211,12 @@ extern "C" atb_status_t atb_linear_cross_entropy_backward(int64_t M, int64_t V, 
         q.A[0] = {X_dev, ldx}; q.B[0] = {Wv, ldw};
         q.C[0] = dl; q.ldc[0] = words;
         q.labels = labels_dev; q.ignore_index = ignore_index; q.col0 = v0;
-        q.lse = lse_dev; q.scale = dloss_dev;
+        q.lse = lse_dev; q.scale = dloss_dev; q.unit = unit; q.first = v0 == 0;
         s = atb::mm_launch(&q, 1, nullptr, st);
         if (s != ATB_OK) return s;
         atb::MmProblem grad[atb::kMmGroup];
         const int products = gradient_products(grad, M, n, D, words < V, dX_dev, dW_dev);
+        for (int j = 0; j < products; ++j) grad[j].factor = unit;
         if (dX_dev) {
             atb::MmProblem& dx = grad[0];
             dx.A[0] = {dl, words}; dx.B[0] = {Wv, ldw};

@@ -39,7 +39,7 @@ def _check_forward(x, w, labels, loss, lse, ignore=IGNORE):
 
 
 def _check_backward(x, w, labels, dloss, lse, dl, dX, dW, ignore=IGNORE):
-    """dl: the workspace's dL where the vocabulary is one piece, else None."""
+    """dl: the workspace's dL, in units of the largest dloss that counts, where the vocabulary is one piece, else None."""
     M, V = x.shape[0], w.shape[0]
     xd, wd = x.double(), w.double()
     _, want_lse, p = ref.cross_entropy(xd, wd, labels, ignore)
@@ -47,11 +47,11 @@ def _check_backward(x, w, labels, dloss, lse, dl, dX, dW, ignore=IGNORE):
     hot = torch.zeros_like(p).scatter_(1, labels.clamp(min=0)[:, None], 1.0)
     want = (p - hot) * scale
     # exp(l - lse): both exponents' errors, the fast exponential as above
-    err = scale * (p * (3 * _logit_error(xd, wd)[:, None] + 2.0 ** -14 + 16 * U32 * want_lse.abs()[:, None]) + 2 * U32)
+    err = scale * (p * (3 * _logit_error(xd, wd)[:, None] + 2.0 ** -14 + 16 * U32 * want_lse.abs()[:, None]) + 3 * U32)
     err = err + U16 * (want.abs() + err)
     if dl is not None:
-        ref.check(dl, want, err, "dl")
-        exact = dl.double()
+        exact = dl.double() * scale.max()
+        ref.check(exact, want, err, "dl")
         for got, left, right, name in ((dX, exact, wd, "dx"), (dW, exact.t(), xd, "dw")):
             res, e = left @ right, product_bound(left, right)
             ref.check(got, res, e + U16 * (res.abs() + e), name)
@@ -180,3 +180,42 @@ def test_gradient_against_differences():
         slope = (loss(up) - loss(down)) / (2 * h)
         # two roundings to bf16: dl and the result
         assert abs(slope - float((grads[i] * d).sum())) <= 3 * U16 * float((grads[i] * d).abs().sum()), i
+
+
+@pytest.mark.parametrize("M,V,D,piece", [(255, 3000, 256, 0), (255, 3000, 256, 1024), (12, 5003, 512, 0)])
+def test_a_mean_is_not_rounded(M, V, D, piece):
+    """dloss = 1 / 255, half way between two bf16 numbers, in every row: rounded as it is it would move both gradients by
+    2^-8 of their size.  Left are dL's other roundings and the result's, of 2^-8 / sqrt(3) at most in the mean square each; along the
+    result only a label's p - 1 counts, which is off by at most 2^-9."""
+    x, w, labels, _ = _inputs(M, V, D)
+    dloss = torch.full((M,), 1 / 255, device="cuda")
+    dloss[labels == IGNORE] = 1e30                             # does not count
+    _, lse = atb.atb_linear_cross_entropy(x, w, labels)
+    dX, dW = atb.atb_linear_cross_entropy_backward(dloss, x, w, labels, lse, piece=piece)
+    _, _, p = ref.cross_entropy(x.double(), w.double(), labels, IGNORE)
+    d = (p - torch.zeros_like(p).scatter_(1, labels.clamp(min=0)[:, None], 1.0)) * ((labels != IGNORE) * float(dloss[0]))[:, None]
+    for got, want, name in ((dX, d @ w.double(), "dx"), (dW, d.t() @ x.double(), "dw")):
+        off = float((got.double() - want).norm() / want.norm())
+        along = float((got.double() * want).sum() / (want * want).sum()) - 1
+        assert off <= 2.0 ** -8 * (2 / 3) ** 0.5, (name, off)
+        assert abs(along) <= 2.0 ** -9, (name, along)
+
+
+def test_scales_of_every_kind():
+    """0 in every row, numbers near the ends of FP32, an infinite and a NaN one beside finite ones."""
+    x, w, labels, dloss = _inputs(40, 300, 64)
+    labels[:] = torch.arange(40, device="cuda")
+    _, lse = atb.atb_linear_cross_entropy(x, w, labels)
+    back = lambda s: atb.atb_linear_cross_entropy_backward(s, x, w, labels, lse)  # noqa: E731
+    dX, dW = back(torch.zeros_like(dloss))
+    assert bool((dX == 0).all()) and bool((dW == 0).all())
+    one = back(dloss)
+    for power in (-60, 60):                                    # a power of two changes no rounding
+        dX, dW = back(dloss * 2.0 ** power)
+        assert torch.equal(dX.double(), one[0].double() * 2.0 ** power) and torch.equal(dW.double(), one[1].double() * 2.0 ** power)
+    dloss[7], dloss[9] = float("inf"), float("nan")
+    dX, dW = back(dloss)
+    rest = [i for i in range(40) if i not in (7, 9)]
+    assert not bool(torch.isfinite(dX[[7, 9]]).any()) and bool(torch.isfinite(dX[rest]).all())
+    assert bool(torch.isnan(dW).all())
+    _check_backward(x[rest], w, labels[rest], dloss[rest], lse[rest], None, dX[rest], back(torch.where(torch.isfinite(dloss), dloss, 0.0))[1])
