@@ -17,8 +17,8 @@
 // the same bits on every call.
 // Measured (compulsory bytes, of a measured copy rate of 6.55 TB/s): 16384 x 8192 bf16, FP32 weights: forward 94 us, 5.7 TB/s,
 // backward 139 us, 5.8 TB/s; 8192 x 8192 FP32: 97 and 132 us, 5.5 and 6.1 TB/s; 8192 x 4096 bf16: 28 and 41 us, 4.8 TB/s;
-// 12265 x 2494 off 16-byte boundaries: FP32 46 and 70 us, 5.4 and 5.2 TB/s, bf16 43 and 57 us, 2.9 and 3.2 TB/s (bound by
-// instructions: an element at a time).  With one block per row and nothing on its way the first of these took 117 and 268 us.
+// 12265 x 2499 off 16-byte boundaries: FP32 45 and 70 us, 5.5 and 5.3 TB/s, bf16 38 and 57 us, 3.2 and 3.2 TB/s (bound by
+// instructions: an element at a time; groups of 8 shifted into place on both ways through shared memory took 48 and 73 us).  With one block per row and nothing on its way the first of these took 117 and 268 us.
 #include <cuda_bf16.h>
 #include <cuda_runtime.h>
 
@@ -27,9 +27,26 @@
 #include "dependent_launch.cuh"
 #include "f32x2.cuh"
 
+#include <type_traits>
+
 namespace {
 
 constexpr int kElems = 16;           // most elements of a row per thread
+// Threads per row: the fewest that hold it, so that a thread has 11 to 16 elements.  8192 rows of 6000 bf16 elements take 37.7 us
+// forward with 384 threads, 44.5 us with 512; 65536 rows of 1024 45 us with 64, 57 us with 128 threads of 8 elements.
+constexpr int kThreadCounts[] = {32, 64, 96, 128, 192, 256, 384, 512, 768, 1024};
+// Single elements of a thread that lie inside every row that `tpr` threads get: they need no test against N.  12265 x 2499 bf16 forward
+// 38 instead of 43 us, 131072 x 333 53 instead of 72, 5000 x 12001 backward 129 instead of 164.  (32 threads also take rows
+// of half their elements, in kernels of nv groups that hold no more.)  Groups of 8 need two tests in all, and without the
+// first the compiler kept more alive than 64 registers hold: 16384 x 8192 101 instead of 93 us.
+__host__ __device__ constexpr int full_groups(int tpr, int vec, int nv) {
+    if (vec > 1) return 0;
+    int fewer = tpr == 32 && nv * vec == kElems ? 16 : 0;
+    for (const int t : kThreadCounts)
+        if (t < tpr) fewer = t;
+    const int full = fewer * kElems / tpr;
+    return full < nv ? full : nv;
+}
 // Rows on their way per block: what the shared memory holds beside the row in hand.
 template <class T, int TPR>
 constexpr int kAhead = sizeof(T) == 2 ? (TPR < 1024 ? 3 : 2) : (TPR < 768 ? 2 : 1);
@@ -110,6 +127,20 @@ __device__ __forceinline__ void load_or(const T* p, int64_t n, int64_t N, float 
         else r.w[i] = half | half << 16;
     }
     if (p && n < N) load_raw<T, VEC>(p + n, r);
+}
+// What a thread keeps of them: as they are in memory, or, one by one, in FP32 (a register each either way).
+template <class T, int VEC>
+using Kept = std::conditional_t<VEC == 1, float, T>;
+template <class T, int VEC>
+__device__ __forceinline__ void keep_or(const T* p, int64_t n, int64_t N, float none, Raw<Kept<T, VEC>, VEC>& r) {
+    if constexpr (VEC == 1 && sizeof(T) == 2) {
+        Raw<T, 1> raw;
+        load_or<T, 1>(p, n, N, none, raw);
+        // kept: the compiler otherwise widens them again in every row
+        asm volatile("shl.b32 %0, %1, 16;" : "=r"(r.w[0]) : "r"(static_cast<uint32_t>(raw.w[0])));
+    } else {
+        load_or<T, VEC>(p, n, N, none, r);
+    }
 }
 template <class T, int VEC>
 __device__ __forceinline__ void store_f(T* p, const float (&v)[VEC]) {
@@ -323,7 +354,7 @@ template <class TX, class TW, int VEC, int TPR, int NV, bool BFP>
 __global__ void __launch_bounds__(TPR == 32 ? 128 : TPR, blocks_per_sm(TPR, false, VEC > 1)) layer_norm_kernel(const FwdParams p) {
     using Source = RowSource<TX, VEC, TPR, NV>;
     constexpr int WALKERS = TPR == 32 ? 4 : 1, W = TPR / 32;
-    constexpr int STAGES = kAheadFwd<TX, TPR> + 1;
+    constexpr int STAGES = kAheadFwd<TX, TPR> + 1, FULL = full_groups(TPR, VEC, NV);
     extern __shared__ __align__(16) uint8_t ring[];
     __shared__ float2 red[2][W];
     const int t = TPR == 32 ? threadIdx.x & 31 : threadIdx.x, lane = threadIdx.x & 31, warp = TPR == 32 ? 0 : threadIdx.x >> 5;
@@ -345,11 +376,11 @@ __global__ void __launch_bounds__(TPR == 32 ? 128 : TPR, blocks_per_sm(TPR, fals
         if (first + s * step < p.M) src.fetch(s, first + s * step);
         async_commit();
     }
-    Raw<TW, VEC> w[NV], b[NV];
+    Raw<Kept<TW, VEC>, VEC> w[NV], b[NV];
 #pragma unroll
     for (int i = 0; i < NV; ++i) {
-        load_or<TW, VEC>(static_cast<const TW*>(p.w), col + i * TPR * VEC, N, 1.f, w[i]);
-        load_or<TW, VEC>(static_cast<const TW*>(p.b), col + i * TPR * VEC, N, 0.f, b[i]);
+        keep_or<TW, VEC>(static_cast<const TW*>(p.w), col + i * TPR * VEC, N, 1.f, w[i]);
+        keep_or<TW, VEC>(static_cast<const TW*>(p.b), col + i * TPR * VEC, N, 0.f, b[i]);
     }
     int stage = 0, turn = 0;
     for (int64_t m = first; m < p.rows; m += step, turn ^= 1) {
@@ -363,7 +394,7 @@ __global__ void __launch_bounds__(TPR == 32 ? 128 : TPR, blocks_per_sm(TPR, fals
             float v[NV][VEC], s[1] = {0.f};
 #pragma unroll
             for (int i = 0; i < NV; ++i) {
-                if (col + i * TPR * VEC < N) {
+                if (i < FULL || col + i * TPR * VEC < N) {
                     Raw<TX, VEC> raw;
                     src.read(stage, m, i, raw);
                     to_float(raw, v[i]);
@@ -376,7 +407,7 @@ __global__ void __launch_bounds__(TPR == 32 ? 128 : TPR, blocks_per_sm(TPR, fals
             s[0] = 0.f;
 #pragma unroll
             for (int i = 0; i < NV; ++i)
-                if (col + i * TPR * VEC < N)
+                if (i < FULL || col + i * TPR * VEC < N)
 #pragma unroll
                     for (int e = 0; e < VEC; ++e) s[0] += (v[i][e] - mu) * (v[i][e] - mu);
             warp_sum(s);
@@ -401,10 +432,10 @@ __global__ void __launch_bounds__(TPR == 32 ? 128 : TPR, blocks_per_sm(TPR, fals
             TX* const y = BFP ? nullptr : static_cast<TX*>(p.y) + m * p.ldy + col;
 #pragma unroll
             for (int i = 0; i < NV; ++i) {
-                if (col + i * TPR * VEC < N) {
+                if (i < FULL || col + i * TPR * VEC < N) {
                     float fw[VEC], fb[VEC];
-                    to_float(w[i], fw);
-                    to_float(b[i], fb);
+                    to_float<Kept<TW, VEC>, VEC>(w[i], fw);
+                    to_float<Kept<TW, VEC>, VEC>(b[i], fb);
 #pragma unroll
                     for (int e = 0; e < VEC; ++e) v[i][e] = fmaf(fmaf(v[i][e], r, shift), fw[e], fb[e]);
                     if constexpr (BFP) put_block(p, m, col + i * TPR * VEC, v[i]);
@@ -475,7 +506,7 @@ template <class TX, class TW, int VEC, int TPR, int NV>
 __global__ void __launch_bounds__(TPR == 32 ? 128 : TPR, blocks_per_sm(TPR, true, VEC > 1)) layer_norm_backward_kernel(const BwdParams p) {
     using Source = RowSource<TX, VEC, TPR, NV>;
     constexpr int WALKERS = TPR == 32 ? 4 : 1, W = TPR / 32;
-    constexpr int STAGES = kAhead<TX, TPR> + 1, P = NV * VEC / 2;
+    constexpr int STAGES = kAhead<TX, TPR> + 1, P = NV * VEC / 2, FULL = full_groups(TPR, VEC, NV);
     // 768 and 1024 threads have 80 and 64 registers each: the row is read from shared memory again after the sums
     constexpr bool REREAD = TPR >= 768;
     extern __shared__ __align__(16) uint8_t ring[];
@@ -495,10 +526,10 @@ __global__ void __launch_bounds__(TPR == 32 ? 128 : TPR, blocks_per_sm(TPR, true
         }
         async_commit();
     }
-    Raw<TW, VEC> w[NV];
+    Raw<Kept<TW, VEC>, VEC> w[NV];
     float2 dw[P], db[P];
 #pragma unroll
-    for (int i = 0; i < NV; ++i) load_or<TW, VEC>(static_cast<const TW*>(p.w), col + i * TPR * VEC, N, 1.f, w[i]);
+    for (int i = 0; i < NV; ++i) keep_or<TW, VEC>(static_cast<const TW*>(p.w), col + i * TPR * VEC, N, 1.f, w[i]);
 #pragma unroll
     for (int k = 0; k < P; ++k) dw[k] = db[k] = make_float2(0.f, 0.f);
     int stage = 0, turn = 0;
@@ -522,7 +553,7 @@ __global__ void __launch_bounds__(TPR == 32 ? 128 : TPR, blocks_per_sm(TPR, true
             Raw<TX, VEC> raw[NV];
 #pragma unroll
             for (int i = 0; i < NV; ++i) {
-                if (col + i * TPR * VEC < N) sx.read(stage, m, i, raw[i]);
+                if (i < FULL || col + i * TPR * VEC < N) sx.read(stage, m, i, raw[i]);
                 else clear(raw[i]);
             }
             to_pairs<TX, VEC, NV>(raw, z);
@@ -530,7 +561,7 @@ __global__ void __launch_bounds__(TPR == 32 ? 128 : TPR, blocks_per_sm(TPR, true
             for (int k = 0; k < P; ++k) z[k] = fma2(z[k], scale, shift);
 #pragma unroll
             for (int i = 0; i < NV; ++i) {
-                if (col + i * TPR * VEC < N) sd.read(stage, m, i, raw[i]);
+                if (i < FULL || col + i * TPR * VEC < N) sd.read(stage, m, i, raw[i]);
                 else clear(raw[i]);
             }
             to_pairs<TX, VEC, NV>(raw, g);
@@ -538,7 +569,7 @@ __global__ void __launch_bounds__(TPR == 32 ? 128 : TPR, blocks_per_sm(TPR, true
         load();
         {
             float2 f[P];
-            to_pairs<TW, VEC, NV>(w, f);
+            to_pairs<Kept<TW, VEC>, VEC, NV>(w, f);
 #pragma unroll
             for (int k = 0; k < P; ++k) {
                 dw[k] = fma2(g[k], z[k], dw[k]);
@@ -556,7 +587,7 @@ __global__ void __launch_bounds__(TPR == 32 ? 128 : TPR, blocks_per_sm(TPR, true
             if constexpr (REREAD) {
                 load();
                 float2 f[P];
-                to_pairs<TW, VEC, NV>(w, f);
+                to_pairs<Kept<TW, VEC>, VEC, NV>(w, f);
 #pragma unroll
                 for (int k = 0; k < P; ++k) g[k] = mul2(g[k], f[k]);
             }
@@ -565,7 +596,7 @@ __global__ void __launch_bounds__(TPR == 32 ? 128 : TPR, blocks_per_sm(TPR, true
             for (int k = 0; k < P; ++k) g[k] = fma2(z[k], c1, fma2(g[k], scale, c0));
 #pragma unroll
             for (int i = 0; i < NV; ++i) {
-                if (col + i * TPR * VEC < N) {
+                if (i < FULL || col + i * TPR * VEC < N) {
                     float f[VEC];
                     group<VEC, P>(g, i, f);
                     store_f<TX, VEC>(dx + i * TPR * VEC, f);
@@ -581,7 +612,7 @@ __global__ void __launch_bounds__(TPR == 32 ? 128 : TPR, blocks_per_sm(TPR, true
         float* out = p.part + first * 2 * p.N + col;
 #pragma unroll
         for (int i = 0; i < NV; ++i) {
-            if (col + i * TPR * VEC < N) {
+            if (i < FULL || col + i * TPR * VEC < N) {
                 float f[VEC];
                 group<VEC, P>(dw, i, f);
                 store_f<float, VEC>(out + i * TPR * VEC, f);
@@ -662,11 +693,9 @@ __global__ void __launch_bounds__(32 * kSumWarps) layer_norm_backward_sum_kernel
 }
 
 // ---------------------------------------------------------------------------------- host
-// Threads per row: the fewest (at most `most`) that hold a row of N elements, so that a thread has 11 to 16; 0: a wide kernel.
-// 8192 rows of 6000 bf16 elements take 37.7 us forward with 384 threads, 44.5 us with 512; 65536 rows of 1024 45 us with 64, 57 us
-// with 128 threads of 8 elements.
+// Threads per row, at most `most`; 0: a wide kernel.
 int threads_per_row(int64_t N, int most) {
-    for (int t : {32, 64, 96, 128, 192, 256, 384, 512, 768, 1024})
+    for (const int t : kThreadCounts)
         if (t <= most && N <= static_cast<int64_t>(t) * kElems) return t;
     return 0;
 }
