@@ -317,7 +317,8 @@ struct RowSource<T, 1, TPR, NV> {
         else asm volatile("ld.shared.b16 %0, [%1];" : "=h"(r.w[0]) : "r"(at + i * TPR * 2) : "memory");
     }
 };
-// Between this thread's wait for its copies and its reads: the other threads' copies have landed too.
+// Between this thread's wait for its copies and its reads: the other threads' copies have landed too.  Between reads that no sum over
+// the row's threads follows and the next copies into their stage: the other threads have read.
 template <class Source, int VEC, int TPR>
 __device__ __forceinline__ void row_barrier() {
     if constexpr (Source::SHARED) {
@@ -603,7 +604,8 @@ __global__ void __launch_bounds__(TPR == 32 ? 128 : TPR, blocks_per_sm(TPR, true
                 }
             }
         }
-        if constexpr (REREAD && VEC == 1) __syncthreads();      // the row's stage is the next to be filled
+        // the row's stage is the next to be filled, by other threads than those that have just read it again
+        if constexpr (REREAD) row_barrier<Source, VEC, TPR>();
         mu = next_mu;
         r = next_r;
         stage = stage + 1 == STAGES ? 0 : stage + 1;
