@@ -374,6 +374,8 @@ def atb_select_tiling(M: int, N: int, K: int, hw: atb_hw_params_t | None = None,
 
 
 # ------------------------------------------------------------------ between the products: norm, feed-forward, loss
+# stream: None (the current one), a torch stream or a handle.  What a call allocates belongs to the stream that it runs on; the
+# caller orders the inputs before it and the use of the results behind it, as between any two streams.
 ACTIVATIONS = {"silu": 0, "gelu": 1, "gelu_tanh": 2}
 
 

@@ -8,11 +8,13 @@
 
 #include <ATen/ATen.h>
 #include <c10/cuda/CUDAFunctions.h>
+#include <c10/cuda/CUDAGuard.h>
 #include <c10/cuda/CUDAStream.h>
 #include <torch/csrc/Exceptions.h>
 #include <torch/csrc/autograd/python_variable.h>
 
 #include <cstring>
+#include <optional>
 #include <vector>
 
 #include "atb.h"
@@ -47,22 +49,25 @@ std::string told(const at::Tensor& t) {
     return t.defined() ? c10::str(t.sizes(), " of ", t.scalar_type(), " on ", t.device(), ", strides ", t.strides()) : std::string("None");
 }
 // The rest of a call: the device of its first matrix, which has to be the current one, its stream, and what it allocates.
+// What a call allocates belongs to the stream that its kernels run on: a block that was freed on another stream may still
+// be read or written there.
 struct Call {
     c10::DeviceIndex device = -1;
     cudaStream_t stream = nullptr;
-    bool other_stream = false;             // not the current one: what is allocated here is used there
-    std::vector<at::Tensor> made;
+    std::optional<c10::cuda::CUDAStream> current;
+    bool other_stream = false;             // not the current one
+    std::vector<at::Tensor> made;          // results that were allocated on it
 
     Call(const at::Tensor& first, const char* name, PyObject* stream_arg) {
         if (!first.defined() || !first.is_cuda() || first.dim() != 2) refuse(c10::str(name, ": a CUDA matrix, got ", told(first)));
         device = first.get_device();
         if (device != c10::cuda::current_device()) refuse(c10::str(name, " is on cuda:", int(device), ", the current device is cuda:", int(c10::cuda::current_device())));
-        const cudaStream_t current = c10::cuda::getCurrentCUDAStream(device).stream();
-        stream = current;
+        current = c10::cuda::getCurrentCUDAStream(device);
+        stream = current->stream();
         if (stream_arg != Py_None) {
             stream = static_cast<cudaStream_t>(PyLong_AsVoidPtr(stream_arg));
             if (PyErr_Occurred()) throw python_error();
-            other_stream = stream != current;
+            other_stream = stream != current->stream();
         }
     }
     // Row-major matrix on this device; returns its leading dimension.
@@ -78,26 +83,34 @@ struct Call {
         if (!(t.defined() && t.is_cuda() && t.get_device() == device && t.scalar_type() == type && t.dim() == 1 && t.size(0) == n && t.is_contiguous()))
             refuse(c10::str(name, ": a contiguous vector of ", n, " ", type, " on cuda:", int(device), ", got ", told(t)));
     }
-    at::Tensor make(at::IntArrayRef size, at::ScalarType type) {
-        at::Tensor t = at::empty(size, at::TensorOptions().dtype(type).device(c10::Device(c10::kCUDA, device)));
+    at::Tensor make(at::IntArrayRef size, at::ScalarType type) const {
+        const auto options = at::TensorOptions().dtype(type).device(c10::Device(c10::kCUDA, device));
+        if (!other_stream) return at::empty(size, options);
+        // 0 and 1 are names of the default stream
+        const bool is_default = reinterpret_cast<uintptr_t>(stream) <= 1;
+        const c10::cuda::CUDAStreamGuard guard(is_default ? c10::cuda::getDefaultCUDAStream(device) : c10::cuda::getStreamFromExternal(stream, device));
+        return at::empty(size, options);
+    }
+    at::Tensor make_result(at::IntArrayRef size, at::ScalarType type) {
+        at::Tensor t = make(size, type);
         if (other_stream) made.push_back(t);
         return t;
     }
     // An output: the caller's, checked, or a new one.
     int64_t out_matrix(at::Tensor& t, int64_t rows, int64_t cols, at::ScalarType type, const char* name) {
         if (t.defined()) return matrix(t, rows, cols, type, name);
-        t = make({rows, cols}, type);
+        t = make_result({rows, cols}, type);
         return cols;
     }
     void out_vector(at::Tensor& t, int64_t n, at::ScalarType type, const char* name) {
         if (t.defined()) vector(t, n, type, name);
-        else t = make({n}, type);
+        else t = make_result({n}, type);
     }
     void out_contiguous(at::Tensor& t, int64_t rows, int64_t cols, at::ScalarType type, const char* name) {
         if (out_matrix(t, rows, cols, type, name) != cols) refuse(c10::str(name, ": contiguous"));
     }
     // Room for `need` bytes: the caller's workspace, or a new one.
-    size_t workspace(at::Tensor& t, size_t need) {
+    size_t workspace(at::Tensor& t, size_t need) const {
         if (!t.defined()) {
             if (need == 0) return 0;
             t = make({static_cast<int64_t>(need)}, at::kByte);
@@ -106,12 +119,10 @@ struct Call {
         if (!t.is_cuda() || t.get_device() != device || !t.is_contiguous()) refuse("workspace: contiguous, on the tensors' device");
         return t.nbytes();
     }
-    // Ends the call: memory made here stays with the stream that uses it until that is through.
+    // Ends the call.  The caller will use the results on the current stream (once it has waited for the one given): they are not
+    // handed out again before that is through with them either.
     PyObject* done(atb_status_t status, std::initializer_list<at::Tensor> result) {
-        if (other_stream) {
-            const auto s = c10::cuda::getStreamFromExternal(stream, device);
-            for (at::Tensor& t : made) t.record_stream(s);
-        }
+        for (const at::Tensor& t : made) t.record_stream(*current);
         if (status != ATB_OK) return PyLong_FromLong(status);
         PyObject* tuple = PyTuple_New(static_cast<Py_ssize_t>(result.size()));
         if (!tuple) throw python_error();
