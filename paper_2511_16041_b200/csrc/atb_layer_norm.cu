@@ -12,7 +12,8 @@
 // their first element on, and read element by element from there.
 // The variance is summed around means: of a warp's elements around their own mean in registers, and the warps' pairs
 // (mean, sum of squares) joined by sum n_w (mean_w - mu)^2, in one exchange; sum(x^2) - N mu^2 would lose its digits
-// where |mu| >> sqrt(v).  All sums are FP32.  Rows wider than the widest kernel are read again for every sum (*_wide kernels).
+// where |mu| >> sqrt(v).  Means are quotients, not products with a rounded 1 / N, and z is made of distances to a mean, so that z is 0
+// where all elements are one number (x r - mu r by one fma is off by the rounding of mu r: 1e-3 for rows of 100).  All sums are FP32.  Rows wider than the widest kernel are read again for every sum (*_wide kernels).
 // Blocks write their sums of dw and db to the workspace, a second kernel adds those up in a fixed order: no atomics,
 // the same bits on every call.
 // Measured (compulsory bytes, of a measured copy rate of 6.55 TB/s): 16384 x 8192 bf16, FP32 weights: forward 94 us, 5.7 TB/s,
@@ -216,6 +217,12 @@ __device__ __forceinline__ void warp_sum(float (&v)[K]) {
 #pragma unroll
         for (int k = 0; k < K; ++k) v[k] += __shfl_xor_sync(0xFFFFFFFFu, v[k], o);
 }
+// s / n from inv = 1 / n: the product's remainder, which an fma gives exactly, takes it to the quotient where that is a number of
+// FP32 (and to the nearest but for rare ties of its rounding), without a division's branches.  An infinite sum stays what it is.
+__device__ __forceinline__ float quotient(float s, float n, float inv) {
+    const float q = s * inv;
+    return fabsf(q) <= 3.402823466e38f ? fmaf(fmaf(-q, n, s), inv, q) : q;
+}
 // Every thread of the row gets the sum of K values over the TPR threads.  TPR = 32: one warp; else the whole block,
 // through `red`, of which a row takes another slice than the row before it (a slice is written again only after a
 // barrier that follows its last read).
@@ -404,22 +411,26 @@ __global__ void __launch_bounds__(TPR == 32 ? 128 : TPR, blocks_per_sm(TPR, fals
                 }
             }
             warp_sum(s);
-            float mu = s[0] * inv_own;
+            const float mine = quotient(s[0], __shfl_sync(0xFFFFFFFFu, elems, warp), inv_own);       // the mean of the warp's elements
             s[0] = 0.f;
 #pragma unroll
             for (int i = 0; i < NV; ++i)
                 if (i < FULL || col + i * TPR * VEC < N)
 #pragma unroll
-                    for (int e = 0; e < VEC; ++e) s[0] += (v[i][e] - mu) * (v[i][e] - mu);
+                    for (int e = 0; e < VEC; ++e) {
+                        v[i][e] -= mine;
+                        s[0] += v[i][e] * v[i][e];
+                    }
             warp_sum(s);
+            float mu = mine;
             if constexpr (TPR > 32) {
-                if (lane == 0) red[turn][warp] = make_float2(mu, s[0]);
+                if (lane == 0) red[turn][warp] = make_float2(mine, s[0]);
                 __syncthreads();
                 // every warp joins the warps' pairs: lane l has warp l's
                 const float2 part = lane < W ? red[turn][lane] : make_float2(0.f, 0.f);
                 float sum[1] = {elems * part.x};
                 warp_sum(sum);
-                mu = sum[0] * inv_n;
+                mu = quotient(sum[0], static_cast<float>(N), inv_n);
                 s[0] = part.y + elems * (part.x - mu) * (part.x - mu);
                 warp_sum(s);
             }
@@ -428,8 +439,8 @@ __global__ void __launch_bounds__(TPR == 32 ? 128 : TPR, blocks_per_sm(TPR, fals
                 if (p.mean) p.mean[m] = mu;
                 if (p.rstd) p.rstd[m] = r;
             }
-            // z = x r - mu r: the rounded mu r is off by 2^-24 |mu| r, less than what the rounded mean is
-            const float shift = -mu * r;
+            // z = (x - mu) r from the distances to the warp's mean
+            const float shift = (mine - mu) * r;
             TX* const y = BFP ? nullptr : static_cast<TX*>(p.y) + m * p.ldy + col;
 #pragma unroll
             for (int i = 0; i < NV; ++i) {
@@ -466,7 +477,7 @@ __global__ void __launch_bounds__(1024) layer_norm_wide_kernel(const FwdParams p
     }
     const float inv_n = 1.f / static_cast<float>(p.N);
     row_sum<1024, 1>(s, red[0]);
-    const float mu = s[0] * inv_n;
+    const float mu = quotient(s[0], static_cast<float>(p.N), inv_n);
     s[0] = 0.f;
     for (int64_t n = threadIdx.x * VEC; n < p.N; n += 1024 * VEC) {
         load_f<TX, VEC>(x + n, v);
@@ -548,8 +559,8 @@ __global__ void __launch_bounds__(TPR == 32 ? 128 : TPR, blocks_per_sm(TPR, true
         async_wait<kAhead<TX, TPR>>();
         row_barrier<Source, VEC, TPR>();
         // z, dy and g = dy w of this thread; elements past the row's end have dy = 0 and count in no sum
-        float2 z[P], g[P], s0 = make_float2(0.f, 0.f), s1 = s0;
-        const float2 scale = both(r), shift = both(-mu * r);
+        float2 z[P], g[P], s0 = make_float2(0.f, 0.f), s1 = s0;        // z: x - mu as loaded
+        const float2 scale = both(r), shift = both(-mu);
         const auto load = [&] {
             Raw<TX, VEC> raw[NV];
 #pragma unroll
@@ -559,7 +570,7 @@ __global__ void __launch_bounds__(TPR == 32 ? 128 : TPR, blocks_per_sm(TPR, true
             }
             to_pairs<TX, VEC, NV>(raw, z);
 #pragma unroll
-            for (int k = 0; k < P; ++k) z[k] = fma2(z[k], scale, shift);
+            for (int k = 0; k < P; ++k) z[k] = add2(z[k], shift);
 #pragma unroll
             for (int i = 0; i < NV; ++i) {
                 if (i < FULL || col + i * TPR * VEC < N) sd.read(stage, m, i, raw[i]);
@@ -573,6 +584,7 @@ __global__ void __launch_bounds__(TPR == 32 ? 128 : TPR, blocks_per_sm(TPR, true
             to_pairs<Kept<TW, VEC>, VEC, NV>(w, f);
 #pragma unroll
             for (int k = 0; k < P; ++k) {
+                z[k] = mul2(z[k], scale);
                 dw[k] = fma2(g[k], z[k], dw[k]);
                 db[k] = add2(db[k], g[k]);
                 g[k] = mul2(g[k], f[k]);
@@ -583,18 +595,20 @@ __global__ void __launch_bounds__(TPR == 32 ? 128 : TPR, blocks_per_sm(TPR, true
         float s[2] = {s0.x + s0.y, s1.x + s1.y};
         row_sum<TPR, 2>(s, red[turn]);
         if (p.dx) {
-            // r (g - c0 - z c1)
-            const float2 c0 = both(-r * (s[0] * inv_n)), c1 = both(-r * (s[1] * inv_n));
-            if constexpr (REREAD) {
+            TX* const dx = static_cast<TX*>(p.dx) + m * p.lddx + col;
+            const float m0 = s[0] * inv_n, m1 = s[1] * inv_n;
+            if constexpr (REREAD) {        // r (dy w - m0 - (x - mu) (r m1))
                 load();
                 float2 f[P];
                 to_pairs<Kept<TW, VEC>, VEC, NV>(w, f);
+                const float2 c0 = both(-m0), c1 = both(-r * m1);
 #pragma unroll
-                for (int k = 0; k < P; ++k) g[k] = mul2(g[k], f[k]);
+                for (int k = 0; k < P; ++k) g[k] = mul2(fma2(z[k], c1, fma2(g[k], f[k], c0)), scale);
+            } else {                       // r g - r m0 - z (r m1)
+                const float2 c0 = both(-r * m0), c1 = both(-r * m1);
+#pragma unroll
+                for (int k = 0; k < P; ++k) g[k] = fma2(z[k], c1, fma2(g[k], scale, c0));
             }
-            TX* const dx = static_cast<TX*>(p.dx) + m * p.lddx + col;
-#pragma unroll
-            for (int k = 0; k < P; ++k) g[k] = fma2(z[k], c1, fma2(g[k], scale, c0));
 #pragma unroll
             for (int i = 0; i < NV; ++i) {
                 if (i < FULL || col + i * TPR * VEC < N) {
