@@ -11,6 +11,7 @@ raises if the library cannot be loaded.
 from __future__ import annotations
 
 import ctypes
+import operator
 import os
 from typing import NamedTuple
 
@@ -436,7 +437,11 @@ def atb_layer_norm_backward(dY, X, W, mean, rstd, dX=None, dW=None, dB=None, wor
 
 
 def _act(act):
-    return ACTIVATIONS[act] if act in ACTIVATIONS else int(act)
+    if not isinstance(act, str):
+        return operator.index(act)
+    if act not in ACTIVATIONS:
+        raise ValueError(f"act={act!r}: one of {', '.join(ACTIVATIONS)}")
+    return ACTIVATIONS[act]
 
 
 def atb_gated_ffn_workspace_bytes(M: int, D: int, F: int) -> int:

@@ -144,6 +144,16 @@ int64_t integer(PyObject* o) {
     if (v == -1 && PyErr_Occurred()) throw python_error();
     return v;
 }
+// The number of an enum; what an int does not hold becomes -1, which no enum has.
+int enumerator(PyObject* o) {
+    const int64_t v = integer(o);
+    return v == static_cast<int>(v) ? static_cast<int>(v) : -1;
+}
+bool truth(PyObject* o) {
+    const int v = PyObject_IsTrue(o);
+    if (v < 0) throw python_error();
+    return v == 1;
+}
 void expect(Py_ssize_t given, Py_ssize_t wanted) {
     if (given != wanted) refuse(c10::str("takes ", wanted, " arguments, got ", given));
 }
@@ -242,9 +252,9 @@ PyObject* gated_ffn(PyObject*, PyObject* const* a, Py_ssize_t n) {
     HANDLE_TH_ERRORS
     expect(n, 12);
     const at::Tensor X = tensor(a[0], "X"), Wg = tensor(a[1], "Wg"), Wu = tensor(a[2], "Wu"), Wd = tensor(a[3], "Wd");
-    const int act = static_cast<int>(integer(a[4]));
+    const int act = enumerator(a[4]);
     at::Tensor Y = tensor(a[6], "Y"), H = tensor(a[7], "H"), G = tensor(a[8], "G"), U = tensor(a[9], "U"), ws = tensor(a[10], "workspace");
-    const bool save = PyObject_IsTrue(a[5]) == 1 || G.defined() || U.defined();
+    const bool save = truth(a[5]) || G.defined() || U.defined();
     Call c(X, "X", a[11]);
     const FfnShapes s(c, X, Wg, Wu, Wd);
     const int64_t ldy = c.out_matrix(Y, s.M, s.D, at::kBFloat16, "Y");
@@ -265,7 +275,7 @@ PyObject* gated_ffn_backward(PyObject*, PyObject* const* a, Py_ssize_t n) {
     expect(n, 15);
     const at::Tensor dY = tensor(a[0], "dY"), X = tensor(a[1], "X"), Wg = tensor(a[2], "Wg"), Wu = tensor(a[3], "Wu"), Wd = tensor(a[4], "Wd");
     const at::Tensor H = tensor(a[5], "H"), G = tensor(a[6], "G"), U = tensor(a[7], "U");
-    const int act = static_cast<int>(integer(a[8]));
+    const int act = enumerator(a[8]);
     at::Tensor dX = tensor(a[9], "dX"), dWg = tensor(a[10], "dWg"), dWu = tensor(a[11], "dWu"), dWd = tensor(a[12], "dWd"), ws = tensor(a[13], "workspace");
     Call c(X, "X", a[14]);
     const FfnShapes s(c, X, Wg, Wu, Wd);
