@@ -70,13 +70,11 @@ struct Call {
             other_stream = stream != current->stream();
         }
     }
-    // Row-major matrix on this device; returns its leading dimension.
+    // Row-major matrix on this device; returns its leading dimension (of a single row, whose stride says nothing, the columns).
     int64_t matrix(const at::Tensor& t, int64_t rows, int64_t cols, at::ScalarType type, const char* name) const {
         if (t.defined() && t.is_cuda() && t.get_device() == device && t.scalar_type() == type && t.dim() == 2 && t.size(0) == rows && t.size(1) == cols &&
-            (cols <= 1 || t.stride(1) == 1)) {
-            const int64_t ld = t.stride(0);
-            return rows > 1 || ld > cols ? ld : cols;
-        }
+            (cols <= 1 || t.stride(1) == 1))
+            return rows > 1 ? t.stride(0) : cols;
         refuse(c10::str(name, ": a row-major matrix [", rows, ", ", cols, "] of ", type, " on cuda:", int(device), ", got ", told(t)));
     }
     void vector(const at::Tensor& t, int64_t n, at::ScalarType type, const char* name) const {
