@@ -377,6 +377,7 @@ def atb_select_tiling(M: int, N: int, K: int, hw: atb_hw_params_t | None = None,
 # ------------------------------------------------------------------ between the products: norm, feed-forward, loss
 # stream: None (the current one), a torch stream or a handle.  What a call allocates belongs to the stream that it runs on; the
 # caller orders the inputs before it and the use of the results behind it, as between any two streams.
+# Gradients: None (a new tensor), the tensor to write, or False (not wanted, not computed; None comes back in its place).
 ACTIVATIONS = {"silu": 0, "gelu": 1, "gelu_tanh": 2}
 
 
@@ -432,7 +433,7 @@ def atb_layer_norm_backward_workspace_bytes(M: int, N: int) -> int:
 
 
 def atb_layer_norm_backward(dY, X, W, mean, rstd, dX=None, dW=None, dB=None, workspace=None, stream=None):
-    """Gradients ``(dX, dW, dB)`` of ``atb_layer_norm``; dW and dB in W's type (float32 where W is None)."""
+    """Gradients ``(dX, dW, dB)`` of ``atb_layer_norm``; dW and dB in W's type (float32 where W is None).  False: not wanted."""
     return _result((_ops or load_ops()).layer_norm_backward(dY, X, W, mean, rstd, dX, dW, dB, workspace, _raw(stream)))
 
 
@@ -461,7 +462,9 @@ def atb_gated_ffn_backward_workspace_bytes(M: int, D: int, F: int) -> int:
 
 
 def atb_gated_ffn_backward(dY, X, Wg, Wu, Wd, H, G, U, act="silu", dX=None, dWg=None, dWu=None, dWd=None, workspace=None, stream=None):
-    """Gradients ``(dX, dWg, dWu, dWd)`` of ``atb_gated_ffn`` from ``dY`` and the ``H``, ``G``, ``U`` that it saved."""
+    """Gradients ``(dX, dWg, dWu, dWd)`` of ``atb_gated_ffn`` from ``dY`` and the ``H``, ``G``, ``U`` that it saved.
+
+    False: not wanted (dWg and dWu both or neither)."""
     return _result((_ops or load_ops()).gated_ffn_backward(dY, X, Wg, Wu, Wd, H, G, U, _act(act), dX, dWg, dWu, dWd, workspace, _raw(stream)))
 
 
@@ -481,7 +484,9 @@ def atb_linear_cross_entropy_backward_workspace_bytes(M: int, V: int, D: int, pi
 
 
 def atb_linear_cross_entropy_backward(dloss, X, W, labels, lse, ignore_index=-100, dX=None, dW=None, piece=0, workspace=None, stream=None):
-    """Gradients ``(dX, dW)`` (bfloat16) of ``sum(dloss * loss)``; ``piece``: words of the vocabulary per pass (0: chosen)."""
+    """Gradients ``(dX, dW)`` (bfloat16) of ``sum(dloss * loss)``; ``piece``: words of the vocabulary per pass (0: chosen).
+
+    False: not wanted."""
     return _result((_ops or load_ops()).linear_cross_entropy_backward(dloss, X, W, labels, lse, ignore_index, dX, dW, piece, workspace, _raw(stream)))
 
 

@@ -48,6 +48,14 @@ at::Tensor tensor(PyObject* o, const char* name) {
 std::string told(const at::Tensor& t) {
     return t.defined() ? c10::str(t.sizes(), " of ", t.scalar_type(), " on ", t.device(), ", strides ", t.strides()) : std::string("None");
 }
+// A gradient: the tensor to write it to, None for a new one, False where it is not wanted.
+struct Gradient {
+    at::Tensor t;
+    bool wanted;
+    Gradient(PyObject* o, const char* name) : wanted(o != Py_False) {
+        if (wanted) t = tensor(o, name);
+    }
+};
 // The rest of a call: the device of its first matrix, which has to be the current one, its stream, and what it allocates.
 // What a call allocates belongs to the stream that its kernels run on: a block that was freed on another stream may still
 // be read or written there.
@@ -100,6 +108,12 @@ struct Call {
         t = make_result({rows, cols}, type);
         return cols;
     }
+    int64_t out_matrix(Gradient& g, int64_t rows, int64_t cols, at::ScalarType type, const char* name) {
+        return g.wanted ? out_matrix(g.t, rows, cols, type, name) : cols;
+    }
+    void out_vector(Gradient& g, int64_t n, at::ScalarType type, const char* name) {
+        if (g.wanted) out_vector(g.t, n, type, name);
+    }
     void out_vector(at::Tensor& t, int64_t n, at::ScalarType type, const char* name) {
         if (t.defined()) vector(t, n, type, name);
         else t = make_result({n}, type);
@@ -130,11 +144,12 @@ struct Call {
     }
 };
 
-int type_code(const at::Tensor& t, const char* name) {
-    if (t.scalar_type() == at::kFloat) return ATB_F32;
-    if (t.scalar_type() == at::kBFloat16) return ATB_BF16;
-    refuse(c10::str(name, ": float32 or bfloat16, got ", t.scalar_type()));
+int type_code(at::ScalarType type, const char* name) {
+    if (type == at::kFloat) return ATB_F32;
+    if (type == at::kBFloat16) return ATB_BF16;
+    refuse(c10::str(name, ": float32 or bfloat16, got ", type));
 }
+int type_code(const at::Tensor& t, const char* name) { return type_code(t.scalar_type(), name); }
 void* ptr(const at::Tensor& t) { return t.defined() ? t.data_ptr() : nullptr; }
 float* fptr(const at::Tensor& t) { return static_cast<float*>(ptr(t)); }
 int64_t integer(PyObject* o) {
@@ -214,7 +229,8 @@ PyObject* layer_norm_backward(PyObject*, PyObject* const* a, Py_ssize_t n) {
     HANDLE_TH_ERRORS
     expect(n, 10);
     const at::Tensor dY = tensor(a[0], "dY"), X = tensor(a[1], "X"), W = tensor(a[2], "W"), mean = tensor(a[3], "mean"), rstd = tensor(a[4], "rstd");
-    at::Tensor dX = tensor(a[5], "dX"), dW = tensor(a[6], "dW"), dB = tensor(a[7], "dB"), ws = tensor(a[8], "workspace");
+    Gradient dX(a[5], "dX"), dW(a[6], "dW"), dB(a[7], "dB");
+    at::Tensor ws = tensor(a[8], "workspace");
     Call c(X, "X", a[9]);
     const int64_t M = X.size(0), N = X.size(1);
     const at::ScalarType type = X.scalar_type(), w_dtype = W.defined() ? W.scalar_type() : at::kFloat;
@@ -226,9 +242,9 @@ PyObject* layer_norm_backward(PyObject*, PyObject* const* a, Py_ssize_t n) {
     const int64_t lddx = c.out_matrix(dX, M, N, type, "dX");
     c.out_vector(dW, N, w_dtype, "dW");
     c.out_vector(dB, N, w_dtype, "dB");
-    const size_t bytes = c.workspace(ws, g_entry.atb_layer_norm_backward_workspace_bytes(M, N));
-    return c.done(g_entry.atb_layer_norm_backward(M, N, x_type, ptr(dY), lddy, ptr(X), ldx, type_code(dW, "W"), ptr(W), fptr(mean), fptr(rstd), ptr(dX), lddx,
-                                                  ptr(dW), ptr(dB), ptr(ws), bytes, c.stream), {dX, dW, dB});
+    const size_t bytes = c.workspace(ws, dW.wanted || dB.wanted ? g_entry.atb_layer_norm_backward_workspace_bytes(M, N) : 0);
+    return c.done(g_entry.atb_layer_norm_backward(M, N, x_type, ptr(dY), lddy, ptr(X), ldx, type_code(w_dtype, "W"), ptr(W), fptr(mean), fptr(rstd), ptr(dX.t), lddx,
+                                                  ptr(dW.t), ptr(dB.t), ptr(ws), bytes, c.stream), {dX.t, dW.t, dB.t});
     END_HANDLE_TH_ERRORS
 }
 
@@ -274,7 +290,9 @@ PyObject* gated_ffn_backward(PyObject*, PyObject* const* a, Py_ssize_t n) {
     const at::Tensor dY = tensor(a[0], "dY"), X = tensor(a[1], "X"), Wg = tensor(a[2], "Wg"), Wu = tensor(a[3], "Wu"), Wd = tensor(a[4], "Wd");
     const at::Tensor H = tensor(a[5], "H"), G = tensor(a[6], "G"), U = tensor(a[7], "U");
     const int act = enumerator(a[8]);
-    at::Tensor dX = tensor(a[9], "dX"), dWg = tensor(a[10], "dWg"), dWu = tensor(a[11], "dWu"), dWd = tensor(a[12], "dWd"), ws = tensor(a[13], "workspace");
+    Gradient dX(a[9], "dX"), dWg(a[10], "dWg"), dWu(a[11], "dWu"), dWd(a[12], "dWd");
+    at::Tensor ws = tensor(a[13], "workspace");
+    if (dWg.wanted != dWu.wanted) refuse("dWg and dWu: both or neither");
     Call c(X, "X", a[14]);
     const FfnShapes s(c, X, Wg, Wu, Wd);
     const at::ScalarType bf16 = at::kBFloat16;
@@ -286,8 +304,8 @@ PyObject* gated_ffn_backward(PyObject*, PyObject* const* a, Py_ssize_t n) {
     const int64_t lddwd = c.out_matrix(dWd, s.F, s.D, bf16, "dWd");
     const size_t bytes = c.workspace(ws, g_entry.atb_gated_ffn_backward_workspace_bytes(s.M, s.D, s.F));
     return c.done(g_entry.atb_gated_ffn_backward(s.M, s.D, s.F, act, ptr(dY), lddy, ptr(X), s.ldx, ptr(Wg), ptr(Wu), s.ldw, ptr(Wd), s.ldwd, ptr(H), ptr(G),
-                                                 ptr(U), ptr(dX), lddx, ptr(dWg), ptr(dWu), lddw, ptr(dWd), lddwd, ptr(ws), bytes, c.stream),
-                  {dX, dWg, dWu, dWd});
+                                                 ptr(U), ptr(dX.t), lddx, ptr(dWg.t), ptr(dWu.t), lddw, ptr(dWd.t), lddwd, ptr(ws), bytes, c.stream),
+                  {dX.t, dWg.t, dWu.t, dWd.t});
     END_HANDLE_TH_ERRORS
 }
 
@@ -326,7 +344,8 @@ PyObject* linear_cross_entropy_backward(PyObject*, PyObject* const* a, Py_ssize_
     expect(n, 11);
     const at::Tensor dloss = tensor(a[0], "dloss"), X = tensor(a[1], "X"), W = tensor(a[2], "W"), labels = tensor(a[3], "labels"), lse = tensor(a[4], "lse");
     const int64_t ignore = integer(a[5]), piece = integer(a[8]);
-    at::Tensor dX = tensor(a[6], "dX"), dW = tensor(a[7], "dW"), ws = tensor(a[9], "workspace");
+    Gradient dX(a[6], "dX"), dW(a[7], "dW");
+    at::Tensor ws = tensor(a[9], "workspace");
     Call c(X, "X", a[10]);
     const HeadShapes s(c, X, W, labels);
     c.vector(dloss, s.M, at::kFloat, "dloss");
@@ -334,8 +353,8 @@ PyObject* linear_cross_entropy_backward(PyObject*, PyObject* const* a, Py_ssize_
     const int64_t lddx = c.out_matrix(dX, s.M, s.D, at::kBFloat16, "dX"), lddw = c.out_matrix(dW, s.V, s.D, at::kBFloat16, "dW");
     const size_t bytes = c.workspace(ws, g_entry.atb_linear_cross_entropy_backward_workspace_bytes(s.M, s.V, s.D, piece));
     return c.done(g_entry.atb_linear_cross_entropy_backward(s.M, s.V, s.D, ptr(X), s.ldx, ptr(W), s.ldw, static_cast<const int64_t*>(ptr(labels)), ignore,
-                                                            fptr(lse), fptr(dloss), ptr(dX), lddx, ptr(dW), lddw, piece, ptr(ws), bytes, c.stream),
-                  {dX, dW});
+                                                            fptr(lse), fptr(dloss), ptr(dX.t), lddx, ptr(dW.t), lddw, piece, ptr(ws), bytes, c.stream),
+                  {dX.t, dW.t});
     END_HANDLE_TH_ERRORS
 }
 
