@@ -170,6 +170,22 @@ def _stream_ptr(stream):
     return ctypes.c_void_p(stream.cuda_stream)
 
 
+def _empty(shape, dtype, device, stream):
+    """New memory for a call on ``stream``, from that stream's own: what the current one has freed may still be in use there.  The
+    current stream is recorded, since the caller goes on with the result on it."""
+    import torch
+    if stream is not None:
+        current, handle = torch.cuda.current_stream(device), _raw(stream)
+        if handle != current.cuda_stream:
+            # 0 and 1 are names of the default stream
+            own = torch.cuda.default_stream(device) if handle <= 1 else torch.cuda.ExternalStream(handle, device=device)
+            with torch.cuda.stream(own):
+                t = torch.empty(shape, dtype=dtype, device=device)
+            t.record_stream(current)
+            return t
+    return torch.empty(shape, dtype=dtype, device=device)
+
+
 def _dev_ptr(t):
     return ctypes.c_void_p(t if isinstance(t, int) else t.data_ptr())
 
@@ -210,9 +226,9 @@ def atb_quantize_bfp16(A, mant=None, exp=None, stream=None):
     assert A.is_cuda and A.dtype == torch.float32 and A.dim() == 2 and A.stride(1) == 1
     M, K = A.shape
     if mant is None:
-        mant = torch.empty((M, K), dtype=torch.int8, device=A.device)
+        mant = _empty((M, K), torch.int8, A.device, stream)
     if exp is None:
-        exp = torch.empty(atb_bfp16_exp_bytes(M, K), dtype=torch.uint8, device=A.device)
+        exp = _empty(atb_bfp16_exp_bytes(M, K), torch.uint8, A.device, stream)
     _check(load_library().atb_quantize_bfp16(_dev_ptr(A), M, K, A.stride(0) if M > 1 else max(K, A.stride(0)),
                                               _dev_ptr(mant), _dev_ptr(exp), _stream_ptr(stream)))
     return mant, exp
@@ -222,7 +238,7 @@ def atb_gemm(M, N, K, T_MA, T_MC, T_K, T_N, A_mant, A_exp, B, C=None, ldb=None, 
     """``C[M][N] = dequant(A) @ B``; B, C are bf16 CUDA tensors (row-major).  Returns C."""
     import torch
     if C is None:
-        C = torch.empty((M, N), dtype=torch.bfloat16, device=B.device)
+        C = _empty((M, N), torch.bfloat16, B.device, stream)
     if ldb is None:
         ldb = B.stride(0) if not isinstance(B, int) else N
     if ldc is None:
@@ -245,10 +261,9 @@ def atb_gemm_splitk(M, N, K, T_MA, T_MC, T_K, T_N, A_mant, A_exp, B, splits, wor
     """Split-K ``C[M][N] = dequant(A) @ B``; ``workspace`` is a float32 CUDA tensor (allocated if None)."""
     import torch
     if C is None:
-        C = torch.empty((M, N), dtype=torch.bfloat16, device=B.device)
+        C = _empty((M, N), torch.bfloat16, B.device, stream)
     if workspace is None:
-        workspace = torch.empty(atb_gemm_splitk_workspace_bytes(M, N, T_MC, splits) // 4, dtype=torch.float32,
-                                device=B.device)
+        workspace = _empty(atb_gemm_splitk_workspace_bytes(M, N, T_MC, splits) // 4, torch.float32, B.device, stream)
     if ldb is None:
         ldb = B.stride(0)
     if ldc is None:
@@ -264,9 +279,9 @@ def atb_gemm_bfp16_out(M, N, K, T_MA, T_MC, T_K, T_N, A_mant, A_exp, B, C_mant=N
     an int8 ``[M, N]`` tensor and the exponent plane, both usable as the A operand of the next GEMM."""
     import torch
     if C_mant is None:
-        C_mant = torch.empty((M, N), dtype=torch.int8, device=B.device)
+        C_mant = _empty((M, N), torch.int8, B.device, stream)
     if C_exp is None:
-        C_exp = torch.empty(atb_bfp16_exp_bytes(M, N), dtype=torch.uint8, device=B.device)
+        C_exp = _empty(atb_bfp16_exp_bytes(M, N), torch.uint8, B.device, stream)
     if ldb is None:
         ldb = B.stride(0)
     _check(load_library().atb_gemm_bfp16_out(M, N, K, T_MA, T_MC, T_K, T_N, _dev_ptr(A_mant), _dev_ptr(A_exp), _dev_ptr(B),
@@ -285,15 +300,15 @@ def atb_gemm_config_tiled(config, M, N, K, T_MA, T_MC, T_K, T_N, A, A_exp, Bt_ma
     dev = Bt_mant.device
     if config == 1:
         if C is None:
-            C = torch.empty((M, N), dtype=torch.bfloat16, device=dev)
+            C = _empty((M, N), torch.bfloat16, dev, stream)
         _check(load_library().atb_gemm_config_tiled(1, M, N, K, T_MA, T_MC, T_K, T_N, _dev_ptr(A), None, A.stride(0),
                                                     _dev_ptr(Bt_mant), _dev_ptr(Bt_exp), _dev_ptr(C), None, C.stride(0),
                                                     _stream_ptr(stream)))
         return C
     if C is None:
-        C = torch.empty((M, N), dtype=torch.int8, device=dev)
+        C = _empty((M, N), torch.int8, dev, stream)
     if C_exp is None:
-        C_exp = torch.empty(atb_bfp16_exp_bytes(M, N), dtype=torch.uint8, device=dev)
+        C_exp = _empty(atb_bfp16_exp_bytes(M, N), torch.uint8, dev, stream)
     _check(load_library().atb_gemm_config_tiled(config, M, N, K, T_MA, T_MC, T_K, T_N, _dev_ptr(A),
                                                 _dev_ptr(A_exp) if A_exp is not None else None, K, _dev_ptr(Bt_mant),
                                                 _dev_ptr(Bt_exp), _dev_ptr(C), _dev_ptr(C_exp), N, _stream_ptr(stream)))
@@ -307,14 +322,14 @@ def atb_gemm_config(config, M, N, K, A, A_exp, Bt_mant, Bt_exp, C=None, C_exp=No
     dev = Bt_mant.device
     if config == 1:
         if C is None:
-            C = torch.empty((M, N), dtype=torch.bfloat16, device=dev)
+            C = _empty((M, N), torch.bfloat16, dev, stream)
         _check(load_library().atb_gemm_config(1, M, N, K, _dev_ptr(A), None, A.stride(0), _dev_ptr(Bt_mant), _dev_ptr(Bt_exp),
                                               _dev_ptr(C), None, C.stride(0), _stream_ptr(stream)))
         return C
     if C is None:
-        C = torch.empty((M, N), dtype=torch.int8, device=dev)
+        C = _empty((M, N), torch.int8, dev, stream)
     if C_exp is None:
-        C_exp = torch.empty(atb_bfp16_exp_bytes(M, N), dtype=torch.uint8, device=dev)
+        C_exp = _empty(atb_bfp16_exp_bytes(M, N), torch.uint8, dev, stream)
     _check(load_library().atb_gemm_config(config, M, N, K, _dev_ptr(A), _dev_ptr(A_exp) if A_exp is not None else None, K,
                                           _dev_ptr(Bt_mant), _dev_ptr(Bt_exp), _dev_ptr(C), _dev_ptr(C_exp), N,
                                           _stream_ptr(stream)))
