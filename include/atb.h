@@ -351,6 +351,10 @@ atb_status_t atb_select_tiling(int64_t M, int64_t N, int64_t K, const atb_hw_par
  *   - an output must not overlap an input, another output or the workspace;
  *   - sums, norms' statistics, softmax statistics and losses are FP32; every call with the same arguments
  *     on the same GPU model gives the same bits (no atomics);
+ *   - what is rounded to bf16 on the way: operands that one product makes for the next (H, dG, dU, dL: the tensor
+ *     cores take bf16), and G and U kept for the backward pass (they could be FP32, at twice the memory; the
+ *     gradients are 0.0030 of their norm off instead of 0.0024, rounding the results alone is 0.0017); exponentials and
+ *     reciprocals of the activations and the softmax are the fast instructions (1 to 2 units in the last place of FP32);
  *   - a workspace is device memory, 16-byte aligned, of at least the bytes that the function beside the
  *     operator returns; it is overwritten and may be reused by the next call on the same stream.
  * ===================================================================================================== */
@@ -411,7 +415,8 @@ atb_status_t atb_gated_ffn_backward(int64_t M, int64_t D, int64_t F, int act, co
 /* Softmax cross entropy of a linear head, L = X W^T (M x V), without keeping L:
  *   lse[m] = log sum_v exp(L[m][v]),  loss[m] = lse[m] - L[m][label[m]], 0 where label[m] == ignore_index.
  *   X_dev bf16 [M][ldx], W_dev bf16 [V][ldw] (D columns each), labels_dev int64 [M], loss_dev and lse_dev FP32 [M].
- * A label outside [0, V) that is not ignore_index makes loss and lse of its row NaN (and with them every gradient).
+ * A label outside [0, V) that is not ignore_index makes loss and lse of its row NaN (and with them every gradient): the
+ * labels are on the device, so that no status tells of it; the loss does.
  * M >= 0 (0: nothing is done), V >= 1 (any value), D >= 8 and a multiple of 8.
  * Errors: BAD_SHAPE, NULL_POINTER, MISALIGNED, BUFFER_TOO_SMALL, UNSUPPORTED_DEVICE, CUDA. */
 size_t atb_linear_cross_entropy_workspace_bytes(int64_t M, int64_t V, int64_t D);
@@ -421,6 +426,7 @@ atb_status_t atb_linear_cross_entropy(int64_t M, int64_t V, int64_t D, const voi
 /* Gradients of sum_m dloss[m] * loss[m]:  dL = (exp(L - lse) - onehot(label)) * dloss / unit (bf16; 0 in ignored rows),
  *   dX = unit * dL W, dW = unit * dL^T X (bf16, written; each may be NULL), where unit is the largest finite |dloss| of the
  *   rows that count, so that equal dloss (a mean) are not rounded.  M == 0 writes dW = 0.
+ *   A row that is ignored has dX = 0 whatever is in it, and adds 0 times its X to dW: X has to be finite there too.
  *   L is computed again, `piece` words of the vocabulary at a time (rounded up to whole tiles; 0: the library's choice,
  *   which keeps dL within 512 MB or 2048 words), so that the workspace holds M x piece of dL, FP32 sums of dX
  *   where there is more than one piece, and FP32 sums of products that are split along K to fill the SMs.  Results of different `piece` agree within the rounding of the FP32 sums. */

@@ -9,8 +9,7 @@
 // memory, always in the same order: no second kernel, no workspace, no atomics.
 // Measured: one row through a block of 4096 x 10944 (269 MB of weights) 46 us, 5.8 TB/s, 0.89 of the measured copy rate; the
 // second product's first weights are fetched while the first product drains.  The tensor-core products, with 128 rows of
-// which one is real, take 57 us for it; from three rows on they are ahead (four rows here: 71 us, bound by the registers that
-// the rows' sums take from the loads in flight).
+// which one is real, take 57 us for it; which form takes how many rows, and both measured: kFewRows.
 #include <cooperative_groups.h>
 #include <cuda_bf16.h>
 
@@ -37,7 +36,9 @@ struct FewParams {
 
 // CTAs per SM (launch bounds): what leaves every thread the registers for its loads in flight (32 per matrix) and its sums
 // (8 per row and matrix).  Measured at 4096 x 10944, one row, block of both products: 6 for NW = 1: 46.4 us, 7: 50.4 us, 5: 46.9 us;
-// NW = 2 with 5 instead of 4: 51.2 us, with 3: 53.9 us.
+// NW = 2 with 5 instead of 4: 51.2 us, with 3: 53.9 us.  One fewer of each (5 and 3; 4 for two rows) at other sizes, one row and two:
+// 512 x 1024 6.3 and 6.8 us instead of 6.3 and 7.0, 2048 x 5464 18.6 and 20.2 instead of 17.5 and 19.0, 8192 x 24576 188 and 202
+// instead of 194 and 208; one more spills, and takes 239 us for one row of the last (212 as it is, both on a cold L2).
 constexpr int resident(int MT, int NW) { return NW == 2 ? 4 : MT == 1 ? 6 : 5; }
 
 

@@ -6,8 +6,8 @@
 // Bound by memory: the forward pass reads x and writes y, the backward pass reads dy and x and writes dx, and
 // nothing else of that size moves.  TPR threads share a row, at most kElems elements each, in registers: mean,
 // variance and result take one read.  Blocks stay and walk rows blockIdx.x, + gridDim.x, ...: a thread keeps the same
-// columns, so that w and b are loaded once and dw and db add up in registers, and the next kAhead (3, or 2 of FP32) rows are on their way
-// into shared memory (cp.async) while a row is worked on.  Rows on 16-byte boundaries: a thread copies what it will
+// columns, so that w and b are loaded once and dw and db add up in registers, and the next rows (forward 3 of bf16, 2 of FP32; backward 3 and
+// 2, but 2 of bf16 with 1024 threads and 1 of FP32 with 768) are on their way into shared memory (cp.async) while a row is worked on.  Rows on 16-byte boundaries: a thread copies what it will
 // read itself, so that no barrier is needed.  Other rows are copied in 16-byte pieces all the same, from the boundary below
 // their first element on, and read element by element from there.
 // The variance is summed around means: of a warp's elements around their own mean in registers, and the warps' pairs
@@ -16,10 +16,12 @@
 // where all elements are one number (x r - mu r by one fma is off by the rounding of mu r: 1e-3 for rows of 100).  All sums are FP32.  Rows wider than the widest kernel are read again for every sum (*_wide kernels).
 // Blocks write their sums of dw and db to the workspace, a second kernel adds those up in a fixed order: no atomics,
 // the same bits on every call.
-// Measured (compulsory bytes, of a measured copy rate of 6.55 TB/s): 16384 x 8192 bf16, FP32 weights: forward 94 us, 5.7 TB/s,
+// Measured (compulsory bytes, of a measured copy rate of 6.55 TB/s): 16384 x 8192 bf16, FP32 weights: forward 96 us, 5.6 TB/s,
 // backward 139 us, 5.8 TB/s; 8192 x 8192 FP32: 97 and 132 us, 5.5 and 6.1 TB/s; 8192 x 4096 bf16: 28 and 41 us, 4.8 TB/s;
-// 12265 x 2499 off 16-byte boundaries: FP32 45 and 70 us, 5.5 and 5.3 TB/s, bf16 38 and 57 us, 3.2 and 3.2 TB/s (bound by
+// 12265 x 2499 off 16-byte boundaries: FP32 45 and 70 us, 5.4 and 5.2 TB/s, bf16 39 and 56 us, 3.1 and 3.3 TB/s (bound by
 // instructions: an element at a time; groups of 8 shifted into place on both ways through shared memory took 48 and 73 us).  With one block per row and nothing on its way the first of these took 117 and 268 us.
+// BFP16 planes: 8192 x 4096 from bf16 41 us, 2.6 TB/s, from FP32 47 us, 3.7 TB/s (bound by the block quantiser's instructions).  The *_wide
+// kernels, 4096 x 20000: forward 93 us bf16 (3.5 TB/s), 173 us FP32; backward 343 us for both types, an element at a time.
 #include <cuda_bf16.h>
 #include <cuda_runtime.h>
 
@@ -37,7 +39,7 @@ constexpr int kElems = 16;           // most elements of a row per thread
 // forward with 384 threads, 44.5 us with 512; 65536 rows of 1024 45 us with 64, 57 us with 128 threads of 8 elements.
 constexpr int kThreadCounts[] = {32, 64, 96, 128, 192, 256, 384, 512, 768, 1024};
 // Single elements of a thread that lie inside every row that `tpr` threads get: they need no test against N.  12265 x 2499 bf16 forward
-// 38 instead of 43 us, 131072 x 333 53 instead of 72, 5000 x 12001 backward 129 instead of 164.  (32 threads also take rows
+// 39 instead of 43 us, 131072 x 333 55 instead of 72, 5000 x 12001 backward 128 instead of 164.  (32 threads also take rows
 // of half their elements, in kernels of nv groups that hold no more.)  Groups of 8 need two tests in all, and without the
 // first the compiler kept more alive than 64 registers hold: 16384 x 8192 101 instead of 93 us.
 __host__ __device__ constexpr int full_groups(int tpr, int vec, int nv) {

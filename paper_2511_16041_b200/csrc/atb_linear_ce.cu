@@ -7,9 +7,9 @@
 // Backward: the logits are computed again, a piece of the vocabulary at a time; the epilogue turns them into dl, which
 // the workspace holds for one piece (bf16: it is the operand of the next two products; in units of the largest dloss, see mm_unit).  dW of the piece is complete;
 // dx is added up over the pieces in FP32, in their order, and rounded once.
-// Tensor bound from a few hundred rows on: M = 8192, V = 131072, D = 4096 takes 26 ms for loss and gradients, 8 M V D operations
-// at 1.35 PFLOP/s, which is what the library product sustains under the power cap (1.38); M = 4096, V = 131072, D = 2048, loss
-// alone, 1.6 ms, 1.36 PFLOP/s.  Computing the logits again costs a quarter of that; keeping them would take M x V numbers.
+// Tensor bound from a few hundred rows on: M = 8192, V = 131072, D = 4096 takes 25.6 to 27 ms for loss and gradients, 8 M V D operations
+// at 1.30 to 1.37 PFLOP/s; the library product sustains 1.38 under the power cap.  M = 4096, V = 131072, D = 2048, loss
+// alone, 1.62 to 1.66 ms, 1.32 to 1.36 PFLOP/s.  Computing the logits again costs a quarter of that; keeping them would take M x V numbers.
 // A few rows are bound by reading W: 16 rows, V = 32000, D = 2048 28 us, 4.6 TB/s with both launches.
 #include <cuda_bf16.h>
 
@@ -82,7 +82,8 @@ atb_status_t check_head(int64_t M, int64_t V, int64_t D) {
 bool ld_ok(int64_t ld, int64_t least) { return ld >= least && ld % 8 == 0; }
 size_t align256(size_t n) { return (n + 255) / 256 * 256; }
 
-// Words of a piece: the caller's number rounded up to whole tiles, or (0) as many as keep dl within 512 MB.
+// Words of a piece: the caller's number rounded up to whole tiles, or (0) as many as keep dl within 512 MB, but at least 2048 (more for M
+// above 131072).
 int64_t piece_words(int64_t M, int64_t V, int64_t piece) {
     if (piece <= 0) {
         piece = (1ll << 28) / M / 256 * 256;

@@ -1,5 +1,7 @@
 // Launch of a kernel that may be set up while the kernel before it on the stream drains (programmatic stream serialization):
-// it calls sm100::grid_dependency_wait() before it touches memory.
+// it calls sm100::grid_dependency_wait() before it touches memory.  One exception: the second product of a few rows (few_rows_kernel with
+// weights_settled) fetches weights before that.  The kernel ahead of it is the library's own first product, which does not write them
+// and has itself waited for all before it (its launch_dependents comes behind its wait), so they are settled by then.
 #pragma once
 #include <cuda_runtime.h>
 

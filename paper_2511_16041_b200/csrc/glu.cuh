@@ -27,7 +27,7 @@ __device__ __forceinline__ float rcp_fast(float x) {
 // arithmetic and the fast instructions for exp and 1 / x (1 to 2 ulp and the argument's rounding; the results are rounded to
 // bf16, 2^-9).  Phi(-x) = exp(-x^2 / 2) times a polynomial of degree 8 in t = 1 / (1 + 0.3 x) without a constant term, x >= 0, and
 // Phi(x) = 1 - Phi(-x): the exponential is the one that the slope needs.  The form is that of Abramowitz and Stegun 7.1.26, whose
-// five terms are off by 1.5e-7 of 1, and so by more than bf16's half unit of g Phi(g) below g = -5.5; these eight coefficients
+// five terms are off by 1.5e-7 of 1, and so by more than bf16's half unit of g Phi(g) below g = -4.4; these eight coefficients
 // are a least-squares fit, reweighted to even out the relative error on 0 <= x <= 14, which is 1.5e-7 of Phi(-x) (4.4e-7 in FP32).
 template <int ACT>
 __device__ __forceinline__ void act_value_slope(float2 g, float2& a, float2& slope) {
