@@ -352,8 +352,8 @@ atb_status_t atb_select_tiling(int64_t M, int64_t N, int64_t K, const atb_hw_par
  *   - sums, norms' statistics, softmax statistics and losses are FP32; every call with the same arguments
  *     on the same GPU model gives the same bits (no atomics);
  *   - what is rounded to bf16 on the way: operands that one product makes for the next (H, dG, dU, dL: the tensor
- *     cores take bf16), and G and U kept for the backward pass (they could be FP32, at twice the memory; the
- *     gradients are 0.0030 of their norm off instead of 0.0024, rounding the results alone is 0.0017); exponentials and
+ *     cores take bf16), and, without ATB_KEEP_F32, G and U (half the memory; dX, dWg and dWu are 0.0030 of
+ *     their norm off instead of 0.0024, rounding the results alone is 0.0017); exponentials and
  *     reciprocals of the activations and the softmax are the fast instructions (1 to 2 units in the last place of FP32);
  *   - a workspace is device memory, 16-byte aligned, of at least the bytes that the function beside the
  *     operator returns; it is overwritten and may be reused by the next call on the same stream.
@@ -388,19 +388,21 @@ atb_status_t atb_layer_norm_backward(int64_t M, int64_t N, int x_type, const voi
 
 /* act(g): g * sigmoid(g); g * Phi(g) by erf; g * (1 + tanh(sqrt(2/pi) (g + 0.044715 g^3))) / 2 */
 typedef enum { ATB_ACT_SILU = 0, ATB_ACT_GELU = 1, ATB_ACT_GELU_TANH = 2 } atb_act_t;
+/* Added to act: G and U, which the forward call keeps for the backward one, are FP32 instead of bf16. */
+enum { ATB_KEEP_F32 = 256 };
 
 /* Gated feed-forward block in bf16 with FP32 accumulation: H = act(X Wg) * (X Wu), Y = H Wd.
  *   X_dev [M][ldx] (D columns), Wg_dev and Wu_dev [D][ldw] (F columns; they may be the two halves of one matrix),
  *   Wd_dev [F][ldwd] (D columns), Y_dev [M][ldy];
  *   H_dev bf16 [M][F], written: the rounded product that feeds Wd, which the backward pass needs again;
- *   G_dev, U_dev bf16 [M][F]: X Wg and X Wu for the backward pass, both or neither.
+ *   G_dev, U_dev [M][F]: X Wg and X Wu for the backward pass, both or neither; FP32 with ATB_KEEP_F32, else bf16.
  * M >= 0 (0: nothing is done), D and F >= 8 and multiples of 8.
  * Errors: BAD_ARGUMENT (act), BAD_SHAPE, NULL_POINTER, MISALIGNED, BUFFER_TOO_SMALL, UNSUPPORTED_DEVICE, CUDA. */
 size_t atb_gated_ffn_workspace_bytes(int64_t M, int64_t D, int64_t F);      /* may be 0: no workspace, NULL accepted */
 atb_status_t atb_gated_ffn(int64_t M, int64_t D, int64_t F, int act, const void* X_dev, int64_t ldx, const void* Wg_dev,
                            const void* Wu_dev, int64_t ldw, const void* Wd_dev, int64_t ldwd, void* Y_dev, int64_t ldy,
                            void* H_dev, void* G_dev, void* U_dev, void* workspace_dev, size_t workspace_bytes, void* stream);
-/* Gradients of atb_gated_ffn from dY and what the forward call kept:
+/* Gradients of atb_gated_ffn from dY and what the forward call kept (act with ATB_KEEP_F32 where that had it):
  *   dH = dY Wd^T, dU = dH * act(G), dG = dH * U * act'(G) (rounded to bf16 for the products below),
  *   dX = dG Wg^T + dU Wu^T, dWg = X^T dG, dWu = X^T dU, dWd = H^T dY.
  *   dX_dev [M][lddx]; dWg_dev, dWu_dev [D][lddw]; dWd_dev [F][lddwd]: bf16, written (not added to); dX, dWd and the

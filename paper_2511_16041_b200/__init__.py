@@ -467,7 +467,8 @@ def atb_gated_ffn_workspace_bytes(M: int, D: int, F: int) -> int:
 def atb_gated_ffn(X, Wg, Wu, Wd, act="silu", save=False, Y=None, H=None, G=None, U=None, workspace=None, stream=None):
     """``Y = (act(X Wg) * (X Wu)) Wd`` on bfloat16 matrices ``X [M, D]``, ``Wg``, ``Wu`` ``[D, F]``, ``Wd [F, D]``.
 
-    ``act``: "silu", "gelu" or "gelu_tanh".  Returns Y, or with ``save`` ``(Y, H, G, U)``: what the backward pass takes."""
+    ``act``: "silu", "gelu" or "gelu_tanh".  Returns Y, or with ``save`` ``(Y, H, G, U)``: what the backward pass takes, G and U in
+    float32, or with ``save=torch.bfloat16`` in half the memory (one rounding more in dX, dWg and dWu)."""
     r = _result((_ops or load_ops()).gated_ffn(X, Wg, Wu, Wd, _act(act), save, Y, H, G, U, workspace, _raw(stream)))
     return r if save else r[0]
 

@@ -35,7 +35,7 @@ struct MmProblem {
     int k_segs = 1;                   // 2: C = A[0] x B[0] + A[1] x B[1]
     int n_segs = 1;                   // 2: C[0] = A[0] x B[0], C[1] = A[0] x B[1]  (kMmGlu always has two products)
     MmOperand A[2], B[2];
-    void* C[3] = {nullptr, nullptr, nullptr};   // bf16 outputs; kMmGlu: h, g, u (g and u may be NULL); kMmGluBackward: dg, du
+    void* C[3] = {nullptr, nullptr, nullptr};   // bf16 outputs; kMmGlu: h, g, u (g and u may be NULL, or FP32); kMmGluBackward: dg, du
     int64_t ldc[3] = {0, 0, 0};
     // kMmAccumulate
     float* C32 = nullptr;             // [M][N]
@@ -43,7 +43,8 @@ struct MmProblem {
     const float* factor = nullptr;    // kMmStore, kMmAccumulate: the product is multiplied by *factor where given
     // kMmGlu, kMmGluBackward
     int act = 0;
-    const void *G = nullptr, *U = nullptr;      // [M][N] bf16
+    const void *G = nullptr, *U = nullptr;      // [M][N]
+    bool keep32 = false;              // g and u in memory are FP32, else bf16
     // kMmRowStats, kMmDlogits: columns are the words col0 .. col0 + N - 1
     const int64_t* labels = nullptr;
     int64_t ignore_index = 0, col0 = 0;

@@ -15,10 +15,10 @@
 // their tiles are dealt out as one list, so that one product's last wave is filled by the next one's tiles.  A product
 // of few tiles is cut along K into ranges whose FP32 sums a second kernel joins.
 // Bound by the tensor cores where there are tiles enough, at 4096 x 4096 x 10944 and 4096 x 65536 x 2048 (of a measured 1653
-// TFLOP/s for a lone library product): both projections with the activation and g, u, h written 474 us, 1549 TFLOP/s,
-// tensor pipe 90 % busy; gated backward epilogue 269 us, 1364 TFLOP/s (688 tiles are 9.3 rounds of 74 pairs), 80 %; the gradients
-// behind it in one launch 1223 us, 1500 TFLOP/s under the power cap, 97 %; row statistics of the head 666 us, 1650
-// TFLOP/s, 98 %; softmax gradient 701 us, 1568 TFLOP/s, 93 %.  Bound by memory where rows are few: the head of 60 rows over
+// TFLOP/s for a lone library product): both projections with the activation and g, u, h written 461 us, 1593 TFLOP/s (g and u in
+// FP32: 486 us, 1512); gated backward epilogue 257 us, 1429 TFLOP/s (273 us, 1345; 688 tiles are 9.3 rounds of 74 pairs); the gradients
+// behind it in one launch 1196 us, 1535 TFLOP/s under the power cap; row statistics of the head 666 us, 1650
+// TFLOP/s, tensor pipe 98 % busy; softmax gradient 701 us, 1568 TFLOP/s, 93 %.  Bound by memory where rows are few: the head of 60 rows over
 // 131072 x 2048 words 85 us, 6.35 TB/s.  In between by fill, drain and launch, 4 us per kernel.
 // Tried and dropped: plain coalesced stores instead of TMA stores out of the epilogues' boxes (level, +-1 %), two boxes per warp
 // and five stages (level).
@@ -98,7 +98,7 @@ struct MmJoin {
     MmJoinJob job[kMmGroup];
     int n_jobs, act;
     int64_t all;
-    const __nv_bfloat16 *G, *U;
+    const void *G, *U;
 };
 
 constexpr int kMmPlain = 100;          // kMmStore and kMmAccumulate: one kernel
@@ -138,12 +138,12 @@ __device__ __forceinline__ uint32_t glu_pair(float2 g, float2 u) {
     const float2 h = f32x2::mul2(a, u);
     return pack_bf16(h.x, h.y);
 }
-// dg = dh u act'(g) and du = dh act(g) of two neighbours, g and u packed bf16.
+// dg = dh u act'(g) and du = dh act(g) of two neighbours, packed.
 template <int ACT>
-__device__ __forceinline__ void glu_backward_pair(uint32_t g, uint32_t u, float2 dh, uint32_t& dg, uint32_t& du) {
+__device__ __forceinline__ void glu_backward_pair(float2 g, float2 u, float2 dh, uint32_t& dg, uint32_t& du) {
     float2 a, slope;
-    act_value_slope<ACT>(unpack_bf16(g), a, slope);
-    const float2 x = f32x2::mul2(f32x2::mul2(dh, unpack_bf16(u)), slope), y = f32x2::mul2(dh, a);
+    act_value_slope<ACT>(g, a, slope);
+    const float2 x = f32x2::mul2(f32x2::mul2(dh, u), slope), y = f32x2::mul2(dh, a);
     dg = pack_bf16(x.x, x.y);
     du = pack_bf16(y.x, y.y);
 }
@@ -187,7 +187,7 @@ struct BoxWriter {
             if (4 * i < rows_left) *reinterpret_cast<uint4*>(dst + 4 * i * ld) = v;
         }
     }
-    // The other direction: 64 columns of two inputs into the two boxes, and what becomes of them out of the same boxes.
+    // The other direction: 64 bf16 or 32 FP32 columns of two inputs into the two boxes, and what becomes of them out of the same boxes.
     __device__ __forceinline__ void fetch(const CUtensorMap* m0, const CUtensorMap* m1, int64_t col, int64_t row0) {
         if (lane == 0) {
             tma_store_wait_read<0>();
@@ -210,6 +210,19 @@ struct BoxWriter {
         for (int j = 0; j < 4; ++j)
             asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(v[4 * j]), "=r"(v[4 * j + 1]), "=r"(v[4 * j + 2]), "=r"(v[4 * j + 3])
                          : "r"(row + ((static_cast<uint32_t>(4 * part + j) ^ sw) << 4)) : "memory");
+    }
+    // This lane's row, 32 FP32 columns.
+    __device__ __forceinline__ void read_row(int b, uint32_t (&v)[32]) const {
+        const uint32_t row = box(b) + lane * 128, sw = lane & 7;
+#pragma unroll
+        for (int j = 0; j < 8; ++j)
+            asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(v[4 * j]), "=r"(v[4 * j + 1]), "=r"(v[4 * j + 2]), "=r"(v[4 * j + 3])
+                         : "r"(row + ((static_cast<uint32_t>(j) ^ sw) << 4)) : "memory");
+    }
+    // Between reads of the boxes and the next fetch, where no write stands between.
+    __device__ __forceinline__ void rows_read() const {
+        fence_proxy_async_smem();
+        __syncwarp();
     }
     __device__ __forceinline__ void put_in_place(const CUtensorMap* map, const uint32_t (&o)[32], int64_t col, int64_t row0) {
         write(next, o);
@@ -264,7 +277,7 @@ __device__ __forceinline__ float mm_unit(const MmParams& p, uint32_t boxes, uint
 // ------------------------------------------------------------------------------------------ epilogue of one warp
 // Rows row0 .. row0 + 31 (one per lane); t_addr: the warp's lanes of the tile's accumulator, column 0; half: which of
 // the tile's column groups this warp has, of `cols` columns; col0: first column of the tile in C.
-template <class C, int EPI>
+template <class C, int EPI, bool KEEP32>
 __device__ __forceinline__ void mm_epilogue(const MmMaps<C::JOBS>& tm, const MmParams& p, const MmJob& jb, int c_map, BoxWriter<C::BOXES>& out,
                                             uint32_t t_addr, int half, int64_t row0, int64_t col0, int cols, int split, float unit, int lane, const Ctx& cx) {
     const int64_t row = row0 + lane;
@@ -303,54 +316,101 @@ __device__ __forceinline__ void mm_epilogue(const MmMaps<C::JOBS>& tm, const MmP
         }
     } else if constexpr (EPI == atb::kMmGlu) {
         // accumulator columns 0 .. TILE_N - 1 hold g, the next TILE_N hold u
+        const bool inside = warp_in && col0 < jb.N;
         with_act(p.act, [&](auto act) {
-            uint32_t h[32], og[32], ou[32];
-#pragma unroll
-            for (int part = 0; part < 2; ++part) {
-                uint32_t g[32], u[32];
+            uint32_t h[32];
+            // 32 columns of both and h of them
+            const auto part_of = [&](int part, uint32_t (&g)[32], uint32_t (&u)[32]) {
                 tmem_ld_32x32b_x32(t_addr + 32 * part, g);
                 tmem_ld_32x32b_x32(t_addr + C::TILE_N + 32 * part, u);
                 tmem_ld_wait_for(g);
                 tmem_ld_wait_for(u);
 #pragma unroll
-                for (int e = 0; e < 16; ++e) {
+                for (int e = 0; e < 16; ++e)
                     h[16 * part + e] = glu_pair<act.value>(make_float2(__uint_as_float(g[2 * e]), __uint_as_float(g[2 * e + 1])),
                                                            make_float2(__uint_as_float(u[2 * e]), __uint_as_float(u[2 * e + 1])));
-                    og[16 * part + e] = pack_bf16(__uint_as_float(g[2 * e]), __uint_as_float(g[2 * e + 1]));
-                    ou[16 * part + e] = pack_bf16(__uint_as_float(u[2 * e]), __uint_as_float(u[2 * e + 1]));
+            };
+            if constexpr (KEEP32) {
+#pragma unroll
+                for (int part = 0; part < 2; ++part) {
+                    uint32_t g[32], u[32];
+                    part_of(part, g, u);
+                    out.put(&tm.c[1], g, col0 + 32 * part, row0, warp_in && col0 + 32 * part < jb.N);
+                    out.put(&tm.c[2], u, col0 + 32 * part, row0, warp_in && col0 + 32 * part < jb.N);
                 }
-            }
-            const bool inside = warp_in && col0 < jb.N;
-            out.put(&tm.c[0], h, col0, row0, inside);
-            if (p.save) {
-                out.put(&tm.c[1], og, col0, row0, inside);
-                out.put(&tm.c[2], ou, col0, row0, inside);
-            }
-        });
-    } else if constexpr (EPI == atb::kMmGluBackward) {
-        // g and u of 64 columns arrive in the two boxes (the first ones fetched before the accumulator was waited for); a lane
-        // replaces its row in them by dg and du
-        if (!warp_in) return;
-        with_act(p.act, [&](auto act) {
-#pragma unroll 1
-            for (int c = 0; c < C::COLS && col0 + c < jb.N; c += 64) {
-                if (c > 0) out.fetch(&tm.c[2], &tm.c[3], col0 + c, row0);
-                if (!out.fetched(cx)) return;
+                out.put(&tm.c[0], h, col0, row0, inside);
+            } else {
                 uint32_t og[32], ou[32];
 #pragma unroll
                 for (int part = 0; part < 2; ++part) {
-                    uint32_t dh[32], g[16], u[16];
-                    tmem_ld_32x32b_x32(t_addr + c + 32 * part, dh);
-                    out.read(0, part, g);
-                    out.read(1, part, u);
-                    tmem_ld_wait_for(dh);
+                    uint32_t g[32], u[32];
+                    part_of(part, g, u);
 #pragma unroll
-                    for (int e = 0; e < 16; ++e)
-                        glu_backward_pair<act.value>(g[e], u[e], make_float2(__uint_as_float(dh[2 * e]), __uint_as_float(dh[2 * e + 1])),
-                                                     og[16 * part + e], ou[16 * part + e]);
+                    for (int e = 0; e < 16; ++e) {
+                        og[16 * part + e] = pack_bf16(__uint_as_float(g[2 * e]), __uint_as_float(g[2 * e + 1]));
+                        ou[16 * part + e] = pack_bf16(__uint_as_float(u[2 * e]), __uint_as_float(u[2 * e + 1]));
+                    }
                 }
-                out.put_in_place(&tm.c[0], og, col0 + c, row0);
-                out.put_in_place(&tm.c[1], ou, col0 + c, row0);
+                out.put(&tm.c[0], h, col0, row0, inside);
+                if (p.save) {
+                    out.put(&tm.c[1], og, col0, row0, inside);
+                    out.put(&tm.c[2], ou, col0, row0, inside);
+                }
+            }
+        });
+    } else if constexpr (EPI == atb::kMmGluBackward) {
+        // g and u of 64 columns (of 32 twice, where they are FP32) arrive in the two boxes, the first ones fetched before the accumulator
+        // was waited for; a lane replaces its row in them by dg and du
+        if (!warp_in) return;
+        with_act(p.act, [&](auto act) {
+            if constexpr (KEEP32) {
+#pragma unroll 1
+                for (int c = 0; c < C::COLS && col0 + c < jb.N; c += 64) {
+                    if (c > 0) out.fetch(&tm.c[2], &tm.c[3], col0 + c, row0);
+                    uint32_t og[32], ou[32];
+#pragma unroll
+                    for (int part = 0; part < 2; ++part) {
+                        uint32_t dh[32], g[32], u[32];
+                        if (!out.fetched(cx)) return;
+                        out.read_row(0, g);
+                        out.read_row(1, u);
+                        if (part == 0) {       // columns past the last one are zeros
+                            out.rows_read();
+                            out.fetch(&tm.c[2], &tm.c[3], col0 + c + 32, row0);
+                        }
+                        tmem_ld_32x32b_x32(t_addr + c + 32 * part, dh);
+                        tmem_ld_wait_for(dh);
+#pragma unroll
+                        for (int e = 0; e < 16; ++e)
+                            glu_backward_pair<act.value>(make_float2(__uint_as_float(g[2 * e]), __uint_as_float(g[2 * e + 1])),
+                                                         make_float2(__uint_as_float(u[2 * e]), __uint_as_float(u[2 * e + 1])),
+                                                         make_float2(__uint_as_float(dh[2 * e]), __uint_as_float(dh[2 * e + 1])),
+                                                         og[16 * part + e], ou[16 * part + e]);
+                    }
+                    out.put_in_place(&tm.c[0], og, col0 + c, row0);
+                    out.put_in_place(&tm.c[1], ou, col0 + c, row0);
+                }
+            } else {
+#pragma unroll 1
+                for (int c = 0; c < C::COLS && col0 + c < jb.N; c += 64) {
+                    if (c > 0) out.fetch(&tm.c[2], &tm.c[3], col0 + c, row0);
+                    if (!out.fetched(cx)) return;
+                    uint32_t og[32], ou[32];
+#pragma unroll
+                    for (int part = 0; part < 2; ++part) {
+                        uint32_t dh[32], g[16], u[16];
+                        tmem_ld_32x32b_x32(t_addr + c + 32 * part, dh);
+                        out.read(0, part, g);
+                        out.read(1, part, u);
+                        tmem_ld_wait_for(dh);
+#pragma unroll
+                        for (int e = 0; e < 16; ++e)
+                            glu_backward_pair<act.value>(unpack_bf16(g[e]), unpack_bf16(u[e]), make_float2(__uint_as_float(dh[2 * e]), __uint_as_float(dh[2 * e + 1])),
+                                                         og[16 * part + e], ou[16 * part + e]);
+                    }
+                    out.put_in_place(&tm.c[0], og, col0 + c, row0);
+                    out.put_in_place(&tm.c[1], ou, col0 + c, row0);
+                }
             }
         });
     } else if constexpr (EPI == atb::kMmRowStats) {
@@ -469,7 +529,9 @@ __device__ __forceinline__ MmItem mm_item(const MmParams& p, int item) {
     return w;
 }
 
-template <bool PAIR, int EPI>
+// KEEP32 (kMmGlu, kMmGluBackward): g and u are FP32 in memory.  A kernel of its own: with both forms in one, their code, which a launch
+// finds in no cache after other kernels, took 6 us more of each launch.
+template <bool PAIR, int EPI, bool KEEP32>
 __global__ void __launch_bounds__(kMmThreads, 1)
 bf16_mm_kernel(const __grid_constant__ MmMaps<MmCfg<PAIR, EPI>::JOBS> tm, const __grid_constant__ MmParams p) {
     using C = MmCfg<PAIR, EPI>;
@@ -599,7 +661,7 @@ bf16_mm_kernel(const __grid_constant__ MmMaps<MmCfg<PAIR, EPI>::JOBS> tm, const 
             if (!(ok = wait_bar_t<false, PAIR>(cx, acc_full + 8 * acc, static_cast<uint32_t>(it >> 1) & 1u, 0x201))) break;
             tcgen05_fence_after_sync();
             if (half * C::COLS < tile_n)
-                mm_epilogue<C, EPI>(tm, p, jb, 2 * w.job + w.seg, out, tmem_base + (static_cast<uint32_t>(q * 32) << 16) + static_cast<uint32_t>(acc * C::BN),
+                mm_epilogue<C, EPI, KEEP32>(tm, p, jb, 2 * w.job + w.seg, out, tmem_base + (static_cast<uint32_t>(q * 32) << 16) + static_cast<uint32_t>(acc * C::BN),
                                     half, row0, col0, min(C::COLS, tile_n - half * C::COLS), w.split, unit, lane, cx);
             tcgen05_fence_before_sync();
             __syncwarp();
@@ -647,7 +709,7 @@ bool operand_map(CUtensorMap* m, const atb::MmOperand& o, bool mn_major, int64_t
 
 // Joins the K ranges of split products: sums of the ranges in their order, then what the epilogue would have done.
 // src: [splits][split_rows][cols]; eight columns per thread.
-template <int EPI>
+template <int EPI, bool KEEP32>
 __global__ void __launch_bounds__(256) bf16_mm_join_kernel(const __grid_constant__ MmJoin p) {
     grid_dependency_wait();
     grid_dependency_launch();
@@ -699,7 +761,15 @@ __global__ void __launch_bounds__(256) bf16_mm_join_kernel(const __grid_constant
                 for (int e = 0; e < 4; ++e) o[e] = glu_pair<act.value>(make_float2(v[2 * e], v[2 * e + 1]), make_float2(u[2 * e], u[2 * e + 1]));
             });
             put(q.C[0], m * q.ldc[0] + n, o);
-            if (q.C[1]) {
+            if constexpr (KEEP32) {
+                const auto put32 = [&](void* C, int64_t ld, const float (&f)[8]) {
+                    float4* const dst = reinterpret_cast<float4*>(static_cast<float*>(C) + m * ld + n);
+                    dst[0] = make_float4(f[0], f[1], f[2], f[3]);
+                    dst[1] = make_float4(f[4], f[5], f[6], f[7]);
+                };
+                put32(q.C[1], q.ldc[1], v);
+                put32(q.C[2], q.ldc[2], u);
+            } else if (q.C[1]) {
 #pragma unroll
                 for (int e = 0; e < 4; ++e) o[e] = pack_bf16(v[2 * e], v[2 * e + 1]);
                 put(q.C[1], m * q.ldc[1] + n, o);
@@ -708,12 +778,24 @@ __global__ void __launch_bounds__(256) bf16_mm_join_kernel(const __grid_constant
                 put(q.C[2], m * q.ldc[2] + n, o);
             }
         } else {
-            const uint4 g = *reinterpret_cast<const uint4*>(p.G + m * q.N + n), u = *reinterpret_cast<const uint4*>(p.U + m * q.N + n);
-            const uint32_t gw[4] = {g.x, g.y, g.z, g.w}, uw[4] = {u.x, u.y, u.z, u.w};
+            float2 g[4], u[4];
+            const auto load = [&](const void* src, float2 (&f)[4]) {
+                if constexpr (KEEP32) {
+                    const float4* const at4 = reinterpret_cast<const float4*>(static_cast<const float*>(src) + m * q.N + n);
+                    const float4 a = at4[0], b = at4[1];
+                    f[0] = make_float2(a.x, a.y); f[1] = make_float2(a.z, a.w);
+                    f[2] = make_float2(b.x, b.y); f[3] = make_float2(b.z, b.w);
+                } else {
+                    const uint4 a = *reinterpret_cast<const uint4*>(static_cast<const __nv_bfloat16*>(src) + m * q.N + n);
+                    f[0] = unpack_bf16(a.x); f[1] = unpack_bf16(a.y); f[2] = unpack_bf16(a.z); f[3] = unpack_bf16(a.w);
+                }
+            };
+            load(p.G, g);
+            load(p.U, u);
             uint32_t o2[4];
             with_act(p.act, [&](auto act) {
 #pragma unroll
-                for (int e = 0; e < 4; ++e) glu_backward_pair<act.value>(gw[e], uw[e], make_float2(v[2 * e], v[2 * e + 1]), o[e], o2[e]);
+                for (int e = 0; e < 4; ++e) glu_backward_pair<act.value>(g[e], u[e], make_float2(v[2 * e], v[2 * e + 1]), o[e], o2[e]);
             });
             put(q.C[0], m * q.ldc[0] + n, o);
             put(q.C[1], m * q.ldc[1] + n, o2);
@@ -839,7 +921,7 @@ bool output_map(CUtensorMap* m, const void* base, int64_t N, int64_t M, int64_t 
 }
 
 // One kernel over the n products of q.  EPI == kMmPlain: bf16, FP32, or the sums of K ranges in `partial`.
-template <bool PAIR, int EPI>
+template <bool PAIR, int EPI, bool KEEP32 = false>
 atb_status_t launch(const atb::MmProblem* q, int n, const MmPlan& plan, char* partial, const MmDevice& dev, cudaStream_t stream) {
     using C = MmCfg<PAIR, EPI>;
     MmMaps<C::JOBS> tm;
@@ -900,7 +982,9 @@ atb_status_t launch(const atb::MmProblem* q, int n, const MmPlan& plan, char* pa
             for (int s = 0; s < 4; ++s) {
                 if (!c[s]) { tm.c[s] = s ? tm.c[0] : tm.a[0]; continue; }              // not written: any valid map
                 const int64_t ld = EPI == atb::kMmGluBackward && s >= 2 ? x.N : x.ldc[s];
-                if (!output_map<__nv_bfloat16>(&tm.c[s], c[s], x.N, x.M, ld)) return atb::fail(ATB_ERR_CUDA, "cuTensorMapEncodeTiled failed for C");
+                const bool fp32 = KEEP32 && (EPI == atb::kMmGlu ? s == 1 || s == 2 : s >= 2);        // g and u
+                if (!(fp32 ? output_map<float>(&tm.c[s], c[s], x.N, x.M, ld) : output_map<__nv_bfloat16>(&tm.c[s], c[s], x.N, x.M, ld)))
+                    return atb::fail(ATB_ERR_CUDA, "cuTensorMapEncodeTiled failed for C");
             }
         }
     }
@@ -921,7 +1005,7 @@ atb_status_t launch(const atb::MmProblem* q, int n, const MmPlan& plan, char* pa
     p.unit = q->unit; p.rows = q->M; p.first = q->first;
     const int units = PAIR ? dev.sms / 2 : dev.sms;
     const int n_units = static_cast<int>(items < units ? items : units);
-    auto kernel = bf16_mm_kernel<PAIR, EPI>;
+    auto kernel = bf16_mm_kernel<PAIR, EPI, KEEP32>;
     cudaError_t e = cudaSuccess;
     static std::atomic<uint64_t> allowed{0};         // devices on which this kernel has its shared memory allowed
     const uint64_t bit = 1ull << dev.ordinal;
@@ -935,7 +1019,7 @@ atb_status_t launch(const atb::MmProblem* q, int n, const MmPlan& plan, char* pa
     return ATB_OK;
 }
 
-template <int EPI>
+template <int EPI, bool KEEP32>
 atb_status_t join(const atb::MmProblem* q, int n, const MmPlan& plan, const char* partial, const MmDevice& dev, cudaStream_t stream) {
     MmJoin p = {};
     size_t offset = 0;
@@ -958,22 +1042,22 @@ atb_status_t join(const atb::MmProblem* q, int n, const MmPlan& plan, const char
         offset += partial_bytes(q[j], plan.splits[j]);
     }
     p.act = q->act;
-    p.G = static_cast<const __nv_bfloat16*>(q->G); p.U = static_cast<const __nv_bfloat16*>(q->U);
+    p.G = q->G; p.U = q->U;
     const int64_t blocks = atb::ceil_div(p.all, 256), most = static_cast<int64_t>(dev.sms) * 8;
-    const cudaError_t e = atb::launch_dependent(bf16_mm_join_kernel<EPI>, static_cast<unsigned>(blocks < most ? blocks : most), 256u, 1u, 0, stream, p);
+    const cudaError_t e = atb::launch_dependent(bf16_mm_join_kernel<EPI, KEEP32>, static_cast<unsigned>(blocks < most ? blocks : most), 256u, 1u, 0, stream, p);
     if (e != cudaSuccess) return atb::fail(ATB_ERR_CUDA, "bf16 product join launch: %s", cudaGetErrorString(e));
     return ATB_OK;
 }
 
-template <int EPI>
+template <int EPI, bool KEEP32 = false>
 atb_status_t run(const atb::MmProblem* q, int n, const MmPlan& plan, char* partial, const MmDevice& dev, cudaStream_t stream) {
-    if (!plan.split) return plan.pair ? launch<true, EPI>(q, n, plan, partial, dev, stream) : launch<false, EPI>(q, n, plan, partial, dev, stream);
+    if (!plan.split) return plan.pair ? launch<true, EPI, KEEP32>(q, n, plan, partial, dev, stream) : launch<false, EPI, KEEP32>(q, n, plan, partial, dev, stream);
     if constexpr (EPI == atb::kMmRowStats || EPI == atb::kMmDlogits) {
         return atb::fail(ATB_ERR_BAD_ARGUMENT, "this epilogue takes whole sums");
     } else {
         if (!partial) return atb::fail(ATB_ERR_NULL_POINTER, "a product that is split along K needs room for its sums");
         const atb_status_t s = plan.pair ? launch<true, kMmPlain>(q, n, plan, partial, dev, stream) : launch<false, kMmPlain>(q, n, plan, partial, dev, stream);
-        return s != ATB_OK ? s : join<EPI>(q, n, plan, partial, dev, stream);
+        return s != ATB_OK ? s : join<EPI, KEEP32>(q, n, plan, partial, dev, stream);
     }
 }
 
@@ -1046,8 +1130,8 @@ atb_status_t mm_launch(const MmProblem* q, int n, void* partial, cudaStream_t st
     char* const room = static_cast<char*>(partial);
     switch (q->epilogue) {
         case kMmStore: case kMmAccumulate: return run<kMmPlain>(q, n, plan, room, *dev, stream);
-        case kMmGlu: return run<kMmGlu>(q, n, plan, room, *dev, stream);
-        case kMmGluBackward: return run<kMmGluBackward>(q, n, plan, room, *dev, stream);
+        case kMmGlu: return q->keep32 ? run<kMmGlu, true>(q, n, plan, room, *dev, stream) : run<kMmGlu>(q, n, plan, room, *dev, stream);
+        case kMmGluBackward: return q->keep32 ? run<kMmGluBackward, true>(q, n, plan, room, *dev, stream) : run<kMmGluBackward>(q, n, plan, room, *dev, stream);
         case kMmRowStats: return run<kMmRowStats>(q, n, plan, room, *dev, stream);
         case kMmDlogits: return run<kMmDlogits>(q, n, plan, room, *dev, stream);
     }

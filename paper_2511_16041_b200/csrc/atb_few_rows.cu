@@ -28,9 +28,10 @@ constexpr int kWarps = 4, kThreads = kWarps * 32;
 struct FewParams {
     int64_t K, N, ldx, ldw, ldy;
     const __nv_bfloat16 *x, *w0, *w1;
-    __nv_bfloat16 *y, *g, *u;              // g, u: the two products themselves, or NULL
+    __nv_bfloat16* y;
+    void *g, *u;                           // the two products themselves, FP32 with keep32, else bf16, or NULL
     int64_t ldg;
-    int M, act;
+    int M, act, keep32;
     int weights_settled;                   // the weights are not written by the kernel before this one on the stream
 };
 
@@ -161,9 +162,13 @@ __global__ void __launch_bounds__(kThreads, resident(MT, NW)) few_rows_kernel(co
                     glu::act_value_slope<act.value>(make_float2(v[0], v[0]), a, slope);
                     p.y[m * p.ldy + col0 + c] = __float2bfloat16_rn(a.x * v[NW - 1]);
                 });
-                if (p.g) {
-                    p.g[m * p.ldg + col0 + c] = __float2bfloat16_rn(v[0]);
-                    p.u[m * p.ldg + col0 + c] = __float2bfloat16_rn(v[NW - 1]);
+                const int64_t at = m * p.ldg + col0 + c;
+                if (p.g && p.keep32) {
+                    static_cast<float*>(p.g)[at] = v[0];
+                    static_cast<float*>(p.u)[at] = v[NW - 1];
+                } else if (p.g) {
+                    static_cast<__nv_bfloat16*>(p.g)[at] = __float2bfloat16_rn(v[0]);
+                    static_cast<__nv_bfloat16*>(p.u)[at] = __float2bfloat16_rn(v[NW - 1]);
                 }
             }
         }
@@ -227,12 +232,12 @@ atb_status_t few_rows_product(int64_t M, int64_t K, int64_t N, const void* X, in
 }
 
 atb_status_t few_rows_glu(int64_t M, int64_t K, int64_t N, int act, const void* X, int64_t ldx, const void* Wg, const void* Wu, int64_t ldw, void* H,
-                          void* G, void* U, cudaStream_t stream) {
+                          void* G, void* U, bool keep32, cudaStream_t stream) {
     FewParams p = {};
     p.M = static_cast<int>(M); p.K = K; p.N = N; p.ldx = ldx; p.ldw = ldw; p.ldy = N; p.ldg = N; p.act = act;
     p.x = static_cast<const __nv_bfloat16*>(X);
     p.w0 = static_cast<const __nv_bfloat16*>(Wg); p.w1 = static_cast<const __nv_bfloat16*>(Wu);
-    p.y = static_cast<__nv_bfloat16*>(H); p.g = static_cast<__nv_bfloat16*>(G); p.u = static_cast<__nv_bfloat16*>(U);
+    p.y = static_cast<__nv_bfloat16*>(H); p.g = G; p.u = U; p.keep32 = keep32;
     return run<2>(p, stream);
 }
 

@@ -5,9 +5,9 @@
 //
 // Forward: one kernel for both projections, the activation and the product (x is loaded once for both), one for y.
 // Backward: dh never reaches memory - the epilogue of its product turns it into dg and du; the two products
-// behind dx are one walk over 2 F, and dx and the three weight gradients are one launch.  h, g and u are kept in bf16 between the products: they
-// are (h) or were (the accumulators of g and u, FP32) operands of the tensor cores, which take bf16; the one
-// rounding costs 2^-9 of the value.
+// behind dx are one walk over 2 F, and dx and the three weight gradients are one launch.  h, dg and du are bf16 between the products: they
+// are operands of the tensor cores, which take bf16; the rounding costs 2^-9 of the value.  g and u, which no product takes, are kept
+// as the caller asks: FP32, or bf16 at half the memory (one rounding more in dx, dWg, dWu: 0.0030 of their norm off instead of 0.0024).
 #include <algorithm>
 
 #include "atb_bf16_mm.h"
@@ -17,7 +17,7 @@ namespace {
 
 struct Block {
     int64_t M, D, F;
-    int act;
+    int act;                               // without ATB_KEEP_F32
 };
 
 atb_status_t check_block(const Block& b) {
@@ -61,6 +61,8 @@ extern "C" atb_status_t atb_gated_ffn(int64_t M, int64_t D, int64_t F, int act, 
                                       const void* Wu_dev, int64_t ldw, const void* Wd_dev, int64_t ldwd, void* Y_dev, int64_t ldy,
                                       void* H_dev, void* G_dev, void* U_dev, void* workspace_dev, size_t workspace_bytes, void* stream) {
     atb::clear_error();
+    const bool keep32 = act >= 0 && (act & ATB_KEEP_F32);
+    if (keep32) act &= ~ATB_KEEP_F32;
     atb_status_t s = check_block({M, D, F, act});
     if (s != ATB_OK) return s;
     if (M == 0) return ATB_OK;
@@ -77,12 +79,12 @@ extern "C" atb_status_t atb_gated_ffn(int64_t M, int64_t D, int64_t F, int act, 
     cudaStream_t st = static_cast<cudaStream_t>(stream);
 
     if (M <= atb::kFewRows) {
-        s = atb::few_rows_glu(M, D, F, act, X_dev, ldx, Wg_dev, Wu_dev, ldw, H_dev, G_dev, U_dev, st);
+        s = atb::few_rows_glu(M, D, F, act, X_dev, ldx, Wg_dev, Wu_dev, ldw, H_dev, G_dev, U_dev, keep32, st);
         return s != ATB_OK ? s : atb::few_rows_product(M, F, D, H_dev, F, Wd_dev, ldwd, Y_dev, ldy, true, st);
     }
     atb::MmProblem up;
     up.layout = atb::kMmNN; up.epilogue = atb::kMmGlu;
-    up.M = M; up.N = F; up.K = D; up.act = act;
+    up.M = M; up.N = F; up.K = D; up.act = act; up.keep32 = keep32 && G_dev;
     up.A[0] = {X_dev, ldx}; up.B[0] = {Wg_dev, ldw}; up.B[1] = {Wu_dev, ldw};
     up.C[0] = H_dev; up.C[1] = G_dev; up.C[2] = U_dev;
     up.ldc[0] = up.ldc[1] = up.ldc[2] = F;
@@ -110,6 +112,8 @@ extern "C" atb_status_t atb_gated_ffn_backward(int64_t M, int64_t D, int64_t F, 
                                                void* dWu_dev, int64_t lddw, void* dWd_dev, int64_t lddwd, void* workspace_dev,
                                                size_t workspace_bytes, void* stream) {
     atb::clear_error();
+    const bool keep32 = act >= 0 && (act & ATB_KEEP_F32);
+    if (keep32) act &= ~ATB_KEEP_F32;
     atb_status_t s = check_block({M, D, F, act});
     if (s != ATB_OK) return s;
     if (!dWg_dev != !dWu_dev) return atb::fail(ATB_ERR_NULL_POINTER, "dWg and dWu are written both or neither");
@@ -143,7 +147,7 @@ extern "C" atb_status_t atb_gated_ffn_backward(int64_t M, int64_t D, int64_t F, 
         dh.layout = atb::kMmNT; dh.epilogue = atb::kMmGluBackward;
         dh.M = M; dh.N = F; dh.K = D; dh.act = act;
         dh.A[0] = {dY_dev, lddy}; dh.B[0] = {Wd_dev, ldwd};
-        dh.G = G_dev; dh.U = U_dev;
+        dh.G = G_dev; dh.U = U_dev; dh.keep32 = keep32;
         dh.C[0] = dG; dh.C[1] = dU; dh.ldc[0] = dh.ldc[1] = F;
         s = atb::mm_launch(&dh, 1, partial, st);
         if (s != ATB_OK) return s;

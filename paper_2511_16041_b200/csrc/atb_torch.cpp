@@ -10,6 +10,7 @@
 #include <c10/cuda/CUDAFunctions.h>
 #include <c10/cuda/CUDAGuard.h>
 #include <c10/cuda/CUDAStream.h>
+#include <torch/csrc/Dtype.h>
 #include <torch/csrc/Exceptions.h>
 #include <torch/csrc/autograd/python_variable.h>
 
@@ -157,11 +158,12 @@ int64_t integer(PyObject* o) {
     if (v == -1 && PyErr_Occurred()) throw python_error();
     return v;
 }
-// The number of an enum; what an int does not hold becomes -1, which no enum has.
-int enumerator(PyObject* o) {
+// The number of an activation; what is none, an int's excess or a flag of the entries, becomes -1, which they refuse.
+int activation(PyObject* o) {
     const int64_t v = integer(o);
-    return v == static_cast<int>(v) ? static_cast<int>(v) : -1;
+    return v >= 0 && v < ATB_KEEP_F32 ? static_cast<int>(v) : -1;
 }
+int with_kept(int act, at::ScalarType kept) { return act >= 0 && kept == at::kFloat ? act | ATB_KEEP_F32 : act; }
 bool truth(PyObject* o) {
     const int v = PyObject_IsTrue(o);
     if (v < 0) throw python_error();
@@ -261,24 +263,33 @@ struct FfnShapes {
     }
 };
 
-// (X, Wg, Wu, Wd, act, save, Y, H, G, U, workspace, stream) -> (Y, H, G, U), G and U None where not saved
+// Type of G and U: of those given, which have to agree, else of `fallback`.
+at::ScalarType kept_type(const at::Tensor& G, const at::Tensor& U, at::ScalarType fallback) {
+    const at::ScalarType type = G.defined() ? G.scalar_type() : U.defined() ? U.scalar_type() : fallback;
+    if (type != at::kFloat && type != at::kBFloat16) refuse(c10::str("G and U: float32 or bfloat16, got ", type));
+    return type;
+}
+
+// (X, Wg, Wu, Wd, act, save, Y, H, G, U, workspace, stream) -> (Y, H, G, U), G and U None where not saved; save: a truth value, or the
+// type of G and U
 PyObject* gated_ffn(PyObject*, PyObject* const* a, Py_ssize_t n) {
     HANDLE_TH_ERRORS
     expect(n, 12);
     const at::Tensor X = tensor(a[0], "X"), Wg = tensor(a[1], "Wg"), Wu = tensor(a[2], "Wu"), Wd = tensor(a[3], "Wd");
-    const int act = enumerator(a[4]);
+    const int act = activation(a[4]);
     at::Tensor Y = tensor(a[6], "Y"), H = tensor(a[7], "H"), G = tensor(a[8], "G"), U = tensor(a[9], "U"), ws = tensor(a[10], "workspace");
-    const bool save = truth(a[5]) || G.defined() || U.defined();
+    const bool typed = THPDtype_Check(a[5]), save = typed || truth(a[5]) || G.defined() || U.defined();
+    const at::ScalarType kept = kept_type(G, U, typed ? reinterpret_cast<THPDtype*>(a[5])->scalar_type : at::kFloat);
     Call c(X, "X", a[11]);
     const FfnShapes s(c, X, Wg, Wu, Wd);
     const int64_t ldy = c.out_matrix(Y, s.M, s.D, at::kBFloat16, "Y");
     c.out_contiguous(H, s.M, s.F, at::kBFloat16, "H");
     if (save) {
-        c.out_contiguous(G, s.M, s.F, at::kBFloat16, "G");
-        c.out_contiguous(U, s.M, s.F, at::kBFloat16, "U");
+        c.out_contiguous(G, s.M, s.F, kept, "G");
+        c.out_contiguous(U, s.M, s.F, kept, "U");
     }
     const size_t bytes = c.workspace(ws, g_entry.atb_gated_ffn_workspace_bytes(s.M, s.D, s.F));
-    return c.done(g_entry.atb_gated_ffn(s.M, s.D, s.F, act, ptr(X), s.ldx, ptr(Wg), ptr(Wu), s.ldw, ptr(Wd), s.ldwd, ptr(Y), ldy, ptr(H), ptr(G), ptr(U),
+    return c.done(g_entry.atb_gated_ffn(s.M, s.D, s.F, with_kept(act, kept), ptr(X), s.ldx, ptr(Wg), ptr(Wu), s.ldw, ptr(Wd), s.ldwd, ptr(Y), ldy, ptr(H), ptr(G), ptr(U),
                                         ptr(ws), bytes, c.stream), {Y, H, G, U});
     END_HANDLE_TH_ERRORS
 }
@@ -289,7 +300,7 @@ PyObject* gated_ffn_backward(PyObject*, PyObject* const* a, Py_ssize_t n) {
     expect(n, 15);
     const at::Tensor dY = tensor(a[0], "dY"), X = tensor(a[1], "X"), Wg = tensor(a[2], "Wg"), Wu = tensor(a[3], "Wu"), Wd = tensor(a[4], "Wd");
     const at::Tensor H = tensor(a[5], "H"), G = tensor(a[6], "G"), U = tensor(a[7], "U");
-    const int act = enumerator(a[8]);
+    const int act = activation(a[8]);
     Gradient dX(a[9], "dX"), dWg(a[10], "dWg"), dWu(a[11], "dWu"), dWd(a[12], "dWd");
     at::Tensor ws = tensor(a[13], "workspace");
     if (dWg.wanted != dWu.wanted) refuse("dWg and dWu: both or neither");
@@ -297,13 +308,14 @@ PyObject* gated_ffn_backward(PyObject*, PyObject* const* a, Py_ssize_t n) {
     const FfnShapes s(c, X, Wg, Wu, Wd);
     const at::ScalarType bf16 = at::kBFloat16;
     const int64_t lddy = c.matrix(dY, s.M, s.D, bf16, "dY");
-    if (c.matrix(H, s.M, s.F, bf16, "H") != s.F || c.matrix(G, s.M, s.F, bf16, "G") != s.F || c.matrix(U, s.M, s.F, bf16, "U") != s.F)
+    const at::ScalarType kept = kept_type(G, U, bf16);
+    if (c.matrix(H, s.M, s.F, bf16, "H") != s.F || c.matrix(G, s.M, s.F, kept, "G") != s.F || c.matrix(U, s.M, s.F, kept, "U") != s.F)
         refuse("H, G, U: contiguous");
     const int64_t lddx = c.out_matrix(dX, s.M, s.D, bf16, "dX"), lddw = c.out_matrix(dWg, s.D, s.F, bf16, "dWg");
     if (c.out_matrix(dWu, s.D, s.F, bf16, "dWu") != lddw) refuse("dWg and dWu need the same row stride");
     const int64_t lddwd = c.out_matrix(dWd, s.F, s.D, bf16, "dWd");
     const size_t bytes = c.workspace(ws, g_entry.atb_gated_ffn_backward_workspace_bytes(s.M, s.D, s.F));
-    return c.done(g_entry.atb_gated_ffn_backward(s.M, s.D, s.F, act, ptr(dY), lddy, ptr(X), s.ldx, ptr(Wg), ptr(Wu), s.ldw, ptr(Wd), s.ldwd, ptr(H), ptr(G),
+    return c.done(g_entry.atb_gated_ffn_backward(s.M, s.D, s.F, with_kept(act, kept), ptr(dY), lddy, ptr(X), s.ldx, ptr(Wg), ptr(Wu), s.ldw, ptr(Wd), s.ldwd, ptr(H), ptr(G),
                                                  ptr(U), ptr(dX.t), lddx, ptr(dWg.t), ptr(dWu.t), lddw, ptr(dWd.t), lddwd, ptr(ws), bytes, c.stream),
                   {dX.t, dWg.t, dWu.t, dWd.t});
     END_HANDLE_TH_ERRORS

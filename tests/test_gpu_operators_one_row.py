@@ -25,7 +25,7 @@ def test_one_token(pad):
     x, dy, wd = _row(D, pad), _row(D, pad), torch.randn(F, D, device="cuda").to(BF16)
     wg, wu = (torch.randn(D, F, device="cuda").to(BF16) for _ in range(2))
     keep = [_row(F, pad) for _ in range(3)]                    # H, G, U
-    plain = atb.atb_gated_ffn(x.clone(), wg, wu, wd, save=True)
+    plain = atb.atb_gated_ffn(x.clone(), wg, wu, wd, save=BF16)
     outs = atb.atb_gated_ffn(x, wg, wu, wd, save=True, Y=_row(D, pad), H=keep[0], G=keep[1], U=keep[2])
     _same(outs, plain)
     _same(atb.atb_gated_ffn_backward(dy, x, wg, wu, wd, *outs[1:], dX=_row(D, pad)),
