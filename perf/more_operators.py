@@ -33,29 +33,29 @@ def _sample(name, M, V, dtype, temperature, top_k=0, top_p=1.0, min_p=0.0, per_r
 def listed():
     return [
         # one token through a block's last projection while an answer is written, added to the residual stream: latency, memory
-        _linear("linear, one token", "forward", 1, 10944, 4096, "none", residual=True),
+        _linear("linear: one token", "forward", 1, 10944, 4096, "none", residual=True),
         # FP32 logits of a few answers from a head that is stored word by word, with a bias
-        _linear("linear, logits", "forward", 16, 2048, 32000, "none", out=F32, transposed=True),
+        _linear("linear: logits", "forward", 16, 2048, 32000, "none", out=F32, transposed=True),
         # a prompt of odd length through a block's first projection
-        _linear("linear, prompt", "forward", 509, 2048, 5464, "gelu_tanh", bias=BF16),
+        _linear("linear: prompt", "forward", 509, 2048, 5464, "gelu_tanh", bias=BF16),
         # a training step of one card's batch through a block's first projection
-        _linear("linear, training step", "train", 8192, 4096, 10944, "gelu"),
+        _linear("linear: training step", "train", 8192, 4096, 10944, "gelu"),
         # one token joins the residual stream and is normed again: latency
-        _norm("residual norm, one token", "forward", 1, 4096, BF16, BF16, BF16, "rms", True, False),
+        _norm("residual norm: one token", "forward", 1, 4096, BF16, BF16, BF16, "rms", True, False),
         # prompts through a network that norms a block's result before it is added and after
-        _norm("residual norm, prompts", "forward", 8192, 4096, BF16, BF16, BF16, "rms", False, True),
+        _norm("residual norm: prompts", "forward", 8192, 4096, BF16, BF16, BF16, "rms", False, True),
         # a small model's step with an FP32 stream of odd width, rows a slice of a wider buffer
-        _norm("residual norm, odd training step", "train", 1021, 1001, F32, BF16, F32, "layer", True, True, pad=6),
+        _norm("residual norm: odd training step", "train", 1021, 1001, F32, BF16, F32, "layer", True, True, pad=6),
         # a training step of a wide model with a gate
-        _norm("residual norm, wide training step", "train", 16384, 8192, BF16, BF16, F32, "layer", True, False),
+        _norm("residual norm: wide training step", "train", 16384, 8192, BF16, BF16, F32, "layer", True, False),
         # one answer's next word from a large vocabulary: latency
-        _sample("sample, one answer", 1, 131072, F32, 0.8, top_k=50, top_p=0.95),
+        _sample("sample: one answer", 1, 131072, F32, 0.8, top_k=50, top_p=0.95),
         # a few answers from bf16 logits, where many words tie
-        _sample("sample, few answers", 16, 32000, BF16, 0.7, top_p=0.9),
+        _sample("sample: few answers", 16, 32000, BF16, 0.7, top_p=0.9),
         # a server's batch: every request with its own settings, some of them greedy, an odd vocabulary, forbidden words
-        _sample("sample, batch", 64, 50003, F32, 1.0, top_k=100, top_p=0.95, min_p=0.02, per_row=True, masked=0.1),
+        _sample("sample: batch", 64, 50003, F32, 1.0, top_k=100, top_p=0.95, min_p=0.02, per_row=True, masked=0.1),
         # answers drawn for training
-        _sample("sample, many answers", 512, 131072, F32, 1.0, top_p=0.99),
+        _sample("sample: many answers", 512, 131072, F32, 1.0, top_p=0.99),
     ]
 
 
