@@ -388,6 +388,8 @@ atb_status_t atb_layer_norm_backward(int64_t M, int64_t N, int x_type, const voi
 
 /* act(g): g * sigmoid(g); g * Phi(g) by erf; g * (1 + tanh(sqrt(2/pi) (g + 0.044715 g^3))) / 2 */
 typedef enum { ATB_ACT_SILU = 0, ATB_ACT_GELU = 1, ATB_ACT_GELU_TANH = 2 } atb_act_t;
+/* What the linear layer takes besides: max(z, 0), whose slope at 0 is 0; z itself. */
+enum { ATB_ACT_RELU = 3, ATB_ACT_NONE = 4 };
 /* Added to act: G and U, which the forward call keeps for the backward one, are FP32 instead of bf16. */
 enum { ATB_KEEP_F32 = 256 };
 
@@ -437,6 +439,30 @@ atb_status_t atb_linear_cross_entropy_backward(int64_t M, int64_t V, int64_t D, 
                                                int64_t ldw, const int64_t* labels_dev, int64_t ignore_index, const float* lse_dev,
                                                const float* dloss_dev, void* dX_dev, int64_t lddx, void* dW_dev, int64_t lddw,
                                                int64_t piece, void* workspace_dev, size_t workspace_bytes, void* stream);
+
+/* Linear layer in bf16 with FP32 accumulation: Z = X W + bias, Y = act(Z) + R.
+ *   act: atb_act_t, ATB_ACT_RELU or ATB_ACT_NONE;  y_type: of Y and R;  w_layout: how W is stored (and dW below);
+ *   X_dev bf16 [M][ldx] (K columns);  W_dev bf16, ATB_W_KN: [K][ldw] (N columns), ATB_W_NK: [N][ldw] (K columns);
+ *   bias_dev bias_type [N], or NULL;  R_dev y_type [M][ldr], or NULL;  Y_dev y_type [M][ldy];
+ *   Z_dev z_type [M][N], or NULL: the sums before the activation, which the backward call takes where act is not
+ *   ATB_ACT_NONE.  bf16 puts one rounding more (2^-9 of z) into the slope there.
+ * Nothing is rounded between the accumulator and Y.  M >= 0 (0: nothing is done), K and N >= 8 and multiples of 8; ldr and
+ * ldy multiples of 8 (bf16) or 4 (FP32) elements; every pointer 16-byte aligned.
+ * Errors: BAD_ARGUMENT (act, types, w_layout), BAD_SHAPE, NULL_POINTER, MISALIGNED, BUFFER_TOO_SMALL, UNSUPPORTED_DEVICE, CUDA. */
+enum { ATB_W_KN = 0, ATB_W_NK = 1 };
+size_t atb_linear_workspace_bytes(int64_t M, int64_t K, int64_t N);      /* may be 0: no workspace, NULL accepted */
+atb_status_t atb_linear(int64_t M, int64_t K, int64_t N, int act, int y_type, const void* X_dev, int64_t ldx, int w_layout, const void* W_dev,
+                        int64_t ldw, int bias_type, const void* bias_dev, const void* R_dev, int64_t ldr, void* Y_dev, int64_t ldy,
+                        int z_type, void* Z_dev, void* workspace_dev, size_t workspace_bytes, void* stream);
+/* Gradients of atb_linear from dY (y_type [M][lddy]) and Z (NULL accepted with ATB_ACT_NONE); R's is dY itself:
+ *   dZ = dY * act'(Z) (FP32; rounded to bf16 for the products), dX = dZ W^T, dW = X^T dZ, dbias = sum over rows of dZ.
+ *   dX_dev bf16 [M][lddx]; dW_dev bf16 in W's layout with row stride lddw; dbias_dev bias_type [N]: written (not added to), each
+ *   may be NULL (not wanted); X may be NULL without dW, W without dX.  M == 0 writes dW = dbias = 0. */
+size_t atb_linear_backward_workspace_bytes(int64_t M, int64_t K, int64_t N);
+atb_status_t atb_linear_backward(int64_t M, int64_t K, int64_t N, int act, int y_type, const void* dY_dev, int64_t lddy, const void* X_dev, int64_t ldx,
+                                 int w_layout, const void* W_dev, int64_t ldw, int z_type, const void* Z_dev, void* dX_dev, int64_t lddx,
+                                 void* dW_dev, int64_t lddw, int bias_type, void* dbias_dev, void* workspace_dev, size_t workspace_bytes,
+                                 void* stream);
 
 #ifdef __cplusplus
 }

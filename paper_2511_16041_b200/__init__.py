@@ -80,6 +80,7 @@ EXPORTED_SYMBOLS = [
     "atb_gated_ffn", "atb_gated_ffn_workspace_bytes", "atb_gated_ffn_backward", "atb_gated_ffn_backward_workspace_bytes",
     "atb_linear_cross_entropy", "atb_linear_cross_entropy_workspace_bytes",
     "atb_linear_cross_entropy_backward", "atb_linear_cross_entropy_backward_workspace_bytes",
+    "atb_linear", "atb_linear_workspace_bytes", "atb_linear_backward", "atb_linear_backward_workspace_bytes",
 ]
 
 
@@ -149,7 +150,11 @@ def load_library():
             ("atb_linear_cross_entropy_workspace_bytes", sz, [i64, i64, i64]),
             ("atb_linear_cross_entropy", ci, [i64, i64, i64, vp, i64, vp, i64, vp, i64, vp, vp, vp, sz, vp]),
             ("atb_linear_cross_entropy_backward_workspace_bytes", sz, [i64, i64, i64, i64]),
-            ("atb_linear_cross_entropy_backward", ci, [i64, i64, i64, vp, i64, vp, i64, vp, i64, vp, vp, vp, i64, vp, i64, i64, vp, sz, vp])):
+            ("atb_linear_cross_entropy_backward", ci, [i64, i64, i64, vp, i64, vp, i64, vp, i64, vp, vp, vp, i64, vp, i64, i64, vp, sz, vp]),
+            ("atb_linear_workspace_bytes", sz, [i64, i64, i64]),
+            ("atb_linear", ci, [i64, i64, i64, ci, ci, vp, i64, ci, vp, i64, ci, vp, vp, i64, vp, i64, ci, vp, vp, sz, vp]),
+            ("atb_linear_backward_workspace_bytes", sz, [i64, i64, i64]),
+            ("atb_linear_backward", ci, [i64, i64, i64, ci, ci, vp, i64, vp, i64, ci, vp, i64, ci, vp, vp, i64, vp, i64, ci, vp, vp, sz, vp])):
         fn = getattr(lib, name)
         fn.restype, fn.argtypes = restype, argtypes
     _lib = lib
@@ -504,6 +509,44 @@ def atb_linear_cross_entropy_backward(dloss, X, W, labels, lse, ignore_index=-10
 
     False: not wanted."""
     return _result((_ops or load_ops()).linear_cross_entropy_backward(dloss, X, W, labels, lse, ignore_index, dX, dW, piece, workspace, _raw(stream)))
+
+
+LINEAR_ACTIVATIONS = {**ACTIVATIONS, "relu": 3, "none": 4}
+
+
+def _linear_act(act):
+    if act is None:
+        return LINEAR_ACTIVATIONS["none"]
+    if not isinstance(act, str):
+        return operator.index(act)
+    if act not in LINEAR_ACTIVATIONS:
+        raise ValueError(f"act={act!r}: None or one of {', '.join(LINEAR_ACTIVATIONS)}")
+    return LINEAR_ACTIVATIONS[act]
+
+
+def atb_linear_workspace_bytes(M: int, K: int, N: int) -> int:
+    return int(load_library().atb_linear_workspace_bytes(M, K, N))
+
+
+def atb_linear(X, W, bias=None, act=None, residual=None, dtype=None, save=False, Y=None, Z=None, workspace=None, stream=None):
+    """``Y = act(X W + bias) + residual`` on bfloat16 matrices ``X [M, K]`` and ``W [K, N]`` (row-major, or the transpose of a
+    row-major ``[N, K]``: ``weight.t()``).
+
+    ``act``: None or one of ``LINEAR_ACTIVATIONS``; ``bias [N]``: float32 or bfloat16; Y and ``residual [M, N]``: bfloat16 or float32
+    (``dtype``; where that is None Y's or the residual's type, else bfloat16).  Returns Y, or with ``save`` ``(Y, Z)``: the sums before the activation,
+    which the backward pass takes, in float32, or with ``save=torch.bfloat16`` in half the memory."""
+    r = _result((_ops or load_ops()).linear(X, W, bias, _linear_act(act), residual, dtype, save, Y, Z, workspace, _raw(stream)))
+    return r if r[1] is not None else r[0]
+
+
+def atb_linear_backward_workspace_bytes(M: int, K: int, N: int) -> int:
+    return int(load_library().atb_linear_backward_workspace_bytes(M, K, N))
+
+
+def atb_linear_backward(dY, X, W, Z=None, act=None, dX=None, dW=None, dbias=None, workspace=None, stream=None):
+    """Gradients ``(dX, dW, dbias)`` of ``atb_linear`` from ``dY`` and the ``Z`` that it saved (None without an activation); the
+    residual's is dY.  dW in W's layout, dbias in float32 or the type of the tensor given.  False: not wanted."""
+    return _result((_ops or load_ops()).linear_backward(dY, X, W, Z, _linear_act(act), dX, dW, dbias, workspace, _raw(stream)))
 
 
 # ------------------------------------------------------------------ layout helpers (no arithmetic)

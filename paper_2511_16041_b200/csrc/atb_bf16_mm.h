@@ -1,5 +1,5 @@
-// Internal interface of the BF16 x BF16 product kernels (atb_bf16_mm_sm100.cu), used by the gated feed-forward block and
-// the linear cross entropy.  Not part of the ABI.
+// Internal interface of the BF16 x BF16 product kernels (atb_bf16_mm_sm100.cu), used by the gated feed-forward block, the linear
+// cross entropy and the linear layer.  Not part of the ABI.
 #pragma once
 #include <cuda_runtime.h>
 
@@ -26,6 +26,7 @@ enum MmEpilogue {
     kMmGluBackward = 3,          // the product is dh; with the saved g and u: dg, du
     kMmRowStats = 4,             // per row and group of columns: maximum and sum of exp(c - maximum); the label's c
     kMmDlogits = 5,              // (exp(c - lse) - [column is the label]) * scale / unit (bf16)
+    kMmLinear = 6,               // act(c + bias) + residual; c + bias too where wanted
 };
 
 struct MmProblem {
@@ -35,7 +36,8 @@ struct MmProblem {
     int k_segs = 1;                   // 2: C = A[0] x B[0] + A[1] x B[1]
     int n_segs = 1;                   // 2: C[0] = A[0] x B[0], C[1] = A[0] x B[1]  (kMmGlu always has two products)
     MmOperand A[2], B[2];
-    void* C[3] = {nullptr, nullptr, nullptr};   // bf16 outputs; kMmGlu: h, g, u (g and u may be NULL, or FP32); kMmGluBackward: dg, du
+    void* C[3] = {nullptr, nullptr, nullptr};   // bf16 outputs; kMmGlu: h, g, u (g and u may be NULL, or FP32); kMmGluBackward: dg, du;
+                                                // kMmLinear: the result, and the sum before the activation or NULL
     int64_t ldc[3] = {0, 0, 0};
     // kMmAccumulate
     float* C32 = nullptr;             // [M][N]
@@ -45,6 +47,11 @@ struct MmProblem {
     int act = 0;
     const void *G = nullptr, *U = nullptr;      // [M][N]
     bool keep32 = false;              // g and u in memory are FP32, else bf16
+    // kMmLinear
+    bool y32 = false, z32 = false, bias32 = false;      // result and residual, C[1], bias in FP32, else bf16
+    const void* bias = nullptr;       // [N] or NULL
+    const void* R = nullptr;          // [M][ldr] or NULL
+    int64_t ldr = 0;
     // kMmRowStats, kMmDlogits: columns are the words col0 .. col0 + N - 1
     const int64_t* labels = nullptr;
     int64_t ignore_index = 0, col0 = 0;

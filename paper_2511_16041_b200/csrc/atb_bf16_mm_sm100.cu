@@ -1,4 +1,4 @@
-// BF16 x BF16 products with FP32 accumulation for the gated feed-forward block and the linear cross entropy (sm_100a).
+// BF16 x BF16 products with FP32 accumulation for the gated feed-forward block, the linear cross entropy and the linear layer (sm_100a).
 //
 // C = A x B with either operand stored along K or across it (the three layouts that a layer's forward and backward
 // products need), on tcgen05 with the accumulator in tensor memory, and epilogues that finish the operator's own
@@ -77,10 +77,14 @@ struct MmParams {
     bool first;
     void* dl;                              // kMmDlogits, tiles of any width
     int64_t dl_ld;
+    const void* bias;                      // kMmLinear
+    int bias32, residual, kept;            // kept: 0, kKeptBf16 or kKeptF32
 };
 
+constexpr int kKeptBf16 = 1, kKeptF32 = 2;      // type of the sums before the activation that kMmLinear leaves
+
 // Tensor maps: product j has A at a[2 j], a[2 j + 1] (K segments), B and C alike (segments).  The epilogues of a single product
-// use c[0 .. 3]: h, g, u; dg, du, g, u; dl.
+// use c[0 .. 3]: h, g, u; dg, du, g, u; dl; y, z, r.
 template <int JOBS>
 struct MmMaps {
     CUtensorMap a[2 * JOBS], b[2 * JOBS], c[JOBS == 1 ? 4 : 2 * JOBS];
@@ -99,6 +103,9 @@ struct MmJoin {
     int n_jobs, act;
     int64_t all;
     const void *G, *U;
+    const void *bias, *R;                        // kMmLinear
+    int64_t ldr;
+    int bias32, z32;
 };
 
 constexpr int kMmPlain = 100;          // kMmStore and kMmAccumulate: one kernel
@@ -111,7 +118,8 @@ struct MmCfg {
     static constexpr bool DUAL = EPI == atb::kMmGlu;        // half of the columns from B[0], half from B[1]
     static constexpr int TILE_N = DUAL ? BN / 2 : BN;       // columns of C per tile
     static constexpr int COLS = DUAL ? 64 : BN / 2;         // columns of C of an epilogue warp (a 64-column tile has one group)
-    static constexpr int BOXES = (EPI == atb::kMmGlu || EPI == atb::kMmGluBackward) ? 2 : 1;   // staging boxes of a warp
+    static constexpr int BOXES = (EPI == atb::kMmGlu || EPI == atb::kMmGluBackward || EPI == atb::kMmLinear) ? 2 : 1;   // staging boxes of a warp
+    static constexpr int BOX_BARS = EPI == atb::kMmLinear ? 2 : 1;       // barriers of the loads into them
     static constexpr uint32_t STAGE_BYTES = 2 * kMmTileBytes;
     // Ring of operand stages: 5 or 6, more (single CTAs) where A is a few rows and a stage little more than its B tile
     static constexpr uint32_t BOX_OFF = (BOXES == 2 ? 5 : 6) * STAGE_BYTES;
@@ -119,7 +127,7 @@ struct MmCfg {
     // The tile's width is the launch's (MmParams::tile_n)
     static constexpr bool ANY_WIDTH = !PAIR && (EPI == atb::kMmRowStats || EPI == atb::kMmDlogits);
     static constexpr uint32_t BAR_OFF = BOX_OFF + kMmEpiWarps * BOXES * kEpilogueBoxBytes;
-    static constexpr uint32_t SMEM_BYTES = 1024 + BAR_OFF + 8 * (2 * MOST_STAGES + 4 + kMmEpiWarps) + 16;
+    static constexpr uint32_t SMEM_BYTES = 1024 + BAR_OFF + 8 * (2 * MOST_STAGES + 4 + kMmEpiWarps * BOX_BARS) + 16;
     static_assert(SMEM_BYTES <= kSmemBudget, "shared memory");
 };
 
@@ -203,6 +211,21 @@ struct BoxWriter {
         next = 0;
         return ok;
     }
+    // One input into box b, whose last store has been read (barrier bar + 8 b; bit b of `phase`).
+    __device__ __forceinline__ void fetch_box(int b, const CUtensorMap* m, int64_t col, int64_t row0) {
+        if (lane == 0) {
+            tma_store_wait_read<0>();
+            mbar_arrive_expect_tx(bar + 8 * b, kEpilogueBoxBytes);
+            tma_load_2d(box(b), m, static_cast<int>(col), static_cast<int>(row0), bar + 8 * b);
+        }
+        __syncwarp();
+    }
+    __device__ __forceinline__ bool box_fetched(const Ctx& cx, int b) {
+        const bool ok = wait_bar(cx, bar + 8 * b, (phase >> b) & 1u, 0x203);
+        phase ^= 1u << b;
+        next = b;
+        return ok;
+    }
     // Columns 32 part .. + 31 of this lane's row (packed bf16).
     __device__ __forceinline__ void read(int b, int part, uint32_t (&v)[16]) const {
         const uint32_t row = box(b) + lane * 128, sw = lane & 7;
@@ -272,6 +295,132 @@ __device__ __forceinline__ float mm_unit(const MmParams& p, uint32_t boxes, uint
     if (most == 0.f) most = 1.f;
     if (blockIdx.x == 0 && e == 0 && lane == 0) *p.unit = most;
     return most;
+}
+
+// ------------------------------------------------------------------------------------------ the linear layer's epilogue
+// Values of N columns from col on, for all lanes alike; 0 past the last column and where there is no bias.
+template <int COUNT>
+__device__ __forceinline__ void load_bias(const void* bias, int bias32, int64_t col, int64_t N, float (&b)[COUNT]) {
+#pragma unroll
+    for (int e = 0; e < COUNT; ++e) b[e] = 0.f;
+    if (!bias) return;
+    if (bias32) {
+        const float4* src = reinterpret_cast<const float4*>(static_cast<const float*>(bias) + col);
+#pragma unroll
+        for (int j = 0; j < COUNT / 4; ++j)
+            if (col + 4 * j < N) {
+                const float4 v = __ldg(src + j);
+                b[4 * j] = v.x; b[4 * j + 1] = v.y; b[4 * j + 2] = v.z; b[4 * j + 3] = v.w;
+            }
+    } else {
+        const uint4* src = reinterpret_cast<const uint4*>(static_cast<const __nv_bfloat16*>(bias) + col);
+#pragma unroll
+        for (int j = 0; j < COUNT / 8; ++j)
+            if (col + 8 * j < N) {
+                const uint4 v = __ldg(src + j);
+                const uint32_t w[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    const float2 f = unpack_bf16(w[e]);
+                    b[8 * j + 2 * e] = f.x; b[8 * j + 2 * e + 1] = f.y;
+                }
+            }
+    }
+}
+
+// act(z + bias) + residual of COLS columns of 32 rows.  A piece is a box: 64 bf16 columns or 32 FP32 ones (Y32).  The residual arrives
+// in the boxes in turn, the first two pieces fetched before the accumulator was waited for (linear_fetch), and the result
+// takes its place.  Where the sums before the activation are kept too, those leave through the boxes first, 64 columns at a time, the
+// residual is fetched piece by piece, and the accumulator is read a second time: nothing has to stay in registers in between.
+template <class C, bool Y32>
+__device__ __forceinline__ void linear_fetch(const MmMaps<1>& tm, const MmParams& p, const MmJob& jb, BoxWriter<2>& out, int64_t row0, int64_t col0) {
+    constexpr int PIECE = Y32 ? 32 : 64;
+    if (!p.residual || p.kept || row0 >= jb.M) return;
+#pragma unroll
+    for (int b = 0; b < 2; ++b)
+        if (b * PIECE < C::COLS && col0 + b * PIECE < jb.N) out.fetch_box(b, &tm.c[2], col0 + b * PIECE, row0);
+}
+template <class C, bool Y32>
+__device__ __forceinline__ void linear_epilogue(const MmMaps<1>& tm, const MmParams& p, const MmJob& jb, BoxWriter<2>& out, uint32_t t_addr, int64_t row0,
+                                                int64_t col0, int lane, const Ctx& cx) {
+    constexpr int PIECE = Y32 ? 32 : 64;
+    if (row0 >= jb.M) return;
+    const bool in_place = p.residual && !p.kept;
+    // z of 32 columns
+    const auto sums = [&](int c, uint32_t (&v)[32]) {
+        tmem_ld_32x32b_x32(t_addr + c, v);
+        tmem_ld_wait_for(v);
+        if (!p.bias) return;
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            float bias[8];
+            load_bias(p.bias, p.bias32, col0 + c + 8 * j, jb.N, bias);
+#pragma unroll
+            for (int e = 0; e < 8; ++e) v[8 * j + e] = __float_as_uint(__uint_as_float(v[8 * j + e]) + bias[e]);
+        }
+    };
+    with_linear_act(p.act, [&](auto act) {
+#pragma unroll 1
+        for (int c = 0; c < C::COLS && col0 + c < jb.N; c += PIECE) {
+            const int64_t col = col0 + c;
+            const int b = in_place ? (c / PIECE) & 1 : 0;
+            uint32_t v[32], o[32];
+            if (p.kept && !(c & 32)) {     // columns past the last one are clipped
+#pragma unroll
+                for (int part = 0; part < 2; ++part) {
+                    sums(c + 32 * part, v);
+                    if (p.kept == kKeptF32) {
+                        out.put(&tm.c[1], v, col + 32 * part, row0, col + 32 * part < jb.N);
+                    } else {
+#pragma unroll
+                        for (int e = 0; e < 16; ++e) o[16 * part + e] = pack_bf16(__uint_as_float(v[2 * e]), __uint_as_float(v[2 * e + 1]));
+                    }
+                }
+                if (p.kept == kKeptBf16) out.put(&tm.c[1], o, col, row0, true);
+            }
+            if (p.residual) {
+                if (!in_place) out.fetch_box(0, &tm.c[2], col, row0);
+                if (!out.box_fetched(cx, b)) return;
+            }
+            if constexpr (Y32) {
+                sums(c, v);
+                if (p.residual) out.read_row(b, o);
+                else
+#pragma unroll
+                    for (int e = 0; e < 32; ++e) o[e] = 0u;
+#pragma unroll
+                for (int e = 0; e < 16; ++e) {
+                    const float2 a = f32x2::add2(act_value<act.value>(make_float2(__uint_as_float(v[2 * e]), __uint_as_float(v[2 * e + 1]))),
+                                                 make_float2(__uint_as_float(o[2 * e]), __uint_as_float(o[2 * e + 1])));
+                    o[2 * e] = __float_as_uint(a.x);
+                    o[2 * e + 1] = __float_as_uint(a.y);
+                }
+            } else {
+#pragma unroll
+                for (int part = 0; part < 2; ++part) {
+                    uint32_t r[16];
+                    sums(c + 32 * part, v);
+                    if (p.residual) out.read(b, part, r);
+                    else
+#pragma unroll
+                        for (int e = 0; e < 16; ++e) r[e] = 0u;
+#pragma unroll
+                    for (int e = 0; e < 16; ++e) {
+                        const float2 a = f32x2::add2(act_value<act.value>(make_float2(__uint_as_float(v[2 * e]), __uint_as_float(v[2 * e + 1]))), unpack_bf16(r[e]));
+                        o[16 * part + e] = pack_bf16(a.x, a.y);
+                    }
+                }
+            }
+            if (in_place) {
+                out.put_in_place(&tm.c[0], o, col, row0);
+                // the piece after the next one, into the box that this one leaves
+                if (c + 2 * PIECE < C::COLS && col + 2 * PIECE < jb.N) out.fetch_box(b, &tm.c[2], col + 2 * PIECE, row0);
+            } else {
+                if (p.residual) out.rows_read();
+                out.put(&tm.c[0], o, col, row0, true);
+            }
+        }
+    });
 }
 
 // ------------------------------------------------------------------------------------------ epilogue of one warp
@@ -413,6 +562,8 @@ __device__ __forceinline__ void mm_epilogue(const MmMaps<C::JOBS>& tm, const MmP
                 }
             }
         });
+    } else if constexpr (EPI == atb::kMmLinear) {
+        linear_epilogue<C, KEEP32>(tm, p, jb, out, t_addr, row0, col0, lane, cx);
     } else if constexpr (EPI == atb::kMmRowStats) {
         // columns of this warp inside the vocabulary; the label's, counted from the first
         const int mine = static_cast<int>(min(static_cast<int64_t>(cols), jb.N - col0));
@@ -540,7 +691,7 @@ bf16_mm_kernel(const __grid_constant__ MmMaps<MmCfg<PAIR, EPI>::JOBS> tm, const 
     const uint32_t bar_base = smem_base + C::BAR_OFF;
     const uint32_t full = bar_base, empty = full + 8 * C::MOST_STAGES;
     const uint32_t acc_full = empty + 8 * C::MOST_STAGES, acc_empty = acc_full + 16, box_bar = acc_empty + 16;
-    const uint32_t misc = box_bar + 8 * kMmEpiWarps;       // [0]: TMEM base, [1]: abort flag
+    const uint32_t misc = box_bar + 8 * kMmEpiWarps * C::BOX_BARS;       // [0]: TMEM base, [1]: abort flag
     volatile uint32_t* const misc_gen = reinterpret_cast<volatile uint32_t*>(smem_raw + (misc - smem_u32(smem_raw)));
 
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
@@ -550,7 +701,7 @@ bf16_mm_kernel(const __grid_constant__ MmMaps<MmCfg<PAIR, EPI>::JOBS> tm, const 
     if (threadIdx.x == 0) {
         for (int i = 0; i < C::MOST_STAGES; ++i) { mbar_init(full + 8 * i, 1); mbar_init(empty + 8 * i, 1); }
         for (int i = 0; i < 2; ++i) { mbar_init(acc_full + 8 * i, 1); mbar_init(acc_empty + 8 * i, kMmEpiWarps * (PAIR ? 2 : 1)); }
-        for (int i = 0; i < kMmEpiWarps; ++i) mbar_init(box_bar + 8 * i, 1);
+        for (int i = 0; i < kMmEpiWarps * C::BOX_BARS; ++i) mbar_init(box_bar + 8 * i, 1);
         misc_gen[1] = 0u;
         fence_mbar_init();
         prefetch_tensormap(&tm.a[0]);
@@ -646,7 +797,7 @@ bf16_mm_kernel(const __grid_constant__ MmMaps<MmCfg<PAIR, EPI>::JOBS> tm, const 
     } else {
         // ================================ epilogue ====================================
         const int e = warp - kMmFirstEpiWarp, q = warp & 3, half = e >> 2;
-        BoxWriter<C::BOXES> out(smem_base + C::BOX_OFF + static_cast<uint32_t>(e) * C::BOXES * kEpilogueBoxBytes, box_bar + 8 * e, lane);
+        BoxWriter<C::BOXES> out(smem_base + C::BOX_OFF + static_cast<uint32_t>(e) * C::BOXES * kEpilogueBoxBytes, box_bar + 8 * e * C::BOX_BARS, lane);
         int it = 0;
         bool ok = true;
         float unit = 1.f;
@@ -656,6 +807,7 @@ bf16_mm_kernel(const __grid_constant__ MmMaps<MmCfg<PAIR, EPI>::JOBS> tm, const 
             const MmJob& jb = p.job[w.job];
             const int64_t row0 = static_cast<int64_t>(w.mt) * C::TILE_M + rank * 128 + q * 32, col0 = static_cast<int64_t>(w.nt) * tile_n;
             const int acc = it & 1;
+            if constexpr (EPI == atb::kMmLinear) linear_fetch<C, KEEP32>(tm, p, jb, out, row0, col0 + half * C::COLS);
             if constexpr (EPI == atb::kMmGluBackward)
                 if (row0 < jb.M && col0 + half * C::COLS < jb.N) out.fetch(&tm.c[2], &tm.c[3], col0 + half * C::COLS, row0);
             if (!(ok = wait_bar_t<false, PAIR>(cx, acc_full + 8 * acc, static_cast<uint32_t>(it >> 1) & 1u, 0x201))) break;
@@ -707,6 +859,36 @@ bool operand_map(CUtensorMap* m, const atb::MmOperand& o, bool mn_major, int64_t
                        static_cast<uint64_t>(mn_major ? K : mn), static_cast<uint64_t>(o.ld) * 2, 64, static_cast<uint32_t>(rows), CU_TENSOR_MAP_SWIZZLE_128B);
 }
 
+// Eight values from element `at` on, FP32 or bf16 in memory.
+template <bool F32>
+__device__ __forceinline__ void load8(const void* src, int64_t at, float (&v)[8]) {
+    if constexpr (F32) {
+        const float4* const s = reinterpret_cast<const float4*>(static_cast<const float*>(src) + at);
+        const float4 a = s[0], b = s[1];
+        v[0] = a.x; v[1] = a.y; v[2] = a.z; v[3] = a.w;
+        v[4] = b.x; v[5] = b.y; v[6] = b.z; v[7] = b.w;
+    } else {
+        const uint4 a = *reinterpret_cast<const uint4*>(static_cast<const __nv_bfloat16*>(src) + at);
+        const uint32_t w[4] = {a.x, a.y, a.z, a.w};
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            const float2 f = unpack_bf16(w[e]);
+            v[2 * e] = f.x; v[2 * e + 1] = f.y;
+        }
+    }
+}
+template <bool F32>
+__device__ __forceinline__ void store8(void* dst, int64_t at, const float (&v)[8]) {
+    if constexpr (F32) {
+        float4* const d = reinterpret_cast<float4*>(static_cast<float*>(dst) + at);
+        d[0] = make_float4(v[0], v[1], v[2], v[3]);
+        d[1] = make_float4(v[4], v[5], v[6], v[7]);
+    } else {
+        *reinterpret_cast<uint4*>(static_cast<__nv_bfloat16*>(dst) + at) =
+            make_uint4(pack_bf16(v[0], v[1]), pack_bf16(v[2], v[3]), pack_bf16(v[4], v[5]), pack_bf16(v[6], v[7]));
+    }
+}
+
 // Joins the K ranges of split products: sums of the ranges in their order, then what the epilogue would have done.
 // src: [splits][split_rows][cols]; eight columns per thread.
 template <int EPI, bool KEEP32>
@@ -753,6 +935,25 @@ __global__ void __launch_bounds__(256) bf16_mm_join_kernel(const __grid_constant
                 for (int e = 0; e < 4; ++e) o[e] = pack_bf16(v[2 * e], v[2 * e + 1]);
                 put(q.C[seg], m * q.ldc[seg] + n, o);
             }
+        } else if constexpr (EPI == atb::kMmLinear) {
+            float b[8], r[8] = {};
+            load_bias(p.bias, p.bias32, n, q.N, b);
+            if (p.R) load8<KEEP32>(p.R, m * p.ldr + n, r);
+#pragma unroll
+            for (int e = 0; e < 8; ++e) v[e] += b[e];
+            if (q.C[1]) {
+                if (p.z32) store8<true>(q.C[1], m * q.ldc[1] + n, v);
+                else store8<false>(q.C[1], m * q.ldc[1] + n, v);
+            }
+            with_linear_act(p.act, [&](auto act) {
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    const float2 a = act_value<act.value>(make_float2(v[2 * e], v[2 * e + 1]));
+                    v[2 * e] = a.x + r[2 * e];
+                    v[2 * e + 1] = a.y + r[2 * e + 1];
+                }
+            });
+            store8<KEEP32>(q.C[0], m * q.ldc[0] + n, v);
         } else if constexpr (EPI == atb::kMmGlu) {
             float u[8];
             sum(m, q.N + n, u);
@@ -977,6 +1178,16 @@ atb_status_t launch(const atb::MmProblem* q, int n, const MmPlan& plan, char* pa
                 else ok = output_map<__nv_bfloat16>(m, x.C[s], x.N, x.M, x.ldc[s]);
                 if (!ok) return atb::fail(ATB_ERR_CUDA, "cuTensorMapEncodeTiled failed for C");
             }
+        } else if constexpr (EPI == atb::kMmLinear) {
+            const auto map = [&](int s, const void* base, int64_t ld, bool fp32) {
+                if (!base) { tm.c[s] = tm.c[0]; return true; }                         // not used: any valid map
+                return fp32 ? output_map<float>(&tm.c[s], base, x.N, x.M, ld) : output_map<__nv_bfloat16>(&tm.c[s], base, x.N, x.M, ld);
+            };
+            if (!map(0, x.C[0], x.ldc[0], KEEP32) || !map(1, x.C[1], x.ldc[1], x.z32) || !map(2, x.R, x.ldr, KEEP32))
+                return atb::fail(ATB_ERR_CUDA, "cuTensorMapEncodeTiled failed for C");
+            tm.c[3] = tm.c[0];
+            p.bias = x.bias; p.bias32 = x.bias32; p.residual = x.R != nullptr;
+            p.kept = !x.C[1] ? 0 : x.z32 ? kKeptF32 : kKeptBf16;
         } else {
             const void* const c[4] = {x.C[0], x.C[1], EPI == atb::kMmGluBackward ? x.G : x.C[2], EPI == atb::kMmGluBackward ? x.U : nullptr};
             for (int s = 0; s < 4; ++s) {
@@ -1043,6 +1254,7 @@ atb_status_t join(const atb::MmProblem* q, int n, const MmPlan& plan, const char
     }
     p.act = q->act;
     p.G = q->G; p.U = q->U;
+    p.bias = q->bias; p.bias32 = q->bias32; p.R = q->R; p.ldr = q->ldr; p.z32 = q->z32;
     const int64_t blocks = atb::ceil_div(p.all, 256), most = static_cast<int64_t>(dev.sms) * 8;
     const cudaError_t e = atb::launch_dependent(bf16_mm_join_kernel<EPI, KEEP32>, static_cast<unsigned>(blocks < most ? blocks : most), 256u, 1u, 0, stream, p);
     if (e != cudaSuccess) return atb::fail(ATB_ERR_CUDA, "bf16 product join launch: %s", cudaGetErrorString(e));
@@ -1134,6 +1346,7 @@ atb_status_t mm_launch(const MmProblem* q, int n, void* partial, cudaStream_t st
         case kMmGluBackward: return q->keep32 ? run<kMmGluBackward, true>(q, n, plan, room, *dev, stream) : run<kMmGluBackward>(q, n, plan, room, *dev, stream);
         case kMmRowStats: return run<kMmRowStats>(q, n, plan, room, *dev, stream);
         case kMmDlogits: return run<kMmDlogits>(q, n, plan, room, *dev, stream);
+        case kMmLinear: return q->y32 ? run<kMmLinear, true>(q, n, plan, room, *dev, stream) : run<kMmLinear>(q, n, plan, room, *dev, stream);
     }
     return fail(ATB_ERR_BAD_ARGUMENT, "no product kernel for epilogue %d", static_cast<int>(q->epilogue));
 }

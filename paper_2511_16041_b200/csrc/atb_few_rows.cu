@@ -33,6 +33,11 @@ struct FewParams {
     int64_t ldg;
     int M, act, keep32;
     int weights_settled;                   // the weights are not written by the kernel before this one on the stream
+    // the linear layer's epilogue: y = act(z) + r, z = x W + bias; y and r FP32 with y32
+    const void *bias, *r;
+    int64_t ldr;
+    void *out, *z;                         // z [M][N]
+    int y32, bias32, z32;
 };
 
 // CTAs per SM (launch bounds): what leaves every thread the registers for its loads in flight (32 per matrix) and its sums
@@ -51,7 +56,24 @@ __device__ __forceinline__ uint4 load_stream(const __nv_bfloat16* p) {
     return v;
 }
 
-template <int MT, int NW, int COLS>
+__device__ __forceinline__ float value_at(const void* p, int64_t at, int fp32) {
+    return fp32 ? static_cast<const float*>(p)[at] : __bfloat162float(static_cast<const __nv_bfloat16*>(p)[at]);
+}
+__device__ __forceinline__ void value_to(void* p, int64_t at, int fp32, float v) {
+    if (fp32) static_cast<float*>(p)[at] = v;
+    else static_cast<__nv_bfloat16*>(p)[at] = __float2bfloat16_rn(v);
+}
+// What the linear layer makes of the product v of row m and column n.
+__device__ __forceinline__ void finish_linear(const FewParams& p, int m, int64_t n, float v) {
+    if (p.bias) v += value_at(p.bias, n, p.bias32);
+    if (p.z) value_to(p.z, m * p.N + n, p.z32, v);
+    glu::with_linear_act(p.act, [&](auto act) { v = glu::act_value<act.value>(make_float2(v, v)).x; });
+    if (p.r) v += value_at(p.r, m * p.ldr + n, p.y32);
+    value_to(p.out, m * p.ldy + n, p.y32, v);
+}
+
+// LINEAR (NW = 1): finish_linear instead of a bf16 store.
+template <int MT, int NW, int COLS, bool LINEAR>
 __global__ void __launch_bounds__(kThreads, resident(MT, NW)) few_rows_kernel(const FewParams p) {
     constexpr int LANES = COLS / 8, SUBS = 32 / LANES, ROUND = kWarps * SUBS * 8;      // rows that a CTA takes at a time
     __shared__ __align__(16) float sums[kWarps][MT * NW][COLS];
@@ -154,7 +176,9 @@ __global__ void __launch_bounds__(kThreads, resident(MT, NW)) few_rows_kernel(co
             for (int n = 0; n < NW; ++n) v[n] += s[(n * MT + m) * COLS + c];
         }
         if (col0 + c < p.N) {
-            if constexpr (NW == 1) {
+            if constexpr (LINEAR) {
+                finish_linear(p, m, col0 + c, v[0]);
+            } else if constexpr (NW == 1) {
                 p.y[m * p.ldy + col0 + c] = __float2bfloat16_rn(v[0]);
             } else {
                 glu::with_act(p.act, [&](auto act) {
@@ -174,6 +198,78 @@ __global__ void __launch_bounds__(kThreads, resident(MT, NW)) few_rows_kernel(co
         }
     }
     cluster.sync();                        // nobody leaves while its sums may still be read
+}
+
+// The linear layer with W stored [N][K]: a warp takes kNkCols rows of W, lanes side by side along K, so that 2 kNkCols loads of 16
+// bytes are in flight per thread.  SPLIT: the CTA's warps share one group of rows of W and deal K out among themselves (few
+// columns), else each has its own.  Sums joined in a fixed order, as above.
+constexpr int kNkCols = 4;
+template <int MT, bool SPLIT>
+__global__ void __launch_bounds__(kThreads, 8) few_rows_nk_kernel(const FewParams p) {
+    __shared__ float sums[SPLIT ? kWarps : 1][MT * kNkCols];
+    constexpr int SHARE = SPLIT ? kWarps : 1;
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const int64_t n0 = (SPLIT ? static_cast<int64_t>(blockIdx.x) : static_cast<int64_t>(blockIdx.x) * kWarps + warp) * kNkCols;
+    sm100::grid_dependency_wait();
+    sm100::grid_dependency_launch();
+    float acc[MT][kNkCols] = {};
+    if (n0 < p.N) {                        // N is a multiple of 8, and so of kNkCols
+        constexpr int64_t STEP = 256 * SHARE;
+        const __nv_bfloat16* const w = p.w0 + n0 * p.ldw;
+        const auto take = [&](const uint4 (&wv)[kNkCols], const uint4 (&xv)[MT]) {
+#pragma unroll
+            for (int m = 0; m < MT; ++m) {
+                const uint32_t xw[4] = {xv[m].x, xv[m].y, xv[m].z, xv[m].w};
+#pragma unroll
+                for (int c = 0; c < kNkCols; ++c) {
+                    const uint32_t ww[4] = {wv[c].x, wv[c].y, wv[c].z, wv[c].w};
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) {
+                        acc[m][c] = fmaf(lo(xw[e]), lo(ww[e]), acc[m][c]);
+                        acc[m][c] = fmaf(hi(xw[e]), hi(ww[e]), acc[m][c]);
+                    }
+                }
+            }
+        };
+        const auto load = [&](int64_t k, uint4 (&wv)[kNkCols], uint4 (&xv)[MT]) {
+#pragma unroll
+            for (int c = 0; c < kNkCols; ++c) wv[c] = load_stream(w + c * p.ldw + k);
+#pragma unroll
+            for (int m = 0; m < MT; ++m) xv[m] = __ldg(reinterpret_cast<const uint4*>(p.x + m * p.ldx + k));
+        };
+        int64_t k = (SPLIT ? warp * 256 : 0) + lane * 8;
+        for (; k + STEP < p.K; k += 2 * STEP) {
+            uint4 w0[kNkCols], w1[kNkCols], x0[MT], x1[MT];
+            load(k, w0, x0);
+            load(k + STEP, w1, x1);
+            take(w0, x0);
+            take(w1, x1);
+        }
+        if (k < p.K) {
+            uint4 w0[kNkCols], x0[MT];
+            load(k, w0, x0);
+            take(w0, x0);
+        }
+#pragma unroll
+        for (int m = 0; m < MT; ++m)
+#pragma unroll
+            for (int c = 0; c < kNkCols; ++c)
+#pragma unroll
+                for (int o = 16; o > 0; o >>= 1) acc[m][c] += __shfl_xor_sync(0xFFFFFFFFu, acc[m][c], o);
+    }
+    float v = 0.f;                         // lane i has sum i
+#pragma unroll
+    for (int i = 0; i < MT * kNkCols; ++i)
+        if (lane == i) v = acc[i / kNkCols][i % kNkCols];
+    if constexpr (SPLIT) {
+        if (lane < MT * kNkCols) sums[warp][lane] = v;
+        __syncthreads();
+        if (warp > 0) return;
+        if (lane < MT * kNkCols)
+#pragma unroll
+            for (int i = 1; i < kWarps; ++i) v += sums[i][lane];
+    }
+    if (n0 < p.N && lane < MT * kNkCols) finish_linear(p, lane / kNkCols, n0 + lane % kNkCols, v);
 }
 
 // Columns per cluster and CTAs per cluster: all CTAs resident at once.  An SM draws its share of the memory's rate only with all
@@ -199,20 +295,20 @@ Deal deal(int64_t K, int64_t N, int per_sm, int sms) {
     return best;
 }
 
-template <int MT, int NW>
+template <int MT, int NW, bool LINEAR>
 cudaError_t launch(const FewParams& p, int sms, cudaStream_t stream) {
     const Deal d = deal(p.K, p.N, resident(MT, NW), sms);
     const unsigned grid = static_cast<unsigned>(atb::ceil_div(p.N, d.cols) * d.ranks), ranks = static_cast<unsigned>(d.ranks);
-    return d.cols == 64 ? atb::launch_dependent(few_rows_kernel<MT, NW, 64>, grid, kThreads, ranks, 0, stream, p)
-                        : atb::launch_dependent(few_rows_kernel<MT, NW, 32>, grid, kThreads, ranks, 0, stream, p);
+    return d.cols == 64 ? atb::launch_dependent(few_rows_kernel<MT, NW, 64, LINEAR>, grid, kThreads, ranks, 0, stream, p)
+                        : atb::launch_dependent(few_rows_kernel<MT, NW, 32, LINEAR>, grid, kThreads, ranks, 0, stream, p);
 }
 
-template <int NW>
+template <int NW, bool LINEAR = false>
 atb_status_t run(const FewParams& p, cudaStream_t stream) {
     int sms = 0;
     const atb_status_t s = atb::op_device(&sms);
     if (s != ATB_OK) return s;
-    const cudaError_t e = p.M == 1 ? launch<1, NW>(p, sms, stream) : launch<2, NW>(p, sms, stream);
+    const cudaError_t e = p.M == 1 ? launch<1, NW, LINEAR>(p, sms, stream) : launch<2, NW, LINEAR>(p, sms, stream);
     if (e != cudaSuccess) return atb::fail(ATB_ERR_CUDA, "few-row product launch: %s", cudaGetErrorString(e));
     return ATB_OK;
 }
@@ -229,6 +325,29 @@ atb_status_t few_rows_product(int64_t M, int64_t K, int64_t N, const void* X, in
     p.y = static_cast<__nv_bfloat16*>(Y);
     p.weights_settled = weights_settled;
     return run<1>(p, stream);
+}
+
+atb_status_t few_rows_linear(const MmProblem& q, cudaStream_t stream) {
+    FewParams p = {};
+    p.M = static_cast<int>(q.M); p.K = q.K; p.N = q.N; p.ldx = q.A[0].ld; p.ldw = q.B[0].ld; p.ldy = q.ldc[0]; p.act = q.act;
+    p.x = static_cast<const __nv_bfloat16*>(q.A[0].base); p.w0 = static_cast<const __nv_bfloat16*>(q.B[0].base);
+    p.bias = q.bias; p.bias32 = q.bias32;
+    p.r = q.R; p.ldr = q.ldr;
+    p.out = q.C[0]; p.y32 = q.y32;
+    p.z = q.C[1]; p.z32 = q.z32;
+    if (q.layout == kMmNN) return run<1, true>(p, stream);
+    int sms = 0;
+    const atb_status_t s = op_device(&sms);
+    if (s != ATB_OK) return s;
+    // a group of columns to a warp where those fill the SMs, else to a CTA
+    const int64_t groups = ceil_div(q.N, kNkCols);
+    const bool split = groups < static_cast<int64_t>(sms) * 8 * kWarps;
+    const unsigned grid = static_cast<unsigned>(split ? groups : ceil_div(groups, kWarps));
+    const auto go = [&](auto kernel) { return launch_dependent(kernel, grid, static_cast<unsigned>(kThreads), 1u, 0, stream, p); };
+    const cudaError_t e = p.M == 1 ? (split ? go(few_rows_nk_kernel<1, true>) : go(few_rows_nk_kernel<1, false>))
+                                   : (split ? go(few_rows_nk_kernel<2, true>) : go(few_rows_nk_kernel<2, false>));
+    if (e != cudaSuccess) return fail(ATB_ERR_CUDA, "few-row linear launch: %s", cudaGetErrorString(e));
+    return ATB_OK;
 }
 
 atb_status_t few_rows_glu(int64_t M, int64_t K, int64_t N, int act, const void* X, int64_t ldx, const void* Wg, const void* Wu, int64_t ldw, void* H,

@@ -2,6 +2,7 @@
 #pragma once
 #include <cuda_runtime.h>
 
+#include "atb_bf16_mm.h"
 #include "atb_internal.h"
 
 namespace atb {
@@ -23,6 +24,8 @@ constexpr int64_t kFewRows = 2;
 // M <= kFewRows; the alignment rules of the entry points (16 bytes, leading dimensions, K and N multiples of 8).
 atb_status_t few_rows_product(int64_t M, int64_t K, int64_t N, const void* X, int64_t ldx, const void* W, int64_t ldw, void* Y, int64_t ldy,
                               bool weights_settled, cudaStream_t stream);
+// A product with kMmLinear's epilogue, W in either layout (kMmNN or kMmNT).
+atb_status_t few_rows_linear(const MmProblem& q, cudaStream_t stream);
 atb_status_t few_rows_glu(int64_t M, int64_t K, int64_t N, int act, const void* X, int64_t ldx, const void* Wg, const void* Wu, int64_t ldw, void* H,
                           void* G, void* U, bool keep32, cudaStream_t stream);
 

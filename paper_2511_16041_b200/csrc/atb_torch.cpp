@@ -1,4 +1,4 @@
-// The tensor side of the Python binding of layer norm, the gated feed-forward block and the linear cross entropy: checks,
+// The tensor side of the Python binding of the operators that stand between the products of a network: checks,
 // outputs, workspaces and the call of the C entry point, in one step.  Those calls come many times per layer and, for
 // small sizes, take less time on the GPU than their marshalling does in Python (16 us for a layer norm against 6 here).
 // The entry points of libatb.so are handed in by address (bind), so that this module serves whichever build of the
@@ -26,7 +26,8 @@ namespace {
     X(atb_layer_norm) X(atb_layer_norm_bfp16) X(atb_layer_norm_backward) X(atb_layer_norm_backward_workspace_bytes)     \
     X(atb_gated_ffn) X(atb_gated_ffn_workspace_bytes) X(atb_gated_ffn_backward) X(atb_gated_ffn_backward_workspace_bytes) \
     X(atb_linear_cross_entropy) X(atb_linear_cross_entropy_workspace_bytes) X(atb_linear_cross_entropy_backward)        \
-    X(atb_linear_cross_entropy_backward_workspace_bytes) X(atb_bfp16_exp_bytes)
+    X(atb_linear_cross_entropy_backward_workspace_bytes) X(atb_bfp16_exp_bytes)                                         \
+    X(atb_linear) X(atb_linear_workspace_bytes) X(atb_linear_backward) X(atb_linear_backward_workspace_bytes)
 struct Entries {
 #define ATB_ENTRY(name) decltype(&::name) name = nullptr;
     ATB_ENTRIES(ATB_ENTRY)
@@ -89,6 +90,14 @@ struct Call {
     void vector(const at::Tensor& t, int64_t n, at::ScalarType type, const char* name) const {
         if (!(t.defined() && t.is_cuda() && t.get_device() == device && t.scalar_type() == type && t.dim() == 1 && t.size(0) == n && t.is_contiguous()))
             refuse(c10::str(name, ": a contiguous vector of ", n, " ", type, " on cuda:", int(device), ", got ", told(t)));
+    }
+    // Weights [rows, cols] in either layout: row-major, or the transpose of a row-major [cols, rows].  Returns the stored rows' stride.
+    int64_t weights(const at::Tensor& t, int64_t rows, int64_t cols, const char* name, int* layout) const {
+        if (t.defined() && t.is_cuda() && t.get_device() == device && t.scalar_type() == at::kBFloat16 && t.dim() == 2 && t.size(0) == rows && t.size(1) == cols) {
+            if (cols <= 1 || t.stride(1) == 1) { *layout = ATB_W_KN; return rows > 1 ? t.stride(0) : cols; }
+            if (rows <= 1 || t.stride(0) == 1) { *layout = ATB_W_NK; return cols > 1 ? t.stride(1) : rows; }
+        }
+        refuse(c10::str(name, ": a matrix [", rows, ", ", cols, "] of BFloat16 on cuda:", int(device), " whose rows or columns are contiguous, got ", told(t)));
     }
     at::Tensor make(at::IntArrayRef size, at::ScalarType type) const {
         const auto options = at::TensorOptions().dtype(type).device(c10::Device(c10::kCUDA, device));
@@ -370,6 +379,84 @@ PyObject* linear_cross_entropy_backward(PyObject*, PyObject* const* a, Py_ssize_
     END_HANDLE_TH_ERRORS
 }
 
+// ---------------------------------------------------------------------------------- linear layer
+at::ScalarType row_type(const at::Tensor& t, const char* name) {
+    type_code(t, name);
+    return t.scalar_type();
+}
+int vector_type(const Call& c, const at::Tensor& t, int64_t n, const char* name) {
+    if (!t.defined()) return ATB_F32;
+    const int code = type_code(t, name);
+    c.vector(t, n, t.scalar_type(), name);
+    return code;
+}
+
+// (X, W, bias, act, residual, dtype, save, Y, Z, workspace, stream) -> (Y, Z), Z None where not saved; dtype: None, or Y's type; save: a
+// truth value, or the type of Z
+PyObject* linear(PyObject*, PyObject* const* a, Py_ssize_t n) {
+    HANDLE_TH_ERRORS
+    expect(n, 11);
+    const at::Tensor X = tensor(a[0], "X"), W = tensor(a[1], "W"), bias = tensor(a[2], "bias"), R = tensor(a[4], "residual");
+    const int act = activation(a[3]);
+    at::Tensor Y = tensor(a[7], "Y"), Z = tensor(a[8], "Z"), ws = tensor(a[9], "workspace");
+    if (a[5] != Py_None && !THPDtype_Check(a[5])) refuse("dtype: a torch type or None");
+    const bool typed = THPDtype_Check(a[6]), save = typed || truth(a[6]) || Z.defined();
+    Call c(X, "X", a[10]);
+    if (!W.defined() || W.dim() != 2) refuse(c10::str("W: a matrix, got ", told(W)));
+    const int64_t M = X.size(0), K = X.size(1), N = W.size(1);
+    const at::ScalarType y_type = a[5] != Py_None ? reinterpret_cast<THPDtype*>(a[5])->scalar_type : Y.defined() ? Y.scalar_type() : R.defined() ? R.scalar_type() : at::kBFloat16;
+    const at::ScalarType z_type = typed ? reinterpret_cast<THPDtype*>(a[6])->scalar_type : Z.defined() ? Z.scalar_type() : at::kFloat;
+    const int y_code = type_code(y_type, "Y"), z_code = type_code(z_type, "Z");
+    int layout = 0;
+    const int64_t ldx = c.matrix(X, M, K, at::kBFloat16, "X"), ldw = c.weights(W, K, N, "W", &layout);
+    const int bias_code = vector_type(c, bias, N, "bias");
+    const int64_t ldr = R.defined() ? c.matrix(R, M, N, y_type, "residual") : N, ldy = c.out_matrix(Y, M, N, y_type, "Y");
+    if (save) c.out_contiguous(Z, M, N, z_type, "Z");
+    const size_t bytes = c.workspace(ws, g_entry.atb_linear_workspace_bytes(M, K, N));
+    return c.done(g_entry.atb_linear(M, K, N, act, y_code, ptr(X), ldx, layout, ptr(W), ldw, bias_code, ptr(bias), ptr(R), ldr, ptr(Y), ldy, z_code, ptr(Z), ptr(ws),
+                                     bytes, c.stream), {Y, Z});
+    END_HANDLE_TH_ERRORS
+}
+
+// (dY, X, W, Z, act, dX, dW, dbias, workspace, stream) -> (dX, dW, dbias)
+PyObject* linear_backward(PyObject*, PyObject* const* a, Py_ssize_t n) {
+    HANDLE_TH_ERRORS
+    expect(n, 10);
+    const at::Tensor dY = tensor(a[0], "dY"), X = tensor(a[1], "X"), W = tensor(a[2], "W"), Z = tensor(a[3], "Z");
+    const int act = activation(a[4]);
+    Gradient dX(a[5], "dX"), dW(a[6], "dW"), db(a[7], "dbias");
+    at::Tensor ws = tensor(a[8], "workspace");
+    Call c(X, "X", a[9]);
+    if (!W.defined() || W.dim() != 2) refuse(c10::str("W: a matrix, got ", told(W)));
+    const int64_t M = X.size(0), K = X.size(1), N = W.size(1);
+    int layout = 0, w_layout = 0;
+    const int64_t ldx = c.matrix(X, M, K, at::kBFloat16, "X"), ldw = c.weights(W, K, N, "W", &w_layout);
+    if (!dY.defined()) refuse("dY: a matrix, got None");
+    const at::ScalarType y_type = row_type(dY, "dY");
+    const int64_t lddy = c.matrix(dY, M, N, y_type, "dY");
+    int z_code = ATB_F32;
+    if (Z.defined()) {
+        z_code = type_code(Z, "Z");
+        if (c.matrix(Z, M, N, Z.scalar_type(), "Z") != N) refuse("Z: contiguous");
+    }
+    const int64_t lddx = c.out_matrix(dX, M, K, at::kBFloat16, "dX");
+    int64_t lddw = w_layout == ATB_W_KN ? N : K;
+    if (dW.wanted) {
+        if (dW.t.defined()) {
+            lddw = c.weights(dW.t, K, N, "dW", &layout);
+            if (layout != w_layout) refuse("dW: in W's layout");
+        } else {
+            dW.t = w_layout == ATB_W_KN ? c.make_result({K, N}, at::kBFloat16) : c.make_result({N, K}, at::kBFloat16).t();
+        }
+    }
+    const at::ScalarType b_type = db.t.defined() ? row_type(db.t, "dbias") : at::kFloat;
+    c.out_vector(db, N, b_type, "dbias");
+    const size_t bytes = c.workspace(ws, g_entry.atb_linear_backward_workspace_bytes(M, K, N));
+    return c.done(g_entry.atb_linear_backward(M, K, N, act, type_code(y_type, "dY"), ptr(dY), lddy, ptr(X), ldx, w_layout, ptr(W), ldw, z_code, ptr(Z), ptr(dX.t), lddx,
+                                              ptr(dW.t), lddw, type_code(b_type, "dbias"), ptr(db.t), ptr(ws), bytes, c.stream), {dX.t, dW.t, db.t});
+    END_HANDLE_TH_ERRORS
+}
+
 // (name, address) of an entry point of the library
 PyObject* bind(PyObject*, PyObject* const* a, Py_ssize_t n) {
     HANDLE_TH_ERRORS
@@ -387,7 +474,7 @@ PyObject* bind(PyObject*, PyObject* const* a, Py_ssize_t n) {
 
 #define ATB_METHOD(name) {#name, reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(name)), METH_FASTCALL, nullptr}
 PyMethodDef g_methods[] = {ATB_METHOD(layer_norm), ATB_METHOD(layer_norm_bfp16), ATB_METHOD(layer_norm_backward), ATB_METHOD(gated_ffn),
-                           ATB_METHOD(gated_ffn_backward), ATB_METHOD(linear_cross_entropy), ATB_METHOD(linear_cross_entropy_backward), ATB_METHOD(bind),
+                           ATB_METHOD(gated_ffn_backward), ATB_METHOD(linear_cross_entropy), ATB_METHOD(linear_cross_entropy_backward), ATB_METHOD(linear), ATB_METHOD(linear_backward), ATB_METHOD(bind),
                            {nullptr, nullptr, 0, nullptr}};
 PyModuleDef g_module = {PyModuleDef_HEAD_INIT, "_atb_torch", nullptr, -1, g_methods, nullptr, nullptr, nullptr, nullptr};
 

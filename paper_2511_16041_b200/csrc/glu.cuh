@@ -1,4 +1,4 @@
-// Activations of the gated feed-forward block and their slopes, in registers.
+// Activations of the gated feed-forward block and the linear layer and their slopes, in registers.
 #pragma once
 #include <cuda_runtime.h>
 
@@ -62,6 +62,34 @@ __device__ __forceinline__ void act_value_slope(float2 g, float2& a, float2& slo
         a = mul2(g, s);
         slope = fma2(mul2(a, fma2(q, both(2.f * c * 0.134145f), both(2.f * c))), fma2(s, both(-1.f), one), s);
     }
+}
+// The same with relu and none at all, which only the linear layer takes.
+template <int ACT>
+__device__ __forceinline__ void linear_act(float2 z, float2& a, float2& slope) {
+    if constexpr (ACT == ATB_ACT_NONE) {
+        a = z;
+        slope = f32x2::both(1.f);
+    } else if constexpr (ACT == ATB_ACT_RELU) {
+        // NaN stays NaN
+        a = make_float2(z.x < 0.f ? 0.f : z.x, z.y < 0.f ? 0.f : z.y);
+        slope = make_float2(z.x > 0.f ? 1.f : 0.f, z.y > 0.f ? 1.f : 0.f);
+    } else {
+        act_value_slope<ACT>(z, a, slope);
+    }
+}
+template <int ACT>
+__device__ __forceinline__ float2 act_value(float2 z) {
+    float2 a, slope;
+    linear_act<ACT>(z, a, slope);
+    return a;
+}
+template <class F>
+__device__ __forceinline__ void with_linear_act(int act, F&& f) {
+    if (act == ATB_ACT_NONE) f(std::integral_constant<int, ATB_ACT_NONE>());
+    else if (act == ATB_ACT_RELU) f(std::integral_constant<int, ATB_ACT_RELU>());
+    else if (act == ATB_ACT_SILU) f(std::integral_constant<int, ATB_ACT_SILU>());
+    else if (act == ATB_ACT_GELU) f(std::integral_constant<int, ATB_ACT_GELU>());
+    else f(std::integral_constant<int, ATB_ACT_GELU_TANH>());
 }
 // f<ACT>() for the runtime value, one branch for a whole tile.
 template <class F>
