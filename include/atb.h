@@ -464,6 +464,33 @@ atb_status_t atb_linear_backward(int64_t M, int64_t K, int64_t N, int act, int y
                                  void* dW_dev, int64_t lddw, int bias_type, void* dbias_dev, void* workspace_dev, size_t workspace_bytes,
                                  void* stream);
 
+/* Residual norm: a branch's result F joins the residual stream X, and the sum is normed again, in one pass:
+ *   U = norm(F) * PW + PB with ATB_NORM_POST, else F;   H = scale * X + gate * U;   Z = norm(H) * W + B.
+ *   kind: ATB_NORM_LAYER, norm(v) = (v - mean(v)) / sqrt(mean((v - mean(v))^2) + eps), or ATB_NORM_RMS, where the mean is taken as 0;
+ *   with ATB_NORM_POST added or not.
+ *   X_dev, H_dev: x_type [M][ldx], [M][ldh];  F_dev, Z_dev: f_type [M][ldf], [M][ldz];  x_type and f_type are one type, or FP32 and bf16;
+ *   gate_dev, PW_dev, PB_dev, W_dev, B_dev: w_type [N], each may be NULL (1, 1, 0, 1, 0);
+ *   stats_dev: FP32 [2][M], the mean and 1 / spread of H, with ATB_NORM_POST [4][M], those of F behind them; written for the backward pass,
+ *   may be NULL.
+ * Z is made of H before its rounding.  Any M, N >= 0 (0: nothing is done), any leading dimension >= N, any alignment of whole
+ * elements; rows that are multiples of 8 elements on 16-byte boundaries run on 16-byte accesses.
+ * Errors: BAD_ARGUMENT (kind, types, eps < 0, PW or PB without ATB_NORM_POST), BAD_SHAPE, NULL_POINTER, MISALIGNED, UNSUPPORTED_DEVICE, CUDA. */
+enum { ATB_NORM_LAYER = 0, ATB_NORM_RMS = 1, ATB_NORM_POST = 2 };
+atb_status_t atb_residual_norm(int64_t M, int64_t N, int kind, int x_type, const void* X_dev, int64_t ldx, int f_type, const void* F_dev, int64_t ldf,
+                               float scale, int w_type, const void* gate_dev, const void* PW_dev, const void* PB_dev, const void* W_dev,
+                               const void* B_dev, float eps, void* H_dev, int64_t ldh, void* Z_dev, int64_t ldz, float* stats_dev, void* stream);
+/* Gradients of atb_residual_norm from dZ (f_type) and dH (x_type, NULL: 0; the gradient that reaches H by itself), X, F and the statistics:
+ *   T = dH + (the norm's gradient of dZ * W at H),  dX = scale * T,  dF = gate * T, with ATB_NORM_POST the norm's gradient of gate * T * PW at F,
+ *   dgate = sum over rows of T * U, dPW = sum of gate * T * norm(F), dPB = sum of gate * T, dW = sum of dZ * norm(H), dB = sum of dZ.
+ *   dX_dev: x_type; dF_dev: f_type; the others w_type [N]; each may be NULL (not wanted).  H is computed again from X and F, unrounded.
+ *   M == 0 writes zero sums.  The workspace is needed only for those. */
+size_t atb_residual_norm_backward_workspace_bytes(int64_t M, int64_t N);
+atb_status_t atb_residual_norm_backward(int64_t M, int64_t N, int kind, int x_type, const void* dZ_dev, int64_t lddz, const void* dH_dev, int64_t lddh,
+                                        const void* X_dev, int64_t ldx, int f_type, const void* F_dev, int64_t ldf, float scale, int w_type,
+                                        const void* gate_dev, const void* PW_dev, const void* PB_dev, const void* W_dev, const float* stats_dev,
+                                        void* dX_dev, int64_t lddx, void* dF_dev, int64_t lddf, void* dgate_dev, void* dPW_dev, void* dPB_dev,
+                                        void* dW_dev, void* dB_dev, void* workspace_dev, size_t workspace_bytes, void* stream);
+
 #ifdef __cplusplus
 }
 #endif

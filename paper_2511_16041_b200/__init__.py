@@ -81,6 +81,7 @@ EXPORTED_SYMBOLS = [
     "atb_linear_cross_entropy", "atb_linear_cross_entropy_workspace_bytes",
     "atb_linear_cross_entropy_backward", "atb_linear_cross_entropy_backward_workspace_bytes",
     "atb_linear", "atb_linear_workspace_bytes", "atb_linear_backward", "atb_linear_backward_workspace_bytes",
+    "atb_residual_norm", "atb_residual_norm_backward", "atb_residual_norm_backward_workspace_bytes",
 ]
 
 
@@ -154,7 +155,11 @@ def load_library():
             ("atb_linear_workspace_bytes", sz, [i64, i64, i64]),
             ("atb_linear", ci, [i64, i64, i64, ci, ci, vp, i64, ci, vp, i64, ci, vp, vp, i64, vp, i64, ci, vp, vp, sz, vp]),
             ("atb_linear_backward_workspace_bytes", sz, [i64, i64, i64]),
-            ("atb_linear_backward", ci, [i64, i64, i64, ci, ci, vp, i64, vp, i64, ci, vp, i64, ci, vp, vp, i64, vp, i64, ci, vp, vp, sz, vp])):
+            ("atb_linear_backward", ci, [i64, i64, i64, ci, ci, vp, i64, vp, i64, ci, vp, i64, ci, vp, vp, i64, vp, i64, ci, vp, vp, sz, vp]),
+            ("atb_residual_norm", ci, [i64, i64, ci, ci, vp, i64, ci, vp, i64, cf, ci, vp, vp, vp, vp, vp, cf, vp, i64, vp, i64, vp, vp]),
+            ("atb_residual_norm_backward_workspace_bytes", sz, [i64, i64]),
+            ("atb_residual_norm_backward", ci, [i64, i64, ci, ci, vp, i64, vp, i64, vp, i64, ci, vp, i64, cf, ci, vp, vp, vp, vp, vp, vp, i64, vp, i64, vp, vp, vp,
+                                                vp, vp, vp, sz, vp])):
         fn = getattr(lib, name)
         fn.restype, fn.argtypes = restype, argtypes
     _lib = lib
@@ -547,6 +552,38 @@ def atb_linear_backward(dY, X, W, Z=None, act=None, dX=None, dW=None, dbias=None
     """Gradients ``(dX, dW, dbias)`` of ``atb_linear`` from ``dY`` and the ``Z`` that it saved (None without an activation); the
     residual's is dY.  dW in W's layout, dbias in float32 or the type of the tensor given.  False: not wanted."""
     return _result((_ops or load_ops()).linear_backward(dY, X, W, Z, _linear_act(act), dX, dW, dbias, workspace, _raw(stream)))
+
+
+NORM_KINDS = {"layer": 0, "rms": 1}
+
+
+def _norm_kind(kind):
+    if kind not in NORM_KINDS:
+        raise ValueError(f"kind={kind!r}: one of {', '.join(NORM_KINDS)}")
+    return NORM_KINDS[kind]
+
+
+def atb_residual_norm(X, F, W=None, B=None, gate=None, scale=1.0, post_norm=False, post_W=None, post_B=None, kind="layer", eps=1e-5, H=None, Z=None,
+                      stats=None, stream=None):
+    """A branch's result ``F`` joins the residual stream ``X``, and the sum is normed: ``H = scale * X + gate * U``, ``Z = norm(H) * W + B``, where U is
+    F, or with ``post_norm`` ``norm(F) * post_W + post_B``.
+
+    ``X``, ``H [M, N]``: float32 or bfloat16; ``F``, ``Z``: X's type or bfloat16; ``gate`` and the norms' vectors ``[N]``: one type, each may be None;
+    ``kind``: "layer" or "rms".  Returns ``(H, Z, stats)``: the last is float32 ``[2, M]`` (``[4, M]`` with ``post_norm``), for the backward pass."""
+    return _result((_ops or load_ops()).residual_norm(X, F, W, B, gate, scale, post_norm, post_W, post_B, _norm_kind(kind), eps, H, Z, stats, _raw(stream)))
+
+
+def atb_residual_norm_backward_workspace_bytes(M: int, N: int) -> int:
+    return int(load_library().atb_residual_norm_backward_workspace_bytes(M, N))
+
+
+def atb_residual_norm_backward(dZ, dH, X, F, stats, W=None, gate=None, scale=1.0, post_norm=False, post_W=None, post_B=None, kind="layer", dX=None, dF=None,
+                               dgate=None, dW=None, dB=None, dpost_W=None, dpost_B=None, workspace=None, stream=None):
+    """Gradients ``(dX, dF, dgate, dW, dB, dpost_W, dpost_B)`` of ``atb_residual_norm`` from ``dZ`` and ``dH`` (None: nothing but the norm reads
+    H).  The vectors' are of the vectors' type (float32 where there are none); dgate is None without a gate, dpost_W and dpost_B without
+    ``post_norm``.  False: not wanted.  Without a gate, a post norm and a scale dF is dX: False saves writing it twice."""
+    return _result((_ops or load_ops()).residual_norm_backward(dZ, dH, X, F, stats, W, gate, scale, post_norm, post_W, post_B, _norm_kind(kind), dX, dF, dgate, dW, dB,
+                                                               dpost_W, dpost_B, workspace, _raw(stream)))
 
 
 # ------------------------------------------------------------------ layout helpers (no arithmetic)

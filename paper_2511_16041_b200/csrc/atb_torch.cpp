@@ -27,7 +27,8 @@ namespace {
     X(atb_gated_ffn) X(atb_gated_ffn_workspace_bytes) X(atb_gated_ffn_backward) X(atb_gated_ffn_backward_workspace_bytes) \
     X(atb_linear_cross_entropy) X(atb_linear_cross_entropy_workspace_bytes) X(atb_linear_cross_entropy_backward)        \
     X(atb_linear_cross_entropy_backward_workspace_bytes) X(atb_bfp16_exp_bytes)                                         \
-    X(atb_linear) X(atb_linear_workspace_bytes) X(atb_linear_backward) X(atb_linear_backward_workspace_bytes)
+    X(atb_linear) X(atb_linear_workspace_bytes) X(atb_linear_backward) X(atb_linear_backward_workspace_bytes)     \
+    X(atb_residual_norm) X(atb_residual_norm_backward) X(atb_residual_norm_backward_workspace_bytes)
 struct Entries {
 #define ATB_ENTRY(name) decltype(&::name) name = nullptr;
     ATB_ENTRIES(ATB_ENTRY)
@@ -411,7 +412,7 @@ PyObject* linear(PyObject*, PyObject* const* a, Py_ssize_t n) {
     const int64_t ldx = c.matrix(X, M, K, at::kBFloat16, "X"), ldw = c.weights(W, K, N, "W", &layout);
     const int bias_code = vector_type(c, bias, N, "bias");
     const int64_t ldr = R.defined() ? c.matrix(R, M, N, y_type, "residual") : N, ldy = c.out_matrix(Y, M, N, y_type, "Y");
-    if (save) c.out_contiguous(Z, M, N, z_type, "Z");
+    if (save && c.out_matrix(Z, M, N, z_type, "Z") != N) refuse("Z: contiguous");
     const size_t bytes = c.workspace(ws, g_entry.atb_linear_workspace_bytes(M, K, N));
     return c.done(g_entry.atb_linear(M, K, N, act, y_code, ptr(X), ldx, layout, ptr(W), ldw, bias_code, ptr(bias), ptr(R), ldr, ptr(Y), ldy, z_code, ptr(Z), ptr(ws),
                                      bytes, c.stream), {Y, Z});
@@ -457,6 +458,96 @@ PyObject* linear_backward(PyObject*, PyObject* const* a, Py_ssize_t n) {
     END_HANDLE_TH_ERRORS
 }
 
+// ---------------------------------------------------------------------------------- residual norm
+// The vectors of weights, all of one type.
+struct NormWeights {
+    at::ScalarType type = at::kFloat;
+    bool any = false;
+    int code(const Call& c, int64_t N, std::initializer_list<std::pair<const at::Tensor*, const char*>> vectors) {
+        int found = ATB_F32;
+        for (const auto& [t, name] : vectors) {
+            if (!t->defined()) continue;
+            if (!any) { found = type_code(*t, name); type = t->scalar_type(); any = true; }
+            c.vector(*t, N, type, name);
+        }
+        return found;
+    }
+};
+// layer (0) or rms (1), and whether the branch is normed
+int norm_kind(PyObject* kind, PyObject* post) {
+    const int64_t v = integer(kind);
+    return (v == 0 || v == 1 ? static_cast<int>(v) : -8) | (truth(post) ? ATB_NORM_POST : 0);
+}
+double number(PyObject* o) {
+    const double v = PyFloat_AsDouble(o);
+    if (PyErr_Occurred()) throw python_error();
+    return v;
+}
+
+// (X, F, W, B, gate, scale, post, post_W, post_B, kind, eps, H, Z, stats, stream) -> (H, Z, stats)
+PyObject* residual_norm(PyObject*, PyObject* const* a, Py_ssize_t n) {
+    HANDLE_TH_ERRORS
+    expect(n, 15);
+    const at::Tensor X = tensor(a[0], "X"), F = tensor(a[1], "F"), W = tensor(a[2], "W"), B = tensor(a[3], "B"), gate = tensor(a[4], "gate");
+    const at::Tensor PW = tensor(a[7], "post_W"), PB = tensor(a[8], "post_B");
+    at::Tensor H = tensor(a[11], "H"), Z = tensor(a[12], "Z"), stats = tensor(a[13], "stats");
+    const double scale = number(a[5]), eps = number(a[10]);
+    const int kind = norm_kind(a[9], a[6]);
+    Call c(X, "X", a[14]);
+    if (!F.defined()) refuse("F: a matrix, got None");
+    const int64_t M = X.size(0), N = X.size(1);
+    const at::ScalarType x_type = row_type(X, "X"), f_type = row_type(F, "F");
+    const int64_t ldx = c.matrix(X, M, N, x_type, "X"), ldf = c.matrix(F, M, N, f_type, "F");
+    NormWeights weights;
+    const int w_code = weights.code(c, N, {{&gate, "gate"}, {&PW, "post_W"}, {&PB, "post_B"}, {&W, "W"}, {&B, "B"}});
+    const int64_t ldh = c.out_matrix(H, M, N, x_type, "H"), ldz = c.out_matrix(Z, M, N, f_type, "Z");
+    if (c.out_matrix(stats, kind & ATB_NORM_POST ? 4 : 2, M, at::kFloat, "stats") != M && M > 0) refuse("stats: contiguous");
+    return c.done(g_entry.atb_residual_norm(M, N, kind, type_code(x_type, "X"), ptr(X), ldx, type_code(f_type, "F"), ptr(F), ldf, static_cast<float>(scale), w_code,
+                                            ptr(gate), ptr(PW), ptr(PB), ptr(W), ptr(B), static_cast<float>(eps), ptr(H), ldh, ptr(Z), ldz, fptr(stats), c.stream),
+                  {H, Z, stats});
+    END_HANDLE_TH_ERRORS
+}
+
+// (dZ, dH, X, F, stats, W, gate, scale, post, post_W, post_B, kind, dX, dF, dgate, dW, dB, dpost_W, dpost_B, workspace, stream)
+// -> (dX, dF, dgate, dW, dB, dpost_W, dpost_B)
+PyObject* residual_norm_backward(PyObject*, PyObject* const* a, Py_ssize_t n) {
+    HANDLE_TH_ERRORS
+    expect(n, 21);
+    const at::Tensor dZ = tensor(a[0], "dZ"), dH = tensor(a[1], "dH"), X = tensor(a[2], "X"), F = tensor(a[3], "F"), stats = tensor(a[4], "stats");
+    const at::Tensor W = tensor(a[5], "W"), gate = tensor(a[6], "gate"), PW = tensor(a[9], "post_W"), PB = tensor(a[10], "post_B");
+    const double scale = number(a[7]);
+    const int kind = norm_kind(a[11], a[8]);
+    const bool post = kind & ATB_NORM_POST;
+    Gradient dX(a[12], "dX"), dF(a[13], "dF"), dgate(a[14], "dgate"), dW(a[15], "dW"), dB(a[16], "dB"), dPW(a[17], "dpost_W"), dPB(a[18], "dpost_B");
+    at::Tensor ws = tensor(a[19], "workspace");
+    Call c(X, "X", a[20]);
+    if (!F.defined()) refuse("F: a matrix, got None");
+    const int64_t M = X.size(0), N = X.size(1);
+    const at::ScalarType x_type = row_type(X, "X"), f_type = row_type(F, "F");
+    const int64_t ldx = c.matrix(X, M, N, x_type, "X"), ldf = c.matrix(F, M, N, f_type, "F"), lddz = c.matrix(dZ, M, N, f_type, "dZ");
+    const int64_t lddh = dH.defined() ? c.matrix(dH, M, N, x_type, "dH") : N;
+    if (c.matrix(stats, post ? 4 : 2, M, at::kFloat, "stats") != M && M > 0) refuse("stats: contiguous");
+    NormWeights weights;
+    const int w_code = weights.code(c, N, {{&gate, "gate"}, {&PW, "post_W"}, {&PB, "post_B"}, {&W, "W"}});
+    // without their vectors there are no gradients to make, unless the caller brings the place
+    if (!gate.defined() && !dgate.t.defined()) dgate.wanted = false;
+    if (!post && !dPW.t.defined()) dPW.wanted = false;
+    if (!post && !dPB.t.defined()) dPB.wanted = false;
+    const int64_t lddx = c.out_matrix(dX, M, N, x_type, "dX"), lddf = c.out_matrix(dF, M, N, f_type, "dF");
+    c.out_vector(dgate, N, weights.type, "dgate");
+    c.out_vector(dW, N, weights.type, "dW");
+    c.out_vector(dB, N, weights.type, "dB");
+    c.out_vector(dPW, N, weights.type, "dpost_W");
+    c.out_vector(dPB, N, weights.type, "dpost_B");
+    const bool sums = dgate.wanted || dW.wanted || dB.wanted || dPW.wanted || dPB.wanted;
+    const size_t bytes = c.workspace(ws, sums ? g_entry.atb_residual_norm_backward_workspace_bytes(M, N) : 0);
+    return c.done(g_entry.atb_residual_norm_backward(M, N, kind, type_code(x_type, "X"), ptr(dZ), lddz, ptr(dH), lddh, ptr(X), ldx, type_code(f_type, "F"), ptr(F), ldf,
+                                                     static_cast<float>(scale), w_code, ptr(gate), ptr(PW), ptr(PB), ptr(W), fptr(stats), ptr(dX.t), lddx, ptr(dF.t), lddf,
+                                                     ptr(dgate.t), ptr(dPW.t), ptr(dPB.t), ptr(dW.t), ptr(dB.t), ptr(ws), bytes, c.stream),
+                  {dX.t, dF.t, dgate.t, dW.t, dB.t, dPW.t, dPB.t});
+    END_HANDLE_TH_ERRORS
+}
+
 // (name, address) of an entry point of the library
 PyObject* bind(PyObject*, PyObject* const* a, Py_ssize_t n) {
     HANDLE_TH_ERRORS
@@ -474,7 +565,8 @@ PyObject* bind(PyObject*, PyObject* const* a, Py_ssize_t n) {
 
 #define ATB_METHOD(name) {#name, reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(name)), METH_FASTCALL, nullptr}
 PyMethodDef g_methods[] = {ATB_METHOD(layer_norm), ATB_METHOD(layer_norm_bfp16), ATB_METHOD(layer_norm_backward), ATB_METHOD(gated_ffn),
-                           ATB_METHOD(gated_ffn_backward), ATB_METHOD(linear_cross_entropy), ATB_METHOD(linear_cross_entropy_backward), ATB_METHOD(linear), ATB_METHOD(linear_backward), ATB_METHOD(bind),
+                           ATB_METHOD(gated_ffn_backward), ATB_METHOD(linear_cross_entropy), ATB_METHOD(linear_cross_entropy_backward), ATB_METHOD(linear), ATB_METHOD(linear_backward), ATB_METHOD(residual_norm), ATB_METHOD(residual_norm_backward),
+                           ATB_METHOD(bind),
                            {nullptr, nullptr, 0, nullptr}};
 PyModuleDef g_module = {PyModuleDef_HEAD_INIT, "_atb_torch", nullptr, -1, g_methods, nullptr, nullptr, nullptr, nullptr};
 
