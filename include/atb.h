@@ -358,7 +358,7 @@ atb_status_t atb_select_tiling(int64_t M, int64_t N, int64_t K, const atb_hw_par
  *   - a workspace is device memory, 16-byte aligned, of at least the bytes that the function beside the
  *     operator returns; it is overwritten and may be reused by the next call on the same stream.
  * ===================================================================================================== */
-typedef enum { ATB_F32 = 0, ATB_BF16 = 1 } atb_dtype_t;
+typedef enum { ATB_F32 = 0, ATB_BF16 = 1, ATB_F64 = 2 } atb_dtype_t;      /* ATB_F64: atb_sample's random numbers only */
 
 /* Layer norm of the M rows of X (N columns):
  *   mean = sum(x) / N, rstd = 1 / sqrt(sum((x - mean)^2) / N + eps), y = (x - mean) * rstd * W + B.
@@ -490,6 +490,24 @@ atb_status_t atb_residual_norm_backward(int64_t M, int64_t N, int kind, int x_ty
                                         const void* gate_dev, const void* PW_dev, const void* PB_dev, const void* W_dev, const float* stats_dev,
                                         void* dX_dev, int64_t lddx, void* dF_dev, int64_t lddf, void* dgate_dev, void* dPW_dev, void* dPB_dev,
                                         void* dW_dev, void* dB_dev, void* workspace_dev, size_t workspace_bytes, void* stream);
+
+/* One word for each row of logits, drawn with the row's random number.
+ *   weight(l) = exp((l - max) / T); the words' order: falling logit, rising index among equals.
+ *   Kept are the first n words in that order: at most top_k; those before which the weight is less than top_p times the weight of the first
+ *   top_k; those of weight >= min_p (the largest is 1).  Always one at least.
+ *   The token is the first word, in the vocabulary's order, at which the sum of the kept weights exceeds u times all kept weight; its
+ *   probability among the kept goes to probs.  Weights are held as multiples of 2^-45 (of 2^-(62 - log2 V) where V > 2^17) in 64-bit
+ *   integers, so that sums are exact: what weighs less than half of that is never drawn, and the draw is that of arithmetic in 64 bits.
+ *   logits_dev: type [M][ld] (V columns), any alignment of whole elements;  u_dev: u_type (ATB_F32 or ATB_F64) [M], in [0, 1): what is outside is
+ *   taken for the nearer end, NaN for 0;  tokens_dev int64 [M];  probs_dev FP32 [M] or NULL.
+ *   Settings: one number for all rows, or, where its pointer is not NULL, one of each row (FP32, top_k int32) [M]:
+ *   temperature 0 (per row also below 0, NaN) is the argmax, infinity evens the weights; top_k <= 0 or >= V, top_p >= 1, min_p <= 0 keep all (per row NaN too).
+ *   A logit of -inf or NaN is never drawn; a row of nothing else gives token -1 and probability 0.  Where a logit is +inf only such words are.
+ * M >= 0 (0: nothing is done), V >= 1.
+ * Errors: BAD_ARGUMENT (types, temperature < 0 or NaN, top_p or min_p NaN), BAD_SHAPE, NULL_POINTER, MISALIGNED, UNSUPPORTED_DEVICE, CUDA. */
+atb_status_t atb_sample(int64_t M, int64_t V, int type, const void* logits_dev, int64_t ld, int u_type, const void* u_dev, double temperature,
+                        const float* temperature_dev, int64_t top_k, const int32_t* top_k_dev, double top_p, const float* top_p_dev, double min_p,
+                        const float* min_p_dev, int64_t* tokens_dev, float* probs_dev, void* stream);
 
 #ifdef __cplusplus
 }

@@ -82,6 +82,7 @@ EXPORTED_SYMBOLS = [
     "atb_linear_cross_entropy_backward", "atb_linear_cross_entropy_backward_workspace_bytes",
     "atb_linear", "atb_linear_workspace_bytes", "atb_linear_backward", "atb_linear_backward_workspace_bytes",
     "atb_residual_norm", "atb_residual_norm_backward", "atb_residual_norm_backward_workspace_bytes",
+    "atb_sample",
 ]
 
 
@@ -137,7 +138,7 @@ def load_library():
     lib.atb_select_tiling.argtypes = [i64, i64, i64, ctypes.POINTER(atb_hw_params_t),
                                       ctypes.POINTER(atb_tiling_t), ctypes.POINTER(atb_tiling_score_t),
                                       ctypes.POINTER(ci)]
-    cf, sz = ctypes.c_float, ctypes.c_size_t
+    cf, cd, sz = ctypes.c_float, ctypes.c_double, ctypes.c_size_t
     for name, restype, argtypes in (
             ("atb_layer_norm", ci, [i64, i64, ci, vp, i64, ci, vp, vp, cf, vp, i64, vp, vp, vp]),
             ("atb_layer_norm_bfp16", ci, [i64, i64, ci, vp, i64, ci, vp, vp, cf, vp, vp, vp, vp, vp]),
@@ -159,7 +160,8 @@ def load_library():
             ("atb_residual_norm", ci, [i64, i64, ci, ci, vp, i64, ci, vp, i64, cf, ci, vp, vp, vp, vp, vp, cf, vp, i64, vp, i64, vp, vp]),
             ("atb_residual_norm_backward_workspace_bytes", sz, [i64, i64]),
             ("atb_residual_norm_backward", ci, [i64, i64, ci, ci, vp, i64, vp, i64, vp, i64, ci, vp, i64, cf, ci, vp, vp, vp, vp, vp, vp, i64, vp, i64, vp, vp, vp,
-                                                vp, vp, vp, sz, vp])):
+                                                vp, vp, vp, sz, vp]),
+            ("atb_sample", ci, [i64, i64, ci, vp, i64, ci, vp, cd, vp, i64, vp, cd, vp, cd, vp, vp, vp, vp])):
         fn = getattr(lib, name)
         fn.restype, fn.argtypes = restype, argtypes
     _lib = lib
@@ -584,6 +586,16 @@ def atb_residual_norm_backward(dZ, dH, X, F, stats, W=None, gate=None, scale=1.0
     ``post_norm``.  False: not wanted.  Without a gate, a post norm and a scale dF is dX: False saves writing it twice."""
     return _result((_ops or load_ops()).residual_norm_backward(dZ, dH, X, F, stats, W, gate, scale, post_norm, post_W, post_B, _norm_kind(kind), dX, dF, dgate, dW, dB,
                                                                dpost_W, dpost_B, workspace, _raw(stream)))
+
+
+def atb_sample(logits, u, temperature=1.0, top_k=0, top_p=1.0, min_p=0.0, tokens=None, probs=None, stream=None):
+    """One word for each row of ``logits [M, V]`` (float32 or bfloat16), drawn with the row's random number ``u [M]`` (float32 or float64 in [0, 1)).
+
+    Of the words in order of falling logit (rising index among equals) the first ``top_k`` are kept, of those the ones before which the probability
+    is less than ``top_p`` of theirs, and of those the ones that have at least ``min_p`` of the largest's; the draw goes through the kept in
+    the vocabulary's order.  ``temperature`` 0: the argmax.  Each setting is a number or a vector ``[M]`` (float32, ``top_k`` int32).
+    Returns ``(tokens, probs)``: int64, and the float32 probabilities among the kept.  -1 and 0 where no logit is above -inf."""
+    return _result((_ops or load_ops()).sample(logits, u, temperature, top_k, top_p, min_p, tokens, probs, _raw(stream)))
 
 
 # ------------------------------------------------------------------ layout helpers (no arithmetic)

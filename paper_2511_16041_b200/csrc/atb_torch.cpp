@@ -28,7 +28,7 @@ namespace {
     X(atb_linear_cross_entropy) X(atb_linear_cross_entropy_workspace_bytes) X(atb_linear_cross_entropy_backward)        \
     X(atb_linear_cross_entropy_backward_workspace_bytes) X(atb_bfp16_exp_bytes)                                         \
     X(atb_linear) X(atb_linear_workspace_bytes) X(atb_linear_backward) X(atb_linear_backward_workspace_bytes)     \
-    X(atb_residual_norm) X(atb_residual_norm_backward) X(atb_residual_norm_backward_workspace_bytes)
+    X(atb_residual_norm) X(atb_residual_norm_backward) X(atb_residual_norm_backward_workspace_bytes) X(atb_sample)
 struct Entries {
 #define ATB_ENTRY(name) decltype(&::name) name = nullptr;
     ATB_ENTRIES(ATB_ENTRY)
@@ -548,6 +548,48 @@ PyObject* residual_norm_backward(PyObject*, PyObject* const* a, Py_ssize_t n) {
     END_HANDLE_TH_ERRORS
 }
 
+// ---------------------------------------------------------------------------------- sampling
+// A number for all rows, or a vector with one of each.
+struct Setting {
+    double all = 0.0;
+    at::Tensor rows;
+    Setting(PyObject* o, const char* name) {
+        if (THPVariable_Check(o)) rows = tensor(o, name);
+        else all = number(o);
+    }
+    void* pointer(const Call& c, int64_t M, at::ScalarType type, const char* name) const {
+        if (rows.defined()) c.vector(rows, M, type, name);
+        return ptr(rows);
+    }
+};
+
+// (logits, u, temperature, top_k, top_p, min_p, tokens, probs, stream) -> (tokens, probs)
+PyObject* sample(PyObject*, PyObject* const* a, Py_ssize_t n) {
+    HANDLE_TH_ERRORS
+    expect(n, 9);
+    const at::Tensor X = tensor(a[0], "logits"), u = tensor(a[1], "u");
+    const Setting temperature(a[2], "temperature"), top_p(a[4], "top_p"), min_p(a[5], "min_p");
+    at::Tensor k_rows, tokens = tensor(a[6], "tokens"), probs = tensor(a[7], "probs");
+    int64_t k = 0;
+    if (THPVariable_Check(a[3])) k_rows = tensor(a[3], "top_k");
+    else k = integer(a[3]);
+    Call c(X, "logits", a[8]);
+    const int64_t M = X.size(0), V = X.size(1);
+    const int64_t ld = c.matrix(X, M, V, row_type(X, "logits"), "logits");
+    if (!u.defined() || (u.scalar_type() != at::kFloat && u.scalar_type() != at::kDouble)) refuse(c10::str("u: a vector of float32 or float64, got ", told(u)));
+    c.vector(u, M, u.scalar_type(), "u");
+    const float* const t_ptr = static_cast<const float*>(temperature.pointer(c, M, at::kFloat, "temperature"));
+    const float* const p_ptr = static_cast<const float*>(top_p.pointer(c, M, at::kFloat, "top_p"));
+    const float* const m_ptr = static_cast<const float*>(min_p.pointer(c, M, at::kFloat, "min_p"));
+    if (k_rows.defined()) c.vector(k_rows, M, at::kInt, "top_k");
+    c.out_vector(tokens, M, at::kLong, "tokens");
+    c.out_vector(probs, M, at::kFloat, "probs");
+    return c.done(g_entry.atb_sample(M, V, type_code(X, "logits"), ptr(X), ld, u.scalar_type() == at::kDouble ? ATB_F64 : ATB_F32, ptr(u), temperature.all, t_ptr, k,
+                                     static_cast<const int32_t*>(ptr(k_rows)), top_p.all, p_ptr, min_p.all, m_ptr, static_cast<int64_t*>(ptr(tokens)), fptr(probs),
+                                     c.stream), {tokens, probs});
+    END_HANDLE_TH_ERRORS
+}
+
 // (name, address) of an entry point of the library
 PyObject* bind(PyObject*, PyObject* const* a, Py_ssize_t n) {
     HANDLE_TH_ERRORS
@@ -566,7 +608,7 @@ PyObject* bind(PyObject*, PyObject* const* a, Py_ssize_t n) {
 #define ATB_METHOD(name) {#name, reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(name)), METH_FASTCALL, nullptr}
 PyMethodDef g_methods[] = {ATB_METHOD(layer_norm), ATB_METHOD(layer_norm_bfp16), ATB_METHOD(layer_norm_backward), ATB_METHOD(gated_ffn),
                            ATB_METHOD(gated_ffn_backward), ATB_METHOD(linear_cross_entropy), ATB_METHOD(linear_cross_entropy_backward), ATB_METHOD(linear), ATB_METHOD(linear_backward), ATB_METHOD(residual_norm), ATB_METHOD(residual_norm_backward),
-                           ATB_METHOD(bind),
+                           ATB_METHOD(sample), ATB_METHOD(bind),
                            {nullptr, nullptr, 0, nullptr}};
 PyModuleDef g_module = {PyModuleDef_HEAD_INIT, "_atb_torch", nullptr, -1, g_methods, nullptr, nullptr, nullptr, nullptr};
 
