@@ -4,13 +4,19 @@
 //   kept: the first n words in that order: n <= k;  the weight before a word < p * (weight of the first k);  weight >= min_p
 //   token: the first word, in the vocabulary's order, at which the kept weights' sum exceeds u * (all kept weight)
 //
-// No sort: the kept words are those above a logit tau, and the first c (by index) of those that equal it.  tau is found by
-// histograms of counts or weights over ever narrower ranges of logits (512 bins: first of equal width, then of the numbers'
-// ordered bit patterns, down to one number), which is 2 to 4 passes over logits that stay in registers.
 // Weights are 64-bit integers: their sums are exact, whatever the order they are added in, so that atomics leave no trace and a draw near
-// a border falls as it does in 64 bits.
-// A cluster of CTAs takes a row, 16 logits a thread: the row is read from memory once, and histograms and sums are joined through
-// distributed shared memory.  Rows of more than kMostCtas * 16384 words are read again in every pass.
+// a border falls as it does in 64 bits.  The row is not sorted: the kept words are those above a logit tau, and the first c (by index) of
+// those that equal it.
+//   few words at most (small k): the k-th largest of 256 groups' largest logits is below the k-th largest logit, so that the words that reach
+//     it are few (about 60 for k = 50): one CTA ranks those and draws
+//   else tau is found by histograms over ever narrower ranges of logits (512 bins: first of equal width, then of the numbers' ordered bit
+//     patterns, down to one number), of counts for top-k; for top-p a first histogram of counts bounds the weight in its bins, so that only
+//     the few bins that the border may be in are looked at word by word
+// A cluster of CTAs takes a row, 32 logits a thread in shared memory: the row is read from memory once, and histograms and sums are
+// joined through distributed shared memory.  Rows of more than kMostCtas * 16384 words are read again in every pass.
+// Bound by instructions, of which a word takes about 100 where top-p looks at all of them; two CTAs of different rows share an SM, so that one
+// works while the other waits for its cluster.  (Logits in registers, 16 of 1024 threads and loops unrolled over them, took 250
+// instructions a word and twice the time: what a warp does once per pass counts for half as many words.)
 #include <cooperative_groups.h>
 #include <cuda_bf16.h>
 #include <cuda_runtime.h>
@@ -22,7 +28,7 @@ namespace {
 
 namespace cg = cooperative_groups;
 
-constexpr int kPerThread = 16, kBins = 512, kMostCtas = 8, kMostThreads = 1024, kMostWarps = kMostThreads / 32;
+constexpr int kVectors = 8, kPerThread = 4 * kVectors, kBins = 512, kMostCtas = 8, kMostThreads = 512, kMostWarps = kMostThreads / 32;
 constexpr float kBinsPerUnit = 16.f;       // of the first pass: 32 units below the largest logit, what lies below in the last bin
 
 // A setting: of every row, or one for all.
@@ -38,24 +44,59 @@ struct SampleParams {
     Setting temperature, top_k, top_p, min_p;      // rows: float, int32, float, float
     int64_t* tokens;
     float* probs;
-    int chunks, shift;                             // pieces of 16 logits per thread; S
+    int chunks, shift;                             // pieces of 32 logits per thread; S
+    int group;                                     // lanes that share a largest logit
 };
-
+constexpr int kMostGroups = 256, kCandidates = 512, kWords = 2048, kSpans = kBins / 32;
+struct Candidate {
+    float l;
+    int word;
+};
+// What the row's first CTA has found, for all.
+struct Found {
+    int first, last;                               // bins; first -1: the goal is not reached
+    uint32_t active, above_count;                  // words in those bins, words above them
+    uint32_t tau, equal;                           // where done: the number, and the words that equal it
+    int done;
+    unsigned long long above;                      // weight above them
+    double goal;
+};
+struct FewWords {                                  // all candidates; the first k of them in their order
+    Candidate all[kCandidates], kept[kCandidates];
+    unsigned long long weight[kCandidates];
+};
 struct Shared {
-    uint32_t count[2][kBins];                      // histograms of this CTA, in turn
-    unsigned long long weight[2][kBins];
-    uint32_t all_count[kBins];                     // of the cluster
-    unsigned long long all_weight[kBins];
-    float top;                                     // this CTA's largest logit
+    union {                                        // the first CTA's, when it goes on alone
+        FewWords few;
+        float words[kWords];
+    };
+    union {                                        // this CTA's
+        Candidate candidate[kCandidates];
+        float active[kWords];
+    };
+    uint32_t candidates;                           // of either
+    uint32_t count[kBins];                         // histogram
+    unsigned long long weight[kBins];
+    uint32_t span_count[kSpans];                   // sums over 32 bins
+    unsigned long long span_weight[kSpans];
+    double span_most[kSpans], span_least[kSpans];
+    Found found;
+    unsigned long long beyond;                     // weight above the bins looked at
+    float group_top[kMostGroups];                  // this CTA's groups' largest logits
+    float all_groups[kMostGroups];
+    float floor;
+    float top;                                     // this CTA's largest logit, and the row's
+    float row_top;
     unsigned long long total;                      // this CTA's kept weight
+    unsigned long long base, all;                  // that of the CTAs before this one, of all
     uint32_t equal;                                // this CTA's words at tau
+    uint32_t joined;                               // a sum over the cluster
     unsigned long long warp_total[kMostWarps];
+    unsigned long long warp_beyond[kMostWarps];
     uint32_t warp_equal[kMostWarps];
     float warp_top[kMostWarps];
-    // what a pass finds
-    int bin;
-    unsigned long long above;
-    uint32_t above_count, bin_count;
+    double u, top_p, deepest;                      // the row's; deepest: powers of 2 below the largest that min_p leaves
+    double table[16];                              // 2^(j / 16)
 };
 
 __device__ __forceinline__ uint32_t key_of(float l) {            // ordered like the logits; -0 does not occur
@@ -67,32 +108,56 @@ __device__ __forceinline__ float of_key(uint32_t k) { return __uint_as_float(k &
 // -inf for NaN, and +0 for -0, which compare alike.
 __device__ __forceinline__ float canonical(float l) { return l == l ? l + 0.f : -INFINITY; }
 
+// A warp's logits: chunks of 32 x 32 consecutive words, in shared memory as vectors of 4, vector j of lane i at words 128 j + 4 i of the chunk.
 template <class T>
 struct Row {
-    static constexpr int VEC = 16 / sizeof(T), NV = kPerThread / VEC;
     const T* row;
-    int64_t V, first;                      // first: word of this lane's first element in the warp's first chunk (may lie before the row)
-    // word of element e of vector j of chunk c
-    __device__ __forceinline__ int64_t word(int c, int j, int e) const { return first + c * (kPerThread * 32) + j * (32 * VEC) + e; }
-    __device__ __forceinline__ void load(int c, float (&v)[kPerThread]) const {
+    int V, first;                          // first: word of the warp's first logit (may lie before the row)
+    // word of element e of this lane's vector j of chunk c
+    __device__ __forceinline__ int word(int c, int j, int lane, int e) const { return first + c * (32 * kPerThread) + j * 128 + lane * 4 + e; }
+    // Chunk c to `to`, this warp's place.  Vectors of 16 bytes that lie inside the row are loaded whole.
+    __device__ __forceinline__ void load(int c, float4* to, int lane) const {
+        constexpr int PER = 16 / sizeof(T), LOADS = kPerThread / PER;
+        const int from = first + c * (32 * kPerThread) + lane * PER;
+        __syncwarp();                      // the warp has read the chunk before
 #pragma unroll
-        for (int j = 0; j < NV; ++j) {
-            const int64_t at = word(c, j, 0);
-            if (at >= 0 && at + VEC <= V) {
-                const uint4 q = __ldg(reinterpret_cast<const uint4*>(row + at));
-                const uint32_t w[4] = {q.x, q.y, q.z, q.w};
+        for (int half = 0; half < 2; ++half) {
+            uint4 q[LOADS / 2];
 #pragma unroll
-                for (int e = 0; e < VEC; ++e) {
-                    if constexpr (sizeof(T) == 4) v[j * VEC + e] = __uint_as_float(w[e]);
-                    else v[j * VEC + e] = __uint_as_float(e & 1 ? w[e / 2] & 0xFFFF0000u : w[e / 2] << 16);
+            for (int i = 0; i < LOADS / 2; ++i) {
+                const int at = from + (half * (LOADS / 2) + i) * 32 * PER;
+                if (at >= 0 && at <= V - PER) {
+                    q[i] = __ldg(reinterpret_cast<const uint4*>(row + at));
+                } else {
+                    uint32_t w[4];
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) {
+                        if constexpr (sizeof(T) == 4) {
+                            w[e] = at + e >= 0 && at + e < V ? reinterpret_cast<const uint32_t*>(row)[at + e] : 0xFF800000u;
+                        } else {
+                            const auto one = [&](int a) -> uint32_t { return a >= 0 && a < V ? reinterpret_cast<const uint16_t*>(row)[a] : 0xFF80u; };
+                            w[e] = one(at + 2 * e) | one(at + 2 * e + 1) << 16;
+                        }
+                    }
+                    q[i] = make_uint4(w[0], w[1], w[2], w[3]);
                 }
-            } else {
+            }
 #pragma unroll
-                for (int e = 0; e < VEC; ++e) v[j * VEC + e] = at + e >= 0 && at + e < V ? static_cast<float>(row[at + e]) : -INFINITY;
+            for (int i = 0; i < LOADS / 2; ++i) {
+                const uint32_t w[4] = {q[i].x, q[i].y, q[i].z, q[i].w};
+                const int at = (half * (LOADS / 2) + i) * 32 * PER + lane * PER;       // word of the chunk
+                float4* const dst = to + at / 4;
+                if constexpr (sizeof(T) == 4) {
+                    *dst = make_float4(canonical(__uint_as_float(w[0])), canonical(__uint_as_float(w[1])), canonical(__uint_as_float(w[2])), canonical(__uint_as_float(w[3])));
+                } else {
+                    const auto lo = [&](int e) { return canonical(__uint_as_float(w[e] << 16)); };
+                    const auto hi = [&](int e) { return canonical(__uint_as_float(w[e] & 0xFFFF0000u)); };
+                    dst[0] = make_float4(lo(0), hi(0), lo(1), hi(1));
+                    dst[1] = make_float4(lo(2), hi(2), lo(3), hi(3));
+                }
             }
         }
-#pragma unroll
-        for (int i = 0; i < kPerThread; ++i) v[i] = canonical(v[i]);
+        __syncwarp();
     }
 };
 
@@ -112,67 +177,95 @@ __device__ __forceinline__ V warp_scan(V v, int lane) {          // inclusive
     return v;
 }
 
+// 2^(S - d slope), d >= 0, to the nearest integer, where slope16 = 16 slope: 2^(-round(16 y) / 16) from a table and the rest, at most 2^-5,
+// by the first terms of its series (Tang's table-driven method), relative error below 2^-50.  The sums with 1.5 * 2^52 and 2^52
+// round to an integer.  Sixteen entries lie in banks of their own.  d slope <= S + 3.
+__device__ __forceinline__ unsigned long long fixed_exp2(double d, double slope16, int shift, const double* table) {
+    const double near = fma(d, slope16, 0x1.8p52);
+    const int q = -__double2loint(near);
+    const double r = fma(-d, slope16, near - 0x1.8p52);          // -16 y = q + r
+    constexpr double c1 = 0.69314718055994530942 / 16, c2 = c1 * c1 / 2, c3 = c2 * c1 / 3, c4 = c3 * c1 / 4, c5 = c4 * c1 / 5, c6 = c5 * c1 / 6;
+    const double p = fma(r, fma(r, fma(r, fma(r, fma(r, fma(r, c6, c5), c4), c3), c2), c1), 1.0) * table[q & 15];
+    const double scaled = __hiloint2double(__double2hiint(p) + (((q >> 4) + shift) << 20), __double2loint(p));
+    const double whole = scaled + 0x1p52;
+    return static_cast<unsigned long long>(__double_as_longlong(whole)) - 0x4330000000000000ull;
+}
+
+// Sum over the first `ranks` CTAs of what they have at `own`: by one warp, a lane to a CTA, so that a value crosses once.
+template <class V>
+__device__ __forceinline__ V cluster_sum(const cg::cluster_group& cluster, int ranks, V* own, int lane) {
+    return warp_add(lane < ranks ? *cluster.map_shared_rank(own, lane) : V(0));
+}
+
 // T: type of the logits.  RESIDENT: a thread's logits are 16, and stay in registers.
 template <class T, bool RESIDENT>
-__global__ void __launch_bounds__(kMostThreads, 1) sample_kernel(const SampleParams p) {
+__global__ void __launch_bounds__(kMostThreads, 2) sample_kernel(const SampleParams p) {
     __shared__ Shared sh;
+    extern __shared__ float4 logits[];     // [warps][32 kVectors]
     cg::cluster_group cluster = cg::this_cluster();
     const int ranks = static_cast<int>(cluster.num_blocks()), rank = static_cast<int>(cluster.block_rank());
     const int64_t m = blockIdx.x / ranks;
     const int t = threadIdx.x, lane = t & 31, warp = t >> 5, warps = blockDim.x >> 5;
-    for (int i = t; i < kBins; i += blockDim.x)
-#pragma unroll
-        for (int b = 0; b < 2; ++b) {
-            sh.count[b][i] = 0;
-            sh.weight[b][i] = 0;
-        }
+    for (int i = t; i < kBins; i += blockDim.x) {
+        sh.count[i] = 0;
+        sh.weight[i] = 0;
+    }
+    if (t == 0) { sh.beyond = 0; sh.candidates = 0; }
+    if (t < 16) sh.table[t] = exp2(t * 0.0625);
     sm100::grid_dependency_wait();
     sm100::grid_dependency_launch();
 
     Row<T> row;
     row.row = static_cast<const T*>(p.logits) + m * p.ld;
-    row.V = p.V;
+    row.V = static_cast<int>(p.V);
     {
         // vectors start on 16-byte boundaries: positions are counted from the one at or below the row's first word
         const int64_t skip = static_cast<int64_t>(reinterpret_cast<uintptr_t>(row.row) & 15u) / static_cast<int64_t>(sizeof(T));
-        row.first = (static_cast<int64_t>(rank) * warps + warp) * p.chunks * (kPerThread * 32) + lane * Row<T>::VEC - skip;
+        row.first = (rank * warps + warp) * p.chunks * (32 * kPerThread) - static_cast<int>(skip);
     }
-    float kept_in_registers[kPerThread];
-    if constexpr (RESIDENT) row.load(0, kept_in_registers);
-    // f(chunk, logits) over this thread's logits
+    float4* const mine4 = logits + warp * 32 * kVectors;
+    if constexpr (RESIDENT) row.load(0, mine4, lane);
+    // f(chunk, vector, logits) over this thread's logits in the words' order
     const auto each = [&](auto&& f) {
-        if constexpr (RESIDENT) {
-            f(0, kept_in_registers);
-        } else {
 #pragma unroll 1
-            for (int c = 0; c < p.chunks; ++c) {
-                float v[kPerThread];
-                row.load(c, v);
-                f(c, v);
+        for (int c = 0; c < (RESIDENT ? 1 : p.chunks); ++c) {
+            if constexpr (!RESIDENT) row.load(c, mine4, lane);
+#pragma unroll 2
+            for (int j = 0; j < kVectors; ++j) {
+                const float4 q = mine4[j * 32 + lane];
+                const float v[4] = {q.x, q.y, q.z, q.w};
+                f(c, j, v);
             }
         }
     };
 
     // ---- the row's settings
     const auto real = [&](const Setting& s) { return s.rows ? static_cast<double>(static_cast<const float*>(s.rows)[m]) : s.all; };
-    const double temperature = real(p.temperature), top_p = real(p.top_p), min_p = real(p.min_p);
+    const double temperature = real(p.temperature);
     int64_t k = p.top_k.rows ? static_cast<const int32_t*>(p.top_k.rows)[m] : static_cast<int64_t>(p.top_k.all);
-    double u = p.u64 ? static_cast<const double*>(p.u)[m] : static_cast<double>(static_cast<const float*>(p.u)[m]);
     const bool greedy = !(temperature > 0.0);
     if (greedy) k = 1;
     if (k <= 0 || k > p.V) k = p.V;
     const double slope = greedy ? 1.4426950408889634074 : 1.4426950408889634074 / temperature;
-    // weight >= min_p by the exponents; 1 and more keep what weighs 1 in 64 bits, which is more than 1 - 2^-54
-    const double deepest = min_p > 0.0 ? fmax(min_p < 1.0 ? -log2(min_p) : 0.0, 0x1p-54 * 1.4426950408889634074) : INFINITY;
+    if (t == 0) {                          // what is needed late waits in shared memory
+        const double min_p = real(p.min_p);
+        sh.u = p.u64 ? static_cast<const double*>(p.u)[m] : static_cast<double>(static_cast<const float*>(p.u)[m]);
+        sh.top_p = greedy ? 1.0 : real(p.top_p);
+        // weight >= min_p by the exponents; 1 and more keep what weighs 1 in 64 bits, which is more than 1 - 2^-54
+        sh.deepest = min_p > 0.0 ? fmax(min_p < 1.0 ? -log2(min_p) : 0.0, 0x1p-54 * 1.4426950408889634074) : INFINITY;
+    }
 
-    // ---- the largest logit
+    // ---- the largest logit, and those of the groups
     float top = -INFINITY;
-    each([&](int, const float (&v)[kPerThread]) {
+    each([&](int, int, const float (&v)[4]) {
 #pragma unroll
-        for (int i = 0; i < kPerThread; ++i) top = fmaxf(top, v[i]);
+        for (int i = 0; i < 4; ++i) top = fmaxf(top, v[i]);
     });
-#pragma unroll
-    for (int o = 16; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xFFFFFFFFu, top, o));
+    for (int o = 1; o < 32; o <<= 1) {
+        if (o == p.group && !(lane & (o - 1))) sh.group_top[t / o] = top;
+        top = fmaxf(top, __shfl_xor_sync(0xFFFFFFFFu, top, o));
+    }
+    if (p.group == 32 && lane == 0) sh.group_top[warp] = top;
     if (lane == 0) sh.warp_top[warp] = top;
     __syncthreads();
     if (warp == 0) {
@@ -182,7 +275,14 @@ __global__ void __launch_bounds__(kMostThreads, 1) sample_kernel(const SamplePar
         if (lane == 0) sh.top = top;
     }
     cluster.sync();
-    for (int r = 0; r < ranks; ++r) top = fmaxf(r ? top : -INFINITY, *cluster.map_shared_rank(&sh.top, r));
+    if (warp == 0) {
+        top = lane < ranks ? *cluster.map_shared_rank(&sh.top, lane) : -INFINITY;
+#pragma unroll
+        for (int o = 4; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xFFFFFFFFu, top, o));
+        if (lane == 0) sh.row_top = top;
+    }
+    __syncthreads();
+    top = sh.row_top;
     if (top == -INFINITY) {                // nothing to draw from: the same for the whole cluster
         if (rank == 0 && t == 0) {
             p.tokens[m] = -1;
@@ -194,137 +294,348 @@ __global__ void __launch_bounds__(kMostThreads, 1) sample_kernel(const SamplePar
 
     // depth of a logit below the largest, in powers of 2
     const auto depth = [&](float l) { return l == top ? 0.0 : (static_cast<double>(top) - static_cast<double>(l)) * slope; };
+    const double slope16 = 16.0 * slope;
+    const float slope_f = static_cast<float>(slope);
     const auto weight = [&](float l) -> unsigned long long {
-        const double y = depth(l);
-        return y < p.shift + 2 ? __double2ull_rn(exp2(static_cast<double>(p.shift) - y)) : 0ull;
+        if (l == top) return 1ull << p.shift;
+        // a difference that is too far, infinite or no number weighs nothing (halves: that of two finite numbers is finite)
+        if (!((0.5f * top - 0.5f * l) * slope_f < 0.5f * static_cast<float>(p.shift + 2))) return 0ull;
+        return fixed_exp2(static_cast<double>(top) - static_cast<double>(l), slope16, p.shift, sh.table);
     };
-    const auto bin_of = [&](float l) {     // falls with l, as every step of it does
-        const float d = (top - l) * kBinsPerUnit;
-        return l == top ? 0 : d < static_cast<float>(kBins - 1) ? static_cast<int>(d) : kBins - 1;
+    // the first word whose sum exceeds u * all: at least this much
+    const auto target_of = [&](unsigned long long all) {
+        const double u = sh.u, at = u > 0.0 ? u * static_cast<double>(all) : 0.0;
+        return (at < static_cast<double>(all) ? min(static_cast<unsigned long long>(at), all - 1) : all - 1) + 1;
     };
+
+    // ---- few words
+    const int groups = static_cast<int>(blockDim.x) / p.group;   // of a CTA
+    if (k <= groups * ranks * 3 / 4) {
+        const int n = groups * ranks;      // at most 256
+        for (int i = t; i < n; i += blockDim.x) sh.all_groups[i] = *cluster.map_shared_rank(&sh.group_top[i % groups], i / groups);
+        __syncthreads();
+        // the rank of each: four lanes to a group
+        for (int i = t >> 2; i < ((n + 7) & ~7); i += blockDim.x >> 2) {
+            const float mine = i < n ? sh.all_groups[i] : 0.f;
+            int before = 0;
+            for (int j = t & 3; j < n; j += 4) {
+                const float other = sh.all_groups[j];
+                before += other > mine || (other == mine && j < i);
+            }
+            before += __shfl_xor_sync(0xFFFFFFFFu, before, 1);
+            before += __shfl_xor_sync(0xFFFFFFFFu, before, 2);
+            if (i < n && before == k - 1) sh.floor = mine;
+        }
+        __syncthreads();
+        const float floor = sh.floor;
+        each([&](int c, int j, const float (&v)[4]) {
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+                if (v[i] >= floor && v[i] > -INFINITY) {
+                    const uint32_t at = atomicAdd(&sh.candidates, 1u);
+                    if (at < kCandidates) sh.candidate[at] = {v[i], row.word(c, j, lane, i)};
+                }
+        });
+        cluster.sync();
+        if (warp == 0) {
+            const uint32_t n = cluster_sum(cluster, ranks, &sh.candidates, lane);
+            if (lane == 0) sh.joined = n;
+        }
+        __syncthreads();
+        const uint32_t all = sh.joined;
+        if (all <= kCandidates) {
+            if (rank == 0) {
+                const int count = static_cast<int>(all);
+                for (int i = t; i < count; i += blockDim.x) {
+                    int r = 0, at = i;
+                    for (uint32_t own; at >= static_cast<int>(own = *cluster.map_shared_rank(&sh.candidates, r)); ++r) at -= static_cast<int>(own);
+                    sh.few.all[i] = cluster.map_shared_rank(&sh, r)->candidate[at];
+                }
+                __syncthreads();
+                // in their order, the first k
+                for (int i = t; i < count; i += blockDim.x) {
+                    const Candidate mine = sh.few.all[i];
+                    int before = 0;
+                    for (int j = 0; j < count; ++j) {
+                        const Candidate other = sh.few.all[j];
+                        before += other.l > mine.l || (other.l == mine.l && other.word < mine.word);
+                    }
+                    if (before < k) {
+                        sh.few.kept[before] = mine;
+                        sh.few.weight[before] = weight(mine.l);
+                    }
+                }
+                __syncthreads();
+                // the first of those by top_p and min_p
+                const int first = static_cast<int>(k < count ? k : count);
+                unsigned long long whole = 0;
+                for (int j = 0; j < first; ++j) whole += sh.few.weight[j];
+                const double top_p = sh.top_p, deepest = sh.deepest;
+                const bool by_p = top_p < 1.0;
+                const double goal = top_p > 0.0 ? top_p * static_cast<double>(whole) : 0.0;
+                int kept = 0;
+                unsigned long long sum = 0;
+                for (; kept < first; ++kept) {
+                    if (kept > 0 && ((by_p && !(static_cast<double>(sum) < goal)) || !(depth(sh.few.kept[kept].l) <= deepest))) break;
+                    sum += sh.few.weight[kept];
+                }
+                const unsigned long long target = target_of(sum);
+                for (int i = t; i < kept; i += blockDim.x) {
+                    const int word = sh.few.kept[i].word;
+                    const unsigned long long own = sh.few.weight[i];
+                    unsigned long long run = 0;
+                    for (int j = 0; j < kept; ++j) run += sh.few.kept[j].word <= word ? sh.few.weight[j] : 0ull;
+                    if (run >= target && run - own < target) {
+                        p.tokens[m] = word;
+                        if (p.probs) p.probs[m] = static_cast<float>(static_cast<double>(own) / static_cast<double>(sum));
+                    }
+                }
+            }
+            cluster.sync();                // nobody leaves while its candidates may still be read
+            return;
+        }
+    }
 
     // ---- the kept words: above tau, and `quota` of those that equal it
     uint32_t tau = 0;                      // key; nothing that can be drawn is at 0
     uint32_t quota = 0, equal_all = 0;     // equal_all: words at tau
     int turn = 0;
-    // One search: the first number, from the largest logit down, at which the sum (of counts, or of weights, over the words that `in` admits)
-    // reaches `goal`.
-    const auto search = [&](bool by_weight, auto&& reached, auto&& admits) {
-        // the words looked at: the first pass's bin, and keys low .. high
-        int bin = -1;
-        uint32_t low = 0, high = 0xFFFFFFFFu;
-        int width = 0;                     // a bin holds 2^width keys
-        unsigned long long above = 0;
-        uint32_t above_count = 0;
-        while (true) {
-            each([&](int, const float (&v)[kPerThread]) {
+    // bins of equal width below the largest logit; falls with l, as every step of it does
+    const auto bin_of = [&](float l, float scale) {
+        const float d = (0.5f * top - 0.5f * l) * (2.f * scale);         // halves: the difference of two finite numbers is finite
+        // floor(d), read off the sum with 2^23
+        return l == top ? 0 : d < static_cast<float>(kBins - 1) ? static_cast<int>(__float_as_uint(__fadd_rd(d, 8388608.f)) & (kBins - 1)) : kBins - 1;
+    };
+    // f(bin of this lane, span) in the first CTA: a warp takes 32 bins at a time
+    const auto spans = [&](auto&& f) {
+        for (int span = warp; span < kSpans; span += warps) f(span * 32 + lane, span);
+    };
+    // The histograms of the cluster's CTAs, joined in the first one's own.
+    const auto join = [&](bool by_weight) {
+        for (int i = t; i < kBins; i += blockDim.x) {
+            uint32_t n[kMostCtas];
+            unsigned long long w[kMostCtas] = {};
 #pragma unroll
-                for (int i = 0; i < kPerThread; ++i) {
+            for (int r = 0; r < kMostCtas; ++r) n[r] = r < ranks ? *cluster.map_shared_rank(&sh.count[i], r) : 0u;
+            if (by_weight)
+#pragma unroll
+                for (int r = 0; r < kMostCtas; ++r) w[r] = r < ranks ? *cluster.map_shared_rank(&sh.weight[i], r) : 0ull;
+#pragma unroll
+            for (int r = 1; r < kMostCtas; ++r) { n[0] += n[r]; w[0] += w[r]; }
+            sh.count[i] = n[0];
+            sh.weight[i] = w[0];
+        }
+        __syncthreads();
+    };
+    // The first bin of the first CTA's histogram at which `reached` holds of the sums from the first bin on and what stands above them: to sh.found
+    // (first, above_count, above, active: the words in it).  For all its threads.
+    const auto find = [&](auto&& reached) {
+        const uint32_t above_count = sh.found.above_count;
+        const unsigned long long above = sh.found.above;
+        spans([&](int b, int span) {
+            const uint32_t n = warp_add(sh.count[b]);
+            const unsigned long long w = warp_add(sh.weight[b]);
+            if (lane == 0) { sh.span_count[span] = n; sh.span_weight[span] = w; }
+        });
+        __syncthreads();
+        if (t == 0) sh.found.first = -1;
+        __syncthreads();
+        spans([&](int b, int span) {
+            uint32_t n = above_count + warp_add(lane < span ? sh.span_count[lane] : 0u);
+            unsigned long long w = above + warp_add(lane < span ? sh.span_weight[lane] : 0ull);
+            const uint32_t own = sh.count[b];
+            const unsigned long long own_weight = sh.weight[b];
+            n += warp_scan(own, lane);
+            w += warp_scan(own_weight, lane);
+            // sums do not fall, so that one bin is the first
+            if (reached(n, w) && !(b > 0 && reached(n - own, w - own_weight))) {
+                sh.found.first = b;
+                sh.found.active = own;
+                sh.found.above_count = n - own;
+                sh.found.above = w - own_weight;
+            }
+        });
+        __syncthreads();
+    };
+    // Behind the first CTA's search: what it found comes into every CTA's own sh.found.  (It is written next behind another
+    // cluster.sync.)  The histograms and the lists of words have been read, and are emptied.
+    const auto publish = [&] {
+        cluster.sync();
+        if (rank > 0 && warp == 0)
+            for (int i = lane; i < static_cast<int>(sizeof(Found) / 4); i += 32)
+                reinterpret_cast<uint32_t*>(&sh.found)[i] = *cluster.map_shared_rank(reinterpret_cast<uint32_t*>(&sh.found) + i, 0);
+        for (int i = t; i < kBins; i += blockDim.x) {
+            sh.count[i] = 0;
+            sh.weight[i] = 0;
+        }
+        if (t == 0) sh.candidates = 0;
+        __syncthreads();
+    };
+    const auto width_of = [](uint32_t keys) {                    // a bin holds 2^width keys
+        int width = 0;
+        while ((keys >> width) >= kBins) ++width;
+        return width;
+    };
+    // The first number, from the largest logit down, at which the sum over the words of keys >= `least` reaches its goal, when it is known to lie in
+    // the bins sh.found.first .. last of width 1 / scale, with sh.found.active words.  Weights: the weight above those bins is added up on the way.
+    // Sets tau and equal_all.
+    uint32_t whole_above = 0xFFFFFFFFu;    // keys above it are in the warps' sums of the weight above the bins, sh.warp_beyond
+    const auto narrow = [&](bool by_weight, auto&& reached, uint32_t least, float scale) {
+        const int first = sh.found.first, last = sh.found.last;
+        // keys of the bins' words: their ends, and more than the roundings of bin_of and of the ends can be
+        uint32_t low = 0, high = key_of(top);
+        if (top < INFINITY && scale > 1e-30f && scale < 1e30f) {
+            const float up = static_cast<float>(first) / scale, down = static_cast<float>(last + 1) / scale;
+            const float slack = (fabsf(top) + down) * 0x1p-21f;
+            if (first > 0) high = key_of(canonical(fminf(top, top - up + slack)));
+            if (last < kBins - 1) low = key_of(canonical(top - down - slack));
+        } else if (first == 0 && last == 0 && !(top < INFINITY)) {
+            low = high;                    // an infinite logit stands alone
+        }
+        bool begin = by_weight;            // the weight above is still to be added up
+        if (by_weight) whole_above = high;
+        while (true) {
+            const bool alone = sh.found.active <= kWords;        // few enough for the first CTA
+            const int width = width_of(high - low);
+            unsigned long long beyond = 0, extra = 0;           // of keys above `high`; of the few below it in earlier bins
+            each([&](int, int, const float (&v)[4]) {
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
                     const uint32_t key = key_of(v[i]);
-                    if (v[i] == -INFINITY || !admits(key)) continue;
-                    int b = bin_of(v[i]);
-                    if (bin >= 0) {
-                        if (b != bin || key < low || key > high) continue;
-                        b = static_cast<int>((high - key) >> width);
+                    if (key < low || key < least || v[i] == -INFINITY) continue;
+                    if (key > high) {
+                        if (begin) beyond += weight(v[i]);
+                        continue;
                     }
-                    atomicAdd(&sh.count[turn][b], 1u);
-                    if (by_weight) atomicAdd(&sh.weight[turn][b], weight(v[i]));
+                    const int b = bin_of(v[i], scale);
+                    if (b < first) {
+                        if (begin) extra += weight(v[i]);
+                    } else if (b <= last) {
+                        if (alone) {
+                            const uint32_t at = atomicAdd(&sh.candidates, 1u);
+                            if (at < kWords) sh.active[at] = v[i];
+                        } else {
+                            const int at = static_cast<int>((high - key) >> width);
+                            atomicAdd(&sh.count[at], 1u);
+                            if (by_weight) atomicAdd(&sh.weight[at], weight(v[i]));
+                        }
+                    }
                 }
             });
+            if (begin) {
+                beyond = warp_add(beyond);
+                extra = warp_add(extra);
+                if (lane == 0) {
+                    sh.warp_beyond[warp] = beyond;
+                    atomicAdd(&sh.beyond, beyond + extra);
+                }
+            }
             cluster.sync();
-            for (int i = t; i < kBins; i += blockDim.x) {
-                uint32_t n = 0;
-                unsigned long long w = 0;
-                for (int r = 0; r < ranks; ++r) {
-                    const Shared* other = cluster.map_shared_rank(&sh, r);
-                    n += other->count[turn][i];
-                    if (by_weight) w += other->weight[turn][i];
+            if (rank == 0) {
+                if (begin && warp == 0) {
+                    const unsigned long long w = cluster_sum(cluster, ranks, &sh.beyond, lane);
+                    if (lane == 0) sh.found.above += w;
                 }
-                sh.all_count[i] = n;
-                sh.all_weight[i] = w;
-                // the histogram of the pass before, which nobody reads any more, is the next one's
-                sh.count[turn ^ 1][i] = 0;
-                sh.weight[turn ^ 1][i] = 0;
-            }
-            __syncthreads();
-            if (warp == 0) {
-                // a lane has 16 bins; it reads them from another one on than its neighbours (banks)
-                constexpr int PER = kBins / 32;
-                uint32_t n = 0;
-                unsigned long long w = 0;
-                for (int i = 0; i < PER; ++i) {
-                    const int b = lane * PER + ((i + lane) & (PER - 1));
-                    n += sh.all_count[b];
-                    w += sh.all_weight[b];
-                }
-                const uint32_t n_to = warp_scan(n, lane);
-                const unsigned long long w_to = warp_scan(w, lane);
-                const unsigned here = __ballot_sync(0xFFFFFFFFu, reached(above_count + n_to, above + w_to));
-                if (here == 0) {
-                    if (lane == 0) sh.bin = -1;
-                } else if (lane == __ffs(here) - 1) {
-                    uint32_t cn = above_count + n_to - n;
-                    unsigned long long cw = above + w_to - w;
-                    int b = lane * PER;
-                    for (; b < lane * PER + PER - 1; ++b) {
-                        if (reached(cn + sh.all_count[b], cw + sh.all_weight[b])) break;
-                        cn += sh.all_count[b];
-                        cw += sh.all_weight[b];
+                if (!alone) {
+                    join(by_weight);
+                    find(reached);
+                    if (t == 0) {
+                        sh.found.done = width == 0;
+                        sh.found.tau = high - static_cast<uint32_t>(sh.found.first);
+                        sh.found.equal = sh.found.active;
                     }
-                    sh.bin = b;
-                    sh.above_count = cn;
-                    sh.above = cw;
-                    sh.bin_count = sh.all_count[b];
+                } else {
+                    // the words into this CTA's own memory, and the same search among them
+                    int n = 0;
+                    for (int r = 0; r < ranks; ++r) {
+                        const Shared* other = cluster.map_shared_rank(&sh, r);
+                        const int own = static_cast<int>(min(other->candidates, static_cast<uint32_t>(kWords)));
+                        for (int i = t; i < own && n + i < kWords; i += blockDim.x) sh.words[n + i] = other->active[i];
+                        n = min(n + own, kWords);
+                    }
+                    uint32_t from = low, to = high;
+                    while (true) {
+                        const int w = width_of(to - from);
+                        __syncthreads();
+                        for (int i = t; i < n; i += blockDim.x) {
+                            const uint32_t key = key_of(sh.words[i]);
+                            if (key < from || key > to) continue;
+                            const int at = static_cast<int>((to - key) >> w);
+                            atomicAdd(&sh.count[at], 1u);
+                            if (by_weight) atomicAdd(&sh.weight[at], weight(sh.words[i]));
+                        }
+                        __syncthreads();
+                        find(reached);
+                        const int bin = sh.found.first;
+                        if (w == 0 || bin < 0) {
+                            if (t == 0) {
+                                sh.found.done = 1;
+                                sh.found.tau = to - static_cast<uint32_t>(bin);
+                                sh.found.equal = sh.found.active;
+                            }
+                            break;
+                        }
+                        for (int i = t; i < kBins; i += blockDim.x) {
+                            sh.count[i] = 0;
+                            sh.weight[i] = 0;
+                        }
+                        to -= static_cast<uint32_t>(bin) << w;
+                        const uint32_t span = (1u << w) - 1u;
+                        if (to - from > span) from = to - span;
+                    }
                 }
             }
-            __syncthreads();
-            turn ^= 1;
-            const int found = sh.bin;
-            above = sh.above;
-            above_count = sh.above_count;
-            const uint32_t in_bin = sh.bin_count;
-            __syncthreads();               // sh.bin is written again
-            if (found < 0) return false;   // not reached by all of them
-            if (bin < 0) {
-                // keys of the bin's words: its ends, and more than the roundings of bin_of and of the ends can be
-                bin = found;
-                const float up = static_cast<float>(found) / kBinsPerUnit, down = static_cast<float>(found + 1) / kBinsPerUnit;
-                const float slack = (fabsf(top) + down) * 0x1p-22f;
-                high = found == 0 ? key_of(top) : key_of(canonical(fminf(top, top - up + slack)));
-                low = found == kBins - 1 ? 0u : key_of(canonical(top - down - slack));
-                if (!(top < INFINITY)) {   // an infinite logit stands alone, all others are in the last bin
-                    high = found == 0 ? key_of(top) : key_of(top) - 1u;
-                    low = found == 0 ? high : 0u;
-                }
-            } else if (width == 0) {
-                tau = high - static_cast<uint32_t>(found);
-                equal_all = in_bin;
-                quota = in_bin;
+            publish();
+            begin = false;
+            const int bin = sh.found.first;
+            const bool done = sh.found.done;
+            if (bin < 0) return false;
+            if (done) {
+                tau = sh.found.tau;
+                equal_all = quota = sh.found.equal;
                 return true;
-            } else {
-                high -= static_cast<uint32_t>(found) << width;
-                const uint32_t span = (1u << width) - 1u;
-                if (high - low > span) low = high - span;
             }
-            const uint32_t keys = high - low;
-            width = 0;
-            while ((keys >> width) >= kBins) ++width;
+            high -= static_cast<uint32_t>(bin) << width;
+            const uint32_t span = (1u << width) - 1u;
+            if (high - low > span) low = high - span;
         }
+    };
+    const auto count_bins = [&](float scale) {
+        each([&](int, int, const float (&v)[4]) {
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+                if (v[i] > -INFINITY) atomicAdd(&sh.count[bin_of(v[i], scale)], 1u);
+        });
     };
 
     if (k < p.V) {
-        if (search(false, [&](uint32_t n, unsigned long long) { return n >= static_cast<uint64_t>(k); }, [](uint32_t) { return true; }))
-            quota = static_cast<uint32_t>(k - sh.above_count);
+        const auto reached = [&](uint32_t n, unsigned long long) { return n >= static_cast<uint64_t>(k); };
+        count_bins(kBinsPerUnit);
+        cluster.sync();
+        if (rank == 0) {
+            if (t == 0) { sh.found.above_count = 0; sh.found.above = 0; sh.found.done = 0; }
+            join(false);
+            find(reached);
+            if (t == 0) sh.found.last = sh.found.first;
+        }
+        publish();
+        if (sh.found.first >= 0 && narrow(false, reached, 0, kBinsPerUnit)) quota = static_cast<uint32_t>(k - sh.found.above_count);
+        __syncthreads();
     }
-    __syncthreads();
-    if (top_p < 1.0 && !greedy) {
+    // the weight of the first k: all above tau, and `quota` words of tau's own
+    const bool by_p = sh.top_p < 1.0;
+    unsigned long long mine = 0;
+    if (by_p) {
         const uint32_t tau_k = tau, quota_k = quota, equal_k = equal_all;
-        // the weight of the first k: all above tau, and `quota` times tau's own
-        unsigned long long mine = 0;
-        each([&](int, const float (&v)[kPerThread]) {
+        const float scale = static_cast<float>(slope * kBinsPerUnit);
+        each([&](int, int, const float (&v)[4]) {
 #pragma unroll
-            for (int i = 0; i < kPerThread; ++i)
-                if (key_of(v[i]) > tau_k) mine += weight(v[i]);
+            for (int i = 0; i < 4; ++i) {
+                const uint32_t key = key_of(v[i]);
+                if (key < tau_k || v[i] == -INFINITY) continue;
+                atomicAdd(&sh.count[bin_of(v[i], scale)], 1u);
+                if (key > tau_k) mine += weight(v[i]);
+            }
         });
         mine = warp_add(mine);
         if (lane == 0) sh.warp_total[warp] = mine;
@@ -334,15 +645,51 @@ __global__ void __launch_bounds__(kMostThreads, 1) sample_kernel(const SamplePar
             if (lane == 0) sh.total = mine;
         }
         cluster.sync();
-        unsigned long long sum = 0;
-        for (int r = 0; r < ranks; ++r) sum += *cluster.map_shared_rank(&sh.total, r);
-        const unsigned long long at_tau = tau_k ? weight(of_key(tau_k)) : 0ull;
-        const double whole = static_cast<double>(sum + quota_k * at_tau), goal = top_p > 0.0 ? top_p * whole : 0.0;
-        // the words that equal tau count all here: where they take the sum to the goal, `quota` is cut below
-        const bool found = search(true, [&](uint32_t n, unsigned long long w) { return n > 0 && static_cast<double>(w) >= goal; }, [&](uint32_t key) { return key >= tau_k; });
+        if (rank == 0) {
+            if (warp == 0) {
+                const unsigned long long sum = cluster_sum(cluster, ranks, &sh.total, lane);
+                if (lane == 0) { sh.all = sum; sh.found.above_count = 0; sh.found.above = 0; sh.found.done = 0; }
+            }
+            join(false);
+            const unsigned long long sum = sh.all, at_tau = tau_k ? weight(of_key(tau_k)) : 0ull;
+            const double top_p = sh.top_p, goal = top_p > 0.0 ? top_p * static_cast<double>(sum + quota_k * at_tau) : 0.0;
+            // What the words of bin b weigh together: their count times what its ends weigh, a little more or less for bin_of's roundings and
+            // the weights' own.  All words at tau count here, kept or not: the sum of all is `sum` and their weight.
+            const double one = static_cast<double>(1ull << p.shift), all = static_cast<double>(sum + equal_k * at_tau);
+            const auto most_of = [&](int b) { return sh.count[b] * (one * exp2f(static_cast<float>(b) / -kBinsPerUnit) * 1.0001 + 1.0); };
+            const auto least_of = [&](int b) {
+                return b == kBins - 1 ? 0.0 : sh.count[b] * fmax(one * exp2f(static_cast<float>(b + 1) / -kBinsPerUnit) * 0.9999 - 1.0, 0.0);
+            };
+            spans([&](int b, int span) {
+                const double most = warp_add(most_of(b)), least = warp_add(least_of(b));
+                if (lane == 0) { sh.span_most[span] = most; sh.span_least[span] = least; }
+            });
+            if (t == 0) { sh.found.first = sh.found.last = kBins - 1; sh.found.active = 0; }
+            __syncthreads();
+            spans([&](int b, int span) {
+                const double most_span = lane < kSpans ? sh.span_most[lane] : 0.0, least_span = lane < kSpans ? sh.span_least[lane] : 0.0;
+                const double most_all = warp_add(most_span), least_all = warp_add(least_span);
+                const double most = warp_add(lane < span ? most_span : 0.0) + warp_scan(most_of(b), lane);
+                const double least = warp_add(lane < span ? least_span : 0.0) + warp_scan(least_of(b), lane);
+                // the sum up to bin b, from above and as all but what is below it: may it, and must it have reached the goal?
+                const double up = fmin(most, all - (least_all - least) * (1.0 - 1e-9)), down = fmax(least, all - (most_all - most) * (1.0 + 1e-9));
+                if (up >= goal * (1.0 - 1e-9)) atomicMin(&sh.found.first, b);
+                if (down >= goal * (1.0 + 1e-9)) atomicMin(&sh.found.last, b);
+            });
+            __syncthreads();
+            spans([&](int b, int) {
+                const uint32_t n = warp_add(b >= sh.found.first && b <= sh.found.last ? sh.count[b] : 0u);
+                if (lane == 0 && n) atomicAdd(&sh.found.active, n);
+            });
+            if (t == 0) sh.found.goal = goal;
+        }
+        publish();
+        const double goal = sh.found.goal;
+        // (the words above the bins looked at are not counted, but there is one at least in every sum: the bins that can reach the goal begin at a word)
+        const bool found = narrow(true, [&](uint32_t n, unsigned long long w) { return n > 0 && static_cast<double>(w) >= goal; }, tau_k, scale);
         if (found) {
             // of the words at tau, those before which the weight is below the goal
-            const double before = static_cast<double>(sh.above), each_one = static_cast<double>(weight(of_key(tau)));
+            const double before = static_cast<double>(sh.found.above), each_one = static_cast<double>(weight(of_key(tau)));
             const double n = goal > before ? ceil((goal - before) / each_one) : 0.0;
             quota = n < 1.0 ? 1u : n < static_cast<double>(equal_all) ? static_cast<uint32_t>(n) : equal_all;
             if (tau == tau_k && quota > quota_k) quota = quota_k;
@@ -351,7 +698,6 @@ __global__ void __launch_bounds__(kMostThreads, 1) sample_kernel(const SamplePar
             quota = quota_k;
             equal_all = equal_k;
         }
-        __syncthreads();
     }
 
     // ---- the draw
@@ -360,9 +706,9 @@ __global__ void __launch_bounds__(kMostThreads, 1) sample_kernel(const SamplePar
     uint32_t equals_before = 0;
     if (ranked) {
         uint32_t n = 0;
-        each([&](int, const float (&v)[kPerThread]) {
+        each([&](int, int, const float (&v)[4]) {
 #pragma unroll
-            for (int i = 0; i < kPerThread; ++i) n += key_of(v[i]) == tau;
+            for (int i = 0; i < 4; ++i) n += key_of(v[i]) == tau;
         });
         n = warp_add(n);
         if (lane == 0) sh.warp_equal[warp] = n;
@@ -374,44 +720,49 @@ __global__ void __launch_bounds__(kMostThreads, 1) sample_kernel(const SamplePar
             if (lane == 31) sh.equal = to;
         }
         cluster.sync();
-        for (int r = 0; r < rank; ++r) equals_before += *cluster.map_shared_rank(&sh.equal, r);
+        if (warp == 0) {
+            n = cluster_sum(cluster, rank, &sh.equal, lane);
+            if (lane == 0) sh.joined = n;
+        }
+        __syncthreads();
+        equals_before = sh.joined;
         equals_before += sh.warp_equal[warp];
     }
-    // f(chunk, vector, weights of its elements) over the warp's vectors in the words' order, weight 0 for what is not kept
-    constexpr int VEC = Row<T>::VEC, NV = Row<T>::NV;
-    const auto walk = [&](auto&& f) {
+    // f(chunk, vector, weights of its elements) over this lane's vectors in the words' order, weight 0 for what is not kept.  skip: words of keys
+    // above it are left out.
+    const bool by_depth = sh.deepest < INFINITY;
+    const auto walk = [&](uint32_t skip, auto&& f) {
         uint32_t before = equals_before;
-        each([&](int c, const float (&v)[kPerThread]) {
+        each([&](int c, int j, const float (&v)[4]) {
+            uint32_t rank_here = 0;
+            if (ranked) {
+                uint32_t n = 0;
 #pragma unroll
-            for (int j = 0; j < NV; ++j) {
-                uint32_t rank_here = 0;
-                if (ranked) {
-                    uint32_t n = 0;
-#pragma unroll
-                    for (int e = 0; e < VEC; ++e) n += key_of(v[j * VEC + e]) == tau;
+                for (int e = 0; e < 4; ++e) n += key_of(v[e]) == tau;
+                if (__any_sync(0xFFFFFFFFu, n > 0)) {
                     const uint32_t to = warp_scan(n, lane);
                     rank_here = before + to - n;
                     before += __shfl_sync(0xFFFFFFFFu, to, 31);
                 }
-                unsigned long long w[VEC];
-#pragma unroll
-                for (int e = 0; e < VEC; ++e) {
-                    const float l = v[j * VEC + e];
-                    const uint32_t key = key_of(l);
-                    bool in = key > tau;
-                    if (key == tau) in = !ranked || rank_here++ < quota;
-                    w[e] = in && l > -INFINITY && depth(l) <= deepest ? weight(l) : 0ull;
-                }
-                f(c, j, w);
             }
+            unsigned long long w[4];
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                const uint32_t key = key_of(v[e]);
+                bool in = key > tau;
+                if (key == tau) in = !ranked || rank_here++ < quota;
+                in = in && key <= skip && v[e] > -INFINITY;
+                if (by_depth && in) in = depth(v[e]) <= sh.deepest;
+                w[e] = in ? weight(v[e]) : 0ull;
+            }
+            f(c, j, w);
         });
     };
-    unsigned long long mine = 0;
-    walk([&](int, int, const unsigned long long (&w)[VEC]) {
-#pragma unroll
-        for (int e = 0; e < VEC; ++e) mine += w[e];
-    });
-    mine = warp_add(mine);
+    mine = 0;
+    // (what lies above the bins that top-p's border was looked for in has been added up there)
+    const bool summed = by_p && !by_depth && whole_above != 0xFFFFFFFFu;
+    walk(summed ? whole_above : 0xFFFFFFFFu, [&](int, int, const unsigned long long (&w)[4]) { mine += w[0] + w[1] + (w[2] + w[3]); });
+    mine = warp_add(mine) + (summed ? sh.warp_beyond[warp] : 0ull);
     if (lane == 0) sh.warp_total[warp] = mine;
     __syncthreads();
     if (warp == 0) {
@@ -420,37 +771,32 @@ __global__ void __launch_bounds__(kMostThreads, 1) sample_kernel(const SamplePar
         if (lane == 31) sh.total = to;
     }
     cluster.sync();
-    unsigned long long base = 0, all = 0;
-    for (int r = 0; r < ranks; ++r) {
-        const unsigned long long v = *cluster.map_shared_rank(&sh.total, r);
-        if (r < rank) base += v;
-        all += v;
+    if (warp == 0) {
+        const unsigned long long own = lane < ranks ? *cluster.map_shared_rank(&sh.total, lane) : 0ull;
+        const unsigned long long before = warp_add(lane < rank ? own : 0ull), sum = warp_add(own);
+        if (lane == 0) { sh.base = before; sh.all = sum; }
     }
+    __syncthreads();
+    const unsigned long long all = sh.all;
+    unsigned long long base = sh.base;
     base += sh.warp_total[warp];
-    // the first word whose sum exceeds u * all: at least `target`
-    if (!(u > 0.0)) u = 0.0;
-    const double at = u * static_cast<double>(all);
-    const unsigned long long target = (at < static_cast<double>(all) ? min(static_cast<unsigned long long>(at), all - 1) : all - 1) + 1;
+    const unsigned long long target = target_of(all);
     if (base < target && target <= base + mine) {                // this warp has it
         unsigned long long before = base;
         bool done = false;
-        walk([&](int c, int j, const unsigned long long (&w)[VEC]) {
-            unsigned long long own = 0;
-#pragma unroll
-            for (int e = 0; e < VEC; ++e) own += w[e];
+        walk(0xFFFFFFFFu, [&](int c, int j, const unsigned long long (&w)[4]) {
+            const unsigned long long own = w[0] + w[1] + (w[2] + w[3]);
             const unsigned long long to = warp_scan(own, lane) + before;
             before = __shfl_sync(0xFFFFFFFFu, to, 31);
             if (!done && to >= target && to - own < target) {
-                unsigned long long run = to - own;
-                int word = 0;
-                unsigned long long its = 0;
-                bool found = false;
+                unsigned long long run = to - own, its = 0;
+                int word = -1;
 #pragma unroll
-                for (int e = 0; e < VEC; ++e) {
+                for (int e = 0; e < 4; ++e) {
                     run += w[e];
-                    if (!found && run >= target) { found = true; word = e; its = w[e]; }
+                    if (word < 0 && run >= target) { word = e; its = w[e]; }
                 }
-                p.tokens[m] = row.word(c, j, word);
+                p.tokens[m] = row.word(c, j, lane, word);
                 if (p.probs) p.probs[m] = static_cast<float>(static_cast<double>(its) / static_cast<double>(all));
                 done = true;
             }
@@ -464,19 +810,27 @@ bool aligned_to(const void* p, int64_t bytes) { return reinterpret_cast<uintptr_
 
 template <class T>
 cudaError_t launch(SampleParams p, cudaStream_t st) {
-    const int64_t positions = p.V + 16 / static_cast<int64_t>(sizeof(T)) - 1;       // a row may start inside a vector
+    // a row may start inside a vector
+    const bool aligned = atb::aligned16(p.logits) && (p.M == 1 || p.ld * static_cast<int64_t>(sizeof(T)) % 16 == 0);
+    const int64_t positions = p.V + (aligned ? 0 : 16 / static_cast<int64_t>(sizeof(T)) - 1);
     const int64_t threads = atb::ceil_div(positions, kPerThread);
+    // CTAs per row: what its words need, and more, of 128 threads at least, while the rows leave SMs idle
     int ctas = 1;
-    while (ctas < kMostCtas && threads > static_cast<int64_t>(ctas) * kMostThreads) ctas *= 2;
+    while (ctas < kMostCtas && (threads > static_cast<int64_t>(ctas) * kMostThreads || (p.M * ctas * 2 <= atb::kSmCount && threads >= ctas * 2 * 128))) ctas *= 2;
     p.chunks = static_cast<int>(atb::ceil_div(threads, static_cast<int64_t>(ctas) * kMostThreads));
     int block = static_cast<int>(atb::round_up(atb::ceil_div(threads, static_cast<int64_t>(ctas) * p.chunks), 32));
     if (block < 64) block = 64;
+    p.group = 1;                           // 256 groups at most, in all
+    while (block / p.group * ctas > kMostGroups) p.group *= 2;
     int log2v = 0;
     while ((1ll << log2v) < p.V) ++log2v;
     p.shift = 62 - log2v < 45 ? 62 - log2v : 45;
     const unsigned grid = static_cast<unsigned>(p.M * ctas);
-    return p.chunks == 1 ? atb::launch_dependent(sample_kernel<T, true>, grid, static_cast<unsigned>(block), static_cast<unsigned>(ctas), 0, st, p)
-                         : atb::launch_dependent(sample_kernel<T, false>, grid, static_cast<unsigned>(block), static_cast<unsigned>(ctas), 0, st, p);
+    const size_t smem = static_cast<size_t>(block) * kPerThread * sizeof(float);
+    auto kernel = p.chunks == 1 ? sample_kernel<T, true> : sample_kernel<T, false>;
+    const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kMostThreads * kPerThread * static_cast<int>(sizeof(float)));
+    if (e != cudaSuccess) return e;
+    return atb::launch_dependent(kernel, grid, static_cast<unsigned>(block), static_cast<unsigned>(ctas), smem, st, p);
 }
 
 }  // namespace

@@ -162,7 +162,7 @@ def test_masked_and_infinite_logits(V, dtype):
     x[11] = x[11] * 1e30
     x[12, 5:] = -INF
     for s in (dict(), dict(top_k=4), dict(top_p=0.6), dict(top_k=30, top_p=0.8, min_p=0.01), dict(temperature=0.0), dict(temperature=INF), dict(temperature=1e-4), dict(min_p=1.0),
-              dict(temperature=INF, top_k=9), dict(temperature=1e30, top_p=0.5)):
+              dict(temperature=INF, top_k=9), dict(temperature=1e30, top_p=0.5), dict(temperature=1e38, top_p=0.7), dict(temperature=1e38, top_k=V // 3)):
         tokens, probs = compare(x, u, **s)
         assert tokens[:3].tolist() == [-1, -1, V // 2] and probs[:3].tolist() == [0.0, 0.0, 1.0]
 
