@@ -9,7 +9,7 @@
 // those that equal it.
 //   few words at most (small k): the k-th largest of 256 groups' largest logits is below the k-th largest logit, so that the words that reach
 //     it are few (about 60 for k = 50): one CTA ranks those and draws
-//   else tau is found by histograms over ever narrower ranges of logits (512 bins: first of equal width, then of the numbers' ordered bit
+//   else tau is found by histograms over ever narrower ranges of logits (1024 bins: first of equal width, then of the numbers' ordered bit
 //     patterns, down to one number), of counts for top-k; for top-p a first histogram of counts bounds the weight in its bins, so that only
 //     the few bins that the border may be in are looked at word by word
 // A cluster of CTAs takes a row, 32 logits a thread in shared memory: the row is read from memory once, and histograms and sums are
@@ -28,8 +28,8 @@ namespace {
 
 namespace cg = cooperative_groups;
 
-constexpr int kVectors = 8, kPerThread = 4 * kVectors, kBins = 512, kMostCtas = 8, kMostThreads = 512, kMostWarps = kMostThreads / 32;
-constexpr float kBinsPerUnit = 16.f;       // of the first pass: 32 units below the largest logit, what lies below in the last bin
+constexpr int kVectors = 8, kPerThread = 4 * kVectors, kBins = 1024, kMostCtas = 8, kMostThreads = 512, kMostWarps = kMostThreads / 32;
+constexpr float kBinsPerUnit = 32.f;       // of the first pass: 32 units below the largest logit, what lies below in the last bin
 
 // A setting: of every row, or one for all.
 struct Setting {
@@ -44,7 +44,8 @@ struct SampleParams {
     Setting temperature, top_k, top_p, min_p;      // rows: float, int32, float, float
     int64_t* tokens;
     float* probs;
-    int chunks, shift;                             // pieces of 32 logits per thread; S
+    int chunks, shift;                             // pieces of 4 * vectors logits per thread; S
+    int vectors;                                   // even
     int group;                                     // lanes that share a largest logit
 };
 constexpr int kMostGroups = 256, kCandidates = 512, kWords = 2048, kSpans = kBins / 32;
@@ -72,16 +73,18 @@ struct Shared {
     };
     union {                                        // this CTA's
         Candidate candidate[kCandidates];
-        float active[kWords];
+        Candidate active[kWords];
     };
-    uint32_t candidates;                           // of either
+    uint32_t candidates, listed;                   // of either; of the last list
     uint32_t count[kBins];                         // histogram
     unsigned long long weight[kBins];
     uint32_t span_count[kSpans];                   // sums over 32 bins
     unsigned long long span_weight[kSpans];
     double span_most[kSpans], span_least[kSpans];
     Found found;
-    unsigned long long beyond;                     // weight above the bins looked at
+    unsigned long long beyond, whole;              // weight above the bins looked at, of all words
+    double real;                                   // this CTA's weight, about
+    double warp_real[kMostWarps];
     float group_top[kMostGroups];                  // this CTA's groups' largest logits
     float all_groups[kMostGroups];
     float floor;
@@ -91,6 +94,7 @@ struct Shared {
     unsigned long long base, all;                  // that of the CTAs before this one, of all
     uint32_t equal;                                // this CTA's words at tau
     uint32_t joined;                               // a sum over the cluster
+    uint32_t ends[kMostCtas];                      // of the CTAs' words in the first one's list
     unsigned long long warp_total[kMostWarps];
     unsigned long long warp_beyond[kMostWarps];
     uint32_t warp_equal[kMostWarps];
@@ -108,24 +112,24 @@ __device__ __forceinline__ float of_key(uint32_t k) { return __uint_as_float(k &
 // -inf for NaN, and +0 for -0, which compare alike.
 __device__ __forceinline__ float canonical(float l) { return l == l ? l + 0.f : -INFINITY; }
 
-// A warp's logits: chunks of 32 x 32 consecutive words, in shared memory as vectors of 4, vector j of lane i at words 128 j + 4 i of the chunk.
+// A warp's logits: chunks of 128 * vectors consecutive words, in shared memory as vectors of 4, vector j of lane i at words 128 j + 4 i of the chunk.
 template <class T>
 struct Row {
     const T* row;
-    int V, first;                          // first: word of the warp's first logit (may lie before the row)
+    int V, vectors, first;                 // first: word of the warp's first logit (may lie before the row)
     // word of element e of this lane's vector j of chunk c
-    __device__ __forceinline__ int word(int c, int j, int lane, int e) const { return first + c * (32 * kPerThread) + j * 128 + lane * 4 + e; }
+    __device__ __forceinline__ int word(int c, int j, int lane, int e) const { return first + (c * vectors + j) * 128 + lane * 4 + e; }
     // Chunk c to `to`, this warp's place.  Vectors of 16 bytes that lie inside the row are loaded whole.
     __device__ __forceinline__ void load(int c, float4* to, int lane) const {
-        constexpr int PER = 16 / sizeof(T), LOADS = kPerThread / PER;
-        const int from = first + c * (32 * kPerThread) + lane * PER;
+        constexpr int PER = 16 / sizeof(T), AT_ONCE = 16 / PER, STEP = AT_ONCE * PER / 4;      // loads in flight, of STEP vectors
+        const int from = first + c * vectors * 128 + lane * PER;
         __syncwarp();                      // the warp has read the chunk before
+#pragma unroll 1
+        for (int j = 0; j < vectors; j += STEP) {
+            uint4 q[AT_ONCE];
 #pragma unroll
-        for (int half = 0; half < 2; ++half) {
-            uint4 q[LOADS / 2];
-#pragma unroll
-            for (int i = 0; i < LOADS / 2; ++i) {
-                const int at = from + (half * (LOADS / 2) + i) * 32 * PER;
+            for (int i = 0; i < AT_ONCE; ++i) {
+                const int at = j + i * PER / 4 < vectors ? from + j * 128 + i * 32 * PER : V;
                 if (at >= 0 && at <= V - PER) {
                     q[i] = __ldg(reinterpret_cast<const uint4*>(row + at));
                 } else {
@@ -143,10 +147,10 @@ struct Row {
                 }
             }
 #pragma unroll
-            for (int i = 0; i < LOADS / 2; ++i) {
+            for (int i = 0; i < AT_ONCE; ++i) {
+                if (j + i * PER / 4 >= vectors) continue;
                 const uint32_t w[4] = {q[i].x, q[i].y, q[i].z, q[i].w};
-                const int at = (half * (LOADS / 2) + i) * 32 * PER + lane * PER;       // word of the chunk
-                float4* const dst = to + at / 4;
+                float4* const dst = to + (j * 128 + i * 32 * PER + lane * PER) / 4;
                 if constexpr (sizeof(T) == 4) {
                     *dst = make_float4(canonical(__uint_as_float(w[0])), canonical(__uint_as_float(w[1])), canonical(__uint_as_float(w[2])), canonical(__uint_as_float(w[3])));
                 } else {
@@ -201,7 +205,7 @@ __device__ __forceinline__ V cluster_sum(const cg::cluster_group& cluster, int r
 template <class T, bool RESIDENT>
 __global__ void __launch_bounds__(kMostThreads, 2) sample_kernel(const SampleParams p) {
     __shared__ Shared sh;
-    extern __shared__ float4 logits[];     // [warps][32 kVectors]
+    extern __shared__ float4 logits[];     // [warps][32 vectors]
     cg::cluster_group cluster = cg::this_cluster();
     const int ranks = static_cast<int>(cluster.num_blocks()), rank = static_cast<int>(cluster.block_rank());
     const int64_t m = blockIdx.x / ranks;
@@ -210,7 +214,7 @@ __global__ void __launch_bounds__(kMostThreads, 2) sample_kernel(const SamplePar
         sh.count[i] = 0;
         sh.weight[i] = 0;
     }
-    if (t == 0) { sh.beyond = 0; sh.candidates = 0; }
+    if (t == 0) { sh.beyond = 0; sh.whole = 0; sh.candidates = 0; }
     if (t < 16) sh.table[t] = exp2(t * 0.0625);
     sm100::grid_dependency_wait();
     sm100::grid_dependency_launch();
@@ -221,9 +225,10 @@ __global__ void __launch_bounds__(kMostThreads, 2) sample_kernel(const SamplePar
     {
         // vectors start on 16-byte boundaries: positions are counted from the one at or below the row's first word
         const int64_t skip = static_cast<int64_t>(reinterpret_cast<uintptr_t>(row.row) & 15u) / static_cast<int64_t>(sizeof(T));
-        row.first = (rank * warps + warp) * p.chunks * (32 * kPerThread) - static_cast<int>(skip);
+        row.vectors = p.vectors;
+        row.first = (rank * warps + warp) * p.chunks * p.vectors * 128 - static_cast<int>(skip);
     }
-    float4* const mine4 = logits + warp * 32 * kVectors;
+    float4* const mine4 = logits + warp * 32 * p.vectors;
     if constexpr (RESIDENT) row.load(0, mine4, lane);
     // f(chunk, vector, logits) over this thread's logits in the words' order
     const auto each = [&](auto&& f) {
@@ -231,7 +236,7 @@ __global__ void __launch_bounds__(kMostThreads, 2) sample_kernel(const SamplePar
         for (int c = 0; c < (RESIDENT ? 1 : p.chunks); ++c) {
             if constexpr (!RESIDENT) row.load(c, mine4, lane);
 #pragma unroll 2
-            for (int j = 0; j < kVectors; ++j) {
+            for (int j = 0; j < p.vectors; ++j) {
                 const float4 q = mine4[j * 32 + lane];
                 const float v[4] = {q.x, q.y, q.z, q.w};
                 f(c, j, v);
@@ -296,11 +301,13 @@ __global__ void __launch_bounds__(kMostThreads, 2) sample_kernel(const SamplePar
     const auto depth = [&](float l) { return l == top ? 0.0 : (static_cast<double>(top) - static_cast<double>(l)) * slope; };
     const double slope16 = 16.0 * slope;
     const float slope_f = static_cast<float>(slope);
+    // without branches, so that several run at once
     const auto weight = [&](float l) -> unsigned long long {
-        if (l == top) return 1ull << p.shift;
         // a difference that is too far, infinite or no number weighs nothing (halves: that of two finite numbers is finite)
-        if (!((0.5f * top - 0.5f * l) * slope_f < 0.5f * static_cast<float>(p.shift + 2))) return 0ull;
-        return fixed_exp2(static_cast<double>(top) - static_cast<double>(l), slope16, p.shift, sh.table);
+        const bool some = (0.5f * top - 0.5f * l) * slope_f < 0.5f * static_cast<float>(p.shift + 2);
+        const double d = static_cast<double>(top) - static_cast<double>(some ? l : top);
+        const unsigned long long w = fixed_exp2(d, some ? slope16 : 0.0, p.shift, sh.table);
+        return l == top ? 1ull << p.shift : some ? w : 0ull;
     };
     // the first word whose sum exceeds u * all: at least this much
     const auto target_of = [&](unsigned long long all) {
@@ -338,18 +345,18 @@ __global__ void __launch_bounds__(kMostThreads, 2) sample_kernel(const SamplePar
         });
         cluster.sync();
         if (warp == 0) {
-            const uint32_t n = cluster_sum(cluster, ranks, &sh.candidates, lane);
-            if (lane == 0) sh.joined = n;
+            const uint32_t end = warp_scan(lane < ranks ? *cluster.map_shared_rank(&sh.candidates, lane) : 0u, lane);
+            if (lane < kMostCtas) sh.ends[lane] = end;
         }
         __syncthreads();
-        const uint32_t all = sh.joined;
+        const uint32_t all = sh.ends[kMostCtas - 1];
         if (all <= kCandidates) {
             if (rank == 0) {
                 const int count = static_cast<int>(all);
                 for (int i = t; i < count; i += blockDim.x) {
-                    int r = 0, at = i;
-                    for (uint32_t own; at >= static_cast<int>(own = *cluster.map_shared_rank(&sh.candidates, r)); ++r) at -= static_cast<int>(own);
-                    sh.few.all[i] = cluster.map_shared_rank(&sh, r)->candidate[at];
+                    int r = 0;
+                    while (i >= static_cast<int>(sh.ends[r])) ++r;
+                    sh.few.all[i] = cluster.map_shared_rank(&sh, r)->candidate[i - static_cast<int>(r ? sh.ends[r - 1] : 0u)];
                 }
                 __syncthreads();
                 // in their order, the first k
@@ -468,7 +475,7 @@ __global__ void __launch_bounds__(kMostThreads, 2) sample_kernel(const SamplePar
             sh.count[i] = 0;
             sh.weight[i] = 0;
         }
-        if (t == 0) sh.candidates = 0;
+        if (t == 0) { sh.listed = sh.candidates; sh.candidates = 0; }
         __syncthreads();
     };
     const auto width_of = [](uint32_t keys) {                    // a bin holds 2^width keys
@@ -477,10 +484,10 @@ __global__ void __launch_bounds__(kMostThreads, 2) sample_kernel(const SamplePar
         return width;
     };
     // The first number, from the largest logit down, at which the sum over the words of keys >= `least` reaches its goal, when it is known to lie in
-    // the bins sh.found.first .. last of width 1 / scale, with sh.found.active words.  Weights: the weight above those bins is added up on the way.
-    // Sets tau and equal_all.
-    uint32_t whole_above = 0xFFFFFFFFu;    // keys above it are in the warps' sums of the weight above the bins, sh.warp_beyond
-    const auto narrow = [&](bool by_weight, auto&& reached, uint32_t least, float scale) {
+    // the bins sh.found.first .. last of width 1 / scale, with sh.found.active words.  Sets tau and equal_all.
+    // Weights: every word's weight is made here, once, and added up, of all and of those above those bins; all less `excess`, times top_p, is the goal.
+    bool listed = false;                   // the words in the bins are in the CTAs' lists, the weight above them in sh.warp_beyond
+    const auto narrow = [&](bool by_weight, auto&& reached, uint32_t least, float scale, unsigned long long excess) {
         const int first = sh.found.first, last = sh.found.last;
         // keys of the bins' words: their ends, and more than the roundings of bin_of and of the ends can be
         uint32_t low = 0, high = key_of(top);
@@ -492,52 +499,82 @@ __global__ void __launch_bounds__(kMostThreads, 2) sample_kernel(const SamplePar
         } else if (first == 0 && last == 0 && !(top < INFINITY)) {
             low = high;                    // an infinite logit stands alone
         }
-        bool begin = by_weight;            // the weight above is still to be added up
-        if (by_weight) whole_above = high;
+        bool begin = by_weight;            // the weights are still to be added up
         while (true) {
             const bool alone = sh.found.active <= kWords;        // few enough for the first CTA
             const int width = width_of(high - low);
-            unsigned long long beyond = 0, extra = 0;           // of keys above `high`; of the few below it in earlier bins
-            each([&](int, int, const float (&v)[4]) {
+            unsigned long long beyond = 0, whole = 0;
+            each([&](int c, int j, const float (&v)[4]) {
+                unsigned long long w[4] = {};
+                if (begin) {
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) w[i] = weight(v[i]);
+                }
 #pragma unroll
                 for (int i = 0; i < 4; ++i) {
                     const uint32_t key = key_of(v[i]);
-                    if (key < low || key < least || v[i] == -INFINITY) continue;
-                    if (key > high) {
-                        if (begin) beyond += weight(v[i]);
-                        continue;
-                    }
-                    const int b = bin_of(v[i], scale);
-                    if (b < first) {
-                        if (begin) extra += weight(v[i]);
-                    } else if (b <= last) {
-                        if (alone) {
-                            const uint32_t at = atomicAdd(&sh.candidates, 1u);
-                            if (at < kWords) sh.active[at] = v[i];
-                        } else {
-                            const int at = static_cast<int>((high - key) >> width);
-                            atomicAdd(&sh.count[at], 1u);
-                            if (by_weight) atomicAdd(&sh.weight[at], weight(v[i]));
+                    w[i] = key >= least ? w[i] : 0ull;
+                    whole += w[i];
+                    beyond += key > high ? w[i] : 0ull;
+                    if (key <= high && key >= low && key >= least && v[i] > -INFINITY) {
+                        const int b = bin_of(v[i], scale);
+                        if (b < first) {
+                            beyond += w[i];
+                        } else if (b <= last) {
+                            if (alone) {
+                                const uint32_t at = atomicAdd(&sh.candidates, 1u);
+                                if (at < kWords) sh.active[at] = {v[i], row.word(c, j, lane, i)};
+                            } else {
+                                const int at = static_cast<int>((high - key) >> width);
+                                atomicAdd(&sh.count[at], 1u);
+                                if (by_weight) atomicAdd(&sh.weight[at], begin ? w[i] : weight(v[i]));
+                            }
                         }
                     }
                 }
             });
             if (begin) {
                 beyond = warp_add(beyond);
-                extra = warp_add(extra);
+                whole = warp_add(whole);
                 if (lane == 0) {
                     sh.warp_beyond[warp] = beyond;
-                    atomicAdd(&sh.beyond, beyond + extra);
+                    atomicAdd(&sh.beyond, beyond);
+                    atomicAdd(&sh.whole, whole);
                 }
+                listed = alone;
             }
             cluster.sync();
             if (rank == 0) {
-                if (begin && warp == 0) {
-                    const unsigned long long w = cluster_sum(cluster, ranks, &sh.beyond, lane);
-                    if (lane == 0) sh.found.above += w;
-                }
+                int n = 0;
                 if (!alone) {
                     join(by_weight);
+                } else {
+                    // the words into this CTA's own memory
+                    if (warp == 0) {
+                        const uint32_t own = lane < ranks ? min(*cluster.map_shared_rank(&sh.candidates, lane), static_cast<uint32_t>(kWords)) : 0u;
+                        const uint32_t end = warp_scan(own, lane);
+                        if (lane < kMostCtas) sh.ends[lane] = end;
+                    }
+                    __syncthreads();
+                    n = static_cast<int>(min(sh.ends[kMostCtas - 1], static_cast<uint32_t>(kWords)));
+                    for (int i = t; i < n; i += blockDim.x) {
+                        int r = 0;
+                        while (i >= static_cast<int>(sh.ends[r])) ++r;
+                        sh.words[i] = cluster.map_shared_rank(&sh, r)->active[i - static_cast<int>(r ? sh.ends[r - 1] : 0u)].l;
+                    }
+                    __syncthreads();
+                }
+                if (begin) {
+                    if (warp == 0) {
+                        const unsigned long long up = cluster_sum(cluster, ranks, &sh.beyond, lane), all = cluster_sum(cluster, ranks, &sh.whole, lane);
+                        if (lane == 0) {
+                            sh.found.above += up;
+                            sh.found.goal = sh.top_p > 0.0 ? sh.top_p * static_cast<double>(all - excess) : 0.0;
+                        }
+                    }
+                    __syncthreads();
+                }
+                if (!alone) {
                     find(reached);
                     if (t == 0) {
                         sh.found.done = width == 0;
@@ -545,18 +582,10 @@ __global__ void __launch_bounds__(kMostThreads, 2) sample_kernel(const SamplePar
                         sh.found.equal = sh.found.active;
                     }
                 } else {
-                    // the words into this CTA's own memory, and the same search among them
-                    int n = 0;
-                    for (int r = 0; r < ranks; ++r) {
-                        const Shared* other = cluster.map_shared_rank(&sh, r);
-                        const int own = static_cast<int>(min(other->candidates, static_cast<uint32_t>(kWords)));
-                        for (int i = t; i < own && n + i < kWords; i += blockDim.x) sh.words[n + i] = other->active[i];
-                        n = min(n + own, kWords);
-                    }
+                    // the same search among the words
                     uint32_t from = low, to = high;
                     while (true) {
                         const int w = width_of(to - from);
-                        __syncthreads();
                         for (int i = t; i < n; i += blockDim.x) {
                             const uint32_t key = key_of(sh.words[i]);
                             if (key < from || key > to) continue;
@@ -582,6 +611,7 @@ __global__ void __launch_bounds__(kMostThreads, 2) sample_kernel(const SamplePar
                         to -= static_cast<uint32_t>(bin) << w;
                         const uint32_t span = (1u << w) - 1u;
                         if (to - from > span) from = to - span;
+                        __syncthreads();
                     }
                 }
             }
@@ -619,43 +649,51 @@ __global__ void __launch_bounds__(kMostThreads, 2) sample_kernel(const SamplePar
             if (t == 0) sh.found.last = sh.found.first;
         }
         publish();
-        if (sh.found.first >= 0 && narrow(false, reached, 0, kBinsPerUnit)) quota = static_cast<uint32_t>(k - sh.found.above_count);
+        if (sh.found.first >= 0 && narrow(false, reached, 0, kBinsPerUnit, 0)) quota = static_cast<uint32_t>(k - sh.found.above_count);
         __syncthreads();
     }
-    // the weight of the first k: all above tau, and `quota` words of tau's own
+    // top-p: among the words from tau on
     const bool by_p = sh.top_p < 1.0;
     unsigned long long mine = 0;
     if (by_p) {
         const uint32_t tau_k = tau, quota_k = quota, equal_k = equal_all;
         const float scale = static_cast<float>(slope * kBinsPerUnit);
+        // their weight, about, and how many there are in bins of depth
+        double sum = 0.0;
         each([&](int, int, const float (&v)[4]) {
+            float some = 0.f;
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
-                const uint32_t key = key_of(v[i]);
-                if (key < tau_k || v[i] == -INFINITY) continue;
-                atomicAdd(&sh.count[bin_of(v[i], scale)], 1u);
-                if (key > tau_k) mine += weight(v[i]);
+                const bool in = key_of(v[i]) >= tau_k && v[i] > -INFINITY;
+                const float y = (0.5f * top - 0.5f * v[i]) * (2.f * slope_f);
+                float w;
+                asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(w) : "f"(-y));
+                some += in && y < 120.f ? w : 0.f;
+                if (in) atomicAdd(&sh.count[bin_of(v[i], scale)], 1u);
             }
+            sum += static_cast<double>(some);
         });
-        mine = warp_add(mine);
-        if (lane == 0) sh.warp_total[warp] = mine;
+        const double about = warp_add(sum);
+        if (lane == 0) sh.warp_real[warp] = about;
         __syncthreads();
         if (warp == 0) {
-            mine = warp_add(lane < warps ? sh.warp_total[lane] : 0ull);
-            if (lane == 0) sh.total = mine;
+            const double all = warp_add(lane < warps ? sh.warp_real[lane] : 0.0);
+            if (lane == 0) sh.real = all;
         }
+        const unsigned long long at_tau = tau_k ? weight(of_key(tau_k)) : 0ull, excess = (equal_k - quota_k) * at_tau;
         cluster.sync();
         if (rank == 0) {
             if (warp == 0) {
-                const unsigned long long sum = cluster_sum(cluster, ranks, &sh.total, lane);
-                if (lane == 0) { sh.all = sum; sh.found.above_count = 0; sh.found.above = 0; sh.found.done = 0; }
+                const double sum_all = cluster_sum(cluster, ranks, &sh.real, lane);
+                if (lane == 0) { sh.real = sum_all; sh.found.above_count = 0; sh.found.above = 0; sh.found.done = 0; }
             }
             join(false);
-            const unsigned long long sum = sh.all, at_tau = tau_k ? weight(of_key(tau_k)) : 0ull;
-            const double top_p = sh.top_p, goal = top_p > 0.0 ? top_p * static_cast<double>(sum + quota_k * at_tau) : 0.0;
-            // What the words of bin b weigh together: their count times what its ends weigh, a little more or less for bin_of's roundings and
-            // the weights' own.  All words at tau count here, kept or not: the sum of all is `sum` and their weight.
-            const double one = static_cast<double>(1ull << p.shift), all = static_cast<double>(sum + equal_k * at_tau);
+            // What the words of bin b weigh together: their count times what its ends weigh, a little more or less for bin_of's roundings and the
+            // weights' own.  The sum of all is within 1e-4 of what was added up (FP32: 2^-18 where y is 47), but where the largest logit
+            // is infinite, or differences are too small for FP32: there the bins say nothing, and all words are looked at.
+            const double one = static_cast<double>(1ull << p.shift), all = sh.real * one, low_all = all * (1.0 - 1e-4), high_all = all * (1.0 + 1e-4);
+            const bool known = top < INFINITY && scale > 1e-30f && scale < 1e30f;
+            const double cut = static_cast<double>(excess), low_goal = sh.top_p * fmax(low_all - cut, 0.0), high_goal = sh.top_p * fmax(high_all - cut, 0.0);
             const auto most_of = [&](int b) { return sh.count[b] * (one * exp2f(static_cast<float>(b) / -kBinsPerUnit) * 1.0001 + 1.0); };
             const auto least_of = [&](int b) {
                 return b == kBins - 1 ? 0.0 : sh.count[b] * fmax(one * exp2f(static_cast<float>(b + 1) / -kBinsPerUnit) * 0.9999 - 1.0, 0.0);
@@ -664,29 +702,29 @@ __global__ void __launch_bounds__(kMostThreads, 2) sample_kernel(const SamplePar
                 const double most = warp_add(most_of(b)), least = warp_add(least_of(b));
                 if (lane == 0) { sh.span_most[span] = most; sh.span_least[span] = least; }
             });
-            if (t == 0) { sh.found.first = sh.found.last = kBins - 1; sh.found.active = 0; }
+            if (t == 0) { sh.found.first = known ? kBins - 1 : 0; sh.found.last = kBins - 1; sh.found.active = 0; }
             __syncthreads();
-            spans([&](int b, int span) {
-                const double most_span = lane < kSpans ? sh.span_most[lane] : 0.0, least_span = lane < kSpans ? sh.span_least[lane] : 0.0;
-                const double most_all = warp_add(most_span), least_all = warp_add(least_span);
-                const double most = warp_add(lane < span ? most_span : 0.0) + warp_scan(most_of(b), lane);
-                const double least = warp_add(lane < span ? least_span : 0.0) + warp_scan(least_of(b), lane);
-                // the sum up to bin b, from above and as all but what is below it: may it, and must it have reached the goal?
-                const double up = fmin(most, all - (least_all - least) * (1.0 - 1e-9)), down = fmax(least, all - (most_all - most) * (1.0 + 1e-9));
-                if (up >= goal * (1.0 - 1e-9)) atomicMin(&sh.found.first, b);
-                if (down >= goal * (1.0 + 1e-9)) atomicMin(&sh.found.last, b);
-            });
+            if (known)
+                spans([&](int b, int span) {
+                    const double most_span = lane < kSpans ? sh.span_most[lane] : 0.0, least_span = lane < kSpans ? sh.span_least[lane] : 0.0;
+                    const double most_all = warp_add(most_span), least_all = warp_add(least_span);
+                    const double most = warp_add(lane < span ? most_span : 0.0) + warp_scan(most_of(b), lane);
+                    const double least = warp_add(lane < span ? least_span : 0.0) + warp_scan(least_of(b), lane);
+                    // the sum up to bin b, from above and as all but what is below it: may it, and must it have reached the goal?
+                    const double up = fmin(most, high_all - (least_all - least) * (1.0 - 1e-9)), down = fmax(least, low_all - (most_all - most) * (1.0 + 1e-9));
+                    if (up >= low_goal * (1.0 - 1e-9)) atomicMin(&sh.found.first, b);
+                    if (down >= high_goal * (1.0 + 1e-9)) atomicMin(&sh.found.last, b);
+                });
             __syncthreads();
             spans([&](int b, int) {
                 const uint32_t n = warp_add(b >= sh.found.first && b <= sh.found.last ? sh.count[b] : 0u);
                 if (lane == 0 && n) atomicAdd(&sh.found.active, n);
             });
-            if (t == 0) sh.found.goal = goal;
         }
         publish();
-        const double goal = sh.found.goal;
         // (the words above the bins looked at are not counted, but there is one at least in every sum: the bins that can reach the goal begin at a word)
-        const bool found = narrow(true, [&](uint32_t n, unsigned long long w) { return n > 0 && static_cast<double>(w) >= goal; }, tau_k, scale);
+        const bool found = narrow(true, [&](uint32_t n, unsigned long long w) { return n > 0 && static_cast<double>(w) >= sh.found.goal; }, tau_k, scale, excess);
+        const double goal = sh.found.goal;
         if (found) {
             // of the words at tau, those before which the weight is below the goal
             const double before = static_cast<double>(sh.found.above), each_one = static_cast<double>(weight(of_key(tau)));
@@ -728,10 +766,9 @@ __global__ void __launch_bounds__(kMostThreads, 2) sample_kernel(const SamplePar
         equals_before = sh.joined;
         equals_before += sh.warp_equal[warp];
     }
-    // f(chunk, vector, weights of its elements) over this lane's vectors in the words' order, weight 0 for what is not kept.  skip: words of keys
-    // above it are left out.
+    // f(chunk, vector, weights of its elements) over this lane's vectors in the words' order, weight 0 for what is not kept.
     const bool by_depth = sh.deepest < INFINITY;
-    const auto walk = [&](uint32_t skip, auto&& f) {
+    const auto walk = [&](auto&& f) {
         uint32_t before = equals_before;
         each([&](int c, int j, const float (&v)[4]) {
             uint32_t rank_here = 0;
@@ -745,24 +782,43 @@ __global__ void __launch_bounds__(kMostThreads, 2) sample_kernel(const SamplePar
                     before += __shfl_sync(0xFFFFFFFFu, to, 31);
                 }
             }
-            unsigned long long w[4];
+            unsigned long long w[4] = {};
+            bool in[4], some = false;
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
                 const uint32_t key = key_of(v[e]);
-                bool in = key > tau;
-                if (key == tau) in = !ranked || rank_here++ < quota;
-                in = in && key <= skip && v[e] > -INFINITY;
-                if (by_depth && in) in = depth(v[e]) <= sh.deepest;
-                w[e] = in ? weight(v[e]) : 0ull;
+                in[e] = key > tau;
+                if (key == tau) in[e] = !ranked || rank_here++ < quota;
+                in[e] = in[e] && v[e] > -INFINITY;
+                if (by_depth && in[e]) in[e] = depth(v[e]) <= sh.deepest;
+                some = some || in[e];
+            }
+            if (__any_sync(0xFFFFFFFFu, some)) {
+#pragma unroll
+                for (int e = 0; e < 4; ++e) w[e] = weight(v[e]);
+#pragma unroll
+                for (int e = 0; e < 4; ++e) w[e] = in[e] ? w[e] : 0ull;
             }
             f(c, j, w);
         });
     };
     mine = 0;
-    // (what lies above the bins that top-p's border was looked for in has been added up there)
-    const bool summed = by_p && !by_depth && whole_above != 0xFFFFFFFFu;
-    walk(summed ? whole_above : 0xFFFFFFFFu, [&](int, int, const unsigned long long (&w)[4]) { mine += w[0] + w[1] + (w[2] + w[3]); });
-    mine = warp_add(mine) + (summed ? sh.warp_beyond[warp] : 0ull);
+    if (by_p && listed && !by_depth && !ranked) {
+        // what lies above the bins that top-p's border was looked for in has been added up there; those in them are listed
+        if (lane == 0) sh.warp_total[warp] = sh.warp_beyond[warp];
+        __syncthreads();
+        const int per_warp = p.chunks * p.vectors * 128, base = row.first - warp * per_warp;
+        for (int i = t; i < static_cast<int>(sh.listed); i += blockDim.x) {
+            const Candidate one = sh.active[i];
+            if (key_of(one.l) >= tau) atomicAdd(&sh.warp_total[(one.word - base) / per_warp], weight(one.l));
+        }
+        __syncthreads();
+        mine = sh.warp_total[warp];
+        __syncthreads();                   // sh.warp_total is written again
+    } else {
+        walk([&](int, int, const unsigned long long (&w)[4]) { mine += w[0] + w[1] + (w[2] + w[3]); });
+        mine = warp_add(mine);
+    }
     if (lane == 0) sh.warp_total[warp] = mine;
     __syncthreads();
     if (warp == 0) {
@@ -784,7 +840,7 @@ __global__ void __launch_bounds__(kMostThreads, 2) sample_kernel(const SamplePar
     if (base < target && target <= base + mine) {                // this warp has it
         unsigned long long before = base;
         bool done = false;
-        walk(0xFFFFFFFFu, [&](int c, int j, const unsigned long long (&w)[4]) {
+        walk([&](int c, int j, const unsigned long long (&w)[4]) {
             const unsigned long long own = w[0] + w[1] + (w[2] + w[3]);
             const unsigned long long to = warp_scan(own, lane) + before;
             before = __shfl_sync(0xFFFFFFFFu, to, 31);
@@ -813,12 +869,17 @@ cudaError_t launch(SampleParams p, cudaStream_t st) {
     // a row may start inside a vector
     const bool aligned = atb::aligned16(p.logits) && (p.M == 1 || p.ld * static_cast<int64_t>(sizeof(T)) % 16 == 0);
     const int64_t positions = p.V + (aligned ? 0 : 16 / static_cast<int64_t>(sizeof(T)) - 1);
-    const int64_t threads = atb::ceil_div(positions, kPerThread);
-    // CTAs per row: what its words need, and more, of 128 threads at least, while the rows leave SMs idle
+    // CTAs per row: what its words need, and more, of 1024 words at least, while the rows leave SMs idle.  Vectors per thread: as many as there
+    // are where the SMs are full (what a warp does once per pass counts for more words), else as few as fill the threads.
     int ctas = 1;
-    while (ctas < kMostCtas && (threads > static_cast<int64_t>(ctas) * kMostThreads || (p.M * ctas * 2 <= atb::kSmCount && threads >= ctas * 2 * 128))) ctas *= 2;
-    p.chunks = static_cast<int>(atb::ceil_div(threads, static_cast<int64_t>(ctas) * kMostThreads));
-    int block = static_cast<int>(atb::round_up(atb::ceil_div(threads, static_cast<int64_t>(ctas) * p.chunks), 32));
+    while (ctas < kMostCtas && (positions > static_cast<int64_t>(ctas) * kMostThreads * kPerThread || (p.M * ctas * 2 <= atb::kSmCount && positions >= ctas * 2 * 1024))) ctas *= 2;
+    const int64_t share = atb::ceil_div(positions, ctas);
+    p.vectors = kVectors;
+    if (p.M * ctas <= atb::kSmCount)
+        while (p.vectors > 2 && share <= static_cast<int64_t>(kMostThreads) * 4 * (p.vectors / 2)) p.vectors /= 2;
+    const int64_t threads = atb::ceil_div(share, 4 * p.vectors);
+    p.chunks = static_cast<int>(atb::ceil_div(threads, kMostThreads));
+    int block = static_cast<int>(atb::round_up(atb::ceil_div(threads, p.chunks), 32));
     if (block < 64) block = 64;
     p.group = 1;                           // 256 groups at most, in all
     while (block / p.group * ctas > kMostGroups) p.group *= 2;
@@ -826,7 +887,7 @@ cudaError_t launch(SampleParams p, cudaStream_t st) {
     while ((1ll << log2v) < p.V) ++log2v;
     p.shift = 62 - log2v < 45 ? 62 - log2v : 45;
     const unsigned grid = static_cast<unsigned>(p.M * ctas);
-    const size_t smem = static_cast<size_t>(block) * kPerThread * sizeof(float);
+    const size_t smem = static_cast<size_t>(block) * p.vectors * sizeof(float4);
     auto kernel = p.chunks == 1 ? sample_kernel<T, true> : sample_kernel<T, false>;
     const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kMostThreads * kPerThread * static_cast<int>(sizeof(float)));
     if (e != cudaSuccess) return e;
