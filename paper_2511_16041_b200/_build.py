@@ -11,9 +11,10 @@ LIB = os.path.join(HERE, "libatb.so")
 SOURCES = ["atb_status.cpp", "atb_model.cpp", "atb_quantize.cu", "atb_gemm_sm100.cu", "atb_gemm_pair_sm100.cu",
            "atb_gemm_cfg_sm100.cu", "atb_layer_norm.cu", "atb_bf16_mm_sm100.cu", "atb_gated_ffn.cu", "atb_linear_ce.cu",
            "atb_few_rows.cu", "atb_linear.cu",
-           "atb_residual_norm.cu", "atb_residual_norm_backward.cu", "atb_sample.cu"]
+           "atb_residual_norm.cu", "atb_residual_norm_f32.cu", "atb_residual_norm_bf16.cu", "atb_residual_norm_backward_f32.cu",
+           "atb_residual_norm_backward_bf16.cu", "atb_sample.cu"]
 HEADERS = ["atb_internal.h", "sm100_ptx.cuh", "atb_gemm_device.cuh", "bfp16_block.cuh", "atb_bf16_mm.h", "atb_few_rows.h", "glu.cuh", "dependent_launch.cuh", "f32x2.cuh", "norm_rows.cuh",
-           "atb_residual_norm.cuh"]
+           "atb_residual_norm.cuh", "residual_norm_forward.cuh", "residual_norm_backward.cuh"]
 
 
 def _nvcc() -> str:

@@ -1,289 +1,11 @@
-// Residual norm, forward (sm_100a), and the entry points of both directions: what joins a branch to the residual stream and norms it.
-//
-//   u = norm(f) pw + pb, or f;   h = scale x + gate u;   z = norm(h) w + b
-//   norm(v) = (v - mean) r, r = 1 / sqrt(mean((v - mean)^2) + eps); rms: the mean is taken as 0
-//
-// Bound by memory: x and f are read and h and z written, once.  A row's threads hold at most 16 elements each, h stays in registers (FP32)
-// between the two norms, so that z is made of the unrounded h.  Blocks stay and walk the rows; the next rows of x and f are
-// on their way into shared memory (cp.async) meanwhile.  Sums as in the layer norm: around the warps' own means, joined in one exchange per
-// norm.  Rows wider than the widest kernel are read again for every sum.
+// Residual norm: the entry points of both directions, and the sums of its weights' gradients (sm_100a).  The row kernels are in
+// residual_norm_forward.cuh and residual_norm_backward.cuh.
 #include <algorithm>
 
 #include "atb_residual_norm.cuh"
 
 namespace residual_norm {
 namespace {
-
-constexpr int kThreads[] = {32, 64, 128, 256, 384, 512, 768, 1024};
-template <class TX, class TF>
-constexpr int kMostThreads = sizeof(TX) + sizeof(TF) == 8 ? 768 : 1024;        // two stages of rows in shared memory
-template <class TX, class TF>
-constexpr int kAhead = sizeof(TX) + sizeof(TF) == 4 ? 2 : 1;
-// Blocks that stay on an SM: 1024 threads of 64 registers (768 an element at a time), 200 KB of rows.
-__host__ __device__ constexpr int resident(int threads, int stage_bytes, bool vec) {
-    const int by_threads = (vec ? 1024 : 768) / threads, by_room = 200 * 1024 / stage_bytes;
-    const int most = by_threads < by_room ? by_threads : by_room;
-    return most < 1 ? 1 : most;
-}
-template <class TX, class TF, int TPR, int NV, int VEC>
-constexpr int kRoom = (kAhead<TX, TF> + 1) * static_cast<int>(RowSource<TX, VEC, TPR, NV>::STAGE_BYTES + RowSource<TF, VEC, TPR, NV>::STAGE_BYTES);
-
-// Mean and 1 / spread of a row whose elements its threads hold in v; v becomes distances d, and norm(v) is d r + shift.
-template <int TPR>
-struct RowNorm {
-    static constexpr int W = TPR / 32;
-    int lane, warp, center;
-    float elems, n, inv_n, inv_own, eps;
-    template <int NV, int VEC>
-    __device__ __forceinline__ void operator()(float (&v)[NV][VEC], const bool (&in)[NV], float2* red, float& mu, float& r, float& shift) const {
-        float s[1] = {0.f}, mine = 0.f;
-        if (center) {
-#pragma unroll
-            for (int i = 0; i < NV; ++i)
-                if (in[i])
-#pragma unroll
-                    for (int e = 0; e < VEC; ++e) s[0] += v[i][e];
-            warp_sum(s);
-            mine = quotient(s[0], __shfl_sync(0xFFFFFFFFu, elems, warp), inv_own);       // the mean of the warp's elements
-            s[0] = 0.f;
-        }
-#pragma unroll
-        for (int i = 0; i < NV; ++i)
-            if (in[i])
-#pragma unroll
-                for (int e = 0; e < VEC; ++e) {
-                    v[i][e] -= mine;
-                    s[0] += v[i][e] * v[i][e];
-                }
-        warp_sum(s);
-        mu = mine;
-        if constexpr (TPR > 32) {
-            if (lane == 0) red[warp] = make_float2(mine, s[0]);
-            __syncthreads();
-            const float2 part = lane < W ? red[lane] : make_float2(0.f, 0.f);
-            if (center) {
-                float sum[1] = {elems * part.x};
-                warp_sum(sum);
-                mu = quotient(sum[0], n, inv_n);
-            }
-            s[0] = part.y + elems * (part.x - mu) * (part.x - mu);
-            warp_sum(s);
-        }
-        r = rsqrtf(s[0] * inv_n + eps);
-        shift = (mine - mu) * r;
-    }
-};
-
-template <class TX, class TF, int VEC, int TPR, int NV, bool POST>
-__global__ void __launch_bounds__(TPR == 32 ? 128 : TPR, resident(TPR == 32 ? 128 : TPR, kRoom<TX, TF, TPR, NV, VEC>, VEC > 1))
-residual_norm_kernel(const FwdParams p) {
-    using SX = RowSource<TX, VEC, TPR, NV>;
-    using SF = RowSource<TF, VEC, TPR, NV>;
-    using Shared = std::conditional_t<SX::SHARED, SX, SF>;
-    constexpr int WALKERS = TPR == 32 ? 4 : 1, W = TPR / 32, AHEAD = kAhead<TX, TF>, STAGES = AHEAD + 1;
-    extern __shared__ __align__(16) uint8_t ring[];
-    __shared__ float2 red[2][2][W];
-    const int t = TPR == 32 ? threadIdx.x & 31 : threadIdx.x, lane = threadIdx.x & 31;
-    const int N = static_cast<int>(p.N), col = t * VEC;                 // group i: columns col + i TPR VEC ..
-    const int64_t first = static_cast<int64_t>(blockIdx.x) * WALKERS + (TPR == 32 ? threadIdx.x >> 5 : 0), step = static_cast<int64_t>(gridDim.x) * WALKERS;
-    const SX sx(sm100::smem_u32(ring), p.x, p.ldx, p.M, N, t);
-    const SF sf(sm100::smem_u32(ring) + STAGES * SX::STAGE_BYTES, p.f, p.ldf, p.M, N, t);
-    RowNorm<TPR> norm;
-    {
-        int count = 0;                     // elements of warp `lane`
-#pragma unroll
-        for (int i = 0; i < NV; ++i) count += max(0, min(32 * VEC, N - (i * TPR + lane * 32) * VEC));
-        if (lane >= W) count = 0;
-        norm.lane = lane;
-        norm.warp = TPR == 32 ? 0 : threadIdx.x >> 5;
-        norm.center = p.center;
-        norm.elems = static_cast<float>(count);
-        norm.n = static_cast<float>(N);
-        norm.inv_n = 1.f / norm.n;
-        norm.eps = p.eps;
-        const int own = __shfl_sync(0xFFFFFFFFu, count, norm.warp);
-        norm.inv_own = own > 0 ? 1.f / static_cast<float>(own) : 0.f;
-    }
-    bool in[NV];
-#pragma unroll
-    for (int i = 0; i < NV; ++i) in[i] = col + i * TPR * VEC < N;
-    sm100::grid_dependency_wait();
-    sm100::grid_dependency_launch();
-#pragma unroll
-    for (int s = 0; s < AHEAD; ++s) {
-        if (first + s * step < p.M) {
-            sx.fetch(s, first + s * step);
-            sf.fetch(s, first + s * step);
-        }
-        async_commit();
-    }
-    int stage = 0, turn = 0;
-    for (int64_t m = first; m < p.M; m += step, turn ^= 1) {
-        const int ahead = stage == 0 ? AHEAD : stage - 1;               // the stage that the row before this one has left
-        if (m + AHEAD * step < p.M) {
-            sx.fetch(ahead, m + AHEAD * step);
-            sf.fetch(ahead, m + AHEAD * step);
-        }
-        async_commit();
-        async_wait<AHEAD>();
-        row_barrier<Shared, VEC, TPR>();
-        float v[NV][VEC];
-#pragma unroll
-        for (int i = 0; i < NV; ++i)
-            if (in[i]) {
-                Raw<TF, VEC> raw;
-                sf.read(stage, m, i, raw);
-                to_float(raw, v[i]);
-            }
-        float mu, r, shift;
-        if constexpr (POST) {
-            norm(v, in, red[0][turn], mu, r, shift);
-            if (t == 0 && p.stats) { p.stats[2 * p.M + m] = mu; p.stats[3 * p.M + m] = r; }
-        }
-#pragma unroll
-        for (int i = 0; i < NV; ++i)
-            if (in[i]) {
-                const int n = col + i * TPR * VEC;
-                float a[VEC], b[VEC];
-                if constexpr (POST) {
-                    weights<VEC>(p.v.pw, p.v.w32, n, 1.f, a);
-                    weights<VEC>(p.v.pb, p.v.w32, n, 0.f, b);
-#pragma unroll
-                    for (int e = 0; e < VEC; ++e) v[i][e] = fmaf(fmaf(v[i][e], r, shift), a[e], b[e]);
-                }
-                Raw<TX, VEC> raw;
-                sx.read(stage, m, i, raw);
-                to_float(raw, b);
-                weights<VEC>(p.v.gate, p.v.w32, n, 1.f, a);
-#pragma unroll
-                for (int e = 0; e < VEC; ++e) v[i][e] = fmaf(p.scale, b[e], a[e] * v[i][e]);
-                store_f<TX, VEC>(static_cast<TX*>(p.h) + m * p.ldh + n, v[i]);
-            }
-        norm(v, in, red[1][turn], mu, r, shift);
-        if (t == 0 && p.stats) { p.stats[m] = mu; p.stats[p.M + m] = r; }
-#pragma unroll
-        for (int i = 0; i < NV; ++i)
-            if (in[i]) {
-                const int n = col + i * TPR * VEC;
-                float a[VEC], b[VEC];
-                weights<VEC>(p.v.w, p.v.w32, n, 1.f, a);
-                weights<VEC>(p.v.b, p.v.w32, n, 0.f, b);
-#pragma unroll
-                for (int e = 0; e < VEC; ++e) v[i][e] = fmaf(fmaf(v[i][e], r, shift), a[e], b[e]);
-                store_f<TF, VEC>(static_cast<TF*>(p.z) + m * p.ldz + n, v[i]);
-            }
-        stage = stage + 1 == STAGES ? 0 : stage + 1;
-    }
-}
-
-// Any width: x and f are read again for every sum.
-template <class TX, class TF, int VEC, bool POST>
-__global__ void __launch_bounds__(1024) residual_norm_wide_kernel(const FwdParams p) {
-    __shared__ float red[4][32][1];
-    const int64_t m = blockIdx.x;
-    const TX* x = static_cast<const TX*>(p.x) + m * p.ldx;
-    const TF* f = static_cast<const TF*>(p.f) + m * p.ldf;
-    const float n_all = static_cast<float>(p.N), inv_n = 1.f / n_all;
-    float fmu = 0.f, fr = 1.f, mu = 0.f, s[1] = {0.f}, v[VEC], a[VEC];
-    const auto each = [&](auto&& body) {
-        for (int64_t n = threadIdx.x * VEC; n < p.N; n += 1024 * VEC) body(static_cast<int>(n));
-    };
-    if constexpr (POST) {
-        if (p.center) {
-            each([&](int n) {
-                load_f<TF, VEC>(f + n, v);
-#pragma unroll
-                for (int e = 0; e < VEC; ++e) s[0] += v[e];
-            });
-            row_sum<1024, 1>(s, red[0]);
-            fmu = quotient(s[0], n_all, inv_n);
-            s[0] = 0.f;
-        }
-        each([&](int n) {
-            load_f<TF, VEC>(f + n, v);
-#pragma unroll
-            for (int e = 0; e < VEC; ++e) s[0] += (v[e] - fmu) * (v[e] - fmu);
-        });
-        row_sum<1024, 1>(s, red[1]);
-        fr = rsqrtf(s[0] * inv_n + p.eps);
-        s[0] = 0.f;
-        if (threadIdx.x == 0 && p.stats) { p.stats[2 * p.M + m] = fmu; p.stats[3 * p.M + m] = fr; }
-    }
-    const auto h_of = [&](int n) {
-        float b[VEC];
-        load_f<TF, VEC>(f + n, v);
-        if constexpr (POST) {
-            weights<VEC>(p.v.pw, p.v.w32, n, 1.f, a);
-            weights<VEC>(p.v.pb, p.v.w32, n, 0.f, b);
-#pragma unroll
-            for (int e = 0; e < VEC; ++e) v[e] = fmaf((v[e] - fmu) * fr, a[e], b[e]);
-        }
-        load_f<TX, VEC>(x + n, b);
-        weights<VEC>(p.v.gate, p.v.w32, n, 1.f, a);
-#pragma unroll
-        for (int e = 0; e < VEC; ++e) v[e] = fmaf(p.scale, b[e], a[e] * v[e]);
-    };
-    if (p.center) {
-        each([&](int n) {
-            h_of(n);
-#pragma unroll
-            for (int e = 0; e < VEC; ++e) s[0] += v[e];
-        });
-        row_sum<1024, 1>(s, red[2]);
-        mu = quotient(s[0], n_all, inv_n);
-        s[0] = 0.f;
-    }
-    each([&](int n) {
-        h_of(n);
-#pragma unroll
-        for (int e = 0; e < VEC; ++e) s[0] += (v[e] - mu) * (v[e] - mu);
-    });
-    row_sum<1024, 1>(s, red[3]);
-    const float r = rsqrtf(s[0] * inv_n + p.eps);
-    if (threadIdx.x == 0 && p.stats) { p.stats[m] = mu; p.stats[p.M + m] = r; }
-    each([&](int n) {
-        float b[VEC];
-        h_of(n);
-        store_f<TX, VEC>(static_cast<TX*>(p.h) + m * p.ldh + n, v);
-        weights<VEC>(p.v.w, p.v.w32, n, 1.f, a);
-        weights<VEC>(p.v.b, p.v.w32, n, 0.f, b);
-#pragma unroll
-        for (int e = 0; e < VEC; ++e) v[e] = fmaf((v[e] - mu) * r, a[e], b[e]);
-        store_f<TF, VEC>(static_cast<TF*>(p.z) + m * p.ldz + n, v);
-    });
-}
-
-// ---------------------------------------------------------------------------------- host
-template <class TX, class TF, int VEC, bool POST, int TPR>
-cudaError_t launch_rows(const FwdParams& p, cudaStream_t st) {
-    constexpr int NV = kElems / VEC, THREADS = TPR == 32 ? 128 : TPR, ROOM = kRoom<TX, TF, TPR, NV, VEC>;
-    const int64_t all = atb::ceil_div(p.M, TPR == 32 ? 4 : 1), most = static_cast<int64_t>(atb::kSmCount) * resident(THREADS, ROOM, VEC > 1);
-    return launch_ring(residual_norm_kernel<TX, TF, VEC, TPR, NV, POST>, static_cast<unsigned>(all < most ? all : most), THREADS, ROOM, st, p);
-}
-template <class TX, class TF, int VEC, bool POST>
-cudaError_t launch(const FwdParams& p, cudaStream_t st) {
-    for (const int t : kThreads) {
-        if (t > kMostThreads<TX, TF> || p.N > static_cast<int64_t>(t) * kElems) continue;
-        switch (t) {
-            case 32: return launch_rows<TX, TF, VEC, POST, 32>(p, st);
-            case 64: return launch_rows<TX, TF, VEC, POST, 64>(p, st);
-            case 128: return launch_rows<TX, TF, VEC, POST, 128>(p, st);
-            case 256: return launch_rows<TX, TF, VEC, POST, 256>(p, st);
-            case 384: return launch_rows<TX, TF, VEC, POST, 384>(p, st);
-            case 512: return launch_rows<TX, TF, VEC, POST, 512>(p, st);
-            case 768: return launch_rows<TX, TF, VEC, POST, 768>(p, st);
-            case 1024:
-                if constexpr (kMostThreads<TX, TF> == 1024) return launch_rows<TX, TF, VEC, POST, 1024>(p, st);
-        }
-    }
-    residual_norm_wide_kernel<TX, TF, VEC, POST><<<static_cast<unsigned>(p.M), 1024, 0, st>>>(p);
-    return cudaGetLastError();
-}
-template <class TX, class TF>
-cudaError_t launch_types(const FwdParams& p, bool vec, bool post, cudaStream_t st) {
-    if (vec) return post ? launch<TX, TF, 8, true>(p, st) : launch<TX, TF, 8, false>(p, st);
-    return post ? launch<TX, TF, 1, true>(p, st) : launch<TX, TF, 1, false>(p, st);
-}
 
 // ---------------------------------------------------------------------------------- checks
 bool known_type(int t) { return t == ATB_F32 || t == ATB_BF16; }
@@ -302,9 +24,27 @@ atb_status_t check_common(int64_t M, int64_t N, int kind, int x_type, int f_type
 }
 Types types_of(int x_type, int f_type) { return x_type == ATB_BF16 ? kBf16 : f_type == ATB_BF16 ? kMixed : kF32; }
 
-// The sums of walkers and columns -> the weights' gradients, 32 columns per block, 16 warps that take every 16th walker's sums, then the 16 in
-// turn.  S0 = sum dz norm(h), S1 = sum dz, S2 = sum t norm(f) (or t f), S3 = sum t, where t is the gradient that arrives at h.
-constexpr int kSumWarps = 16;
+// Walkers of the backward kernels: threads of a row and elements of a thread; none: the wide kernel.
+struct Grid {
+    int blocks, walkers;
+};
+// All that are resident, while each still has 4 rows, since its sums go through the workspace, but one per SM at least.
+Grid grid_of(int64_t M, int64_t N) {
+    const int w = width_of(N), per_block = w < kWidthCount && kWidths[w].threads == 32 ? 4 : 1, per_sm = w < kWidthCount ? blocks_of(kWidths[w].threads) : 2;
+    const int64_t all = atb::ceil_div(M, per_block), most = static_cast<int64_t>(atb::kSmCount) * per_sm;
+    int64_t blocks = atb::ceil_div(M, 4 * per_block);
+    if (blocks < atb::kSmCount) blocks = atb::kSmCount;
+    if (blocks > most) blocks = most;
+    if (blocks > all) blocks = all;
+    if (blocks < 1) blocks = 1;
+    return {static_cast<int>(blocks), static_cast<int>(blocks) * per_block};
+}
+int walkers(int64_t M, int64_t N) { return grid_of(M, N).walkers; }
+
+// The sums of walkers and columns -> the weights' gradients.  A block takes 8 columns; a warp's lanes four walkers' sums of them (32 bytes
+// each), its 16 warps every 64th walker; then the 64 in turn.  S0 = sum dz norm(h), S1 = sum dz, S2 = sum t norm(f) (or t f), S3 =
+// sum t, where t is the gradient that arrives at h.
+constexpr int kSumWarps = 16, kSumCols = 8, kSumRows = kSumWarps * 32 / kSumCols;
 struct SumParams {
     const float* part;
     int walkers, post;
@@ -313,15 +53,15 @@ struct SumParams {
     void *dw, *db, *dgate, *dpw, *dpb;
 };
 __global__ void __launch_bounds__(32 * kSumWarps) residual_norm_sum_kernel(const SumParams p) {
-    __shared__ float s[kSumWarps][4][32];
-    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, sums = p.post ? 4 : 3;
-    const int64_t n = static_cast<int64_t>(blockIdx.x) * 32 + lane;
+    __shared__ float s[kSumRows][4][kSumCols];
+    const int c = threadIdx.x % kSumCols, first = threadIdx.x / kSumCols, sums = p.post ? 4 : 3;
+    const int64_t n = static_cast<int64_t>(blockIdx.x) * kSumCols + c;
     sm100::grid_dependency_wait();
     sm100::grid_dependency_launch();
     float v[4] = {};
     if (n < p.N) {
 #pragma unroll 4
-        for (int i = warp; i < p.walkers; i += kSumWarps) {
+        for (int i = first; i < p.walkers; i += kSumRows) {
             const float* src = p.part + static_cast<int64_t>(i) * sums * p.N + n;
 #pragma unroll
             for (int k = 0; k < 4; ++k)
@@ -329,15 +69,23 @@ __global__ void __launch_bounds__(32 * kSumWarps) residual_norm_sum_kernel(const
         }
     }
 #pragma unroll
-    for (int k = 0; k < 4; ++k) s[warp][k][lane] = v[k];
+    for (int k = 0; k < 4; ++k) s[first][k][c] = v[k];
     __syncthreads();
-    if (warp != 0 || n >= p.N) return;
-    for (int i = 1; i < kSumWarps; ++i)
+    // a thread to a sum and column
+    if (threadIdx.x < 4 * kSumCols) {
+        float total = 0.f;
+#pragma unroll 16
+        for (int i = 0; i < kSumRows; ++i) total += s[i][threadIdx.x / kSumCols][c];
+        s[0][threadIdx.x / kSumCols][c] = total;
+    }
+    __syncthreads();
+    if (threadIdx.x >= kSumCols || n >= p.N) return;
 #pragma unroll
-        for (int k = 0; k < 4; ++k) v[k] += s[i][k][lane];
+    for (int k = 0; k < 4; ++k) v[k] = s[0][k][c];
     const auto weight = [&](const void* w, float none) {
         float o[1];
-        weights<1>(w, p.v.w32, static_cast<int>(n), none, o);
+        if (p.v.w32) weights<float, 1>(w, static_cast<int>(n), none, o);
+        else weights<__nv_bfloat16, 1>(w, static_cast<int>(n), none, o);
         return o[0];
     };
     const auto put = [&](void* out, float value) {
@@ -389,12 +137,8 @@ extern "C" atb_status_t atb_residual_norm(int64_t M, int64_t N, int kind, int x_
     const FwdParams p{M, N, ldx, ldf, ldh, ldz, X_dev, F_dev, {W_dev, B_dev, gate_dev, PW_dev, PB_dev, w_type == ATB_F32}, scale, eps, !(kind & ATB_NORM_RMS),
                       H_dev, Z_dev, stats_dev};
     cudaStream_t st = static_cast<cudaStream_t>(stream);
-    cudaError_t e = cudaSuccess;
-    switch (types_of(x_type, f_type)) {
-        case kBf16: e = launch_types<__nv_bfloat16, __nv_bfloat16>(p, vec, post, st); break;
-        case kMixed: e = launch_types<float, __nv_bfloat16>(p, vec, post, st); break;
-        case kF32: e = launch_types<float, float>(p, vec, post, st); break;
-    }
+    const auto launch = w_type == ATB_F32 ? launch_forward_f32 : launch_forward_bf16;
+    const cudaError_t e = launch(p, types_of(x_type, f_type), vec, post, st);
     if (e != cudaSuccess) return atb::fail(ATB_ERR_CUDA, "residual norm launch: %s", cudaGetErrorString(e));
     return ATB_OK;
 }
@@ -441,12 +185,13 @@ extern "C" atb_status_t atb_residual_norm_backward(int64_t M, int64_t N, int kin
     cudaError_t e = cudaSuccess;
     if (M > 0 && (dX_dev || dF_dev || sums)) {
         const BwdParams p{M, N, lddz, lddh, ldx, ldf, lddx, lddf, dZ_dev, dH_dev, X_dev, F_dev, v, scale, !(kind & ATB_NORM_RMS), stats_dev, dX_dev, dF_dev,
-                          sums ? static_cast<float*>(workspace_dev) : nullptr};
-        e = launch_backward(p, types_of(x_type, f_type), vec, post, st);
+                          sums ? static_cast<float*>(workspace_dev) : nullptr, grid_of(M, N).blocks};
+        const auto launch = w_type == ATB_F32 ? launch_backward_f32 : launch_backward_bf16;
+        e = launch(p, types_of(x_type, f_type), vec, post, st);
     }
     if (e == cudaSuccess && sums) {
         const SumParams p{static_cast<const float*>(workspace_dev), M > 0 ? walkers(M, N) : 0, post, N, v, dW_dev, dB_dev, dgate_dev, dPW_dev, dPB_dev};
-        e = atb::launch_dependent(residual_norm_sum_kernel, static_cast<unsigned>(atb::ceil_div(N, 32)), 32u * kSumWarps, 1u, 0, st, p);
+        e = atb::launch_dependent(residual_norm_sum_kernel, static_cast<unsigned>(atb::ceil_div(N, kSumCols)), 32u * kSumWarps, 1u, 0, st, p);
     }
     if (e != cudaSuccess) return atb::fail(ATB_ERR_CUDA, "residual norm backward launch: %s", cudaGetErrorString(e));
     return ATB_OK;

@@ -12,7 +12,7 @@ using namespace norm_rows;
 
 struct Weights {
     const void *w, *b, *gate, *pw, *pb;    // each [N] of one type, or NULL
-    int w32;                               // that type is FP32, else bf16
+    int w32;                               // that type is FP32, else bf16 (the kernels' TW)
 };
 struct FwdParams {
     int64_t M, N, ldx, ldf, ldh, ldz;
@@ -32,34 +32,30 @@ struct BwdParams {
     const float* stats;
     void *dx, *df;                         // each may be NULL
     float* part;                           // [walkers][sums][N], or NULL
+    int blocks;                            // that walk the rows
 };
 
 // Elements n .. n + VEC - 1 of a vector of weights, or `none` where there is no vector.  They are read again for every row, from the L1:
 // five of them would take more registers than a row does.
-template <int VEC>
-__device__ __forceinline__ void weights(const void* p, int w32, int n, float none, float (&v)[VEC]) {
-    if (!p) {
+template <class TW, int VEC>
+__device__ __forceinline__ void weights(const void* p, int n, float none, float (&v)[VEC]) {
 #pragma unroll
-        for (int e = 0; e < VEC; ++e) v[e] = none;
-    } else if constexpr (VEC == 1) {
-        v[0] = w32 ? __ldg(static_cast<const float*>(p) + n) : __uint_as_float(static_cast<uint32_t>(__ldg(static_cast<const uint16_t*>(p) + n)) << 16);
-    } else if (w32) {
+    for (int e = 0; e < VEC; ++e) v[e] = none;
+    if (p) {
+        Raw<TW, VEC> raw;
+        const TW* const at = static_cast<const TW*>(p) + n;
+        if constexpr (VEC > 1) {
 #pragma unroll
-        for (int i = 0; i < VEC / 4; ++i) {
-            const float4 f = __ldg(reinterpret_cast<const float4*>(static_cast<const float*>(p) + n) + i);
-            v[4 * i] = f.x; v[4 * i + 1] = f.y; v[4 * i + 2] = f.z; v[4 * i + 3] = f.w;
-        }
-    } else {
-#pragma unroll
-        for (int i = 0; i < VEC / 8; ++i) {
-            const uint4 u = __ldg(reinterpret_cast<const uint4*>(static_cast<const uint16_t*>(p) + n) + i);
-            const uint32_t q[4] = {u.x, u.y, u.z, u.w};
-#pragma unroll
-            for (int e = 0; e < 4; ++e) {
-                v[8 * i + 2 * e] = __uint_as_float(q[e] << 16);
-                v[8 * i + 2 * e + 1] = __uint_as_float(q[e] & 0xFFFF0000u);
+            for (int i = 0; i < static_cast<int>(sizeof(raw.w) / 16); ++i) {
+                const uint4 u = __ldg(reinterpret_cast<const uint4*>(at) + i);
+                raw.w[4 * i] = u.x; raw.w[4 * i + 1] = u.y; raw.w[4 * i + 2] = u.z; raw.w[4 * i + 3] = u.w;
             }
+        } else if constexpr (sizeof(TW) == 4) {
+            raw.w[0] = __ldg(reinterpret_cast<const uint32_t*>(at));
+        } else {
+            raw.w[0] = __ldg(reinterpret_cast<const uint16_t*>(at));
         }
+        to_float(raw, v);
     }
 }
 
@@ -75,9 +71,23 @@ cudaError_t launch_ring(void (*kernel)(Args...), unsigned grid, unsigned block, 
 
 // Types of the stream (x, h and their gradients) and of the branch (f, z and theirs).
 enum Types { kBf16 = 0, kMixed = 1, kF32 = 2 };
-// sums: of the rows' products that the weights' gradients are made of
-inline int sums_per_column(bool post) { return post ? 4 : 3; }
-int walkers(int64_t M, int64_t N);
-cudaError_t launch_backward(const BwdParams& p, Types types, bool vec, bool post, cudaStream_t stream);
+// Backward: threads of a row and elements of a thread (kWidthCount: the wide kernel), and blocks that stay on an SM.
+constexpr int kBlockThreads = 512;         // per SM, 128 registers each
+struct Width {
+    int threads, elems;
+};
+constexpr Width kWidths[] = {{32, 8}, {32, 16}, {128, 8}, {256, 8}, {512, 8}, {512, 16}};
+constexpr int kWidthCount = 6;
+inline int width_of(int64_t N) {
+    for (int i = 0; i < kWidthCount; ++i)
+        if (N <= static_cast<int64_t>(kWidths[i].threads) * kWidths[i].elems) return i;
+    return kWidthCount;
+}
+__host__ __device__ constexpr int blocks_of(int tpr) { return kBlockThreads / (tpr == 32 ? 128 : tpr); }
+// A translation unit for each type of the weights.
+cudaError_t launch_forward_f32(const FwdParams& p, Types types, bool vec, bool post, cudaStream_t stream);
+cudaError_t launch_forward_bf16(const FwdParams& p, Types types, bool vec, bool post, cudaStream_t stream);
+cudaError_t launch_backward_f32(const BwdParams& p, Types types, bool vec, bool post, cudaStream_t stream);
+cudaError_t launch_backward_bf16(const BwdParams& p, Types types, bool vec, bool post, cudaStream_t stream);
 
 }  // namespace residual_norm

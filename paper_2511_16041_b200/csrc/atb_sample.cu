@@ -214,7 +214,7 @@ __global__ void __launch_bounds__(kMostThreads, 2) sample_kernel(const SamplePar
         sh.count[i] = 0;
         sh.weight[i] = 0;
     }
-    if (t == 0) { sh.beyond = 0; sh.whole = 0; sh.candidates = 0; }
+    if (t == 0) sh.candidates = 0;
     if (t < 16) sh.table[t] = exp2(t * 0.0625);
     sm100::grid_dependency_wait();
     sm100::grid_dependency_launch();
@@ -538,8 +538,13 @@ __global__ void __launch_bounds__(kMostThreads, 2) sample_kernel(const SamplePar
                 whole = warp_add(whole);
                 if (lane == 0) {
                     sh.warp_beyond[warp] = beyond;
-                    atomicAdd(&sh.beyond, beyond);
-                    atomicAdd(&sh.whole, whole);
+                    sh.warp_total[warp] = whole;
+                }
+                __syncthreads();
+                if (warp == 0) {
+                    beyond = warp_add(lane < warps ? sh.warp_beyond[lane] : 0ull);
+                    whole = warp_add(lane < warps ? sh.warp_total[lane] : 0ull);
+                    if (lane == 0) { sh.beyond = beyond; sh.whole = whole; }
                 }
                 listed = alone;
             }
