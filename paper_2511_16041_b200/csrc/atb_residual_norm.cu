@@ -41,10 +41,10 @@ Grid grid_of(int64_t M, int64_t N) {
 }
 int walkers(int64_t M, int64_t N) { return grid_of(M, N).walkers; }
 
-// The sums of walkers and columns -> the weights' gradients.  A block takes 8 columns; a warp's lanes four walkers' sums of them (32 bytes
-// each), its 16 warps every 64th walker; then the 64 in turn.  S0 = sum dz norm(h), S1 = sum dz, S2 = sum t norm(f) (or t f), S3 =
+// The sums of walkers and columns -> the weights' gradients.  A block takes COLS columns: 32, or 8 where 32 would leave SMs without a block;
+// its threads 512 / COLS walkers' sums of them at a time; then those in turn.  S0 = sum dz norm(h), S1 = sum dz, S2 = sum t norm(f) (or t f), S3 =
 // sum t, where t is the gradient that arrives at h.
-constexpr int kSumWarps = 16, kSumCols = 8, kSumRows = kSumWarps * 32 / kSumCols;
+constexpr int kSumWarps = 16;
 struct SumParams {
     const float* part;
     int walkers, post;
@@ -52,10 +52,12 @@ struct SumParams {
     Weights v;
     void *dw, *db, *dgate, *dpw, *dpb;
 };
+template <int COLS>
 __global__ void __launch_bounds__(32 * kSumWarps) residual_norm_sum_kernel(const SumParams p) {
-    __shared__ float s[kSumRows][4][kSumCols];
-    const int c = threadIdx.x % kSumCols, first = threadIdx.x / kSumCols, sums = p.post ? 4 : 3;
-    const int64_t n = static_cast<int64_t>(blockIdx.x) * kSumCols + c;
+    constexpr int kSumRows = kSumWarps * 32 / COLS;
+    __shared__ float s[kSumRows][4][COLS];
+    const int c = threadIdx.x % COLS, first = threadIdx.x / COLS, sums = p.post ? 4 : 3;
+    const int64_t n = static_cast<int64_t>(blockIdx.x) * COLS + c;
     sm100::grid_dependency_wait();
     sm100::grid_dependency_launch();
     float v[4] = {};
@@ -72,14 +74,14 @@ __global__ void __launch_bounds__(32 * kSumWarps) residual_norm_sum_kernel(const
     for (int k = 0; k < 4; ++k) s[first][k][c] = v[k];
     __syncthreads();
     // a thread to a sum and column
-    if (threadIdx.x < 4 * kSumCols) {
+    if (threadIdx.x < 4 * COLS) {
         float total = 0.f;
 #pragma unroll 16
-        for (int i = 0; i < kSumRows; ++i) total += s[i][threadIdx.x / kSumCols][c];
-        s[0][threadIdx.x / kSumCols][c] = total;
+        for (int i = 0; i < kSumRows; ++i) total += s[i][threadIdx.x / COLS][c];
+        s[0][threadIdx.x / COLS][c] = total;
     }
     __syncthreads();
-    if (threadIdx.x >= kSumCols || n >= p.N) return;
+    if (threadIdx.x >= COLS || n >= p.N) return;
 #pragma unroll
     for (int k = 0; k < 4; ++k) v[k] = s[0][k][c];
     const auto weight = [&](const void* w, float none) {
@@ -191,7 +193,8 @@ extern "C" atb_status_t atb_residual_norm_backward(int64_t M, int64_t N, int kin
     }
     if (e == cudaSuccess && sums) {
         const SumParams p{static_cast<const float*>(workspace_dev), M > 0 ? walkers(M, N) : 0, post, N, v, dW_dev, dB_dev, dgate_dev, dPW_dev, dPB_dev};
-        e = atb::launch_dependent(residual_norm_sum_kernel, static_cast<unsigned>(atb::ceil_div(N, kSumCols)), 32u * kSumWarps, 1u, 0, st, p);
+        e = N < 32 * atb::kSmCount ? atb::launch_dependent(residual_norm_sum_kernel<8>, static_cast<unsigned>(atb::ceil_div(N, 8)), 32u * kSumWarps, 1u, 0, st, p)
+                                   : atb::launch_dependent(residual_norm_sum_kernel<32>, static_cast<unsigned>(atb::ceil_div(N, 32)), 32u * kSumWarps, 1u, 0, st, p);
     }
     if (e != cudaSuccess) return atb::fail(ATB_ERR_CUDA, "residual norm backward launch: %s", cudaGetErrorString(e));
     return ATB_OK;

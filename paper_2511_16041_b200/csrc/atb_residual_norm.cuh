@@ -59,6 +59,117 @@ __device__ __forceinline__ void weights(const void* p, int n, float none, float 
     }
 }
 
+// A thread's elements in eights, as four pairs: a group of VEC = 8, or eight single elements.
+template <class T, int VEC>
+__device__ __forceinline__ void pairs_of(const Raw<T, VEC> (&r)[8 / VEC], float2 (&v)[4]) {
+    if constexpr (VEC == 8) {
+        float f[8];
+        to_float(r[0], f);
+#pragma unroll
+        for (int k = 0; k < 4; ++k) v[k] = make_float2(f[2 * k], f[2 * k + 1]);
+    } else {
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+            float a[1], b[1];
+            to_float(r[2 * k], a);
+            to_float(r[2 * k + 1], b);
+            v[k] = make_float2(a[0], b[0]);
+        }
+    }
+}
+// Where they are: eight c of a thread whose first column is `col`.  Elements past the row's end are 0, as are their weights.
+template <int VEC, int TPR>
+struct Eight {
+    static constexpr int G = 8 / VEC;      // groups
+    int N, col, c;
+    __device__ __forceinline__ int n(int g) const { return col + (c * G + g) * TPR * VEC; }
+    __device__ __forceinline__ bool in(int g) const { return n(g) < N; }
+    template <class T, class Source>
+    __device__ __forceinline__ void read(const Source& src, int stage, int64_t m, float2 (&v)[4]) const {
+        Raw<T, VEC> r[G];
+#pragma unroll
+        for (int g = 0; g < G; ++g) {
+            if (in(g)) src.read(stage, m, c * G + g, r[g]);
+            else clear(r[g]);
+        }
+        pairs_of(r, v);
+    }
+    template <class T>
+    __device__ __forceinline__ void load(const void* row, float2 (&v)[4]) const {
+        Raw<T, VEC> r[G];
+#pragma unroll
+        for (int g = 0; g < G; ++g) {
+            if (in(g)) load_raw<T, VEC>(static_cast<const T*>(row) + n(g), r[g]);
+            else clear(r[g]);
+        }
+        pairs_of(r, v);
+    }
+    // ... of a vector of weights.
+    template <class TW>
+    __device__ __forceinline__ void weight(const void* w, float none, float2 (&v)[4]) const {
+        float f[G][VEC];
+#pragma unroll
+        for (int g = 0; g < G; ++g) {
+#pragma unroll
+            for (int e = 0; e < VEC; ++e) f[g][e] = 0.f;
+            if (in(g)) weights<TW, VEC>(w, n(g), none, f[g]);
+        }
+#pragma unroll
+        for (int k = 0; k < 4; ++k) v[k] = VEC == 8 ? make_float2(f[0][(2 * k) % VEC], f[0][(2 * k + 1) % VEC]) : make_float2(f[(2 * k) % G][0], f[(2 * k + 1) % G][0]);
+    }
+    template <class T>
+    __device__ __forceinline__ void store(void* row, const float2 (&v)[4]) const {
+#pragma unroll
+        for (int g = 0; g < G; ++g)
+            if (in(g)) {
+                float f[VEC];
+#pragma unroll
+                for (int e = 0; e < VEC; ++e) {
+                    const int k = g * VEC + e;
+                    f[e] = k & 1 ? v[k / 2].y : v[k / 2].x;
+                }
+                store_f<T, VEC>(static_cast<T*>(row) + n(g), f);
+            }
+    }
+};
+
+// A vector of weights at a thread's CH eights.  KEEP: in registers, loaded once, as they are in memory (single elements: in FP32); else read
+// again wherever they are used.
+template <class TW, int VEC, int TPR, int CH, bool KEEP>
+struct Vector {
+    const void* p;
+    float none;
+    Raw<TW, 8> raw[KEEP && VEC == 8 ? CH : 1];
+    float2 one[KEEP && VEC == 1 ? CH : 1][4];
+    __device__ __forceinline__ Vector(const void* p_, float none_, int N, int col) : p(p_), none(none_) {
+        if constexpr (KEEP) {
+#pragma unroll
+            for (int c = 0; c < CH; ++c) {
+                const Eight<VEC, TPR> at{N, col, c};
+                if constexpr (VEC == 8) {
+                    load_or<TW, 8>(static_cast<const TW*>(p), at.n(0), N, none, raw[c]);
+                } else {
+                    at.template weight<TW>(p, none, one[c]);
+#pragma unroll
+                    for (int k = 0; k < 4; ++k)      // kept: not converted again in every row
+                        asm volatile("" : "+f"(one[c][k].x), "+f"(one[c][k].y));
+                }
+            }
+        }
+    }
+    __device__ __forceinline__ void get(const Eight<VEC, TPR>& at, float2 (&v)[4]) const {
+        if constexpr (!KEEP) {
+            at.template weight<TW>(p, none, v);
+        } else if constexpr (VEC == 8) {
+            const Raw<TW, 8> r[1] = {raw[at.c]};
+            pairs_of<TW, 8>(r, v);
+        } else {
+#pragma unroll
+            for (int k = 0; k < 4; ++k) v[k] = one[at.c][k];
+        }
+    }
+};
+
 // A kernel whose rows on their way may take more, with its static arrays, than the 48 KB of shared memory that need no leave.
 template <class... Args>
 cudaError_t launch_ring(void (*kernel)(Args...), unsigned grid, unsigned block, size_t smem, cudaStream_t stream, Args... args) {

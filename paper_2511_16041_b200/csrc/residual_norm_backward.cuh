@@ -27,79 +27,6 @@ __host__ __device__ constexpr int ahead_of() {
     return stages > 4 ? 3 : stages - 1;
 }
 
-// A thread's elements in eights, as four pairs: a group of VEC = 8, or eight single elements.
-template <class T, int VEC>
-__device__ __forceinline__ void pairs_of(const Raw<T, VEC> (&r)[8 / VEC], float2 (&v)[4]) {
-    if constexpr (VEC == 8) {
-        float f[8];
-        to_float(r[0], f);
-#pragma unroll
-        for (int k = 0; k < 4; ++k) v[k] = make_float2(f[2 * k], f[2 * k + 1]);
-    } else {
-#pragma unroll
-        for (int k = 0; k < 4; ++k) {
-            float a[1], b[1];
-            to_float(r[2 * k], a);
-            to_float(r[2 * k + 1], b);
-            v[k] = make_float2(a[0], b[0]);
-        }
-    }
-}
-// Where they are: eight c of a thread whose first column is `col`.  Elements past the row's end are 0, as are their weights.
-template <int VEC, int TPR>
-struct Eight {
-    static constexpr int G = 8 / VEC;      // groups
-    int N, col, c;
-    __device__ __forceinline__ int n(int g) const { return col + (c * G + g) * TPR * VEC; }
-    __device__ __forceinline__ bool in(int g) const { return n(g) < N; }
-    template <class T, class Source>
-    __device__ __forceinline__ void read(const Source& src, int stage, int64_t m, float2 (&v)[4]) const {
-        Raw<T, VEC> r[G];
-#pragma unroll
-        for (int g = 0; g < G; ++g) {
-            if (in(g)) src.read(stage, m, c * G + g, r[g]);
-            else clear(r[g]);
-        }
-        pairs_of(r, v);
-    }
-    template <class T>
-    __device__ __forceinline__ void load(const void* row, float2 (&v)[4]) const {
-        Raw<T, VEC> r[G];
-#pragma unroll
-        for (int g = 0; g < G; ++g) {
-            if (in(g)) load_raw<T, VEC>(static_cast<const T*>(row) + n(g), r[g]);
-            else clear(r[g]);
-        }
-        pairs_of(r, v);
-    }
-    template <class TW>
-    __device__ __forceinline__ void weight(const void* w, float none, float2 (&v)[4]) const {
-        float f[G][VEC];
-#pragma unroll
-        for (int g = 0; g < G; ++g) {
-#pragma unroll
-            for (int e = 0; e < VEC; ++e) f[g][e] = 0.f;
-            if (in(g)) weights<TW, VEC>(w, n(g), none, f[g]);
-        }
-#pragma unroll
-        for (int k = 0; k < 4; ++k) v[k] = VEC == 8 ? make_float2(f[0][(2 * k) % VEC], f[0][(2 * k + 1) % VEC]) : make_float2(f[(2 * k) % G][0], f[(2 * k + 1) % G][0]);
-    }
-    template <class T>
-    __device__ __forceinline__ void store(void* row, const float2 (&v)[4]) const {
-#pragma unroll
-        for (int g = 0; g < G; ++g)
-            if (in(g)) {
-                float f[VEC];
-#pragma unroll
-                for (int e = 0; e < VEC; ++e) {
-                    const int k = g * VEC + e;
-                    f[e] = k & 1 ? v[k / 2].y : v[k / 2].x;
-                }
-                store_f<T, VEC>(static_cast<T*>(row) + n(g), f);
-            }
-    }
-};
-
 template <class TX, class TF, class TW, int VEC, int TPR, int NV, bool POST>
 __global__ void __launch_bounds__(TPR == 32 ? 128 : TPR, blocks_of(TPR)) residual_norm_backward_kernel(const BwdParams p) {
     using SX = RowSource<TX, VEC, TPR, NV>;
@@ -132,6 +59,9 @@ __global__ void __launch_bounds__(TPR == 32 ? 128 : TPR, blocks_of(TPR)) residua
         if (first + s * step < p.M) fetch(s, first + s * step);
         async_commit();
     }
+    // w and gate stay in registers, and, where a thread has 8 elements, pw and pb: as many as there is room for beside the sums
+    const Vector<TW, VEC, TPR, CH, (!POST || CH == 1)> w_of(p.v.w, 1.f, N, col), gate_of(p.v.gate, 1.f, N, col);
+    const Vector<TW, VEC, TPR, CH, POST && CH == 1> pw_of(p.v.pw, 1.f, N, col), pb_of(p.v.pb, 0.f, N, col);
     const float2 zero = both(0.f), scale = both(p.scale);
     float2 s0[CH][4], s1[CH][4], s2[CH][4], s3[POST ? CH : 1][4];
 #pragma unroll
@@ -163,8 +93,8 @@ __global__ void __launch_bounds__(TPR == 32 ? 128 : TPR, blocks_of(TPR)) residua
             float2 a[4], b[4];
             at.template read<TF>(sf, stage, m, f);
             if constexpr (POST) {
-                at.template weight<TW>(p.v.pw, 1.f, a);
-                at.template weight<TW>(p.v.pb, 0.f, b);
+                pw_of.get(at, a);
+                pb_of.get(at, b);
                 const float2 shift = both(-fmu), spread = both(fr);
 #pragma unroll
                 for (int k = 0; k < 4; ++k) {
@@ -176,7 +106,7 @@ __global__ void __launch_bounds__(TPR == 32 ? 128 : TPR, blocks_of(TPR)) residua
                 for (int k = 0; k < 4; ++k) h[k] = f[k];
             }
             at.template read<TX>(sx, stage, m, b);
-            at.template weight<TW>(p.v.gate, 1.f, a);
+            gate_of.get(at, a);
             const float2 shift = both(-mu), spread = both(r);
 #pragma unroll
             for (int k = 0; k < 4; ++k) h[k] = mul2(add2(fma2(scale, b[k], mul2(a[k], h[k])), shift), spread);
@@ -189,7 +119,7 @@ __global__ void __launch_bounds__(TPR == 32 ? 128 : TPR, blocks_of(TPR)) residua
             float2 f[4], h[4], dz[4], w[4];
             values(at, f, h);
             at.template read<TF>(sdz, stage, m, dz);
-            at.template weight<TW>(p.v.w, 1.f, w);
+            w_of.get(at, w);
 #pragma unroll
             for (int k = 0; k < 4; ++k) {
                 s0[c][k] = fma2(dz[k], h[k], s0[c][k]);
@@ -211,7 +141,7 @@ __global__ void __launch_bounds__(TPR == 32 ? 128 : TPR, blocks_of(TPR)) residua
             float2 f[4], h[4], d[4], w[4];
             values(at, f, h);
             at.template read<TF>(sdz, stage, m, d);
-            at.template weight<TW>(p.v.w, 1.f, w);
+            w_of.get(at, w);
 #pragma unroll
             for (int k = 0; k < 4; ++k) d[k] = mul2(spread, fma2(h[k], m1, fma2(d[k], w[k], m0)));
             if (has_dh) {
@@ -227,10 +157,10 @@ __global__ void __launch_bounds__(TPR == 32 ? 128 : TPR, blocks_of(TPR)) residua
                 w[k] = mul2(scale, d[k]);
             }
             if (p.dx) at.template store<TX>(static_cast<TX*>(p.dx) + m * p.lddx, w);
-            at.template weight<TW>(p.v.gate, 1.f, w);
+            gate_of.get(at, w);
             if constexpr (POST) {
                 float2 pw[4];
-                at.template weight<TW>(p.v.pw, 1.f, pw);
+                pw_of.get(at, pw);
 #pragma unroll
                 for (int k = 0; k < 4; ++k) {
                     q[c][k] = mul2(mul2(d[k], w[k]), pw[k]);

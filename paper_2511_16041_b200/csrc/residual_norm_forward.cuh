@@ -16,16 +16,19 @@ namespace {
 constexpr int kThreads[] = {32, 64, 128, 256, 384, 512, 768, 1024};
 template <class TX, class TF>
 constexpr int kMostThreads = sizeof(TX) + sizeof(TF) == 8 ? 768 : 1024;        // two stages of rows in shared memory
-template <class TX, class TF>
-constexpr int kAhead = sizeof(TX) + sizeof(TF) == 4 ? 2 : 1;
-// Blocks that stay on an SM: 1024 threads of 64 registers (768 an element at a time), 200 KB of rows.
-__host__ __device__ constexpr int resident(int threads, int stage_bytes, bool vec) {
-    const int by_threads = (vec ? 1024 : 768) / threads, by_room = 200 * 1024 / stage_bytes;
-    const int most = by_threads < by_room ? by_threads : by_room;
-    return most < 1 ? 1 : most;
-}
+// The vectors of weights stay in registers (a thread has the same columns of every row), but in the widest kernels, whose threads
+// have too few, and FP32 pw and pb, which would be two too many.
+__host__ __device__ constexpr bool keeps(int tpr) { return tpr <= 512; }
+// Blocks that stay on an SM: 512 threads of 128 registers.
+__host__ __device__ constexpr int resident(int tpr) { return tpr == 32 ? 4 : tpr >= 512 ? 1 : 512 / tpr; }
 template <class TX, class TF, int TPR, int NV, int VEC>
-constexpr int kRoom = (kAhead<TX, TF> + 1) * static_cast<int>(RowSource<TX, VEC, TPR, NV>::STAGE_BYTES + RowSource<TF, VEC, TPR, NV>::STAGE_BYTES);
+constexpr int kStageBytes = static_cast<int>(RowSource<TX, VEC, TPR, NV>::STAGE_BYTES + RowSource<TF, VEC, TPR, NV>::STAGE_BYTES);
+// Rows on their way: 3, or what 200 KB per SM hold beside the row in hand.
+template <class TX, class TF, int TPR, int NV, int VEC>
+__host__ __device__ constexpr int ahead_of() {
+    const int stages = 200 * 1024 / (resident(TPR) * kStageBytes<TX, TF, TPR, NV, VEC>);
+    return stages > 4 ? 3 : stages - 1;
+}
 
 // Mean and 1 / spread of a row whose elements its threads hold in v; v becomes distances d, and norm(v) is d r + shift.
 template <int TPR>
@@ -33,27 +36,30 @@ struct RowNorm {
     static constexpr int W = TPR / 32;
     int lane, warp, center;
     float elems, n, inv_n, inv_own, eps;
-    template <int NV, int VEC>
-    __device__ __forceinline__ void operator()(float (&v)[NV][VEC], const bool (&in)[NV], float2* red, float& mu, float& r, float& shift) const {
+    // Elements past the row's end: `in` tells (eights of single elements: by pairs' halves, eights of 8: whole eights)
+    template <int CH, class In>
+    __device__ __forceinline__ void operator()(float2 (&v)[CH][4], const In& in, float2* red, float& mu, float& r, float& shift) const {
         float s[1] = {0.f}, mine = 0.f;
         if (center) {
+            float2 sum = both(0.f);
 #pragma unroll
-            for (int i = 0; i < NV; ++i)
-                if (in[i])
+            for (int c = 0; c < CH; ++c)
 #pragma unroll
-                    for (int e = 0; e < VEC; ++e) s[0] += v[i][e];
+                for (int k = 0; k < 4; ++k) sum = add2(sum, v[c][k]);      // 0 past the row's end
+            s[0] = sum.x + sum.y;
             warp_sum(s);
             mine = quotient(s[0], __shfl_sync(0xFFFFFFFFu, elems, warp), inv_own);       // the mean of the warp's elements
-            s[0] = 0.f;
         }
+        float2 sq = both(0.f);
+        const float2 from = both(-mine);
 #pragma unroll
-        for (int i = 0; i < NV; ++i)
-            if (in[i])
+        for (int c = 0; c < CH; ++c)
 #pragma unroll
-                for (int e = 0; e < VEC; ++e) {
-                    v[i][e] -= mine;
-                    s[0] += v[i][e] * v[i][e];
-                }
+            for (int k = 0; k < 4; ++k) {
+                v[c][k] = in.only(add2(v[c][k], from), c, k);
+                sq = fma2(v[c][k], v[c][k], sq);
+            }
+        s[0] = sq.x + sq.y;
         warp_sum(s);
         mu = mine;
         if constexpr (TPR > 32) {
@@ -73,13 +79,29 @@ struct RowNorm {
     }
 };
 
+// Which of a thread's elements are in the row.
+template <int VEC, int TPR, int CH>
+struct Inside {
+    bool in[CH][VEC == 8 ? 1 : 8];
+    __device__ __forceinline__ Inside(int N, int col) {
+#pragma unroll
+        for (int c = 0; c < CH; ++c)
+#pragma unroll
+            for (int g = 0; g < 8 / VEC; ++g) in[c][g] = Eight<VEC, TPR>{N, col, c}.in(g);
+    }
+    __device__ __forceinline__ float2 only(float2 v, int c, int k) const {
+        if constexpr (VEC == 8) return in[c][0] ? v : both(0.f);
+        else return make_float2(in[c][(2 * k) % (8 / VEC)] ? v.x : 0.f, in[c][(2 * k + 1) % (8 / VEC)] ? v.y : 0.f);
+    }
+};
+
 template <class TX, class TF, class TW, int VEC, int TPR, int NV, bool POST>
-__global__ void __launch_bounds__(TPR == 32 ? 128 : TPR, resident(TPR == 32 ? 128 : TPR, kRoom<TX, TF, TPR, NV, VEC>, VEC > 1))
-residual_norm_kernel(const FwdParams p) {
+__global__ void __launch_bounds__(TPR == 32 ? 128 : TPR, resident(TPR)) residual_norm_kernel(const FwdParams p) {
     using SX = RowSource<TX, VEC, TPR, NV>;
     using SF = RowSource<TF, VEC, TPR, NV>;
     using Shared = std::conditional_t<SX::SHARED, SX, SF>;
-    constexpr int WALKERS = TPR == 32 ? 4 : 1, W = TPR / 32, AHEAD = kAhead<TX, TF>, STAGES = AHEAD + 1;
+    constexpr int WALKERS = TPR == 32 ? 4 : 1, W = TPR / 32, AHEAD = ahead_of<TX, TF, TPR, NV, VEC>(), STAGES = AHEAD + 1, CH = NV * VEC / 8;
+    static_assert(AHEAD >= 1, "shared memory");
     extern __shared__ __align__(16) uint8_t ring[];
     __shared__ float2 red[2][2][W];
     const int t = TPR == 32 ? threadIdx.x & 31 : threadIdx.x, lane = threadIdx.x & 31;
@@ -103,9 +125,7 @@ residual_norm_kernel(const FwdParams p) {
         const int own = __shfl_sync(0xFFFFFFFFu, count, norm.warp);
         norm.inv_own = own > 0 ? 1.f / static_cast<float>(own) : 0.f;
     }
-    bool in[NV];
-#pragma unroll
-    for (int i = 0; i < NV; ++i) in[i] = col + i * TPR * VEC < N;
+    const Inside<VEC, TPR, CH> in(N, col);
     sm100::grid_dependency_wait();
     sm100::grid_dependency_launch();
 #pragma unroll
@@ -116,6 +136,10 @@ residual_norm_kernel(const FwdParams p) {
         }
         async_commit();
     }
+    constexpr bool KEEP = keeps(TPR), KEEP_POST = KEEP && POST && sizeof(TW) == 2 && VEC == 8;
+    const Vector<TW, VEC, TPR, CH, KEEP> w_of(p.v.w, 1.f, N, col), b_of(p.v.b, 0.f, N, col), gate_of(p.v.gate, 1.f, N, col);
+    const Vector<TW, VEC, TPR, CH, KEEP_POST> pw_of(p.v.pw, 1.f, N, col), pb_of(p.v.pb, 0.f, N, col);
+    const float2 scale = both(p.scale);
     int stage = 0, turn = 0;
     for (int64_t m = first; m < p.M; m += step, turn ^= 1) {
         const int ahead = stage == 0 ? AHEAD : stage - 1;               // the stage that the row before this one has left
@@ -126,51 +150,44 @@ residual_norm_kernel(const FwdParams p) {
         async_commit();
         async_wait<AHEAD>();
         row_barrier<Shared, VEC, TPR>();
-        float v[NV][VEC];
+        float2 v[CH][4];
 #pragma unroll
-        for (int i = 0; i < NV; ++i)
-            if (in[i]) {
-                Raw<TF, VEC> raw;
-                sf.read(stage, m, i, raw);
-                to_float(raw, v[i]);
-            }
+        for (int c = 0; c < CH; ++c) Eight<VEC, TPR>{N, col, c}.template read<TF>(sf, stage, m, v[c]);
         float mu, r, shift;
         if constexpr (POST) {
             norm(v, in, red[0][turn], mu, r, shift);
             if (t == 0 && p.stats) { p.stats[2 * p.M + m] = mu; p.stats[3 * p.M + m] = r; }
         }
 #pragma unroll
-        for (int i = 0; i < NV; ++i)
-            if (in[i]) {
-                const int n = col + i * TPR * VEC;
-                float a[VEC], b[VEC];
-                if constexpr (POST) {
-                    weights<TW, VEC>(p.v.pw, n, 1.f, a);
-                    weights<TW, VEC>(p.v.pb, n, 0.f, b);
+        for (int c = 0; c < CH; ++c) {
+            const Eight<VEC, TPR> at{N, col, c};
+            float2 a[4], b[4];
+            if constexpr (POST) {
+                pw_of.get(at, a);
+                pb_of.get(at, b);
+                const float2 r2 = both(r), shift2 = both(shift);
 #pragma unroll
-                    for (int e = 0; e < VEC; ++e) v[i][e] = fmaf(fmaf(v[i][e], r, shift), a[e], b[e]);
-                }
-                Raw<TX, VEC> raw;
-                sx.read(stage, m, i, raw);
-                to_float(raw, b);
-                weights<TW, VEC>(p.v.gate, n, 1.f, a);
-#pragma unroll
-                for (int e = 0; e < VEC; ++e) v[i][e] = fmaf(p.scale, b[e], a[e] * v[i][e]);
-                store_f<TX, VEC>(static_cast<TX*>(p.h) + m * p.ldh + n, v[i]);
+                for (int k = 0; k < 4; ++k) v[c][k] = fma2(fma2(v[c][k], r2, shift2), a[k], b[k]);
             }
+            at.template read<TX>(sx, stage, m, b);
+            gate_of.get(at, a);
+#pragma unroll
+            for (int k = 0; k < 4; ++k) v[c][k] = in.only(fma2(scale, b[k], mul2(a[k], v[c][k])), c, k);
+            at.template store<TX>(static_cast<TX*>(p.h) + m * p.ldh, v[c]);
+        }
         norm(v, in, red[1][turn], mu, r, shift);
         if (t == 0 && p.stats) { p.stats[m] = mu; p.stats[p.M + m] = r; }
+        const float2 r2 = both(r), shift2 = both(shift);
 #pragma unroll
-        for (int i = 0; i < NV; ++i)
-            if (in[i]) {
-                const int n = col + i * TPR * VEC;
-                float a[VEC], b[VEC];
-                weights<TW, VEC>(p.v.w, n, 1.f, a);
-                weights<TW, VEC>(p.v.b, n, 0.f, b);
+        for (int c = 0; c < CH; ++c) {
+            const Eight<VEC, TPR> at{N, col, c};
+            float2 a[4], b[4];
+            w_of.get(at, a);
+            b_of.get(at, b);
 #pragma unroll
-                for (int e = 0; e < VEC; ++e) v[i][e] = fmaf(fmaf(v[i][e], r, shift), a[e], b[e]);
-                store_f<TF, VEC>(static_cast<TF*>(p.z) + m * p.ldz + n, v[i]);
-            }
+            for (int k = 0; k < 4; ++k) v[c][k] = fma2(fma2(v[c][k], r2, shift2), a[k], b[k]);
+            at.template store<TF>(static_cast<TF*>(p.z) + m * p.ldz, v[c]);
+        }
         stage = stage + 1 == STAGES ? 0 : stage + 1;
     }
 }
@@ -255,8 +272,8 @@ __global__ void __launch_bounds__(1024) residual_norm_wide_kernel(const FwdParam
 // ---------------------------------------------------------------------------------- host
 template <class TX, class TF, class TW, int VEC, bool POST, int TPR>
 cudaError_t launch_rows(const FwdParams& p, cudaStream_t st) {
-    constexpr int NV = kElems / VEC, THREADS = TPR == 32 ? 128 : TPR, ROOM = kRoom<TX, TF, TPR, NV, VEC>;
-    const int64_t all = atb::ceil_div(p.M, TPR == 32 ? 4 : 1), most = static_cast<int64_t>(atb::kSmCount) * resident(THREADS, ROOM, VEC > 1);
+    constexpr int NV = kElems / VEC, THREADS = TPR == 32 ? 128 : TPR, ROOM = (ahead_of<TX, TF, TPR, NV, VEC>() + 1) * kStageBytes<TX, TF, TPR, NV, VEC>;
+    const int64_t all = atb::ceil_div(p.M, TPR == 32 ? 4 : 1), most = static_cast<int64_t>(atb::kSmCount) * resident(TPR);
     return launch_ring(residual_norm_kernel<TX, TF, TW, VEC, TPR, NV, POST>, static_cast<unsigned>(all < most ? all : most), THREADS, ROOM, st, p);
 }
 template <class TX, class TF, class TW, int VEC, bool POST>
