@@ -80,7 +80,7 @@ struct Shared {
     unsigned long long weight[kBins];
     uint32_t span_count[kSpans];                   // sums over 32 bins
     unsigned long long span_weight[kSpans];
-    double span_most[kSpans], span_least[kSpans];
+    float span_most[kSpans], span_least[kSpans];
     Found found;
     unsigned long long beyond, whole;              // weight above the bins looked at, of all words
     double real;                                   // this CTA's weight, about
@@ -95,6 +95,7 @@ struct Shared {
     uint32_t equal;                                // this CTA's words at tau
     uint32_t joined;                               // a sum over the cluster
     uint32_t ends[kMostCtas];                      // of the CTAs' words in the first one's list
+    float lanes[32];                               // the last words of a search
     unsigned long long warp_total[kMostWarps];
     unsigned long long warp_beyond[kMostWarps];
     uint32_t warp_equal[kMostWarps];
@@ -110,17 +111,28 @@ __device__ __forceinline__ uint32_t key_of(float l) {            // ordered like
 __device__ __forceinline__ float of_key(uint32_t k) { return __uint_as_float(k & 0x80000000u ? k ^ 0x80000000u : ~k); }
 
 // -inf for NaN, and +0 for -0, which compare alike.
-__device__ __forceinline__ float canonical(float l) { return l == l ? l + 0.f : -INFINITY; }
+__device__ __forceinline__ float canonical(float l) {
+    float v;
+    asm("max.f32 %0, %1, 0fFF800000;" : "=f"(v) : "f"(l + 0.f));
+    return v;
+}
 
 // A warp's logits: chunks of 128 * vectors consecutive words, in shared memory as vectors of 4, vector j of lane i at words 128 j + 4 i of the chunk.
 template <class T>
 struct Row {
     const T* row;
     int V, vectors, first;                 // first: word of the warp's first logit (may lie before the row)
+    bool alone;                            // logits that are not `only` become -inf, those that are 0
+    float only;
     // word of element e of this lane's vector j of chunk c
     __device__ __forceinline__ int word(int c, int j, int lane, int e) const { return first + (c * vectors + j) * 128 + lane * 4 + e; }
-    // Chunk c to `to`, this warp's place.  Vectors of 16 bytes that lie inside the row are loaded whole.
-    __device__ __forceinline__ void load(int c, float4* to, int lane) const {
+    __device__ __forceinline__ float taken(float l) const {
+        const float v = canonical(l);
+        return !alone ? v : v == only ? 0.f : -INFINITY;
+    }
+    // Chunk c to `to`, this warp's place; returns this lane's largest.  Vectors of 16 bytes that lie inside the row are loaded whole.
+    __device__ __forceinline__ float load(int c, float4* to, int lane) const {
+        float top = -INFINITY;
         constexpr int PER = 16 / sizeof(T), AT_ONCE = 16 / PER, STEP = AT_ONCE * PER / 4;      // loads in flight, of STEP vectors
         const int from = first + c * vectors * 128 + lane * PER;
         __syncwarp();                      // the warp has read the chunk before
@@ -152,16 +164,22 @@ struct Row {
                 const uint32_t w[4] = {q[i].x, q[i].y, q[i].z, q[i].w};
                 float4* const dst = to + (j * 128 + i * 32 * PER + lane * PER) / 4;
                 if constexpr (sizeof(T) == 4) {
-                    *dst = make_float4(canonical(__uint_as_float(w[0])), canonical(__uint_as_float(w[1])), canonical(__uint_as_float(w[2])), canonical(__uint_as_float(w[3])));
+                    const float4 v = make_float4(taken(__uint_as_float(w[0])), taken(__uint_as_float(w[1])), taken(__uint_as_float(w[2])), taken(__uint_as_float(w[3])));
+                    *dst = v;
+                    top = fmaxf(top, fmaxf(fmaxf(v.x, v.y), fmaxf(v.z, v.w)));
                 } else {
-                    const auto lo = [&](int e) { return canonical(__uint_as_float(w[e] << 16)); };
-                    const auto hi = [&](int e) { return canonical(__uint_as_float(w[e] & 0xFFFF0000u)); };
-                    dst[0] = make_float4(lo(0), hi(0), lo(1), hi(1));
-                    dst[1] = make_float4(lo(2), hi(2), lo(3), hi(3));
+#pragma unroll
+                    for (int h = 0; h < 2; ++h) {
+                        const auto at = [&](int e) { return taken(__uint_as_float(e & 1 ? w[2 * h + e / 2] & 0xFFFF0000u : w[2 * h + e / 2] << 16)); };
+                        const float4 v = make_float4(at(0), at(1), at(2), at(3));
+                        dst[h] = v;
+                        top = fmaxf(top, fmaxf(fmaxf(v.x, v.y), fmaxf(v.z, v.w)));
+                    }
                 }
             }
         }
         __syncwarp();
+        return top;
     }
 };
 
@@ -183,15 +201,25 @@ __device__ __forceinline__ V warp_scan(V v, int lane) {          // inclusive
 
 // 2^(S - d slope), d >= 0, to the nearest integer, where slope16 = 16 slope: 2^(-round(16 y) / 16) from a table and the rest, at most 2^-5,
 // by the first terms of its series (Tang's table-driven method), relative error below 2^-50.  The sums with 1.5 * 2^52 and 2^52
-// round to an integer.  Sixteen entries lie in banks of their own.  d slope <= S + 3.
+// round to an integer.  Sixteen entries lie in banks of their own; the series' terms are operands from constant memory.  d slope < 1060.
+constexpr double kLn2of16 = 0.69314718055994530942 / 16;
+__constant__ double kSeries[6] = {kLn2of16,
+                                  kLn2of16* kLn2of16 / 2,
+                                  kLn2of16* kLn2of16* kLn2of16 / 6,
+                                  kLn2of16* kLn2of16* kLn2of16* kLn2of16 / 24,
+                                  kLn2of16* kLn2of16* kLn2of16* kLn2of16* kLn2of16 / 120,
+                                  kLn2of16* kLn2of16* kLn2of16* kLn2of16* kLn2of16* kLn2of16 / 720};
+__constant__ double kRound[2] = {0x1.8p52, 0x1p52};
 __device__ __forceinline__ unsigned long long fixed_exp2(double d, double slope16, int shift, const double* table) {
-    const double near = fma(d, slope16, 0x1.8p52);
+    const double near = fma(d, slope16, kRound[0]);
     const int q = -__double2loint(near);
-    const double r = fma(-d, slope16, near - 0x1.8p52);          // -16 y = q + r
-    constexpr double c1 = 0.69314718055994530942 / 16, c2 = c1 * c1 / 2, c3 = c2 * c1 / 3, c4 = c3 * c1 / 4, c5 = c4 * c1 / 5, c6 = c5 * c1 / 6;
-    const double p = fma(r, fma(r, fma(r, fma(r, fma(r, fma(r, c6, c5), c4), c3), c2), c1), 1.0) * table[q & 15];
+    const double r = fma(-d, slope16, near - kRound[0]);         // -16 y = q + r
+    double p = fma(r, kSeries[5], kSeries[4]);
+#pragma unroll
+    for (int i = 3; i >= 0; --i) p = fma(r, p, kSeries[i]);
+    p = fma(r, p, 1.0) * table[q & 15];
     const double scaled = __hiloint2double(__double2hiint(p) + (((q >> 4) + shift) << 20), __double2loint(p));
-    const double whole = scaled + 0x1p52;
+    const double whole = scaled + kRound[1];
     return static_cast<unsigned long long>(__double_as_longlong(whole)) - 0x4330000000000000ull;
 }
 
@@ -201,7 +229,7 @@ __device__ __forceinline__ V cluster_sum(const cg::cluster_group& cluster, int r
     return warp_add(lane < ranks ? *cluster.map_shared_rank(own, lane) : V(0));
 }
 
-// T: type of the logits.  RESIDENT: a thread's logits are 16, and stay in registers.
+// T: type of the logits.  RESIDENT: a row's logits fit the cluster's shared memory.
 template <class T, bool RESIDENT>
 __global__ void __launch_bounds__(kMostThreads, 2) sample_kernel(const SampleParams p) {
     __shared__ Shared sh;
@@ -228,8 +256,16 @@ __global__ void __launch_bounds__(kMostThreads, 2) sample_kernel(const SamplePar
         row.vectors = p.vectors;
         row.first = (rank * warps + warp) * p.chunks * p.vectors * 128 - static_cast<int>(skip);
     }
+    row.alone = false;
+    row.only = 0.f;
     float4* const mine4 = logits + warp * 32 * p.vectors;
-    if constexpr (RESIDENT) row.load(0, mine4, lane);
+    float top = -INFINITY;
+    if constexpr (RESIDENT) {
+        top = row.load(0, mine4, lane);
+    } else {
+#pragma unroll 1
+        for (int c = 0; c < p.chunks; ++c) top = fmaxf(top, row.load(c, mine4, lane));
+    }
     // f(chunk, vector, logits) over this thread's logits in the words' order
     const auto each = [&](auto&& f) {
 #pragma unroll 1
@@ -251,7 +287,7 @@ __global__ void __launch_bounds__(kMostThreads, 2) sample_kernel(const SamplePar
     const bool greedy = !(temperature > 0.0);
     if (greedy) k = 1;
     if (k <= 0 || k > p.V) k = p.V;
-    const double slope = greedy ? 1.4426950408889634074 : 1.4426950408889634074 / temperature;
+    double slope = greedy ? 1.4426950408889634074 : 1.4426950408889634074 / temperature;
     if (t == 0) {                          // what is needed late waits in shared memory
         const double min_p = real(p.min_p);
         sh.u = p.u64 ? static_cast<const double*>(p.u)[m] : static_cast<double>(static_cast<const float*>(p.u)[m]);
@@ -261,11 +297,6 @@ __global__ void __launch_bounds__(kMostThreads, 2) sample_kernel(const SamplePar
     }
 
     // ---- the largest logit, and those of the groups
-    float top = -INFINITY;
-    each([&](int, int, const float (&v)[4]) {
-#pragma unroll
-        for (int i = 0; i < 4; ++i) top = fmaxf(top, v[i]);
-    });
     for (int o = 1; o < 32; o <<= 1) {
         if (o == p.group && !(lane & (o - 1))) sh.group_top[t / o] = top;
         top = fmaxf(top, __shfl_xor_sync(0xFFFFFFFFu, top, o));
@@ -297,18 +328,25 @@ __global__ void __launch_bounds__(kMostThreads, 2) sample_kernel(const SamplePar
         return;
     }
 
+    // Where only words that equal the largest weigh anything - it is infinite, or its neighbour is more than 250 powers of 2 below it - the others
+    // become -inf and those 0, so that all differences below are finite and no product of them is too large.
+    const double nearest = fmax(static_cast<double>(fabsf(top)) * 0x1p-24, 0x1p-149);         // no two numbers at the largest are nearer
+    const bool alone = !(top < INFINITY) || !(slope * nearest <= 250.0);
+    if (alone) {
+        row.alone = true;
+        row.only = top;
+        top = 0.f;
+        slope = 1.0;
+        if constexpr (RESIDENT) row.load(0, mine4, lane);
+    }
     // depth of a logit below the largest, in powers of 2
-    const auto depth = [&](float l) { return l == top ? 0.0 : (static_cast<double>(top) - static_cast<double>(l)) * slope; };
-    const double slope16 = 16.0 * slope;
-    const float slope_f = static_cast<float>(slope);
-    // without branches, so that several run at once
-    const auto weight = [&](float l) -> unsigned long long {
-        // a difference that is too far, infinite or no number weighs nothing (halves: that of two finite numbers is finite)
-        const bool some = (0.5f * top - 0.5f * l) * slope_f < 0.5f * static_cast<float>(p.shift + 2);
-        const double d = static_cast<double>(top) - static_cast<double>(some ? l : top);
-        const unsigned long long w = fixed_exp2(d, some ? slope16 : 0.0, p.shift, sh.table);
-        return l == top ? 1ull << p.shift : some ? w : 0ull;
-    };
+    const auto depth = [&](float l) { return (static_cast<double>(top) - static_cast<double>(l)) * slope; };
+    const float half_top = 0.5f * top, slope_f = fminf(static_cast<float>(slope), 1e30f);
+    const double slope16 = 16.0 * slope, top64 = top;
+    // no logit deeper than this weighs anything, and neither does this (depth below 48.5 + 1000, by the rounding down)
+    const float floor_l = fmaxf(__fsub_rd(top, static_cast<float>(48.5 / slope)), -3.402823466e38f);
+    // of a finite logit, without branches, so that several run at once
+    const auto weight = [&](float l) { return fixed_exp2(top64 - static_cast<double>(fmaxf(l, floor_l)), slope16, p.shift, sh.table); };
     // the first word whose sum exceeds u * all: at least this much
     const auto target_of = [&](unsigned long long all) {
         const double u = sh.u, at = u > 0.0 ? u * static_cast<double>(all) : 0.0;
@@ -317,7 +355,7 @@ __global__ void __launch_bounds__(kMostThreads, 2) sample_kernel(const SamplePar
 
     // ---- few words
     const int groups = static_cast<int>(blockDim.x) / p.group;   // of a CTA
-    if (k <= groups * ranks * 3 / 4) {
+    if (!alone && k <= groups * ranks * 3 / 4) {
         const int n = groups * ranks;      // at most 256
         for (int i = t; i < n; i += blockDim.x) sh.all_groups[i] = *cluster.map_shared_rank(&sh.group_top[i % groups], i / groups);
         __syncthreads();
@@ -406,13 +444,13 @@ __global__ void __launch_bounds__(kMostThreads, 2) sample_kernel(const SamplePar
     // ---- the kept words: above tau, and `quota` of those that equal it
     uint32_t tau = 0;                      // key; nothing that can be drawn is at 0
     uint32_t quota = 0, equal_all = 0;     // equal_all: words at tau
-    int turn = 0;
-    // bins of equal width below the largest logit; falls with l, as every step of it does
+    // bins of equal width below the largest logit; falls with l, as every step of it does (halves: the difference of two finite numbers is
+    // finite; the floor is read off a sum with 2^23)
     const auto bin_of = [&](float l, float scale) {
-        const float d = (0.5f * top - 0.5f * l) * (2.f * scale);         // halves: the difference of two finite numbers is finite
-        // floor(d), read off the sum with 2^23
-        return l == top ? 0 : d < static_cast<float>(kBins - 1) ? static_cast<int>(__float_as_uint(__fadd_rd(d, 8388608.f)) & (kBins - 1)) : kBins - 1;
+        const float d = fminf(fmaf(l, -0.5f, half_top) * (2.f * scale), static_cast<float>(kBins - 1));
+        return static_cast<int>(__float_as_uint(__fadd_rd(d, 8388608.f)) & (kBins - 1));
     };
+    const auto at_least = [](uint32_t key) { return key ? of_key(key) : -3.402823466e38f; };       // keys from `key` on that are no -inf
     // f(bin of this lane, span) in the first CTA: a warp takes 32 bins at a time
     const auto spans = [&](auto&& f) {
         for (int span = warp; span < kSpans; span += warps) f(span * 32 + lane, span);
@@ -436,24 +474,28 @@ __global__ void __launch_bounds__(kMostThreads, 2) sample_kernel(const SamplePar
     };
     // The first bin of the first CTA's histogram at which `reached` holds of the sums from the first bin on and what stands above them: to sh.found
     // (first, above_count, above, active: the words in it).  For all its threads.
-    const auto find = [&](auto&& reached) {
+    const auto find = [&](bool by_weight, auto&& reached) {
         const uint32_t above_count = sh.found.above_count;
         const unsigned long long above = sh.found.above;
         spans([&](int b, int span) {
-            const uint32_t n = warp_add(sh.count[b]);
-            const unsigned long long w = warp_add(sh.weight[b]);
-            if (lane == 0) { sh.span_count[span] = n; sh.span_weight[span] = w; }
+            if (by_weight) {
+                const unsigned long long w = warp_add(sh.weight[b]);
+                if (lane == 0) sh.span_weight[span] = w;
+            } else {
+                const uint32_t n = __reduce_add_sync(0xFFFFFFFFu, sh.count[b]);
+                if (lane == 0) sh.span_count[span] = n;
+            }
         });
         __syncthreads();
         if (t == 0) sh.found.first = -1;
         __syncthreads();
         spans([&](int b, int span) {
-            uint32_t n = above_count + warp_add(lane < span ? sh.span_count[lane] : 0u);
-            unsigned long long w = above + warp_add(lane < span ? sh.span_weight[lane] : 0ull);
             const uint32_t own = sh.count[b];
             const unsigned long long own_weight = sh.weight[b];
-            n += warp_scan(own, lane);
-            w += warp_scan(own_weight, lane);
+            uint32_t n = 0;
+            unsigned long long w = 0;
+            if (by_weight) w = above + warp_add(lane < span ? sh.span_weight[lane] : 0ull) + warp_scan(own_weight, lane);
+            else n = above_count + __reduce_add_sync(0xFFFFFFFFu, lane < span ? sh.span_count[lane] : 0u) + warp_scan(own, lane);
             // sums do not fall, so that one bin is the first
             if (reached(n, w) && !(b > 0 && reached(n - own, w - own_weight))) {
                 sh.found.first = b;
@@ -501,9 +543,10 @@ __global__ void __launch_bounds__(kMostThreads, 2) sample_kernel(const SamplePar
         }
         bool begin = by_weight;            // the weights are still to be added up
         while (true) {
-            const bool alone = sh.found.active <= kWords;        // few enough for the first CTA
+            const bool few = sh.found.active <= kWords;          // enough for the first CTA
             const int width = width_of(high - low);
             unsigned long long beyond = 0, whole = 0;
+            const float high_l = of_key(high), least_l = at_least(least), low_l = fmaxf(least_l, low > 0x007FFFFFu ? of_key(low) : -INFINITY);
             each([&](int c, int j, const float (&v)[4]) {
                 unsigned long long w[4] = {};
                 if (begin) {
@@ -512,20 +555,19 @@ __global__ void __launch_bounds__(kMostThreads, 2) sample_kernel(const SamplePar
                 }
 #pragma unroll
                 for (int i = 0; i < 4; ++i) {
-                    const uint32_t key = key_of(v[i]);
-                    w[i] = key >= least ? w[i] : 0ull;
-                    whole += w[i];
-                    beyond += key > high ? w[i] : 0ull;
-                    if (key <= high && key >= low && key >= least && v[i] > -INFINITY) {
+                    const bool in = v[i] >= least_l;
+                    whole += in ? w[i] : 0ull;
+                    beyond += in && v[i] > high_l ? w[i] : 0ull;
+                    if (v[i] <= high_l && v[i] >= low_l) {
                         const int b = bin_of(v[i], scale);
                         if (b < first) {
                             beyond += w[i];
                         } else if (b <= last) {
-                            if (alone) {
+                            if (few) {
                                 const uint32_t at = atomicAdd(&sh.candidates, 1u);
                                 if (at < kWords) sh.active[at] = {v[i], row.word(c, j, lane, i)};
                             } else {
-                                const int at = static_cast<int>((high - key) >> width);
+                                const int at = static_cast<int>((high - key_of(v[i])) >> width);
                                 atomicAdd(&sh.count[at], 1u);
                                 if (by_weight) atomicAdd(&sh.weight[at], begin ? w[i] : weight(v[i]));
                             }
@@ -546,12 +588,12 @@ __global__ void __launch_bounds__(kMostThreads, 2) sample_kernel(const SamplePar
                     whole = warp_add(lane < warps ? sh.warp_total[lane] : 0ull);
                     if (lane == 0) { sh.beyond = beyond; sh.whole = whole; }
                 }
-                listed = alone;
+                listed = few;
             }
             cluster.sync();
             if (rank == 0) {
                 int n = 0;
-                if (!alone) {
+                if (!few) {
                     join(by_weight);
                 } else {
                     // the words into this CTA's own memory
@@ -574,13 +616,13 @@ __global__ void __launch_bounds__(kMostThreads, 2) sample_kernel(const SamplePar
                         const unsigned long long up = cluster_sum(cluster, ranks, &sh.beyond, lane), all = cluster_sum(cluster, ranks, &sh.whole, lane);
                         if (lane == 0) {
                             sh.found.above += up;
-                            sh.found.goal = sh.top_p > 0.0 ? sh.top_p * static_cast<double>(all - excess) : 0.0;
+                            sh.found.goal = fmax(sh.top_p > 0.0 ? sh.top_p * static_cast<double>(all - excess) : 0.0, 0.5);       // one word at least
                         }
                     }
                     __syncthreads();
                 }
-                if (!alone) {
-                    find(reached);
+                if (!few) {
+                    find(by_weight, reached);
                     if (t == 0) {
                         sh.found.done = width == 0;
                         sh.found.tau = high - static_cast<uint32_t>(sh.found.first);
@@ -599,13 +641,48 @@ __global__ void __launch_bounds__(kMostThreads, 2) sample_kernel(const SamplePar
                             if (by_weight) atomicAdd(&sh.weight[at], weight(sh.words[i]));
                         }
                         __syncthreads();
-                        find(reached);
+                        find(by_weight, reached);
                         const int bin = sh.found.first;
                         if (w == 0 || bin < 0) {
                             if (t == 0) {
                                 sh.found.done = 1;
                                 sh.found.tau = to - static_cast<uint32_t>(bin);
                                 sh.found.equal = sh.found.active;
+                            }
+                            break;
+                        }
+                        if (sh.found.active <= 32) {
+                            // the words of that bin, to a lane of one warp each
+                            const uint32_t last_key = to - (static_cast<uint32_t>(bin) << w), first_key = last_key - ((1u << w) - 1u);
+                            if (t == 0) sh.joined = 0;
+                            __syncthreads();
+                            for (int i = t; i < n; i += blockDim.x) {
+                                const uint32_t key = key_of(sh.words[i]);
+                                if (key <= last_key && key >= first_key && key >= from) sh.lanes[atomicAdd(&sh.joined, 1u) & 31u] = sh.words[i];
+                            }
+                            __syncthreads();
+                            if (warp == 0) {
+                                const int count = static_cast<int>(min(sh.joined, 32u));
+                                const float l = lane < count ? sh.lanes[lane] : -INFINITY;
+                                const unsigned long long own = by_weight && lane < count ? weight(l) : 0ull;
+                                uint32_t above_n = sh.found.above_count, equal = 0;
+                                unsigned long long above_w = sh.found.above;
+                                for (int j = 0; j < count; ++j) {
+                                    const float other = __shfl_sync(0xFFFFFFFFu, l, j);
+                                    const unsigned long long its = __shfl_sync(0xFFFFFFFFu, own, j);
+                                    above_n += other > l;
+                                    above_w += other > l ? its : 0ull;
+                                    equal += other == l;
+                                }
+                                const bool here = lane < count && reached(above_n + equal, above_w + equal * own) && !reached(above_n, above_w);
+                                const unsigned lanes_here = __ballot_sync(0xFFFFFFFFu, here);          // of one number
+                                if (lane == __ffs(lanes_here) - 1) {
+                                    sh.found.done = 1;
+                                    sh.found.tau = key_of(l);
+                                    sh.found.equal = equal;
+                                    sh.found.above_count = above_n;
+                                    sh.found.above = above_w;
+                                }
                             }
                             break;
                         }
@@ -650,7 +727,7 @@ __global__ void __launch_bounds__(kMostThreads, 2) sample_kernel(const SamplePar
         if (rank == 0) {
             if (t == 0) { sh.found.above_count = 0; sh.found.above = 0; sh.found.done = 0; }
             join(false);
-            find(reached);
+            find(false, reached);
             if (t == 0) sh.found.last = sh.found.first;
         }
         publish();
@@ -662,18 +739,17 @@ __global__ void __launch_bounds__(kMostThreads, 2) sample_kernel(const SamplePar
     unsigned long long mine = 0;
     if (by_p) {
         const uint32_t tau_k = tau, quota_k = quota, equal_k = equal_all;
-        const float scale = static_cast<float>(slope * kBinsPerUnit);
+        const float scale = fminf(static_cast<float>(slope * kBinsPerUnit), 1e30f), least_l = at_least(tau_k);
         // their weight, about, and how many there are in bins of depth
         double sum = 0.0;
         each([&](int, int, const float (&v)[4]) {
             float some = 0.f;
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
-                const bool in = key_of(v[i]) >= tau_k && v[i] > -INFINITY;
-                const float y = (0.5f * top - 0.5f * v[i]) * (2.f * slope_f);
+                const bool in = v[i] >= least_l;
                 float w;
-                asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(w) : "f"(-y));
-                some += in && y < 120.f ? w : 0.f;
+                asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(w) : "f"(fmaf(v[i], -0.5f, half_top) * (-2.f * slope_f)));
+                some += in ? w : 0.f;
                 if (in) atomicAdd(&sh.count[bin_of(v[i], scale)], 1u);
             }
             sum += static_cast<double>(some);
@@ -693,42 +769,47 @@ __global__ void __launch_bounds__(kMostThreads, 2) sample_kernel(const SamplePar
                 if (lane == 0) { sh.real = sum_all; sh.found.above_count = 0; sh.found.above = 0; sh.found.done = 0; }
             }
             join(false);
-            // What the words of bin b weigh together: their count times what its ends weigh, a little more or less for bin_of's roundings and the
-            // weights' own.  The sum of all is within 1e-4 of what was added up (FP32: 2^-18 where y is 47), but where the largest logit
-            // is infinite, or differences are too small for FP32: there the bins say nothing, and all words are looked at.
-            const double one = static_cast<double>(1ull << p.shift), all = sh.real * one, low_all = all * (1.0 - 1e-4), high_all = all * (1.0 + 1e-4);
-            const bool known = top < INFINITY && scale > 1e-30f && scale < 1e30f;
-            const double cut = static_cast<double>(excess), low_goal = sh.top_p * fmax(low_all - cut, 0.0), high_goal = sh.top_p * fmax(high_all - cut, 0.0);
-            const auto most_of = [&](int b) { return sh.count[b] * (one * exp2f(static_cast<float>(b) / -kBinsPerUnit) * 1.0001 + 1.0); };
+            // What the words of bin b weigh together, in units of 2^S: their count times what its ends weigh, a little more or less for
+            // bin_of's roundings and the weights' own.  The sum of all is within 1.5e-5 of what was added up (a product of y <= 47 is
+            // off by 3 * 2^-24 of it, and its power by as much times y ln 2), all sums here within 1e-6.  Where the scale has
+            // left its range, the bins say nothing, and all words are looked at.
+            const float all = static_cast<float>(sh.real), cut = static_cast<float>(static_cast<double>(excess) / static_cast<double>(1ull << p.shift));
+            const float low_all = all * (1.f - 1.5e-5f), high_all = all * (1.f + 1.5e-5f), top_p = static_cast<float>(sh.top_p);
+            const float low_goal = top_p * fmaxf(low_all - cut, 0.f) * (1.f - 1e-6f), high_goal = top_p * fmaxf(high_all - cut, 0.f) * (1.f + 1e-6f);
+            const bool known = scale > 1e-30f && scale < 1e30f;
+            const float unit = exp2f(static_cast<float>(-p.shift));
+            const auto most_of = [&](int b) { return static_cast<float>(sh.count[b]) * (exp2f(static_cast<float>(b) / -kBinsPerUnit) * (1.f + 2e-5f) + unit); };
             const auto least_of = [&](int b) {
-                return b == kBins - 1 ? 0.0 : sh.count[b] * fmax(one * exp2f(static_cast<float>(b + 1) / -kBinsPerUnit) * 0.9999 - 1.0, 0.0);
+                return b == kBins - 1 ? 0.f : static_cast<float>(sh.count[b]) * fmaxf(exp2f(static_cast<float>(b + 1) / -kBinsPerUnit) * (1.f - 2e-5f) - unit, 0.f);
             };
             spans([&](int b, int span) {
-                const double most = warp_add(most_of(b)), least = warp_add(least_of(b));
+                const float most = warp_add(most_of(b)), least = warp_add(least_of(b));
                 if (lane == 0) { sh.span_most[span] = most; sh.span_least[span] = least; }
             });
             if (t == 0) { sh.found.first = known ? kBins - 1 : 0; sh.found.last = kBins - 1; sh.found.active = 0; }
             __syncthreads();
             if (known)
                 spans([&](int b, int span) {
-                    const double most_span = lane < kSpans ? sh.span_most[lane] : 0.0, least_span = lane < kSpans ? sh.span_least[lane] : 0.0;
-                    const double most_all = warp_add(most_span), least_all = warp_add(least_span);
-                    const double most = warp_add(lane < span ? most_span : 0.0) + warp_scan(most_of(b), lane);
-                    const double least = warp_add(lane < span ? least_span : 0.0) + warp_scan(least_of(b), lane);
-                    // the sum up to bin b, from above and as all but what is below it: may it, and must it have reached the goal?
-                    const double up = fmin(most, high_all - (least_all - least) * (1.0 - 1e-9)), down = fmax(least, low_all - (most_all - most) * (1.0 + 1e-9));
-                    if (up >= low_goal * (1.0 - 1e-9)) atomicMin(&sh.found.first, b);
-                    if (down >= high_goal * (1.0 + 1e-9)) atomicMin(&sh.found.last, b);
+                    const float most_span = lane < kSpans ? sh.span_most[lane] : 0.f, least_span = lane < kSpans ? sh.span_least[lane] : 0.f;
+                    // the sum up to bin b, and what is below it
+                    const float most_own = most_of(b), least_own = least_of(b), most_to = warp_scan(most_own, lane), least_to = warp_scan(least_own, lane);
+                    const float most = warp_add(lane < span ? most_span : 0.f) + most_to, least = warp_add(lane < span ? least_span : 0.f) + least_to;
+                    const float most_below = warp_add(lane > span ? most_span : 0.f) + (__shfl_sync(0xFFFFFFFFu, most_to, 31) - most_to);
+                    const float least_below = warp_add(lane > span ? least_span : 0.f) + (__shfl_sync(0xFFFFFFFFu, least_to, 31) - least_to);
+                    // from above, and as all but what is below: may it, and must it have reached the goal?
+                    const float slack = 1e-6f * (most + most_below);
+                    const float up = fminf(most, high_all - least_below) + slack, down = fmaxf(least, low_all - most_below) - slack;
+                    if (up >= low_goal) atomicMin(&sh.found.first, b);
+                    if (down >= high_goal) atomicMin(&sh.found.last, b);
                 });
             __syncthreads();
             spans([&](int b, int) {
-                const uint32_t n = warp_add(b >= sh.found.first && b <= sh.found.last ? sh.count[b] : 0u);
+                const uint32_t n = __reduce_add_sync(0xFFFFFFFFu, b >= sh.found.first && b <= sh.found.last ? sh.count[b] : 0u);
                 if (lane == 0 && n) atomicAdd(&sh.found.active, n);
             });
         }
         publish();
-        // (the words above the bins looked at are not counted, but there is one at least in every sum: the bins that can reach the goal begin at a word)
-        const bool found = narrow(true, [&](uint32_t n, unsigned long long w) { return n > 0 && static_cast<double>(w) >= sh.found.goal; }, tau_k, scale, excess);
+        const bool found = narrow(true, [&](uint32_t, unsigned long long w) { return static_cast<double>(w) >= sh.found.goal; }, tau_k, scale, excess);
         const double goal = sh.found.goal;
         if (found) {
             // of the words at tau, those before which the weight is below the goal
