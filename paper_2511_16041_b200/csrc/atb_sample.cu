@@ -48,6 +48,7 @@ struct SampleParams {
     int vectors;                                   // even
     int group;                                     // lanes that share a largest logit
 };
+static_assert(kBins == 1024, "32 spans of 32 bins: a lane to a span");
 constexpr int kMostGroups = 256, kCandidates = 512, kWords = 2048, kSpans = kBins / 32;
 struct Candidate {
     float l;
@@ -80,7 +81,7 @@ struct Shared {
     unsigned long long weight[kBins];
     uint32_t span_count[kSpans];                   // sums over 32 bins
     unsigned long long span_weight[kSpans];
-    float span_most[kSpans], span_least[kSpans];
+    float span_most[kSpans], span_least[kSpans], most, least;
     Found found;
     unsigned long long beyond, whole;              // weight above the bins looked at, of all words
     double real;                                   // this CTA's weight, about
@@ -101,7 +102,7 @@ struct Shared {
     uint32_t warp_equal[kMostWarps];
     float warp_top[kMostWarps];
     double u, top_p, deepest;                      // the row's; deepest: powers of 2 below the largest that min_p leaves
-    double table[16];                              // 2^(j / 16)
+    double table[16];                              // 2^(S - j / 16)
 };
 
 __device__ __forceinline__ uint32_t key_of(float l) {            // ordered like the logits; -0 does not occur
@@ -199,9 +200,10 @@ __device__ __forceinline__ V warp_scan(V v, int lane) {          // inclusive
     return v;
 }
 
-// 2^(S - d slope), d >= 0, to the nearest integer, where slope16 = 16 slope: 2^(-round(16 y) / 16) from a table and the rest, at most 2^-5,
-// by the first terms of its series (Tang's table-driven method), relative error below 2^-50.  The sums with 1.5 * 2^52 and 2^52
-// round to an integer.  Sixteen entries lie in banks of their own; the series' terms are operands from constant memory.  d slope < 1060.
+// 2^(S - d slope), d >= 0, to the nearest integer, where slope16 = 16 slope: 2^(-round(16 y) / 16), from a table times 2^S, and the rest, at
+// most 2^-5, by the first terms of its series (Tang's table-driven method), relative error below 2^-50.  The sums with
+// 1.5 * 2^52 and 2^52 round to an integer.  Sixteen entries lie in banks of their own; the series' terms are operands from constant
+// memory.  d slope < 1060.  As a double, and with 2^52 added, whose bits are the integer's.
 constexpr double kLn2of16 = 0.69314718055994530942 / 16;
 __constant__ double kSeries[6] = {kLn2of16,
                                   kLn2of16* kLn2of16 / 2,
@@ -210,17 +212,15 @@ __constant__ double kSeries[6] = {kLn2of16,
                                   kLn2of16* kLn2of16* kLn2of16* kLn2of16* kLn2of16 / 120,
                                   kLn2of16* kLn2of16* kLn2of16* kLn2of16* kLn2of16* kLn2of16 / 720};
 __constant__ double kRound[2] = {0x1.8p52, 0x1p52};
-__device__ __forceinline__ unsigned long long fixed_exp2(double d, double slope16, int shift, const double* table) {
+__device__ __forceinline__ double fixed_exp2_biased(double d, double slope16, const double* table) {
     const double near = fma(d, slope16, kRound[0]);
-    const int q = -__double2loint(near);
-    const double r = fma(-d, slope16, near - kRound[0]);         // -16 y = q + r
+    const int n = __double2loint(near);
+    const double r = fma(-d, slope16, near - kRound[0]);         // 16 y = n - r
     double p = fma(r, kSeries[5], kSeries[4]);
 #pragma unroll
     for (int i = 3; i >= 0; --i) p = fma(r, p, kSeries[i]);
-    p = fma(r, p, 1.0) * table[q & 15];
-    const double scaled = __hiloint2double(__double2hiint(p) + (((q >> 4) + shift) << 20), __double2loint(p));
-    const double whole = scaled + kRound[1];
-    return static_cast<unsigned long long>(__double_as_longlong(whole)) - 0x4330000000000000ull;
+    p = fma(r, p, 1.0) * table[n & 15];
+    return __hiloint2double(__double2hiint(p) - (n & ~15) * 65536, __double2loint(p)) + kRound[1];
 }
 
 // Sum over the first `ranks` CTAs of what they have at `own`: by one warp, a lane to a CTA, so that a value crosses once.
@@ -243,7 +243,7 @@ __global__ void __launch_bounds__(kMostThreads, 2) sample_kernel(const SamplePar
         sh.weight[i] = 0;
     }
     if (t == 0) sh.candidates = 0;
-    if (t < 16) sh.table[t] = exp2(t * 0.0625);
+    if (t < 16) sh.table[t] = exp2(p.shift - t * 0.0625);
     sm100::grid_dependency_wait();
     sm100::grid_dependency_launch();
 
@@ -346,7 +346,8 @@ __global__ void __launch_bounds__(kMostThreads, 2) sample_kernel(const SamplePar
     // no logit deeper than this weighs anything, and neither does this (depth below 48.5 + 1000, by the rounding down)
     const float floor_l = fmaxf(__fsub_rd(top, static_cast<float>(48.5 / slope)), -3.402823466e38f);
     // of a finite logit, without branches, so that several run at once
-    const auto weight = [&](float l) { return fixed_exp2(top64 - static_cast<double>(fmaxf(l, floor_l)), slope16, p.shift, sh.table); };
+    const auto biased = [&](float l) { return fixed_exp2_biased(top64 - static_cast<double>(fmaxf(l, floor_l)), slope16, sh.table); };
+    const auto weight = [&](float l) { return static_cast<unsigned long long>(__double_as_longlong(biased(l))) - 0x4330000000000000ull; };
     // the first word whose sum exceeds u * all: at least this much
     const auto target_of = [&](unsigned long long all) {
         const double u = sh.u, at = u > 0.0 ? u * static_cast<double>(all) : 0.0;
@@ -475,8 +476,6 @@ __global__ void __launch_bounds__(kMostThreads, 2) sample_kernel(const SamplePar
     // The first bin of the first CTA's histogram at which `reached` holds of the sums from the first bin on and what stands above them: to sh.found
     // (first, above_count, above, active: the words in it).  For all its threads.
     const auto find = [&](bool by_weight, auto&& reached) {
-        const uint32_t above_count = sh.found.above_count;
-        const unsigned long long above = sh.found.above;
         spans([&](int b, int span) {
             if (by_weight) {
                 const unsigned long long w = warp_add(sh.weight[b]);
@@ -487,15 +486,24 @@ __global__ void __launch_bounds__(kMostThreads, 2) sample_kernel(const SamplePar
             }
         });
         __syncthreads();
-        if (t == 0) sh.found.first = -1;
+        if (warp == 0) {                   // to the sums before each span
+            if (by_weight) {
+                const unsigned long long own = sh.span_weight[lane];
+                sh.span_weight[lane] = sh.found.above + warp_scan(own, lane) - own;
+            } else {
+                const uint32_t own = sh.span_count[lane];
+                sh.span_count[lane] = sh.found.above_count + warp_scan(own, lane) - own;
+            }
+            if (lane == 0) sh.found.first = -1;
+        }
         __syncthreads();
         spans([&](int b, int span) {
             const uint32_t own = sh.count[b];
             const unsigned long long own_weight = sh.weight[b];
             uint32_t n = 0;
             unsigned long long w = 0;
-            if (by_weight) w = above + warp_add(lane < span ? sh.span_weight[lane] : 0ull) + warp_scan(own_weight, lane);
-            else n = above_count + __reduce_add_sync(0xFFFFFFFFu, lane < span ? sh.span_count[lane] : 0u) + warp_scan(own, lane);
+            if (by_weight) w = sh.span_weight[span] + warp_scan(own_weight, lane);
+            else n = sh.span_count[span] + warp_scan(own, lane);
             // sums do not fall, so that one bin is the first
             if (reached(n, w) && !(b > 0 && reached(n - own, w - own_weight))) {
                 sh.found.first = b;
@@ -545,23 +553,26 @@ __global__ void __launch_bounds__(kMostThreads, 2) sample_kernel(const SamplePar
         while (true) {
             const bool few = sh.found.active <= kWords;          // enough for the first CTA
             const int width = width_of(high - low);
-            unsigned long long beyond = 0, whole = 0;
+            // (a thread's sums are below 2^53: 2^50 at most)
+            double beyond64 = 0.0, whole64 = 0.0;
             const float high_l = of_key(high), least_l = at_least(least), low_l = fmaxf(least_l, low > 0x007FFFFFu ? of_key(low) : -INFINITY);
             each([&](int c, int j, const float (&v)[4]) {
-                unsigned long long w[4] = {};
+                double w[4] = {};
                 if (begin) {
 #pragma unroll
-                    for (int i = 0; i < 4; ++i) w[i] = weight(v[i]);
+                    for (int i = 0; i < 4; ++i) w[i] = biased(v[i]) - kRound[1];
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) {
+                        if (v[i] >= least_l) whole64 += w[i];
+                        if (v[i] >= least_l && v[i] > high_l) beyond64 += w[i];
+                    }
                 }
 #pragma unroll
                 for (int i = 0; i < 4; ++i) {
-                    const bool in = v[i] >= least_l;
-                    whole += in ? w[i] : 0ull;
-                    beyond += in && v[i] > high_l ? w[i] : 0ull;
                     if (v[i] <= high_l && v[i] >= low_l) {
                         const int b = bin_of(v[i], scale);
                         if (b < first) {
-                            beyond += w[i];
+                            beyond64 += w[i];
                         } else if (b <= last) {
                             if (few) {
                                 const uint32_t at = atomicAdd(&sh.candidates, 1u);
@@ -569,15 +580,14 @@ __global__ void __launch_bounds__(kMostThreads, 2) sample_kernel(const SamplePar
                             } else {
                                 const int at = static_cast<int>((high - key_of(v[i])) >> width);
                                 atomicAdd(&sh.count[at], 1u);
-                                if (by_weight) atomicAdd(&sh.weight[at], begin ? w[i] : weight(v[i]));
+                                if (by_weight) atomicAdd(&sh.weight[at], weight(v[i]));
                             }
                         }
                     }
                 }
             });
             if (begin) {
-                beyond = warp_add(beyond);
-                whole = warp_add(whole);
+                unsigned long long beyond = warp_add(static_cast<unsigned long long>(beyond64)), whole = warp_add(static_cast<unsigned long long>(whole64));
                 if (lane == 0) {
                     sh.warp_beyond[warp] = beyond;
                     sh.warp_total[warp] = whole;
@@ -771,7 +781,7 @@ __global__ void __launch_bounds__(kMostThreads, 2) sample_kernel(const SamplePar
             join(false);
             // What the words of bin b weigh together, in units of 2^S: their count times what its ends weigh, a little more or less for
             // bin_of's roundings and the weights' own.  The sum of all is within 1.5e-5 of what was added up (a product of y <= 47 is
-            // off by 3 * 2^-24 of it, and its power by as much times y ln 2), all sums here within 1e-6.  Where the scale has
+            // off by 3 * 2^-24 of it, and its power by as much times y ln 2), the sums of a thousand terms here within 1e-6 of all.  Where the scale has
             // left its range, the bins say nothing, and all words are looked at.
             const float all = static_cast<float>(sh.real), cut = static_cast<float>(static_cast<double>(excess) / static_cast<double>(1ull << p.shift));
             const float low_all = all * (1.f - 1.5e-5f), high_all = all * (1.f + 1.5e-5f), top_p = static_cast<float>(sh.top_p);
@@ -786,21 +796,25 @@ __global__ void __launch_bounds__(kMostThreads, 2) sample_kernel(const SamplePar
                 const float most = warp_add(most_of(b)), least = warp_add(least_of(b));
                 if (lane == 0) { sh.span_most[span] = most; sh.span_least[span] = least; }
             });
-            if (t == 0) { sh.found.first = known ? kBins - 1 : 0; sh.found.last = kBins - 1; sh.found.active = 0; }
+            __syncthreads();
+            if (warp == 0) {               // to the sums before each span
+                const float most = sh.span_most[lane], least = sh.span_least[lane], most_to = warp_scan(most, lane), least_to = warp_scan(least, lane);
+                sh.span_most[lane] = most_to - most;
+                sh.span_least[lane] = least_to - least;
+                if (lane == 31) { sh.most = most_to; sh.least = least_to; }
+                if (lane == 0) { sh.found.first = known ? kBins - 1 : 0; sh.found.last = kBins - 1; sh.found.active = 0; }
+            }
             __syncthreads();
             if (known)
                 spans([&](int b, int span) {
-                    const float most_span = lane < kSpans ? sh.span_most[lane] : 0.f, least_span = lane < kSpans ? sh.span_least[lane] : 0.f;
-                    // the sum up to bin b, and what is below it
-                    const float most_own = most_of(b), least_own = least_of(b), most_to = warp_scan(most_own, lane), least_to = warp_scan(least_own, lane);
-                    const float most = warp_add(lane < span ? most_span : 0.f) + most_to, least = warp_add(lane < span ? least_span : 0.f) + least_to;
-                    const float most_below = warp_add(lane > span ? most_span : 0.f) + (__shfl_sync(0xFFFFFFFFu, most_to, 31) - most_to);
-                    const float least_below = warp_add(lane > span ? least_span : 0.f) + (__shfl_sync(0xFFFFFFFFu, least_to, 31) - least_to);
-                    // from above, and as all but what is below: may it, and must it have reached the goal?
-                    const float slack = 1e-6f * (most + most_below);
-                    const float up = fminf(most, high_all - least_below) + slack, down = fmaxf(least, low_all - most_below) - slack;
-                    if (up >= low_goal) atomicMin(&sh.found.first, b);
-                    if (down >= high_goal) atomicMin(&sh.found.last, b);
+                    // the sum up to bin b, from above and as all but what is below it: may it, and must it have reached the goal?
+                    const float most = sh.span_most[span] + warp_scan(most_of(b), lane), least = sh.span_least[span] + warp_scan(least_of(b), lane);
+                    const float slack = 3e-6f * sh.most;
+                    const float up = fminf(most, high_all - (sh.least - least)) + slack, down = fmaxf(least, low_all - (sh.most - most)) - slack;
+                    const uint32_t may = __reduce_min_sync(0xFFFFFFFFu, static_cast<uint32_t>(up >= low_goal ? b : kBins));
+                    const uint32_t must = __reduce_min_sync(0xFFFFFFFFu, static_cast<uint32_t>(down >= high_goal ? b : kBins));
+                    if (lane == 0 && may < kBins) atomicMin(&sh.found.first, static_cast<int>(may));
+                    if (lane == 0 && must < kBins) atomicMin(&sh.found.last, static_cast<int>(must));
                 });
             __syncthreads();
             spans([&](int b, int) {
