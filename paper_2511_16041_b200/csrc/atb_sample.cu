@@ -554,6 +554,8 @@ __global__ void __launch_bounds__(kMostThreads, 2) sample_kernel(const SamplePar
             const bool few = sh.found.active <= kWords;          // enough for the first CTA
             const int width = width_of(high - low);
             // (a thread's sums are below 2^53: 2^50 at most)
+            // words below `least` count for nothing; -inf weighs nothing by itself, but where even the lowest number weighs something
+            const bool masked = least != 0 || floor_l == -3.402823466e38f;
             double beyond64 = 0.0, whole64 = 0.0;
             const float high_l = of_key(high), least_l = at_least(least), low_l = fmaxf(least_l, low > 0x007FFFFFu ? of_key(low) : -INFINITY);
             each([&](int c, int j, const float (&v)[4]) {
@@ -561,10 +563,15 @@ __global__ void __launch_bounds__(kMostThreads, 2) sample_kernel(const SamplePar
                 if (begin) {
 #pragma unroll
                     for (int i = 0; i < 4; ++i) w[i] = biased(v[i]) - kRound[1];
+                    if (masked) {
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) w[i] = v[i] >= least_l ? w[i] : 0.0;
+                    }
 #pragma unroll
                     for (int i = 0; i < 4; ++i) {
-                        if (v[i] >= least_l) whole64 += w[i];
-                        if (v[i] >= least_l && v[i] > high_l) beyond64 += w[i];
+                        whole64 += w[i];
+                        // without its upper half a number is as good as 0
+                        beyond64 += __hiloint2double(v[i] > high_l ? __double2hiint(w[i]) : 0, __double2loint(w[i]));
                     }
                 }
 #pragma unroll
