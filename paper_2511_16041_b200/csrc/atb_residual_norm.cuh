@@ -170,14 +170,11 @@ struct Vector {
     }
 };
 
-// A kernel whose rows on their way may take more, with its static arrays, than the 48 KB of shared memory that need no leave.
-template <class... Args>
-cudaError_t launch_ring(void (*kernel)(Args...), unsigned grid, unsigned block, size_t smem, cudaStream_t stream, Args... args) {
-    if (smem > 40 * 1024) {
-        const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(smem));
-        if (e != cudaSuccess) return e;
-    }
-    return atb::launch_dependent(kernel, grid, block, 1u, smem, stream, args...);
+// A kernel whose rows on their way take more than the 48 KB of shared memory that need no leave is given it once per device.
+template <auto KERNEL, class Params>
+cudaError_t launch_ring(unsigned grid, unsigned block, size_t smem, cudaStream_t stream, const Params& p) {
+    const cudaError_t e = atb::allow_shared_memory<KERNEL>(smem);
+    return e != cudaSuccess ? e : atb::launch_dependent(KERNEL, grid, block, 1u, smem, stream, p);
 }
 
 // Types of the stream (x, h and their gradients) and of the branch (f, z and theirs).

@@ -995,9 +995,10 @@ cudaError_t launch(SampleParams p, cudaStream_t st) {
     p.shift = 62 - log2v < 45 ? 62 - log2v : 45;
     const unsigned grid = static_cast<unsigned>(p.M * ctas);
     const size_t smem = static_cast<size_t>(block) * p.vectors * sizeof(float4);
-    auto kernel = p.chunks == 1 ? sample_kernel<T, true> : sample_kernel<T, false>;
-    const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kMostThreads * kPerThread * static_cast<int>(sizeof(float)));
+    constexpr size_t most = static_cast<size_t>(kMostThreads) * kPerThread * sizeof(float);
+    const cudaError_t e = p.chunks == 1 ? atb::allow_shared_memory<&sample_kernel<T, true>>(most) : atb::allow_shared_memory<&sample_kernel<T, false>>(most);
     if (e != cudaSuccess) return e;
+    auto kernel = p.chunks == 1 ? sample_kernel<T, true> : sample_kernel<T, false>;
     return atb::launch_dependent(kernel, grid, static_cast<unsigned>(block), static_cast<unsigned>(ctas), smem, st, p);
 }
 

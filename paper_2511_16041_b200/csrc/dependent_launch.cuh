@@ -5,9 +5,26 @@
 #pragma once
 #include <cuda_runtime.h>
 
+#include <atomic>
+
 #include "sm100_ptx.cuh"
 
 namespace atb {
+
+// Leave for a kernel to take `most` bytes of dynamic shared memory (the same at every call), asked for once per device: the call takes about as
+// long as a launch.
+template <auto KERNEL>
+cudaError_t allow_shared_memory(size_t most) {
+    static std::atomic<uint64_t> allowed{0};
+    if (most <= 40 * 1024) return cudaSuccess;
+    int device = 0;
+    cudaError_t e = cudaGetDevice(&device);
+    const uint64_t bit = device >= 0 && device < 64 ? 1ull << device : 0ull;
+    if (e != cudaSuccess || (allowed.load(std::memory_order_acquire) & bit)) return e;
+    e = cudaFuncSetAttribute(KERNEL, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(most));
+    if (e == cudaSuccess) allowed.fetch_or(bit, std::memory_order_release);
+    return e;
+}
 
 template <class... Args>
 cudaError_t launch_dependent(void (*kernel)(Args...), unsigned grid, unsigned block, unsigned cluster, size_t smem, cudaStream_t stream, Args... args) {

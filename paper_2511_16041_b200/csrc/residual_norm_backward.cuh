@@ -303,8 +303,8 @@ __global__ void __launch_bounds__(1024) residual_norm_backward_wide_kernel(const
 template <class TX, class TF, class TW, int VEC, bool POST, int W>
 cudaError_t launch_rows(const BwdParams& p, cudaStream_t st) {
     constexpr int TPR = kWidths[W].threads, NV = kWidths[W].elems / VEC, STAGES = ahead_of<TX, TF, VEC, TPR, NV>() + 1;
-    return launch_ring(residual_norm_backward_kernel<TX, TF, TW, VEC, TPR, NV, POST>, static_cast<unsigned>(p.blocks), TPR == 32 ? 128u : TPR,
-                       static_cast<size_t>(STAGES) * kStage<TX, TF, VEC, TPR, NV>, st, p);
+    return launch_ring<&residual_norm_backward_kernel<TX, TF, TW, VEC, TPR, NV, POST>>(static_cast<unsigned>(p.blocks), TPR == 32 ? 128u : TPR,
+                                                                                       static_cast<size_t>(STAGES) * kStage<TX, TF, VEC, TPR, NV>, st, p);
 }
 template <class TX, class TF, class TW, int VEC, bool POST>
 cudaError_t launch(const BwdParams& p, cudaStream_t st) {

@@ -274,7 +274,7 @@ template <class TX, class TF, class TW, int VEC, bool POST, int TPR>
 cudaError_t launch_rows(const FwdParams& p, cudaStream_t st) {
     constexpr int NV = kElems / VEC, THREADS = TPR == 32 ? 128 : TPR, ROOM = (ahead_of<TX, TF, TPR, NV, VEC>() + 1) * kStageBytes<TX, TF, TPR, NV, VEC>;
     const int64_t all = atb::ceil_div(p.M, TPR == 32 ? 4 : 1), most = static_cast<int64_t>(atb::kSmCount) * resident(TPR);
-    return launch_ring(residual_norm_kernel<TX, TF, TW, VEC, TPR, NV, POST>, static_cast<unsigned>(all < most ? all : most), THREADS, ROOM, st, p);
+    return launch_ring<&residual_norm_kernel<TX, TF, TW, VEC, TPR, NV, POST>>(static_cast<unsigned>(all < most ? all : most), THREADS, ROOM, st, p);
 }
 template <class TX, class TF, class TW, int VEC, bool POST>
 cudaError_t launch(const FwdParams& p, cudaStream_t st) {
