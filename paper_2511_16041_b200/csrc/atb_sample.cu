@@ -271,7 +271,7 @@ __global__ void __launch_bounds__(kMostThreads, 2) sample_kernel(const SamplePar
 #pragma unroll 1
         for (int c = 0; c < (RESIDENT ? 1 : p.chunks); ++c) {
             if constexpr (!RESIDENT) row.load(c, mine4, lane);
-#pragma unroll 2
+#pragma unroll 1
             for (int j = 0; j < p.vectors; ++j) {
                 const float4 q = mine4[j * 32 + lane];
                 const float v[4] = {q.x, q.y, q.z, q.w};
@@ -412,25 +412,35 @@ __global__ void __launch_bounds__(kMostThreads, 2) sample_kernel(const SamplePar
                     }
                 }
                 __syncthreads();
-                // the first of those by top_p and min_p
+                // the first of those by top_p and min_p: what stands before each of them, one to a thread
                 const int first = static_cast<int>(k < count ? k : count);
-                unsigned long long whole = 0;
-                for (int j = 0; j < first; ++j) whole += sh.few.weight[j];
                 const double top_p = sh.top_p, deepest = sh.deepest;
-                const bool by_p = top_p < 1.0;
-                const double goal = top_p > 0.0 ? top_p * static_cast<double>(whole) : 0.0;
                 int kept = 0;
-                unsigned long long sum = 0;
-                for (; kept < first; ++kept) {
-                    if (kept > 0 && ((by_p && !(static_cast<double>(sum) < goal)) || !(depth(sh.few.kept[kept].l) <= deepest))) break;
-                    sum += sh.few.weight[kept];
+                for (int from = 0; from < first; from += blockDim.x) {
+                    const int i = from + t;
+                    unsigned long long whole = 0, before = 0;
+#pragma unroll 4
+                    for (int j = 0; j < first; ++j) {
+                        const unsigned long long w = sh.few.weight[j];
+                        whole += w;
+                        before += j < i ? w : 0ull;
+                    }
+                    const double goal = top_p > 0.0 ? top_p * static_cast<double>(whole) : 0.0;
+                    // (what is kept is a beginning of their order)
+                    const bool keep = i < first && (i == 0 || ((!(top_p < 1.0) || static_cast<double>(before) < goal) && depth(sh.few.kept[i].l) <= deepest));
+                    kept += __syncthreads_count(keep);
                 }
-                const unsigned long long target = target_of(sum);
                 for (int i = t; i < kept; i += blockDim.x) {
                     const int word = sh.few.kept[i].word;
                     const unsigned long long own = sh.few.weight[i];
-                    unsigned long long run = 0;
-                    for (int j = 0; j < kept; ++j) run += sh.few.kept[j].word <= word ? sh.few.weight[j] : 0ull;
+                    unsigned long long run = 0, sum = 0;
+#pragma unroll 4
+                    for (int j = 0; j < kept; ++j) {
+                        const unsigned long long w = sh.few.weight[j];
+                        sum += w;
+                        run += sh.few.kept[j].word <= word ? w : 0ull;
+                    }
+                    const unsigned long long target = target_of(sum);
                     if (run >= target && run - own < target) {
                         p.tokens[m] = word;
                         if (p.probs) p.probs[m] = static_cast<float>(static_cast<double>(own) / static_cast<double>(sum));
