@@ -340,9 +340,33 @@ __device__ __forceinline__ void linear_fetch(const MmMaps<1>& tm, const MmParams
     for (int b = 0; b < 2; ++b)
         if (b * PIECE < C::COLS && col0 + b * PIECE < jb.N) out.fetch_box(b, &tm.c[2], col0 + b * PIECE, row0);
 }
+// A warp's bias: lane i has columns i, 32 + i, ... of its own, loaded while the accumulator is waited for.  (Loaded where it is used, a few columns
+// at a time for all lanes alike, it cost a prompt of 509 rows 3.5 of 22 us.)
+template <class C>
+struct LinearBias {
+    float v[C::COLS / 32];
+    __device__ __forceinline__ LinearBias(const MmParams& p, const MmJob& jb, int64_t col0, int lane) {
+#pragma unroll
+        for (int i = 0; i < C::COLS / 32; ++i) {
+            const int64_t col = col0 + 32 * i + lane;
+            v[i] = 0.f;
+            if (p.bias && col < jb.N)
+                v[i] = p.bias32 ? __ldg(static_cast<const float*>(p.bias) + col)
+                                : __uint_as_float(static_cast<uint32_t>(__ldg(static_cast<const uint16_t*>(p.bias) + col)) << 16);
+        }
+    }
+    // of this lane's column of the 32 from column c of the warp's on
+    __device__ __forceinline__ float at(int c) const {
+        float b = v[0];
+#pragma unroll
+        for (int i = 1; i < C::COLS / 32; ++i) b = c == 32 * i ? v[i] : b;
+        return b;
+    }
+};
+
 template <class C, bool Y32>
-__device__ __forceinline__ void linear_epilogue(const MmMaps<1>& tm, const MmParams& p, const MmJob& jb, BoxWriter<2>& out, uint32_t t_addr, int64_t row0,
-                                                int64_t col0, int lane, const Ctx& cx) {
+__device__ __forceinline__ void linear_epilogue(const MmMaps<1>& tm, const MmParams& p, const MmJob& jb, BoxWriter<2>& out, const LinearBias<C>& bias, uint32_t t_addr,
+                                                int64_t row0, int64_t col0, int lane, const Ctx& cx) {
     constexpr int PIECE = Y32 ? 32 : 64;
     if (row0 >= jb.M) return;
     const bool in_place = p.residual && !p.kept;
@@ -351,13 +375,9 @@ __device__ __forceinline__ void linear_epilogue(const MmMaps<1>& tm, const MmPar
         tmem_ld_32x32b_x32(t_addr + c, v);
         tmem_ld_wait_for(v);
         if (!p.bias) return;
+        const float mine = bias.at(c);
 #pragma unroll
-        for (int j = 0; j < 4; ++j) {
-            float bias[8];
-            load_bias(p.bias, p.bias32, col0 + c + 8 * j, jb.N, bias);
-#pragma unroll
-            for (int e = 0; e < 8; ++e) v[8 * j + e] = __float_as_uint(__uint_as_float(v[8 * j + e]) + bias[e]);
-        }
+        for (int e = 0; e < 32; ++e) v[e] = __float_as_uint(__uint_as_float(v[e]) + __shfl_sync(0xFFFFFFFFu, mine, e));
     };
     with_linear_act(p.act, [&](auto act) {
 #pragma unroll 1
@@ -562,8 +582,6 @@ __device__ __forceinline__ void mm_epilogue(const MmMaps<C::JOBS>& tm, const MmP
                 }
             }
         });
-    } else if constexpr (EPI == atb::kMmLinear) {
-        linear_epilogue<C, KEEP32>(tm, p, jb, out, t_addr, row0, col0, lane, cx);
     } else if constexpr (EPI == atb::kMmRowStats) {
         // columns of this warp inside the vocabulary; the label's, counted from the first
         const int mine = static_cast<int>(min(static_cast<int64_t>(cols), jb.N - col0));
@@ -807,14 +825,23 @@ bf16_mm_kernel(const __grid_constant__ MmMaps<MmCfg<PAIR, EPI>::JOBS> tm, const 
             const MmJob& jb = p.job[w.job];
             const int64_t row0 = static_cast<int64_t>(w.mt) * C::TILE_M + rank * 128 + q * 32, col0 = static_cast<int64_t>(w.nt) * tile_n;
             const int acc = it & 1;
-            if constexpr (EPI == atb::kMmLinear) linear_fetch<C, KEEP32>(tm, p, jb, out, row0, col0 + half * C::COLS);
-            if constexpr (EPI == atb::kMmGluBackward)
-                if (row0 < jb.M && col0 + half * C::COLS < jb.N) out.fetch(&tm.c[2], &tm.c[3], col0 + half * C::COLS, row0);
-            if (!(ok = wait_bar_t<false, PAIR>(cx, acc_full + 8 * acc, static_cast<uint32_t>(it >> 1) & 1u, 0x201))) break;
-            tcgen05_fence_after_sync();
-            if (half * C::COLS < tile_n)
-                mm_epilogue<C, EPI, KEEP32>(tm, p, jb, 2 * w.job + w.seg, out, tmem_base + (static_cast<uint32_t>(q * 32) << 16) + static_cast<uint32_t>(acc * C::BN),
-                                    half, row0, col0, min(C::COLS, tile_n - half * C::COLS), w.split, unit, lane, cx);
+            if constexpr (EPI == atb::kMmLinear) {
+                const int64_t own0 = col0 + half * C::COLS;
+                linear_fetch<C, KEEP32>(tm, p, jb, out, row0, own0);
+                const LinearBias<C> bias(p, jb, own0, lane);
+                if (!(ok = wait_bar_t<false, PAIR>(cx, acc_full + 8 * acc, static_cast<uint32_t>(it >> 1) & 1u, 0x201))) break;
+                tcgen05_fence_after_sync();
+                linear_epilogue<C, KEEP32>(tm, p, jb, out, bias, tmem_base + (static_cast<uint32_t>(q * 32) << 16) + static_cast<uint32_t>(acc * C::BN + half * C::COLS), row0,
+                                           own0, lane, cx);
+            } else {
+                if constexpr (EPI == atb::kMmGluBackward)
+                    if (row0 < jb.M && col0 + half * C::COLS < jb.N) out.fetch(&tm.c[2], &tm.c[3], col0 + half * C::COLS, row0);
+                if (!(ok = wait_bar_t<false, PAIR>(cx, acc_full + 8 * acc, static_cast<uint32_t>(it >> 1) & 1u, 0x201))) break;
+                tcgen05_fence_after_sync();
+                if (half * C::COLS < tile_n)
+                    mm_epilogue<C, EPI, KEEP32>(tm, p, jb, 2 * w.job + w.seg, out, tmem_base + (static_cast<uint32_t>(q * 32) << 16) + static_cast<uint32_t>(acc * C::BN),
+                                        half, row0, col0, min(C::COLS, tile_n - half * C::COLS), w.split, unit, lane, cx);
+            }
             tcgen05_fence_before_sync();
             __syncwarp();
 #ifdef ATB_TEST_WITHHOLD_ACC_ARRIVAL
