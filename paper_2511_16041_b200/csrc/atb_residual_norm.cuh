@@ -78,12 +78,13 @@ __device__ __forceinline__ void pairs_of(const Raw<T, VEC> (&r)[8 / VEC], float2
     }
 }
 // Where they are: eight c of a thread whose first column is `col`.  Elements past the row's end are 0, as are their weights.
-template <int VEC, int TPR>
+// The first FULL groups of a thread lie inside every row that the kernel gets.
+template <int VEC, int TPR, int FULL>
 struct Eight {
     static constexpr int G = 8 / VEC;      // groups
     int N, col, c;
     __device__ __forceinline__ int n(int g) const { return col + (c * G + g) * TPR * VEC; }
-    __device__ __forceinline__ bool in(int g) const { return n(g) < N; }
+    __device__ __forceinline__ bool in(int g) const { return c * G + g < FULL || n(g) < N; }
     template <class T, class Source>
     __device__ __forceinline__ void read(const Source& src, int stage, int64_t m, float2 (&v)[4]) const {
         Raw<T, VEC> r[G];
@@ -133,39 +134,65 @@ struct Eight {
     }
 };
 
-// A vector of weights at a thread's CH eights.  KEEP: in registers, loaded once, as they are in memory (single elements: in FP32); else read
-// again wherever they are used.
-template <class TW, int VEC, int TPR, int CH, bool KEEP>
+// A vector of weights at a thread's CH eights, or the product of two.  Elements past the row's end are 0.
+//   kRead: read again wherever it is used;  kKept: in registers, loaded once, as it is in memory (single elements and products: in FP32);
+//   kShared: in shared memory in FP32, each thread's own 16-byte pieces at `place`
+enum Place { kRead = 0, kKept = 1, kShared = 2 };
+template <class TW, int VEC, int TPR, int CH, int FULL, int PLACE, bool PRODUCT = false>
 struct Vector {
-    const void* p;
-    float none;
-    Raw<TW, 8> raw[KEEP && VEC == 8 ? CH : 1];
-    float2 one[KEEP && VEC == 1 ? CH : 1][4];
-    __device__ __forceinline__ Vector(const void* p_, float none_, int N, int col) : p(p_), none(none_) {
-        if constexpr (KEEP) {
+    static constexpr bool RAW = PLACE == kKept && VEC == 8 && !PRODUCT, VALUES = PLACE == kKept && !RAW;
+    static constexpr uint32_t BYTES = CH * 2 * TPR * 16;
+    const void *p, *q;
+    float none, none_q;
+    uint32_t place;
+    Raw<TW, 8> raw[RAW ? CH : 1];
+    float2 value[VALUES ? CH : 1][4];
+    using At = Eight<VEC, TPR, FULL>;
+    __device__ __forceinline__ Vector(int N, int col, const void* p_, float none_, const void* q_ = nullptr, float none_q_ = 1.f, uint32_t place_ = 0)
+        : p(p_), q(q_), none(none_), none_q(none_q_), place(place_ + threadIdx.x * 16) {
 #pragma unroll
-            for (int c = 0; c < CH; ++c) {
-                const Eight<VEC, TPR> at{N, col, c};
-                if constexpr (VEC == 8) {
-                    load_or<TW, 8>(static_cast<const TW*>(p), at.n(0), N, none, raw[c]);
-                } else {
-                    at.template weight<TW>(p, none, one[c]);
+        for (int c = 0; c < CH; ++c) {
+            const At at{N, col, c};
+            if constexpr (RAW) {
+                load_or<TW, 8>(static_cast<const TW*>(p), at.n(0), N, none, raw[c]);
+            } else if constexpr (VALUES) {
+                read(at, value[c]);
 #pragma unroll
-                    for (int k = 0; k < 4; ++k)      // kept: not converted again in every row
-                        asm volatile("" : "+f"(one[c][k].x), "+f"(one[c][k].y));
-                }
+                for (int k = 0; k < 4; ++k)          // kept: not made again in every row
+                    asm volatile("" : "+f"(value[c][k].x), "+f"(value[c][k].y));
+            } else if constexpr (PLACE == kShared) {
+                float2 v[4];
+                read(at, v);
+#pragma unroll
+                for (int half = 0; half < 2; ++half)
+                    asm volatile("st.shared.v4.f32 [%0], {%1, %2, %3, %4};" ::"r"(place + (c * 2 + half) * TPR * 16), "f"(v[2 * half].x), "f"(v[2 * half].y),
+                                 "f"(v[2 * half + 1].x), "f"(v[2 * half + 1].y) : "memory");
             }
         }
     }
-    __device__ __forceinline__ void get(const Eight<VEC, TPR>& at, float2 (&v)[4]) const {
-        if constexpr (!KEEP) {
-            at.template weight<TW>(p, none, v);
-        } else if constexpr (VEC == 8) {
+    __device__ __forceinline__ void read(const At& at, float2 (&v)[4]) const {
+        at.template weight<TW>(p, none, v);
+        if constexpr (PRODUCT) {
+            float2 f[4];
+            at.template weight<TW>(q, none_q, f);
+#pragma unroll
+            for (int k = 0; k < 4; ++k) v[k] = mul2(v[k], f[k]);
+        }
+    }
+    __device__ __forceinline__ void get(const At& at, float2 (&v)[4]) const {
+        if constexpr (RAW) {
             const Raw<TW, 8> r[1] = {raw[at.c]};
             pairs_of<TW, 8>(r, v);
-        } else {
+        } else if constexpr (VALUES) {
 #pragma unroll
-            for (int k = 0; k < 4; ++k) v[k] = one[at.c][k];
+            for (int k = 0; k < 4; ++k) v[k] = value[at.c][k];
+        } else if constexpr (PLACE == kShared) {
+#pragma unroll
+            for (int half = 0; half < 2; ++half)
+                asm volatile("ld.shared.v4.f32 {%0, %1, %2, %3}, [%4];" : "=f"(v[2 * half].x), "=f"(v[2 * half].y), "=f"(v[2 * half + 1].x), "=f"(v[2 * half + 1].y)
+                             : "r"(place + (at.c * 2 + half) * TPR * 16));
+        } else {
+            read(at, v);
         }
     }
 };
@@ -184,8 +211,13 @@ constexpr int kBlockThreads = 512;         // per SM, 128 registers each
 struct Width {
     int threads, elems;
 };
-constexpr Width kWidths[] = {{32, 8}, {32, 16}, {128, 8}, {256, 8}, {512, 8}, {512, 16}};
-constexpr int kWidthCount = 6;
+constexpr int kWidthCount = 10;
+constexpr Width kWidths[kWidthCount] = {{32, 8}, {32, 16}, {96, 8}, {128, 8}, {192, 8}, {256, 8}, {384, 8}, {512, 8}, {384, 16}, {512, 16}};
+// Groups of a thread that lie inside every row of a width: the rows are wider than the width before it takes.
+__host__ __device__ constexpr int full_of(int threads, int elems, int vec, int fewer) {
+    const int groups = vec > 1 ? 0 : fewer / threads;
+    return groups < elems ? groups : elems;
+}
 inline int width_of(int64_t N) {
     for (int i = 0; i < kWidthCount; ++i)
         if (N <= static_cast<int64_t>(kWidths[i].threads) * kWidths[i].elems) return i;

@@ -21,19 +21,29 @@ template <class TX, class TF, int VEC, int NV>
 constexpr bool kDirect = sizeof(TX) + sizeof(TF) == 8 && NV * VEC > 8;
 template <class TX, class TF, int VEC, int TPR, int NV>
 constexpr int kStage = static_cast<int>((kDirect<TX, TF, VEC, NV> ? 1 : 2) * RowSource<TX, VEC, TPR, NV>::STAGE_BYTES + 2 * RowSource<TF, VEC, TPR, NV>::STAGE_BYTES);
-template <class TX, class TF, int VEC, int TPR, int NV>
+// Bytes of the vectors of weights in shared memory: three, where a thread's registers are full of sums (16 elements, four sums) and two stages
+// of rows leave the room.
+constexpr int kRoom = 226 * 1024;
+template <class TX, class TF, int VEC, int TPR, int NV, bool POST>
+__host__ __device__ constexpr int vector_bytes() {
+    const int bytes = 3 * NV * 2 * TPR * 16;
+    return POST && VEC == 8 && NV == 2 && TPR > 32 && kRoom - bytes >= 2 * kStage<TX, TF, VEC, TPR, NV> ? bytes : 0;
+}
+template <class TX, class TF, int VEC, int TPR, int NV, bool POST>
 __host__ __device__ constexpr int ahead_of() {
-    const int stages = 208 * 1024 / (blocks_of(TPR) * kStage<TX, TF, VEC, TPR, NV>);
+    const int vectors = vector_bytes<TX, TF, VEC, TPR, NV, POST>();
+    const int stages = (vectors ? kRoom - vectors : 208 * 1024) / (blocks_of(TPR) * kStage<TX, TF, VEC, TPR, NV>);
     return stages > 4 ? 3 : stages - 1;
 }
 
-template <class TX, class TF, class TW, int VEC, int TPR, int NV, bool POST>
+template <class TX, class TF, class TW, int VEC, int TPR, int NV, int FULL, bool POST>
 __global__ void __launch_bounds__(TPR == 32 ? 128 : TPR, blocks_of(TPR)) residual_norm_backward_kernel(const BwdParams p) {
     using SX = RowSource<TX, VEC, TPR, NV>;
     using SF = RowSource<TF, VEC, TPR, NV>;
     using Shared = std::conditional_t<SX::SHARED, SX, SF>;
     constexpr bool DIRECT = kDirect<TX, TF, VEC, NV>;
-    constexpr int WALKERS = TPR == 32 ? 4 : 1, W = TPR / 32, AHEAD = ahead_of<TX, TF, VEC, TPR, NV>(), STAGES = AHEAD + 1, CH = NV * VEC / 8;
+    constexpr int WALKERS = TPR == 32 ? 4 : 1, W = TPR / 32, AHEAD = ahead_of<TX, TF, VEC, TPR, NV, POST>(), STAGES = AHEAD + 1, CH = NV * VEC / 8;
+    using At = Eight<VEC, TPR, FULL>;
     static_assert(AHEAD >= 1, "shared memory");
     extern __shared__ __align__(16) uint8_t ring[];
     __shared__ float red[2][2][W][2];
@@ -59,9 +69,18 @@ __global__ void __launch_bounds__(TPR == 32 ? 128 : TPR, blocks_of(TPR)) residua
         if (first + s * step < p.M) fetch(s, first + s * step);
         async_commit();
     }
-    // w and gate stay in registers, and, where a thread has 8 elements, pw and pb: as many as there is room for beside the sums
-    const Vector<TW, VEC, TPR, CH, (!POST || CH == 1)> w_of(p.v.w, 1.f, N, col), gate_of(p.v.gate, 1.f, N, col);
-    const Vector<TW, VEC, TPR, CH, POST && CH == 1> pw_of(p.v.pw, 1.f, N, col), pb_of(p.v.pb, 0.f, N, col);
+    // The vectors that a row meets: w, gate, pw and pb.  Single elements, which are kept in FP32, are met by a and b of h = scale x + a m + b instead
+    // (m = norm(f), a = gate pw, b = gate pb): one vector fewer; kept as they are in memory, the four took no more room and time than
+    // the two.  They stay in registers where those have room for them beside the sums: not with 16 elements and four sums a thread, where
+    // w, a and b lie in shared memory if that has the room.
+    constexpr bool IN_SHARED = vector_bytes<TX, TF, VEC, TPR, NV, POST>() > 0, FOLD = POST && (VEC == 1 || IN_SHARED);
+    constexpr int KEEP = IN_SHARED ? kShared : !POST || CH == 1 ? kKept : kRead;
+    const uint32_t place = base + STAGES * kStage<TX, TF, VEC, TPR, NV>;
+    using Kept = Vector<TW, VEC, TPR, CH, FULL, KEEP>;
+    const Kept w_of(N, col, p.v.w, 1.f, nullptr, 1.f, place);
+    const Vector<TW, VEC, TPR, CH, FULL, KEEP, FOLD> a_of(N, col, p.v.gate, 1.f, p.v.pw, 1.f, place + Kept::BYTES);                  // gate, or a
+    const Vector<TW, VEC, TPR, CH, FULL, POST && !FOLD ? KEEP : kRead> pw_of(N, col, p.v.pw, 1.f);
+    const Vector<TW, VEC, TPR, CH, FULL, POST ? KEEP : kRead, FOLD> b_of(N, col, p.v.pb, 0.f, FOLD ? p.v.gate : nullptr, 1.f, place + 2 * Kept::BYTES);   // pb, or b
     const float2 zero = both(0.f), scale = both(p.scale);
     float2 s0[CH][4], s1[CH][4], s2[CH][4], s3[POST ? CH : 1][4];
 #pragma unroll
@@ -88,37 +107,42 @@ __global__ void __launch_bounds__(TPR == 32 ? 128 : TPR, blocks_of(TPR)) residua
         stats(m + step, next[0], next[1], next[2], next[3]);
         async_wait<AHEAD>();
         row_barrier<Shared, VEC, TPR>();
-        // f, or norm(f), and norm(h) of an eight
-        const auto values = [&](const Eight<VEC, TPR>& at, float2 (&f)[4], float2 (&h)[4]) {
-            float2 a[4], b[4];
+        // f, or norm(f), norm(h) and dz of an eight
+        const auto values = [&](const At& at, float2 (&f)[4], float2 (&h)[4], float2 (&dz)[4]) {
+            float2 a[4], x[4];
             at.template read<TF>(sf, stage, m, f);
+            at.template read<TX>(sx, stage, m, x);
+            a_of.get(at, a);
+            const float2 shift = both(-mu), spread = both(r);
             if constexpr (POST) {
-                pw_of.get(at, a);
-                pb_of.get(at, b);
-                const float2 shift = both(-fmu), spread = both(fr);
+                float2 b[4], pw[4];
+                b_of.get(at, b);
+                if constexpr (!FOLD) pw_of.get(at, pw);
+                const float2 f_shift = both(-fmu), f_spread = both(fr);
 #pragma unroll
                 for (int k = 0; k < 4; ++k) {
-                    f[k] = mul2(add2(f[k], shift), spread);
-                    h[k] = fma2(f[k], a[k], b[k]);
+                    f[k] = mul2(add2(f[k], f_shift), f_spread);
+                    h[k] = FOLD ? fma2(f[k], a[k], b[k]) : mul2(a[k], fma2(f[k], pw[k], b[k]));
                 }
             } else {
 #pragma unroll
-                for (int k = 0; k < 4; ++k) h[k] = f[k];
+                for (int k = 0; k < 4; ++k) h[k] = mul2(f[k], a[k]);
             }
-            at.template read<TX>(sx, stage, m, b);
-            gate_of.get(at, a);
-            const float2 shift = both(-mu), spread = both(r);
 #pragma unroll
-            for (int k = 0; k < 4; ++k) h[k] = mul2(add2(fma2(scale, b[k], mul2(a[k], h[k])), shift), spread);
+            for (int k = 0; k < 4; ++k) h[k] = mul2(add2(fma2(scale, x[k], h[k]), shift), spread);
+            at.template read<TF>(sdz, stage, m, dz);
         };
+        // Eight elements stay in registers over the sums, but beside four sums only single ones: else these are made again from the row in shared
+        // memory, which sixteen bytes at a time costs less than the registers (8192 x 4096 with a norm of f 108 us, held 134 us).
+        constexpr int HELD = CH == 1 && (VEC == 1 || !POST) ? 1 : 0;
+        float2 held_f[HELD + 1][4], held_h[HELD + 1][4], held_dz[HELD + 1][4];
         float2 s_g = zero, s_gn = zero;
 #pragma unroll
         for (int c = 0; c < CH; ++c) {
-            const Eight<VEC, TPR> at{N, col, c};
+            const At at{N, col, c};
             if (VEC == 8 && !at.in(0)) continue;
-            float2 f[4], h[4], dz[4], w[4];
-            values(at, f, h);
-            at.template read<TF>(sdz, stage, m, dz);
+            float2 (&f)[4] = held_f[0], (&h)[4] = held_h[0], (&dz)[4] = held_dz[0], w[4];
+            values(at, f, h, dz);
             w_of.get(at, w);
 #pragma unroll
             for (int k = 0; k < 4; ++k) {
@@ -136,11 +160,10 @@ __global__ void __launch_bounds__(TPR == 32 ? 128 : TPR, blocks_of(TPR)) residua
         float2 q[POST ? CH : 1][4], k_q = zero, k_qm = zero;
 #pragma unroll
         for (int c = 0; c < CH; ++c) {
-            const Eight<VEC, TPR> at{N, col, c};
+            const At at{N, col, c};
             if (VEC == 8 && !at.in(0)) continue;
-            float2 f[4], h[4], d[4], w[4];
-            values(at, f, h);
-            at.template read<TF>(sdz, stage, m, d);
+            float2 (&f)[4] = held_f[0], (&h)[4] = held_h[0], (&d)[4] = held_dz[0], w[4];
+            if constexpr (!HELD) values(at, f, h, d);
             w_of.get(at, w);
 #pragma unroll
             for (int k = 0; k < 4; ++k) d[k] = mul2(spread, fma2(h[k], m1, fma2(d[k], w[k], m0)));
@@ -157,13 +180,13 @@ __global__ void __launch_bounds__(TPR == 32 ? 128 : TPR, blocks_of(TPR)) residua
                 w[k] = mul2(scale, d[k]);
             }
             if (p.dx) at.template store<TX>(static_cast<TX*>(p.dx) + m * p.lddx, w);
-            gate_of.get(at, w);
+            a_of.get(at, w);
             if constexpr (POST) {
                 float2 pw[4];
-                pw_of.get(at, pw);
+                if constexpr (!FOLD) pw_of.get(at, pw);
 #pragma unroll
                 for (int k = 0; k < 4; ++k) {
-                    q[c][k] = mul2(mul2(d[k], w[k]), pw[k]);
+                    q[c][k] = FOLD ? mul2(d[k], w[k]) : mul2(mul2(d[k], w[k]), pw[k]);
                     k_q = add2(k_q, q[c][k]);
                     k_qm = fma2(q[c][k], f[k], k_qm);
                 }
@@ -180,12 +203,16 @@ __global__ void __launch_bounds__(TPR == 32 ? 128 : TPR, blocks_of(TPR)) residua
             if (p.df)
 #pragma unroll
                 for (int c = 0; c < CH; ++c) {
-                    const Eight<VEC, TPR> at{N, col, c};
+                    const At at{N, col, c};
                     if (VEC == 8 && !at.in(0)) continue;
-                    float2 f[4];
-                    at.template read<TF>(sf, stage, m, f);
+                    float2 (&f)[4] = held_f[0];
+                    if constexpr (!HELD) {
+                        at.template read<TF>(sf, stage, m, f);
 #pragma unroll
-                    for (int e = 0; e < 4; ++e) f[e] = mul2(fspread, fma2(mul2(add2(f[e], shift), fspread), c1, add2(q[c][e], c0)));
+                        for (int e = 0; e < 4; ++e) f[e] = mul2(add2(f[e], shift), fspread);
+                    }
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) f[e] = mul2(fspread, fma2(f[e], c1, add2(q[c][e], c0)));
                     at.template store<TF>(static_cast<TF*>(p.df) + m * p.lddf, f);
                 }
         }
@@ -198,7 +225,7 @@ __global__ void __launch_bounds__(TPR == 32 ? 128 : TPR, blocks_of(TPR)) residua
         float* const out = p.part + first * (POST ? 4 : 3) * p.N;
 #pragma unroll
         for (int c = 0; c < CH; ++c) {
-            const Eight<VEC, TPR> at{N, col, c};
+            const At at{N, col, c};
             at.template store<float>(out, s0[c]);
             at.template store<float>(out + p.N, s1[c]);
             at.template store<float>(out + 2 * p.N, s2[c]);
@@ -302,9 +329,10 @@ __global__ void __launch_bounds__(1024) residual_norm_backward_wide_kernel(const
 // ---------------------------------------------------------------------------------- host
 template <class TX, class TF, class TW, int VEC, bool POST, int W>
 cudaError_t launch_rows(const BwdParams& p, cudaStream_t st) {
-    constexpr int TPR = kWidths[W].threads, NV = kWidths[W].elems / VEC, STAGES = ahead_of<TX, TF, VEC, TPR, NV>() + 1;
-    return launch_ring<&residual_norm_backward_kernel<TX, TF, TW, VEC, TPR, NV, POST>>(static_cast<unsigned>(p.blocks), TPR == 32 ? 128u : TPR,
-                                                                                       static_cast<size_t>(STAGES) * kStage<TX, TF, VEC, TPR, NV>, st, p);
+    constexpr int TPR = kWidths[W].threads, NV = kWidths[W].elems / VEC, STAGES = ahead_of<TX, TF, VEC, TPR, NV, POST>() + 1;
+    constexpr int FULL = full_of(TPR, kWidths[W].elems, VEC, W > 0 ? kWidths[W > 0 ? W - 1 : 0].threads * kWidths[W > 0 ? W - 1 : 0].elems : 0);
+    return launch_ring<&residual_norm_backward_kernel<TX, TF, TW, VEC, TPR, NV, FULL, POST>>(static_cast<unsigned>(p.blocks), TPR == 32 ? 128u : TPR,
+                                                                                             static_cast<size_t>(STAGES) * kStage<TX, TF, VEC, TPR, NV> + vector_bytes<TX, TF, VEC, TPR, NV, POST>(), st, p);
 }
 template <class TX, class TF, class TW, int VEC, bool POST>
 cudaError_t launch(const BwdParams& p, cudaStream_t st) {
@@ -315,6 +343,10 @@ cudaError_t launch(const BwdParams& p, cudaStream_t st) {
         case 3: return launch_rows<TX, TF, TW, VEC, POST, 3>(p, st);
         case 4: return launch_rows<TX, TF, TW, VEC, POST, 4>(p, st);
         case 5: return launch_rows<TX, TF, TW, VEC, POST, 5>(p, st);
+        case 6: return launch_rows<TX, TF, TW, VEC, POST, 6>(p, st);
+        case 7: return launch_rows<TX, TF, TW, VEC, POST, 7>(p, st);
+        case 8: return launch_rows<TX, TF, TW, VEC, POST, 8>(p, st);
+        case 9: return launch_rows<TX, TF, TW, VEC, POST, 9>(p, st);
     }
     residual_norm_backward_wide_kernel<TX, TF, TW, POST><<<static_cast<unsigned>(p.blocks), 1024, 0, st>>>(p);
     return cudaGetLastError();

@@ -13,11 +13,18 @@
 namespace residual_norm {
 namespace {
 
-constexpr int kThreads[] = {32, 64, 128, 256, 384, 512, 768, 1024};
+constexpr int kThreads[] = {32, 64, 96, 128, 192, 256, 384, 512, 768, 1024};
+// The most that a kernel's predecessor takes: its rows are wider.
+__host__ __device__ constexpr int fewer_of(int tpr) {
+    int fewer = 0;
+    for (const int t : kThreadCounts)
+        if (t < tpr) fewer = t * kElems;
+    return fewer;
+}
 template <class TX, class TF>
 constexpr int kMostThreads = sizeof(TX) + sizeof(TF) == 8 ? 768 : 1024;        // two stages of rows in shared memory
 // The vectors of weights stay in registers (a thread has the same columns of every row), but in the widest kernels, whose threads
-// have too few, and FP32 pw and pb, which would be two too many.
+// have too few, and but for FP32 gate pb, which would be one too many.
 __host__ __device__ constexpr bool keeps(int tpr) { return tpr <= 512; }
 // Blocks that stay on an SM: 512 threads of 128 registers.
 __host__ __device__ constexpr int resident(int tpr) { return tpr == 32 ? 4 : tpr >= 512 ? 1 : 512 / tpr; }
@@ -80,14 +87,15 @@ struct RowNorm {
 };
 
 // Which of a thread's elements are in the row.
-template <int VEC, int TPR, int CH>
+template <int VEC, int TPR, int CH, int FULL>
 struct Inside {
+    using At = Eight<VEC, TPR, FULL>;
     bool in[CH][VEC == 8 ? 1 : 8];
     __device__ __forceinline__ Inside(int N, int col) {
 #pragma unroll
         for (int c = 0; c < CH; ++c)
 #pragma unroll
-            for (int g = 0; g < 8 / VEC; ++g) in[c][g] = Eight<VEC, TPR>{N, col, c}.in(g);
+            for (int g = 0; g < 8 / VEC; ++g) in[c][g] = At{N, col, c}.in(g);
     }
     __device__ __forceinline__ float2 only(float2 v, int c, int k) const {
         if constexpr (VEC == 8) return in[c][0] ? v : both(0.f);
@@ -101,6 +109,8 @@ __global__ void __launch_bounds__(TPR == 32 ? 128 : TPR, resident(TPR)) residual
     using SF = RowSource<TF, VEC, TPR, NV>;
     using Shared = std::conditional_t<SX::SHARED, SX, SF>;
     constexpr int WALKERS = TPR == 32 ? 4 : 1, W = TPR / 32, AHEAD = ahead_of<TX, TF, TPR, NV, VEC>(), STAGES = AHEAD + 1, CH = NV * VEC / 8;
+    constexpr int FULL = full_of(TPR, NV, VEC, fewer_of(TPR));
+    using At = Eight<VEC, TPR, FULL>;
     static_assert(AHEAD >= 1, "shared memory");
     extern __shared__ __align__(16) uint8_t ring[];
     __shared__ float2 red[2][2][W];
@@ -125,7 +135,7 @@ __global__ void __launch_bounds__(TPR == 32 ? 128 : TPR, resident(TPR)) residual
         const int own = __shfl_sync(0xFFFFFFFFu, count, norm.warp);
         norm.inv_own = own > 0 ? 1.f / static_cast<float>(own) : 0.f;
     }
-    const Inside<VEC, TPR, CH> in(N, col);
+    const Inside<VEC, TPR, CH, FULL> in(N, col);
     sm100::grid_dependency_wait();
     sm100::grid_dependency_launch();
 #pragma unroll
@@ -136,9 +146,11 @@ __global__ void __launch_bounds__(TPR == 32 ? 128 : TPR, resident(TPR)) residual
         }
         async_commit();
     }
-    constexpr bool KEEP = keeps(TPR), KEEP_POST = KEEP && POST && sizeof(TW) == 2 && VEC == 8;
-    const Vector<TW, VEC, TPR, CH, KEEP> w_of(p.v.w, 1.f, N, col), b_of(p.v.b, 0.f, N, col), gate_of(p.v.gate, 1.f, N, col);
-    const Vector<TW, VEC, TPR, CH, KEEP_POST> pw_of(p.v.pw, 1.f, N, col), pb_of(p.v.pb, 0.f, N, col);
+    // w, b, and a and c of h = scale x + a f + c (f: norm(f) with a norm of it, where a = gate pw and c = gate pb)
+    constexpr int KEEP = keeps(TPR) ? kKept : kRead, KEEP_C = keeps(TPR) && POST && sizeof(TW) == 2 && VEC == 8 ? kKept : kRead;
+    const Vector<TW, VEC, TPR, CH, FULL, KEEP> w_of(N, col, p.v.w, 1.f), b_of(N, col, p.v.b, 0.f);
+    const Vector<TW, VEC, TPR, CH, FULL, KEEP, POST> a_of(N, col, p.v.gate, 1.f, p.v.pw, 1.f);
+    const Vector<TW, VEC, TPR, CH, FULL, KEEP_C, true> c_of(N, col, POST ? p.v.gate : nullptr, 1.f, p.v.pb, 0.f);
     const float2 scale = both(p.scale);
     int stage = 0, turn = 0;
     for (int64_t m = first; m < p.M; m += step, turn ^= 1) {
@@ -152,7 +164,7 @@ __global__ void __launch_bounds__(TPR == 32 ? 128 : TPR, resident(TPR)) residual
         row_barrier<Shared, VEC, TPR>();
         float2 v[CH][4];
 #pragma unroll
-        for (int c = 0; c < CH; ++c) Eight<VEC, TPR>{N, col, c}.template read<TF>(sf, stage, m, v[c]);
+        for (int c = 0; c < CH; ++c) At{N, col, c}.template read<TF>(sf, stage, m, v[c]);
         float mu, r, shift;
         if constexpr (POST) {
             norm(v, in, red[0][turn], mu, r, shift);
@@ -160,19 +172,22 @@ __global__ void __launch_bounds__(TPR == 32 ? 128 : TPR, resident(TPR)) residual
         }
 #pragma unroll
         for (int c = 0; c < CH; ++c) {
-            const Eight<VEC, TPR> at{N, col, c};
-            float2 a[4], b[4];
+            const At at{N, col, c};
+            float2 a[4], x[4];
+            at.template read<TX>(sx, stage, m, x);
+            a_of.get(at, a);
             if constexpr (POST) {
-                pw_of.get(at, a);
-                pb_of.get(at, b);
+                float2 c_[4];
+                c_of.get(at, c_);
                 const float2 r2 = both(r), shift2 = both(shift);
 #pragma unroll
-                for (int k = 0; k < 4; ++k) v[c][k] = fma2(fma2(v[c][k], r2, shift2), a[k], b[k]);
-            }
-            at.template read<TX>(sx, stage, m, b);
-            gate_of.get(at, a);
+                for (int k = 0; k < 4; ++k) v[c][k] = fma2(fma2(v[c][k], r2, shift2), a[k], c_[k]);
+            } else {
 #pragma unroll
-            for (int k = 0; k < 4; ++k) v[c][k] = in.only(fma2(scale, b[k], mul2(a[k], v[c][k])), c, k);
+                for (int k = 0; k < 4; ++k) v[c][k] = mul2(v[c][k], a[k]);
+            }
+#pragma unroll
+            for (int k = 0; k < 4; ++k) v[c][k] = in.only(fma2(scale, x[k], v[c][k]), c, k);
             at.template store<TX>(static_cast<TX*>(p.h) + m * p.ldh, v[c]);
         }
         norm(v, in, red[1][turn], mu, r, shift);
@@ -180,7 +195,7 @@ __global__ void __launch_bounds__(TPR == 32 ? 128 : TPR, resident(TPR)) residual
         const float2 r2 = both(r), shift2 = both(shift);
 #pragma unroll
         for (int c = 0; c < CH; ++c) {
-            const Eight<VEC, TPR> at{N, col, c};
+            const At at{N, col, c};
             float2 a[4], b[4];
             w_of.get(at, a);
             b_of.get(at, b);
@@ -283,7 +298,9 @@ cudaError_t launch(const FwdParams& p, cudaStream_t st) {
         switch (t) {
             case 32: return launch_rows<TX, TF, TW, VEC, POST, 32>(p, st);
             case 64: return launch_rows<TX, TF, TW, VEC, POST, 64>(p, st);
+            case 96: return launch_rows<TX, TF, TW, VEC, POST, 96>(p, st);
             case 128: return launch_rows<TX, TF, TW, VEC, POST, 128>(p, st);
+            case 192: return launch_rows<TX, TF, TW, VEC, POST, 192>(p, st);
             case 256: return launch_rows<TX, TF, TW, VEC, POST, 256>(p, st);
             case 384: return launch_rows<TX, TF, TW, VEC, POST, 384>(p, st);
             case 512: return launch_rows<TX, TF, TW, VEC, POST, 512>(p, st);
