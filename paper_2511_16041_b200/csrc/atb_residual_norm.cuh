@@ -141,7 +141,7 @@ enum Place { kRead = 0, kKept = 1, kShared = 2 };
 template <class TW, int VEC, int TPR, int CH, int FULL, int PLACE, bool PRODUCT = false>
 struct Vector {
     static constexpr bool RAW = PLACE == kKept && VEC == 8 && !PRODUCT, VALUES = PLACE == kKept && !RAW;
-    static constexpr uint32_t BYTES = CH * 2 * TPR * 16;
+    static constexpr uint32_t PIECES = (TPR == 32 ? 128 : TPR) * 16, BYTES = CH * 2 * PIECES;
     const void *p, *q;
     float none, none_q;
     uint32_t place;
@@ -165,7 +165,7 @@ struct Vector {
                 read(at, v);
 #pragma unroll
                 for (int half = 0; half < 2; ++half)
-                    asm volatile("st.shared.v4.f32 [%0], {%1, %2, %3, %4};" ::"r"(place + (c * 2 + half) * TPR * 16), "f"(v[2 * half].x), "f"(v[2 * half].y),
+                    asm volatile("st.shared.v4.f32 [%0], {%1, %2, %3, %4};" ::"r"(place + (c * 2 + half) * PIECES), "f"(v[2 * half].x), "f"(v[2 * half].y),
                                  "f"(v[2 * half + 1].x), "f"(v[2 * half + 1].y) : "memory");
             }
         }
@@ -190,7 +190,7 @@ struct Vector {
 #pragma unroll
             for (int half = 0; half < 2; ++half)
                 asm volatile("ld.shared.v4.f32 {%0, %1, %2, %3}, [%4];" : "=f"(v[2 * half].x), "=f"(v[2 * half].y), "=f"(v[2 * half + 1].x), "=f"(v[2 * half + 1].y)
-                             : "r"(place + (at.c * 2 + half) * TPR * 16));
+                             : "r"(place + (at.c * 2 + half) * PIECES));
         } else {
             read(at, v);
         }

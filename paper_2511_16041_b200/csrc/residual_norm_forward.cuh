@@ -24,16 +24,21 @@ __host__ __device__ constexpr int fewer_of(int tpr) {
 template <class TX, class TF>
 constexpr int kMostThreads = sizeof(TX) + sizeof(TF) == 8 ? 768 : 1024;        // two stages of rows in shared memory
 // The vectors of weights stay in registers (a thread has the same columns of every row), but in the widest kernels, whose threads
-// have too few, and but for FP32 gate pb, which would be one too many.
+// have too few, and but for FP32 gate pb, which would be one too many: it lies in shared memory (read again from the L1, which the rows on
+// their way leave little of, 16384 x 8192 took 276 us).
 __host__ __device__ constexpr bool keeps(int tpr) { return tpr <= 512; }
 // Blocks that stay on an SM: 512 threads of 128 registers.
 __host__ __device__ constexpr int resident(int tpr) { return tpr == 32 ? 4 : tpr >= 512 ? 1 : 512 / tpr; }
 template <class TX, class TF, int TPR, int NV, int VEC>
 constexpr int kStageBytes = static_cast<int>(RowSource<TX, VEC, TPR, NV>::STAGE_BYTES + RowSource<TF, VEC, TPR, NV>::STAGE_BYTES);
-// Rows on their way: 3, or what 200 KB per SM hold beside the row in hand.
-template <class TX, class TF, int TPR, int NV, int VEC>
+template <class TW, int TPR, int VEC, bool POST>
+__host__ __device__ constexpr int c_bytes() { return keeps(TPR) && POST && !(sizeof(TW) == 2 && VEC == 8) ? kElems / 4 * (TPR == 32 ? 128 : TPR) * 16 : 0; }
+// Rows on their way: 3, or what 200 KB per SM (with gate pb all 228 KB, of which a block takes 1 KB and its static arrays besides) hold beside the
+// row in hand.
+template <class TX, class TF, class TW, int TPR, int NV, int VEC, bool POST>
 __host__ __device__ constexpr int ahead_of() {
-    const int stages = 200 * 1024 / (resident(TPR) * kStageBytes<TX, TF, TPR, NV, VEC>);
+    const int room = c_bytes<TW, TPR, VEC, POST>() ? 228 * 1024 / resident(TPR) - 1664 - c_bytes<TW, TPR, VEC, POST>() : 200 * 1024 / resident(TPR);
+    const int stages = room / kStageBytes<TX, TF, TPR, NV, VEC>;
     return stages > 4 ? 3 : stages - 1;
 }
 
@@ -108,7 +113,7 @@ __global__ void __launch_bounds__(TPR == 32 ? 128 : TPR, resident(TPR)) residual
     using SX = RowSource<TX, VEC, TPR, NV>;
     using SF = RowSource<TF, VEC, TPR, NV>;
     using Shared = std::conditional_t<SX::SHARED, SX, SF>;
-    constexpr int WALKERS = TPR == 32 ? 4 : 1, W = TPR / 32, AHEAD = ahead_of<TX, TF, TPR, NV, VEC>(), STAGES = AHEAD + 1, CH = NV * VEC / 8;
+    constexpr int WALKERS = TPR == 32 ? 4 : 1, W = TPR / 32, AHEAD = ahead_of<TX, TF, TW, TPR, NV, VEC, POST>(), STAGES = AHEAD + 1, CH = NV * VEC / 8;
     constexpr int FULL = full_of(TPR, NV, VEC, fewer_of(TPR));
     using At = Eight<VEC, TPR, FULL>;
     static_assert(AHEAD >= 1, "shared memory");
@@ -147,10 +152,11 @@ __global__ void __launch_bounds__(TPR == 32 ? 128 : TPR, resident(TPR)) residual
         async_commit();
     }
     // w, b, and a and c of h = scale x + a f + c (f: norm(f) with a norm of it, where a = gate pw and c = gate pb)
-    constexpr int KEEP = keeps(TPR) ? kKept : kRead, KEEP_C = keeps(TPR) && POST && sizeof(TW) == 2 && VEC == 8 ? kKept : kRead;
+    constexpr int KEEP = keeps(TPR) ? kKept : kRead, KEEP_C = c_bytes<TW, TPR, VEC, POST>() ? kShared : keeps(TPR) && POST ? kKept : kRead;
     const Vector<TW, VEC, TPR, CH, FULL, KEEP> w_of(N, col, p.v.w, 1.f), b_of(N, col, p.v.b, 0.f);
     const Vector<TW, VEC, TPR, CH, FULL, KEEP, POST> a_of(N, col, p.v.gate, 1.f, p.v.pw, 1.f);
-    const Vector<TW, VEC, TPR, CH, FULL, KEEP_C, true> c_of(N, col, POST ? p.v.gate : nullptr, 1.f, p.v.pb, 0.f);
+    const Vector<TW, VEC, TPR, CH, FULL, KEEP_C, true> c_of(N, col, POST ? p.v.gate : nullptr, 1.f, p.v.pb, 0.f,
+                                                               sm100::smem_u32(ring) + STAGES * kStageBytes<TX, TF, TPR, NV, VEC>);
     const float2 scale = both(p.scale);
     int stage = 0, turn = 0;
     for (int64_t m = first; m < p.M; m += step, turn ^= 1) {
@@ -287,7 +293,7 @@ __global__ void __launch_bounds__(1024) residual_norm_wide_kernel(const FwdParam
 // ---------------------------------------------------------------------------------- host
 template <class TX, class TF, class TW, int VEC, bool POST, int TPR>
 cudaError_t launch_rows(const FwdParams& p, cudaStream_t st) {
-    constexpr int NV = kElems / VEC, THREADS = TPR == 32 ? 128 : TPR, ROOM = (ahead_of<TX, TF, TPR, NV, VEC>() + 1) * kStageBytes<TX, TF, TPR, NV, VEC>;
+    constexpr int NV = kElems / VEC, THREADS = TPR == 32 ? 128 : TPR, ROOM = (ahead_of<TX, TF, TW, TPR, NV, VEC, POST>() + 1) * kStageBytes<TX, TF, TPR, NV, VEC> + c_bytes<TW, TPR, VEC, POST>();
     const int64_t all = atb::ceil_div(p.M, TPR == 32 ? 4 : 1), most = static_cast<int64_t>(atb::kSmCount) * resident(TPR);
     return launch_ring<&residual_norm_kernel<TX, TF, TW, VEC, TPR, NV, POST>>(static_cast<unsigned>(all < most ? all : most), THREADS, ROOM, st, p);
 }
