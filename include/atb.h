@@ -343,14 +343,14 @@ atb_status_t atb_select_tiling(int64_t M, int64_t N, int64_t K, const atb_hw_par
                                atb_tiling_t* best, atb_tiling_score_t* scores, int* n_scores);
 
 /* =====================================================================================================
- * What stands between the products of a network: layer norm, the gated feed-forward block, and the softmax
- * cross entropy of a linear head, each forward and backward.  The general rules above hold for them too; in
- * addition
+ * What stands between the products of a network: layer norm, the gated feed-forward block, the softmax cross
+ * entropy of a linear head, the linear layer and the residual norm, each forward and backward, and sampling.
+ * The general rules above hold for them too; in addition
  *   - matrices are row-major, ld* is the number of elements between rows; bf16 operands of products are
  *     16-byte aligned with leading dimensions that are multiples of 8;
  *   - an output must not overlap an input, another output or the workspace;
  *   - sums, norms' statistics, softmax statistics and losses are FP32; every call with the same arguments
- *     on the same GPU model gives the same bits (no atomics);
+ *     on the same GPU model gives the same bits (no atomics but of integers);
  *   - what is rounded to bf16 on the way: operands that one product makes for the next (H, dG, dU, dL: the tensor
  *     cores take bf16), and, without ATB_KEEP_F32, G and U (half the memory; dX, dWg and dWu are 0.0030 of
  *     their norm off instead of 0.0024, rounding the results alone is 0.0017); exponentials and
@@ -497,7 +497,8 @@ atb_status_t atb_residual_norm_backward(int64_t M, int64_t N, int kind, int x_ty
  *   top_k; those of weight >= min_p (the largest is 1).  Always one at least.
  *   The token is the first word, in the vocabulary's order, at which the sum of the kept weights exceeds u times all kept weight; its
  *   probability among the kept goes to probs.  Weights are held as multiples of 2^-45 (of 2^-(62 - log2 V) where V > 2^17) in 64-bit
- *   integers, so that sums are exact: what weighs less than half of that is never drawn, and the draw is that of arithmetic in 64 bits.
+ *   integers, so that sums are exact: what weighs less than half of that is never drawn; a border or a draw falls otherwise than in 64 bits
+ *   only where it is within the sum of those roundings of another word (top_p = 0.99 of 131072 words: one row in a million).
  *   logits_dev: type [M][ld] (V columns), any alignment of whole elements;  u_dev: u_type (ATB_F32 or ATB_F64) [M], in [0, 1): what is outside is
  *   taken for the nearer end, NaN for 0;  tokens_dev int64 [M];  probs_dev FP32 [M] or NULL.
  *   Settings: one number for all rows, or, where its pointer is not NULL, one of each row (FP32, top_k int32) [M]:

@@ -826,6 +826,8 @@ bf16_mm_kernel(const __grid_constant__ MmMaps<MmCfg<PAIR, EPI>::JOBS> tm, const 
             const int64_t row0 = static_cast<int64_t>(w.mt) * C::TILE_M + rank * 128 + q * 32, col0 = static_cast<int64_t>(w.nt) * tile_n;
             const int acc = it & 1;
             if constexpr (EPI == atb::kMmLinear) {
+                // Residual and bias are asked for before the accumulator is waited for: after it, 509 x 2048 x 5464 took 24.1 us instead of 22.0 and
+                // 16 x 2048 x 32000 28.4 instead of 26.6.
                 const int64_t own0 = col0 + half * C::COLS;
                 linear_fetch<C, KEEP32>(tm, p, jb, out, row0, own0);
                 const LinearBias<C> bias(p, jb, own0, lane);

