@@ -10,7 +10,7 @@
 // only sums, and is left out where the bias has no gradient.
 // The forward pass is bound by the product (8192 x 4096 x 10944 with z in FP32 504 us, 1.46 PFLOP/s) or, where rows are few, by W (16 rows,
 // 2048 x 32000 stored [N][K]: 27 us, 4.9 TB/s); a prompt of one wave of tiles by its launch, fill and drain (509 x 2048 x 5464: 22 us, of which
-// 18.5 are the product alone).  The gradient's pass is bound by memory: 8192 x 10944, z in FP32, 160 us (4.5 TB/s).  The two
+// 18.5 are the product alone).  The gradient's pass is bound by memory: 8192 x 10944, z in FP32, 118 us (6.1 TB/s).  The two
 // products after it run at 1.54 PFLOP/s alone (955 us) and slower under the power cap behind a forward pass.
 #include <algorithm>
 
@@ -43,13 +43,14 @@ struct GradParams {
     const void *dy, *z;
     __nv_bfloat16* dz;                     // [M][N], or NULL
     float* part;                           // [gridDim.y][N], or NULL
-    int act, y32, z32;
+    int act;
 };
 
 constexpr int kGradWarps = 8, kGradThreads = kGradWarps * 32, kGradCols = 256;
 
-__device__ __forceinline__ void load8(const void* p, int64_t at, int fp32, float (&v)[8]) {
-    if (fp32) {
+template <bool FP32>
+__device__ __forceinline__ void load8(const void* p, int64_t at, float (&v)[8]) {
+    if constexpr (FP32) {
         const float4* s = reinterpret_cast<const float4*>(static_cast<const float*>(p) + at);
         const float4 a = __ldcs(s), b = __ldcs(s + 1);
         v[0] = a.x; v[1] = a.y; v[2] = a.z; v[3] = a.w;
@@ -66,6 +67,7 @@ __device__ __forceinline__ void load8(const void* p, int64_t at, int fp32, float
 }
 
 // A block takes 256 columns (a lane 8 of them) and the rows blockIdx.y kGradWarps + warp, + gridDim.y kGradWarps, ...
+template <bool Y32, bool Z32>
 __global__ void __launch_bounds__(kGradThreads, 4) linear_grad_kernel(const GradParams p) {
     __shared__ float sums[kGradWarps][kGradCols];
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
@@ -78,10 +80,10 @@ __global__ void __launch_bounds__(kGradThreads, 4) linear_grad_kernel(const Grad
 #pragma unroll 2
             for (int64_t m = static_cast<int64_t>(blockIdx.y) * kGradWarps + warp; m < p.M; m += static_cast<int64_t>(gridDim.y) * kGradWarps) {
                 float d[8];
-                load8(p.dy, m * p.lddy + n, p.y32, d);
+                load8<Y32>(p.dy, m * p.lddy + n, d);
                 if constexpr (act.value != ATB_ACT_NONE) {
                     float z[8];
-                    load8(p.z, m * p.N + n, p.z32, z);
+                    load8<Z32>(p.z, m * p.N + n, z);
 #pragma unroll
                     for (int e = 0; e < 4; ++e) {
                         float2 a, slope;
@@ -137,10 +139,11 @@ __global__ void __launch_bounds__(256) linear_bias_kernel(const float* part, int
     }
 }
 
-// Blocks along the rows: four blocks per SM in all, at least 4 rows for each warp.
+// Blocks along the rows: four blocks per SM in all, and no more, which would be a second round (8192 x 10944: 602 blocks for 592 places took
+// 160 us); at least 4 rows for each warp.
 int row_blocks(int64_t M, int64_t N) {
     const int64_t across = atb::ceil_div(N, kGradCols), most = atb::ceil_div(M, 4 * kGradWarps);
-    int64_t blocks = atb::ceil_div(4 * atb::kSmCount, across);
+    int64_t blocks = 4 * atb::kSmCount / across;
     if (blocks > most) blocks = most;
     return static_cast<int>(blocks < 1 ? 1 : blocks);
 }
@@ -244,7 +247,8 @@ extern "C" atb_status_t atb_linear_backward(int64_t M, int64_t K, int64_t N, int
         GradParams g = {};
         g.M = M; g.N = N; g.lddy = lddy;
         g.dy = dY_dev; g.z = Z_dev;
-        g.act = act; g.y32 = y_type == ATB_F32; g.z32 = z_type == ATB_F32;
+        g.act = act;
+        const bool y32 = y_type == ATB_F32, z32 = z_type == ATB_F32;
         if (!is_dy && any) {
             g.dz = reinterpret_cast<__nv_bfloat16*>(room);
             dz = {room, N};
@@ -260,7 +264,9 @@ extern "C" atb_status_t atb_linear_backward(int64_t M, int64_t K, int64_t N, int
         attr[0].val.programmaticStreamSerializationAllowed = 1;
         cfg.attrs = attr;
         cfg.numAttrs = 1;
-        cudaError_t e = cudaLaunchKernelEx(&cfg, linear_grad_kernel, static_cast<const GradParams>(g));
+        const auto kernel = y32 ? (z32 ? linear_grad_kernel<true, true> : linear_grad_kernel<true, false>)
+                                : (z32 ? linear_grad_kernel<false, true> : linear_grad_kernel<false, false>);
+        cudaError_t e = cudaLaunchKernelEx(&cfg, kernel, static_cast<const GradParams>(g));
         if (e == cudaSuccess && dbias_dev)
             e = atb::launch_dependent(linear_bias_kernel, static_cast<unsigned>(atb::ceil_div(N, 32)), 256u, 1u, 0, st, static_cast<const float*>(g.part), parts, N,
                                       dbias_dev, static_cast<int>(bias_type == ATB_F32));
