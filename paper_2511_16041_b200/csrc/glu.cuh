@@ -74,7 +74,11 @@ __device__ __forceinline__ void linear_act(float2 z, float2& a, float2& slope) {
         a = make_float2(z.x < 0.f ? 0.f : z.x, z.y < 0.f ? 0.f : z.y);
         slope = make_float2(z.x > 0.f ? 1.f : 0.f, z.y > 0.f ? 1.f : 0.f);
     } else {
-        act_value_slope<ACT>(z, a, slope);
+        // slopes are 0 or 1 long before 1e9, and no product of larger z and 0 is in them; NaN stays NaN.  A caller takes a or the slope.
+        const auto near = [](float v) { return v > 1e9f ? 1e9f : v < -1e9f ? -1e9f : v; };
+        float2 unused;
+        act_value_slope<ACT>(z, a, unused);
+        act_value_slope<ACT>(make_float2(near(z.x), near(z.y)), unused, slope);
     }
 }
 template <int ACT>

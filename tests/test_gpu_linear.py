@@ -215,3 +215,21 @@ def test_gradients_against_differences(M, act):
         rounding = U16 * float((1.13 * cd * reach).sum()) + U16 * float(got.double().abs().sum())
         slopes = ACT_REL * float((((Z.double().abs() + 1) ** 3) * cd * (reach if i < 2 else 1)).sum())
         assert abs(along - want) <= third + values + rounding + slopes, (i, along, want)
+
+
+@pytest.mark.parametrize("act", ["silu", "gelu", "gelu_tanh"])
+@pytest.mark.parametrize("z_type", [torch.float32, torch.bfloat16])
+def test_the_slopes_of_large_and_infinite_sums(act, z_type):
+    """Beyond |z| = 150 the slope's distance to 1 or 0 is less than e^-140 z, below FP32's range: dZ is dY or 0.  A NaN stays one."""
+    at = [150.0, 1e5, 1e10, 1e20, 1e31, 3e38, float("inf")]
+    Z = torch.tensor([s * v for v in at for s in (1.0, -1.0)] + [float("nan"), 0.0], device="cuda").to(z_type).expand(3, 16).contiguous()
+    dy = torch.full((3, 16), 0.5, device="cuda", dtype=torch.bfloat16)
+    x = torch.ones(3, 8, device="cuda", dtype=torch.bfloat16)
+    w = torch.ones(8, 16, device="cuda", dtype=torch.bfloat16)
+    _, dw, db = atb.atb_linear_backward(dy, x, w, Z, act=act, dX=False)
+    want = torch.tensor([1.5, 0.0] * len(at) + [float("nan"), 0.75], device="cuda")
+    assert torch.equal(db.isnan(), want.isnan()) and torch.equal(db[:-2], want[:-2])
+    # Phi(0) of the erf form comes from a polynomial, off by at most 4.4e-7 of it in FP32; the two additions of three rows are off by 2^-24 each:
+    # 4.4e-7 + 1.2e-7 = 5.6e-7 < 2^-20 = 9.5e-7 of the sum
+    assert abs(float(db[-1]) - 0.75) <= 0.75 * 2.0 ** -20
+    assert torch.equal(dw.float().nan_to_num(7.0), want.nan_to_num(7.0).expand(8, 16))
