@@ -18,23 +18,25 @@
 namespace residual_norm {
 namespace {
 
-// Two FP32 rows of more than 4096 elements leave no room for dh beside x, f and dz twice: it is loaded where it is used.
-template <class TX, class TF, int VEC, int NV>
-constexpr bool kDirect = sizeof(TX) + sizeof(TF) == 8 && NV * VEC > 8;
-template <class TX, class TF, int VEC, int TPR, int NV>
-constexpr int kStage = static_cast<int>((kDirect<TX, TF, VEC, NV> ? 1 : 2) * RowSource<TX, VEC, TPR, NV>::STAGE_BYTES + 2 * RowSource<TF, VEC, TPR, NV>::STAGE_BYTES);
+// Two FP32 rows of more than 4096 elements leave no room for dh beside x, f and dz twice, nor do those of an FP32 stream of more than 6144 where the
+// vectors of weights need it (8192 x 8192 with a norm of f 301 us; with dh on its way and the vectors read where they are used 396): it is
+// loaded where it is used.
+template <class TX, class TF, int VEC, int TPR, int NV, bool POST>
+constexpr bool kDirect = NV * VEC > 8 && (sizeof(TX) + sizeof(TF) == 8 || (sizeof(TX) + sizeof(TF) == 6 && POST && TPR >= 512));
+template <class TX, class TF, int VEC, int TPR, int NV, bool POST>
+constexpr int kStage = static_cast<int>((kDirect<TX, TF, VEC, TPR, NV, POST> ? 1 : 2) * RowSource<TX, VEC, TPR, NV>::STAGE_BYTES + 2 * RowSource<TF, VEC, TPR, NV>::STAGE_BYTES);
 // Bytes of the vectors of weights in shared memory: three, where a thread's registers are full of sums (16 elements, four sums) and two stages
 // of rows leave the room (read where they are used, 8192 x 6001 bf16 took 616 us instead of 264).
 constexpr int kRoom = 226 * 1024;
 template <class TX, class TF, int VEC, int TPR, int NV, bool POST>
 __host__ __device__ constexpr int vector_bytes() {
     const int bytes = 3 * (NV * VEC / 8) * 2 * TPR * 16;
-    return POST && NV * VEC == 16 && kRoom - bytes >= 2 * kStage<TX, TF, VEC, TPR, NV> ? bytes : 0;
+    return POST && NV * VEC == 16 && kRoom - bytes >= 2 * kStage<TX, TF, VEC, TPR, NV, POST> ? bytes : 0;
 }
 template <class TX, class TF, int VEC, int TPR, int NV, bool POST>
 __host__ __device__ constexpr int ahead_of() {
     const int vectors = vector_bytes<TX, TF, VEC, TPR, NV, POST>();
-    const int stages = (vectors ? kRoom - vectors : 208 * 1024) / (blocks_of(TPR) * kStage<TX, TF, VEC, TPR, NV>);
+    const int stages = (vectors ? kRoom - vectors : 208 * 1024) / (blocks_of(TPR) * kStage<TX, TF, VEC, TPR, NV, POST>);
     return stages > 4 ? 3 : stages - 1;
 }
 
@@ -43,7 +45,7 @@ __global__ void __launch_bounds__(TPR == 32 ? 128 : TPR, blocks_of(TPR)) residua
     using SX = RowSource<TX, VEC, TPR, NV>;
     using SF = RowSource<TF, VEC, TPR, NV>;
     using Shared = std::conditional_t<SX::SHARED, SX, SF>;
-    constexpr bool DIRECT = kDirect<TX, TF, VEC, NV>;
+    constexpr bool DIRECT = kDirect<TX, TF, VEC, TPR, NV, POST>;
     constexpr int WALKERS = TPR == 32 ? 4 : 1, W = TPR / 32, AHEAD = ahead_of<TX, TF, VEC, TPR, NV, POST>(), STAGES = AHEAD + 1, CH = NV * VEC / 8;
     using At = Eight<VEC, TPR, FULL>;
     static_assert(AHEAD >= 1, "shared memory");
@@ -77,7 +79,7 @@ __global__ void __launch_bounds__(TPR == 32 ? 128 : TPR, blocks_of(TPR)) residua
     // w, a and b lie in shared memory if that has the room.
     constexpr bool IN_SHARED = vector_bytes<TX, TF, VEC, TPR, NV, POST>() > 0, FOLD = POST && (VEC == 1 || IN_SHARED);
     constexpr int KEEP = IN_SHARED ? kShared : !POST || CH == 1 ? kKept : kRead;
-    const uint32_t place = base + STAGES * kStage<TX, TF, VEC, TPR, NV>;
+    const uint32_t place = base + STAGES * kStage<TX, TF, VEC, TPR, NV, POST>;
     using Kept = Vector<TW, VEC, TPR, CH, FULL, KEEP>;
     const Kept w_of(N, col, p.v.w, 1.f, nullptr, 1.f, place);
     const Vector<TW, VEC, TPR, CH, FULL, KEEP, FOLD> a_of(N, col, p.v.gate, 1.f, p.v.pw, 1.f, place + Kept::BYTES);                  // gate, or a
@@ -334,7 +336,7 @@ cudaError_t launch_rows(const BwdParams& p, cudaStream_t st) {
     constexpr int TPR = kWidths[W].threads, NV = kWidths[W].elems / VEC, STAGES = ahead_of<TX, TF, VEC, TPR, NV, POST>() + 1;
     constexpr int FULL = full_of(TPR, kWidths[W].elems, VEC, W > 0 ? kWidths[W > 0 ? W - 1 : 0].threads * kWidths[W > 0 ? W - 1 : 0].elems : 0);
     return launch_ring<&residual_norm_backward_kernel<TX, TF, TW, VEC, TPR, NV, FULL, POST>>(static_cast<unsigned>(p.blocks), TPR == 32 ? 128u : TPR,
-                                                                                             static_cast<size_t>(STAGES) * kStage<TX, TF, VEC, TPR, NV> + vector_bytes<TX, TF, VEC, TPR, NV, POST>(), st, p);
+                                                                                             static_cast<size_t>(STAGES) * kStage<TX, TF, VEC, TPR, NV, POST> + vector_bytes<TX, TF, VEC, TPR, NV, POST>(), st, p);
 }
 template <class TX, class TF, class TW, int VEC, bool POST>
 cudaError_t launch(const BwdParams& p, cudaStream_t st) {

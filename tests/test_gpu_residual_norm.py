@@ -172,6 +172,14 @@ def test_rows(M, N):
     Case(M, N, TYPES[(M + 1) % 3], post=False, seed=M).run(dh=False)
 
 
+@pytest.mark.parametrize("types", TYPES)
+@pytest.mark.parametrize("N", [258, 400, 512, 6001, 6152, 8001, 8192])
+def test_several_rows_of_a_walker(N, types):
+    """More rows than are on their way at once, for the layouts that keep the weights in places of their own beside four sums."""
+    M = 5000 if N < 1000 else 900
+    Case(M, N, types, (F32, BF16)[N % 2], ("layer", "rms")[N // 2 % 2], gate=True, post=True, seed=N).run(dh=N != 6152)
+
+
 @pytest.mark.parametrize("pad", [8, 24, 1, 3, 6])
 @pytest.mark.parametrize("types", TYPES)
 @pytest.mark.parametrize("N", [77, 512, 4097])
