@@ -347,8 +347,9 @@ __global__ void __launch_bounds__(kMostThreads, 2) sample_kernel(const SamplePar
     const auto depth = [&](float l) { return (static_cast<double>(top) - static_cast<double>(l)) * slope; };
     const float half_top = 0.5f * top, slope_f = fminf(static_cast<float>(slope), 1e30f);
     const double slope16 = 16.0 * slope, top64 = top;
-    // no logit deeper than this weighs anything, and neither does this (depth below 48.5 + 1000, by the rounding down)
-    const float floor_l = fmaxf(__fsub_rd(top, static_cast<float>(48.5 / slope)), -3.402823466e38f);
+    // no logit deeper than this weighs anything, and neither does this: depth 48.5 and, by the distance's rounding up (250 at most, where it is
+    // subnormal) and the difference's rounding down (500), less than 800.  To the nearest, the distance became 0 at T < 2.1e-47.
+    const float floor_l = fmaxf(__fsub_rd(top, __double2float_ru(48.5 / slope)), -3.402823466e38f);
     // of a finite logit, without branches, so that several run at once
     const auto biased = [&](float l) { return fixed_exp2_biased(top64 - static_cast<double>(fmaxf(l, floor_l)), slope16, sh.table); };
     const auto weight = [&](float l) { return static_cast<unsigned long long>(__double_as_longlong(biased(l))) - 0x4330000000000000ull; };
