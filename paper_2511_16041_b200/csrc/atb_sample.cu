@@ -803,13 +803,14 @@ __global__ void __launch_bounds__(kMostThreads, 2) sample_kernel(const SamplePar
             join(false);
             // What the words of bin b weigh together, in units of 2^S: their count times what its ends weigh, a little more or less for
             // bin_of's roundings and the weights' own.  The sum of all is within 1.5e-5 of what was added up (a product of y <= 47 is
-            // off by 3 * 2^-24 of it, and its power by as much times y ln 2), the sums of a thousand terms here within 1e-6 of all.  Where the scale has
+            // off by 3 * 2^-24 of it, and its power by as much times y ln 2) and of the weights' own roundings, half a unit each (2^-29 of the largest
+            // weight in all at 2^17 words, 2^-13 at 2^25, 1/8 at 2^30); the sums of a thousand terms here within 1e-6 of all.  Where the scale has
             // left its range, the bins say nothing, and all words are looked at.
+            const float unit = exp2f(static_cast<float>(-p.shift)), roundings = 0.5f * unit * static_cast<float>(p.V);
             const float all = static_cast<float>(sh.real), cut = static_cast<float>(static_cast<double>(excess) / static_cast<double>(1ull << p.shift));
-            const float low_all = all * (1.f - 1.5e-5f), high_all = all * (1.f + 1.5e-5f), top_p = static_cast<float>(sh.top_p);
+            const float low_all = all * (1.f - 1.5e-5f) - roundings, high_all = all * (1.f + 1.5e-5f) + roundings, top_p = static_cast<float>(sh.top_p);
             const float low_goal = top_p * fmaxf(low_all - cut, 0.f) * (1.f - 1e-6f), high_goal = top_p * fmaxf(high_all - cut, 0.f) * (1.f + 1e-6f);
             const bool known = scale > 1e-30f && scale < 1e30f;
-            const float unit = exp2f(static_cast<float>(-p.shift));
             const auto most_of = [&](int b) { return static_cast<float>(sh.count[b]) * (exp2f(static_cast<float>(b) / -kBinsPerUnit) * (1.f + 2e-5f) + unit); };
             const auto least_of = [&](int b) {
                 return b == kBins - 1 ? 0.f : static_cast<float>(sh.count[b]) * fmaxf(exp2f(static_cast<float>(b + 1) / -kBinsPerUnit) * (1.f - 2e-5f) - unit, 0.f);
@@ -845,18 +846,14 @@ __global__ void __launch_bounds__(kMostThreads, 2) sample_kernel(const SamplePar
             });
         }
         publish();
-        const bool found = narrow(true, [&](uint32_t, unsigned long long w) { return static_cast<double>(w) >= sh.found.goal; }, tau_k, scale, excess);
-        const double goal = sh.found.goal;
-        if (found) {
+        // (all words' sum reaches the goal, so that there is a border)
+        if (narrow(true, [&](uint32_t, unsigned long long w) { return static_cast<double>(w) >= sh.found.goal; }, tau_k, scale, excess)) {
+            const double goal = sh.found.goal;
             // of the words at tau, those before which the weight is below the goal
             const double before = static_cast<double>(sh.found.above), each_one = static_cast<double>(weight(of_key(tau)));
             const double n = goal > before ? ceil((goal - before) / each_one) : 0.0;
             quota = n < 1.0 ? 1u : n < static_cast<double>(equal_all) ? static_cast<uint32_t>(n) : equal_all;
             if (tau == tau_k && quota > quota_k) quota = quota_k;
-        } else {
-            tau = tau_k;
-            quota = quota_k;
-            equal_all = equal_k;
         }
     }
 

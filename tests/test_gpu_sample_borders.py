@@ -1,4 +1,6 @@
 """Sampling where a border or a draw hangs on the weights' and the borders' own arithmetic."""
+import math
+
 import pytest
 import torch
 
@@ -23,3 +25,37 @@ def test_temperatures_near_the_least_distance_of_logits(V, settings, T):
     x[4] -= 2.0 ** -126
     x[5] += 2.0 ** -120
     compare(x, torch.rand(6, generator=gen, device="cuda"), temperature=T, **settings)
+
+
+# A temperature at which a logit is its word's power of 2.
+POWERS = 1.4426950408889634
+
+
+def test_weights_that_round_to_nothing():
+    """2^25 words, units of 2^-37: 2^-38.001 rounds to 0, and 2^-13 of the largest weight with it, in all.  The largest word alone reaches the goal,
+    which is a millionth of its weight below it; all other weights are whole numbers of units."""
+    V = 1 << 25
+    x = torch.full((1, V), -38.001, device="cuda")
+    x[0, 10], x[0, 20] = 0.0, -14.0
+    x[0, 30:62] = -15.0
+    p = 2 ** 37 / (2 ** 37 + 2 ** 23 + 32 * 2 ** 22) * (1 - 1e-6)
+    for u in (0.0, 0.5, 0.99999):
+        tokens, probs = atb.atb_sample(x, torch.tensor([u], device="cuda", dtype=torch.float64), temperature=POWERS, top_p=p)
+        assert int(tokens) == 10 and float(probs) == 1.0
+
+
+def test_weights_that_round_to_a_unit():
+    """2^29 words, units of 2^-33: 2^-33.999 rounds to one, and all of them weigh 1/16 of the largest instead of 1/32.  Sums are whole numbers of units,
+    and what is kept is the largest word and the first few per cent of the others."""
+    V = 1 << 29
+    x = torch.full((2, V), -34.0, device="cuda", dtype=torch.bfloat16)
+    x[:, 0] = 0.0
+    p, u = 0.945, torch.tensor([0.0, 0.9999], device="cuda", dtype=torch.float64)
+    tokens, probs = atb.atb_sample(x, u, temperature=POWERS * 34.0 / 33.999, top_p=p, min_p=1e-12)
+    goal = p * float(2 ** 33 + V - 1)
+    total = 2 ** 33 + math.ceil(goal - 2.0 ** 33)
+    # the word behind the largest that u lies in; the j-th of them has 2^33 + j units up to its own
+    target = int(float(u[1]) * float(total)) + 1
+    assert tokens.tolist() == [0, target - 2 ** 33]
+    want = torch.tensor([2.0 ** 33 / total, 1.0 / total], dtype=torch.float64).float()
+    assert torch.equal(probs.cpu(), want)
