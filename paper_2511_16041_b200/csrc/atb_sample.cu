@@ -293,9 +293,9 @@ __global__ void __launch_bounds__(kMostThreads, 2) sample_kernel(const SamplePar
     if (k <= 0 || k > p.V) k = p.V;
     double slope = greedy ? 1.4426950408889634074 : 1.4426950408889634074 / temperature;
     if (t == 0) {                          // what is needed late waits in shared memory
-        const double min_p = real(p.min_p);
+        const double min_p = real(p.min_p), top_p = real(p.top_p);
         sh.u = p.u64 ? static_cast<const double*>(p.u)[m] : static_cast<double>(static_cast<const float*>(p.u)[m]);
-        sh.top_p = greedy ? 1.0 : real(p.top_p);
+        sh.top_p = greedy ? 1.0 : top_p < 0.0 ? 0.0 : top_p;     // (-inf times no weight would be NaN)
         // weight >= min_p by the exponents; 1 and more keep what weighs 1 in 64 bits, which is more than 1 - 2^-54
         sh.deepest = min_p > 0.0 ? fmax(min_p < 1.0 ? -log2(min_p) : 0.0, 0x1p-54 * 1.4426950408889634074) : INFINITY;
     }

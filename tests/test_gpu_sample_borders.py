@@ -59,3 +59,16 @@ def test_weights_that_round_to_a_unit():
     assert tokens.tolist() == [0, target - 2 ** 33]
     want = torch.tensor([2.0 ** 33 / total, 1.0 / total], dtype=torch.float64).float()
     assert torch.equal(probs.cpu(), want)
+
+
+@pytest.mark.parametrize("V", [1000, 131072, 500000])
+@pytest.mark.parametrize("top_k", [0, 1, 4, 300])
+@pytest.mark.parametrize("top_p", [-math.inf, -1.0, 0.0])
+def test_top_p_of_nothing_and_less(V, top_k, top_p):
+    """The first word in the order is kept, also where top-k cuts through so many equals that what it leaves is lost in the weight of all."""
+    x = torch.zeros((3, V), device="cuda")
+    x[1, :V // 2] = -1.0
+    u = torch.tensor([0.0, 0.5, 0.999], device="cuda")
+    for p in (top_p, torch.full((3,), top_p, device="cuda")):
+        tokens, probs = atb.atb_sample(x, u, top_k=top_k, top_p=p)
+        assert tokens.tolist() == [0, V // 2, 0] and probs.tolist() == [1.0] * 3
