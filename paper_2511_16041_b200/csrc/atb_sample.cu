@@ -556,13 +556,11 @@ __global__ void __launch_bounds__(kMostThreads, 2) sample_kernel(const SamplePar
         const int first = sh.found.first, last = sh.found.last;
         // keys of the bins' words: their ends, and more than the roundings of bin_of and of the ends can be
         uint32_t low = 0, high = key_of(top);
-        if (top < INFINITY && scale > 1e-30f && scale < 1e30f) {
+        if (scale > 1e-30f && scale < 1e30f) {
             const float up = static_cast<float>(first) / scale, down = static_cast<float>(last + 1) / scale;
             const float slack = (fabsf(top) + down) * 0x1p-21f;
             if (first > 0) high = key_of(canonical(fminf(top, top - up + slack)));
             if (last < kBins - 1) low = key_of(canonical(top - down - slack));
-        } else if (first == 0 && last == 0 && !(top < INFINITY)) {
-            low = high;                    // an infinite logit stands alone
         }
         bool begin = by_weight;            // the weights are still to be added up
         while (true) {
