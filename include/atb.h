@@ -459,6 +459,9 @@ atb_status_t atb_linear(int64_t M, int64_t K, int64_t N, int act, int y_type, co
  *   dX_dev bf16 [M][lddx]; dW_dev bf16 in W's layout with row stride lddw; dbias_dev bias_type [N]: written (not added to), each
  *   may be NULL (not wanted); X may be NULL without dW, W without dX.  M == 0 writes dW = dbias = 0. */
 size_t atb_linear_backward_workspace_bytes(int64_t M, int64_t K, int64_t N);
+/* What one call takes of it, with dX, dW and dbias wanted or not (0): no room for dZ where dZ is dY itself (ATB_ACT_NONE, y_type bf16) or no product
+ * takes it, none for sums over rows without dbias.  May be 0: no workspace, NULL accepted. */
+size_t atb_linear_backward_call_workspace_bytes(int64_t M, int64_t K, int64_t N, int act, int y_type, int w_layout, int dX, int dW, int dbias);
 atb_status_t atb_linear_backward(int64_t M, int64_t K, int64_t N, int act, int y_type, const void* dY_dev, int64_t lddy, const void* X_dev, int64_t ldx,
                                  int w_layout, const void* W_dev, int64_t ldw, int z_type, const void* Z_dev, void* dX_dev, int64_t lddx,
                                  void* dW_dev, int64_t lddw, int bias_type, void* dbias_dev, void* workspace_dev, size_t workspace_bytes,

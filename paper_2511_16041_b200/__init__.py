@@ -80,7 +80,7 @@ EXPORTED_SYMBOLS = [
     "atb_gated_ffn", "atb_gated_ffn_workspace_bytes", "atb_gated_ffn_backward", "atb_gated_ffn_backward_workspace_bytes",
     "atb_linear_cross_entropy", "atb_linear_cross_entropy_workspace_bytes",
     "atb_linear_cross_entropy_backward", "atb_linear_cross_entropy_backward_workspace_bytes",
-    "atb_linear", "atb_linear_workspace_bytes", "atb_linear_backward", "atb_linear_backward_workspace_bytes",
+    "atb_linear", "atb_linear_workspace_bytes", "atb_linear_backward", "atb_linear_backward_workspace_bytes", "atb_linear_backward_call_workspace_bytes",
     "atb_residual_norm", "atb_residual_norm_backward", "atb_residual_norm_backward_workspace_bytes",
     "atb_sample",
 ]
@@ -156,6 +156,7 @@ def load_library():
             ("atb_linear_workspace_bytes", sz, [i64, i64, i64]),
             ("atb_linear", ci, [i64, i64, i64, ci, ci, vp, i64, ci, vp, i64, ci, vp, vp, i64, vp, i64, ci, vp, vp, sz, vp]),
             ("atb_linear_backward_workspace_bytes", sz, [i64, i64, i64]),
+            ("atb_linear_backward_call_workspace_bytes", sz, [i64, i64, i64, ci, ci, ci, ci, ci, ci]),
             ("atb_linear_backward", ci, [i64, i64, i64, ci, ci, vp, i64, vp, i64, ci, vp, i64, ci, vp, vp, i64, vp, i64, ci, vp, vp, sz, vp]),
             ("atb_residual_norm", ci, [i64, i64, ci, ci, vp, i64, ci, vp, i64, cf, ci, vp, vp, vp, vp, vp, cf, vp, i64, vp, i64, vp, vp]),
             ("atb_residual_norm_backward_workspace_bytes", sz, [i64, i64]),
@@ -548,6 +549,12 @@ def atb_linear(X, W, bias=None, act=None, residual=None, dtype=None, save=False,
 
 def atb_linear_backward_workspace_bytes(M: int, K: int, N: int) -> int:
     return int(load_library().atb_linear_backward_workspace_bytes(M, K, N))
+
+
+def atb_linear_backward_call_workspace_bytes(M: int, K: int, N: int, act, y_type: int, w_layout: int, dX: bool = True, dW: bool = True, dbias: bool = True) -> int:
+    """What one call takes of ``atb_linear_backward_workspace_bytes``: less where dZ is dY (no activation, bfloat16: ``y_type`` 1) or a gradient is not wanted;
+    ``w_layout``: 0 where W is stored ``[K, N]``, 1 where ``[N, K]``."""
+    return int(load_library().atb_linear_backward_call_workspace_bytes(M, K, N, _linear_act(act), y_type, w_layout, bool(dX), bool(dW), bool(dbias)))
 
 
 def atb_linear_backward(dY, X, W, Z=None, act=None, dX=None, dW=None, dbias=None, workspace=None, stream=None):

@@ -164,6 +164,16 @@ size_t split_bytes(int64_t M, int64_t K, int64_t N, int w_layout, bool dx, bool 
     const int n = products(q, M, K, N, w_layout, dx, dw);
     return n ? atb::mm_partial_bytes(q, n) : 0;
 }
+// The workspace of a call, one area behind another: dz, where it is not dy and a product takes it; the blocks' sums, where the bias has a
+// gradient; sums of split products.
+struct Room {
+    size_t dz, part, split;
+    size_t all() const { return dz + part + split; }
+};
+Room room_of(int64_t M, int64_t K, int64_t N, int act, int y_type, int w_layout, bool dx, bool dw, bool db) {
+    const bool is_dy = act == ATB_ACT_NONE && y_type == ATB_BF16;
+    return {!is_dy && (dx || dw) ? dz_bytes(M, N) : 0, db ? part_bytes(M, N) : 0, split_bytes(M, K, N, w_layout, dx, dw)};
+}
 
 }  // namespace
 
@@ -211,6 +221,9 @@ extern "C" size_t atb_linear_backward_workspace_bytes(int64_t M, int64_t K, int6
         for (const int layout : {ATB_W_KN, ATB_W_NK}) split = std::max(split, split_bytes(M, K, N, layout, wanted & 1, wanted & 2));
     return dz_bytes(M, N) + part_bytes(M, N) + split;
 }
+extern "C" size_t atb_linear_backward_call_workspace_bytes(int64_t M, int64_t K, int64_t N, int act, int y_type, int w_layout, int dX, int dW, int dbias) {
+    return M < 1 || K < 1 || N < 1 ? 0 : room_of(M, K, N, act, y_type, w_layout, dX, dW, dbias).all();
+}
 
 extern "C" atb_status_t atb_linear_backward(int64_t M, int64_t K, int64_t N, int act, int y_type, const void* dY_dev, int64_t lddy, const void* X_dev,
                                             int64_t ldx, int w_layout, const void* W_dev, int64_t ldw, int z_type, const void* Z_dev, void* dX_dev,
@@ -221,14 +234,15 @@ extern "C" atb_status_t atb_linear_backward(int64_t M, int64_t K, int64_t N, int
     if (s != ATB_OK) return s;
     const bool kn = w_layout == ATB_W_KN;
     const int64_t w_rows = kn ? K : N, w_cols = kn ? N : K;
-    if (M > 0 && (!dY_dev || (!Z_dev && act != ATB_ACT_NONE) || (!X_dev && dW_dev) || (!W_dev && dX_dev) || !workspace_dev))
-        return atb::fail(ATB_ERR_NULL_POINTER, "dY, Z (with an activation), X (for dW), W (for dX) and the workspace must be non-NULL");
+    const Room room = M > 0 ? room_of(M, K, N, act, y_type, w_layout, dX_dev, dW_dev, dbias_dev) : Room{};
+    const size_t need = room.all();
+    if (M > 0 && (!dY_dev || (!Z_dev && act != ATB_ACT_NONE) || (!X_dev && dW_dev) || (!W_dev && dX_dev) || (need > 0 && !workspace_dev)))
+        return atb::fail(ATB_ERR_NULL_POINTER, "dY, Z (with an activation), X (for dW), W (for dX) and a workspace of %zu bytes must be non-NULL", need);
     if ((M > 0 && (!ld_ok(lddy, N, y_type) || (dW_dev && !ld_ok(ldx, K, ATB_BF16)) || (dX_dev && (!ld_ok(ldw, w_cols, ATB_BF16) || !ld_ok(lddx, K, ATB_BF16))))) ||
         (dW_dev && !ld_ok(lddw, w_cols, ATB_BF16)))
         return atb::fail(ATB_ERR_BAD_SHAPE, "lddy must be >= N, ldx and lddx >= K, ldw and lddw >= the columns that W is stored with, multiples of 8 (FP32: of 4)");
     for (const void* p : {dY_dev, X_dev, W_dev, Z_dev, (const void*)dX_dev, (const void*)dW_dev, (const void*)dbias_dev, (const void*)workspace_dev})
         if (!atb::aligned16(p)) return atb::fail(ATB_ERR_MISALIGNED, "all device pointers must be 16-byte aligned");
-    const size_t need = M > 0 ? dz_bytes(M, N) + part_bytes(M, N) + split_bytes(M, K, N, w_layout, dX_dev, dW_dev) : 0;
     if (workspace_bytes < need) return atb::fail(ATB_ERR_BUFFER_TOO_SMALL, "workspace of %zu bytes is smaller than the %zu needed", workspace_bytes, need);
     cudaStream_t st = static_cast<cudaStream_t>(stream);
     int sms = 0;
@@ -240,20 +254,19 @@ extern "C" atb_status_t atb_linear_backward(int64_t M, int64_t K, int64_t N, int
         if (e == cudaSuccess && dbias_dev) e = cudaMemsetAsync(dbias_dev, 0, N * (bias_type == ATB_F32 ? 4 : 2), st);
         return e == cudaSuccess ? ATB_OK : atb::fail(ATB_ERR_CUDA, "cudaMemsetAsync: %s", cudaGetErrorString(e));
     }
-    char* const room = static_cast<char*>(workspace_dev);
-    const bool is_dy = act == ATB_ACT_NONE && y_type == ATB_BF16, any = dX_dev || dW_dev;
+    char* const area = static_cast<char*>(workspace_dev);
     atb::MmOperand dz = {dY_dev, lddy};
-    if ((!is_dy && any) || dbias_dev) {
+    if (room.dz > 0 || dbias_dev) {
         GradParams g = {};
         g.M = M; g.N = N; g.lddy = lddy;
         g.dy = dY_dev; g.z = Z_dev;
         g.act = act;
         const bool y32 = y_type == ATB_F32, z32 = z_type == ATB_F32;
-        if (!is_dy && any) {
-            g.dz = reinterpret_cast<__nv_bfloat16*>(room);
-            dz = {room, N};
+        if (room.dz > 0) {
+            g.dz = reinterpret_cast<__nv_bfloat16*>(area);
+            dz = {area, N};
         }
-        if (dbias_dev) g.part = reinterpret_cast<float*>(room + dz_bytes(M, N));
+        if (dbias_dev) g.part = reinterpret_cast<float*>(area + room.dz);
         const int parts = row_blocks(M, N);
         cudaLaunchConfig_t cfg = {};
         cfg.gridDim = dim3(static_cast<unsigned>(atb::ceil_div(N, kGradCols)), static_cast<unsigned>(parts), 1);
@@ -287,5 +300,5 @@ extern "C" atb_status_t atb_linear_backward(int64_t M, int64_t K, int64_t N, int
         dw.A[0] = kn ? x : dz; dw.B[0] = kn ? dz : x;
         dw.C[0] = dW_dev; dw.ldc[0] = lddw;
     }
-    return atb::mm_launch(q, n, room + dz_bytes(M, N) + part_bytes(M, N), st);
+    return atb::mm_launch(q, n, area + room.dz + room.part, st);
 }

@@ -27,7 +27,7 @@ namespace {
     X(atb_gated_ffn) X(atb_gated_ffn_workspace_bytes) X(atb_gated_ffn_backward) X(atb_gated_ffn_backward_workspace_bytes) \
     X(atb_linear_cross_entropy) X(atb_linear_cross_entropy_workspace_bytes) X(atb_linear_cross_entropy_backward)        \
     X(atb_linear_cross_entropy_backward_workspace_bytes) X(atb_bfp16_exp_bytes)                                         \
-    X(atb_linear) X(atb_linear_workspace_bytes) X(atb_linear_backward) X(atb_linear_backward_workspace_bytes)     \
+    X(atb_linear) X(atb_linear_workspace_bytes) X(atb_linear_backward) X(atb_linear_backward_call_workspace_bytes) \
     X(atb_residual_norm) X(atb_residual_norm_backward) X(atb_residual_norm_backward_workspace_bytes) X(atb_sample)
 struct Entries {
 #define ATB_ENTRY(name) decltype(&::name) name = nullptr;
@@ -452,8 +452,9 @@ PyObject* linear_backward(PyObject*, PyObject* const* a, Py_ssize_t n) {
     }
     const at::ScalarType b_type = db.t.defined() ? row_type(db.t, "dbias") : at::kFloat;
     c.out_vector(db, N, b_type, "dbias");
-    const size_t bytes = c.workspace(ws, g_entry.atb_linear_backward_workspace_bytes(M, K, N));
-    return c.done(g_entry.atb_linear_backward(M, K, N, act, type_code(y_type, "dY"), ptr(dY), lddy, ptr(X), ldx, w_layout, ptr(W), ldw, z_code, ptr(Z), ptr(dX.t), lddx,
+    const int y_code = type_code(y_type, "dY");
+    const size_t bytes = c.workspace(ws, g_entry.atb_linear_backward_call_workspace_bytes(M, K, N, act, y_code, w_layout, dX.t.defined(), dW.t.defined(), db.t.defined()));
+    return c.done(g_entry.atb_linear_backward(M, K, N, act, y_code, ptr(dY), lddy, ptr(X), ldx, w_layout, ptr(W), ldw, z_code, ptr(Z), ptr(dX.t), lddx,
                                               ptr(dW.t), lddw, type_code(b_type, "dbias"), ptr(db.t), ptr(ws), bytes, c.stream), {dX.t, dW.t, db.t});
     END_HANDLE_TH_ERRORS
 }
