@@ -354,7 +354,8 @@ atb_status_t atb_select_tiling(int64_t M, int64_t N, int64_t K, const atb_hw_par
  *   - what is rounded to bf16 on the way: operands that one product makes for the next (H, dG, dU, dL: the tensor
  *     cores take bf16), and, without ATB_KEEP_F32, G and U (half the memory; dX, dWg and dWu are 0.0030 of
  *     their norm off instead of 0.0024, rounding the results alone is 0.0017); exponentials and
- *     reciprocals of the activations and the softmax are the fast instructions (1 to 2 units in the last place of FP32);
+ *     reciprocals of the activations and the softmax are the fast instructions (1 to 2 units in the last place of FP32, and an
+ *     exponential besides its argument's size times 2^-24: act(z) in FP32 is within 6e-7 of itself for z >= -1, 1.3e-5 for z >= -10);
  *   - a workspace is device memory, 16-byte aligned, of at least the bytes that the function beside the
  *     operator returns; it is overwritten and may be reused by the next call on the same stream.
  * ===================================================================================================== */

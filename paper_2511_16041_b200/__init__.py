@@ -559,7 +559,8 @@ def atb_linear_backward_call_workspace_bytes(M: int, K: int, N: int, act, y_type
 
 def atb_linear_backward(dY, X, W, Z=None, act=None, dX=None, dW=None, dbias=None, workspace=None, stream=None):
     """Gradients ``(dX, dW, dbias)`` of ``atb_linear`` from ``dY`` and the ``Z`` that it saved (None without an activation); the
-    residual's is dY.  dW in W's layout, dbias in float32 or the type of the tensor given.  False: not wanted."""
+    residual's is dY.  dW in W's layout, dbias in float32 or the type of the tensor given.  False: not wanted; a layer without a bias
+    says so for dbias, which costs a pass over dY otherwise."""
     return _result((_ops or load_ops()).linear_backward(dY, X, W, Z, _linear_act(act), dX, dW, dbias, workspace, _raw(stream)))
 
 
@@ -590,7 +591,7 @@ def atb_residual_norm_backward(dZ, dH, X, F, stats, W=None, gate=None, scale=1.0
                                dgate=None, dW=None, dB=None, dpost_W=None, dpost_B=None, workspace=None, stream=None):
     """Gradients ``(dX, dF, dgate, dW, dB, dpost_W, dpost_B)`` of ``atb_residual_norm`` from ``dZ`` and ``dH`` (None: nothing but the norm reads
     H).  The vectors' are of the vectors' type (float32 where there are none); dgate is None without a gate, dpost_W and dpost_B without
-    ``post_norm``.  False: not wanted.  Without a gate, a post norm and a scale dF is dX: False saves writing it twice."""
+    ``post_norm``.  False: not wanted (the call has not seen whether the norm has a B).  Without a gate, a post norm and a scale dF is dX: False saves writing it twice."""
     return _result((_ops or load_ops()).residual_norm_backward(dZ, dH, X, F, stats, W, gate, scale, post_norm, post_W, post_B, _norm_kind(kind), dX, dF, dgate, dW, dB,
                                                                dpost_W, dpost_B, workspace, _raw(stream)))
 

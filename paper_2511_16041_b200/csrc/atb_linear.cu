@@ -9,8 +9,8 @@
 // is rounded, the sums of the blocks' rows, and one launch of the two products.  Where dz is dy (no activation, bf16) the pass
 // only sums, and is left out where the bias has no gradient.
 // The forward pass is bound by the product (8192 x 4096 x 10944 with z in FP32 504 us, 1.46 PFLOP/s) or, where rows are few, by W (16 rows,
-// 2048 x 32000 stored [N][K]: 27 us, 4.9 TB/s); a prompt of one wave of tiles by its launch, fill and drain (509 x 2048 x 5464: 22 us, of which
-// 18.5 are the product alone).  The gradient's pass is bound by memory: 8192 x 10944, z in FP32, 118 us (6.1 TB/s).  The two
+// 2048 x 32000 stored [N][K]: 26.6 to 28.8 us, 4.6 to 5.0 TB/s; 250 tiles on 148 SMs, which take one or two); a prompt by launch, fill, one K loop
+// and drain, 44 tiles on 74 pairs of SMs (509 x 2048 x 5464: 22 us, of which 18.5 are the product alone).  The gradient's pass is bound by memory: 8192 x 10944, z in FP32, 118 us (6.1 TB/s).  The two
 // products after it run at 1.54 PFLOP/s alone (955 us) and slower under the power cap behind a forward pass.
 #include <algorithm>
 

@@ -35,8 +35,7 @@ struct BwdParams {
     int blocks;                            // that walk the rows
 };
 
-// Elements n .. n + VEC - 1 of a vector of weights, or `none` where there is no vector.  They are read again for every row, from the L1:
-// five of them would take more registers than a row does.
+// Elements n .. n + VEC - 1 of a vector of weights, or `none` where there is no vector.  (Where they are kept between rows: Vector, below.)
 template <class TW, int VEC>
 __device__ __forceinline__ void weights(const void* p, int n, float none, float (&v)[VEC]) {
 #pragma unroll

@@ -16,7 +16,9 @@
 //     the few bins that the border may be in are looked at word by word
 // A cluster of CTAs takes a row, 32 logits a thread in shared memory: the row is read from memory once, and histograms and sums are
 // joined through distributed shared memory.  Rows of more than kMostCtas * 16384 words are read again in every pass.
-// Bound by instructions and by the waits of a cluster's CTAs for one another: top-p takes about 100 instructions a word (one exact weight
+// Bound by instructions and by the waits of a cluster's CTAs for one another.  A row's load, maximum, waits and exit follow one another, with the other
+// row on the SM to cover them: 512 rows of 131072 words are 14 rounds of 37 clusters, and the greedy draw, which needs the maximum and
+// its place, takes 218 us.  top-p takes about 100 instructions a word (one exact weight
 // is 21, the bounds' approximate weight and count 20) and seven waits; two CTAs of different rows share an SM, so that one works
 // while the other waits.  131072 words, FP32: one row, k = 50, 12 us, plain temperature 13 us, top-p 30 us; 512 rows 262, 282 and 560 us (the
 // logits are 41 us of memory traffic).  Logits in registers, 16 of 1024 threads and loops unrolled over them, took 250 instructions

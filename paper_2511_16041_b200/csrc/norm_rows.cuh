@@ -123,9 +123,9 @@ __device__ __forceinline__ void store_f(T* p, const float (&v)[VEC]) {
 }
 
 // ---------------------------------------------------------------------------------- pairs
-// The backward kernel works on its elements in pairs by the two-wide FP32 instructions, which round each half like the scalar
-// ones: 3 to 10 % faster than scalar arithmetic.  (The forward kernel, with half the arithmetic per byte, was 5 to 15 %
-// slower in this form.)
+// The layer norm's backward kernel and both of the residual norm's work on their elements in pairs by the two-wide FP32 instructions, which
+// round each half like the scalar ones: 3 to 10 % faster than scalar arithmetic in the former.  (The layer norm's forward kernel,
+// with half the arithmetic per byte, was 5 to 15 % slower in this form, and is scalar.)
 using namespace f32x2;
 
 // A thread's elements as pairs: NV groups of VEC, pairs of neighbours (VEC = 8) or of one element each of two groups (VEC = 1).
